@@ -489,6 +489,102 @@ int bhtsne_debug_tree_3d(const float *Y, int64_t n, float theta, int64_t *n_node
 int bhtsne_debug_walk(const float *Y, int64_t n, int dim, float theta, int form, float *frep, double *Z,
                       uint64_t *interactions, void *workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Operators of a trained map.  Instead of a free embedding, a run may learn a
+ * map from features to places (an encoder of dense layers, each followed by a
+ * layer norm), so that new points can be placed too: the gradient dC/dY of
+ * bhtsne_gradient at the places goes back through the layer norms to the
+ * weight matrices, and each matrix takes a step along its orthogonalised
+ * momentum.
+ *
+ * Matrices are device arrays, row-major with unit stride inside a row and
+ * `*_stride` elements between rows.  Their elements are of type `type` (one of
+ * BHTSNE_F32, BHTSNE_F16, BHTSNE_BF16), aligned to their own size.  Sums and
+ * statistics are fp32 or fp64; outputs are rounded once.  The calls return
+ * before the work completes, never synchronise, allocate nothing and can be
+ * captured in a HIP graph.  NaN and infinities in the data propagate as in the
+ * formulas; they are not reported. */
+enum {
+    BHTSNE_F32 = 0,
+    BHTSNE_F16 = 1,
+    BHTSNE_BF16 = 2
+};
+
+/* Layer norm of n rows (points) of d features:
+ *     y = (x - mean) rstd weight + bias,  mean = 1/d sum x,
+ *     rstd = (1/d sum (x - mean)^2 + eps)^(-1/2)
+ *   x, y    n x d of `type`; y may be x (with x's stride).  x_stride >= d, or 0
+ *           for one row that stands for all; y_stride >= d.
+ *   weight, bias  d values of `param_type`, each nullable (1 and 0).
+ *   mean, rstd    n fp32 values, each nullable: what the backward pass takes.
+ * 0 <= n < 2^31, 1 <= d <= 2^24, strides < 2^31, eps finite and >= 0.
+ * Errors: BHTSNE_EINVAL, BHTSNE_EDEVICE. */
+int bhtsne_layer_norm(const void *x, int64_t x_stride, const void *weight, const void *bias, int64_t n, int64_t d,
+                      double eps, int type, int param_type, void *y, int64_t y_stride, float *mean, float *rstd,
+                      hipStream_t stream);
+
+/* The backward pass, with the reduction of the weights' gradients over all
+ * rows: with g = dy weight and xh = (x - mean) rstd,
+ *     dx = rstd (g - 1/d sum g - xh 1/d sum g xh),
+ *     dweight = sum over rows of dy xh,  dbias = sum over rows of dy
+ *   dy, x   n x d of `type`; a stride of 0 as above.
+ *   weight  as in the forward pass (nullable); mean, rstd: its outputs.
+ *   dx      n x d of `type`, nullable; may be dy or x (with their stride).
+ *   dweight, dbias  d values of `param_type`, each nullable, overwritten (zero
+ *           for n = 0); their sums are joined in a fixed order, so the same
+ *           inputs give the same bits.
+ * One output at least is wanted.  The workspace
+ * (bhtsne_layer_norm_workspace_size bytes, 256-byte aligned; 0 for sizes out of
+ * range) is needed for dweight and dbias alone.
+ * Errors: BHTSNE_EINVAL, BHTSNE_EWORKSPACE, BHTSNE_EDEVICE. */
+size_t bhtsne_layer_norm_workspace_size(int64_t n, int64_t d);
+int bhtsne_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,
+                               const void *weight, const float *mean, const float *rstd, int64_t n, int64_t d,
+                               int type, int param_type, void *dx, int64_t dx_stride, void *dweight, void *dbias,
+                               void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* `batch` matrices of one shape and layout: matrix k starts k batch_stride
+ * elements behind `data`. */
+typedef struct bhtsne_matrices {
+    void *data;           /* device */
+    int64_t stride;       /* elements between rows, >= cols */
+    int64_t batch_stride; /* elements between matrices */
+} bhtsne_matrices;
+
+/* Orthogonalisation by Newton-Schulz products: X = G / (|G|_F + eps), then
+ * `steps` times, with A = X X^T on the shorter side (X^T X for tall G),
+ *     X <- a X + (b A + c A^2) X;     O = X.
+ *   G, O    `batch` matrices of rows x cols of `type`; O may be G.
+ *   coefficients  host, steps x 3 doubles (a, b, c of each step), nullable: the
+ *           quintic (3.4445, -4.7750, 2.0315) for every step.  A singular value
+ *           of X in [0, 1] must stay below 64 under them (BHTSNE_EINVAL).
+ *   1 <= steps <= 32; eps finite and >= 0 (a zero matrix stays zero for eps > 0).
+ * The products run on the matrix cores with fp16 operands, fp32 sums: for bf16
+ * with both sides above 64 at 11 bits an operand (a X at 22), else at 22 bits.
+ * 0 <= batch <= 65535, 1 <= rows, cols <= 65536.  O's matrices must not overlap.
+ * The workspace is bhtsne_orthogonalise_workspace_size bytes (256-byte
+ * aligned; 0 for sizes out of range).
+ * Errors: BHTSNE_EINVAL, BHTSNE_EWORKSPACE, BHTSNE_EDEVICE. */
+size_t bhtsne_orthogonalise_workspace_size(int64_t batch, int64_t rows, int64_t cols);
+int bhtsne_orthogonalise(const bhtsne_matrices *G, int64_t batch, int64_t rows, int64_t cols, int type,
+                         const double *coefficients, int steps, double eps, const bhtsne_matrices *O,
+                         void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* One momentum step of weight matrices along the orthogonalised update:
+ *     M <- momentum M + G;   U = G + momentum M (nesterov) or M;
+ *     W <- (1 - learning_rate weight_decay) W - learning_rate scale O(U)
+ * with O as above.
+ *   W, G    `batch` matrices of rows x cols of `type`; W is updated in place.
+ *   M       the momentum, fp32, updated in place (zero before the first step).
+ *   learning_rate finite > 0; momentum in [0, 1); weight_decay finite >= 0;
+ *   scale finite (the usual choice is sqrt(max(1, rows / cols))).
+ * No two of W, G and M overlap.  Other arguments, workspace and errors as
+ * bhtsne_orthogonalise. */
+int bhtsne_muon_step(const bhtsne_matrices *W, const bhtsne_matrices *G, const bhtsne_matrices *M, int64_t batch,
+                     int64_t rows, int64_t cols, int type, double learning_rate, double momentum, int nesterov,
+                     double weight_decay, double scale, const double *coefficients, int steps, double eps,
+                     void *workspace, size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

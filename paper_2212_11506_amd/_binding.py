@@ -120,6 +120,15 @@ def load_library():
         "bhtsne_debug_sort": (C.c_int, [vp, i64, vp, vp, vp, f64p, vp, C.c_size_t, vp]),
         "bhtsne_debug_tree": (C.c_int, [vp, i64, f32, C.POINTER(C.c_int64), vp, vp, vp, vp, vp, vp, vp,
                                         C.c_size_t, vp]),
+        "bhtsne_layer_norm": (C.c_int, [vp, i64, vp, vp, i64, i64, C.c_double, C.c_int, C.c_int, vp, i64, vp, vp, vp]),
+        "bhtsne_layer_norm_workspace_size": (C.c_size_t, [i64, i64]),
+        "bhtsne_layer_norm_backward": (C.c_int, [vp, i64, vp, i64, vp, vp, vp, i64, i64, C.c_int, C.c_int, vp, i64,
+                                                 vp, vp, vp, C.c_size_t, vp]),
+        "bhtsne_orthogonalise_workspace_size": (C.c_size_t, [i64, i64, i64]),
+        "bhtsne_orthogonalise": (C.c_int, [vp, i64, i64, i64, C.c_int, f64p, C.c_int, C.c_double, vp, vp, C.c_size_t,
+                                           vp]),
+        "bhtsne_muon_step": (C.c_int, [vp, vp, vp, i64, i64, i64, C.c_int, C.c_double, C.c_double, C.c_int,
+                                       C.c_double, C.c_double, f64p, C.c_int, C.c_double, vp, C.c_size_t, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -654,3 +663,172 @@ def debug_walk(Y: torch.Tensor, theta: float = 0.5, form: int = -1):
                                C.byref(inter), _ptr(ws), ws.numel(), _stream())
     _check(rc, "bhtsne_debug_walk")
     return frep, Z.value, inter.value
+
+
+# ------------------------------------------------------------------ operators of a trained map
+class _Matrices(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("batch_stride", C.c_int64)]
+
+
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}  # BHTSNE_F32, BHTSNE_F16, BHTSNE_BF16
+
+
+def _type(t: torch.Tensor, where: str) -> int:
+    if t.dtype not in _TYPES:
+        raise ValueError(f"{where} must be float32, float16 or bfloat16, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _rows(t: torch.Tensor, where: str, n: int, d: int, dtype) -> int:
+    """Checks an n x d matrix with unit stride inside a row; the stride between its rows."""
+    if not t.is_cuda:
+        raise ValueError(f"{where} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{where} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != (n, d):
+        raise ValueError(f"{where} must be {n} x {d}, got {tuple(t.shape)}")
+    if d > 1 and t.stride(1) != 1:
+        raise ValueError(f"{where} must be contiguous inside a row")
+    return t.stride(0) if n > 1 else d
+
+
+def _vector(t: Optional[torch.Tensor], where: str, size: int, dtype=None):
+    if t is not None and t.numel() != size:
+        raise ValueError(f"{where} must have {size} values, got {t.numel()}")
+    return _ptr(t, dtype, where)
+
+
+def _param_type(weight, bias, dtype) -> int:
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise ValueError(f"weight and bias must have one type, got {weight.dtype} and {bias.dtype}")
+    p = weight if weight is not None else bias
+    return _type(p, "weight") if p is not None else _TYPES[dtype]
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+               eps: float = 1e-5, out: Optional[torch.Tensor] = None):
+    """bhtsne_layer_norm over the rows of x (n x d, rows any distance apart): (y, mean, rstd); out may be x."""
+    lib = load_library()
+    if x.dim() != 2:
+        raise ValueError(f"x must be n x d, got {tuple(x.shape)}")
+    n, d = x.shape
+    y = out if out is not None else torch.empty((n, d), dtype=x.dtype, device=x.device)
+    mean = torch.empty(n, dtype=torch.float32, device=x.device)
+    rstd = torch.empty(n, dtype=torch.float32, device=x.device)
+    rc = lib.bhtsne_layer_norm(C.c_void_p(x.data_ptr()), _rows(x, "x", n, d, x.dtype), _vector(weight, "weight", d),
+                               _vector(bias, "bias", d), n, d, float(eps), _type(x, "x"),
+                               _param_type(weight, bias, x.dtype), C.c_void_p(y.data_ptr()),
+                               _rows(y, "out", n, d, x.dtype), C.c_void_p(mean.data_ptr()),
+                               C.c_void_p(rstd.data_ptr()), _stream())
+    _check(rc, "bhtsne_layer_norm")
+    return y, mean, rstd
+
+
+def layer_norm_workspace_size(n: int, d: int) -> int:
+    return int(load_library().bhtsne_layer_norm_workspace_size(int(n), int(d)))
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor,
+                        rstd: torch.Tensor, dx: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None):
+    """bhtsne_layer_norm_backward: (dx, dweight, dbias), the last two of weight's type (x's without a weight);
+    dx may be dy or x."""
+    lib = load_library()
+    if x.dim() != 2:
+        raise ValueError(f"x must be n x d, got {tuple(x.shape)}")
+    n, d = x.shape
+    need = layer_norm_workspace_size(n, d)
+    if need == 0:
+        raise BhtsneError(BHTSNE_EINVAL, "bhtsne_layer_norm_workspace_size")
+    if dx is None:
+        dx = torch.empty((n, d), dtype=x.dtype, device=x.device)
+    ws = workspace if workspace is not None else torch.empty(need, dtype=torch.uint8, device=x.device)
+    ptype = weight.dtype if weight is not None else x.dtype
+    dweight = torch.empty(d, dtype=ptype, device=x.device)
+    dbias = torch.empty(d, dtype=ptype, device=x.device)
+    rc = lib.bhtsne_layer_norm_backward(C.c_void_p(dy.data_ptr()), _rows(dy, "dy", n, d, x.dtype),
+                                        C.c_void_p(x.data_ptr()), _rows(x, "x", n, d, x.dtype),
+                                        _vector(weight, "weight", d), _vector(mean, "mean", n, torch.float32),
+                                        _vector(rstd, "rstd", n, torch.float32), n, d, _type(x, "x"),
+                                        _param_type(weight, None, x.dtype), C.c_void_p(dx.data_ptr()),
+                                        _rows(dx, "dx", n, d, x.dtype), C.c_void_p(dweight.data_ptr()),
+                                        C.c_void_p(dbias.data_ptr()), _ptr(ws, None, "workspace"),
+                                        ws.numel() * ws.element_size(), _stream())
+    _check(rc, "bhtsne_layer_norm_backward")
+    return dx, dweight, dbias
+
+
+def _matrices(t: torch.Tensor, where: str, shape, dtype) -> _Matrices:
+    if not t.is_cuda:
+        raise ValueError(f"{where} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{where} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{where} must be {tuple(shape)}, got {tuple(t.shape)}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{where} must be contiguous inside a row")
+    return _Matrices(t.data_ptr(), t.stride(-2) if t.shape[-2] > 1 else t.shape[-1], t.stride(0) if t.dim() == 3 else 0)
+
+
+def _matrix_sizes(t: torch.Tensor, where: str):
+    if t.dim() not in (2, 3):
+        raise ValueError(f"{where} must be rows x cols or batch x rows x cols, got {tuple(t.shape)}")
+    return (t.shape[0] if t.dim() == 3 else 1), t.shape[-2], t.shape[-1]
+
+
+def _coefficients(coefficients, steps: int):
+    """None, one (a, b, c) for every step, or one for each."""
+    if coefficients is None:
+        return None
+    flat = [float(v) for row in coefficients for v in (row if hasattr(row, "__len__") else (row,))]
+    if len(flat) == 3:
+        flat = flat * steps
+    if len(flat) != 3 * steps:
+        raise ValueError(f"coefficients must be one (a, b, c) or {steps} of them")
+    return (C.c_double * len(flat))(*flat)
+
+
+def orthogonalise_workspace_size(batch: int, rows: int, cols: int) -> int:
+    return int(load_library().bhtsne_orthogonalise_workspace_size(int(batch), int(rows), int(cols)))
+
+
+def _orthogonal_workspace(sizes, device, ws):
+    need = orthogonalise_workspace_size(*sizes)
+    if need == 0:
+        raise BhtsneError(BHTSNE_EINVAL, "bhtsne_orthogonalise_workspace_size")
+    return ws if ws is not None else torch.empty(need, dtype=torch.uint8, device=device)
+
+
+def orthogonalise(G: torch.Tensor, steps: int = 5, coefficients=None, eps: float = 1e-7,
+                  out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """bhtsne_orthogonalise of G (rows x cols, or batch x rows x cols); out may be G."""
+    lib = load_library()
+    sizes = _matrix_sizes(G, "G")
+    kind = _type(G, "G")
+    O = out if out is not None else torch.empty(G.shape, dtype=G.dtype, device=G.device)
+    g, o = _matrices(G, "G", G.shape, G.dtype), _matrices(O, "out", G.shape, G.dtype)
+    ws = _orthogonal_workspace(sizes, G.device, workspace)
+    rc = lib.bhtsne_orthogonalise(C.byref(g), *sizes, kind, _coefficients(coefficients, steps), int(steps), float(eps),
+                                  C.byref(o), _ptr(ws, None, "workspace"), ws.numel() * ws.element_size(), _stream())
+    _check(rc, "bhtsne_orthogonalise")
+    return O
+
+
+def muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, learning_rate: float, momentum: float = 0.95,
+              nesterov: bool = True, weight_decay: float = 0.0, scale: Optional[float] = None, steps: int = 5,
+              coefficients=None, eps: float = 1e-7, workspace: Optional[torch.Tensor] = None) -> None:
+    """bhtsne_muon_step: one step in place on the weights W and the fp32 momentum M (rows x cols, or batch x rows x
+    cols).  scale: None is sqrt(max(1, rows / cols))."""
+    lib = load_library()
+    sizes = _matrix_sizes(W, "W")
+    kind = _type(W, "W")
+    w, g = _matrices(W, "W", W.shape, W.dtype), _matrices(G, "G", W.shape, W.dtype)
+    m = _matrices(M, "M", W.shape, torch.float32)
+    if scale is None:
+        scale = max(1.0, sizes[1] / max(1, sizes[2])) ** 0.5
+    ws = _orthogonal_workspace(sizes, W.device, workspace)
+    rc = lib.bhtsne_muon_step(C.byref(w), C.byref(g), C.byref(m), *sizes, kind, float(learning_rate), float(momentum),
+                              int(bool(nesterov)), float(weight_decay), float(scale),
+                              _coefficients(coefficients, steps), int(steps), float(eps),
+                              _ptr(ws, None, "workspace"), ws.numel() * ws.element_size(), _stream())
+    _check(rc, "bhtsne_muon_step")

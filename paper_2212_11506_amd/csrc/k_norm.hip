@@ -1,0 +1,534 @@
+// Layer norm over the rows (points) of an n x d matrix, forward and backward.
+//
+//   y = (x - mean) rstd w + b,   rstd = (1/d sum (x - mean)^2 + eps)^(-1/2)
+//   g = dy w, xh = (x - mean) rstd:
+//   dx = rstd (g - 1/d sum g - xh 1/d sum g xh),  dw = sum_n dy xh,  db = sum_n dy
+//
+// Both passes move each element once (two or three of them) for about ten
+// operations: HBM bounds them.  A row is held in the registers of a team of
+// 2^k lanes of a wave (up to 1024 features at 16 a lane), or of a whole block
+// (up to 16384), so that the mean, the centred sum of squares and the outputs
+// come from one read; the next row's loads are in flight while a row is
+// computed.  All sums are fp32 (the weight gradients' last join fp64); the only
+// rounding to fewer bits is that of the outputs.
+#include <type_traits>
+
+#include "map.hpp"
+
+namespace bht {
+namespace {
+
+template <typename E, int VEC> struct alignas(sizeof(E) * VEC) Pack {
+    E v[VEC];
+};
+
+template <typename E, int VEC> __device__ inline Pack<E, VEC> load_pack(const E *p)
+{
+    return *reinterpret_cast<const Pack<E, VEC> *>(p);
+}
+template <typename E, int VEC> __device__ inline void store_pack(E *p, const Pack<E, VEC> &v)
+{
+    *reinterpret_cast<Pack<E, VEC> *>(p) = v;
+}
+
+__device__ inline float load_param(const void *p, Elem t, int64_t i)
+{
+    if (t == Elem::kF32) return static_cast<const float *>(p)[i];
+    if (t == Elem::kF16) return float(static_cast<const f16 *>(p)[i]);
+    return float(static_cast<const bf16 *>(p)[i]);
+}
+__device__ inline void store_param(void *p, Elem t, int64_t i, float v)
+{
+    if (t == Elem::kF32)
+        static_cast<float *>(p)[i] = v;
+    else if (t == Elem::kF16)
+        static_cast<f16 *>(p)[i] = f16(v);
+    else
+        static_cast<bf16 *>(p)[i] = bf16(v);
+}
+
+// v of the lane at the other end of a fixed permutation within 16 lanes
+template <int kCtrl> __device__ inline float dpp(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kCtrl, 0xF, 0xF, true));
+}
+
+// Sum over aligned teams of `team` lanes (a power of two up to 64), in every
+// lane.  Once all lanes of an aligned half hold that half's sum, any lane of
+// the other half will do: mirrors serve for the exchanges over 4 and 8 lanes.
+__device__ inline float team_sum(float v, int team)
+{
+    if (team > 1) v += dpp<0xB1>(v);  // quad_perm 1,0,3,2
+    if (team > 2) v += dpp<0x4E>(v);  // quad_perm 2,3,0,1
+    if (team > 4) v += dpp<0x141>(v); // row_half_mirror
+    if (team > 8) v += dpp<0x140>(v); // row_mirror
+    if (team > 16) v += __shfl_xor(v, 16, kWave);
+    if (team > 32) v += __shfl_xor(v, 32, kWave);
+    return v;
+}
+
+// Sum over the team of a row: lanes of a wave (team <= 64), or the whole block.
+// `red`: kNormMaxThreads / 64 floats of LDS for this sum alone.
+__device__ inline float row_sum(float v, int team, float *red)
+{
+    v = team_sum(v, team < kWave ? team : kWave);
+    if (team <= kWave) return v;
+    if (lane_id() == 0) red[threadIdx.x / kWave] = v;
+    __syncthreads();
+    float s = 0.0f;
+    for (int w = 0; w < team / kWave; ++w) s += red[w];
+    return s;
+}
+
+// ------------------------------------------------------------------ forward
+template <typename E, int VEC, int NV>
+__global__ __launch_bounds__(kNormMaxThreads) void norm_kernel(NormArgs a, int team)
+{
+    __shared__ float s_red[2][kNormMaxThreads / kWave];
+    const int sub = threadIdx.x & (team - 1);      // lane in the team (team is a power of two up to 64) ...
+    const int lane = team <= kWave ? sub : threadIdx.x; // ... or in the block
+    const int rows = team <= kWave ? int(blockDim.x) / team : 1;
+    const int mine = team <= kWave ? int(threadIdx.x) / team : 0;
+    const E *x = static_cast<const E *>(a.x);
+    E *y = static_cast<E *>(a.out);
+    const int d = int(a.d);
+    const float count = float(d);
+
+    int col[NV];
+    float w[NV * VEC], b[NV * VEC];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        col[k] = (k * team + lane) * VEC;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const int c = col[k] + j;
+            w[k * VEC + j] = c < d && a.weight ? load_param(a.weight, a.param, c) : 1.0f;
+            b[k * VEC + j] = c < d && a.bias ? load_param(a.bias, a.param, c) : 0.0f;
+        }
+    }
+    const int64_t step = int64_t(gridDim.x) * rows;
+    int64_t row = int64_t(blockIdx.x) * rows + mine;
+    Pack<E, VEC> next[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+        if (row < a.n && col[k] < d) next[k] = load_pack<E, VEC>(x + row * a.x_stride + col[k]);
+
+    // every lane of a block makes the same number of rounds
+    for (int64_t first = int64_t(blockIdx.x) * rows; first < a.n; first += step, row += step) {
+        float v[NV * VEC];
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                v[k * VEC + j] = row < a.n && col[k] < d ? float(next[k].v[j]) : 0.0f;
+                sum += v[k * VEC + j];
+            }
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (row + step < a.n && col[k] < d) next[k] = load_pack<E, VEC>(x + (row + step) * a.x_stride + col[k]);
+        const float mean = row_sum(sum, team, s_red[0]) / count;
+        float sq = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                v[k * VEC + j] -= mean;
+                if (col[k] < d) sq += v[k * VEC + j] * v[k * VEC + j];
+            }
+        const float rstd = 1.0f / sqrtf(row_sum(sq, team, s_red[1]) / count + float(a.eps));
+        if (row >= a.n) continue;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (col[k] >= d) continue;
+            Pack<E, VEC> o;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) o.v[j] = E(v[k * VEC + j] * rstd * w[k * VEC + j] + b[k * VEC + j]);
+            store_pack<E, VEC>(y + row * a.out_stride + col[k], o);
+        }
+        if (lane == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+    }
+}
+
+// rows longer than a block's registers: one block a row, three passes over it
+template <typename E, int VEC>
+__global__ __launch_bounds__(kNormMaxThreads) void norm_long_kernel(NormArgs a)
+{
+    __shared__ float s_red[2][kNormMaxThreads / kWave];
+    const int team = blockDim.x;
+    const float count = float(a.d);
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        const E *x = static_cast<const E *>(a.x) + row * a.x_stride;
+        E *y = static_cast<E *>(a.out) + row * a.out_stride;
+        float sum = 0.0f;
+        for (int64_t c = int64_t(threadIdx.x) * VEC; c < a.d; c += int64_t(team) * VEC) {
+            const Pack<E, VEC> p = load_pack<E, VEC>(x + c);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) sum += float(p.v[j]);
+        }
+        const float mean = row_sum(sum, team, s_red[0]) / count;
+        float sq = 0.0f;
+        for (int64_t c = int64_t(threadIdx.x) * VEC; c < a.d; c += int64_t(team) * VEC) {
+            const Pack<E, VEC> p = load_pack<E, VEC>(x + c);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) sq += (float(p.v[j]) - mean) * (float(p.v[j]) - mean);
+        }
+        const float rstd = 1.0f / sqrtf(row_sum(sq, team, s_red[1]) / count + float(a.eps));
+        for (int64_t c = int64_t(threadIdx.x) * VEC; c < a.d; c += int64_t(team) * VEC) {
+            const Pack<E, VEC> p = load_pack<E, VEC>(x + c);
+            Pack<E, VEC> o;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float w = a.weight ? load_param(a.weight, a.param, c + j) : 1.0f;
+                const float b = a.bias ? load_param(a.bias, a.param, c + j) : 0.0f;
+                o.v[j] = E((float(p.v[j]) - mean) * rstd * w + b);
+            }
+            store_pack<E, VEC>(y + c, o);
+        }
+        if (threadIdx.x == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+    }
+}
+
+// ------------------------------------------------------------------ backward
+// Each team keeps the sums of its rows' dy xh and dy in registers; a block's
+// teams are joined in LDS, in order, into one partial row [2][d] of the block.
+template <typename E, int VEC, int NV>
+__global__ __launch_bounds__(kNormMaxThreads) void norm_back_kernel(NormArgs a, int team)
+{
+    __shared__ float s_red[2][kNormMaxThreads / kWave];
+    extern __shared__ float s_part[]; // [rows][team * NV * VEC], where a wave holds several teams or a block several waves
+    const int sub = threadIdx.x & (team - 1);
+    const int lane = team <= kWave ? sub : threadIdx.x;
+    const int rows = team <= kWave ? int(blockDim.x) / team : 1;
+    const int mine = team <= kWave ? int(threadIdx.x) / team : 0;
+    const E *x = static_cast<const E *>(a.x), *dy = static_cast<const E *>(a.dy);
+    E *dx = static_cast<E *>(a.out);
+    const int d = int(a.d);
+    const float count = float(d);
+
+    int col[NV];
+    float w[NV * VEC], dw[NV * VEC], db[NV * VEC];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        col[k] = (k * team + lane) * VEC;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const int c = col[k] + j;
+            w[k * VEC + j] = c < d && a.weight ? load_param(a.weight, a.param, c) : 1.0f;
+            dw[k * VEC + j] = db[k * VEC + j] = 0.0f;
+        }
+    }
+    const int64_t step = int64_t(gridDim.x) * rows;
+    int64_t row = int64_t(blockIdx.x) * rows + mine;
+    Pack<E, VEC> nx[NV], ndy[NV];
+    float nmean = 0.0f, nrstd = 0.0f;
+    if (row < a.n) {
+        nmean = a.mean[row];
+        nrstd = a.rstd[row];
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (col[k] < d) {
+                nx[k] = load_pack<E, VEC>(x + row * a.x_stride + col[k]);
+                ndy[k] = load_pack<E, VEC>(dy + row * a.dy_stride + col[k]);
+            }
+    }
+    for (int64_t first = int64_t(blockIdx.x) * rows; first < a.n; first += step, row += step) {
+        const float mean = nmean, rstd = nrstd;
+        float xh[NV * VEC], g[NV * VEC];
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (row >= a.n || col[k] >= d) continue;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const int i = k * VEC + j;
+                const float t = float(ndy[k].v[j]);
+                xh[i] = (float(nx[k].v[j]) - mean) * rstd;
+                g[i] = t * w[i];
+                dw[i] += t * xh[i];
+                db[i] += t;
+                s1 += g[i];
+                s2 += g[i] * xh[i];
+            }
+        }
+        if (row + step < a.n) {
+            nmean = a.mean[row + step];
+            nrstd = a.rstd[row + step];
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (col[k] < d) {
+                    nx[k] = load_pack<E, VEC>(x + (row + step) * a.x_stride + col[k]);
+                    ndy[k] = load_pack<E, VEC>(dy + (row + step) * a.dy_stride + col[k]);
+                }
+        }
+        s1 = row_sum(s1, team, s_red[0]) / count;
+        s2 = row_sum(s2, team, s_red[1]) / count;
+        if (row >= a.n || !dx) continue;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (col[k] >= d) continue;
+            Pack<E, VEC> o;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const int i = k * VEC + j;
+                o.v[j] = E(rstd * (g[i] - s1 - xh[i] * s2));
+            }
+            store_pack<E, VEC>(dx + row * a.out_stride + col[k], o);
+        }
+    }
+    if (!a.part) return;
+    const int width = team * NV * VEC;
+    for (int which = 0; which < 2; ++which) {
+        float *part = a.part + (int64_t(blockIdx.x) * 2 + which) * d;
+        if (rows == 1) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j)
+                    if (col[k] + j < d) part[col[k] + j] = which ? db[k * VEC + j] : dw[k * VEC + j];
+            continue;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) s_part[mine * width + col[k] + j] = which ? db[k * VEC + j] : dw[k * VEC + j];
+        __syncthreads();
+        for (int c = threadIdx.x; c < d; c += blockDim.x) {
+            float s = 0.0f;
+            for (int r = 0; r < rows; ++r) s += s_part[r * width + c];
+            part[c] = s;
+        }
+    }
+}
+
+// rows longer than a block's registers: dx, one block a row
+template <typename E, int VEC>
+__global__ __launch_bounds__(kNormMaxThreads) void norm_back_long_kernel(NormArgs a)
+{
+    __shared__ float s_red[2][kNormMaxThreads / kWave];
+    const int team = blockDim.x;
+    const float count = float(a.d);
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        const E *x = static_cast<const E *>(a.x) + row * a.x_stride;
+        const E *dy = static_cast<const E *>(a.dy) + row * a.dy_stride;
+        E *dx = static_cast<E *>(a.out) + row * a.out_stride;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int64_t c = int64_t(threadIdx.x) * VEC; c < a.d; c += int64_t(team) * VEC) {
+            const Pack<E, VEC> p = load_pack<E, VEC>(x + c), q = load_pack<E, VEC>(dy + c);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float w = a.weight ? load_param(a.weight, a.param, c + j) : 1.0f;
+                const float g = float(q.v[j]) * w;
+                s1 += g;
+                s2 += g * ((float(p.v[j]) - mean) * rstd);
+            }
+        }
+        s1 = row_sum(s1, team, s_red[0]) / count;
+        s2 = row_sum(s2, team, s_red[1]) / count;
+        for (int64_t c = int64_t(threadIdx.x) * VEC; c < a.d; c += int64_t(team) * VEC) {
+            const Pack<E, VEC> p = load_pack<E, VEC>(x + c), q = load_pack<E, VEC>(dy + c);
+            Pack<E, VEC> o;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float w = a.weight ? load_param(a.weight, a.param, c + j) : 1.0f;
+                o.v[j] = E(rstd * (float(q.v[j]) * w - s1 - (float(p.v[j]) - mean) * rstd * s2));
+            }
+            store_pack<E, VEC>(dx + c, o);
+        }
+    }
+}
+
+// ... and its weight gradients, before dx is written (dx may be dy): a block
+// owns blockDim columns and the rows of its blockIdx.y, whose partial it writes
+template <typename E> __global__ __launch_bounds__(256) void norm_back_columns_kernel(NormArgs a)
+{
+    const int64_t c = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
+    if (c >= a.d) return;
+    const E *x = static_cast<const E *>(a.x), *dy = static_cast<const E *>(a.dy);
+    float dw = 0.0f, db = 0.0f;
+    for (int64_t row = blockIdx.y; row < a.n; row += gridDim.y) {
+        const float t = float(dy[row * a.dy_stride + c]);
+        dw += t * ((float(x[row * a.x_stride + c]) - a.mean[row]) * a.rstd[row]);
+        db += t;
+    }
+    float *part = a.part + int64_t(blockIdx.y) * 2 * a.d;
+    part[c] = dw;
+    part[a.d + c] = db;
+}
+
+// Joins the blocks' partial rows: 32 columns and 32 strands of partial rows a
+// block; sums in fp64 and in a fixed order, whatever the blocks' timing.
+constexpr int kJoinCols = 32, kJoinStrands = 32;
+__global__ __launch_bounds__(kJoinCols *kJoinStrands) void norm_join_kernel(const float *part, int blocks, int64_t d,
+                                                                          void *dweight, void *dbias, Elem param)
+{
+    __shared__ double s_sum[kJoinStrands][kJoinCols + 1];
+    const int cx = threadIdx.x % kJoinCols, strand = threadIdx.x / kJoinCols;
+    const int64_t c = int64_t(blockIdx.x) * kJoinCols + cx; // column of [dw | db]
+    double s = 0.0;
+    if (c < 2 * d) {
+#pragma unroll 8
+        for (int b = strand; b < blocks; b += kJoinStrands) s += double(part[int64_t(b) * 2 * d + c]);
+    }
+    s_sum[strand][cx] = s;
+    __syncthreads();
+    if (strand != 0 || c >= 2 * d) return;
+    s = 0.0;
+    for (int k = 0; k < kJoinStrands; ++k) s += s_sum[k][cx];
+    if (c < d) {
+        if (dweight) store_param(dweight, param, c, float(s));
+    } else if (dbias)
+        store_param(dbias, param, c - d, float(s));
+}
+
+// ------------------------------------------------------------------ launch shapes
+struct Shape {
+    int vec, nv, team, block, rows;
+    bool in_regs;
+};
+
+// the widest vectors that every row's start and the row length allow, 16 bytes at most
+int vector_of(const NormArgs &a)
+{
+    const int e = elem_bytes(a.type);
+    uintptr_t bits = uintptr_t(a.d) * e | reinterpret_cast<uintptr_t>(a.x) | uintptr_t(a.x_stride) * e | 16u;
+    if (a.out) bits |= reinterpret_cast<uintptr_t>(a.out) | uintptr_t(a.out_stride) * e;
+    if (a.dy) bits |= reinterpret_cast<uintptr_t>(a.dy) | uintptr_t(a.dy_stride) * e;
+    return int((bits & (~bits + 1)) / e);
+}
+
+// A team as small as holds a row at kNormLane features a lane, but of a whole
+// wave before a lane takes more than one vector.
+Shape shape_of(int vec, int64_t d)
+{
+    Shape s;
+    s.vec = vec;
+    const int64_t vecs = (d + vec - 1) / vec;
+    const int most = kNormLane / vec;
+    s.nv = 1;
+    while (s.nv < most && vecs > int64_t(s.nv) * kWave) s.nv *= 2;
+    s.team = 1;
+    while (s.team < kWave && int64_t(s.team) * s.nv < vecs) s.team *= 2;
+    s.block = 256;
+    if (int64_t(s.team) * s.nv < vecs) {
+        const int64_t waves = (vecs + int64_t(s.nv) * kWave - 1) / (int64_t(s.nv) * kWave);
+        s.team = s.block = int(waves * kWave < kNormMaxThreads ? waves * kWave : kNormMaxThreads);
+    }
+    s.in_regs = int64_t(s.team) * s.nv >= vecs;
+    if (!s.in_regs) s.team = s.block = kNormMaxThreads;
+    s.rows = s.team <= kWave ? s.block / s.team : 1;
+    return s;
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
+
+// blocks of the backward pass: a partial row of the weights' gradient each
+int64_t back_blocks(int64_t n, const Shape &s) { return least(ceil_div(n, s.rows), kNormBackBlocks); }
+
+template <typename E, int VEC, int NV> void forward_regs(const NormArgs &a, const Shape &s, hipStream_t st)
+{
+    const int64_t blocks = least(ceil_div(a.n, s.rows), int64_t(kCus) * (2048 / s.block));
+    norm_kernel<E, VEC, NV><<<dim3(uint32_t(blocks)), dim3(s.block), 0, st>>>(a, s.team);
+}
+template <typename E, int VEC, int NV> void backward_regs(const NormArgs &a, const Shape &s, hipStream_t st)
+{
+    const int64_t blocks = back_blocks(a.n, s);
+    const size_t lds = s.rows > 1 ? size_t(s.block) * NV * VEC * sizeof(float) : 0;
+    norm_back_kernel<E, VEC, NV><<<dim3(uint32_t(blocks)), dim3(s.block), lds, st>>>(a, s.team);
+}
+
+template <typename E, int VEC> void forward_vec(const NormArgs &a, const Shape &s, hipStream_t st)
+{
+    if (!s.in_regs) {
+        const int64_t blocks = least(a.n, 2 * kCus);
+        norm_long_kernel<E, VEC><<<dim3(uint32_t(blocks)), dim3(s.block), 0, st>>>(a);
+        return;
+    }
+    switch (s.nv) {
+    case 1: return forward_regs<E, VEC, 1>(a, s, st);
+    case 2:
+        if constexpr (VEC * 2 <= kNormLane) return forward_regs<E, VEC, 2>(a, s, st);
+    case 4:
+        if constexpr (VEC * 4 <= kNormLane) return forward_regs<E, VEC, 4>(a, s, st);
+    case 8:
+        if constexpr (VEC * 8 <= kNormLane) return forward_regs<E, VEC, 8>(a, s, st);
+    default:
+        if constexpr (VEC * 16 <= kNormLane) return forward_regs<E, VEC, 16>(a, s, st);
+    }
+}
+template <typename E, int VEC> void backward_vec(const NormArgs &a, const Shape &s, hipStream_t st)
+{
+    if (!s.in_regs) {
+        if (a.part) {
+            const int64_t blocks = back_blocks(a.n, s);
+            norm_back_columns_kernel<E><<<dim3(uint32_t(ceil_div(a.d, 256)), uint32_t(blocks)), dim3(256), 0, st>>>(a);
+        }
+        if (a.out) norm_back_long_kernel<E, VEC><<<dim3(uint32_t(least(a.n, 2 * kCus))), dim3(s.block), 0, st>>>(a);
+        return;
+    }
+    switch (s.nv) {
+    case 1: return backward_regs<E, VEC, 1>(a, s, st);
+    case 2:
+        if constexpr (VEC * 2 <= kNormLane) return backward_regs<E, VEC, 2>(a, s, st);
+    case 4:
+        if constexpr (VEC * 4 <= kNormLane) return backward_regs<E, VEC, 4>(a, s, st);
+    case 8:
+        if constexpr (VEC * 8 <= kNormLane) return backward_regs<E, VEC, 8>(a, s, st);
+    default:
+        if constexpr (VEC * 16 <= kNormLane) return backward_regs<E, VEC, 16>(a, s, st);
+    }
+}
+
+template <bool kBack, typename E> void run_type(const NormArgs &a, hipStream_t st)
+{
+    const Shape s = shape_of(vector_of(a), a.d);
+    const auto go = [&](auto vec) {
+        if constexpr (kBack)
+            backward_vec<E, decltype(vec)::value>(a, s, st);
+        else
+            forward_vec<E, decltype(vec)::value>(a, s, st);
+    };
+    if constexpr (sizeof(E) == 2)
+        if (s.vec == 8) return go(std::integral_constant<int, 8>());
+    if (s.vec == 4) return go(std::integral_constant<int, 4>());
+    if (s.vec == 2) return go(std::integral_constant<int, 2>());
+    return go(std::integral_constant<int, 1>());
+}
+
+template <bool kBack> void run_norm(const NormArgs &a, hipStream_t st)
+{
+    if (a.type == Elem::kF32)
+        run_type<kBack, float>(a, st);
+    else if (a.type == Elem::kF16)
+        run_type<kBack, f16>(a, st);
+    else
+        run_type<kBack, bf16>(a, st);
+}
+
+} // namespace
+
+void launch_layer_norm(const NormArgs &a, hipStream_t st)
+{
+    if (a.n > 0) run_norm<false>(a, st);
+}
+
+void launch_layer_norm_backward(const NormArgs &a, void *dweight, void *dbias, hipStream_t st)
+{
+    if (a.n > 0) run_norm<true>(a, st);
+    if (a.part) {
+        const int blocks = int(back_blocks(a.n, shape_of(vector_of(a), a.d)));
+        norm_join_kernel<<<dim3(uint32_t(ceil_div(2 * a.d, kJoinCols))), dim3(kJoinCols * kJoinStrands), 0, st>>>(
+            a.part, blocks, a.d, dweight, dbias, a.param);
+    }
+}
+
+} // namespace bht

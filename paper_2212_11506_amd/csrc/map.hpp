@@ -1,0 +1,92 @@
+// Internal declarations of the operators that train a map from features to
+// the embedding: layer norm over all points, and the orthogonalised momentum
+// step of its weight matrices.
+#pragma once
+
+#include "common.hpp"
+
+namespace bht {
+
+typedef _Float16 f16;
+typedef __bf16 bf16;
+
+// element types of the C ABI (BHTSNE_F32, BHTSNE_F16, BHTSNE_BF16)
+enum class Elem { kF32 = 0, kF16 = 1, kBF16 = 2 };
+inline int elem_bytes(Elem e) { return e == Elem::kF32 ? 4 : 2; }
+
+constexpr int kCus = 256; // compute units of the card
+
+// ---------------------------------------------------------------- layer norm
+// Rows are kNormMaxRow features or fewer in registers; longer rows are read
+// again from the caches for each pass.
+constexpr int kNormLane = 16;                      // features of a lane
+constexpr int kNormMaxThreads = 1024;              // lanes of a row
+constexpr int64_t kNormMaxFeatures = int64_t(1) << 24;
+constexpr int kNormBackBlocks = 4 * kCus;          // partial sums of the weights' gradient
+
+struct NormArgs {
+    const void *x;
+    const void *dy;     // backward
+    const void *weight; // nullable
+    const void *bias;   // nullable (forward)
+    void *out;          // y, or dx (nullable in the backward pass)
+    float *mean, *rstd; // written by the forward pass (nullable), read by the backward pass
+    float *part;        // backward: [blocks][2][d] partial sums, nullable (no weight gradient wanted)
+    int64_t x_stride, dy_stride, out_stride;
+    int64_t n, d;
+    double eps;
+    Elem type, param;
+};
+void launch_layer_norm(const NormArgs &a, hipStream_t st);
+// at most min(n, kNormBackBlocks) partial rows are written
+void launch_layer_norm_backward(const NormArgs &a, void *dweight, void *dbias, hipStream_t st);
+
+// ------------------------------------------------------- orthogonalised update
+// Newton-Schulz steps on `batch` matrices U of rows x cols.  U is kept in fp16
+// planes (high and low halves) scaled by powers of two, in its own orientation
+// and transposed, padded with zeros to tiles of kOrthTile.
+constexpr int kOrthTile = 64;
+constexpr int kOrthMaxSteps = 32;
+constexpr int kOrthNormBlocks = 256; // partial sums of squares of a matrix
+constexpr int64_t kOrthMaxSide = 65536;
+
+struct OrthStep {
+    float a, b, c;     // X' = a X + (b A + c A A) X
+    float sx, sa, sb;  // powers of two: scales of X, A and B (the polynomial) in this step
+};
+
+struct OrthArgs {
+    const void *G;
+    float *M;      // nullable: momentum, fp32, updated in place
+    void *W;       // output: the orthogonal factor, or (M given) the weights, updated in place
+    int64_t g_stride, g_batch, m_stride, m_batch, w_stride, w_batch; // in elements: between rows, between matrices
+    int64_t batch, rows, cols;
+    double eps;
+    float momentum, nesterov, keep, rate; // W <- keep W - rate X
+    Elem type;
+    int steps;
+    OrthStep step[kOrthMaxSteps + 1];     // [steps].sx: scale of the last X, unused
+};
+
+// Outputs of 8 bits (bf16) take one product of the high halves, finer ones three.
+// A direction's error is then up to 4e-3 where a + b + c cancels (the largest
+// singular values); it counts 1 / sqrt(m) in a matrix of m directions, so narrow
+// matrices, whose products cost little, take three too.
+constexpr int64_t kOrthOneProduct = 64;
+inline bool orth_split(Elem type, int64_t rows, int64_t cols)
+{
+    return type != Elem::kBF16 || (rows < cols ? rows : cols) <= kOrthOneProduct;
+}
+
+struct OrthLayout {
+    int64_t m, n;         // shorter and longer side, padded
+    int64_t rows, cols;   // padded sides in the caller's orientation
+    size_t u[2], v[2];    // U and its transpose, two buffers each: high plane, low plane behind it
+    size_t a, b;          // A and B, planes as above
+    size_t norm;          // kOrthNormBlocks doubles
+    size_t stride;        // bytes of one matrix' workspace
+};
+OrthLayout make_orth_layout(int64_t rows, int64_t cols);
+void launch_orthogonalise(const OrthArgs &a, void *ws, hipStream_t st);
+
+} // namespace bht
