@@ -52,7 +52,7 @@ float power_of_two_below(double x) { return float(std::exp2(std::floor(std::log2
 
 // The scales of every step.  Singular values of X start in [0, 1]; `most` bounds
 // them through the steps, and with them every value of X (most), of A = X X^T
-// (most^2) and of B = b A + c A^2 (its largest on [0, most^2]).  Half of what fp16
+// (most^2) and of B = a I + b A + c A^2 (|a| and b t + c t^2's largest on [0, most^2]).  Half of what fp16
 // holds is kept for rounding errors' growth.
 bool plan_steps(const double *coefficients, int steps, OrthArgs *a)
 {
@@ -80,7 +80,7 @@ bool plan_steps(const double *coefficients, int steps, OrthArgs *a)
         s.c = float(q[2]);
         s.sx = power_of_two_below(kRoom / std::fmax(most, 1.0));
         s.sa = power_of_two_below(kRoom / std::fmax(t1, 1.0));
-        s.sb = power_of_two_below(kRoom / std::fmax(b, 1.0));
+        s.sb = power_of_two_below(kRoom / std::fmax(b + std::fabs(q[0]), 1.0));
         if (!(x < 64.0)) return false;
         most = x;
     }
@@ -191,7 +191,7 @@ int bhtsne_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x,
 size_t bhtsne_orthogonalise_workspace_size(int64_t batch, int64_t rows, int64_t cols)
 {
     if (batch < 0 || batch > 65535 || rows < 1 || rows > kOrthMaxSide || cols < 1 || cols > kOrthMaxSide) return 0;
-    return size_t(batch > 0 ? batch : 1) * make_orth_layout(rows, cols).stride;
+    return size_t(batch > 0 ? batch : 1) * orth_workspace(rows, cols);
 }
 
 int bhtsne_orthogonalise(const bhtsne_matrices *G, int64_t batch, int64_t rows, int64_t cols, int type,

@@ -71,12 +71,23 @@ struct OrthArgs {
 // Outputs of 8 bits (bf16) take one product of the high halves, finer ones three.
 // A direction's error is then up to 4e-3 where a + b + c cancels (the largest
 // singular values); it counts 1 / sqrt(m) in a matrix of m directions, so narrow
-// matrices, whose products cost little, take three too.
-constexpr int64_t kOrthOneProduct = 64;
-inline bool orth_split(Elem type, int64_t rows, int64_t cols)
-{
-    return type != Elem::kBF16 || (rows < cols ? rows : cols) <= kOrthOneProduct;
-}
+// matrices take three for every type.
+constexpr int64_t kNarrow = 64;             // directions of a narrow matrix
+constexpr int64_t kNarrowWhole = 64 * 256;  // values (padded) of one that a block holds whole, in 128 KB of LDS
+inline bool orth_narrow(int64_t rows, int64_t cols) { return (rows < cols ? rows : cols) <= kNarrow; }
+
+struct NarrowLayout {
+    int blocks;        // 32-row blocks of the shorter side
+    int width, slices; // columns of a slice, slices (1: one launch does everything)
+    int norm_blocks;   // partial sums of squares
+    int64_t n;         // longer side, padded
+    size_t x;          // X^T, planes as below
+    size_t gram[2];    // the slices' Gram matrices, of this step and of the next
+    size_t total;      // their sum
+    size_t norm;
+    size_t stride;
+};
+NarrowLayout make_narrow_layout(int64_t rows, int64_t cols);
 
 struct OrthLayout {
     int64_t m, n;         // shorter and longer side, padded
@@ -87,6 +98,7 @@ struct OrthLayout {
     size_t stride;        // bytes of one matrix' workspace
 };
 OrthLayout make_orth_layout(int64_t rows, int64_t cols);
+size_t orth_workspace(int64_t rows, int64_t cols); // bytes for one matrix
 void launch_orthogonalise(const OrthArgs &a, void *ws, hipStream_t st);
 
 } // namespace bht

@@ -64,6 +64,20 @@ def test_shapes(shape, dtype):
     assert rel(O, plain(G)) <= TOL[dtype]
 
 
+# few directions: X in one block up to its LDS, then cut into slices, few and many; one value over each end
+NARROW = [(64, 256), (64, 257), (32, 512), (32, 513), (33, 256), (257, 64), (5, 1000), (1500, 40), (33, 2048), (33, 2049), (64, 5000),
+          (9000, 20), (1, 65536)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", NARROW)
+def test_few_directions(shape, dtype):
+    say(f"[orth] {shape} {dtype}")
+    G = gauss(2, *shape, seed=shape[0] + shape[1], dtype=dtype, scale=1e-3)
+    O, want = bh.orthogonalise(G), plain(G)
+    assert max(rel(O[k], want[k]) for k in range(2)) <= TOL[dtype]
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_spectra(dtype):
     """Singular values that fall off by 1e4, and eight large ones over noise: errors against the largest would show."""
