@@ -25,9 +25,7 @@ namespace {
 typedef f16 half8 __attribute__((ext_vector_type(8)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
-constexpr int kT = kOrthTile;
-constexpr int kK = 64;          // depth of a staged slice: 128 bytes a row
-constexpr int kProdBlock = 256; // 4 waves
+constexpr int kT = 64; // tile of the planes' kernel
 
 __device__ inline float load_elem(const void *p, Elem t, int64_t i)
 {
@@ -51,25 +49,62 @@ __device__ inline float update_value(const OrthArgs &a, float g, float m)
     return a.M ? (a.nesterov != 0.0f ? g + a.momentum * m : m) : g;
 }
 
+// Eight values of a row from p, of which `left` exist; vec: p and the row are aligned for 16-byte loads
+template <typename E> struct alignas(16) Vec16 {
+    E v[16 / sizeof(E)];
+};
+template <typename E> __device__ inline void load8(const E *p, int left, bool vec, float (&v)[8])
+{
+    constexpr int kV = 16 / sizeof(E);
+    if (vec && left >= 8) {
+#pragma unroll
+        for (int h = 0; h < 8 / kV; ++h) {
+            const Vec16<E> x = reinterpret_cast<const Vec16<E> *>(p)[h];
+#pragma unroll
+            for (int e = 0; e < kV; ++e) v[h * kV + e] = float(x.v[e]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < left ? float(p[e]) : 0.0f;
+}
+__device__ inline void store8(float *p, int left, bool vec, const float (&v)[8])
+{
+    if (vec && left >= 8) {
+        reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < left) p[e] = v[e];
+}
+
 // The momentum's update, and partial sums of U's squares: fp64, in a fixed order.
+template <typename E>
 __global__ __launch_bounds__(256) void orth_norm_kernel(OrthArgs a, char *ws, int64_t ws_stride, size_t at)
 {
     __shared__ double s_w[256 / kWave];
     const int64_t z = blockIdx.y;
     double sum = 0.0;
-    const int64_t total = a.rows * a.cols;
-    const int64_t per = (total + gridDim.x - 1) / gridDim.x; // a contiguous range of elements each
-    const int64_t lo = blockIdx.x * per, hi = lo + per < total ? lo + per : total;
-    for (int64_t e = lo + threadIdx.x; e < hi; e += 256) {
-        const int64_t r = e / a.cols, c = e - r * a.cols;
-        float g = load_elem(a.G, a.type, z * a.g_batch + r * a.g_stride + c), m = 0.0f;
+    const uint32_t across = uint32_t((a.cols + 7) / 8), total = across * uint32_t(a.rows); // < 2^29
+    for (uint32_t e = blockIdx.x * 256 + threadIdx.x; e < total; e += gridDim.x * 256) {
+        const uint32_t r = e / across, c = (e - r * across) * 8;
+        const int left = int(a.cols - c);
+        float g[8], m[8] = {};
+        load8(static_cast<const E *>(a.G) + z * a.g_batch + r * a.g_stride + c, left, a.g_vec, g);
         if (a.M) {
             float *M = a.M + z * a.m_batch + r * a.m_stride + c;
-            m = a.momentum * *M + g;
-            *M = m;
+            load8(M, left, a.m_vec, m);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) m[k] = a.momentum * m[k] + g[k];
+            store8(M, left, a.m_vec, m);
         }
-        const double u = double(update_value(a, g, m));
-        sum += u * u;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const double u = double(update_value(a, g[k], m[k]));
+            sum += u * u;
+        }
     }
     sum = wave_sum(sum);
     if (lane_id() == 0) s_w[threadIdx.x / kWave] = sum;
@@ -87,12 +122,25 @@ __device__ inline void split(float v, f16 &h, f16 &l)
     l = f16(v - float(h));
 }
 
-// U / (|U| + eps) in planes, in both orientations, zeros in the padding
-__global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, OrthLayout L, int norm_blocks)
+// U / (|U| + eps) in planes, in both orientations, zeros in the padding; low_t: the transposed low plane has a reader
+template <typename E>
+__global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, OrthLayout L, int norm_blocks, bool low_t)
 {
-    __shared__ f16 s_t[2][kT][kT + 2];
+    __shared__ float s_t[kT][kT + 1];
     const int64_t z = blockIdx.z, r0 = int64_t(blockIdx.y) * kT, c0 = int64_t(blockIdx.x) * kT;
     char *base = ws + z * L.stride;
+    const int piece = threadIdx.x % 8 * 8;
+    float v[2][8];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const int64_t r = r0 + threadIdx.x / 8 + 32 * s, c = c0 + piece;
+        const int left = r < a.rows ? int(a.cols - c) : 0;
+        float m[8] = {};
+        load8(static_cast<const E *>(a.G) + z * a.g_batch + r * a.g_stride + c, left, a.g_vec, v[s]);
+        if (a.M) load8(a.M + z * a.m_batch + r * a.m_stride + c, left, a.m_vec, m);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[s][e] = update_value(a, v[s][e], m[e]);
+    }
     const double *part = reinterpret_cast<const double *>(base + L.norm);
     double sq = 0.0;
     for (int k = lane_id(); k < norm_blocks; k += kWave) sq += part[k];
@@ -100,54 +148,63 @@ __global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, 
     const double scale = double(a.step[0].sx) / (sqrt(sq) + a.eps);
     f16 *uh = reinterpret_cast<f16 *>(base + L.u[0]), *ul = uh + L.rows * L.cols;
     f16 *vh = reinterpret_cast<f16 *>(base + L.v[0]), *vl = vh + L.rows * L.cols;
-    for (int e = threadIdx.x; e < kT * kT; e += 256) {
-        const int i = e / kT, j = e % kT;
-        const int64_t r = r0 + i, c = c0 + j;
-        float v = 0.0f;
-        if (r < a.rows && c < a.cols) {
-            const float g = load_elem(a.G, a.type, z * a.g_batch + r * a.g_stride + c);
-            const float m = a.M ? a.M[z * a.m_batch + r * a.m_stride + c] : 0.0f;
-            v = float(double(update_value(a, g, m)) * scale);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const int row = threadIdx.x / 8 + 32 * s;
+        half8 h, l;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = float(double(v[s][e]) * scale);
+            f16 xh, xl;
+            split(x, xh, xl);
+            h[e] = xh;
+            l[e] = xl;
+            s_t[row][piece + e] = x;
         }
-        f16 h, l;
-        split(v, h, l);
-        uh[r * L.cols + c] = h;
-        ul[r * L.cols + c] = l;
-        s_t[0][j][i] = h;
-        s_t[1][j][i] = l;
+        *reinterpret_cast<half8 *>(uh + (r0 + row) * L.cols + c0 + piece) = h;
+        *reinterpret_cast<half8 *>(ul + (r0 + row) * L.cols + c0 + piece) = l;
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < kT * kT; e += 256) {
-        const int j = e / kT, i = e % kT;
-        vh[(c0 + j) * L.rows + r0 + i] = s_t[0][j][i];
-        vl[(c0 + j) * L.rows + r0 + i] = s_t[1][j][i];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const int col = threadIdx.x / 8 + 32 * s;
+        half8 h, l;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            f16 xh, xl;
+            split(s_t[piece + e][col], xh, xl);
+            h[e] = xh;
+            l[e] = xl;
+        }
+        *reinterpret_cast<half8 *>(vh + (c0 + col) * L.rows + r0 + piece) = h;
+        if (low_t) *reinterpret_cast<half8 *>(vl + (c0 + col) * L.rows + r0 + piece) = l;
     }
 }
 
 // ------------------------------------------------------------------ products
 enum class Prod { kGram, kPoly, kApply, kLast };
 
-// One tile of C = P Q^T, P and Q row-major with K values a row.  Operands are staged in
-// LDS by loads that write it directly; a row's eight 16-byte pieces are stored in
-// an order that depends on the row (piece c of row r in place c ^ (r % 8)), so
-// that the lanes of a fragment read, which take the same piece of 32 rows, fall on
+// A block makes a kM x kN tile of C = P Q^T, P and Q row-major with K values a row, by kWm x kWn waves.  Slices of
+// 64 values a row (128 bytes) go through a ring of kStages buffers in LDS, filled by loads that write LDS directly,
+// kStages - 1 slices ahead.  A row's eight 16-byte pieces are stored in an order that depends on the row (piece c of
+// row r in place c ^ (r % 8)), so that the lanes of a fragment read, which take the same piece of 32 rows, fall on
 // different banks.
-template <bool kSplit> struct Staged {
-    f16 p[kSplit ? 2 : 1][kT * kK];
-    f16 q[kSplit ? 2 : 1][kT * kK];
-};
-template <bool kSplit> union alignas(16) Shared {
-    Staged<kSplit> in;
-    float out[kT][kT + 1];
+constexpr int kK = 64;
+template <int M, int N, int Wm, int Wn, int Stages> struct Tile {
+    static constexpr int kM = M, kN = N, kWm = Wm, kWn = Wn, kStages = Stages;
+    static constexpr int kWaves = Wm * Wn, kThreads = kWaves * kWave;
+    static constexpr int kI = M / Wm / 32, kJ = N / Wn / 32; // 32 x 32 blocks of a wave
 };
 
-__device__ inline void stage(const f16 *src, int64_t ld, f16 *dst)
+// rows of one plane, kRows / 8 groups of eight dealt to the waves
+template <typename T, int kRows> __device__ inline void stage(const f16 *src, int64_t ld, f16 *dst)
 {
-    const int w = threadIdx.x / kWave, lane = lane_id();
+    static_assert(kRows / 8 % T::kWaves == 0, "every wave loads as much");
+    const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id();
     const int r = lane / 8, piece = (lane % 8) ^ r;
 #pragma unroll
-    for (int k = 0; k < kT / 32; ++k) {
-        const int row = (k * 4 + w) * 8;
+    for (int k = 0; k < kRows / 8 / T::kWaves; ++k) {
+        const int row = (k * T::kWaves + w) * 8;
         __builtin_amdgcn_global_load_lds(
             (const __attribute__((address_space(1))) void *)(src + (row + r) * ld + piece * 8),
             (__attribute__((address_space(3))) void *)(dst + row * kK), 16, 0, 0);
@@ -159,23 +216,37 @@ __device__ inline half8 fragment(const f16 *tile, int row, int piece)
     return *reinterpret_cast<const half8 *>(tile + row * kK + ((piece ^ (row & 7)) * 8));
 }
 
-template <bool kSplit, Prod kProd>
-__global__ __launch_bounds__(kProdBlock) void orth_product_kernel(OrthArgs a, char *ws, OrthLayout L, int k)
+// Logical tile of a block: blocks are dealt to the 8 XCDs in turn, each XCD gets consecutive tiles
+__device__ inline int xcd_tile(int b, int blocks)
 {
-    __shared__ Shared<kSplit> s;
+    const int x = b % 8, q = blocks / 8, r = blocks % 8;
+    return x * q + (x < r ? x : r) + b / 8;
+}
+
+constexpr int kPatch = 33; // row of a wave's 32 x 32 patch in LDS, floats
+
+template <typename T, bool kSplit, Prod kProd>
+__global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, char *ws, OrthLayout L, int k)
+{
+    constexpr int kPlanes = kSplit ? 2 : 1;
+    constexpr int kP = T::kM * kK, kQ = T::kN * kK;        // values of a staged plane
+    constexpr int kStage = kPlanes * (kP + kQ);
+    constexpr int kLoads = kPlanes * (T::kM + T::kN) / 8 / T::kWaves; // of a wave and stage
+    extern __shared__ __align__(16) char s_mem[];
+    f16 *ring = reinterpret_cast<f16 *>(s_mem);
     const OrthStep &S = a.step[k];
     const bool wide = a.rows <= a.cols;
     char *base = ws + int64_t(blockIdx.z) * L.stride;
     const int64_t plane = L.rows * L.cols, square = L.m * L.m;
     f16 *U = reinterpret_cast<f16 *>(base + L.u[k & 1]), *V = reinterpret_cast<f16 *>(base + L.v[k & 1]);
     f16 *A = reinterpret_cast<f16 *>(base + L.a), *B = reinterpret_cast<f16 *>(base + L.b);
-    int64_t bi, bj;
+    int bi, bj;
     const f16 *P, *Q;
     int64_t K, p_plane, q_plane;
+    const int t = xcd_tile(blockIdx.x, gridDim.x);
     if constexpr (kProd == Prod::kGram || kProd == Prod::kPoly) {
         // tiles on and below the diagonal, row by row
-        const int t = blockIdx.x;
-        bi = int64_t((sqrtf(8.0f * float(t) + 1.0f) - 1.0f) * 0.5f);
+        bi = int((sqrtf(8.0f * float(t) + 1.0f) - 1.0f) * 0.5f);
         while ((bi + 1) * (bi + 2) / 2 <= t) ++bi;
         while (bi * (bi + 1) / 2 > t) --bi;
         bj = t - bi * (bi + 1) / 2;
@@ -189,121 +260,195 @@ __global__ __launch_bounds__(kProdBlock) void orth_product_kernel(OrthArgs a, ch
             p_plane = q_plane = square;
         }
     } else {
-        bi = blockIdx.y;
-        bj = blockIdx.x;
+        // four rows of tiles at a time, column by column
+        const int across = int(L.cols) / T::kN, down = int(L.rows) / T::kM;
+        const int group = t / (4 * across), top = group * 4, high = down - top < 4 ? down - top : 4;
+        const int in = t - group * 4 * across;
+        bi = top + in % high;
+        bj = in / high;
         K = L.m;
         P = wide ? B : U;
         Q = wide ? V : B;
         p_plane = wide ? square : plane;
         q_plane = wide ? plane : square;
     }
-    P += bi * kT * K;
-    Q += bj * kT * K;
-    const int w = threadIdx.x / kWave, lane = lane_id();
-    const int wi = (w / 2) * 32, wj = (w % 2) * 32;
-    float16v acc = {};
-    for (int64_t k0 = 0; k0 < K; k0 += kK) {
-        __syncthreads();
-        stage(P + k0, K, s.in.p[0]);
-        stage(Q + k0, K, s.in.q[0]);
+    P += int64_t(bi) * T::kM * K;
+    Q += int64_t(bj) * T::kN * K;
+    const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id();
+    const int wi = w / T::kWn * (T::kI * 32), wj = w % T::kWn * (T::kJ * 32);
+
+    const int slices = int(K / kK);
+    const auto fetch = [&](int slice) {
+        // past the end the last slice again, into a buffer that nobody reads: every wait counts alike
+        const int64_t k0 = int64_t(slice < slices ? slice : slices - 1) * kK;
+        f16 *to = ring + slice % T::kStages * kStage;
+        stage<T, T::kM>(P + k0, K, to);
+        stage<T, T::kN>(Q + k0, K, to + kPlanes * kP);
         if constexpr (kSplit) {
-            stage(P + p_plane + k0, K, s.in.p[1]);
-            stage(Q + q_plane + k0, K, s.in.q[1]);
+            stage<T, T::kM>(P + p_plane + k0, K, to + kP);
+            stage<T, T::kN>(Q + q_plane + k0, K, to + kPlanes * kP + kQ);
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // the staged slice is in LDS
-        __syncthreads();
+    };
+    float16v acc[T::kI][T::kJ] = {};
+#pragma unroll
+    for (int p = 0; p < T::kStages - 1; ++p) fetch(p);
+    for (int slice = 0; slice < slices; ++slice) {
+        // this wave's loads of the slice have landed, then everybody's; and everybody has read the slice before
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((T::kStages - 2) * kLoads) : "memory");
+        fetch(slice + T::kStages - 1);
+        const f16 *in = ring + slice % T::kStages * kStage;
 #pragma unroll
         for (int kk = 0; kk < kK / 16; ++kk) {
             const int piece = kk * 2 + lane / 32;
-            const half8 ph = fragment(s.in.p[0], wi + lane % 32, piece), qh = fragment(s.in.q[0], wj + lane % 32, piece);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc, 0, 0, 0);
-            if constexpr (kSplit) {
-                const half8 pl = fragment(s.in.p[1], wi + lane % 32, piece), ql = fragment(s.in.q[1], wj + lane % 32, piece);
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, acc, 0, 0, 0);
+            half8 p[kPlanes][T::kI], q[kPlanes][T::kJ];
+#pragma unroll
+            for (int h = 0; h < kPlanes; ++h) {
+#pragma unroll
+                for (int i = 0; i < T::kI; ++i) p[h][i] = fragment(in + h * kP, wi + 32 * i + lane % 32, piece);
+#pragma unroll
+                for (int j = 0; j < T::kJ; ++j) q[h][j] = fragment(in + kPlanes * kP + h * kQ, wj + 32 * j + lane % 32, piece);
             }
+#pragma unroll
+            for (int i = 0; i < T::kI; ++i)
+#pragma unroll
+                for (int j = 0; j < T::kJ; ++j) {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[0][i], q[0][j], acc[i][j], 0, 0, 0);
+                    if constexpr (kSplit) {
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[0][i], q[1][j], acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[1][i], q[0][j], acc[i][j], 0, 0, 0);
+                    }
+                }
         }
     }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s.out[wi + 8 * (r / 4) + 4 * (lane / 32) + r % 4][wj + lane % 32] = acc[r];
-    __syncthreads();
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); // the ring is free
 
-    const int64_t r0 = bi * kT, c0 = bj * kT;
-    // values in the tile's own orientation
-    f16 *out_h = nullptr;
-    int64_t ld = 0, out_plane = 0;
-    if constexpr (kProd == Prod::kGram) {
-        out_h = A;
-        ld = L.m;
-        out_plane = square;
-    } else if constexpr (kProd == Prod::kPoly) {
-        out_h = B;
-        ld = L.m;
+    // Each wave puts its blocks through a patch of its own in LDS, for rows of 16 bytes in either orientation
+    float *patch = reinterpret_cast<float *>(s_mem) + w * 32 * kPatch;
+    f16 *out = nullptr, *out_t = nullptr;
+    int64_t ld = 0, ld_t = 0, out_plane = 0;
+    if constexpr (kProd == Prod::kGram || kProd == Prod::kPoly) {
+        out = out_t = kProd == Prod::kGram ? A : B;
+        ld = ld_t = L.m;
         out_plane = square;
     } else if constexpr (kProd == Prod::kApply) {
-        out_h = reinterpret_cast<f16 *>(base + L.u[(k + 1) & 1]);
+        out = reinterpret_cast<f16 *>(base + L.u[(k + 1) & 1]);
+        out_t = reinterpret_cast<f16 *>(base + L.v[(k + 1) & 1]);
         ld = L.cols;
+        ld_t = L.rows;
         out_plane = plane;
     }
-    const float xs = kProd == Prod::kApply ? a.step[k + 1].sx / S.sx : 1.0f / S.sx;
-    for (int e = threadIdx.x; e < kT * kT; e += kProdBlock) {
-        const int i = e / kT, j = e % kT;
-        const int64_t r = r0 + i, c = c0 + j;
-        float v = s.out[i][j];
-        if constexpr (kProd == Prod::kGram) {
-            v *= S.sa / (S.sx * S.sx);
-        } else if constexpr (kProd == Prod::kPoly) {
-            const float av = float(A[r * L.m + c]) + float(A[square + r * L.m + c]);
-            v = av * (S.b * S.sb / S.sa) + v * (S.c * S.sb / (S.sa * S.sa));
-            if (kSplit && r == c) v += S.a * S.sb;
-        } else {
-            v *= 1.0f / S.sb;
-            if constexpr (!kSplit) v += S.a * (float(U[r * L.cols + c]) + float(U[plane + r * L.cols + c]));
-            v *= xs;
-        }
-        if constexpr (kProd == Prod::kLast) {
-            if (r < a.rows && c < a.cols) {
-                const int64_t at = int64_t(blockIdx.z) * a.w_batch + r * a.w_stride + c;
-                if (a.M) v = a.keep * load_elem(a.W, a.type, at) - a.rate * v;
-                store_elem(a.W, a.type, at, v);
+    const float xs = kProd == Prod::kApply ? a.step[k + 1].sx : 1.0f;
+    // what has a second reader or user: A's low plane (B's terms), X's (a X), the transposed X's in split products
+    constexpr bool kLow = kSplit || kProd != Prod::kPoly, kLowT = kSplit || kProd == Prod::kGram;
+#pragma unroll
+    for (int i = 0; i < T::kI; ++i)
+#pragma unroll
+        for (int j = 0; j < T::kJ; ++j) {
+            const int64_t r0 = int64_t(bi) * T::kM + wi + 32 * i, c0 = int64_t(bj) * T::kN + wj + 32 * j;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) patch[(8 * (r / 4) + 4 * (lane / 32) + r % 4) * kPatch + lane % 32] = acc[i][j][r];
+            if constexpr (kProd == Prod::kLast) {
+                const int64_t c = c0 + lane % 32;
+#pragma unroll 4
+                for (int s = 0; s < 16; ++s) {
+                    const int64_t r = r0 + 2 * s + lane / 32;
+                    if (r >= a.rows || c >= a.cols) continue;
+                    float v = patch[(2 * s + lane / 32) * kPatch + lane % 32] * (1.0f / (S.sb * S.sx));
+                    if constexpr (!kSplit)
+                        v += (S.a / S.sx) * (float(U[r * L.cols + c]) + float(U[plane + r * L.cols + c]));
+                    const int64_t at = int64_t(blockIdx.z) * a.w_batch + r * a.w_stride + c;
+                    if (a.M) v = a.keep * load_elem(a.W, a.type, at) - a.rate * v;
+                    store_elem(a.W, a.type, at, v);
+                }
+                continue;
             }
-        } else {
-            f16 h, l;
-            split(v, h, l);
-            out_h[r * ld + c] = h;
-            out_h[out_plane + r * ld + c] = l;
-            s.out[i][j] = v;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int row = (lane + 64 * s) / 4, col = lane % 4 * 8;
+                const int64_t at = (r0 + row) * ld + c0 + col;
+                float *v = patch + row * kPatch + col;
+                half8 h, l, xh, xl;
+                if constexpr (kProd == Prod::kPoly) {
+                    xh = *reinterpret_cast<const half8 *>(A + at);
+                    xl = *reinterpret_cast<const half8 *>(A + square + at);
+                } else if constexpr (kProd == Prod::kApply && !kSplit) {
+                    xh = *reinterpret_cast<const half8 *>(U + at);
+                    xl = *reinterpret_cast<const half8 *>(U + plane + at);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float x = v[e];
+                    if constexpr (kProd == Prod::kGram) {
+                        x *= S.sa / (S.sx * S.sx);
+                    } else if constexpr (kProd == Prod::kPoly) {
+                        x = (float(xh[e]) + float(xl[e])) * (S.b * S.sb / S.sa) + x * (S.c * S.sb / (S.sa * S.sa));
+                        if (kSplit && r0 + row == c0 + col + e) x += S.a * S.sb;
+                    } else {
+                        x *= xs / (S.sb * S.sx);
+                        if constexpr (!kSplit) x += (S.a * xs / S.sx) * (float(xh[e]) + float(xl[e]));
+                    }
+                    f16 vh, vl;
+                    split(x, vh, vl);
+                    h[e] = vh;
+                    l[e] = vl;
+                    v[e] = x;
+                }
+                *reinterpret_cast<half8 *>(out + at) = h;
+                if constexpr (kLow) *reinterpret_cast<half8 *>(out + out_plane + at) = l;
+            }
+            if (kProd != Prod::kApply && bi == bj) continue;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int col = (lane + 64 * s) / 4, row = lane % 4 * 8;
+                const int64_t at = (c0 + col) * ld_t + r0 + row;
+                half8 h, l;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    f16 vh, vl;
+                    split(patch[(row + e) * kPatch + col], vh, vl);
+                    h[e] = vh;
+                    l[e] = vl;
+                }
+                *reinterpret_cast<half8 *>(out_t + at) = h;
+                if constexpr (kLowT) *reinterpret_cast<half8 *>(out_t + out_plane + at) = l;
+            }
         }
+}
+
+template <typename T, bool kSplit, Prod kProd>
+void run_product(const OrthArgs &a, char *ws, const OrthLayout &L, int k, hipStream_t st)
+{
+    constexpr size_t kRing = size_t(T::kStages) * (kSplit ? 2 : 1) * (T::kM + T::kN) * kK * sizeof(f16);
+    constexpr size_t kPatches = size_t(T::kWaves) * 32 * kPatch * sizeof(float);
+    constexpr size_t kLds = kRing > kPatches ? kRing : kPatches;
+    static_assert(kLds <= 160 * 1024, "LDS of a CU");
+    uint32_t tiles;
+    if constexpr (kProd == Prod::kGram || kProd == Prod::kPoly) {
+        static_assert(T::kM == T::kN, "symmetric products");
+        const uint32_t mt = uint32_t(L.m / T::kM);
+        tiles = mt * (mt + 1) / 2;
+    } else {
+        tiles = uint32_t(L.rows / T::kM) * uint32_t(L.cols / T::kN);
     }
-    if constexpr (kProd != Prod::kLast) {
-        if (kProd != Prod::kApply && bi == bj) return;
-        __syncthreads();
-        f16 *t_h = kProd == Prod::kApply ? reinterpret_cast<f16 *>(base + L.v[(k + 1) & 1]) : out_h;
-        const int64_t t_ld = kProd == Prod::kApply ? L.rows : L.m;
-        for (int e = threadIdx.x; e < kT * kT; e += kProdBlock) {
-            const int j = e / kT, i = e % kT;
-            f16 h, l;
-            split(s.out[i][j], h, l);
-            t_h[(c0 + j) * t_ld + r0 + i] = h;
-            t_h[out_plane + (c0 + j) * t_ld + r0 + i] = l;
-        }
+    orth_product_kernel<T, kSplit, kProd><<<dim3(tiles, 1, uint32_t(a.batch)), T::kThreads, kLds, st>>>(a, ws, L, k);
+}
+
+// TS: tiles of the symmetric products, TX: of B X
+template <typename TS, typename TX, bool kSplit> void run_steps(const OrthArgs &a, char *ws, const OrthLayout &L, hipStream_t st)
+{
+    for (int k = 0; k < a.steps; ++k) {
+        run_product<TS, kSplit, Prod::kGram>(a, ws, L, k, st);
+        run_product<TS, kSplit, Prod::kPoly>(a, ws, L, k, st);
+        if (k + 1 < a.steps)
+            run_product<TX, kSplit, Prod::kApply>(a, ws, L, k, st);
+        else
+            run_product<TX, kSplit, Prod::kLast>(a, ws, L, k, st);
     }
 }
 
-template <bool kSplit> void run_steps(const OrthArgs &a, char *ws, const OrthLayout &L, hipStream_t st)
-{
-    const uint32_t mt = uint32_t(L.m / kT), tri = mt * (mt + 1) / 2, z = uint32_t(a.batch);
-    const dim3 square(tri, 1, z), full(uint32_t(L.cols / kT), uint32_t(L.rows / kT), z);
-    for (int k = 0; k < a.steps; ++k) {
-        orth_product_kernel<kSplit, Prod::kGram><<<square, kProdBlock, 0, st>>>(a, ws, L, k);
-        orth_product_kernel<kSplit, Prod::kPoly><<<square, kProdBlock, 0, st>>>(a, ws, L, k);
-        if (k + 1 < a.steps)
-            orth_product_kernel<kSplit, Prod::kApply><<<full, kProdBlock, 0, st>>>(a, ws, L, k);
-        else
-            orth_product_kernel<kSplit, Prod::kLast><<<full, kProdBlock, 0, st>>>(a, ws, L, k);
-    }
-}
+using Tile64 = Tile<64, 64, 2, 2, 4>;    // 4 waves, 32 x 32 each
+using Tile128 = Tile<128, 128, 2, 2, 2>; // 4 waves, 64 x 64
+using Tile256 = Tile<256, 256, 2, 4, 2>; // 8 waves, 128 x 64
 
 // ------------------------------------------------------------------ narrow matrices
 // At most 64 directions (m <= 64).  X lives in LDS, as fp16 halves and in both orientations: rows of X for the
@@ -671,26 +816,18 @@ template <typename E, int MB> void run_narrow(const OrthArgs &a, char *ws, const
         orth_narrow_kernel<E, MB, true><<<grid, kNarrowBlock, lds, st>>>(a, ws, L, 0, 0);
         return;
     }
-    orth_norm_kernel<<<dim3(L.norm_blocks, uint32_t(a.batch)), 256, 0, st>>>(a, ws, int64_t(L.stride), L.norm);
+    orth_norm_kernel<E><<<dim3(L.norm_blocks, uint32_t(a.batch)), 256, 0, st>>>(a, ws, int64_t(L.stride), L.norm);
     const bool sum = L.slices > kSliceSum;
     for (int k = 0; k <= a.steps; ++k) {
         if (k > 0 && sum) orth_sum_kernel<<<dim3(kM * kM / kWave, uint32_t(a.batch)), 256, 0, st>>>(ws, L, k - 1, kM * kM);
         orth_narrow_kernel<E, MB, false><<<grid, kNarrowBlock, lds, st>>>(a, ws, L, k, sum);
     }
 }
-template <typename E> void run_narrow_type(const OrthArgs &a, char *ws, const NarrowLayout &L, hipStream_t st)
-{
-    if (L.blocks == 1)
-        run_narrow<E, 1>(a, ws, L, st);
-    else
-        run_narrow<E, 2>(a, ws, L, st);
-}
-
 } // namespace
 
 int norm_blocks_of(int64_t rows, int64_t cols)
 {
-    const int64_t want = (rows * cols + 4095) / 4096;
+    const int64_t want = (rows * cols + 2047) / 2048; // 8 values a thread
     return int(want < kOrthNormBlocks ? want : kOrthNormBlocks);
 }
 
@@ -722,7 +859,10 @@ NarrowLayout make_narrow_layout(int64_t rows, int64_t cols)
 OrthLayout make_orth_layout(int64_t rows, int64_t cols)
 {
     OrthLayout L;
-    const auto pad = [](int64_t x) { return (x + kT - 1) / kT * kT; };
+    // the largest tile that still gives the chip a tile of B X for each CU
+    const auto tiles = [&](int64_t t) { return ((rows + t - 1) / t) * ((cols + t - 1) / t); };
+    L.tile = tiles(256) >= kCus ? 256 : tiles(128) >= kCus ? 128 : 64;
+    const auto pad = [&](int64_t x) { return (x + L.tile - 1) / L.tile * L.tile; };
     L.rows = pad(rows);
     L.cols = pad(cols);
     L.m = L.rows < L.cols ? L.rows : L.cols;
@@ -750,28 +890,53 @@ size_t orth_workspace(int64_t rows, int64_t cols)
     return orth_narrow(rows, cols) ? make_narrow_layout(rows, cols).stride : make_orth_layout(rows, cols).stride;
 }
 
-void launch_orthogonalise(const OrthArgs &a, void *workspace, hipStream_t st)
+namespace {
+
+template <typename E> void run_type(const OrthArgs &a, char *ws, hipStream_t st)
 {
-    if (a.batch == 0) return;
-    char *ws = static_cast<char *>(workspace);
     if (orth_narrow(a.rows, a.cols)) {
         const NarrowLayout L = make_narrow_layout(a.rows, a.cols);
-        if (a.type == Elem::kF32)
-            run_narrow_type<float>(a, ws, L, st);
-        else if (a.type == Elem::kF16)
-            run_narrow_type<f16>(a, ws, L, st);
+        if (L.blocks == 1)
+            run_narrow<E, 1>(a, ws, L, st);
         else
-            run_narrow_type<bf16>(a, ws, L, st);
+            run_narrow<E, 2>(a, ws, L, st);
         return;
     }
+    constexpr bool kSplit = !std::is_same<E, bf16>::value;
     const OrthLayout L = make_orth_layout(a.rows, a.cols);
     const int norm_blocks = norm_blocks_of(a.rows, a.cols);
-    orth_norm_kernel<<<dim3(norm_blocks, uint32_t(a.batch)), 256, 0, st>>>(a, ws, int64_t(L.stride), L.norm);
-    orth_planes_kernel<<<dim3(uint32_t(L.cols / kT), uint32_t(L.rows / kT), uint32_t(a.batch)), 256, 0, st>>>(a, ws, L, norm_blocks);
-    if (a.type != Elem::kBF16)
-        run_steps<true>(a, ws, L, st);
+    orth_norm_kernel<E><<<dim3(norm_blocks, uint32_t(a.batch)), 256, 0, st>>>(a, ws, int64_t(L.stride), L.norm);
+    orth_planes_kernel<E><<<dim3(uint32_t(L.cols / kT), uint32_t(L.rows / kT), uint32_t(a.batch)), 256, 0, st>>>(
+        a, ws, L, norm_blocks, kSplit);
+    if (L.tile == 64)
+        run_steps<Tile64, Tile64, kSplit>(a, ws, L, st);
+    else if (kSplit || L.tile == 128)
+        run_steps<Tile128, Tile128, kSplit>(a, ws, L, st);
+    else if constexpr (!kSplit)
+        run_steps<Tile128, Tile256, kSplit>(a, ws, L, st);
+}
+
+// rows and matrices start on 16 bytes
+bool vectors(const void *p, int64_t stride, int64_t batch_stride, int64_t batch, int bytes)
+{
+    return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(stride * bytes) | uintptr_t(batch > 1 ? batch_stride * bytes : 0)) & 15u) == 0;
+}
+
+} // namespace
+
+void launch_orthogonalise(const OrthArgs &args, void *workspace, hipStream_t st)
+{
+    if (args.batch == 0) return;
+    OrthArgs a = args;
+    a.g_vec = vectors(a.G, a.g_stride, a.g_batch, a.batch, elem_bytes(a.type));
+    a.m_vec = vectors(a.M, a.m_stride, a.m_batch, a.batch, 4);
+    char *ws = static_cast<char *>(workspace);
+    if (a.type == Elem::kF32)
+        run_type<float>(a, ws, st);
+    else if (a.type == Elem::kF16)
+        run_type<f16>(a, ws, st);
     else
-        run_steps<false>(a, ws, L, st);
+        run_type<bf16>(a, ws, st);
 }
 
 } // namespace bht

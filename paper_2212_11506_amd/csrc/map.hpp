@@ -44,10 +44,9 @@ void launch_layer_norm_backward(const NormArgs &a, void *dweight, void *dbias, h
 // ------------------------------------------------------- orthogonalised update
 // Newton-Schulz steps on `batch` matrices U of rows x cols.  U is kept in fp16
 // planes (high and low halves) scaled by powers of two, in its own orientation
-// and transposed, padded with zeros to tiles of kOrthTile.
-constexpr int kOrthTile = 64;
+// and transposed, padded with zeros to whole tiles.
 constexpr int kOrthMaxSteps = 32;
-constexpr int kOrthNormBlocks = 256; // partial sums of squares of a matrix
+constexpr int kOrthNormBlocks = 512; // partial sums of squares of a matrix
 constexpr int64_t kOrthMaxSide = 65536;
 
 struct OrthStep {
@@ -64,6 +63,7 @@ struct OrthArgs {
     double eps;
     float momentum, nesterov, keep, rate; // W <- keep W - rate X
     Elem type;
+    bool g_vec, m_vec;                    // G and M are aligned for 16-byte loads
     int steps;
     OrthStep step[kOrthMaxSteps + 1];     // [steps].sx: scale of the last X, unused
 };
@@ -90,6 +90,7 @@ struct NarrowLayout {
 NarrowLayout make_narrow_layout(int64_t rows, int64_t cols);
 
 struct OrthLayout {
+    int64_t tile;         // side of the tiles of B X: 64, 128 or 256
     int64_t m, n;         // shorter and longer side, padded
     int64_t rows, cols;   // padded sides in the caller's orientation
     size_t u[2], v[2];    // U and its transpose, two buffers each: high plane, low plane behind it
