@@ -122,9 +122,24 @@ __device__ inline void split(float v, f16 &h, f16 &l)
     l = f16(v - float(h));
 }
 
-// U / (|U| + eps) in planes, in both orientations, zeros in the padding; low_t: the transposed low plane has a reader
-template <typename E>
-__global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, OrthLayout L, int norm_blocks, bool low_t)
+// The low plane of single products keeps 8 bits: x - h in 1/256 of h's unit in the last place.  a X wants no more
+// (19 bits together), and it is a quarter less to move.
+__device__ inline int low_scale(f16 h) // 33 - the exponent that the unit counts from
+{
+    const int e = int(__builtin_bit_cast(uint16_t, h) >> 10) & 31;
+    return 33 - (e > 1 ? e : 1);
+}
+__device__ inline int8_t pack_low(float x, f16 h)
+{
+    const float q = rintf(ldexpf(x - float(h), low_scale(h)));
+    return int8_t(fminf(fmaxf(q, -128.0f), 127.0f));
+}
+__device__ inline float unpack_low(int8_t q, f16 h) { return float(h) + ldexpf(float(q), -low_scale(h)); }
+typedef signed char byte8 __attribute__((ext_vector_type(8)));
+
+// U / (|U| + eps) in planes, in both orientations, zeros in the padding
+template <typename E, bool kSplit>
+__global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, OrthLayout L, int norm_blocks)
 {
     __shared__ float s_t[kT][kT + 1];
     const int64_t z = blockIdx.z, r0 = int64_t(blockIdx.y) * kT, c0 = int64_t(blockIdx.x) * kT;
@@ -151,7 +166,9 @@ __global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, 
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         const int row = threadIdx.x / 8 + 32 * s;
+        const int64_t at = (r0 + row) * L.cols + c0 + piece;
         half8 h, l;
+        byte8 q;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float x = float(double(v[s][e]) * scale);
@@ -159,10 +176,14 @@ __global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, 
             split(x, xh, xl);
             h[e] = xh;
             l[e] = xl;
+            if constexpr (!kSplit) q[e] = pack_low(x, xh);
             s_t[row][piece + e] = x;
         }
-        *reinterpret_cast<half8 *>(uh + (r0 + row) * L.cols + c0 + piece) = h;
-        *reinterpret_cast<half8 *>(ul + (r0 + row) * L.cols + c0 + piece) = l;
+        *reinterpret_cast<half8 *>(uh + at) = h;
+        if constexpr (kSplit)
+            *reinterpret_cast<half8 *>(ul + at) = l;
+        else
+            *reinterpret_cast<byte8 *>(reinterpret_cast<int8_t *>(ul) + at) = q;
     }
     __syncthreads();
 #pragma unroll
@@ -177,7 +198,7 @@ __global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, 
             l[e] = xl;
         }
         *reinterpret_cast<half8 *>(vh + (c0 + col) * L.rows + r0 + piece) = h;
-        if (low_t) *reinterpret_cast<half8 *>(vl + (c0 + col) * L.rows + r0 + piece) = l;
+        if constexpr (kSplit) *reinterpret_cast<half8 *>(vl + (c0 + col) * L.rows + r0 + piece) = l;
     }
 }
 
@@ -186,30 +207,21 @@ enum class Prod { kGram, kPoly, kApply, kLast };
 
 // A block makes a kM x kN tile of C = P Q^T, P and Q row-major with K values a row, by kWm x kWn waves.  Slices of
 // 64 values a row (128 bytes) go through a ring of kStages buffers in LDS, filled by loads that write LDS directly,
-// kStages - 1 slices ahead.  A row's eight 16-byte pieces are stored in an order that depends on the row (piece c of
-// row r in place c ^ (r % 8)), so that the lanes of a fragment read, which take the same piece of 32 rows, fall on
-// different banks.
+// kStages slices ahead.  A row's eight 16-byte pieces are stored in an order that depends on the row (piece c of
+// row r in place c ^ (r % 8)), so that the lanes of a fragment read, which take the same piece of 16 rows, fall on
+// different banks.  Tiles may hang over the padded sides: their loads repeat the last row, nothing is stored there.
 constexpr int kK = 64;
+typedef float float4v __attribute__((ext_vector_type(4)));
 template <int M, int N, int Wm, int Wn, int Stages> struct Tile {
     static constexpr int kM = M, kN = N, kWm = Wm, kWn = Wn, kStages = Stages;
     static constexpr int kWaves = Wm * Wn, kThreads = kWaves * kWave;
-    static constexpr int kI = M / Wm / 32, kJ = N / Wn / 32; // 32 x 32 blocks of a wave
+    static constexpr int kI = M / Wm / 16, kJ = N / Wn / 16;   // 16 x 16 blocks of a wave
+    static constexpr int kGroups = (M + N) / 8;                // groups of 8 rows in a stage and plane, P's first
+    static constexpr int kEach = kGroups / kWaves;             // groups a wave loads
+    static constexpr int kHigh = kI % 3 == 0 ? 3 : kI % 2 == 0 ? 2 : 1; // blocks down a patch of the output
+    static constexpr int kPatch = 16 * kJ + 1;                 // its row in LDS, floats
+    static_assert(kGroups % kWaves == 0 && M % (16 * Wm) == 0 && N % (16 * Wn) == 0, "even shares");
 };
-
-// rows of one plane, kRows / 8 groups of eight dealt to the waves
-template <typename T, int kRows> __device__ inline void stage(const f16 *src, int64_t ld, f16 *dst)
-{
-    static_assert(kRows / 8 % T::kWaves == 0, "every wave loads as much");
-    const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id();
-    const int r = lane / 8, piece = (lane % 8) ^ r;
-#pragma unroll
-    for (int k = 0; k < kRows / 8 / T::kWaves; ++k) {
-        const int row = (k * T::kWaves + w) * 8;
-        __builtin_amdgcn_global_load_lds(
-            (const __attribute__((address_space(1))) void *)(src + (row + r) * ld + piece * 8),
-            (__attribute__((address_space(3))) void *)(dst + row * kK), 16, 0, 0);
-    }
-}
 
 __device__ inline half8 fragment(const f16 *tile, int row, int piece)
 {
@@ -223,15 +235,13 @@ __device__ inline int xcd_tile(int b, int blocks)
     return x * q + (x < r ? x : r) + b / 8;
 }
 
-constexpr int kPatch = 33; // row of a wave's 32 x 32 patch in LDS, floats
-
 template <typename T, bool kSplit, Prod kProd>
 __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, char *ws, OrthLayout L, int k)
 {
     constexpr int kPlanes = kSplit ? 2 : 1;
-    constexpr int kP = T::kM * kK, kQ = T::kN * kK;        // values of a staged plane
-    constexpr int kStage = kPlanes * (kP + kQ);
-    constexpr int kLoads = kPlanes * (T::kM + T::kN) / 8 / T::kWaves; // of a wave and stage
+    constexpr int kPlane = (T::kM + T::kN) * kK;           // values of a staged plane: P's rows, then Q's
+    constexpr int kLoads = kPlanes * T::kEach;             // of a wave and stage
+    constexpr bool kSymmetric = kProd == Prod::kGram || kProd == Prod::kPoly;
     extern __shared__ __align__(16) char s_mem[];
     f16 *ring = reinterpret_cast<f16 *>(s_mem);
     const OrthStep &S = a.step[k];
@@ -242,91 +252,114 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, c
     f16 *A = reinterpret_cast<f16 *>(base + L.a), *B = reinterpret_cast<f16 *>(base + L.b);
     int bi, bj;
     const f16 *P, *Q;
-    int64_t K, p_plane, q_plane;
+    int64_t p_plane, q_plane;
+    int K;
     const int t = xcd_tile(blockIdx.x, gridDim.x);
-    if constexpr (kProd == Prod::kGram || kProd == Prod::kPoly) {
+    if constexpr (kSymmetric) {
         // tiles on and below the diagonal, row by row
         bi = int((sqrtf(8.0f * float(t) + 1.0f) - 1.0f) * 0.5f);
         while ((bi + 1) * (bi + 2) / 2 <= t) ++bi;
         while (bi * (bi + 1) / 2 > t) --bi;
         bj = t - bi * (bi + 1) / 2;
-        if constexpr (kProd == Prod::kGram) {
-            P = Q = wide ? U : V;
-            K = L.n;
-            p_plane = q_plane = plane;
-        } else {
-            P = Q = A;
-            K = L.m;
-            p_plane = q_plane = square;
-        }
+        P = Q = kProd == Prod::kGram ? (wide ? U : V) : A;
+        K = int(kProd == Prod::kGram ? L.n : L.m);
+        p_plane = q_plane = kProd == Prod::kGram ? plane : square;
     } else {
         // four rows of tiles at a time, column by column
-        const int across = int(L.cols) / T::kN, down = int(L.rows) / T::kM;
+        const int across = (int(L.cols) + T::kN - 1) / T::kN, down = (int(L.rows) + T::kM - 1) / T::kM;
         const int group = t / (4 * across), top = group * 4, high = down - top < 4 ? down - top : 4;
         const int in = t - group * 4 * across;
         bi = top + in % high;
         bj = in / high;
-        K = L.m;
         P = wide ? B : U;
         Q = wide ? V : B;
+        K = int(L.m);
         p_plane = wide ? square : plane;
         q_plane = wide ? plane : square;
     }
-    P += int64_t(bi) * T::kM * K;
-    Q += int64_t(bj) * T::kN * K;
+    const int p_rows = int(kSymmetric ? L.m : L.rows), q_rows = int(kSymmetric ? L.m : L.cols);
     const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id();
-    const int wi = w / T::kWn * (T::kI * 32), wj = w % T::kWn * (T::kJ * 32);
 
-    const int slices = int(K / kK);
+    // this lane's piece of each group of eight rows that the wave loads
+    const f16 *src[kLoads];
+#pragma unroll
+    for (int e = 0; e < T::kEach; ++e) {
+        const int row = (e * T::kWaves + w) * 8 + lane / 8;
+        const bool in_p = (e * T::kWaves + w) * 8 < T::kM;
+        int at = in_p ? bi * T::kM + row : bj * T::kN + row - T::kM;
+        const int most = (in_p ? p_rows : q_rows) - 1;
+        at = at < most ? at : most;
+        src[e] = (in_p ? P : Q) + int64_t(at) * K + ((lane % 8) ^ (lane / 8)) * 8;
+        if constexpr (kSplit) src[T::kEach + e] = src[e] + (in_p ? p_plane : q_plane);
+    }
+    const int slices = K / kK;
     const auto fetch = [&](int slice) {
         // past the end the last slice again, into a buffer that nobody reads: every wait counts alike
         const int64_t k0 = int64_t(slice < slices ? slice : slices - 1) * kK;
-        f16 *to = ring + slice % T::kStages * kStage;
-        stage<T, T::kM>(P + k0, K, to);
-        stage<T, T::kN>(Q + k0, K, to + kPlanes * kP);
-        if constexpr (kSplit) {
-            stage<T, T::kM>(P + p_plane + k0, K, to + kP);
-            stage<T, T::kN>(Q + q_plane + k0, K, to + kPlanes * kP + kQ);
+        f16 *to = ring + slice % T::kStages * (kPlanes * kPlane);
+#pragma unroll
+        for (int h = 0; h < kPlanes; ++h)
+#pragma unroll
+            for (int e = 0; e < T::kEach; ++e)
+                __builtin_amdgcn_global_load_lds(
+                    (const __attribute__((address_space(1))) void *)(src[h * T::kEach + e] + k0),
+                    (__attribute__((address_space(3))) void *)(to + h * kPlane + (e * T::kWaves + w) * 8 * kK), 16, 0, 0);
+    };
+    const int wi = w / T::kWn * (T::kI * 16), wj = w % T::kWn * (T::kJ * 16);
+    // Two sets of fragments: one half of a slice is multiplied while the other is read.  In the middle of a slice both
+    // of its halves have been read, by every wave after the barrier, so its buffer is filled again there, and the next
+    // slice, which has landed, is read from there on.
+    float4v acc[T::kI][T::kJ] = {};
+    half8 p[2][kPlanes][T::kI], q[2][kPlanes][T::kJ];
+    const auto read = [&](int slice, int half) {
+        const f16 *in = ring + slice % T::kStages * (kPlanes * kPlane);
+        const int piece = half * 4 + lane / 16;
+#pragma unroll
+        for (int h = 0; h < kPlanes; ++h) {
+#pragma unroll
+            for (int i = 0; i < T::kI; ++i) p[half][h][i] = fragment(in + h * kPlane, wi + 16 * i + lane % 16, piece);
+#pragma unroll
+            for (int j = 0; j < T::kJ; ++j)
+                q[half][h][j] = fragment(in + h * kPlane + T::kM * kK, wj + 16 * j + lane % 16, piece);
         }
     };
-    float16v acc[T::kI][T::kJ] = {};
+    const auto multiply = [&](int half) {
 #pragma unroll
-    for (int p = 0; p < T::kStages - 1; ++p) fetch(p);
-    for (int slice = 0; slice < slices; ++slice) {
-        // this wave's loads of the slice have landed, then everybody's; and everybody has read the slice before
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((T::kStages - 2) * kLoads) : "memory");
-        fetch(slice + T::kStages - 1);
-        const f16 *in = ring + slice % T::kStages * kStage;
+        for (int i = 0; i < T::kI; ++i)
 #pragma unroll
-        for (int kk = 0; kk < kK / 16; ++kk) {
-            const int piece = kk * 2 + lane / 32;
-            half8 p[kPlanes][T::kI], q[kPlanes][T::kJ];
-#pragma unroll
-            for (int h = 0; h < kPlanes; ++h) {
-#pragma unroll
-                for (int i = 0; i < T::kI; ++i) p[h][i] = fragment(in + h * kP, wi + 32 * i + lane % 32, piece);
-#pragma unroll
-                for (int j = 0; j < T::kJ; ++j) q[h][j] = fragment(in + kPlanes * kP + h * kQ, wj + 32 * j + lane % 32, piece);
-            }
-#pragma unroll
-            for (int i = 0; i < T::kI; ++i)
-#pragma unroll
-                for (int j = 0; j < T::kJ; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[0][i], q[0][j], acc[i][j], 0, 0, 0);
-                    if constexpr (kSplit) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[0][i], q[1][j], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[1][i], q[0][j], acc[i][j], 0, 0, 0);
-                    }
+            for (int j = 0; j < T::kJ; ++j) {
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[half][0][i], q[half][0][j], acc[i][j], 0, 0, 0);
+                if constexpr (kSplit) {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[half][0][i], q[half][1][j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[half][1][i], q[half][0][j], acc[i][j], 0, 0, 0);
                 }
-        }
+            }
+    };
+#pragma unroll
+    for (int e = 0; e < T::kStages; ++e) fetch(e);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((T::kStages - 1) * kLoads) : "memory");
+    read(0, 0);
+    for (int slice = 0; slice < slices; ++slice) {
+        read(slice, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(0);
+        __builtin_amdgcn_sched_barrier(0);
+        // this wave's loads of the next slice have landed and its reads of this one are done; then everybody's
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((T::kStages - 2) * kLoads) : "memory");
+        fetch(slice + T::kStages);
+        read(slice + 1, 0); // behind the last slice: a buffer of repeated loads, not used
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(1);
+        __builtin_amdgcn_sched_barrier(0);
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); // the ring is free
 
     // Each wave puts its blocks through a patch of its own in LDS, for rows of 16 bytes in either orientation
-    float *patch = reinterpret_cast<float *>(s_mem) + w * 32 * kPatch;
+    constexpr int kDown = 16 * T::kHigh, kAcross = 16 * T::kJ;
+    float *patch = reinterpret_cast<float *>(s_mem) + w * kDown * T::kPatch;
     f16 *out = nullptr, *out_t = nullptr;
     int64_t ld = 0, ld_t = 0, out_plane = 0;
-    if constexpr (kProd == Prod::kGram || kProd == Prod::kPoly) {
+    if constexpr (kSymmetric) {
         out = out_t = kProd == Prod::kGram ? A : B;
         ld = ld_t = L.m;
         out_plane = square;
@@ -338,117 +371,182 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, c
         out_plane = plane;
     }
     const float xs = kProd == Prod::kApply ? a.step[k + 1].sx : 1.0f;
-    // what has a second reader or user: A's low plane (B's terms), X's (a X), the transposed X's in split products
-    constexpr bool kLow = kSplit || kProd != Prod::kPoly, kLowT = kSplit || kProd == Prod::kGram;
+    // single products keep a low plane for a X alone, of 8 bits
+    const int8_t *u_low = reinterpret_cast<const int8_t *>(U + plane);
 #pragma unroll
-    for (int i = 0; i < T::kI; ++i)
+    for (int i0 = 0; i0 < T::kI; i0 += T::kHigh) {
+        const int r0 = bi * T::kM + wi + 16 * i0, c0 = bj * T::kN + wj;
 #pragma unroll
-        for (int j = 0; j < T::kJ; ++j) {
-            const int64_t r0 = int64_t(bi) * T::kM + wi + 32 * i, c0 = int64_t(bj) * T::kN + wj + 32 * j;
+        for (int i = 0; i < T::kHigh; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) patch[(8 * (r / 4) + 4 * (lane / 32) + r % 4) * kPatch + lane % 32] = acc[i][j][r];
-            if constexpr (kProd == Prod::kLast) {
-                const int64_t c = c0 + lane % 32;
+            for (int j = 0; j < T::kJ; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    patch[(16 * i + 4 * (lane / 16) + r) * T::kPatch + 16 * j + lane % 16] = acc[i0 + i][j][r];
+        if constexpr (kProd == Prod::kLast) {
 #pragma unroll 4
-                for (int s = 0; s < 16; ++s) {
-                    const int64_t r = r0 + 2 * s + lane / 32;
-                    if (r >= a.rows || c >= a.cols) continue;
-                    float v = patch[(2 * s + lane / 32) * kPatch + lane % 32] * (1.0f / (S.sb * S.sx));
-                    if constexpr (!kSplit)
-                        v += (S.a / S.sx) * (float(U[r * L.cols + c]) + float(U[plane + r * L.cols + c]));
-                    const int64_t at = int64_t(blockIdx.z) * a.w_batch + r * a.w_stride + c;
-                    if (a.M) v = a.keep * load_elem(a.W, a.type, at) - a.rate * v;
-                    store_elem(a.W, a.type, at, v);
-                }
-                continue;
+            for (int s = 0; s < kDown * T::kJ / 4; ++s) {
+                // 16 values of four rows
+                const int row = s / T::kJ * 4 + lane / 16, col = s % T::kJ * 16 + lane % 16;
+                const int64_t r = r0 + row, c = c0 + col;
+                if (r >= a.rows || c >= a.cols) continue;
+                float v = patch[row * T::kPatch + col] * (1.0f / (S.sb * S.sx));
+                if constexpr (!kSplit) v += (S.a / S.sx) * unpack_low(u_low[r * L.cols + c], U[r * L.cols + c]);
+                const int64_t at = int64_t(blockIdx.z) * a.w_batch + r * a.w_stride + c;
+                if (a.M) v = a.keep * load_elem(a.W, a.type, at) - a.rate * v;
+                store_elem(a.W, a.type, at, v);
             }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const int row = (lane + 64 * s) / 4, col = lane % 4 * 8;
-                const int64_t at = (r0 + row) * ld + c0 + col;
-                float *v = patch + row * kPatch + col;
-                half8 h, l, xh, xl;
-                if constexpr (kProd == Prod::kPoly) {
-                    xh = *reinterpret_cast<const half8 *>(A + at);
-                    xl = *reinterpret_cast<const half8 *>(A + square + at);
-                } else if constexpr (kProd == Prod::kApply && !kSplit) {
-                    xh = *reinterpret_cast<const half8 *>(U + at);
-                    xl = *reinterpret_cast<const half8 *>(U + plane + at);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float x = v[e];
-                    if constexpr (kProd == Prod::kGram) {
-                        x *= S.sa / (S.sx * S.sx);
-                    } else if constexpr (kProd == Prod::kPoly) {
-                        x = (float(xh[e]) + float(xl[e])) * (S.b * S.sb / S.sa) + x * (S.c * S.sb / (S.sa * S.sa));
-                        if (kSplit && r0 + row == c0 + col + e) x += S.a * S.sb;
-                    } else {
-                        x *= xs / (S.sb * S.sx);
-                        if constexpr (!kSplit) x += (S.a * xs / S.sx) * (float(xh[e]) + float(xl[e]));
-                    }
-                    f16 vh, vl;
-                    split(x, vh, vl);
-                    h[e] = vh;
-                    l[e] = vl;
-                    v[e] = x;
-                }
-                *reinterpret_cast<half8 *>(out + at) = h;
-                if constexpr (kLow) *reinterpret_cast<half8 *>(out + out_plane + at) = l;
-            }
-            if (kProd != Prod::kApply && bi == bj) continue;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const int col = (lane + 64 * s) / 4, row = lane % 4 * 8;
-                const int64_t at = (c0 + col) * ld_t + r0 + row;
-                half8 h, l;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    f16 vh, vl;
-                    split(patch[(row + e) * kPatch + col], vh, vl);
-                    h[e] = vh;
-                    l[e] = vl;
-                }
-                *reinterpret_cast<half8 *>(out_t + at) = h;
-                if constexpr (kLowT) *reinterpret_cast<half8 *>(out_t + out_plane + at) = l;
-            }
+            continue;
         }
+        constexpr int kPieces = kDown * kAcross / 8;
+#pragma unroll
+        for (int s = 0; s < (kPieces + kWave - 1) / kWave; ++s) {
+            const int e = lane + kWave * s, row = e / (kAcross / 8), col = e % (kAcross / 8) * 8;
+            if (e >= kPieces || r0 + row >= p_rows || c0 + col >= q_rows) continue;
+            const int64_t at = (r0 + row) * ld + c0 + col;
+            float *v = patch + row * T::kPatch + col;
+            half8 h, l, xh, xl;
+            byte8 q, xq;
+            if constexpr (kProd == Prod::kPoly) {
+                xh = *reinterpret_cast<const half8 *>(A + at);
+                if constexpr (kSplit) xl = *reinterpret_cast<const half8 *>(A + square + at);
+            } else if constexpr (kProd == Prod::kApply && !kSplit) {
+                xh = *reinterpret_cast<const half8 *>(U + at);
+                xq = *reinterpret_cast<const byte8 *>(u_low + at);
+            }
+#pragma unroll
+            for (int x8 = 0; x8 < 8; ++x8) {
+                float x = v[x8];
+                if constexpr (kProd == Prod::kGram) {
+                    x *= S.sa / (S.sx * S.sx);
+                } else if constexpr (kProd == Prod::kPoly) {
+                    const float av = kSplit ? float(xh[x8]) + float(xl[x8]) : float(xh[x8]);
+                    x = av * (S.b * S.sb / S.sa) + x * (S.c * S.sb / (S.sa * S.sa));
+                    if (kSplit && r0 + row == c0 + col + x8) x += S.a * S.sb;
+                } else {
+                    x *= xs / (S.sb * S.sx);
+                    if constexpr (!kSplit) x += (S.a * xs / S.sx) * unpack_low(xq[x8], xh[x8]);
+                }
+                f16 vh, vl;
+                split(x, vh, vl);
+                h[x8] = vh;
+                l[x8] = vl;
+                if constexpr (!kSplit && kProd == Prod::kApply) q[x8] = pack_low(x, vh);
+                v[x8] = x;
+            }
+            *reinterpret_cast<half8 *>(out + at) = h;
+            if constexpr (kSplit)
+                *reinterpret_cast<half8 *>(out + out_plane + at) = l;
+            else if constexpr (kProd == Prod::kApply)
+                *reinterpret_cast<byte8 *>(reinterpret_cast<int8_t *>(out + out_plane) + at) = q;
+        }
+        if (kSymmetric && bi == bj) continue;
+#pragma unroll
+        for (int s = 0; s < (kPieces + kWave - 1) / kWave; ++s) {
+            const int e = lane + kWave * s, col = e / (kDown / 8), row = e % (kDown / 8) * 8;
+            if (e >= kPieces || r0 + row >= p_rows || c0 + col >= q_rows) continue;
+            const int64_t at = (c0 + col) * ld_t + r0 + row;
+            half8 h, l;
+#pragma unroll
+            for (int x8 = 0; x8 < 8; ++x8) {
+                f16 vh, vl;
+                split(patch[(row + x8) * T::kPatch + col], vh, vl);
+                h[x8] = vh;
+                l[x8] = vl;
+            }
+            *reinterpret_cast<half8 *>(out_t + at) = h;
+            if constexpr (kSplit) *reinterpret_cast<half8 *>(out_t + out_plane + at) = l;
+        }
+    }
 }
 
 template <typename T, bool kSplit, Prod kProd>
 void run_product(const OrthArgs &a, char *ws, const OrthLayout &L, int k, hipStream_t st)
 {
     constexpr size_t kRing = size_t(T::kStages) * (kSplit ? 2 : 1) * (T::kM + T::kN) * kK * sizeof(f16);
-    constexpr size_t kPatches = size_t(T::kWaves) * 32 * kPatch * sizeof(float);
+    constexpr size_t kPatches = size_t(T::kWaves) * 16 * T::kHigh * T::kPatch * sizeof(float);
     constexpr size_t kLds = kRing > kPatches ? kRing : kPatches;
     static_assert(kLds <= 160 * 1024, "LDS of a CU");
     uint32_t tiles;
     if constexpr (kProd == Prod::kGram || kProd == Prod::kPoly) {
         static_assert(T::kM == T::kN, "symmetric products");
-        const uint32_t mt = uint32_t(L.m / T::kM);
+        const uint32_t mt = uint32_t((L.m + T::kM - 1) / T::kM);
         tiles = mt * (mt + 1) / 2;
     } else {
-        tiles = uint32_t(L.rows / T::kM) * uint32_t(L.cols / T::kN);
+        tiles = uint32_t((L.rows + T::kM - 1) / T::kM) * uint32_t((L.cols + T::kN - 1) / T::kN);
     }
     orth_product_kernel<T, kSplit, kProd><<<dim3(tiles, 1, uint32_t(a.batch)), T::kThreads, kLds, st>>>(a, ws, L, k);
 }
 
-// TS: tiles of the symmetric products, TX: of B X
-template <typename TS, typename TX, bool kSplit> void run_steps(const OrthArgs &a, char *ws, const OrthLayout &L, hipStream_t st)
+// The tiles, each the best of several numbers of waves and buffers in the whole chain of products (whose operands come
+// from other XCDs, where a probe that repeats one product finds them in its own L2).
+using Tile32 = Tile<32, 32, 2, 2, 4>;
+using Tile64 = Tile<64, 64, 2, 4, 3>;
+using Tile64Several = Tile<64, 64, 2, 4, 2>; // less LDS: more blocks on a CU (1999 x 777 fp32: 40 us a step against 43)
+using Tile96 = Tile<96, 96, 6, 2, 3>;
+template <bool kSplit> using Tile128 = Tile<128, 128, kSplit ? 2 : 4, 4, 2>;
+using Tile192 = Tile<192, 192, 2, 4, 2>;
+using Tile256 = Tile<256, 256, 2, 4, 2>;
+
+// Which tile: the one whose busiest CU is done first.  Measured nanoseconds for a tile and slice of 64, of a CU that
+// has one tile and of one that has several, with one product of halves and with three.
+struct TileCost {
+    int side;
+    float one[2], three[2];
+};
+constexpr TileCost kTileCosts[] = {{32, {150, 100}, {190, 131}},  {64, {270, 200}, {500, 361}},
+                                   {96, {560, 500}, {900, 820}},  {128, {780, 450}, {1390, 1110}},
+                                   {192, {1045, 1045}, {0, 0}},   {256, {1705, 1705}, {0, 0}}};
+struct TileChoice {
+    int side;
+    bool several; // tiles on a CU
+};
+TileChoice tile_of(bool split, bool symmetric, int64_t rows, int64_t cols, int64_t batch)
 {
-    for (int k = 0; k < a.steps; ++k) {
-        run_product<TS, kSplit, Prod::kGram>(a, ws, L, k, st);
-        run_product<TS, kSplit, Prod::kPoly>(a, ws, L, k, st);
-        if (k + 1 < a.steps)
-            run_product<TX, kSplit, Prod::kApply>(a, ws, L, k, st);
-        else
-            run_product<TX, kSplit, Prod::kLast>(a, ws, L, k, st);
+    TileChoice best = {0, false};
+    float least = 0.0f;
+    for (const TileCost &c : kTileCosts) {
+        const float *ns = split ? c.three : c.one;
+        if (ns[0] == 0.0f) continue; // does not fit LDS
+        const int64_t down = (rows + c.side - 1) / c.side, across = (cols + c.side - 1) / c.side;
+        const int64_t tiles = batch * (symmetric ? down * (down + 1) / 2 : down * across);
+        const int64_t each = (tiles + kCus - 1) / kCus;
+        const float cost = each <= 1 ? ns[0] : float(each) * ns[1];
+        if (best.side == 0 || cost < least) {
+            best = {c.side, each > 1};
+            least = cost;
+        }
     }
+    return best;
 }
 
-using Tile64 = Tile<64, 64, 2, 2, 4>;    // 4 waves, 32 x 32 each
-using Tile128 = Tile<128, 128, 2, 2, 2>; // 4 waves, 64 x 64
-using Tile256 = Tile<256, 256, 2, 4, 2>; // 8 waves, 128 x 64
+template <bool kSplit, Prod kProd>
+void run_tile(TileChoice choice, const OrthArgs &a, char *ws, const OrthLayout &L, int k, hipStream_t st)
+{
+    const int tile = choice.side;
+    if (tile == 32) return run_product<Tile32, kSplit, kProd>(a, ws, L, k, st);
+    if (tile == 64 && choice.several) return run_product<Tile64Several, kSplit, kProd>(a, ws, L, k, st);
+    if (tile == 64) return run_product<Tile64, kSplit, kProd>(a, ws, L, k, st);
+    if (tile == 96) return run_product<Tile96, kSplit, kProd>(a, ws, L, k, st);
+    if constexpr (!kSplit) {
+        if (tile == 192) return run_product<Tile192, kSplit, kProd>(a, ws, L, k, st);
+        if (tile == 256) return run_product<Tile256, kSplit, kProd>(a, ws, L, k, st);
+    }
+    run_product<Tile128<kSplit>, kSplit, kProd>(a, ws, L, k, st);
+}
+
+template <bool kSplit> void run_steps(const OrthArgs &a, char *ws, const OrthLayout &L, hipStream_t st)
+{
+    const TileChoice square = tile_of(kSplit, true, L.m, L.m, a.batch), full = tile_of(kSplit, false, L.rows, L.cols, a.batch);
+    for (int k = 0; k < a.steps; ++k) {
+        run_tile<kSplit, Prod::kGram>(square, a, ws, L, k, st);
+        run_tile<kSplit, Prod::kPoly>(square, a, ws, L, k, st);
+        if (k + 1 < a.steps)
+            run_tile<kSplit, Prod::kApply>(full, a, ws, L, k, st);
+        else
+            run_tile<kSplit, Prod::kLast>(full, a, ws, L, k, st);
+    }
+}
 
 // ------------------------------------------------------------------ narrow matrices
 // At most 64 directions (m <= 64).  X lives in LDS, as fp16 halves and in both orientations: rows of X for the
@@ -859,10 +957,7 @@ NarrowLayout make_narrow_layout(int64_t rows, int64_t cols)
 OrthLayout make_orth_layout(int64_t rows, int64_t cols)
 {
     OrthLayout L;
-    // the largest tile that still gives the chip a tile of B X for each CU
-    const auto tiles = [&](int64_t t) { return ((rows + t - 1) / t) * ((cols + t - 1) / t); };
-    L.tile = tiles(256) >= kCus ? 256 : tiles(128) >= kCus ? 128 : 64;
-    const auto pad = [&](int64_t x) { return (x + L.tile - 1) / L.tile * L.tile; };
+    const auto pad = [&](int64_t x) { return (x + kK - 1) / kK * kK; }; // every row is whole slices
     L.rows = pad(rows);
     L.cols = pad(cols);
     L.m = L.rows < L.cols ? L.rows : L.cols;
@@ -892,6 +987,16 @@ size_t orth_workspace(int64_t rows, int64_t cols)
 
 namespace {
 
+template <typename E, bool kSplit> void run_wide(const OrthArgs &a, char *ws, hipStream_t st)
+{
+    const OrthLayout L = make_orth_layout(a.rows, a.cols);
+    const int norm_blocks = norm_blocks_of(a.rows, a.cols);
+    orth_norm_kernel<E><<<dim3(norm_blocks, uint32_t(a.batch)), 256, 0, st>>>(a, ws, int64_t(L.stride), L.norm);
+    orth_planes_kernel<E, kSplit><<<dim3(uint32_t(L.cols / kT), uint32_t(L.rows / kT), uint32_t(a.batch)), 256, 0, st>>>(
+        a, ws, L, norm_blocks);
+    run_steps<kSplit>(a, ws, L, st);
+}
+
 template <typename E> void run_type(const OrthArgs &a, char *ws, hipStream_t st)
 {
     if (orth_narrow(a.rows, a.cols)) {
@@ -902,18 +1007,9 @@ template <typename E> void run_type(const OrthArgs &a, char *ws, hipStream_t st)
             run_narrow<E, 2>(a, ws, L, st);
         return;
     }
-    constexpr bool kSplit = !std::is_same<E, bf16>::value;
-    const OrthLayout L = make_orth_layout(a.rows, a.cols);
-    const int norm_blocks = norm_blocks_of(a.rows, a.cols);
-    orth_norm_kernel<E><<<dim3(norm_blocks, uint32_t(a.batch)), 256, 0, st>>>(a, ws, int64_t(L.stride), L.norm);
-    orth_planes_kernel<E><<<dim3(uint32_t(L.cols / kT), uint32_t(L.rows / kT), uint32_t(a.batch)), 256, 0, st>>>(
-        a, ws, L, norm_blocks, kSplit);
-    if (L.tile == 64)
-        run_steps<Tile64, Tile64, kSplit>(a, ws, L, st);
-    else if (kSplit || L.tile == 128)
-        run_steps<Tile128, Tile128, kSplit>(a, ws, L, st);
-    else if constexpr (!kSplit)
-        run_steps<Tile128, Tile256, kSplit>(a, ws, L, st);
+    if constexpr (std::is_same<E, bf16>::value)
+        if (orth_single(a.type, a.rows, a.cols)) return run_wide<E, false>(a, ws, st);
+    run_wide<E, true>(a, ws, st);
 }
 
 // rows and matrices start on 16 bytes

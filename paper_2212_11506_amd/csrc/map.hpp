@@ -70,8 +70,15 @@ struct OrthArgs {
 
 // Outputs of 8 bits (bf16) take one product of the high halves, finer ones three.
 // A direction's error is then up to 4e-3 where a + b + c cancels (the largest
-// singular values); it counts 1 / sqrt(m) in a matrix of m directions, so narrow
-// matrices take three for every type.
+// singular values); it counts 1 / sqrt(m) in a matrix of m directions, so matrices
+// of few directions, whose products are bound by latency, take three for every type
+// (gaussian values at m = 65: 2.2e-3 before the rounding to bf16, whose own is 1.7e-3;
+// at m = 512 1.5e-3).
+constexpr int64_t kOrthSingle = 256;
+inline bool orth_single(Elem type, int64_t rows, int64_t cols)
+{
+    return type == Elem::kBF16 && (rows < cols ? rows : cols) > kOrthSingle;
+}
 constexpr int64_t kNarrow = 64;             // directions of a narrow matrix
 constexpr int64_t kNarrowWhole = 64 * 256;  // values (padded) of one that a block holds whole, in 128 KB of LDS
 inline bool orth_narrow(int64_t rows, int64_t cols) { return (rows < cols ? rows : cols) <= kNarrow; }
@@ -90,7 +97,6 @@ struct NarrowLayout {
 NarrowLayout make_narrow_layout(int64_t rows, int64_t cols);
 
 struct OrthLayout {
-    int64_t tile;         // side of the tiles of B X: 64, 128 or 256
     int64_t m, n;         // shorter and longer side, padded
     int64_t rows, cols;   // padded sides in the caller's orientation
     size_t u[2], v[2];    // U and its transpose, two buffers each: high plane, low plane behind it

@@ -64,6 +64,30 @@ def test_shapes(shape, dtype):
     assert rel(O, plain(G)) <= TOL[dtype]
 
 
+def plain_there(G, steps=5, eps=1e-7):
+    """plain() of one matrix on the GPU: 64-bit products are the library's."""
+    tall = G.shape[0] > G.shape[1]
+    X = (G.t() if tall else G).double().contiguous()
+    X = X / (X.norm() + eps)
+    a, b, c = COEF
+    for _ in range(steps):
+        A = X @ X.t().contiguous()
+        X = a * X + (b * A + c * (A @ A)) @ X
+    return (X.t() if tall else X).cpu()
+
+
+# large enough for each of the larger tiles, with ends inside them
+@pytest.mark.parametrize("shape,dtype", [((1999, 777), torch.float32), ((777, 1999), torch.float16), ((2100, 2048), torch.float32),
+                                         ((1300, 2500), torch.bfloat16), ((2500, 2200), torch.bfloat16),
+                                         ((3000, 2900), torch.float32), ((4000, 4160), torch.bfloat16), ((900, 6000), torch.bfloat16)])
+def test_large(shape, dtype):
+    say(f"[orth] {shape} {dtype}")
+    G = gauss(*shape, seed=11, dtype=dtype)
+    r = rel(bh.orthogonalise(G), plain_there(G))
+    say(f"[orth] {r:.2e}")
+    assert r <= TOL[dtype]
+
+
 # few directions: X in one block up to its LDS, then cut into slices, few and many; one value over each end
 NARROW = [(64, 256), (64, 257), (32, 512), (32, 513), (33, 256), (257, 64), (5, 1000), (1500, 40), (33, 2048), (33, 2049), (64, 5000),
           (9000, 20), (1, 65536)]
