@@ -549,378 +549,322 @@ template <bool kSplit> void run_steps(const OrthArgs &a, char *ws, const OrthLay
 }
 
 // ------------------------------------------------------------------ narrow matrices
-// At most 64 directions (m <= 64).  X lives in LDS, as fp16 halves and in both orientations: rows of X for the
-// Gram matrix (the sum runs along n), rows of X^T for B X (along m).  A matrix whose X fits one block's LDS takes
-// one launch for everything: all steps between two reads and one write.  A longer one is cut into slices of
-// kSlice columns, a block each, and takes one launch a step: every block adds up the slices' Gram matrices (or
-// reads their sum, made by a launch of its own, where slices are many), forms B = a I + b A + c A^2 itself, applies
-// it to its slice and leaves the new X's partial Gram matrix for the next launch.  The sums are in a fixed order.
-constexpr int kNarrowBlock = 512; // 8 waves
-constexpr int kSlice = 128;
-constexpr int kSliceSum = 16;     // slices whose Gram matrices every block adds up itself
+// At most 64 directions (m <= 64).  Every step is a polynomial of A = X X^T, m x m, and these commute: with
+// B = a I + b A + c A^2 the product of the steps is Q <- B Q, and the next A is B A B.  So U is read for one Gram
+// matrix, the steps run on m x m matrices in one block's LDS, and Q is applied to U once: n enters twice, not
+// 3 steps times.  In fewer than 64 bits A would lose the small singular values (their squares against the largest's;
+// 1e-4 with 32); in fp64 on the matrix cores the result is off by its own rounding alone, and |U|^2 is A's trace.
+// One launch where one block is quick with all of it; else one for the slices' Gram matrices and one in which every
+// block adds them up in a fixed order, repeats the steps and applies Q to its columns.
 
-typedef f16 half4 __attribute__((ext_vector_type(4)));
+typedef double double4v __attribute__((ext_vector_type(4)));
 
-// place of 8-value piece p of row r in planes of ld values a row (32 or a multiple of 64): the same piece of
-// consecutive rows on different banks
-__device__ inline int piece_at(int r, int p, int ld)
-{
-    return r * ld + ((ld == 32 ? p ^ ((r >> 2) & 3) : p ^ (r & 7)) * 8);
-}
+// A tile of 16 x 16: lane l holds rows l / 16 + 4 r of column l % 16
+__device__ inline int tile_row(int r) { return lane_id() / 16 + 4 * r; }
+__device__ inline int tile_col() { return lane_id() % 16; }
 
-struct Planes {
-    f16 *h, *l;
-    int ld;
-    __device__ half8 high(int r, int p) const { return *reinterpret_cast<const half8 *>(h + piece_at(r, p, ld)); }
-    __device__ half8 low(int r, int p) const { return *reinterpret_cast<const half8 *>(l + piece_at(r, p, ld)); }
-    __device__ int at(int r, int c) const { return piece_at(r, c / 8, ld) + c % 8; }
+constexpr int narrow_waves(int tiles) { return tiles > 2 ? 16 : 8; }
+
+// Tiles on and below the diagonal, in order of rows
+template <int MT> struct Lower {
+    static constexpr int kTiles = MT * (MT + 1) / 2;
+    static constexpr int kParts = narrow_waves(MT) / kTiles; // waves that share the sum of a tile of the Gram matrix
+    __device__ static int row(int t) { return t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3; }
+    __device__ static int col(int t) { return t - row(t) * (row(t) + 1) / 2; }
 };
 
-// acc += P Q^T over the kSpan values from k0 of 32 rows from pr and 32 from qr
-template <int kSpan>
-__device__ inline float16v block_product(const Planes &P, int pr, const Planes &Q, int qr, int k0, float16v acc)
+enum class Narrow { kWhole, kGram, kApply };
+
+template <int MT> constexpr int narrow_matrix() { return 16 * MT * (16 * MT + 2); } // doubles: 16 rows apart on all banks
+template <int MT, Narrow kMode> constexpr size_t narrow_lds(int width)
 {
-    const int lane = lane_id(), r = lane % 32;
-    float16v mixed = {};
-#pragma unroll
-    for (int kk = 0; kk < kSpan / 16; ++kk) {
-        const int k = k0 / 8 + 2 * kk + lane / 32;
-        const half8 ph = P.high(pr + r, k), pl = P.low(pr + r, k), qh = Q.high(qr + r, k), ql = Q.low(qr + r, k);
-        mixed = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, mixed, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc, 0, 0, 0);
-        mixed = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, mixed, 0, 0, 0);
-    }
-    return acc + mixed;
+    const size_t scratch = size_t(Lower<MT>::kParts - 1) * Lower<MT>::kTiles * 256, three = 3 * narrow_matrix<MT>();
+    const size_t doubles = kMode == Narrow::kGram ? scratch : three > scratch ? three : scratch;
+    return size_t(16 * MT) * (width + 4) * sizeof(float) + doubles * sizeof(double);
 }
 
-// row of accumulator value 4 q, of which the next three follow (columns: lane % 32)
-__device__ inline int acc_row(int q) { return 8 * q + 4 * (lane_id() / 32); }
-
-// four values of an accumulator as halves
-__device__ inline void split4(const float *v, half4 &h, half4 &l)
+template <typename E, int MT, Narrow kMode>
+__global__ __launch_bounds__(narrow_waves(MT) *kWave) void orth_narrow_kernel(OrthArgs a, char *ws, NarrowLayout L, int width, int shift)
 {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        f16 vh, vl;
-        split(v[r], vh, vl);
-        h[r] = vh;
-        l[r] = vl;
-    }
-}
-
-// kAll: one block a matrix, every step.  Otherwise launch `k`: 0 loads U's slice and leaves its Gram matrix, k > 0
-// makes step k - 1.  summed: the Gram matrices have been added up.
-template <typename E, int MB, bool kAll>
-__global__ __launch_bounds__(kNarrowBlock) void orth_narrow_kernel(OrthArgs a, char *ws, NarrowLayout L, int k, int summed)
-{
-    constexpr int kM = 32 * MB;
-    constexpr int kGroups = kAll ? int(kNarrowWhole / kM / 64) : kSlice / 64; // 64 columns each, W / 64 of them in use
-    constexpr int kPer = kM * 64 / kNarrowBlock;                             // values of a group and thread
+    constexpr int kNarrowWaves = narrow_waves(MT), kNarrowBlock = kNarrowWaves * kWave;
+    constexpr int kM = 16 * MT, kLd = kM + 2, kTiles = Lower<MT>::kTiles, kParts = Lower<MT>::kParts;
     extern __shared__ __align__(16) char s_mem[];
-    __shared__ double s_norm[kNarrowBlock / kWave];
-    const int W = L.width;
-    f16 *mem = reinterpret_cast<f16 *>(s_mem);
-    const Planes X = {mem, mem + kM * W, W};
-    const Planes T = {mem + 2 * kM * W, mem + 3 * kM * W, kM};
-    const Planes A = {mem + 4 * kM * W, mem + 4 * kM * W + kM * kM, kM};
-    float4 *scratch = reinterpret_cast<float4 *>(A.h); // partial products, before A's planes take the place
-    const int tid = threadIdx.x, lane = lane_id(), w = tid / kWave;
+    __shared__ double s_sum[kNarrowWaves];
+    float *U = reinterpret_cast<float *>(s_mem); // [kM][width + 4]: 16 rows by 4 columns on different banks
+    const int ld_u = width + 4;
+    double *mats = reinterpret_cast<double *>(U + kM * ld_u);
+    double *A = mats, *B = A + narrow_matrix<MT>(), *Q = B + narrow_matrix<MT>();
+    const int tid = threadIdx.x, lane = lane_id(), w = int(uniform(tid / kWave));
     const bool wide = a.rows <= a.cols;
     const int m = int(wide ? a.rows : a.cols);
-    const int64_t n = wide ? a.cols : a.rows;
-    const int64_t z = blockIdx.y, j0 = int64_t(blockIdx.x) * W;
-    char *base = ws + z * L.stride;
-    const int64_t g_i = wide ? a.g_stride : 1, g_j = wide ? 1 : a.g_stride; // steps along m and along n
-    const int64_t m_i = wide ? a.m_stride : 1, m_j = wide ? 1 : a.m_stride;
-    const int64_t w_i = wide ? a.w_stride : 1, w_j = wide ? 1 : a.w_stride;
-    const int cols = int(n - j0 < W ? n - j0 : W);
+    const int64_t n = wide ? a.cols : a.rows, z = blockIdx.y;
+    double *partial = reinterpret_cast<double *>(ws + z * L.stride);
 
-    if (kAll || k == 0) {
-        // U in registers, between one read and the scaled planes
-        float u[kGroups * kPer];
-        // value q of group g is at (ti + q di, tj + q dj + 64 g): along the rows of the caller's matrix
-        const int ti = wide ? tid / 64 : tid % kM, tj = wide ? tid % 64 : tid / kM;
-        const int di = wide ? kNarrowBlock / 64 : 0, dj = wide ? 0 : kNarrowBlock / kM;
-        const auto place = [&](int g, int q, int &i, int &j) {
-            i = ti + q * di;
-            j = tj + q * dj + 64 * g;
-        };
-        const E *G = static_cast<const E *>(a.G) + z * a.g_batch + j0 * g_j + (ti * g_i + tj * g_j);
-        float *M = a.M ? a.M + z * a.m_batch + j0 * m_j + (ti * m_i + tj * m_j) : nullptr;
+    // columns j0 .. of U into LDS, zeros around them; the momentum is updated where U is read first
+    const auto load = [&](int64_t j0) {
+        const int64_t g_i = wide ? a.g_stride : 1, g_j = wide ? 1 : a.g_stride; // steps along m and along n
+        const int64_t m_i = wide ? a.m_stride : 1, m_j = wide ? 1 : a.m_stride;
+        const E *G = static_cast<const E *>(a.G) + z * a.g_batch + j0 * g_j;
+        float *M = a.M ? a.M + z * a.m_batch + j0 * m_j : nullptr;
+        const int cols = int(n - j0 < width ? n - j0 : width);
+        constexpr int kAtOnce = MT == 2 ? 16 : 8;
+        for (int e0 = tid; e0 < kM * width; e0 += kAtOnce * kNarrowBlock) {
+            float g[kAtOnce], mo[kAtOnce];
+            int i[kAtOnce], j[kAtOnce];
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g)
-#pragma unroll
-            for (int q = 0; q < kPer; ++q) {
-                int i, j;
-                place(g, q, i, j);
-                u[g * kPer + q] = i < m && j < cols ? float(G[q * (di * g_i + dj * g_j) + g * (64 * g_j)]) : 0.0f;
+            for (int q = 0; q < kAtOnce; ++q) {
+                const int e = e0 + q * kNarrowBlock;
+                i[q] = wide ? e >> shift : e % kM;
+                j[q] = wide ? e & (width - 1) : e / kM;
+                g[q] = i[q] < m && j[q] < cols ? float(G[i[q] * g_i + j[q] * g_j]) : 0.0f;
             }
-        if (M) {
+            if (M) {
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-                float mo[kPer];
+                for (int q = 0; q < kAtOnce; ++q) mo[q] = i[q] < m && j[q] < cols ? M[i[q] * m_i + j[q] * m_j] : 0.0f;
+            }
 #pragma unroll
-                for (int q = 0; q < kPer; ++q) {
-                    int i, j;
-                    place(g, q, i, j);
-                    mo[q] = i < m && j < cols ? M[q * (di * m_i + dj * m_j) + g * (64 * m_j)] : 0.0f;
+            for (int q = 0; q < kAtOnce; ++q) {
+                if (M && kMode != Narrow::kApply) {
+                    mo[q] = a.momentum * mo[q] + g[q];
+                    if (i[q] < m && j[q] < cols) M[i[q] * m_i + j[q] * m_j] = mo[q];
                 }
-#pragma unroll
-                for (int q = 0; q < kPer; ++q) {
-                    int i, j;
-                    place(g, q, i, j);
-                    if constexpr (kAll) {
-                        mo[q] = a.momentum * mo[q] + u[g * kPer + q];
-                        if (i < m && j < cols) M[q * (di * m_i + dj * m_j) + g * (64 * m_j)] = mo[q];
-                    } // else a launch before has done so
-                    u[g * kPer + q] = update_value(a, u[g * kPer + q], mo[q]);
-                }
+                if (e0 + q * kNarrowBlock < kM * width) U[i[q] * ld_u + j[q]] = M ? update_value(a, g[q], mo[q]) : g[q];
             }
         }
-        // the norm: of this block's values, or of the partial sums that a launch before left
-        double sum = 0.0;
-        if constexpr (kAll) {
+    };
+
+    double scale = 0.0; // 1 / (|U| + eps)
+    if constexpr (kMode != Narrow::kApply) {
+        // the Gram matrix's lower tiles, a wave each, or several that share its columns
+        double4v acc = {};
+        const int t = w % kTiles, part = w / kTiles;
+        const int ti = 16 * Lower<MT>::row(t), tj = 16 * Lower<MT>::col(t);
+        for (int64_t j0 = int64_t(blockIdx.x) * width; j0 < n; j0 += int64_t(gridDim.x) * width) {
+            load(j0);
+            __syncthreads();
+            const int cols = int(n - j0 < width ? n - j0 : width);
+            constexpr int kDeep = 8; // 32 columns at a time
+            for (int k0 = 4 * kDeep * part; part < kParts && k0 < cols; k0 += 4 * kDeep * kParts) {
+                float x[kDeep], y[kDeep];
 #pragma unroll
-            for (int q = 0; q < kGroups * kPer; ++q) sum += double(u[q]) * double(u[q]);
-        } else {
-            const double *part = reinterpret_cast<const double *>(base + L.norm);
-            if (tid < L.norm_blocks) sum = part[tid]; // kOrthNormBlocks at most
+                for (int k = 0; k < kDeep; ++k) {
+                    x[k] = U[(ti + lane % 16) * ld_u + k0 + 4 * k + lane / 16];
+                    y[k] = U[(tj + lane % 16) * ld_u + k0 + 4 * k + lane / 16];
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int k = 0; k < kDeep; ++k) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(double(x[k]), double(y[k]), acc, 0, 0, 0);
+            }
+            if constexpr (kMode == Narrow::kGram) __syncthreads();
         }
-        sum = wave_sum(sum);
-        if (lane == 0) s_norm[w] = sum;
+        if constexpr (kParts > 1) {
+            if (part > 0 && part < kParts) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) mats[((part - 1) * kTiles + t) * 256 + r * kWave + lane] = acc[r];
+            }
+            __syncthreads();
+            if (part == 0) {
+#pragma unroll
+                for (int q = 0; q + 1 < kParts; ++q)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[r] += mats[(q * kTiles + t) * 256 + r * kWave + lane];
+            }
+        }
+        if constexpr (kMode == Narrow::kGram) {
+            if (part == 0) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) partial[int64_t(blockIdx.x) * (kTiles * 256) + t * 256 + r * kWave + lane] = acc[r];
+            }
+            return;
+        }
+        double trace = 0.0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (part == 0 && ti + tile_row(r) == tj + tile_col()) trace += acc[r];
+        trace = wave_sum(trace);
+        if (lane == 0) s_sum[w] = trace;
+        __syncthreads(); // mats is free too
+        trace = 0.0;
+        for (int q = 0; q < kTiles; ++q) trace += s_sum[q];
+        scale = 1.0 / (sqrt(trace) + a.eps);
+        if (part == 0) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = ti + tile_row(r), col = tj + tile_col();
+                A[row * kLd + col] = A[col * kLd + row] = acc[r] * (scale * scale);
+            }
+        }
         __syncthreads();
-        sum = 0.0;
-        for (int v = 0; v < kNarrowBlock / kWave; ++v) sum += s_norm[v];
-        const double scale = double(a.step[0].sx) / (sqrt(sum) + a.eps);
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            if (g * 64 >= W) break;
-#pragma unroll
-            for (int q = 0; q < kPer; ++q) {
-                int i, j;
-                place(g, q, i, j);
-                f16 h, l;
-                split(float(double(u[g * kPer + q]) * scale), h, l);
-                X.h[X.at(i, j)] = T.h[T.at(j, i)] = h;
-                X.l[X.at(i, j)] = T.l[T.at(j, i)] = l;
-            }
-        }
     } else {
-        const half8 *planes = reinterpret_cast<const half8 *>(base + L.x) + j0 * (kM / 8);
+        constexpr int kPer = (kTiles * 256 + kNarrowBlock - 1) / kNarrowBlock;
+        double v[kPer] = {}, trace = 0.0;
+        load(int64_t(blockIdx.x) * width); // on its way with the Gram matrices
+#pragma unroll 8
+        for (int q = 0; q < L.slices; ++q)
 #pragma unroll
-        for (int q = 0; q < kSlice * (kM / 8) / kNarrowBlock; ++q) {
-            const int e = tid + q * kNarrowBlock, j = e / (kM / 8), p = e % (kM / 8);
-            *reinterpret_cast<half8 *>(T.h + piece_at(j, p, kM)) = planes[e];
-            *reinterpret_cast<half8 *>(T.l + piece_at(j, p, kM)) = planes[L.n * (kM / 8) + e];
+            for (int p = 0; p < kPer; ++p)
+                if (tid + p * kNarrowBlock < kTiles * 256) v[p] += partial[int64_t(q) * (kTiles * 256) + tid + p * kNarrowBlock];
+        // value e: tile e / 256, row of the tile (e / 64 % 4) and lane e % 64
+        const auto place = [&](int e, int &row, int &col) {
+            const int t = e / 256;
+            row = 16 * Lower<MT>::row(t) + lane / 16 + 4 * (e / kWave % 4);
+            col = 16 * Lower<MT>::col(t) + lane % 16;
+        };
+#pragma unroll
+        for (int p = 0; p < kPer; ++p) {
+            int row, col;
+            place(tid + p * kNarrowBlock, row, col);
+            if (tid + p * kNarrowBlock < kTiles * 256 && row == col) trace += v[p];
         }
+        trace = wave_sum(trace);
+        if (lane == 0) s_sum[w] = trace;
+        __syncthreads();
+        trace = 0.0;
+        for (int q = 0; q < kNarrowWaves; ++q) trace += s_sum[q];
+        scale = 1.0 / (sqrt(trace) + a.eps);
+#pragma unroll
+        for (int p = 0; p < kPer; ++p) {
+            int row, col;
+            place(tid + p * kNarrowBlock, row, col);
+            if (tid + p * kNarrowBlock < kTiles * 256) A[row * kLd + col] = A[col * kLd + row] = v[p] * (scale * scale);
+        }
+        __syncthreads();
     }
-    __syncthreads();
 
-    const int first = kAll ? 0 : (k == 0 ? 0 : k - 1), last = kAll ? a.steps : (k == 0 ? 0 : k);
-    constexpr int kBlocks = MB * MB;             // 32 x 32 blocks of A
-    constexpr int kParts = MB == 1 ? 4 : 2;      // waves that share one block's sum
-    const int ib = (w % kBlocks) / MB * 32, jb = (w % kBlocks) % MB * 32, part = w / kBlocks;
-    const bool worker = part < kParts;
-
-    // the Gram matrix of X as it is in LDS, the block (ib, jb) in waves below kBlocks
-    const auto gram = [&]() {
-        float16v acc = {};
-        if (worker)
-            for (int k0 = part * 32; k0 < W; k0 += kParts * 32) acc = block_product<32>(X, ib, X, jb, k0, acc);
-        if (worker && part > 0) {
+    // Lower tile t of a product of symmetric matrices, of which rows serve for columns
+    const auto product = [&](const double *P, const double *R, int t) {
+        const double *p = P + (16 * Lower<MT>::row(t) + lane % 16) * kLd + lane / 16;
+        const double *q = R + (16 * Lower<MT>::col(t) + lane % 16) * kLd + lane / 16;
+        // every operand is asked for before the first is used: a chain of products waits for LDS once
+        double x[kM / 4], y[kM / 4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                scratch[(((part - 1) * kBlocks + w % kBlocks) * 4 + q) * kWave + lane] =
-                    make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
+        for (int k = 0; k < kM / 4; ++k) {
+            x[k] = p[4 * k];
+            y[k] = q[4 * k];
         }
-        __syncthreads();
-        if (w < kBlocks) {
+        __builtin_amdgcn_sched_barrier(0);
+        double4v acc = {};
 #pragma unroll
-            for (int p = 0; p + 1 < kParts; ++p)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float4 v = scratch[((p * kBlocks + w) * 4 + q) * kWave + lane];
-                    acc[4 * q] += v.x;
-                    acc[4 * q + 1] += v.y;
-                    acc[4 * q + 2] += v.z;
-                    acc[4 * q + 3] += v.w;
-                }
-        }
-        __syncthreads();
+        for (int k = 0; k < kM / 4; ++k) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(x[k], y[k], acc, 0, 0, 0);
         return acc;
     };
-    // partial Gram matrices keep the accumulators' own order: [block][4][64 lanes][4]
-    const auto partials = [&](int which) { return reinterpret_cast<float4 *>(base + L.gram[which & 1]); };
-
-    for (int s = first; s < last; ++s) {
+    const auto store = [&](double *P, int t, const double4v &v) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = 16 * Lower<MT>::row(t) + tile_row(r), col = 16 * Lower<MT>::col(t) + tile_col();
+            P[row * kLd + col] = P[col * kLd + row] = v[r];
+        }
+    };
+    constexpr int kOne = (kTiles + kNarrowWaves - 1) / kNarrowWaves, kTwo = (2 * kTiles + kNarrowWaves - 1) / kNarrowWaves;
+    for (int s = 0; s < a.steps; ++s) {
         const OrthStep &S = a.step[s];
-        const float to_a = S.sa / (S.sx * S.sx);
-        // A, then B in its place.  Both are symmetric: the value at (row, column) is stored at (column, row),
-        // where four rows of an accumulator lie side by side
-        const int c = jb + lane % 32;
-        if constexpr (kAll) {
-            const float16v acc = gram();
-            if (w < kBlocks) {
+        const bool last = s + 1 == a.steps;
+        // B = a I + b A + c A^2, and the first Q
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float v[4];
+        for (int q = 0; q < kOne; ++q) {
+            const int t = w + q * kNarrowWaves;
+            if (t >= kTiles) continue;
+            double4v v = product(A, A, t);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) v[r] = acc[4 * q + r] * to_a;
-                    half4 h, l;
-                    split4(v, h, l);
-                    *reinterpret_cast<half4 *>(A.h + A.at(c, ib + acc_row(q))) = h;
-                    *reinterpret_cast<half4 *>(A.l + A.at(c, ib + acc_row(q))) = l;
-                }
+            for (int r = 0; r < 4; ++r) {
+                const int row = 16 * Lower<MT>::row(t) + tile_row(r), col = 16 * Lower<MT>::col(t) + tile_col();
+                v[r] = double(S.b) * A[row * kLd + col] + double(S.c) * v[r] + (row == col ? double(S.a) : 0.0);
             }
-        } else {
-            // every thread adds up four values at a time over the slices
-            const float4 *src = summed ? reinterpret_cast<const float4 *>(base + L.total) : partials(k - 1);
-            const int count = summed ? 1 : L.slices;
-            for (int e = tid; e < kM * kM / 4; e += kNarrowBlock) {
-                float v[4] = {};
-#pragma unroll 8
-                for (int q = 0; q < count; ++q) {
-                    const float4 x = src[q * (kM * kM / 4) + e];
-                    v[0] += x.x;
-                    v[1] += x.y;
-                    v[2] += x.z;
-                    v[3] += x.w;
-                }
-                const int b = e / 256, q = e / 64 % 4, ln = e % 64;
-                const int row = (b % MB) * 32 + ln % 32, col = (b / MB) * 32 + 8 * q + 4 * (ln / 32);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] *= to_a;
-                half4 h, l;
-                split4(v, h, l);
-                *reinterpret_cast<half4 *>(A.h + A.at(row, col)) = h;
-                *reinterpret_cast<half4 *>(A.l + A.at(row, col)) = l;
-            }
+            store(B, t, v);
+            if (s == 0) store(Q, t, v);
         }
         __syncthreads();
-        half4 bh[4], bl[4];
-        if (w < kBlocks) {
-            const float16v sq = block_product<kM>(A, ib, A, jb, 0, float16v{});
+        // B Q and A B at once, each in its factor's place when everybody has read it
+        double4v v[kTwo];
+        const int items = (last ? 0 : kTiles) + (s == 0 ? 0 : kTiles), from = s == 0 ? kTiles : 0;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const half4 h = *reinterpret_cast<const half4 *>(A.h + A.at(c, ib + acc_row(q)));
-                const half4 l = *reinterpret_cast<const half4 *>(A.l + A.at(c, ib + acc_row(q)));
-                float v[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    v[r] = (float(h[r]) + float(l[r])) * (S.b * S.sb / S.sa) + sq[4 * q + r] * (S.c * S.sb / (S.sa * S.sa));
-                    if (ib + acc_row(q) + r == c) v[r] += S.a * S.sb;
-                }
-                split4(v, bh[q], bl[q]);
-            }
-        }
-        __syncthreads();
-        if (w < kBlocks) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                *reinterpret_cast<half4 *>(A.h + A.at(c, ib + acc_row(q))) = bh[q];
-                *reinterpret_cast<half4 *>(A.l + A.at(c, ib + acc_row(q))) = bl[q];
-            }
-        }
-        __syncthreads();
-        // X <- B X in 32 x 32 blocks, two a wave at most; in place, once every wave has read its columns
-        const bool done = s + 1 == a.steps;
-        const float xs = (done ? 1.0f : a.step[s + 1].sx) / (S.sb * S.sx);
-        const int items = W / 32 * MB;
-        float16v x[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int item = w + t * (kNarrowBlock / kWave);
-            if (item < items) x[t] = block_product<kM>(A, item % MB * 32, T, item / MB * 32, 0, float16v{});
+        for (int q = 0; q < kTwo; ++q) {
+            const int t = from + w + q * kNarrowWaves;
+            if (t < from + items) v[q] = t < kTiles ? product(B, Q, t) : product(A, B, t - kTiles);
         }
         __syncthreads();
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int item = w + t * (kNarrowBlock / kWave);
-            if (item >= items) continue;
-            const int i0 = item % MB * 32, j = item / MB * 32 + lane % 32;
-            if (done) {
-                E *out = static_cast<E *>(a.W) + z * a.w_batch + (j0 + j) * w_j;
-                float old[16];
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int i = i0 + acc_row(r / 4) + r % 4;
-                    old[r] = a.M && i < m && j < cols ? float(out[i * w_i]) : 0.0f;
-                }
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int i = i0 + acc_row(r / 4) + r % 4;
-                    const float v = x[t][r] * xs;
-                    if (i < m && j < cols) out[i * w_i] = E(a.M ? a.keep * old[r] - a.rate * v : v);
-                }
-                continue;
-            }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int i = i0 + acc_row(q);
-                float v[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = x[t][4 * q + r] * xs;
-                half4 h, l;
-                split4(v, h, l);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    X.h[X.at(i + r, j)] = h[r];
-                    X.l[X.at(i + r, j)] = l[r];
-                }
-                *reinterpret_cast<half4 *>(T.h + T.at(j, i)) = h;
-                *reinterpret_cast<half4 *>(T.l + T.at(j, i)) = l;
-            }
+        for (int q = 0; q < kTwo; ++q) {
+            const int t = from + w + q * kNarrowWaves;
+            if (t < from + items) store(t < kTiles ? Q : A, t < kTiles ? t : t - kTiles, v[q]);
         }
+        __syncthreads();
+        if (last) break;
+        // the next A = (A B) B
+#pragma unroll
+        for (int q = 0; q < kOne; ++q)
+            if (w + q * kNarrowWaves < kTiles) v[q] = product(A, B, w + q * kNarrowWaves);
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < kOne; ++q)
+            if (w + q * kNarrowWaves < kTiles) store(A, w + q * kNarrowWaves, v[q]);
         __syncthreads();
     }
-    if (kAll || k == a.steps) return;
-    const float16v acc = gram();
-    if (w < kBlocks) {
-        float4 *dst = partials(k) + int64_t(blockIdx.x) * (kM * kM / 4) + w * 4 * kWave + lane;
+
+    // X = Q U / (|U| + eps), 16 columns a wave at a time
+    const int64_t w_i = wide ? a.w_stride : 1, w_j = wide ? 1 : a.w_stride;
+    for (int64_t j0 = int64_t(blockIdx.x) * width; j0 < n; j0 += int64_t(gridDim.x) * width) {
+        if (kMode == Narrow::kApply && j0 != int64_t(blockIdx.x) * width) { // the first columns are there
+            __syncthreads();
+            load(j0);
+            __syncthreads();
+        }
+        const int cols = int(n - j0 < width ? n - j0 : width);
+        E *out = static_cast<E *>(a.W) + z * a.w_batch + j0 * w_j;
+        for (int jt = 16 * w; jt < cols; jt += 16 * kNarrowWaves) {
+            double u[kM / 4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) dst[q * kWave] = make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
-    }
-    half8 *planes = reinterpret_cast<half8 *>(base + L.x) + j0 * (kM / 8);
+            for (int k = 0; k < kM / 4; ++k) u[k] = double(U[(4 * k + lane / 16) * ld_u + jt + lane % 16]);
+            const int j = jt + lane % 16;
 #pragma unroll
-    for (int q = 0; q < kSlice * (kM / 8) / kNarrowBlock; ++q) {
-        const int e = tid + q * kNarrowBlock, j = e / (kM / 8), p = e % (kM / 8);
-        planes[e] = *reinterpret_cast<const half8 *>(T.h + piece_at(j, p, kM));
-        planes[L.n * (kM / 8) + e] = *reinterpret_cast<const half8 *>(T.l + piece_at(j, p, kM));
+            for (int i = 0; i < MT; ++i) {
+                const double *p = Q + (16 * i + lane % 16) * kLd + lane / 16;
+                double x[kM / 4];
+#pragma unroll
+                for (int k = 0; k < kM / 4; ++k) x[k] = p[4 * k];
+                __builtin_amdgcn_sched_barrier(0);
+                double4v acc = {};
+#pragma unroll
+                for (int k = 0; k < kM / 4; ++k) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(x[k], u[k], acc, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = 16 * i + tile_row(r);
+                    if (row >= m || j >= cols) continue;
+                    E *o = out + row * w_i + j * w_j;
+                    const float x = float(acc[r] * scale);
+                    *o = E(a.M ? a.keep * float(*o) - a.rate * x : x);
+                }
+            }
+        }
     }
 }
 
-// adds up the slices' Gram matrices: a block takes 64 of its values and four strands of slices
-__global__ __launch_bounds__(256) void orth_sum_kernel(char *ws, NarrowLayout L, int which, int values)
+int log2_of(int x)
 {
-    __shared__ float s_sum[4][kWave];
-    char *base = ws + int64_t(blockIdx.y) * L.stride;
-    const int v = int(blockIdx.x) * kWave + threadIdx.x % kWave, strand = threadIdx.x / kWave;
-    const float *src = reinterpret_cast<const float *>(base + L.gram[which & 1]);
-    float s = 0.0f;
-#pragma unroll 8
-    for (int q = strand; q < L.slices; q += 4) s += src[int64_t(q) * values + v];
-    s_sum[strand][threadIdx.x % kWave] = s;
-    __syncthreads();
-    if (strand == 0)
-        reinterpret_cast<float *>(base + L.total)[v] = (s_sum[0][v % kWave] + s_sum[1][v % kWave]) + (s_sum[2][v % kWave] + s_sum[3][v % kWave]);
+    int s = 0;
+    while ((1 << s) < x) ++s;
+    return s;
 }
 
-template <typename E, int MB> void run_narrow(const OrthArgs &a, char *ws, const NarrowLayout &L, hipStream_t st)
+template <typename E, int MT> void run_narrow(const OrthArgs &a, char *ws, const NarrowLayout &L, hipStream_t st)
 {
-    constexpr int kM = 32 * MB;
-    const size_t lds = size_t(kM) * L.width * 8 + (MB == 1 ? 3 * 4096 : 4 * 4096);
-    const dim3 grid(uint32_t(L.slices), uint32_t(a.batch));
-    if (L.slices == 1) {
-        orth_narrow_kernel<E, MB, true><<<grid, kNarrowBlock, lds, st>>>(a, ws, L, 0, 0);
+    constexpr int kBlock = narrow_waves(MT) * kWave;
+    const int shift = log2_of(L.width);
+    const uint32_t z = uint32_t(a.batch);
+    if (L.slices == 0) {
+        orth_narrow_kernel<E, MT, Narrow::kWhole>
+            <<<dim3(1, z), kBlock, narrow_lds<MT, Narrow::kWhole>(L.width), st>>>(a, ws, L, L.width, shift);
         return;
     }
-    orth_norm_kernel<E><<<dim3(L.norm_blocks, uint32_t(a.batch)), 256, 0, st>>>(a, ws, int64_t(L.stride), L.norm);
-    const bool sum = L.slices > kSliceSum;
-    for (int k = 0; k <= a.steps; ++k) {
-        if (k > 0 && sum) orth_sum_kernel<<<dim3(kM * kM / kWave, uint32_t(a.batch)), 256, 0, st>>>(ws, L, k - 1, kM * kM);
-        orth_narrow_kernel<E, MB, false><<<grid, kNarrowBlock, lds, st>>>(a, ws, L, k, sum);
-    }
+    orth_narrow_kernel<E, MT, Narrow::kGram>
+        <<<dim3(uint32_t(L.slices), z), kBlock, narrow_lds<MT, Narrow::kGram>(L.width), st>>>(a, ws, L, L.width, shift);
+    // each block repeats the steps: no more blocks than find a CU free
+    const int64_t n = a.rows > a.cols ? a.rows : a.cols, chunks = (n + L.width - 1) / L.width;
+    const int64_t most = a.batch < kCus ? kCus / a.batch : 1, blocks = chunks < most ? chunks : most;
+    orth_narrow_kernel<E, MT, Narrow::kApply>
+        <<<dim3(uint32_t(blocks), z), kBlock, narrow_lds<MT, Narrow::kApply>(L.width), st>>>(a, ws, L, L.width, shift);
 }
+
 } // namespace
 
 int norm_blocks_of(int64_t rows, int64_t cols)
@@ -931,26 +875,24 @@ int norm_blocks_of(int64_t rows, int64_t cols)
 
 NarrowLayout make_narrow_layout(int64_t rows, int64_t cols)
 {
+    // one block as long as its Gram matrix and its product with Q take 6 us or less, the cost of a second launch
+    static_assert(narrow_lds<1, Narrow::kWhole>(2048) <= 160 * 1024 && narrow_lds<2, Narrow::kWhole>(512) <= 160 * 1024 &&
+                      narrow_lds<3, Narrow::kWhole>(256) <= 160 * 1024 && narrow_lds<4, Narrow::kWhole>(128) <= 160 * 1024 &&
+                      narrow_lds<4, Narrow::kGram>(kNarrowSlice) <= 160 * 1024,
+                  "LDS of a CU");
+    constexpr int kWhole[4] = {2048, 512, 256, 128};
     NarrowLayout L;
     const int64_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
-    L.blocks = m <= 32 ? 1 : 2;
-    const int64_t side = 32 * L.blocks, whole = (n + 63) / 64 * 64;
-    // one launch as long as X fits LDS: 8 bytes a value
-    L.width = int(whole * side <= kNarrowWhole ? whole : kSlice);
-    L.slices = int((n + L.width - 1) / L.width);
-    L.n = int64_t(L.slices) * L.width;
-    L.norm_blocks = norm_blocks_of(rows, cols);
-    size_t at = 0;
-    const auto take = [&](size_t bytes) {
-        const size_t here = at;
-        at += (bytes + 255) / 256 * 256;
-        return here;
-    };
-    L.x = take(2 * sizeof(f16) * size_t(L.n * side));
-    for (int k = 0; k < 2; ++k) L.gram[k] = take(sizeof(float) * size_t(side * side) * size_t(L.slices));
-    L.total = take(sizeof(float) * size_t(side * side));
-    L.norm = take(sizeof(double) * kOrthNormBlocks);
-    L.stride = at;
+    L.tiles = int((m + 15) / 16);
+    L.slices = 0;
+    L.width = 64;
+    while (L.width < n && L.width < kWhole[L.tiles - 1]) L.width *= 2;
+    if (L.width < n) {
+        L.width = kNarrowSlice;
+        const int64_t chunks = (n + L.width - 1) / L.width;
+        L.slices = int(chunks < kNarrowSlices ? chunks : kNarrowSlices);
+    }
+    L.stride = size_t(L.slices > 0 ? L.slices : 1) * (L.tiles * (L.tiles + 1) / 2) * 256 * sizeof(double);
     return L;
 }
 
@@ -1001,11 +943,10 @@ template <typename E> void run_type(const OrthArgs &a, char *ws, hipStream_t st)
 {
     if (orth_narrow(a.rows, a.cols)) {
         const NarrowLayout L = make_narrow_layout(a.rows, a.cols);
-        if (L.blocks == 1)
-            run_narrow<E, 1>(a, ws, L, st);
-        else
-            run_narrow<E, 2>(a, ws, L, st);
-        return;
+        if (L.tiles == 1) return run_narrow<E, 1>(a, ws, L, st);
+        if (L.tiles == 2) return run_narrow<E, 2>(a, ws, L, st);
+        if (L.tiles == 3) return run_narrow<E, 3>(a, ws, L, st);
+        return run_narrow<E, 4>(a, ws, L, st);
     }
     if constexpr (std::is_same<E, bf16>::value)
         if (orth_single(a.type, a.rows, a.cols)) return run_wide<E, false>(a, ws, st);

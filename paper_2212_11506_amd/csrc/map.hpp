@@ -79,20 +79,16 @@ inline bool orth_single(Elem type, int64_t rows, int64_t cols)
 {
     return type == Elem::kBF16 && (rows < cols ? rows : cols) > kOrthSingle;
 }
-constexpr int64_t kNarrow = 64;             // directions of a narrow matrix
-constexpr int64_t kNarrowWhole = 64 * 256;  // values (padded) of one that a block holds whole, in 128 KB of LDS
+constexpr int64_t kNarrow = 64;    // directions of a narrow matrix, which is stepped in fp64 on its Gram matrix
+constexpr int kNarrowSlice = 128;  // columns in LDS of one that takes two launches
+constexpr int kNarrowSlices = 32;  // partial Gram matrices
 inline bool orth_narrow(int64_t rows, int64_t cols) { return (rows < cols ? rows : cols) <= kNarrow; }
 
 struct NarrowLayout {
-    int blocks;        // 32-row blocks of the shorter side
-    int width, slices; // columns of a slice, slices (1: one launch does everything)
-    int norm_blocks;   // partial sums of squares
-    int64_t n;         // longer side, padded
-    size_t x;          // X^T, planes as below
-    size_t gram[2];    // the slices' Gram matrices, of this step and of the next
-    size_t total;      // their sum
-    size_t norm;
-    size_t stride;
+    int tiles;     // 16-row tiles of the shorter side
+    int width;     // columns of U in LDS, a power of two
+    int slices;    // partial Gram matrices (0: one block, one launch)
+    size_t stride; // bytes of one matrix' workspace: the partial Gram matrices
 };
 NarrowLayout make_narrow_layout(int64_t rows, int64_t cols);
 

@@ -89,7 +89,7 @@ def test_large(shape, dtype):
 
 
 # few directions: X in one block up to its LDS, then cut into slices, few and many; one value over each end
-NARROW = [(64, 256), (64, 257), (32, 512), (32, 513), (33, 256), (257, 64), (5, 1000), (1500, 40), (33, 2048), (33, 2049), (64, 5000),
+NARROW = [(1, 2048), (16, 2049), (16, 4096), (17, 512), (17, 513), (48, 256), (49, 128), (49, 129), (4200, 64), (64, 256), (64, 257), (32, 512), (32, 513), (33, 256), (257, 64), (5, 1000), (1500, 40), (33, 2048), (33, 2049), (64, 5000),
           (9000, 20), (1, 65536)]
 
 
