@@ -8,6 +8,7 @@ fails loudly.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional
 
@@ -666,36 +667,62 @@ def debug_walk(Y: torch.Tensor, theta: float = 0.5, form: int = -1):
 
 
 # ------------------------------------------------------------------ operators of a trained map
+# Their smallest calls run a few microseconds on the GPU, so marshalling is kept short: one look at a tensor where
+# nothing is wrong, and what depends on plain numbers alone is worked out once for them.
 class _Matrices(C.Structure):
     _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("batch_stride", C.c_int64)]
 
 
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}  # BHTSNE_F32, BHTSNE_F16, BHTSNE_BF16
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(t: torch.Tensor) -> int:
+    """The current stream of t's GPU."""
+    return _raw_stream(t.get_device()) if _raw_stream else torch.cuda.current_stream(t.device).cuda_stream
 
 
 def _type(t: torch.Tensor, where: str) -> int:
-    if t.dtype not in _TYPES:
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
         raise ValueError(f"{where} must be float32, float16 or bfloat16, got {t.dtype}")
-    return _TYPES[t.dtype]
+    return kind
 
 
-def _rows(t: torch.Tensor, where: str, n: int, d: int, dtype) -> int:
-    """Checks an n x d matrix with unit stride inside a row; the stride between its rows."""
+def _refuse(t: torch.Tensor, where: str, shape, dtype):
     if not t.is_cuda:
         raise ValueError(f"{where} must be a GPU tensor")
     if t.dtype != dtype:
         raise ValueError(f"{where} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != (n, d):
-        raise ValueError(f"{where} must be {n} x {d}, got {tuple(t.shape)}")
-    if d > 1 and t.stride(1) != 1:
-        raise ValueError(f"{where} must be contiguous inside a row")
-    return t.stride(0) if n > 1 else d
+    if t.shape != shape:
+        raise ValueError(f"{where} must be {tuple(shape)}, got {tuple(t.shape)}")
+    raise ValueError(f"{where} must be contiguous inside a row")
 
 
-def _vector(t: Optional[torch.Tensor], where: str, size: int, dtype=None):
-    if t is not None and t.numel() != size:
+def _rows(t: torch.Tensor, where: str, shape, dtype) -> int:
+    """Checks a matrix with unit stride inside a row; the stride between its rows."""
+    if not (t.is_cuda and t.dtype == dtype and t.shape == shape):
+        _refuse(t, where, shape, dtype)
+    row, inside = t.stride()
+    if inside != 1 and shape[1] > 1:
+        _refuse(t, where, shape, dtype)
+    return row if shape[0] > 1 else shape[1]
+
+
+def _vector(t: Optional[torch.Tensor], where: str, size: int, dtype=None) -> Optional[int]:
+    if t is None:
+        return None
+    if t.is_cuda and t.numel() == size and t.is_contiguous() and (dtype is None or t.dtype == dtype):
+        return t.data_ptr()
+    if t.numel() != size:
         raise ValueError(f"{where} must have {size} values, got {t.numel()}")
-    return _ptr(t, dtype, where)
+    return _ptr(t, dtype, where).value
+
+
+def _workspace_bytes(t: torch.Tensor) -> int:
+    if not t.is_cuda or not t.is_contiguous():
+        _ptr(t, None, "workspace")
+    return t.numel() * t.element_size()
 
 
 def _param_type(weight, bias, dtype) -> int:
@@ -711,19 +738,23 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     lib = load_library()
     if x.dim() != 2:
         raise ValueError(f"x must be n x d, got {tuple(x.shape)}")
-    n, d = x.shape
-    y = out if out is not None else torch.empty((n, d), dtype=x.dtype, device=x.device)
-    mean = torch.empty(n, dtype=torch.float32, device=x.device)
-    rstd = torch.empty(n, dtype=torch.float32, device=x.device)
-    rc = lib.bhtsne_layer_norm(C.c_void_p(x.data_ptr()), _rows(x, "x", n, d, x.dtype), _vector(weight, "weight", d),
-                               _vector(bias, "bias", d), n, d, float(eps), _type(x, "x"),
-                               _param_type(weight, bias, x.dtype), C.c_void_p(y.data_ptr()),
-                               _rows(y, "out", n, d, x.dtype), C.c_void_p(mean.data_ptr()),
-                               C.c_void_p(rstd.data_ptr()), _stream())
-    _check(rc, "bhtsne_layer_norm")
+    shape, dtype, kind = x.shape, x.dtype, _type(x, "x")
+    n, d = shape
+    x_stride = _rows(x, "x", shape, dtype)
+    if out is None:
+        y, y_stride = x.new_empty(shape), d
+    else:
+        y, y_stride = out, _rows(out, "out", shape, dtype)
+    mean, rstd = x.new_empty((2, n), dtype=torch.float32).unbind(0)
+    rc = lib.bhtsne_layer_norm(x.data_ptr(), x_stride, _vector(weight, "weight", d), _vector(bias, "bias", d), n, d, eps,
+                               kind, _param_type(weight, bias, dtype), y.data_ptr(), y_stride, mean.data_ptr(),
+                               rstd.data_ptr(), _stream_of(x))
+    if rc:
+        _check(rc, "bhtsne_layer_norm")
     return y, mean, rstd
 
 
+@functools.lru_cache(maxsize=256)
 def layer_norm_workspace_size(n: int, d: int) -> int:
     return int(load_library().bhtsne_layer_norm_workspace_size(int(n), int(d)))
 
@@ -736,67 +767,78 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
     lib = load_library()
     if x.dim() != 2:
         raise ValueError(f"x must be n x d, got {tuple(x.shape)}")
-    n, d = x.shape
+    shape, dtype, kind = x.shape, x.dtype, _type(x, "x")
+    n, d = shape
     need = layer_norm_workspace_size(n, d)
     if need == 0:
         raise BhtsneError(BHTSNE_EINVAL, "bhtsne_layer_norm_workspace_size")
+    x_stride, dy_stride = _rows(x, "x", shape, dtype), _rows(dy, "dy", shape, dtype)
     if dx is None:
-        dx = torch.empty((n, d), dtype=x.dtype, device=x.device)
-    ws = workspace if workspace is not None else torch.empty(need, dtype=torch.uint8, device=x.device)
-    ptype = weight.dtype if weight is not None else x.dtype
-    dweight = torch.empty(d, dtype=ptype, device=x.device)
-    dbias = torch.empty(d, dtype=ptype, device=x.device)
-    rc = lib.bhtsne_layer_norm_backward(C.c_void_p(dy.data_ptr()), _rows(dy, "dy", n, d, x.dtype),
-                                        C.c_void_p(x.data_ptr()), _rows(x, "x", n, d, x.dtype),
-                                        _vector(weight, "weight", d), _vector(mean, "mean", n, torch.float32),
-                                        _vector(rstd, "rstd", n, torch.float32), n, d, _type(x, "x"),
-                                        _param_type(weight, None, x.dtype), C.c_void_p(dx.data_ptr()),
-                                        _rows(dx, "dx", n, d, x.dtype), C.c_void_p(dweight.data_ptr()),
-                                        C.c_void_p(dbias.data_ptr()), _ptr(ws, None, "workspace"),
-                                        ws.numel() * ws.element_size(), _stream())
-    _check(rc, "bhtsne_layer_norm_backward")
+        dx, dx_stride = x.new_empty(shape), d
+    else:
+        dx_stride = _rows(dx, "dx", shape, dtype)
+    if workspace is None:
+        workspace = x.new_empty(need, dtype=torch.uint8)
+    else:
+        need = _workspace_bytes(workspace)
+    ptype = weight.dtype if weight is not None else dtype
+    dweight, dbias = x.new_empty((2, d), dtype=ptype).unbind(0)
+    rc = lib.bhtsne_layer_norm_backward(dy.data_ptr(), dy_stride, x.data_ptr(), x_stride, _vector(weight, "weight", d),
+                                        _vector(mean, "mean", n, torch.float32), _vector(rstd, "rstd", n, torch.float32),
+                                        n, d, kind, _param_type(weight, None, dtype), dx.data_ptr(), dx_stride,
+                                        dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr(), need, _stream_of(x))
+    if rc:
+        _check(rc, "bhtsne_layer_norm_backward")
     return dx, dweight, dbias
 
 
 def _matrices(t: torch.Tensor, where: str, shape, dtype) -> _Matrices:
-    if not t.is_cuda:
-        raise ValueError(f"{where} must be a GPU tensor")
-    if t.dtype != dtype:
-        raise ValueError(f"{where} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{where} must be {tuple(shape)}, got {tuple(t.shape)}")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{where} must be contiguous inside a row")
-    return _Matrices(t.data_ptr(), t.stride(-2) if t.shape[-2] > 1 else t.shape[-1], t.stride(0) if t.dim() == 3 else 0)
+    if not (t.is_cuda and t.dtype == dtype and t.shape == shape):
+        _refuse(t, where, shape, dtype)
+    stride = t.stride()
+    if stride[-1] != 1 and shape[-1] > 1:
+        _refuse(t, where, shape, dtype)
+    return _Matrices(t.data_ptr(), stride[-2] if shape[-2] > 1 else shape[-1], stride[0] if len(shape) == 3 else 0)
 
 
 def _matrix_sizes(t: torch.Tensor, where: str):
-    if t.dim() not in (2, 3):
-        raise ValueError(f"{where} must be rows x cols or batch x rows x cols, got {tuple(t.shape)}")
-    return (t.shape[0] if t.dim() == 3 else 1), t.shape[-2], t.shape[-1]
+    shape = t.shape
+    if len(shape) == 2:
+        return 1, shape[0], shape[1]
+    if len(shape) == 3:
+        return tuple(shape)
+    raise ValueError(f"{where} must be rows x cols or batch x rows x cols, got {tuple(shape)}")
+
+
+@functools.lru_cache(maxsize=64)
+def _flat_coefficients(coefficients, steps: int):
+    flat = [float(v) for row in coefficients for v in (row if isinstance(row, tuple) else (row,))]
+    if len(flat) == 3:
+        flat = flat * max(1, steps)
+    if len(flat) != 3 * steps and steps > 0:
+        raise ValueError(f"coefficients must be one (a, b, c) or {steps} of them")
+    return (C.c_double * len(flat))(*flat)
 
 
 def _coefficients(coefficients, steps: int):
     """None, one (a, b, c) for every step, or one for each."""
     if coefficients is None:
         return None
-    flat = [float(v) for row in coefficients for v in (row if hasattr(row, "__len__") else (row,))]
-    if len(flat) == 3:
-        flat = flat * steps
-    if len(flat) != 3 * steps:
-        raise ValueError(f"coefficients must be one (a, b, c) or {steps} of them")
-    return (C.c_double * len(flat))(*flat)
+    return _flat_coefficients(tuple(tuple(r) if hasattr(r, "__len__") else r for r in coefficients), int(steps))
 
 
+@functools.lru_cache(maxsize=256)
 def orthogonalise_workspace_size(batch: int, rows: int, cols: int) -> int:
     return int(load_library().bhtsne_orthogonalise_workspace_size(int(batch), int(rows), int(cols)))
 
 
-def _orthogonal_workspace(sizes, device, ws):
+def _orthogonal_workspace(sizes, like, ws):
+    if ws is not None:
+        return ws, _workspace_bytes(ws)
     need = orthogonalise_workspace_size(*sizes)
     if need == 0:
         raise BhtsneError(BHTSNE_EINVAL, "bhtsne_orthogonalise_workspace_size")
-    return ws if ws is not None else torch.empty(need, dtype=torch.uint8, device=device)
+    return like.new_empty(need, dtype=torch.uint8), need
 
 
 def orthogonalise(G: torch.Tensor, steps: int = 5, coefficients=None, eps: float = 1e-7,
@@ -804,13 +846,15 @@ def orthogonalise(G: torch.Tensor, steps: int = 5, coefficients=None, eps: float
     """bhtsne_orthogonalise of G (rows x cols, or batch x rows x cols); out may be G."""
     lib = load_library()
     sizes = _matrix_sizes(G, "G")
-    kind = _type(G, "G")
-    O = out if out is not None else torch.empty(G.shape, dtype=G.dtype, device=G.device)
-    g, o = _matrices(G, "G", G.shape, G.dtype), _matrices(O, "out", G.shape, G.dtype)
-    ws = _orthogonal_workspace(sizes, G.device, workspace)
-    rc = lib.bhtsne_orthogonalise(C.byref(g), *sizes, kind, _coefficients(coefficients, steps), int(steps), float(eps),
-                                  C.byref(o), _ptr(ws, None, "workspace"), ws.numel() * ws.element_size(), _stream())
-    _check(rc, "bhtsne_orthogonalise")
+    kind, shape, dtype = _type(G, "G"), G.shape, G.dtype
+    g = _matrices(G, "G", shape, dtype)
+    O = out if out is not None else G.new_empty(shape)
+    o = _matrices(O, "out", shape, dtype)
+    ws, nbytes = _orthogonal_workspace(sizes, G, workspace)
+    rc = lib.bhtsne_orthogonalise(C.byref(g), *sizes, kind, _coefficients(coefficients, steps), steps, eps, C.byref(o),
+                                  ws.data_ptr(), nbytes, _stream_of(G))
+    if rc:
+        _check(rc, "bhtsne_orthogonalise")
     return O
 
 
@@ -821,14 +865,14 @@ def muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, learning_rate: 
     cols).  scale: None is sqrt(max(1, rows / cols))."""
     lib = load_library()
     sizes = _matrix_sizes(W, "W")
-    kind = _type(W, "W")
-    w, g = _matrices(W, "W", W.shape, W.dtype), _matrices(G, "G", W.shape, W.dtype)
-    m = _matrices(M, "M", W.shape, torch.float32)
+    kind, shape = _type(W, "W"), W.shape
+    w, g = _matrices(W, "W", shape, W.dtype), _matrices(G, "G", shape, W.dtype)
+    m = _matrices(M, "M", shape, torch.float32)
     if scale is None:
         scale = max(1.0, sizes[1] / max(1, sizes[2])) ** 0.5
-    ws = _orthogonal_workspace(sizes, W.device, workspace)
-    rc = lib.bhtsne_muon_step(C.byref(w), C.byref(g), C.byref(m), *sizes, kind, float(learning_rate), float(momentum),
-                              int(bool(nesterov)), float(weight_decay), float(scale),
-                              _coefficients(coefficients, steps), int(steps), float(eps),
-                              _ptr(ws, None, "workspace"), ws.numel() * ws.element_size(), _stream())
-    _check(rc, "bhtsne_muon_step")
+    ws, nbytes = _orthogonal_workspace(sizes, W, workspace)
+    rc = lib.bhtsne_muon_step(C.byref(w), C.byref(g), C.byref(m), *sizes, kind, learning_rate, momentum, bool(nesterov),
+                              weight_decay, scale, _coefficients(coefficients, steps), steps, eps, ws.data_ptr(), nbytes,
+                              _stream_of(W))
+    if rc:
+        _check(rc, "bhtsne_muon_step")

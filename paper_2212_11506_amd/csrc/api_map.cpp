@@ -54,7 +54,7 @@ float power_of_two_below(double x) { return float(std::exp2(std::floor(std::log2
 // them through the steps, and with them every value of X (most), of A = X X^T
 // (most^2) and of B = a I + b A + c A^2 (|a| and b t + c t^2's largest on [0, most^2]).  Half of what fp16
 // holds is kept for rounding errors' growth.
-bool plan_steps(const double *coefficients, int steps, OrthArgs *a)
+bool plan_steps(const double *coefficients, int steps, OrthSteps *plan)
 {
     constexpr double kRoom = 32768.0;
     double most = 1.0;
@@ -74,7 +74,7 @@ bool plan_steps(const double *coefficients, int steps, OrthArgs *a)
                                  (-3.0 * q[1] - std::sqrt(disc)) / (10.0 * q[2]), -q[0] / (3.0 * q[1])};
         for (double t : roots)
             if (t > 0.0 && t < t1) x = std::fmax(x, next(t));
-        OrthStep &s = a->step[k];
+        OrthStep &s = plan->step[k];
         s.a = float(q[0]);
         s.b = float(q[1]);
         s.c = float(q[2]);
@@ -84,8 +84,7 @@ bool plan_steps(const double *coefficients, int steps, OrthArgs *a)
         if (!(x < 64.0)) return false;
         most = x;
     }
-    a->step[steps].sx = power_of_two_below(kRoom / std::fmax(most, 1.0));
-    a->steps = steps;
+    plan->count = steps;
     return true;
 }
 
@@ -98,7 +97,8 @@ int orthogonal_call(OrthArgs &a, const bhtsne_matrices *G, const bhtsne_matrices
     if (!matrices_ok(G, batch, rows, cols, type) || !matrices_ok(W, batch, rows, cols, type)) return BHTSNE_EINVAL;
     if (!apart(W, batch, rows, cols)) return BHTSNE_EINVAL;
     if (steps < 1 || steps > kOrthMaxSteps || !std::isfinite(eps) || eps < 0.0) return BHTSNE_EINVAL;
-    if (!plan_steps(coefficients, steps, &a)) return BHTSNE_EINVAL;
+    OrthSteps plan;
+    if (!plan_steps(coefficients, steps, &plan)) return BHTSNE_EINVAL;
     if (!workspace_ok(workspace, workspace_bytes, need)) return BHTSNE_EWORKSPACE;
     a.G = G->data;
     a.g_stride = G->stride;
@@ -111,7 +111,7 @@ int orthogonal_call(OrthArgs &a, const bhtsne_matrices *G, const bhtsne_matrices
     a.cols = cols;
     a.type = Elem(type);
     a.eps = eps;
-    launch_orthogonalise(a, workspace, stream);
+    launch_orthogonalise(a, plan, workspace, stream);
     return hipGetLastError() == hipSuccess ? BHTSNE_OK : BHTSNE_EDEVICE;
 }
 

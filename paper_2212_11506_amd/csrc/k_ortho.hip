@@ -139,7 +139,7 @@ typedef signed char byte8 __attribute__((ext_vector_type(8)));
 
 // U / (|U| + eps) in planes, in both orientations, zeros in the padding
 template <typename E, bool kSplit>
-__global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, OrthLayout L, int norm_blocks)
+__global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, OrthLayout L, int norm_blocks, float sx)
 {
     __shared__ float s_t[kT][kT + 1];
     const int64_t z = blockIdx.z, r0 = int64_t(blockIdx.y) * kT, c0 = int64_t(blockIdx.x) * kT;
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, 
     double sq = 0.0;
     for (int k = lane_id(); k < norm_blocks; k += kWave) sq += part[k];
     sq = wave_sum(sq);
-    const double scale = double(a.step[0].sx) / (sqrt(sq) + a.eps);
+    const double scale = double(sx) / (sqrt(sq) + a.eps);
     f16 *uh = reinterpret_cast<f16 *>(base + L.u[0]), *ul = uh + L.rows * L.cols;
     f16 *vh = reinterpret_cast<f16 *>(base + L.v[0]), *vl = vh + L.rows * L.cols;
 #pragma unroll
@@ -236,7 +236,7 @@ __device__ inline int xcd_tile(int b, int blocks)
 }
 
 template <typename T, bool kSplit, Prod kProd>
-__global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, char *ws, OrthLayout L, int k)
+__global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, char *ws, OrthLayout L, int k, OrthStep S, float next_sx)
 {
     constexpr int kPlanes = kSplit ? 2 : 1;
     constexpr int kPlane = (T::kM + T::kN) * kK;           // values of a staged plane: P's rows, then Q's
@@ -244,7 +244,6 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, c
     constexpr bool kSymmetric = kProd == Prod::kGram || kProd == Prod::kPoly;
     extern __shared__ __align__(16) char s_mem[];
     f16 *ring = reinterpret_cast<f16 *>(s_mem);
-    const OrthStep &S = a.step[k];
     const bool wide = a.rows <= a.cols;
     char *base = ws + int64_t(blockIdx.z) * L.stride;
     const int64_t plane = L.rows * L.cols, square = L.m * L.m;
@@ -370,7 +369,6 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, c
         ld_t = L.rows;
         out_plane = plane;
     }
-    const float xs = kProd == Prod::kApply ? a.step[k + 1].sx : 1.0f;
     // single products keep a low plane for a X alone, of 8 bits
     const int8_t *u_low = reinterpret_cast<const int8_t *>(U + plane);
 #pragma unroll
@@ -424,8 +422,8 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, c
                     x = av * (S.b * S.sb / S.sa) + x * (S.c * S.sb / (S.sa * S.sa));
                     if (kSplit && r0 + row == c0 + col + x8) x += S.a * S.sb;
                 } else {
-                    x *= xs / (S.sb * S.sx);
-                    if constexpr (!kSplit) x += (S.a * xs / S.sx) * unpack_low(xq[x8], xh[x8]);
+                    x *= next_sx / (S.sb * S.sx);
+                    if constexpr (!kSplit) x += (S.a * next_sx / S.sx) * unpack_low(xq[x8], xh[x8]);
                 }
                 f16 vh, vl;
                 split(x, vh, vl);
@@ -461,7 +459,7 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, c
 }
 
 template <typename T, bool kSplit, Prod kProd>
-void run_product(const OrthArgs &a, char *ws, const OrthLayout &L, int k, hipStream_t st)
+void run_product(const OrthArgs &a, const OrthSteps &steps, char *ws, const OrthLayout &L, int k, hipStream_t st)
 {
     constexpr size_t kRing = size_t(T::kStages) * (kSplit ? 2 : 1) * (T::kM + T::kN) * kK * sizeof(f16);
     constexpr size_t kPatches = size_t(T::kWaves) * 16 * T::kHigh * T::kPatch * sizeof(float);
@@ -475,7 +473,8 @@ void run_product(const OrthArgs &a, char *ws, const OrthLayout &L, int k, hipStr
     } else {
         tiles = uint32_t((L.rows + T::kM - 1) / T::kM) * uint32_t((L.cols + T::kN - 1) / T::kN);
     }
-    orth_product_kernel<T, kSplit, kProd><<<dim3(tiles, 1, uint32_t(a.batch)), T::kThreads, kLds, st>>>(a, ws, L, k);
+    orth_product_kernel<T, kSplit, kProd><<<dim3(tiles, 1, uint32_t(a.batch)), T::kThreads, kLds, st>>>(
+        a, ws, L, k, steps.step[k], k + 1 < steps.count ? steps.step[k + 1].sx : 1.0f);
 }
 
 // The tiles, each the best of several numbers of waves and buffers in the whole chain of products (whose operands come
@@ -521,30 +520,31 @@ TileChoice tile_of(bool split, bool symmetric, int64_t rows, int64_t cols, int64
 }
 
 template <bool kSplit, Prod kProd>
-void run_tile(TileChoice choice, const OrthArgs &a, char *ws, const OrthLayout &L, int k, hipStream_t st)
+void run_tile(TileChoice choice, const OrthArgs &a, const OrthSteps &steps, char *ws, const OrthLayout &L, int k, hipStream_t st)
 {
     const int tile = choice.side;
-    if (tile == 32) return run_product<Tile32, kSplit, kProd>(a, ws, L, k, st);
-    if (tile == 64 && choice.several) return run_product<Tile64Several, kSplit, kProd>(a, ws, L, k, st);
-    if (tile == 64) return run_product<Tile64, kSplit, kProd>(a, ws, L, k, st);
-    if (tile == 96) return run_product<Tile96, kSplit, kProd>(a, ws, L, k, st);
+    if (tile == 32) return run_product<Tile32, kSplit, kProd>(a, steps, ws, L, k, st);
+    if (tile == 64 && choice.several) return run_product<Tile64Several, kSplit, kProd>(a, steps, ws, L, k, st);
+    if (tile == 64) return run_product<Tile64, kSplit, kProd>(a, steps, ws, L, k, st);
+    if (tile == 96) return run_product<Tile96, kSplit, kProd>(a, steps, ws, L, k, st);
     if constexpr (!kSplit) {
-        if (tile == 192) return run_product<Tile192, kSplit, kProd>(a, ws, L, k, st);
-        if (tile == 256) return run_product<Tile256, kSplit, kProd>(a, ws, L, k, st);
+        if (tile == 192) return run_product<Tile192, kSplit, kProd>(a, steps, ws, L, k, st);
+        if (tile == 256) return run_product<Tile256, kSplit, kProd>(a, steps, ws, L, k, st);
     }
-    run_product<Tile128<kSplit>, kSplit, kProd>(a, ws, L, k, st);
+    run_product<Tile128<kSplit>, kSplit, kProd>(a, steps, ws, L, k, st);
 }
 
-template <bool kSplit> void run_steps(const OrthArgs &a, char *ws, const OrthLayout &L, hipStream_t st)
+template <bool kSplit>
+void run_steps(const OrthArgs &a, const OrthSteps &steps, char *ws, const OrthLayout &L, hipStream_t st)
 {
     const TileChoice square = tile_of(kSplit, true, L.m, L.m, a.batch), full = tile_of(kSplit, false, L.rows, L.cols, a.batch);
-    for (int k = 0; k < a.steps; ++k) {
-        run_tile<kSplit, Prod::kGram>(square, a, ws, L, k, st);
-        run_tile<kSplit, Prod::kPoly>(square, a, ws, L, k, st);
-        if (k + 1 < a.steps)
-            run_tile<kSplit, Prod::kApply>(full, a, ws, L, k, st);
+    for (int k = 0; k < steps.count; ++k) {
+        run_tile<kSplit, Prod::kGram>(square, a, steps, ws, L, k, st);
+        run_tile<kSplit, Prod::kPoly>(square, a, steps, ws, L, k, st);
+        if (k + 1 < steps.count)
+            run_tile<kSplit, Prod::kApply>(full, a, steps, ws, L, k, st);
         else
-            run_tile<kSplit, Prod::kLast>(full, a, ws, L, k, st);
+            run_tile<kSplit, Prod::kLast>(full, a, steps, ws, L, k, st);
     }
 }
 
@@ -584,7 +584,7 @@ template <int MT, Narrow kMode> constexpr size_t narrow_lds(int width)
 }
 
 template <typename E, int MT, Narrow kMode>
-__global__ __launch_bounds__(narrow_waves(MT) *kWave) void orth_narrow_kernel(OrthArgs a, char *ws, NarrowLayout L, int width, int shift)
+__global__ __launch_bounds__(narrow_waves(MT) *kWave) void orth_narrow_kernel(OrthArgs a, OrthSteps steps, char *ws, NarrowLayout L, int width, int shift)
 {
     constexpr int kNarrowWaves = narrow_waves(MT), kNarrowBlock = kNarrowWaves * kWave;
     constexpr int kM = 16 * MT, kLd = kM + 2, kTiles = Lower<MT>::kTiles, kParts = Lower<MT>::kParts;
@@ -756,9 +756,9 @@ __global__ __launch_bounds__(narrow_waves(MT) *kWave) void orth_narrow_kernel(Or
         }
     };
     constexpr int kOne = (kTiles + kNarrowWaves - 1) / kNarrowWaves, kTwo = (2 * kTiles + kNarrowWaves - 1) / kNarrowWaves;
-    for (int s = 0; s < a.steps; ++s) {
-        const OrthStep &S = a.step[s];
-        const bool last = s + 1 == a.steps;
+    for (int s = 0; s < steps.count; ++s) {
+        const OrthStep &S = steps.step[s];
+        const bool last = s + 1 == steps.count;
         // B = a I + b A + c A^2, and the first Q
 #pragma unroll
         for (int q = 0; q < kOne; ++q) {
@@ -846,23 +846,23 @@ int log2_of(int x)
     return s;
 }
 
-template <typename E, int MT> void run_narrow(const OrthArgs &a, char *ws, const NarrowLayout &L, hipStream_t st)
+template <typename E, int MT> void run_narrow(const OrthArgs &a, const OrthSteps &steps, char *ws, const NarrowLayout &L, hipStream_t st)
 {
     constexpr int kBlock = narrow_waves(MT) * kWave;
     const int shift = log2_of(L.width);
     const uint32_t z = uint32_t(a.batch);
     if (L.slices == 0) {
         orth_narrow_kernel<E, MT, Narrow::kWhole>
-            <<<dim3(1, z), kBlock, narrow_lds<MT, Narrow::kWhole>(L.width), st>>>(a, ws, L, L.width, shift);
+            <<<dim3(1, z), kBlock, narrow_lds<MT, Narrow::kWhole>(L.width), st>>>(a, steps, ws, L, L.width, shift);
         return;
     }
     orth_narrow_kernel<E, MT, Narrow::kGram>
-        <<<dim3(uint32_t(L.slices), z), kBlock, narrow_lds<MT, Narrow::kGram>(L.width), st>>>(a, ws, L, L.width, shift);
+        <<<dim3(uint32_t(L.slices), z), kBlock, narrow_lds<MT, Narrow::kGram>(L.width), st>>>(a, steps, ws, L, L.width, shift);
     // each block repeats the steps: no more blocks than find a CU free
     const int64_t n = a.rows > a.cols ? a.rows : a.cols, chunks = (n + L.width - 1) / L.width;
     const int64_t most = a.batch < kCus ? kCus / a.batch : 1, blocks = chunks < most ? chunks : most;
     orth_narrow_kernel<E, MT, Narrow::kApply>
-        <<<dim3(uint32_t(blocks), z), kBlock, narrow_lds<MT, Narrow::kApply>(L.width), st>>>(a, ws, L, L.width, shift);
+        <<<dim3(uint32_t(blocks), z), kBlock, narrow_lds<MT, Narrow::kApply>(L.width), st>>>(a, steps, ws, L, L.width, shift);
 }
 
 } // namespace
@@ -929,28 +929,28 @@ size_t orth_workspace(int64_t rows, int64_t cols)
 
 namespace {
 
-template <typename E, bool kSplit> void run_wide(const OrthArgs &a, char *ws, hipStream_t st)
+template <typename E, bool kSplit> void run_wide(const OrthArgs &a, const OrthSteps &steps, char *ws, hipStream_t st)
 {
     const OrthLayout L = make_orth_layout(a.rows, a.cols);
     const int norm_blocks = norm_blocks_of(a.rows, a.cols);
     orth_norm_kernel<E><<<dim3(norm_blocks, uint32_t(a.batch)), 256, 0, st>>>(a, ws, int64_t(L.stride), L.norm);
     orth_planes_kernel<E, kSplit><<<dim3(uint32_t(L.cols / kT), uint32_t(L.rows / kT), uint32_t(a.batch)), 256, 0, st>>>(
-        a, ws, L, norm_blocks);
-    run_steps<kSplit>(a, ws, L, st);
+        a, ws, L, norm_blocks, steps.step[0].sx);
+    run_steps<kSplit>(a, steps, ws, L, st);
 }
 
-template <typename E> void run_type(const OrthArgs &a, char *ws, hipStream_t st)
+template <typename E> void run_type(const OrthArgs &a, const OrthSteps &steps, char *ws, hipStream_t st)
 {
     if (orth_narrow(a.rows, a.cols)) {
         const NarrowLayout L = make_narrow_layout(a.rows, a.cols);
-        if (L.tiles == 1) return run_narrow<E, 1>(a, ws, L, st);
-        if (L.tiles == 2) return run_narrow<E, 2>(a, ws, L, st);
-        if (L.tiles == 3) return run_narrow<E, 3>(a, ws, L, st);
-        return run_narrow<E, 4>(a, ws, L, st);
+        if (L.tiles == 1) return run_narrow<E, 1>(a, steps, ws, L, st);
+        if (L.tiles == 2) return run_narrow<E, 2>(a, steps, ws, L, st);
+        if (L.tiles == 3) return run_narrow<E, 3>(a, steps, ws, L, st);
+        return run_narrow<E, 4>(a, steps, ws, L, st);
     }
     if constexpr (std::is_same<E, bf16>::value)
-        if (orth_single(a.type, a.rows, a.cols)) return run_wide<E, false>(a, ws, st);
-    run_wide<E, true>(a, ws, st);
+        if (orth_single(a.type, a.rows, a.cols)) return run_wide<E, false>(a, steps, ws, st);
+    run_wide<E, true>(a, steps, ws, st);
 }
 
 // rows and matrices start on 16 bytes
@@ -961,7 +961,7 @@ bool vectors(const void *p, int64_t stride, int64_t batch_stride, int64_t batch,
 
 } // namespace
 
-void launch_orthogonalise(const OrthArgs &args, void *workspace, hipStream_t st)
+void launch_orthogonalise(const OrthArgs &args, const OrthSteps &steps, void *workspace, hipStream_t st)
 {
     if (args.batch == 0) return;
     OrthArgs a = args;
@@ -969,11 +969,11 @@ void launch_orthogonalise(const OrthArgs &args, void *workspace, hipStream_t st)
     a.m_vec = vectors(a.M, a.m_stride, a.m_batch, a.batch, 4);
     char *ws = static_cast<char *>(workspace);
     if (a.type == Elem::kF32)
-        run_type<float>(a, ws, st);
+        run_type<float>(a, steps, ws, st);
     else if (a.type == Elem::kF16)
-        run_type<f16>(a, ws, st);
+        run_type<f16>(a, steps, ws, st);
     else
-        run_type<bf16>(a, ws, st);
+        run_type<bf16>(a, steps, ws, st);
 }
 
 } // namespace bht

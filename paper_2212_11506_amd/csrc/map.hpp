@@ -64,8 +64,11 @@ struct OrthArgs {
     float momentum, nesterov, keep, rate; // W <- keep W - rate X
     Elem type;
     bool g_vec, m_vec;                    // G and M are aligned for 16-byte loads
-    int steps;
-    OrthStep step[kOrthMaxSteps + 1];     // [steps].sx: scale of the last X, unused
+};
+
+struct OrthSteps {
+    int count;
+    OrthStep step[kOrthMaxSteps];
 };
 
 // Outputs of 8 bits (bf16) take one product of the high halves, finer ones three.
@@ -102,6 +105,6 @@ struct OrthLayout {
 };
 OrthLayout make_orth_layout(int64_t rows, int64_t cols);
 size_t orth_workspace(int64_t rows, int64_t cols); // bytes for one matrix
-void launch_orthogonalise(const OrthArgs &a, void *ws, hipStream_t st);
+void launch_orthogonalise(const OrthArgs &a, const OrthSteps &steps, void *ws, hipStream_t st);
 
 } // namespace bht
