@@ -31,20 +31,54 @@ template <typename E, int VEC> __device__ inline void store_pack(E *p, const Pac
     *reinterpret_cast<Pack<E, VEC> *>(p) = v;
 }
 
-__device__ inline float load_param(const void *p, Elem t, int64_t i)
+// Weights and their gradients are fp32, or of 16 bits of either kind.  Which is the same for the whole launch, and is
+// asked outside of whatever depends on the lane: kWide, in code of its own; the two kinds of 16 bits by a selection.
+// (Nested in a lane's condition, such branches have cost an address register its value on one of the paths.)
+template <bool kWide> struct Params {
+    const void *p;
+    bool half; // fp16 rather than bf16
+    __device__ float at(int64_t i) const
+    {
+        if constexpr (kWide) return static_cast<const float *>(p)[i];
+        const uint16_t raw = static_cast<const uint16_t *>(p)[i];
+        const float h = float(__builtin_bit_cast(f16, raw)), b = __uint_as_float(uint32_t(raw) << 16);
+        return half ? h : b;
+    }
+};
+template <bool kWide> __device__ inline void store_param(void *p, Elem t, int64_t i, float v)
 {
-    if (t == Elem::kF32) return static_cast<const float *>(p)[i];
-    if (t == Elem::kF16) return float(static_cast<const f16 *>(p)[i]);
-    return float(static_cast<const bf16 *>(p)[i]);
-}
-__device__ inline void store_param(void *p, Elem t, int64_t i, float v)
-{
-    if (t == Elem::kF32)
+    if constexpr (kWide) {
         static_cast<float *>(p)[i] = v;
-    else if (t == Elem::kF16)
-        static_cast<f16 *>(p)[i] = f16(v);
+    } else {
+        const uint16_t h = __builtin_bit_cast(uint16_t, f16(v)), b = __builtin_bit_cast(uint16_t, bf16(v));
+        static_cast<uint16_t *>(p)[i] = t == Elem::kF16 ? h : b;
+    }
+}
+
+// The parameters of a lane's features, `fill` without parameters and behind the last feature, where the last one is read
+template <bool kWide, int VEC, int NV>
+__device__ inline void load_params(const void *p, Elem t, int team, int lane, int d, float fill, float (&out)[NV * VEC])
+{
+    const Params<kWide> from = {p, t == Elem::kF16};
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const int c = (k * team + lane) * VEC + j;
+            const float v = from.at(c < d ? c : d - 1);
+            out[k * VEC + j] = c < d ? v : fill;
+        }
+}
+template <int VEC, int NV>
+__device__ inline void read_params(const void *p, Elem t, int team, int lane, int d, float fill, float (&out)[NV * VEC])
+{
+#pragma unroll
+    for (int i = 0; i < NV * VEC; ++i) out[i] = fill;
+    if (!p) return;
+    if (t == Elem::kF32)
+        load_params<true, VEC, NV>(p, t, team, lane, d, fill, out);
     else
-        static_cast<bf16 *>(p)[i] = bf16(v);
+        load_params<false, VEC, NV>(p, t, team, lane, d, fill, out);
 }
 
 // v of the lane at the other end of a fixed permutation within 16 lanes
@@ -52,6 +86,9 @@ template <int kCtrl> __device__ inline float dpp(float v)
 {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kCtrl, 0xF, 0xF, true));
 }
+
+// what a swap of lane groups leaves in its two registers: each group's value in both groups
+template <typename V> __device__ inline float both(V r) { return __uint_as_float(r[0]) + __uint_as_float(r[1]); }
 
 // Sum over aligned teams of `team` lanes (a power of two up to 64), in every
 // lane.  Once all lanes of an aligned half hold that half's sum, any lane of
@@ -62,9 +99,25 @@ __device__ inline float team_sum(float v, int team)
     if (team > 2) v += dpp<0x4E>(v);  // quad_perm 2,3,0,1
     if (team > 4) v += dpp<0x141>(v); // row_half_mirror
     if (team > 8) v += dpp<0x140>(v); // row_mirror
-    if (team > 16) v += __shfl_xor(v, 16, kWave);
-    if (team > 32) v += __shfl_xor(v, 32, kWave);
+    if (team > 16) v = both(__builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+    if (team > 32) v = both(__builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
     return v;
+}
+
+// s / count with inv = 1 / count: a product put right by its remainder, as exact as the division and a third of it
+__device__ inline float share(float s, float count, float inv)
+{
+    const float q = s * inv;
+    const float r = fmaf(-q, count, s);
+    return fabsf(q) < __FLT_MAX__ ? fmaf(r, inv, q) : q; // an infinite quotient has no remainder
+}
+
+// x^(-1/2), the approximation put right once
+__device__ inline float inverse_root(float x)
+{
+    const float r = rsqrtf(x);
+    const float e = fmaf(-x * r, r, 1.0f);
+    return r > 0.0f && r < __FLT_MAX__ ? fmaf(0.5f * r, e, r) : r;
 }
 
 // Sum over the team of a row: lanes of a wave (team <= 64), or the whole block.
@@ -80,6 +133,14 @@ __device__ inline float row_sum(float v, int team, float *red)
     return s;
 }
 
+// The vectors of a lane: the k-th starts at feature (k team + lane) VEC.  All but the last few are full for every
+// lane, which is known without looking at the lanes.
+template <int VEC> struct Columns {
+    int team, lane, d;
+    __device__ int at(int k) const { return (k * team + lane) * VEC; }
+    __device__ bool has(int k) const { return (k + 1) * team * VEC <= d || at(k) < d; }
+};
+
 // ------------------------------------------------------------------ forward
 template <typename E, int VEC, int NV>
 __global__ __launch_bounds__(kNormMaxThreads) void norm_kernel(NormArgs a, int team)
@@ -89,29 +150,24 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_kernel(NormArgs a, int t
     const int lane = team <= kWave ? sub : threadIdx.x; // ... or in the block
     const int rows = team <= kWave ? int(blockDim.x) / team : 1;
     const int mine = team <= kWave ? int(threadIdx.x) / team : 0;
-    const E *x = static_cast<const E *>(a.x);
-    E *y = static_cast<E *>(a.out);
     const int d = int(a.d);
-    const float count = float(d);
+    const float count = float(d), inv = 1.0f / count, eps = float(a.eps);
+    const Columns<VEC> cols = {team, lane, d};
 
-    int col[NV];
     float w[NV * VEC], b[NV * VEC];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        col[k] = (k * team + lane) * VEC;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            const int c = col[k] + j;
-            w[k * VEC + j] = c < d && a.weight ? load_param(a.weight, a.param, c) : 1.0f;
-            b[k * VEC + j] = c < d && a.bias ? load_param(a.bias, a.param, c) : 0.0f;
-        }
-    }
+    read_params<VEC, NV>(a.weight, a.param, team, lane, d, 1.0f, w);
+    read_params<VEC, NV>(a.bias, a.param, team, lane, d, 0.0f, b);
     const int64_t step = int64_t(gridDim.x) * rows;
     int64_t row = int64_t(blockIdx.x) * rows + mine;
-    Pack<E, VEC> next[NV];
+    const E *x = static_cast<const E *>(a.x) + row * a.x_stride + lane * VEC;
+    E *y = static_cast<E *>(a.out) + row * a.out_stride + lane * VEC;
+    Pack<E, VEC> next[NV] = {};
+    const auto load = [&]() {
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-        if (row < a.n && col[k] < d) next[k] = load_pack<E, VEC>(x + row * a.x_stride + col[k]);
+        for (int k = 0; k < NV; ++k)
+            if (cols.has(k)) next[k] = load_pack<E, VEC>(x + k * team * VEC);
+    };
+    if (row < a.n) load();
 
     // every lane of a block makes the same number of rounds
     for (int64_t first = int64_t(blockIdx.x) * rows; first < a.n; first += step, row += step) {
@@ -121,45 +177,49 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_kernel(NormArgs a, int t
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                v[k * VEC + j] = row < a.n && col[k] < d ? float(next[k].v[j]) : 0.0f;
+                v[k * VEC + j] = float(next[k].v[j]); // zero where there are no features
                 sum += v[k * VEC + j];
             }
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (row + step < a.n && col[k] < d) next[k] = load_pack<E, VEC>(x + (row + step) * a.x_stride + col[k]);
-        const float mean = row_sum(sum, team, s_red[0]) / count;
+        x += step * a.x_stride;
+        if (first + step + rows <= a.n || row + step < a.n) load();
+        const float mean = share(row_sum(sum, team, s_red[0]), count, inv);
         float sq = 0.0f;
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
+        for (int k = 0; k < NV; ++k) {
+            float part = 0.0f;
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 v[k * VEC + j] -= mean;
-                if (col[k] < d) sq += v[k * VEC + j] * v[k * VEC + j];
+                part += v[k * VEC + j] * v[k * VEC + j];
             }
-        const float rstd = 1.0f / sqrtf(row_sum(sq, team, s_red[1]) / count + float(a.eps));
-        if (row >= a.n) continue;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (col[k] >= d) continue;
-            Pack<E, VEC> o;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) o.v[j] = E(v[k * VEC + j] * rstd * w[k * VEC + j] + b[k * VEC + j]);
-            store_pack<E, VEC>(y + row * a.out_stride + col[k], o);
+            sq += cols.has(k) ? part : 0.0f;
         }
-        if (lane == 0) {
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = rstd;
+        const float rstd = inverse_root(share(row_sum(sq, team, s_red[1]), count, inv) + eps);
+        if (first + rows <= a.n || row < a.n) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                Pack<E, VEC> o;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) o.v[j] = E(v[k * VEC + j] * rstd * w[k * VEC + j] + b[k * VEC + j]);
+                if (cols.has(k)) store_pack<E, VEC>(y + k * team * VEC, o);
+            }
+            if (lane == 0) {
+                if (a.mean) a.mean[row] = mean;
+                if (a.rstd) a.rstd[row] = rstd;
+            }
         }
+        y += step * a.out_stride;
     }
 }
 
 // rows longer than a block's registers: one block a row, three passes over it
-template <typename E, int VEC>
+template <typename E, int VEC, bool kWide>
 __global__ __launch_bounds__(kNormMaxThreads) void norm_long_kernel(NormArgs a)
 {
     __shared__ float s_red[2][kNormMaxThreads / kWave];
+    const Params<kWide> weight = {a.weight, a.param == Elem::kF16}, bias = {a.bias, a.param == Elem::kF16};
     const int team = blockDim.x;
-    const float count = float(a.d);
+    const float count = float(a.d), inv = 1.0f / count;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const E *x = static_cast<const E *>(a.x) + row * a.x_stride;
         E *y = static_cast<E *>(a.out) + row * a.out_stride;
@@ -169,21 +229,20 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_long_kernel(NormArgs a)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) sum += float(p.v[j]);
         }
-        const float mean = row_sum(sum, team, s_red[0]) / count;
+        const float mean = share(row_sum(sum, team, s_red[0]), count, inv);
         float sq = 0.0f;
         for (int64_t c = int64_t(threadIdx.x) * VEC; c < a.d; c += int64_t(team) * VEC) {
             const Pack<E, VEC> p = load_pack<E, VEC>(x + c);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) sq += (float(p.v[j]) - mean) * (float(p.v[j]) - mean);
         }
-        const float rstd = 1.0f / sqrtf(row_sum(sq, team, s_red[1]) / count + float(a.eps));
+        const float rstd = inverse_root(share(row_sum(sq, team, s_red[1]), count, inv) + float(a.eps));
         for (int64_t c = int64_t(threadIdx.x) * VEC; c < a.d; c += int64_t(team) * VEC) {
             const Pack<E, VEC> p = load_pack<E, VEC>(x + c);
             Pack<E, VEC> o;
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                const float w = a.weight ? load_param(a.weight, a.param, c + j) : 1.0f;
-                const float b = a.bias ? load_param(a.bias, a.param, c + j) : 0.0f;
+                const float w = a.weight ? weight.at(c + j) : 1.0f, b = a.bias ? bias.at(c + j) : 0.0f;
                 o.v[j] = E((float(p.v[j]) - mean) * rstd * w + b);
             }
             store_pack<E, VEC>(y + c, o);
@@ -207,44 +266,40 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_back_kernel(NormArgs a, 
     const int lane = team <= kWave ? sub : threadIdx.x;
     const int rows = team <= kWave ? int(blockDim.x) / team : 1;
     const int mine = team <= kWave ? int(threadIdx.x) / team : 0;
-    const E *x = static_cast<const E *>(a.x), *dy = static_cast<const E *>(a.dy);
-    E *dx = static_cast<E *>(a.out);
     const int d = int(a.d);
-    const float count = float(d);
+    const float count = float(d), inv = 1.0f / count;
+    const Columns<VEC> cols = {team, lane, d};
 
-    int col[NV];
     float w[NV * VEC], dw[NV * VEC], db[NV * VEC];
+    read_params<VEC, NV>(a.weight, a.param, team, lane, d, 1.0f, w);
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        col[k] = (k * team + lane) * VEC;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            const int c = col[k] + j;
-            w[k * VEC + j] = c < d && a.weight ? load_param(a.weight, a.param, c) : 1.0f;
-            dw[k * VEC + j] = db[k * VEC + j] = 0.0f;
-        }
-    }
+    for (int i = 0; i < NV * VEC; ++i) dw[i] = db[i] = 0.0f;
     const int64_t step = int64_t(gridDim.x) * rows;
     int64_t row = int64_t(blockIdx.x) * rows + mine;
-    Pack<E, VEC> nx[NV], ndy[NV];
+    const E *x = static_cast<const E *>(a.x) + row * a.x_stride + lane * VEC;
+    const E *dy = static_cast<const E *>(a.dy) + row * a.dy_stride + lane * VEC;
+    E *dx = static_cast<E *>(a.out) + row * a.out_stride + lane * VEC;
+    Pack<E, VEC> nx[NV] = {}, ndy[NV] = {};
     float nmean = 0.0f, nrstd = 0.0f;
-    if (row < a.n) {
-        nmean = a.mean[row];
-        nrstd = a.rstd[row];
+    const auto load = [&](int64_t r) {
+        nmean = a.mean[r];
+        nrstd = a.rstd[r];
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            if (col[k] < d) {
-                nx[k] = load_pack<E, VEC>(x + row * a.x_stride + col[k]);
-                ndy[k] = load_pack<E, VEC>(dy + row * a.dy_stride + col[k]);
+            if (cols.has(k)) {
+                nx[k] = load_pack<E, VEC>(x + k * team * VEC);
+                ndy[k] = load_pack<E, VEC>(dy + k * team * VEC);
             }
-    }
+    };
+    if (row < a.n) load(row);
     for (int64_t first = int64_t(blockIdx.x) * rows; first < a.n; first += step, row += step) {
         const float mean = nmean, rstd = nrstd;
+        const bool have = first + rows <= a.n || row < a.n;
         float xh[NV * VEC], g[NV * VEC];
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            if (row >= a.n || col[k] >= d) continue;
+            if (!have || !cols.has(k)) continue;
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 const int i = k * VEC + j;
@@ -257,30 +312,25 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_back_kernel(NormArgs a, 
                 s2 += g[i] * xh[i];
             }
         }
-        if (row + step < a.n) {
-            nmean = a.mean[row + step];
-            nrstd = a.rstd[row + step];
+        x += step * a.x_stride;
+        dy += step * a.dy_stride;
+        if (first + step + rows <= a.n || row + step < a.n) load(row + step);
+        s1 = share(row_sum(s1, team, s_red[0]), count, inv);
+        s2 = share(row_sum(s2, team, s_red[1]), count, inv);
+        if (have && a.out) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
-                if (col[k] < d) {
-                    nx[k] = load_pack<E, VEC>(x + (row + step) * a.x_stride + col[k]);
-                    ndy[k] = load_pack<E, VEC>(dy + (row + step) * a.dy_stride + col[k]);
+            for (int k = 0; k < NV; ++k) {
+                if (!cols.has(k)) continue;
+                Pack<E, VEC> o;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const int i = k * VEC + j;
+                    o.v[j] = E(rstd * (g[i] - s1 - xh[i] * s2));
                 }
-        }
-        s1 = row_sum(s1, team, s_red[0]) / count;
-        s2 = row_sum(s2, team, s_red[1]) / count;
-        if (row >= a.n || !dx) continue;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (col[k] >= d) continue;
-            Pack<E, VEC> o;
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const int i = k * VEC + j;
-                o.v[j] = E(rstd * (g[i] - s1 - xh[i] * s2));
+                store_pack<E, VEC>(dx + k * team * VEC, o);
             }
-            store_pack<E, VEC>(dx + row * a.out_stride + col[k], o);
         }
+        dx += step * a.out_stride;
     }
     if (!a.part) return;
     const int width = team * NV * VEC;
@@ -291,14 +341,14 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_back_kernel(NormArgs a, 
             for (int k = 0; k < NV; ++k)
 #pragma unroll
                 for (int j = 0; j < VEC; ++j)
-                    if (col[k] + j < d) part[col[k] + j] = which ? db[k * VEC + j] : dw[k * VEC + j];
+                    if (cols.at(k) + j < d) part[cols.at(k) + j] = which ? db[k * VEC + j] : dw[k * VEC + j];
             continue;
         }
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) s_part[mine * width + col[k] + j] = which ? db[k * VEC + j] : dw[k * VEC + j];
+            for (int j = 0; j < VEC; ++j) s_part[mine * width + cols.at(k) + j] = which ? db[k * VEC + j] : dw[k * VEC + j];
         __syncthreads();
         for (int c = threadIdx.x; c < d; c += blockDim.x) {
             float s = 0.0f;
@@ -309,12 +359,13 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_back_kernel(NormArgs a, 
 }
 
 // rows longer than a block's registers: dx, one block a row
-template <typename E, int VEC>
+template <typename E, int VEC, bool kWide>
 __global__ __launch_bounds__(kNormMaxThreads) void norm_back_long_kernel(NormArgs a)
 {
     __shared__ float s_red[2][kNormMaxThreads / kWave];
+    const Params<kWide> weight = {a.weight, a.param == Elem::kF16};
     const int team = blockDim.x;
-    const float count = float(a.d);
+    const float count = float(a.d), inv = 1.0f / count;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const E *x = static_cast<const E *>(a.x) + row * a.x_stride;
         const E *dy = static_cast<const E *>(a.dy) + row * a.dy_stride;
@@ -325,20 +376,20 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_back_long_kernel(NormArg
             const Pack<E, VEC> p = load_pack<E, VEC>(x + c), q = load_pack<E, VEC>(dy + c);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                const float w = a.weight ? load_param(a.weight, a.param, c + j) : 1.0f;
+                const float w = a.weight ? weight.at(c + j) : 1.0f;
                 const float g = float(q.v[j]) * w;
                 s1 += g;
                 s2 += g * ((float(p.v[j]) - mean) * rstd);
             }
         }
-        s1 = row_sum(s1, team, s_red[0]) / count;
-        s2 = row_sum(s2, team, s_red[1]) / count;
+        s1 = share(row_sum(s1, team, s_red[0]), count, inv);
+        s2 = share(row_sum(s2, team, s_red[1]), count, inv);
         for (int64_t c = int64_t(threadIdx.x) * VEC; c < a.d; c += int64_t(team) * VEC) {
             const Pack<E, VEC> p = load_pack<E, VEC>(x + c), q = load_pack<E, VEC>(dy + c);
             Pack<E, VEC> o;
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                const float w = a.weight ? load_param(a.weight, a.param, c + j) : 1.0f;
+                const float w = a.weight ? weight.at(c + j) : 1.0f;
                 o.v[j] = E(rstd * (float(q.v[j]) * w - s1 - (float(p.v[j]) - mean) * rstd * s2));
             }
             store_pack<E, VEC>(dx + c, o);
@@ -367,6 +418,7 @@ template <typename E> __global__ __launch_bounds__(256) void norm_back_columns_k
 // Joins the blocks' partial rows: 32 columns and 32 strands of partial rows a
 // block; sums in fp64 and in a fixed order, whatever the blocks' timing.
 constexpr int kJoinCols = 32, kJoinStrands = 32;
+template <bool kWide>
 __global__ __launch_bounds__(kJoinCols *kJoinStrands) void norm_join_kernel(const float *part, int blocks, int64_t d,
                                                                           void *dweight, void *dbias, Elem param)
 {
@@ -380,13 +432,10 @@ __global__ __launch_bounds__(kJoinCols *kJoinStrands) void norm_join_kernel(cons
     }
     s_sum[strand][cx] = s;
     __syncthreads();
-    if (strand != 0 || c >= 2 * d) return;
     s = 0.0;
     for (int k = 0; k < kJoinStrands; ++k) s += s_sum[k][cx];
-    if (c < d) {
-        if (dweight) store_param(dweight, param, c, float(s));
-    } else if (dbias)
-        store_param(dbias, param, c - d, float(s));
+    if (strand == 0 && c < d && dweight) store_param<kWide>(dweight, param, c, float(s));
+    if (strand == 0 && c >= d && c < 2 * d && dbias) store_param<kWide>(dbias, param, c - d, float(s));
 }
 
 // ------------------------------------------------------------------ launch shapes
@@ -450,7 +499,10 @@ template <typename E, int VEC> void forward_vec(const NormArgs &a, const Shape &
 {
     if (!s.in_regs) {
         const int64_t blocks = least(a.n, 2 * kCus);
-        norm_long_kernel<E, VEC><<<dim3(uint32_t(blocks)), dim3(s.block), 0, st>>>(a);
+        if (a.param == Elem::kF32)
+            norm_long_kernel<E, VEC, true><<<dim3(uint32_t(blocks)), dim3(s.block), 0, st>>>(a);
+        else
+            norm_long_kernel<E, VEC, false><<<dim3(uint32_t(blocks)), dim3(s.block), 0, st>>>(a);
         return;
     }
     switch (s.nv) {
@@ -472,7 +524,11 @@ template <typename E, int VEC> void backward_vec(const NormArgs &a, const Shape 
             const int64_t blocks = back_blocks(a.n, s);
             norm_back_columns_kernel<E><<<dim3(uint32_t(ceil_div(a.d, 256)), uint32_t(blocks)), dim3(256), 0, st>>>(a);
         }
-        if (a.out) norm_back_long_kernel<E, VEC><<<dim3(uint32_t(least(a.n, 2 * kCus))), dim3(s.block), 0, st>>>(a);
+        const dim3 grid(uint32_t(least(a.n, 2 * kCus)));
+        if (a.out && a.param == Elem::kF32)
+            norm_back_long_kernel<E, VEC, true><<<grid, dim3(s.block), 0, st>>>(a);
+        else if (a.out)
+            norm_back_long_kernel<E, VEC, false><<<grid, dim3(s.block), 0, st>>>(a);
         return;
     }
     switch (s.nv) {
@@ -526,8 +582,11 @@ void launch_layer_norm_backward(const NormArgs &a, void *dweight, void *dbias, h
     if (a.n > 0) run_norm<true>(a, st);
     if (a.part) {
         const int blocks = int(back_blocks(a.n, shape_of(vector_of(a), a.d)));
-        norm_join_kernel<<<dim3(uint32_t(ceil_div(2 * a.d, kJoinCols))), dim3(kJoinCols * kJoinStrands), 0, st>>>(
-            a.part, blocks, a.d, dweight, dbias, a.param);
+        const dim3 grid(uint32_t(ceil_div(2 * a.d, kJoinCols)));
+        if (a.param == Elem::kF32)
+            norm_join_kernel<true><<<grid, kJoinCols * kJoinStrands, 0, st>>>(a.part, blocks, a.d, dweight, dbias, a.param);
+        else
+            norm_join_kernel<false><<<grid, kJoinCols * kJoinStrands, 0, st>>>(a.part, blocks, a.d, dweight, dbias, a.param);
     }
 }
 

@@ -27,22 +27,6 @@ typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr int kT = 64; // tile of the planes' kernel
 
-__device__ inline float load_elem(const void *p, Elem t, int64_t i)
-{
-    if (t == Elem::kF32) return static_cast<const float *>(p)[i];
-    if (t == Elem::kF16) return float(static_cast<const f16 *>(p)[i]);
-    return float(static_cast<const bf16 *>(p)[i]);
-}
-__device__ inline void store_elem(void *p, Elem t, int64_t i, float v)
-{
-    if (t == Elem::kF32)
-        static_cast<float *>(p)[i] = v;
-    else if (t == Elem::kF16)
-        static_cast<f16 *>(p)[i] = f16(v);
-    else
-        static_cast<bf16 *>(p)[i] = bf16(v);
-}
-
 // ------------------------------------------------------------------ norm and planes
 __device__ inline float update_value(const OrthArgs &a, float g, float m)
 {
@@ -235,7 +219,8 @@ __device__ inline int xcd_tile(int b, int blocks)
     return x * q + (x < r ? x : r) + b / 8;
 }
 
-template <typename T, bool kSplit, Prod kProd>
+// E: elements of the output of kLast
+template <typename T, bool kSplit, Prod kProd, typename E>
 __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, char *ws, OrthLayout L, int k, OrthStep S, float next_sx)
 {
     constexpr int kPlanes = kSplit ? 2 : 1;
@@ -390,9 +375,8 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, c
                 if (r >= a.rows || c >= a.cols) continue;
                 float v = patch[row * T::kPatch + col] * (1.0f / (S.sb * S.sx));
                 if constexpr (!kSplit) v += (S.a / S.sx) * unpack_low(u_low[r * L.cols + c], U[r * L.cols + c]);
-                const int64_t at = int64_t(blockIdx.z) * a.w_batch + r * a.w_stride + c;
-                if (a.M) v = a.keep * load_elem(a.W, a.type, at) - a.rate * v;
-                store_elem(a.W, a.type, at, v);
+                E *o = static_cast<E *>(a.W) + int64_t(blockIdx.z) * a.w_batch + r * a.w_stride + c;
+                *o = E(a.M ? a.keep * float(*o) - a.rate * v : v);
             }
             continue;
         }
@@ -458,7 +442,7 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, c
     }
 }
 
-template <typename T, bool kSplit, Prod kProd>
+template <typename T, bool kSplit, Prod kProd, typename E>
 void run_product(const OrthArgs &a, const OrthSteps &steps, char *ws, const OrthLayout &L, int k, hipStream_t st)
 {
     constexpr size_t kRing = size_t(T::kStages) * (kSplit ? 2 : 1) * (T::kM + T::kN) * kK * sizeof(f16);
@@ -473,7 +457,7 @@ void run_product(const OrthArgs &a, const OrthSteps &steps, char *ws, const Orth
     } else {
         tiles = uint32_t((L.rows + T::kM - 1) / T::kM) * uint32_t((L.cols + T::kN - 1) / T::kN);
     }
-    orth_product_kernel<T, kSplit, kProd><<<dim3(tiles, 1, uint32_t(a.batch)), T::kThreads, kLds, st>>>(
+    orth_product_kernel<T, kSplit, kProd, E><<<dim3(tiles, 1, uint32_t(a.batch)), T::kThreads, kLds, st>>>(
         a, ws, L, k, steps.step[k], k + 1 < steps.count ? steps.step[k + 1].sx : 1.0f);
 }
 
@@ -519,32 +503,32 @@ TileChoice tile_of(bool split, bool symmetric, int64_t rows, int64_t cols, int64
     return best;
 }
 
-template <bool kSplit, Prod kProd>
+template <bool kSplit, Prod kProd, typename E>
 void run_tile(TileChoice choice, const OrthArgs &a, const OrthSteps &steps, char *ws, const OrthLayout &L, int k, hipStream_t st)
 {
     const int tile = choice.side;
-    if (tile == 32) return run_product<Tile32, kSplit, kProd>(a, steps, ws, L, k, st);
-    if (tile == 64 && choice.several) return run_product<Tile64Several, kSplit, kProd>(a, steps, ws, L, k, st);
-    if (tile == 64) return run_product<Tile64, kSplit, kProd>(a, steps, ws, L, k, st);
-    if (tile == 96) return run_product<Tile96, kSplit, kProd>(a, steps, ws, L, k, st);
+    if (tile == 32) return run_product<Tile32, kSplit, kProd, E>(a, steps, ws, L, k, st);
+    if (tile == 64 && choice.several) return run_product<Tile64Several, kSplit, kProd, E>(a, steps, ws, L, k, st);
+    if (tile == 64) return run_product<Tile64, kSplit, kProd, E>(a, steps, ws, L, k, st);
+    if (tile == 96) return run_product<Tile96, kSplit, kProd, E>(a, steps, ws, L, k, st);
     if constexpr (!kSplit) {
-        if (tile == 192) return run_product<Tile192, kSplit, kProd>(a, steps, ws, L, k, st);
-        if (tile == 256) return run_product<Tile256, kSplit, kProd>(a, steps, ws, L, k, st);
+        if (tile == 192) return run_product<Tile192, kSplit, kProd, E>(a, steps, ws, L, k, st);
+        if (tile == 256) return run_product<Tile256, kSplit, kProd, E>(a, steps, ws, L, k, st);
     }
-    run_product<Tile128<kSplit>, kSplit, kProd>(a, steps, ws, L, k, st);
+    run_product<Tile128<kSplit>, kSplit, kProd, E>(a, steps, ws, L, k, st);
 }
 
-template <bool kSplit>
+template <typename E, bool kSplit>
 void run_steps(const OrthArgs &a, const OrthSteps &steps, char *ws, const OrthLayout &L, hipStream_t st)
 {
     const TileChoice square = tile_of(kSplit, true, L.m, L.m, a.batch), full = tile_of(kSplit, false, L.rows, L.cols, a.batch);
     for (int k = 0; k < steps.count; ++k) {
-        run_tile<kSplit, Prod::kGram>(square, a, steps, ws, L, k, st);
-        run_tile<kSplit, Prod::kPoly>(square, a, steps, ws, L, k, st);
+        run_tile<kSplit, Prod::kGram, void>(square, a, steps, ws, L, k, st);
+        run_tile<kSplit, Prod::kPoly, void>(square, a, steps, ws, L, k, st);
         if (k + 1 < steps.count)
-            run_tile<kSplit, Prod::kApply>(full, a, steps, ws, L, k, st);
+            run_tile<kSplit, Prod::kApply, void>(full, a, steps, ws, L, k, st);
         else
-            run_tile<kSplit, Prod::kLast>(full, a, steps, ws, L, k, st);
+            run_tile<kSplit, Prod::kLast, E>(full, a, steps, ws, L, k, st);
     }
 }
 
@@ -936,7 +920,7 @@ template <typename E, bool kSplit> void run_wide(const OrthArgs &a, const OrthSt
     orth_norm_kernel<E><<<dim3(norm_blocks, uint32_t(a.batch)), 256, 0, st>>>(a, ws, int64_t(L.stride), L.norm);
     orth_planes_kernel<E, kSplit><<<dim3(uint32_t(L.cols / kT), uint32_t(L.rows / kT), uint32_t(a.batch)), 256, 0, st>>>(
         a, ws, L, norm_blocks, steps.step[0].sx);
-    run_steps<kSplit>(a, steps, ws, L, st);
+    run_steps<E, kSplit>(a, steps, ws, L, st);
 }
 
 template <typename E> void run_type(const OrthArgs &a, const OrthSteps &steps, char *ws, hipStream_t st)
