@@ -454,18 +454,28 @@ int vector_of(const NormArgs &a)
     return int((bits & (~bits + 1)) / e);
 }
 
-// A team as small as holds a row at kNormLane features a lane, but of a whole
-// wave before a lane takes more than one vector.
-Shape shape_of(int vec, int64_t d)
+// How a row is shared out.  A lane does best with four features and a few vectors: more rows a wave pass through
+// the row sums together, and loads still cover whole lines (1.3M x 50 fp16: 16 lanes of 2 x 2 features 69 us, 32 of
+// 2 features 99, 8 of 4 x 2 87; 2M x 7 fp32: 4 lanes 30 us, 8 lanes 37, 2 lanes 41).  Where rows are too few to fill the
+// chip, one vector a lane (2000 x 128 fp32 3.5 us against 4.1).  `most`: features of a lane, 16 forward and 8 backward,
+// whose sums take the registers (16 there spill: 300k x 255 fp32 540 us against 170).
+Shape shape_of(int vec, int64_t n, int64_t d, int most)
 {
+    const auto power = [](int64_t x) {
+        int p = 1;
+        while (p < x) p *= 2;
+        return p;
+    };
     Shape s;
     s.vec = vec;
     const int64_t vecs = (d + vec - 1) / vec;
-    const int most = kNormLane / vec;
+    const int few = n <= kNormFewRows ? vec : vec > 4 ? vec : 4;
+    int64_t team = power((d + few - 1) / few);
+    const int64_t least = power(vecs < 4 ? vecs : 4);
+    if (team < least) team = least;
+    s.team = int(team < kWave ? team : kWave);
     s.nv = 1;
-    while (s.nv < most && vecs > int64_t(s.nv) * kWave) s.nv *= 2;
-    s.team = 1;
-    while (s.team < kWave && int64_t(s.team) * s.nv < vecs) s.team *= 2;
+    while (s.nv * vec < most && int64_t(s.team) * s.nv < vecs) s.nv *= 2;
     s.block = 256;
     if (int64_t(s.team) * s.nv < vecs) {
         const int64_t waves = (vecs + int64_t(s.nv) * kWave - 1) / (int64_t(s.nv) * kWave);
@@ -534,19 +544,19 @@ template <typename E, int VEC> void backward_vec(const NormArgs &a, const Shape 
     switch (s.nv) {
     case 1: return backward_regs<E, VEC, 1>(a, s, st);
     case 2:
-        if constexpr (VEC * 2 <= kNormLane) return backward_regs<E, VEC, 2>(a, s, st);
+        if constexpr (VEC * 2 <= kNormLaneBack) return backward_regs<E, VEC, 2>(a, s, st);
     case 4:
-        if constexpr (VEC * 4 <= kNormLane) return backward_regs<E, VEC, 4>(a, s, st);
-    case 8:
-        if constexpr (VEC * 8 <= kNormLane) return backward_regs<E, VEC, 8>(a, s, st);
+        if constexpr (VEC * 4 <= kNormLaneBack) return backward_regs<E, VEC, 4>(a, s, st);
     default:
-        if constexpr (VEC * 16 <= kNormLane) return backward_regs<E, VEC, 16>(a, s, st);
+        if constexpr (VEC * 8 <= kNormLaneBack) return backward_regs<E, VEC, 8>(a, s, st);
     }
 }
 
+Shape shape_of(const NormArgs &a, bool back) { return shape_of(vector_of(a), a.n, a.d, back ? kNormLaneBack : kNormLane); }
+
 template <bool kBack, typename E> void run_type(const NormArgs &a, hipStream_t st)
 {
-    const Shape s = shape_of(vector_of(a), a.d);
+    const Shape s = shape_of(a, kBack);
     const auto go = [&](auto vec) {
         if constexpr (kBack)
             backward_vec<E, decltype(vec)::value>(a, s, st);
@@ -581,7 +591,7 @@ void launch_layer_norm_backward(const NormArgs &a, void *dweight, void *dbias, h
 {
     if (a.n > 0) run_norm<true>(a, st);
     if (a.part) {
-        const int blocks = int(back_blocks(a.n, shape_of(vector_of(a), a.d)));
+        const int blocks = int(back_blocks(a.n, shape_of(a, true)));
         const dim3 grid(uint32_t(ceil_div(2 * a.d, kJoinCols)));
         if (a.param == Elem::kF32)
             norm_join_kernel<true><<<grid, kJoinCols * kJoinStrands, 0, st>>>(a.part, blocks, a.d, dweight, dbias, a.param);

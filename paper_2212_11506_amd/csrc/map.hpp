@@ -19,7 +19,9 @@ constexpr int kCus = 256; // compute units of the card
 // ---------------------------------------------------------------- layer norm
 // Rows are kNormMaxRow features or fewer in registers; longer rows are read
 // again from the caches for each pass.
-constexpr int kNormLane = 16;                      // features of a lane
+constexpr int kNormLane = 16;                      // features of a lane, forward
+constexpr int kNormLaneBack = 8;                   // ... and backward
+constexpr int64_t kNormFewRows = 8192;             // rows that do not fill the chip at several vectors a lane
 constexpr int kNormMaxThreads = 1024;              // lanes of a row
 constexpr int64_t kNormMaxFeatures = int64_t(1) << 24;
 constexpr int kNormBackBlocks = 4 * kCus;          // partial sums of the weights' gradient
