@@ -23,6 +23,7 @@ constexpr int kNormLane = 16;                      // features of a lane, forwar
 constexpr int kNormLaneBack = 8;                   // ... and backward
 constexpr int64_t kNormFewRows = 8192;             // rows that do not fill the chip at several vectors a lane
 constexpr int kNormMaxThreads = 1024;              // lanes of a row
+constexpr int64_t kNormStream = int64_t(256) << 20; // bytes of x from which rows do not stay in the last cache
 constexpr int64_t kNormMaxFeatures = int64_t(1) << 24;
 constexpr int kNormBackBlocks = 4 * kCus;          // partial sums of the weights' gradient
 
