@@ -229,6 +229,42 @@ def test_constant_rows_and_far_offsets():
     assert bool((bh.layer_norm(one)[0] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [6, 64, 300, 9000])
+def test_starts_off_every_alignment(d, dtype):
+    """Rows, weights and outputs that begin one element behind an aligned address give what aligned ones give."""
+    n = 41
+    x, dy, w, b = rows(n, d, dtype, 1), rows(n, d, dtype, 2), vec(d, dtype, 3, 1.0, 0.2), vec(d, dtype, 4, 0.0, 0.1)
+    shift = lambda t: torch.cat([t.reshape(-1)[:1], t.reshape(-1)])[1:].view(t.shape)  # noqa: E731
+    got = bh.layer_norm(shift(x), shift(w), shift(b), out=shift(torch.zeros_like(x)))
+    check_forward(x, w, b, got)
+    back = bh.layer_norm_backward(shift(dy), shift(x), shift(w), shift(got[1]), shift(got[2]), dx=shift(torch.zeros_like(x)))
+    check_backward(dy, x, w, got[1], got[2], back)
+
+
+def test_arrays_beyond_the_caches():
+    """Rows of a 280 MB array, which are read and written past the caches, come out as they do in parts."""
+    n, d = 550_000, 256
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn((n, d), generator=g, device=DEV).to(torch.bfloat16)
+    dy = (0.1 * torch.randn((n, d), generator=g, device=DEV) + 0.01).to(torch.bfloat16)
+    w, b = vec(d, torch.float32, 2, 1.0, 0.2), vec(d, torch.float32, 3, 0.0, 0.1)
+    assert x.numel() * 2 > 256 << 20
+    y, mean, rstd = bh.layer_norm(x, w, b)
+    dx, dw, db = bh.layer_norm_backward(dy, x, w, mean, rstd)
+    half, sums = n // 2 + 3, 0.0
+    for i, j in ((0, half), (half, n)):
+        part = bh.layer_norm(x[i:j], w, b)
+        assert all(torch.equal(p, q[i:j]) for p, q in zip(part, (y, mean, rstd)))
+        back = bh.layer_norm_backward(dy[i:j], x[i:j], w, mean[i:j], rstd[i:j])
+        assert torch.equal(back[0], dx[i:j])
+        sums = sums + torch.stack(back[1:]).double()
+    # two sums of n / 2 terms against one of n, each within `kn` of its terms' magnitudes
+    size = torch.stack([(dy.float().abs() * ((x.float() - mean[:, None]) * rstd[:, None]).abs()).sum(0), dy.float().abs().sum(0)])
+    kn = 2 * (64.0 + n / 256) * U
+    assert bool(((torch.stack([dw, db]).double() - sums).abs() <= kn * size.double()).all())
+
+
 def test_no_rows():
     x = torch.empty((0, 24), device=DEV)
     y, mean, rstd = bh.layer_norm(x)

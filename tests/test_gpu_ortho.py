@@ -163,6 +163,20 @@ def test_batches_strides_and_in_place(shape):
     assert bh.orthogonalise(torch.empty((0, r, c), device=DEV)).shape == (0, r, c)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(24, 40), (64, 1000), (96, 136), (400, 304)])
+def test_starts_off_every_alignment(shape, dtype):
+    G = gauss(*shape, seed=12, dtype=dtype)
+    shift = lambda t: torch.cat([t.reshape(-1)[:1], t.reshape(-1)])[1:].view(t.shape)  # noqa: E731
+    W, M = gauss(*shape, seed=13, dtype=dtype, scale=0.1), gauss(*shape, seed=14)
+    want = W.clone(), M.clone()
+    assert torch.equal(bh.orthogonalise(shift(G), out=shift(torch.zeros_like(G))), bh.orthogonalise(G))
+    bh.muon_step(want[0], G, want[1], 0.1)
+    W, M = shift(W), shift(M)
+    bh.muon_step(W, shift(G), M, 0.1)
+    assert torch.equal(W, want[0]) and torch.equal(M, want[1])
+
+
 @pytest.mark.parametrize("shape", [(8, 8), (20, 300), (300, 200)])
 def test_zero_and_nonfinite_matrices(shape):
     G = torch.zeros((3, *shape), device=DEV)
