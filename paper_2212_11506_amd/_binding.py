@@ -742,7 +742,7 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     n, d = shape
     x_stride = _rows(x, "x", shape, dtype)
     if out is None:
-        y, y_stride = x.new_empty(shape), d
+        y, y_stride = torch.empty_like(x) if x_stride == d else x.new_empty(shape), d
     else:
         y, y_stride = out, _rows(out, "out", shape, dtype)
     mean, rstd = x.new_empty((2, n), dtype=torch.float32).unbind(0)
@@ -774,7 +774,7 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
         raise BhtsneError(BHTSNE_EINVAL, "bhtsne_layer_norm_workspace_size")
     x_stride, dy_stride = _rows(x, "x", shape, dtype), _rows(dy, "dy", shape, dtype)
     if dx is None:
-        dx, dx_stride = x.new_empty(shape), d
+        dx, dx_stride = torch.empty_like(x) if x_stride == d else x.new_empty(shape), d
     else:
         dx_stride = _rows(dx, "dx", shape, dtype)
     if workspace is None:
@@ -848,7 +848,7 @@ def orthogonalise(G: torch.Tensor, steps: int = 5, coefficients=None, eps: float
     sizes = _matrix_sizes(G, "G")
     kind, shape, dtype = _type(G, "G"), G.shape, G.dtype
     g = _matrices(G, "G", shape, dtype)
-    O = out if out is not None else G.new_empty(shape)
+    O = out if out is not None else torch.empty_like(G, memory_format=torch.contiguous_format)
     o = _matrices(O, "out", shape, dtype)
     ws, nbytes = _orthogonal_workspace(sizes, G, workspace)
     rc = lib.bhtsne_orthogonalise(C.byref(g), *sizes, kind, _coefficients(coefficients, steps), steps, eps, C.byref(o),

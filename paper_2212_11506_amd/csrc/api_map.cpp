@@ -184,7 +184,9 @@ int bhtsne_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x,
     a.d = d;
     a.type = Elem(type);
     a.param = Elem(param_type);
-    launch_layer_norm_backward(a, dweight, dbias, stream);
+    a.dweight = dweight;
+    a.dbias = dbias;
+    launch_layer_norm_backward(a, stream);
     return hipGetLastError() == hipSuccess ? BHTSNE_OK : BHTSNE_EDEVICE;
 }
 

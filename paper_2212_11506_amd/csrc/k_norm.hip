@@ -265,6 +265,15 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_long_kernel(NormArgs a)
 }
 
 // ------------------------------------------------------------------ backward
+// the partial row of a block that was alone, which it has written itself, as gradients
+template <bool kWide> __device__ inline void finish(const NormArgs &a)
+{
+    for (int c = threadIdx.x; c < int(a.d); c += blockDim.x) {
+        if (a.dweight) store_param<kWide>(a.dweight, a.param, c, a.part[c]);
+        if (a.dbias) store_param<kWide>(a.dbias, a.param, c, a.part[a.d + c]);
+    }
+}
+
 // Each team keeps the sums of its rows' dy xh and dy in registers; a block's
 // teams are joined in LDS, in order, into one partial row [2][d] of the block.
 template <typename E, int VEC, int NV, bool kStream>
@@ -366,6 +375,13 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_back_kernel(NormArgs a, 
             part[c] = s;
         }
     }
+    if (!a.alone) return;
+    // the only block: its sums are the gradients
+    __syncthreads();
+    if (a.param == Elem::kF32)
+        finish<true>(a);
+    else
+        finish<false>(a);
 }
 
 // rows longer than a block's registers: dx, one block a row
@@ -452,6 +468,7 @@ __global__ __launch_bounds__(kJoinCols *kJoinStrands) void norm_join_kernel(cons
 struct Shape {
     int vec, nv, team, block, rows;
     bool in_regs;
+    bool alone; // backward: one block
 };
 
 // the widest vectors that every row's start and the row length allow, 16 bytes at most
@@ -494,6 +511,7 @@ Shape shape_of(int vec, int64_t n, int64_t d, int most)
     s.in_regs = int64_t(s.team) * s.nv >= vecs;
     if (!s.in_regs) s.team = s.block = kNormMaxThreads;
     s.rows = s.team <= kWave ? s.block / s.team : 1;
+    s.alone = false;
     return s;
 }
 
@@ -503,7 +521,7 @@ int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 template <typename E> bool streams(const NormArgs &a) { return a.n * a.d >= kNormStream / int64_t(sizeof(E)); }
 
 // blocks of the backward pass: a partial row of the weights' gradient each
-int64_t back_blocks(int64_t n, const Shape &s) { return least(ceil_div(n, s.rows), kNormBackBlocks); }
+int64_t back_blocks(int64_t n, const Shape &s) { return s.alone ? 1 : least(ceil_div(n, s.rows), kNormBackBlocks); }
 
 template <typename E, int VEC, int NV> void forward_regs(const NormArgs &a, const Shape &s, hipStream_t st)
 {
@@ -574,7 +592,19 @@ template <typename E, int VEC> void backward_vec(const NormArgs &a, const Shape 
     }
 }
 
-Shape shape_of(const NormArgs &a, bool back) { return shape_of(vector_of(a), a.n, a.d, back ? kNormLaneBack : kNormLane); }
+Shape shape_of(const NormArgs &a, bool back)
+{
+    Shape s = shape_of(vector_of(a), a.n, a.d, back ? kNormLaneBack : kNormLane);
+    // Few rows backward: one large block goes over them in less than the launch takes that joins several (250 x 128
+    // fp32 12.4 us a call against 14.8; a row of several waves takes 2 us a round, 8 x 4000 bf16 17.5 against 14.7)
+    const int rows = s.team <= kWave ? kNormMaxThreads / s.team : 1;
+    if (back && s.in_regs && a.n > 0 && a.n <= int64_t(s.team <= kWave ? kNormAlone : kNormAlone / 2) * rows) {
+        s.alone = true;
+        s.rows = rows;
+        if (s.team <= kWave) s.block = kNormMaxThreads;
+    }
+    return s;
+}
 
 template <bool kBack, typename E> void run_type(const NormArgs &a, hipStream_t st)
 {
@@ -609,17 +639,19 @@ void launch_layer_norm(const NormArgs &a, hipStream_t st)
     if (a.n > 0) run_norm<false>(a, st);
 }
 
-void launch_layer_norm_backward(const NormArgs &a, void *dweight, void *dbias, hipStream_t st)
+void launch_layer_norm_backward(const NormArgs &args, hipStream_t st)
 {
+    NormArgs a = args;
+    const Shape s = shape_of(a, true);
+    a.alone = s.alone;
     if (a.n > 0) run_norm<true>(a, st);
-    if (a.part) {
-        const int blocks = int(back_blocks(a.n, shape_of(a, true)));
-        const dim3 grid(uint32_t(ceil_div(2 * a.d, kJoinCols)));
-        if (a.param == Elem::kF32)
-            norm_join_kernel<true><<<grid, kJoinCols * kJoinStrands, 0, st>>>(a.part, blocks, a.d, dweight, dbias, a.param);
-        else
-            norm_join_kernel<false><<<grid, kJoinCols * kJoinStrands, 0, st>>>(a.part, blocks, a.d, dweight, dbias, a.param);
-    }
+    if (!a.part || a.alone) return;
+    const int blocks = int(back_blocks(a.n, s));
+    const dim3 grid(uint32_t(ceil_div(2 * a.d, kJoinCols)));
+    if (a.param == Elem::kF32)
+        norm_join_kernel<true><<<grid, kJoinCols * kJoinStrands, 0, st>>>(a.part, blocks, a.d, a.dweight, a.dbias, a.param);
+    else
+        norm_join_kernel<false><<<grid, kJoinCols * kJoinStrands, 0, st>>>(a.part, blocks, a.d, a.dweight, a.dbias, a.param);
 }
 
 } // namespace bht

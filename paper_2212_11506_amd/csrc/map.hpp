@@ -21,6 +21,7 @@ constexpr int kCus = 256; // compute units of the card
 // again from the caches for each pass.
 constexpr int kNormLane = 16;                      // features of a lane, forward
 constexpr int kNormLaneBack = 8;                   // ... and backward
+constexpr int kNormAlone = 8;                      // rounds of a block of kNormMaxThreads that make a join not worth it
 constexpr int64_t kNormFewRows = 8192;             // rows that do not fill the chip at several vectors a lane
 constexpr int kNormMaxThreads = 1024;              // lanes of a row
 constexpr int64_t kNormStream = int64_t(256) << 20; // bytes of x from which rows do not stay in the last cache
@@ -35,6 +36,8 @@ struct NormArgs {
     void *out;          // y, or dx (nullable in the backward pass)
     float *mean, *rstd; // written by the forward pass (nullable), read by the backward pass
     float *part;        // backward: [blocks][2][d] partial sums, nullable (no weight gradient wanted)
+    void *dweight, *dbias; // backward, each nullable
+    bool alone;         // backward: one block, which writes the weights' gradients itself
     int64_t x_stride, dy_stride, out_stride;
     int64_t n, d;
     double eps;
@@ -42,7 +45,7 @@ struct NormArgs {
 };
 void launch_layer_norm(const NormArgs &a, hipStream_t st);
 // at most min(n, kNormBackBlocks) partial rows are written
-void launch_layer_norm_backward(const NormArgs &a, void *dweight, void *dbias, hipStream_t st);
+void launch_layer_norm_backward(const NormArgs &a, hipStream_t st);
 
 // ------------------------------------------------------- orthogonalised update
 // Newton-Schulz steps on `batch` matrices U of rows x cols.  U is kept in fp16
