@@ -49,8 +49,15 @@ template <typename E> __device__ inline void load8(const E *p, int left, bool ve
         }
         return;
     }
+    // the last value again behind the end, and nothing of a row that does not exist
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < left ? float(p[e]) : 0.0f;
+    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    if (left <= 0) return;
+    E x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = p[e < left ? e : left - 1];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < left ? float(x[e]) : 0.0f;
 }
 __device__ inline void store8(float *p, int left, bool vec, const float (&v)[8])
 {
@@ -142,7 +149,12 @@ __global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, 
     }
     const double *part = reinterpret_cast<const double *>(base + L.norm);
     double sq = 0.0;
-    for (int k = lane_id(); k < norm_blocks; k += kWave) sq += part[k];
+#pragma unroll
+    for (int q = 0; q < kOrthNormBlocks / kWave; ++q) { // all asked for at once
+        const int k = q * kWave + lane_id();
+        const double v = part[k < norm_blocks ? k : 0];
+        sq += k < norm_blocks ? v : 0.0;
+    }
     sq = wave_sum(sq);
     const double scale = double(sx) / (sqrt(sq) + a.eps);
     f16 *uh = reinterpret_cast<f16 *>(base + L.u[0]), *ul = uh + L.rows * L.cols;
