@@ -216,6 +216,22 @@ def test_muon_step(shape, nesterov, dtype):
     assert err <= TOL[dtype] * float(step.norm()) + 4 * half * float(Ww.norm())
 
 
+@pytest.mark.parametrize("shape,dtype", [((1000, 1024), torch.bfloat16), ((1500, 700), torch.float16), ((2048, 2100), torch.float32),
+                                         ((2300, 2048), torch.bfloat16), ((3000, 2900), torch.float16), ((4000, 4160), torch.bfloat16)])
+def test_muon_step_large(shape, dtype):
+    """The weights' update by every larger tile, against 64-bit products: the step's own error, and the weights' rounding."""
+    W, G, M = gauss(*shape, seed=1, dtype=dtype, scale=0.1), gauss(*shape, seed=2, dtype=dtype), gauss(*shape, seed=3)
+    lr, mu, wd, scale = 0.5, 0.9, 0.1, 1.25
+    Mw = mu * M.double() + G.double()
+    step = plain_there(G.double() + mu * Mw).to(DEV)
+    want = (1 - lr * wd) * W.double() - lr * scale * step
+    bh.muon_step(W, G, M, lr, mu, nesterov=True, weight_decay=wd, scale=scale)
+    assert float((M.double() - Mw).abs().max()) <= 4 * 2.0 ** -24 * float(Mw.abs().max() + G.double().abs().max())
+    half = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}[dtype]
+    err = float((W.double() - want).norm())
+    assert err <= TOL[dtype] * lr * scale * float(step.norm()) + 4 * half * float(want.norm())
+
+
 def test_muon_steps_in_a_graph_and_on_another_stream():
     shape = (192, 130)
     W0, G, M0 = gauss(*shape, seed=1, scale=0.1), gauss(*shape, seed=2), gauss(*shape, seed=3)
