@@ -727,6 +727,9 @@ __global__ __launch_bounds__(narrow_waves(MT) *kWave) void orth_narrow_kernel(Or
         __syncthreads();
     }
 
+    // Only the last tile can hold zeros behind the directions: of the groups of four terms all but three are sure to be
+    // needed, and those that hold nothing are left out (256 x 50 fp32, momentum step: 51.5 us against 54.8)
+    constexpr int kSure = kM / 4 - 3;
     // Lower tile t of a product of symmetric matrices, of which rows serve for columns
     const auto product = [&](const double *P, const double *R, int t) {
         const double *p = P + (16 * Lower<MT>::row(t) + lane % 16) * kLd + lane / 16;
@@ -741,7 +744,8 @@ __global__ __launch_bounds__(narrow_waves(MT) *kWave) void orth_narrow_kernel(Or
         __builtin_amdgcn_sched_barrier(0);
         double4v acc = {};
 #pragma unroll
-        for (int k = 0; k < kM / 4; ++k) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(x[k], y[k], acc, 0, 0, 0);
+        for (int k = 0; k < kM / 4; ++k)
+            if (k < kSure || 4 * k < m) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(x[k], y[k], acc, 0, 0, 0);
         return acc;
     };
     const auto store = [&](double *P, int t, const double4v &v) {
@@ -821,7 +825,8 @@ __global__ __launch_bounds__(narrow_waves(MT) *kWave) void orth_narrow_kernel(Or
                 __builtin_amdgcn_sched_barrier(0);
                 double4v acc = {};
 #pragma unroll
-                for (int k = 0; k < kM / 4; ++k) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(x[k], u[k], acc, 0, 0, 0);
+                for (int k = 0; k < kM / 4; ++k)
+                    if (k < kSure || 4 * k < m) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(x[k], u[k], acc, 0, 0, 0);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int row = 16 * i + tile_row(r);
