@@ -149,8 +149,7 @@ int bhtsne_layer_norm(const void *x, int64_t x_stride, const void *weight, const
 size_t bhtsne_layer_norm_workspace_size(int64_t n, int64_t d)
 {
     if (!norm_sizes_ok(n, d)) return 0;
-    const size_t rows = size_t(n < kNormBackBlocks ? (n > 0 ? n : 1) : kNormBackBlocks);
-    return (rows * 2 * size_t(d) * sizeof(float) + 255) / 256 * 256;
+    return (size_t(norm_back_blocks(n, d)) * 2 * size_t(d) * sizeof(float) + 255) / 256 * 256;
 }
 
 int bhtsne_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,

@@ -49,8 +49,12 @@ template <bool kWide> struct Params {
     bool half; // fp16 rather than bf16
     __device__ float at(int64_t i) const
     {
-        if constexpr (kWide) return static_cast<const float *>(p)[i];
-        const uint16_t raw = static_cast<const uint16_t *>(p)[i];
+        using R = typename std::conditional<kWide, float, uint16_t>::type;
+        return value(static_cast<const R *>(p)[i], half);
+    }
+    __device__ static float value(float v, bool) { return v; }
+    __device__ static float value(uint16_t raw, bool half)
+    {
         const float h = float(__builtin_bit_cast(f16, raw)), b = __uint_as_float(uint32_t(raw) << 16);
         return half ? h : b;
     }
@@ -65,30 +69,61 @@ template <bool kWide> __device__ inline void store_param(void *p, Elem t, int64_
     }
 }
 
-// The parameters of a lane's features, `fill` without parameters and behind the last feature, where the last one is read
-template <bool kWide, int VEC, int NV>
-__device__ inline void load_params(const void *p, Elem t, int team, int lane, int d, float fill, float (&out)[NV * VEC])
+// The parameters of a lane's features: kVector, up to 16 bytes at a time, of arrays that are aligned for it and whose
+// last vector is full.  Behind the last feature the last one is read, and `fill` taken.
+template <bool kWide, bool kVector, int VEC, int NV>
+__device__ inline void load_params(const void *p, bool half, int team, int lane, int d, float fill, float (&out)[NV * VEC])
 {
-    const Params<kWide> from = {p, t == Elem::kF16};
+    using R = typename std::conditional<kWide, float, uint16_t>::type;
+    constexpr int kMost = 16 / int(sizeof(R)), kTake = !kVector ? 1 : VEC < kMost ? VEC : kMost;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
+        for (int j = 0; j < VEC; j += kTake) {
             const int c = (k * team + lane) * VEC + j;
-            const float v = from.at(c < d ? c : d - 1);
-            out[k * VEC + j] = c < d ? v : fill;
+            const auto raw = *reinterpret_cast<const Pack<R, kTake> *>(static_cast<const R *>(p) + (c < d ? c : d - kTake));
+#pragma unroll
+            for (int i = 0; i < kTake; ++i) {
+                const float v = Params<kWide>::value(raw.v[i], half);
+                out[k * VEC + j + i] = c < d ? v : fill;
+            }
         }
 }
+// Weight and bias of a lane's features, 1 and 0 without them; both are asked for before either is waited for
 template <int VEC, int NV>
-__device__ inline void read_params(const void *p, Elem t, int team, int lane, int d, float fill, float (&out)[NV * VEC])
+__device__ inline void read_params(const void *weight, const void *bias, Elem t, int team, int lane, int d,
+                                   float (&w)[NV * VEC], float (&b)[NV * VEC])
 {
 #pragma unroll
-    for (int i = 0; i < NV * VEC; ++i) out[i] = fill;
-    if (!p) return;
-    if (t == Elem::kF32)
-        load_params<true, VEC, NV>(p, t, team, lane, d, fill, out);
-    else
-        load_params<false, VEC, NV>(p, t, team, lane, d, fill, out);
+    for (int i = 0; i < NV * VEC; ++i) {
+        w[i] = 1.0f;
+        b[i] = 0.0f;
+    }
+    if (!weight && !bias) return;
+    const void *pw = weight ? weight : bias, *pb = bias ? bias : weight;
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(pw) | reinterpret_cast<uintptr_t>(pb);
+    const auto both = [&](auto wide, auto vector) {
+        load_params<decltype(wide)::value, decltype(vector)::value, VEC, NV>(pw, t == Elem::kF16, team, lane, d, 1.0f, w);
+        load_params<decltype(wide)::value, decltype(vector)::value, VEC, NV>(pb, t == Elem::kF16, team, lane, d, 0.0f, b);
+    };
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    if (t == Elem::kF32) {
+        if (VEC > 1 && (bits & (VEC < 4 ? VEC * 4 - 1 : 15)) == 0)
+            both(yes, yes);
+        else
+            both(yes, no);
+    } else {
+        if (VEC > 1 && (bits & (VEC * 2 - 1)) == 0)
+            both(no, yes);
+        else
+            both(no, no);
+    }
+#pragma unroll
+    for (int i = 0; i < NV * VEC; ++i) {
+        w[i] = weight ? w[i] : 1.0f;
+        b[i] = bias ? b[i] : 0.0f;
+    }
 }
 
 // v of the lane at the other end of a fixed permutation within 16 lanes
@@ -165,8 +200,6 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_kernel(NormArgs a, int t
     const Columns<VEC> cols = {team, lane, d};
 
     float w[NV * VEC], b[NV * VEC];
-    read_params<VEC, NV>(a.weight, a.param, team, lane, d, 1.0f, w);
-    read_params<VEC, NV>(a.bias, a.param, team, lane, d, 0.0f, b);
     const int64_t step = int64_t(gridDim.x) * rows;
     int64_t row = int64_t(blockIdx.x) * rows + mine;
     const E *x = static_cast<const E *>(a.x) + row * a.x_stride + lane * VEC;
@@ -178,6 +211,7 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_kernel(NormArgs a, int t
             if (cols.has(k)) next[k] = load_pack<kStream, E, VEC>(x + k * team * VEC);
     };
     if (row < a.n) load();
+    read_params<VEC, NV>(a.weight, a.bias, a.param, team, lane, d, w, b);
 
     // every lane of a block makes the same number of rounds
     for (int64_t first = int64_t(blockIdx.x) * rows; first < a.n; first += step, row += step) {
@@ -290,9 +324,6 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_back_kernel(NormArgs a, 
     const Columns<VEC> cols = {team, lane, d};
 
     float w[NV * VEC], dw[NV * VEC], db[NV * VEC];
-    read_params<VEC, NV>(a.weight, a.param, team, lane, d, 1.0f, w);
-#pragma unroll
-    for (int i = 0; i < NV * VEC; ++i) dw[i] = db[i] = 0.0f;
     const int64_t step = int64_t(gridDim.x) * rows;
     int64_t row = int64_t(blockIdx.x) * rows + mine;
     const E *x = static_cast<const E *>(a.x) + row * a.x_stride + lane * VEC;
@@ -311,6 +342,9 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_back_kernel(NormArgs a, 
             }
     };
     if (row < a.n) load(row);
+    read_params<VEC, NV>(a.weight, nullptr, a.param, team, lane, d, w, db);
+#pragma unroll
+    for (int i = 0; i < NV * VEC; ++i) dw[i] = db[i] = 0.0f;
     for (int64_t first = int64_t(blockIdx.x) * rows; first < a.n; first += step, row += step) {
         const float mean = nmean, rstd = nrstd;
         const bool have = first + rows <= a.n || row < a.n;
@@ -520,8 +554,14 @@ int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 
 template <typename E> bool streams(const NormArgs &a) { return a.n * a.d >= kNormStream / int64_t(sizeof(E)); }
 
-// blocks of the backward pass: a partial row of the weights' gradient each
-int64_t back_blocks(int64_t n, const Shape &s) { return s.alone ? 1 : least(ceil_div(n, s.rows), kNormBackBlocks); }
+// Blocks of the backward pass, a partial row of the weights' gradient each: 1024 threads a CU (70k x 1000 fp16 by blocks
+// of 128 94 us, by half as many 103; 3000 x 8000 fp32 by 256 blocks of 1024 56, by 1024 87), and of rows that have a block
+// to themselves kNormBackRows at least, so that the partial rows stay
+// few beside them (300 x 8000 bf16 21 us, by a block a row 34; by blocks of 12 rows 30).
+int64_t back_blocks(int64_t n, int64_t d, const Shape &s)
+{
+    return s.alone ? 1 : least(ceil_div(n, s.team > kWave ? kNormBackRows : s.rows), norm_back_blocks(n, d));
+}
 
 template <typename E, int VEC, int NV> void forward_regs(const NormArgs &a, const Shape &s, hipStream_t st)
 {
@@ -535,7 +575,7 @@ template <typename E, int VEC, int NV> void forward_regs(const NormArgs &a, cons
 }
 template <typename E, int VEC, int NV> void backward_regs(const NormArgs &a, const Shape &s, hipStream_t st)
 {
-    const int64_t blocks = back_blocks(a.n, s);
+    const int64_t blocks = back_blocks(a.n, a.d, s);
     const size_t lds = s.rows > 1 ? size_t(s.block) * NV * VEC * sizeof(float) : 0;
     if constexpr (sizeof(E) * VEC == 16)
         if (streams<E>(a)) {
@@ -571,7 +611,7 @@ template <typename E, int VEC> void backward_vec(const NormArgs &a, const Shape 
 {
     if (!s.in_regs) {
         if (a.part) {
-            const int64_t blocks = back_blocks(a.n, s);
+            const int64_t blocks = back_blocks(a.n, a.d, s);
             norm_back_columns_kernel<E><<<dim3(uint32_t(ceil_div(a.d, 256)), uint32_t(blocks)), dim3(256), 0, st>>>(a);
         }
         const dim3 grid(uint32_t(least(a.n, 2 * kCus)));
@@ -594,7 +634,10 @@ template <typename E, int VEC> void backward_vec(const NormArgs &a, const Shape 
 
 Shape shape_of(const NormArgs &a, bool back)
 {
-    Shape s = shape_of(vector_of(a), a.n, a.d, back ? kNormLaneBack : kNormLane);
+    // Few rows are shared out over more lanes forward too (8000 x 1000 fp32 11.4 us against 13.2), which no longer pays
+    // for long ones (8000 x 3333 bf16 34.1 us against 30.4)
+    const bool narrow = back || (a.n <= kNormFewRows && a.d <= kNormFewFeatures);
+    Shape s = shape_of(vector_of(a), a.n, a.d, narrow ? kNormLaneBack : kNormLane);
     // Few rows backward: one large block goes over them in less than the launch takes that joins several (250 x 128
     // fp32 12.4 us a call against 14.8; a row of several waves takes 2 us a round, 8 x 4000 bf16 17.5 against 14.7)
     const int rows = s.team <= kWave ? kNormMaxThreads / s.team : 1;
@@ -646,7 +689,7 @@ void launch_layer_norm_backward(const NormArgs &args, hipStream_t st)
     a.alone = s.alone;
     if (a.n > 0) run_norm<true>(a, st);
     if (!a.part || a.alone) return;
-    const int blocks = int(back_blocks(a.n, s));
+    const int blocks = int(back_blocks(a.n, a.d, s));
     const dim3 grid(uint32_t(ceil_div(2 * a.d, kJoinCols)));
     if (a.param == Elem::kF32)
         norm_join_kernel<true><<<grid, kJoinCols * kJoinStrands, 0, st>>>(a.part, blocks, a.d, a.dweight, a.dbias, a.param);

@@ -17,16 +17,30 @@ inline int elem_bytes(Elem e) { return e == Elem::kF32 ? 4 : 2; }
 constexpr int kCus = 256; // compute units of the card
 
 // ---------------------------------------------------------------- layer norm
-// Rows are kNormMaxRow features or fewer in registers; longer rows are read
-// again from the caches for each pass.
+// Rows of up to kNormLane kNormMaxThreads features (kNormLaneBack of them backward) are held in registers; longer rows
+// are read again from the caches for each pass.
 constexpr int kNormLane = 16;                      // features of a lane, forward
 constexpr int kNormLaneBack = 8;                   // ... and backward
 constexpr int kNormAlone = 8;                      // rounds of a block of kNormMaxThreads that make a join not worth it
 constexpr int64_t kNormFewRows = 8192;             // rows that do not fill the chip at several vectors a lane
+constexpr int kNormFewFeatures = 2048;             // ... and are shared out over more lanes in rows up to this
 constexpr int kNormMaxThreads = 1024;              // lanes of a row
 constexpr int64_t kNormStream = int64_t(256) << 20; // bytes of x from which rows do not stay in the last cache
 constexpr int64_t kNormMaxFeatures = int64_t(1) << 24;
-constexpr int kNormBackBlocks = 4 * kCus;          // partial sums of the weights' gradient
+constexpr int kNormBackRows = 4;                   // backward: rows at least of a block that has one row at a time
+constexpr int kNormBackThreads = 1024;             // backward: threads of a CU, whose blocks write a partial row each
+// lanes of a row of d features backward, in a block of its own from 64 kNormLaneBack features on (smaller rows share
+// blocks of 256)
+inline int norm_back_block(int64_t d)
+{
+    const int64_t waves = (d + 64 * kNormLaneBack - 1) / (64 * kNormLaneBack);
+    return waves <= 1 ? 256 : waves < kNormMaxThreads / 64 ? int(waves) * 64 : kNormMaxThreads;
+}
+inline int64_t norm_back_blocks(int64_t n, int64_t d) // the most partial sums of the weights' gradient
+{
+    const int64_t most = int64_t(kCus) * kNormBackThreads / norm_back_block(d);
+    return n < 1 ? 1 : n < most ? n : most;
+}
 
 struct NormArgs {
     const void *x;
@@ -44,7 +58,7 @@ struct NormArgs {
     Elem type, param;
 };
 void launch_layer_norm(const NormArgs &a, hipStream_t st);
-// at most min(n, kNormBackBlocks) partial rows are written
+// at most norm_back_blocks(n, d) partial rows are written
 void launch_layer_norm_backward(const NormArgs &a, hipStream_t st);
 
 // ------------------------------------------------------- orthogonalised update
