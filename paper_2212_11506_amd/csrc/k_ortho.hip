@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256) void orth_norm_kernel(OrthArgs a, char *ws, in
     const uint32_t across = uint32_t((a.cols + 7) / 8), total = across * uint32_t(a.rows); // < 2^29
     for (uint32_t e = blockIdx.x * 256 + threadIdx.x; e < total; e += gridDim.x * 256) {
         const uint32_t r = e / across, c = (e - r * across) * 8;
-        const int left = int(a.cols - c);
+        const int left = a.cols - c < 8 ? int(a.cols - c) : 8;
         float g[8], m[8] = {};
         load8(static_cast<const E *>(a.G) + z * a.g_batch + r * a.g_stride + c, left, a.g_vec, g);
         if (a.M) {
@@ -930,11 +930,26 @@ size_t orth_workspace(int64_t rows, int64_t cols)
 
 namespace {
 
+// rows and matrices start on 16 bytes
+bool vectors(const void *p, int64_t stride, int64_t batch_stride, int64_t batch, int bytes)
+{
+    return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(stride * bytes) | uintptr_t(batch > 1 ? batch_stride * bytes : 0)) & 15u) == 0;
+}
+
 template <typename E, bool kSplit> void run_wide(const OrthArgs &a, const OrthSteps &steps, char *ws, hipStream_t st)
 {
     const OrthLayout L = make_orth_layout(a.rows, a.cols);
     const int norm_blocks = norm_blocks_of(a.rows, a.cols);
-    orth_norm_kernel<E><<<dim3(norm_blocks, uint32_t(a.batch)), 256, 0, st>>>(a, ws, int64_t(L.stride), L.norm);
+    // matrices without gaps are rows of rows x cols values there, whose 16-byte accesses any length of row allows
+    // (1999 x 777 fp32 with its momentum 5.8 us, by rows 11.9)
+    OrthArgs flat = a;
+    if (a.g_stride == a.cols && (!a.M || a.m_stride == a.cols)) {
+        flat.cols = flat.g_stride = flat.m_stride = a.rows * a.cols;
+        flat.rows = 1;
+        flat.g_vec = vectors(a.G, 0, a.g_batch, a.batch, elem_bytes(a.type));
+        flat.m_vec = vectors(a.M, 0, a.m_batch, a.batch, 4);
+    }
+    orth_norm_kernel<E><<<dim3(norm_blocks, uint32_t(a.batch)), 256, 0, st>>>(flat, ws, int64_t(L.stride), L.norm);
     orth_planes_kernel<E, kSplit><<<dim3(uint32_t(L.cols / kT), uint32_t(L.rows / kT), uint32_t(a.batch)), 256, 0, st>>>(
         a, ws, L, norm_blocks, steps.step[0].sx);
     run_steps<E, kSplit>(a, steps, ws, L, st);
@@ -952,12 +967,6 @@ template <typename E> void run_type(const OrthArgs &a, const OrthSteps &steps, c
     if constexpr (std::is_same<E, bf16>::value)
         if (orth_single(a.type, a.rows, a.cols)) return run_wide<E, false>(a, steps, ws, st);
     run_wide<E, true>(a, steps, ws, st);
-}
-
-// rows and matrices start on 16 bytes
-bool vectors(const void *p, int64_t stride, int64_t batch_stride, int64_t batch, int bytes)
-{
-    return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(stride * bytes) | uintptr_t(batch > 1 ? batch_stride * bytes : 0)) & 15u) == 0;
 }
 
 } // namespace

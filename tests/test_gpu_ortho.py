@@ -232,6 +232,23 @@ def test_muon_step_large(shape, dtype):
     assert err <= TOL[dtype] * lr * scale * float(step.norm()) + 4 * half * float(want.norm())
 
 
+@pytest.mark.parametrize("shape,dtype", [((101, 77), torch.float32), ((65, 131), torch.bfloat16), ((67, 33), torch.float16)])
+def test_muon_step_batch_without_gaps(shape, dtype):
+    """Matrices that follow one another, of an odd number of values: each starts at another alignment."""
+    W, G, M = gauss(3, *shape, seed=1, dtype=dtype, scale=0.1), gauss(3, *shape, seed=2, dtype=dtype), gauss(3, *shape, seed=3)
+    mu = 0.9
+    scale = max(1.0, shape[0] / shape[1]) ** 0.5  # where none is given
+    Mw = mu * M.double() + G.double()
+    steps = [scale * plain_there(G[k].double() + mu * Mw[k]).to(DEV) for k in range(3)]
+    want = [W[k].double() - 0.5 * steps[k] for k in range(3)]
+    bh.muon_step(W, G, M, 0.5, mu, nesterov=True)
+    assert float((M.double() - Mw).abs().max()) <= 4 * 2.0 ** -24 * float(Mw.abs().max() + G.double().abs().max())
+    half = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}[dtype]
+    for k in range(3):
+        err = float((W[k].double() - want[k]).norm())
+        assert err <= TOL[dtype] * 0.5 * float(steps[k].norm()) + 4 * half * float(want[k].norm())
+
+
 def test_muon_steps_in_a_graph_and_on_another_stream():
     shape = (192, 130)
     W0, G, M0 = gauss(*shape, seed=1, scale=0.1), gauss(*shape, seed=2), gauss(*shape, seed=3)
