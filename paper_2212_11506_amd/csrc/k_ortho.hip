@@ -231,9 +231,31 @@ __device__ inline int xcd_tile(int b, int blocks)
     return x * q + (x < r ? x : r) + b / 8;
 }
 
+// What a product's blocks take.  The first 64 bytes are what the loop waits for: one line of the arguments, with the
+// pointers and quotients made on the host, so that the first loads are on their way early (1024 x 1024
+// bf16 127 us a pass against 131, 512 x 512 71 against 75).
+struct alignas(64) OrthProduct {
+    const f16 *P, *Q;         // of the first matrix
+    int64_t stride;           // bytes between matrices
+    int64_t p_plane, q_plane; // values between high and low halves
+    int32_t K, p_rows, q_rows; // padded
+    int32_t tiles, across;    // of a matrix, and of four rows of tiles (not of symmetric products)
+    uint32_t per_four;        // 2^32 / across rounded up: t across < 2^32 for every tile t
+    f16 *out, *out_t;         // C and its transpose in planes
+    const f16 *old;           // A of kPoly, X of kApply and kLast
+    int64_t out_plane;
+    int32_t ld, ld_t;
+    float f_c, f_old, f_one;  // C becomes f_c C + f_old old + f_one I
+    // kLast: the weights, or the output
+    float keep, rate;
+    int32_t update, rows, cols;
+    void *W;
+    int64_t w_batch, w_stride;
+};
+
 // E: elements of the output of kLast
 template <typename T, bool kSplit, Prod kProd, typename E>
-__global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, char *ws, OrthLayout L, int k, OrthStep S, float next_sx)
+__global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a)
 {
     constexpr int kPlanes = kSplit ? 2 : 1;
     constexpr int kPlane = (T::kM + T::kN) * kK;           // values of a staged plane: P's rows, then Q's
@@ -241,39 +263,31 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, c
     constexpr bool kSymmetric = kProd == Prod::kGram || kProd == Prod::kPoly;
     extern __shared__ __align__(16) char s_mem[];
     f16 *ring = reinterpret_cast<f16 *>(s_mem);
-    const bool wide = a.rows <= a.cols;
-    char *base = ws + int64_t(blockIdx.z) * L.stride;
-    const int64_t plane = L.rows * L.cols, square = L.m * L.m;
-    f16 *U = reinterpret_cast<f16 *>(base + L.u[k & 1]), *V = reinterpret_cast<f16 *>(base + L.v[k & 1]);
-    f16 *A = reinterpret_cast<f16 *>(base + L.a), *B = reinterpret_cast<f16 *>(base + L.b);
+    const int64_t shift = int64_t(blockIdx.z) * (a.stride / int64_t(sizeof(f16)));
+    const f16 *P = a.P + shift, *Q = a.Q + shift;
+    const int K = a.K, p_rows = a.p_rows, q_rows = a.q_rows;
     int bi, bj;
-    const f16 *P, *Q;
-    int64_t p_plane, q_plane;
-    int K;
-    const int t = xcd_tile(blockIdx.x, gridDim.x);
+    const int t = xcd_tile(blockIdx.x, a.tiles);
     if constexpr (kSymmetric) {
         // tiles on and below the diagonal, row by row
-        bi = int((sqrtf(8.0f * float(t) + 1.0f) - 1.0f) * 0.5f);
+        bi = int((__builtin_amdgcn_sqrtf(8.0f * float(t) + 1.0f) - 1.0f) * 0.5f);
         while ((bi + 1) * (bi + 2) / 2 <= t) ++bi;
         while (bi * (bi + 1) / 2 > t) --bi;
         bj = t - bi * (bi + 1) / 2;
-        P = Q = kProd == Prod::kGram ? (wide ? U : V) : A;
-        K = int(kProd == Prod::kGram ? L.n : L.m);
-        p_plane = q_plane = kProd == Prod::kGram ? plane : square;
     } else {
         // four rows of tiles at a time, column by column
-        const int across = (int(L.cols) + T::kN - 1) / T::kN, down = (int(L.rows) + T::kM - 1) / T::kM;
-        const int group = t / (4 * across), top = group * 4, high = down - top < 4 ? down - top : 4;
-        const int in = t - group * 4 * across;
-        bi = top + in % high;
-        bj = in / high;
-        P = wide ? B : U;
-        Q = wide ? V : B;
-        K = int(L.m);
-        p_plane = wide ? square : plane;
-        q_plane = wide ? plane : square;
+        const int down = (p_rows + T::kM - 1) / T::kM;
+        const int group = int(__umulhi(uint32_t(t), a.per_four)), top = group * 4;
+        const int in = t - group * a.across;
+        if (down - top >= 4) {
+            bi = top + in % 4;
+            bj = in / 4;
+        } else {
+            const int high = down - top;
+            bi = top + in % high;
+            bj = in / high;
+        }
     }
-    const int p_rows = int(kSymmetric ? L.m : L.rows), q_rows = int(kSymmetric ? L.m : L.cols);
     const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id();
 
     // this lane's piece of each group of eight rows that the wave loads
@@ -286,7 +300,7 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, c
         const int most = (in_p ? p_rows : q_rows) - 1;
         at = at < most ? at : most;
         src[e] = (in_p ? P : Q) + int64_t(at) * K + ((lane % 8) ^ (lane / 8)) * 8;
-        if constexpr (kSplit) src[T::kEach + e] = src[e] + (in_p ? p_plane : q_plane);
+        if constexpr (kSplit) src[T::kEach + e] = src[e] + (in_p ? a.p_plane : a.q_plane);
     }
     const int slices = K / kK;
     const auto fetch = [&](int slice) {
@@ -353,21 +367,11 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, c
     // Each wave puts its blocks through a patch of its own in LDS, for rows of 16 bytes in either orientation
     constexpr int kDown = 16 * T::kHigh, kAcross = 16 * T::kJ;
     float *patch = reinterpret_cast<float *>(s_mem) + w * kDown * T::kPatch;
-    f16 *out = nullptr, *out_t = nullptr;
-    int64_t ld = 0, ld_t = 0, out_plane = 0;
-    if constexpr (kSymmetric) {
-        out = out_t = kProd == Prod::kGram ? A : B;
-        ld = ld_t = L.m;
-        out_plane = square;
-    } else if constexpr (kProd == Prod::kApply) {
-        out = reinterpret_cast<f16 *>(base + L.u[(k + 1) & 1]);
-        out_t = reinterpret_cast<f16 *>(base + L.v[(k + 1) & 1]);
-        ld = L.cols;
-        ld_t = L.rows;
-        out_plane = plane;
-    }
+    f16 *out = a.out + shift, *out_t = a.out_t + shift;
+    const f16 *old = a.old + shift;
+    const int64_t ld = a.ld, ld_t = a.ld_t, out_plane = a.out_plane;
     // single products keep a low plane for a X alone, of 8 bits
-    const int8_t *u_low = reinterpret_cast<const int8_t *>(U + plane);
+    const int8_t *u_low = reinterpret_cast<const int8_t *>(old + out_plane);
 #pragma unroll
     for (int i0 = 0; i0 < T::kI; i0 += T::kHigh) {
         const int r0 = bi * T::kM + wi + 16 * i0, c0 = bj * T::kN + wj;
@@ -385,10 +389,10 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, c
                 const int row = s / T::kJ * 4 + lane / 16, col = s % T::kJ * 16 + lane % 16;
                 const int64_t r = r0 + row, c = c0 + col;
                 if (r >= a.rows || c >= a.cols) continue;
-                float v = patch[row * T::kPatch + col] * (1.0f / (S.sb * S.sx));
-                if constexpr (!kSplit) v += (S.a / S.sx) * unpack_low(u_low[r * L.cols + c], U[r * L.cols + c]);
+                float v = patch[row * T::kPatch + col] * a.f_c;
+                if constexpr (!kSplit) v += a.f_old * unpack_low(u_low[r * ld + c], old[r * ld + c]);
                 E *o = static_cast<E *>(a.W) + int64_t(blockIdx.z) * a.w_batch + r * a.w_stride + c;
-                *o = E(a.M ? a.keep * float(*o) - a.rate * v : v);
+                *o = E(a.update ? a.keep * float(*o) - a.rate * v : v);
             }
             continue;
         }
@@ -402,24 +406,24 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthArgs a, c
             half8 h, l, xh, xl;
             byte8 q, xq;
             if constexpr (kProd == Prod::kPoly) {
-                xh = *reinterpret_cast<const half8 *>(A + at);
-                if constexpr (kSplit) xl = *reinterpret_cast<const half8 *>(A + square + at);
+                xh = *reinterpret_cast<const half8 *>(old + at);
+                if constexpr (kSplit) xl = *reinterpret_cast<const half8 *>(old + out_plane + at);
             } else if constexpr (kProd == Prod::kApply && !kSplit) {
-                xh = *reinterpret_cast<const half8 *>(U + at);
+                xh = *reinterpret_cast<const half8 *>(old + at);
                 xq = *reinterpret_cast<const byte8 *>(u_low + at);
             }
 #pragma unroll
             for (int x8 = 0; x8 < 8; ++x8) {
                 float x = v[x8];
                 if constexpr (kProd == Prod::kGram) {
-                    x *= S.sa / (S.sx * S.sx);
+                    x *= a.f_c;
                 } else if constexpr (kProd == Prod::kPoly) {
                     const float av = kSplit ? float(xh[x8]) + float(xl[x8]) : float(xh[x8]);
-                    x = av * (S.b * S.sb / S.sa) + x * (S.c * S.sb / (S.sa * S.sa));
-                    if (kSplit && r0 + row == c0 + col + x8) x += S.a * S.sb;
+                    x = av * a.f_old + x * a.f_c;
+                    if (kSplit && r0 + row == c0 + col + x8) x += a.f_one;
                 } else {
-                    x *= next_sx / (S.sb * S.sx);
-                    if constexpr (!kSplit) x += (S.a * next_sx / S.sx) * unpack_low(xq[x8], xh[x8]);
+                    x *= a.f_c;
+                    if constexpr (!kSplit) x += a.f_old * unpack_low(xq[x8], xh[x8]);
                 }
                 f16 vh, vl;
                 split(x, vh, vl);
@@ -461,16 +465,60 @@ void run_product(const OrthArgs &a, const OrthSteps &steps, char *ws, const Orth
     constexpr size_t kPatches = size_t(T::kWaves) * 16 * T::kHigh * T::kPatch * sizeof(float);
     constexpr size_t kLds = kRing > kPatches ? kRing : kPatches;
     static_assert(kLds <= 160 * 1024, "LDS of a CU");
-    uint32_t tiles;
+    const auto at = [&](size_t bytes) { return reinterpret_cast<f16 *>(ws + bytes); };
+    f16 *U = at(L.u[k & 1]), *V = at(L.v[k & 1]), *A = at(L.a), *B = at(L.b);
+    const OrthStep &S = steps.step[k];
+    const float next_sx = k + 1 < steps.count ? steps.step[k + 1].sx : 1.0f;
+    const bool wide = a.rows <= a.cols;
+    const int64_t plane = L.rows * L.cols, square = L.m * L.m;
+    OrthProduct p = {};
+    p.stride = int64_t(L.stride);
     if constexpr (kProd == Prod::kGram || kProd == Prod::kPoly) {
         static_assert(T::kM == T::kN, "symmetric products");
-        const uint32_t mt = uint32_t((L.m + T::kM - 1) / T::kM);
-        tiles = mt * (mt + 1) / 2;
+        const int32_t mt = int32_t((L.m + T::kM - 1) / T::kM);
+        p.tiles = mt * (mt + 1) / 2;
+        p.P = p.Q = kProd == Prod::kPoly ? A : wide ? U : V;
+        p.K = int32_t(kProd == Prod::kPoly ? L.m : L.n);
+        p.p_plane = p.q_plane = kProd == Prod::kPoly ? square : plane;
+        p.p_rows = p.q_rows = p.ld = p.ld_t = int32_t(L.m);
+        p.out = p.out_t = kProd == Prod::kGram ? A : B;
+        p.out_plane = square;
+        p.old = A;
+        if constexpr (kProd == Prod::kGram) {
+            p.f_c = S.sa / (S.sx * S.sx);
+        } else {
+            p.f_c = S.c * S.sb / (S.sa * S.sa);
+            p.f_old = S.b * S.sb / S.sa;
+            p.f_one = S.a * S.sb;
+        }
     } else {
-        tiles = uint32_t((L.rows + T::kM - 1) / T::kM) * uint32_t((L.cols + T::kN - 1) / T::kN);
+        const int32_t across = int32_t((L.cols + T::kN - 1) / T::kN);
+        p.tiles = int32_t((L.rows + T::kM - 1) / T::kM) * across;
+        p.across = 4 * across;
+        p.per_four = uint32_t(((uint64_t(1) << 32) + p.across - 1) / p.across);
+        p.P = wide ? B : U;
+        p.Q = wide ? V : B;
+        p.K = int32_t(L.m);
+        p.p_plane = wide ? square : plane;
+        p.q_plane = wide ? plane : square;
+        p.p_rows = p.ld_t = int32_t(L.rows);
+        p.q_rows = p.ld = int32_t(L.cols);
+        p.out = at(L.u[(k + 1) & 1]);
+        p.out_t = at(L.v[(k + 1) & 1]);
+        p.out_plane = plane;
+        p.old = U;
+        p.f_c = next_sx / (S.sb * S.sx);
+        p.f_old = S.a * next_sx / S.sx;
+        p.keep = a.keep;
+        p.rate = a.rate;
+        p.update = a.M != nullptr;
+        p.rows = int32_t(a.rows);
+        p.cols = int32_t(a.cols);
+        p.W = a.W;
+        p.w_batch = a.w_batch;
+        p.w_stride = a.w_stride;
     }
-    orth_product_kernel<T, kSplit, kProd, E><<<dim3(tiles, 1, uint32_t(a.batch)), T::kThreads, kLds, st>>>(
-        a, ws, L, k, steps.step[k], k + 1 < steps.count ? steps.step[k + 1].sx : 1.0f);
+    orth_product_kernel<T, kSplit, kProd, E><<<dim3(uint32_t(p.tiles), 1, uint32_t(a.batch)), T::kThreads, kLds, st>>>(p);
 }
 
 // The tiles, each the best of several numbers of waves and buffers in the whole chain of products (whose operands come
