@@ -7,10 +7,11 @@
 // Both passes move each element once (two or three of them) for about ten
 // operations: HBM bounds them.  A row is held in the registers of a team of
 // 2^k lanes of a wave (up to 1024 features at 16 a lane), or of a whole block
-// (up to 16384), so that the mean, the centred sum of squares and the outputs
-// come from one read; the next row's loads are in flight while a row is
-// computed.  All sums are fp32 (the weight gradients' last join fp64); the only
-// rounding to fewer bits is that of the outputs.
+// (up to 16384; backward, with two rows and the weights' sums, half of both),
+// so that the mean, the centred sum of squares and the outputs come from one
+// read; the next row's loads are in flight while a row is computed.  All sums
+// are fp32 (the weight gradients' last join fp64); the only rounding to fewer
+// bits is that of the outputs.
 #include <type_traits>
 
 #include "map.hpp"
@@ -23,8 +24,8 @@ template <typename E, int VEC> struct alignas(sizeof(E) * VEC) Pack {
 };
 
 // kStream: 16-byte accesses of rows that do not stay in the caches (kNormStream) leave no lines behind: backward of
-// 1.3M x 128 bf16 183 us against 193, forward of 1.3M x 256 271 against 292.  Narrower ones come back to their lines
-// and lose by it (70k x 500 by 8 bytes 52 us against 45).
+// 1.3M x 128 bf16 180 us against 194, forward of 1.3M x 256 257 against 278.  Narrower ones come back to their lines
+// and lose by it (70k x 500 by 8 bytes 52 us against 45, both before the parameters came by vectors).
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 template <bool kStream, typename E, int VEC> __device__ inline Pack<E, VEC> load_pack(const E *p)
 {
@@ -187,6 +188,8 @@ template <int VEC> struct Columns {
 };
 
 // ------------------------------------------------------------------ forward
+// One read and one write of a row.  70k x 777 fp32 82 us, 5.3 TB/s of HBM; 1.3M x 256 bf16 257 us, 5.2.  Short rows are
+// bound by the issue of two row sums each: 1.3M x 50 fp16 69 us, 3.8 TB/s.  One row of 512: 2.4 us, a launch's latency.
 template <typename E, int VEC, int NV, bool kStream>
 __global__ __launch_bounds__(kNormMaxThreads) void norm_kernel(NormArgs a, int team)
 {
@@ -256,7 +259,8 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_kernel(NormArgs a, int t
     }
 }
 
-// rows longer than a block's registers: one block a row, three passes over it
+// rows longer than a block's registers: one block a row, three passes over it, the last two from the caches at the rate
+// of these (2000 x 20000 fp32 130 us, 2.5 TB/s)
 template <typename E, int VEC, bool kWide>
 __global__ __launch_bounds__(kNormMaxThreads) void norm_long_kernel(NormArgs a)
 {
@@ -310,6 +314,8 @@ template <bool kWide> __device__ inline void finish(const NormArgs &a)
 
 // Each team keeps the sums of its rows' dy xh and dy in registers; a block's
 // teams are joined in LDS, in order, into one partial row [2][d] of the block.
+// 1.3M x 256 bf16 334 us, 6.0 TB/s of HBM; 70001 x 500 bf16 by 8 bytes 38 us,
+// 5.6, part of it from the last cache; 2000 x 128 fp32 4.2 us, latency.
 template <typename E, int VEC, int NV, bool kStream>
 __global__ __launch_bounds__(kNormMaxThreads) void norm_back_kernel(NormArgs a, int team)
 {
@@ -476,7 +482,8 @@ template <typename E> __global__ __launch_bounds__(256) void norm_back_columns_k
 }
 
 // Joins the blocks' partial rows: 32 columns and 32 strands of partial rows a
-// block; sums in fp64 and in a fixed order, whatever the blocks' timing.
+// block; sums in fp64 and in a fixed order, whatever the blocks' timing.  Bound
+// by latency: 250 rows of 2 x 128 4.2 us, 1024 of 2 x 256 5.2.
 constexpr int kJoinCols = 32, kJoinStrands = 32;
 template <bool kWide>
 __global__ __launch_bounds__(kJoinCols *kJoinStrands) void norm_join_kernel(const float *part, int blocks, int64_t d,
@@ -515,12 +522,13 @@ int vector_of(const NormArgs &a)
     return int((bits & (~bits + 1)) / e);
 }
 
-// How a row is shared out.  A lane does best with four features and a few vectors: more rows a wave pass through
-// the row sums together, and loads still cover whole lines (1.3M x 50 fp16: 16 lanes of 2 x 2 features 69 us, 32 of
-// 2 features 99, 8 of 4 x 2 87; 2M x 7 fp32: 4 lanes 30 us, 8 lanes 37, 2 lanes 41).  Where rows are too few to fill the
-// chip, one vector a lane (2000 x 128 fp32 3.5 us against 4.1).  `most`: features of a lane, 16 forward and 8 backward,
-// whose sums take the registers (16 there spill: 300k x 255 fp32 540 us against 170).
-Shape shape_of(int vec, int64_t n, int64_t d, int most)
+// How a row is shared out.  A lane does best with some four features and a few vectors (`some`): more rows a wave pass
+// through the row sums together, and loads still cover whole lines (1.3M x 50 fp16: 16 lanes of 2 x 2 features 69 us, 32
+// of 2 features 101, 64 of 1 187; 2M x 7 fp32: 4 lanes 23 us, 8 lanes 31, 2 lanes 26), backward with 16 bytes (1.3M x 50
+// fp16 by eight 101 us, by four 109; 1.3M x 128 fp32 by four 362, by eight 387).  Where rows are too few to fill the
+// chip, one vector a lane (2000 x 128 fp32 3.6 us against 3.7).  `most`: features of a lane, 16 forward and 8 backward,
+// whose sums take the registers (16 there spill: 300k x 255 fp32 540 us against 190).
+Shape shape_of(int vec, int64_t n, int64_t d, int some, int most)
 {
     const auto power = [](int64_t x) {
         int p = 1;
@@ -530,7 +538,7 @@ Shape shape_of(int vec, int64_t n, int64_t d, int most)
     Shape s;
     s.vec = vec;
     const int64_t vecs = (d + vec - 1) / vec;
-    const int few = n <= kNormFewRows ? vec : vec > 4 ? vec : 4;
+    const int few = n <= kNormFewRows || vec > some ? vec : some;
     int64_t team = power((d + few - 1) / few);
     const int64_t least = power(vecs < 4 ? vecs : 4);
     if (team < least) team = least;
@@ -637,7 +645,7 @@ Shape shape_of(const NormArgs &a, bool back)
     // Few rows are shared out over more lanes forward too (8000 x 1000 fp32 11.4 us against 13.2), which no longer pays
     // for long ones (8000 x 3333 bf16 34.1 us against 30.4)
     const bool narrow = back || (a.n <= kNormFewRows && a.d <= kNormFewFeatures);
-    Shape s = shape_of(vector_of(a), a.n, a.d, narrow ? kNormLaneBack : kNormLane);
+    Shape s = shape_of(vector_of(a), a.n, a.d, back ? 16 / elem_bytes(a.type) : 4, narrow ? kNormLaneBack : kNormLane);
     // Few rows backward: one large block goes over them in less than the launch takes that joins several (250 x 128
     // fp32 12.4 us a call against 14.8; a row of several waves takes 2 us a round, 8 x 4000 bf16 17.5 against 14.7)
     const int rows = s.team <= kWave ? kNormMaxThreads / s.team : 1;
