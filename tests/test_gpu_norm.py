@@ -242,6 +242,27 @@ def test_starts_off_every_alignment(d, dtype):
     check_backward(dy, x, w, got[1], got[2], back)
 
 
+@pytest.mark.parametrize("ptype", TYPES)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [8, 50, 96, 504, 1000, 2000])
+def test_parameters_off_every_alignment(d, dtype, ptype):
+    """Weights and biases that start anywhere give what aligned copies of them give, alone and together."""
+    if ptype != dtype and ptype != torch.float32:
+        return  # parameters are fp32 or of x's type
+    x, dy = rows(37, d, dtype, 1), rows(37, d, dtype, 2, 0, 0.1, 0.01)
+    w, b = vec(d + 8, ptype, 3, 1.0, 0.2), vec(d + 8, ptype, 4, 0.0, 0.1)
+    for i, j in ((1, 1), (2, 3), (4, 2), (7, 0), (0, 5)):
+        wi, bj = w[i:i + d], b[j:j + d]
+        wc, bc = wi.clone(), bj.clone()
+        for ww, bb, wa, ba in ((wi, bj, wc, bc), (wi, None, wc, None), (None, bj, None, bc)):
+            got, want = bh.layer_norm(x, ww, bb), bh.layer_norm(x, wa, ba)
+            assert all(torch.equal(p, q) for p, q in zip(got, want))
+        check_forward(x, wi, bj, bh.layer_norm(x, wi, bj, eps=EPS))
+        mean, rstd = want[1:]
+        assert all(torch.equal(p, q) for p, q in zip(bh.layer_norm_backward(dy, x, wi, mean, rstd),
+                                                     bh.layer_norm_backward(dy, x, wc, mean, rstd)))
+
+
 def test_arrays_beyond_the_caches():
     """Rows of a 280 MB array, which are read and written past the caches, come out as they do in parts."""
     n, d = 550_000, 256
