@@ -806,11 +806,13 @@ __global__ __launch_bounds__(narrow_waves(MT) *kWave) void orth_narrow_kernel(Or
             if (k < kSure || 4 * k < m) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(x[k], y[k], acc, 0, 0, 0);
         return acc;
     };
+    // Both places of a pair take the one value below the diagonal: the products read rows for columns, so a difference
+    // between the two, be it of a rounding, would grow (by 40 a step where A has no direction: 1.4 after 12 steps)
     const auto store = [&](double *P, int t, const double4v &v) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int row = 16 * Lower<MT>::row(t) + tile_row(r), col = 16 * Lower<MT>::col(t) + tile_col();
-            P[row * kLd + col] = P[col * kLd + row] = v[r];
+            if (row >= col) P[row * kLd + col] = P[col * kLd + row] = v[r];
         }
     };
     constexpr int kOne = (kTiles + kNarrowWaves - 1) / kNarrowWaves, kTwo = (2 * kTiles + kNarrowWaves - 1) / kNarrowWaves;

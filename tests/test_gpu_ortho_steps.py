@@ -1,0 +1,68 @@
+"""Newton-Schulz steps of matrices of few directions and of low rank, against the recurrence on X itself in 64 bits.
+
+Inputs here are of rank 1 to 5, rounded to their type, with rows that are equal, and gaussian ones.
+
+Tolerances: both sides compute in 64 bits.  Their rounding, some 2^-50, grows with the input's own smallest directions,
+which for a product rounded to 24 bits lie at 1e-9 of its norm or above: 2^-50 / 1e-9 = 1e-6 of these, and ten times that for
+the spread of directions.  Equal rows stay equal where every row's sums run in the same order, as they do on both
+sides.  Then the output's own rounding, half a unit in its last place at most."""
+import pytest
+import torch
+
+import paper_2212_11506_amd as bh
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+COEF = (3.4445, -4.7750, 2.0315)
+HALF = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+
+
+def by_rows(P, Q):
+    """P Q with every row's sums in one order."""
+    return torch.stack([(p[:, None] * Q).sum(0) for p in P])
+
+
+def on_x(G, steps, coef=COEF, eps=1e-7):
+    G = G.double().cpu()
+    X = G.t().contiguous() if G.shape[0] > G.shape[1] else G
+    X = X / (X.square().sum().sqrt() + eps)
+    for k in range(steps):
+        a, b, c = coef[k] if hasattr(coef[0], "__len__") else coef
+        A = torch.stack([(x * X).sum(1) for x in X])
+        X = a * X + by_rows(b * A + c * by_rows(A, A), X)
+    return X.t() if G.shape[0] > G.shape[1] else X
+
+
+def matrix(kind, rows, cols, dtype):
+    g = torch.Generator().manual_seed(rows * 7919 + cols)
+    if kind == "ones":
+        G = torch.ones(rows, cols)
+    elif kind == "equal rows":
+        G = torch.randn(1, cols, generator=g).expand(rows, cols)
+    elif kind == "gauss":
+        G = torch.randn(rows, cols, generator=g)
+    else:
+        G = torch.randn(rows, kind, generator=g) @ torch.randn(kind, cols, generator=g)
+    return G.to(dtype).to(DEV)
+
+
+def rel(got, want):
+    got = got.double().cpu()
+    return float((got - want).norm() / want.norm())
+
+
+# of one launch's size and of two launches', wide and tall
+CASES = [(1, 32, 100), (5, 50, 256), (3, 40, 1500), (2, 700, 48), ("ones", 64, 64), ("ones", 16, 5000), ("equal rows", 2, 128),
+         ("equal rows", 9, 2500), ("gauss", 20, 300), ("gauss", 64, 65)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("steps", [6, 7, 8, 9])
+@pytest.mark.parametrize("kind,rows,cols", CASES)
+def test_steps_of_low_rank(kind, rows, cols, steps, dtype):
+    G = matrix(kind, rows, cols, dtype)
+    want = on_x(G, steps)
+    got = bh.orthogonalise(G, steps=steps)
+    print(f"[orth] {kind} {rows}x{cols} {steps} steps {dtype} {rel(got, want):.1e}", flush=True)
+    assert bool(torch.isfinite(got).all())
+    assert rel(got, want) <= 1e-5 + HALF[dtype]
