@@ -75,9 +75,9 @@ bool plan_steps(const double *coefficients, int steps, OrthSteps *plan)
         for (double t : roots)
             if (t > 0.0 && t < t1) x = std::fmax(x, next(t));
         OrthStep &s = plan->step[k];
-        s.a = float(q[0]);
-        s.b = float(q[1]);
-        s.c = float(q[2]);
+        s.a = q[0];
+        s.b = q[1];
+        s.c = q[2];
         s.sx = power_of_two_below(kRoom / std::fmax(most, 1.0));
         s.sa = power_of_two_below(kRoom / std::fmax(t1, 1.0));
         s.sb = power_of_two_below(kRoom / std::fmax(b + std::fabs(q[0]), 1.0));

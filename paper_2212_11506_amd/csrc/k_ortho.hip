@@ -495,9 +495,9 @@ void run_product(const OrthArgs &a, const OrthSteps &steps, char *ws, const Orth
         if constexpr (kProd == Prod::kGram) {
             p.f_c = S.sa / (S.sx * S.sx);
         } else {
-            p.f_c = S.c * S.sb / (S.sa * S.sa);
-            p.f_old = S.b * S.sb / S.sa;
-            p.f_one = S.a * S.sb;
+            p.f_c = float(S.c * S.sb / (double(S.sa) * S.sa));
+            p.f_old = float(S.b * S.sb / S.sa);
+            p.f_one = float(S.a * S.sb);
         }
     } else {
         const int32_t across = int32_t((L.cols + T::kN - 1) / T::kN);
@@ -516,7 +516,7 @@ void run_product(const OrthArgs &a, const OrthSteps &steps, char *ws, const Orth
         p.out_plane = plane;
         p.old = U;
         p.f_c = next_sx / (S.sb * S.sx);
-        p.f_old = S.a * next_sx / S.sx;
+        p.f_old = float(S.a * next_sx / S.sx);
         p.keep = a.keep;
         p.rate = a.rate;
         p.update = a.M != nullptr;
@@ -629,6 +629,13 @@ template <int MT> struct Lower {
 
 enum class Narrow { kWhole, kGram, kApply };
 
+struct NarrowSteps {
+    int count;
+    struct Step {
+        double a, b, c;
+    } step[kOrthMaxSteps];
+};
+
 template <int MT> constexpr int narrow_matrix() { return 16 * MT * (16 * MT + 2); } // doubles: 16 rows apart on all banks
 template <int MT, Narrow kMode> constexpr size_t narrow_lds(int width)
 {
@@ -638,7 +645,7 @@ template <int MT, Narrow kMode> constexpr size_t narrow_lds(int width)
 }
 
 template <typename E, int MT, Narrow kMode>
-__global__ __launch_bounds__(narrow_waves(MT) *kWave) void orth_narrow_kernel(OrthArgs a, OrthSteps steps, char *ws, NarrowLayout L, int width, int shift)
+__global__ __launch_bounds__(narrow_waves(MT) *kWave) void orth_narrow_kernel(OrthArgs a, NarrowSteps steps, char *ws, NarrowLayout L, int width, int shift)
 {
     constexpr int kNarrowWaves = narrow_waves(MT), kNarrowBlock = kNarrowWaves * kWave;
     constexpr int kM = 16 * MT, kLd = kM + 2, kTiles = Lower<MT>::kTiles, kParts = Lower<MT>::kParts;
@@ -817,7 +824,7 @@ __global__ __launch_bounds__(narrow_waves(MT) *kWave) void orth_narrow_kernel(Or
     };
     constexpr int kOne = (kTiles + kNarrowWaves - 1) / kNarrowWaves, kTwo = (2 * kTiles + kNarrowWaves - 1) / kNarrowWaves;
     for (int s = 0; s < steps.count; ++s) {
-        const OrthStep &S = steps.step[s];
+        const NarrowSteps::Step &S = steps.step[s];
         const bool last = s + 1 == steps.count;
         // B = a I + b A + c A^2, and the first Q
 #pragma unroll
@@ -828,7 +835,7 @@ __global__ __launch_bounds__(narrow_waves(MT) *kWave) void orth_narrow_kernel(Or
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int row = 16 * Lower<MT>::row(t) + tile_row(r), col = 16 * Lower<MT>::col(t) + tile_col();
-                v[r] = double(S.b) * A[row * kLd + col] + double(S.c) * v[r] + (row == col ? double(S.a) : 0.0);
+                v[r] = S.b * A[row * kLd + col] + S.c * v[r] + (row == col ? S.a : 0.0);
             }
             store(B, t, v);
             if (s == 0) store(Q, t, v);
@@ -907,7 +914,7 @@ int log2_of(int x)
     return s;
 }
 
-template <typename E, int MT> void run_narrow(const OrthArgs &a, const OrthSteps &steps, char *ws, const NarrowLayout &L, hipStream_t st)
+template <typename E, int MT> void run_narrow(const OrthArgs &a, const NarrowSteps &steps, char *ws, const NarrowLayout &L, hipStream_t st)
 {
     constexpr int kBlock = narrow_waves(MT) * kWave;
     const int shift = log2_of(L.width);
@@ -1019,10 +1026,13 @@ template <typename E> void run_type(const OrthArgs &a, const OrthSteps &steps, c
 {
     if (orth_narrow(a.rows, a.cols)) {
         const NarrowLayout L = make_narrow_layout(a.rows, a.cols);
-        if (L.tiles == 1) return run_narrow<E, 1>(a, steps, ws, L, st);
-        if (L.tiles == 2) return run_narrow<E, 2>(a, steps, ws, L, st);
-        if (L.tiles == 3) return run_narrow<E, 3>(a, steps, ws, L, st);
-        return run_narrow<E, 4>(a, steps, ws, L, st);
+        NarrowSteps narrow;
+        narrow.count = steps.count;
+        for (int k = 0; k < steps.count; ++k) narrow.step[k] = {steps.step[k].a, steps.step[k].b, steps.step[k].c};
+        if (L.tiles == 1) return run_narrow<E, 1>(a, narrow, ws, L, st);
+        if (L.tiles == 2) return run_narrow<E, 2>(a, narrow, ws, L, st);
+        if (L.tiles == 3) return run_narrow<E, 3>(a, narrow, ws, L, st);
+        return run_narrow<E, 4>(a, narrow, ws, L, st);
     }
     if constexpr (std::is_same<E, bf16>::value)
         if (orth_single(a.type, a.rows, a.cols)) return run_wide<E, false>(a, steps, ws, st);

@@ -70,7 +70,7 @@ constexpr int kOrthNormBlocks = 512; // partial sums of squares of a matrix
 constexpr int64_t kOrthMaxSide = 65536;
 
 struct OrthStep {
-    float a, b, c;     // X' = a X + (b A + c A A) X
+    double a, b, c;    // X' = a X + (b A + c A A) X
     float sx, sa, sb;  // powers of two: scales of X, A and B (the polynomial) in this step
 };
 

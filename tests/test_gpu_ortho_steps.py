@@ -66,3 +66,13 @@ def test_steps_of_low_rank(kind, rows, cols, steps, dtype):
     print(f"[orth] {kind} {rows}x{cols} {steps} steps {dtype} {rel(got, want):.1e}", flush=True)
     assert bool(torch.isfinite(got).all())
     assert rel(got, want) <= 1e-5 + HALF[dtype]
+
+
+@pytest.mark.parametrize("steps", [5, 9])
+@pytest.mark.parametrize("rows,cols", [(20, 300), (64, 100), (33, 900)])
+def test_coefficients_are_taken_as_given(rows, cols, steps):
+    """Coefficients are doubles: in fp32 (1e-8 of them) their rounding would be three times the output's."""
+    G = matrix("gauss", rows, cols, torch.float32)
+    r = rel(bh.orthogonalise(G, steps=steps), on_x(G, steps))
+    print(f"[orth] {rows}x{cols} {steps} steps {r:.1e}", flush=True)
+    assert r <= 2.0 ** -24 + 2.0 ** -27
