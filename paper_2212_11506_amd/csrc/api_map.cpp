@@ -50,6 +50,19 @@ bool apart(const bhtsne_matrices *x, int64_t batch, int64_t rows, int64_t cols)
 
 float power_of_two_below(double x) { return float(std::exp2(std::floor(std::log2(x)))); }
 
+// By how much a step on A multiplies a small error of A at most: the largest derivative of t B(t)^2, which takes an
+// eigenvalue t of A to the next, B(t) = a + b t + c t^2; `most` bounds t.
+double growth(const double *q, double most)
+{
+    constexpr int kPoints = 16;
+    double g = 0.0;
+    for (int i = 0; i <= kPoints; ++i) {
+        const double t = most * i / kPoints, b = q[0] + q[1] * t + q[2] * t * t;
+        g = std::fmax(g, std::fabs(b * (b + 2.0 * t * (q[1] + 2.0 * q[2] * t))));
+    }
+    return g;
+}
+
 // The scales of every step.  Singular values of X start in [0, 1]; `most` bounds
 // them through the steps, and with them every value of X (most), of A = X X^T
 // (most^2) and of B = a I + b A + c A^2 (|a| and b t + c t^2's largest on [0, most^2]).  Half of what fp16
@@ -57,8 +70,10 @@ float power_of_two_below(double x) { return float(std::exp2(std::floor(std::log2
 bool plan_steps(const double *coefficients, int steps, OrthSteps *plan)
 {
     constexpr double kRoom = 32768.0;
-    double most = 1.0;
+    double most = 1.0, noise = 1.0;
+    plan->noise = 1.0;
     for (int k = 0; k < steps; ++k) {
+        plan->noise = std::fmax(plan->noise, noise);
         const double usual[3] = {3.4445, -4.7750, 2.0315};
         const double *q = coefficients ? coefficients + 3 * k : usual;
         if (!std::isfinite(q[0]) || !std::isfinite(q[1]) || !std::isfinite(q[2])) return false;
@@ -83,6 +98,7 @@ bool plan_steps(const double *coefficients, int steps, OrthSteps *plan)
         s.sb = power_of_two_below(kRoom / std::fmax(b + std::fabs(q[0]), 1.0));
         if (!(x < 64.0)) return false;
         most = x;
+        noise = growth(q, t1) * noise + most * most; // and the next A's own rounding
     }
     plan->count = steps;
     return true;

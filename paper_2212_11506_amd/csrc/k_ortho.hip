@@ -907,6 +907,142 @@ __global__ __launch_bounds__(narrow_waves(MT) *kWave) void orth_narrow_kernel(Or
     }
 }
 
+// ------------------------------------------------------------------ narrow matrices, many steps
+// Stepping on A alone loses the directions that X lacks: their eigenvalues are zero but for rounding, of either sign,
+// grow by a^2 a step, and below zero without end.  Where that would show (kNarrowNoise) X itself is stepped on, in fp64:
+// X <- a X + (b A + c A^2) X with A = X X^T formed from X each time, whose errors grow by a and stay bounded, as in the
+// formula.  Two launches a step, by plain products: 32 steps of 32 x 100 fp32 take 0.75 ms, of 64 x 4096 1.7.
+// Every row's sums run in one order, so that equal rows stay equal.
+constexpr int kDirectLd = kDirect + 1;
+constexpr size_t kDirectLds = 2 * size_t(kDirect) * kDirectLd * sizeof(double);
+
+// X = U / (|U| + eps)
+template <typename E>
+__global__ __launch_bounds__(256) void orth_direct_start_kernel(OrthArgs a, char *ws, DirectLayout L, int norm_blocks)
+{
+    const int64_t z = blockIdx.y;
+    char *base = ws + z * L.stride;
+    const double *part = reinterpret_cast<const double *>(base + L.norm);
+    double sq = 0.0;
+    for (int k = lane_id(); k < norm_blocks; k += kWave) sq += part[k];
+    const double scale = 1.0 / (sqrt(wave_sum(sq)) + a.eps);
+    double *X = reinterpret_cast<double *>(base + L.x);
+    const bool wide = a.rows <= a.cols;
+    const uint32_t cols = uint32_t(a.cols), total = uint32_t(a.rows) * cols; // <= 2^22
+    for (uint32_t e = blockIdx.x * 256 + threadIdx.x; e < total; e += gridDim.x * 256) {
+        const uint32_t r = e / cols, c = e - r * cols;
+        const float g = float(static_cast<const E *>(a.G)[z * a.g_batch + r * a.g_stride + c]);
+        const float m = a.M ? a.M[z * a.m_batch + r * a.m_stride + c] : 0.0f;
+        X[wide ? int64_t(e) : c * L.n + r] = double(update_value(a, g, m)) * scale;
+    }
+}
+
+// columns j0 .. j0 + kDirect of X into LDS, zeros around them
+__device__ inline void direct_load(const double *X, const DirectLayout &L, int64_t j0, double *s_x)
+{
+    for (int e = threadIdx.x; e < kDirect * kDirect; e += 256) {
+        const int i = e / kDirect, j = e % kDirect;
+        s_x[i * kDirectLd + j] = i < L.m && j0 + j < L.n ? X[i * L.n + j0 + j] : 0.0;
+    }
+}
+
+// Partial Gram matrices: a thread has rows ty + 16 p and columns tx + 16 q of one
+__global__ __launch_bounds__(256) void orth_direct_gram_kernel(char *ws, DirectLayout L)
+{
+    extern __shared__ __align__(16) char s_mem[];
+    double *s_x = reinterpret_cast<double *>(s_mem);
+    char *base = ws + int64_t(blockIdx.y) * L.stride;
+    const double *X = reinterpret_cast<const double *>(base + L.x);
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    double acc[4][4] = {};
+    for (int64_t j0 = int64_t(blockIdx.x) * kDirect; j0 < L.n; j0 += int64_t(gridDim.x) * kDirect) {
+        __syncthreads();
+        direct_load(X, L, j0, s_x);
+        __syncthreads();
+        for (int k = 0; k < kDirect; ++k)
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    acc[p][q] = fma(s_x[(ty + 16 * p) * kDirectLd + k], s_x[(tx + 16 * q) * kDirectLd + k], acc[p][q]);
+    }
+    double *part = reinterpret_cast<double *>(base + L.gram) + int64_t(blockIdx.x) * L.m * L.m;
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (ty + 16 * p < L.m && tx + 16 * q < L.m) part[(ty + 16 * p) * L.m + tx + 16 * q] = acc[p][q];
+}
+
+// A step: every block adds up A, forms b A + c A^2 and takes its columns of X on; the last writes the output
+template <typename E>
+__global__ __launch_bounds__(256) void orth_direct_step_kernel(OrthArgs a, char *ws, DirectLayout L, NarrowSteps::Step S, bool last)
+{
+    extern __shared__ __align__(16) char s_mem[];
+    double *s_a = reinterpret_cast<double *>(s_mem), *s_x = s_a + kDirect * kDirectLd;
+    const int64_t z = blockIdx.y;
+    char *base = ws + z * L.stride;
+    double *X = reinterpret_cast<double *>(base + L.x);
+    const double *part = reinterpret_cast<const double *>(base + L.gram);
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    for (int e = threadIdx.x; e < kDirect * kDirect; e += 256) {
+        const int i = e / kDirect, j = e % kDirect;
+        double s = 0.0;
+        if (i < L.m && j < L.m)
+#pragma unroll 8
+            for (int k = 0; k < L.slices; ++k) s += part[(int64_t(k) * L.m + i) * L.m + j];
+        s_a[i * kDirectLd + j] = s;
+    }
+    __syncthreads();
+    double acc[4][4] = {};
+    for (int k = 0; k < L.m; ++k)
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                acc[p][q] = fma(s_a[(ty + 16 * p) * kDirectLd + k], s_a[(tx + 16 * q) * kDirectLd + k], acc[p][q]);
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            double &v = s_a[(ty + 16 * p) * kDirectLd + tx + 16 * q];
+            v = S.b * v + S.c * acc[p][q];
+        }
+    const bool wide = a.rows <= a.cols;
+    const int64_t w_i = wide ? a.w_stride : 1, w_j = wide ? 1 : a.w_stride;
+    for (int64_t j0 = int64_t(blockIdx.x) * kDirect; j0 < L.n; j0 += int64_t(gridDim.x) * kDirect) {
+        __syncthreads();
+        direct_load(X, L, j0, s_x);
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[p][q] = S.a * s_x[(ty + 16 * p) * kDirectLd + tx + 16 * q];
+        for (int k = 0; k < L.m; ++k)
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    acc[p][q] = fma(s_a[(ty + 16 * p) * kDirectLd + k], s_x[k * kDirectLd + tx + 16 * q], acc[p][q]);
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int i = ty + 16 * p;
+                const int64_t j = j0 + tx + 16 * q;
+                if (i >= L.m || j >= L.n) continue;
+                if (!last) {
+                    X[i * L.n + j] = acc[p][q];
+                    continue;
+                }
+                E *o = static_cast<E *>(a.W) + z * a.w_batch + i * w_i + j * w_j;
+                const float x = float(acc[p][q]);
+                *o = E(a.M ? a.keep * float(*o) - a.rate * x : x);
+            }
+    }
+}
+
 int log2_of(int x)
 {
     int s = 0;
@@ -990,9 +1126,26 @@ OrthLayout make_orth_layout(int64_t rows, int64_t cols)
     return L;
 }
 
+DirectLayout make_direct_layout(int64_t rows, int64_t cols)
+{
+    DirectLayout L;
+    L.m = int(rows < cols ? rows : cols);
+    L.n = rows < cols ? cols : rows;
+    const int64_t chunks = (L.n + kDirect - 1) / kDirect;
+    L.slices = int(chunks < kDirectSlices ? chunks : kDirectSlices);
+    const auto whole = [](size_t doubles) { return (doubles * sizeof(double) + 255) / 256 * 256; };
+    L.norm = 0;
+    L.gram = whole(kOrthNormBlocks);
+    L.x = L.gram + whole(size_t(L.slices) * L.m * L.m);
+    L.stride = L.x + whole(size_t(L.m) * L.n);
+    return L;
+}
+
 size_t orth_workspace(int64_t rows, int64_t cols)
 {
-    return orth_narrow(rows, cols) ? make_narrow_layout(rows, cols).stride : make_orth_layout(rows, cols).stride;
+    if (!orth_narrow(rows, cols)) return make_orth_layout(rows, cols).stride;
+    const size_t few = make_narrow_layout(rows, cols).stride, many = make_direct_layout(rows, cols).stride;
+    return few > many ? few : many; // how many steps there will be is not asked
 }
 
 namespace {
@@ -1022,8 +1175,25 @@ template <typename E, bool kSplit> void run_wide(const OrthArgs &a, const OrthSt
     run_steps<E, kSplit>(a, steps, ws, L, st);
 }
 
+template <typename E> void run_direct(const OrthArgs &a, const OrthSteps &steps, char *ws, hipStream_t st)
+{
+    const DirectLayout L = make_direct_layout(a.rows, a.cols);
+    const uint32_t z = uint32_t(a.batch);
+    // by rows, whatever lies between them: the norm's sum has one order, and many steps would show another
+    const int norm_blocks = norm_blocks_of(a.rows, a.cols);
+    orth_norm_kernel<E><<<dim3(norm_blocks, z), 256, 0, st>>>(a, ws, int64_t(L.stride), L.norm);
+    orth_direct_start_kernel<E><<<dim3(uint32_t((a.rows * a.cols + 1023) / 1024), z), 256, 0, st>>>(a, ws, L, norm_blocks);
+    const int64_t chunks = (L.n + kDirect - 1) / kDirect, blocks = chunks < kCus ? chunks : kCus;
+    for (int k = 0; k < steps.count; ++k) {
+        const NarrowSteps::Step S = {steps.step[k].a, steps.step[k].b, steps.step[k].c};
+        orth_direct_gram_kernel<<<dim3(uint32_t(L.slices), z), 256, kDirectLds / 2, st>>>(ws, L);
+        orth_direct_step_kernel<E><<<dim3(uint32_t(blocks), z), 256, kDirectLds, st>>>(a, ws, L, S, k + 1 == steps.count);
+    }
+}
+
 template <typename E> void run_type(const OrthArgs &a, const OrthSteps &steps, char *ws, hipStream_t st)
 {
+    if (orth_narrow(a.rows, a.cols) && steps.noise > kNarrowNoise) return run_direct<E>(a, steps, ws, st);
     if (orth_narrow(a.rows, a.cols)) {
         const NarrowLayout L = make_narrow_layout(a.rows, a.cols);
         NarrowSteps narrow;

@@ -88,6 +88,7 @@ struct OrthArgs {
 
 struct OrthSteps {
     int count;
+    double noise; // of stepping on A = X X^T alone: what a rounding error in A grows to, times itself
     OrthStep step[kOrthMaxSteps];
 };
 
@@ -106,6 +107,10 @@ constexpr int64_t kNarrow = 64;    // directions of a narrow matrix, which is st
 constexpr int kNarrowSlice = 128;  // columns in LDS of one that takes two launches
 constexpr int kNarrowSlices = 32;  // partial Gram matrices
 inline bool orth_narrow(int64_t rows, int64_t cols) { return (rows < cols ? rows : cols) <= kNarrow; }
+// ... as long as its rounding errors, 2^-53 of A at first, grow to 1e-7 of A or less; beyond, X itself is stepped on.
+// Nine steps of the usual coefficients are the last (on low-rank inputs 2e-8 against 64 bits or less, less than an fp32
+// rounding; ten steps would be off by 2e-7, twelve by 5e-6, sixteen by all).
+constexpr double kNarrowNoise = 1e9;
 
 struct NarrowLayout {
     int tiles;     // 16-row tiles of the shorter side
@@ -114,6 +119,16 @@ struct NarrowLayout {
     size_t stride; // bytes of one matrix' workspace: the partial Gram matrices
 };
 NarrowLayout make_narrow_layout(int64_t rows, int64_t cols);
+
+// Narrow matrices of many steps: X in fp64, shorter side first, without gaps, and its partial Gram matrices
+constexpr int kDirect = 64;       // columns of X at a time
+constexpr int kDirectSlices = 32; // partial Gram matrices
+struct DirectLayout {
+    int m, slices;
+    int64_t n;
+    size_t norm, gram, x, stride;
+};
+DirectLayout make_direct_layout(int64_t rows, int64_t cols);
 
 struct OrthLayout {
     int64_t m, n;         // shorter and longer side, padded
