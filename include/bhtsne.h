@@ -559,8 +559,8 @@ typedef struct bhtsne_matrices {
  *           quintic (3.4445, -4.7750, 2.0315) for every step.  A singular value
  *           of X in [0, 1] must stay below 64 under them (BHTSNE_EINVAL).
  *   1 <= steps <= 32; eps finite and >= 0 (a zero matrix stays zero for eps > 0).
- * The products run on the matrix cores with fp16 operands, fp32 sums: for bf16
- * with both sides above 256 at 11 bits an operand (a X at 19), else at 22 bits.
+ * With a side of 64 or less the steps are computed in fp64; else the products run
+ * on the matrix cores on pairs of fp16 values (22 bits an operand), with fp32 sums.
  * 0 <= batch <= 65535, 1 <= rows, cols <= 65536.  O's matrices must not overlap.
  * The workspace is bhtsne_orthogonalise_workspace_size bytes (256-byte
  * aligned; 0 for sizes out of range).

@@ -9,12 +9,9 @@
 // The products run on the matrix cores with fp16 operands and fp32 sums.  X is
 // held as two fp16 halves (22 bits together) times a power of two that keeps
 // every value of the step inside fp16's range.  Small singular values grow by a
-// factor of a each step against the largest, so a X must come from both halves;
-// B X may come from rounded operands when the output has 8 bits (bf16) and the
-// matrix is not narrow: the error before the output's
-// rounding is then about 1e-3 (gaussian, decaying and nearly low-rank matrices).
-// Otherwise each product is three, high by high and the two mixed ones, as exact
-// as products in 32 bits, and a I is part of B.
+// factor of a each step against the largest, and the largest come out of terms
+// that cancel, so each product is three, high by high and the two mixed ones, for
+// outputs of every type, and a I is part of B.
 #include <type_traits>
 
 #include "map.hpp"
@@ -114,24 +111,9 @@ __device__ inline void split(float v, f16 &h, f16 &l)
     l = f16(v - float(h));
 }
 
-// The low plane of single products keeps 8 bits: x - h in 1/256 of h's unit in the last place.  a X wants no more
-// (19 bits together), and it is a quarter less to move.
-__device__ inline int low_scale(f16 h) // 33 - the exponent that the unit counts from
-{
-    const int e = int(__builtin_bit_cast(uint16_t, h) >> 10) & 31;
-    return 33 - (e > 1 ? e : 1);
-}
-__device__ inline int8_t pack_low(float x, f16 h)
-{
-    const float q = rintf(ldexpf(x - float(h), low_scale(h)));
-    return int8_t(fminf(fmaxf(q, -128.0f), 127.0f));
-}
-__device__ inline float unpack_low(int8_t q, f16 h) { return float(h) + ldexpf(float(q), -low_scale(h)); }
-typedef signed char byte8 __attribute__((ext_vector_type(8)));
-
 // U / (|U| + eps) in planes, in both orientations, zeros in the padding.  Bound by its writes: 4096 x 4096 bf16 34 us for
 // 118 MB (3.4 TB/s); 1024 x 1024 9 us, of which the partial norms and the first values are some 3 of latency.
-template <typename E, bool kSplit>
+template <typename E>
 __global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, OrthLayout L, int norm_blocks, float sx)
 {
     __shared__ float s_t[kT][kT + 1];
@@ -166,7 +148,6 @@ __global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, 
         const int row = threadIdx.x / 8 + 32 * s;
         const int64_t at = (r0 + row) * L.cols + c0 + piece;
         half8 h, l;
-        byte8 q;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float x = float(double(v[s][e]) * scale);
@@ -174,14 +155,10 @@ __global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, 
             split(x, xh, xl);
             h[e] = xh;
             l[e] = xl;
-            if constexpr (!kSplit) q[e] = pack_low(x, xh);
             s_t[row][piece + e] = x;
         }
         *reinterpret_cast<half8 *>(uh + at) = h;
-        if constexpr (kSplit)
-            *reinterpret_cast<half8 *>(ul + at) = l;
-        else
-            *reinterpret_cast<byte8 *>(reinterpret_cast<int8_t *>(ul) + at) = q;
+        *reinterpret_cast<half8 *>(ul + at) = l;
     }
     __syncthreads();
 #pragma unroll
@@ -196,7 +173,7 @@ __global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, 
             l[e] = xl;
         }
         *reinterpret_cast<half8 *>(vh + (c0 + col) * L.rows + r0 + piece) = h;
-        if constexpr (kSplit) *reinterpret_cast<half8 *>(vl + (c0 + col) * L.rows + r0 + piece) = l;
+        *reinterpret_cast<half8 *>(vl + (c0 + col) * L.rows + r0 + piece) = l;
     }
 }
 
@@ -262,10 +239,10 @@ struct alignas(64) OrthProduct {
 };
 
 // E: elements of the output of kLast
-template <typename T, bool kSplit, Prod kProd, typename E>
+template <typename T, Prod kProd, typename E>
 __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a)
 {
-    constexpr int kPlanes = kSplit ? 2 : 1;
+    constexpr int kPlanes = 2;
     constexpr int kPlane = (T::kM + T::kN) * kK;           // values of a staged plane: P's rows, then Q's
     constexpr int kLoads = kPlanes * T::kEach;             // of a wave and stage
     constexpr bool kSymmetric = kProd == Prod::kGram || kProd == Prod::kPoly;
@@ -308,7 +285,7 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
         const int most = (in_p ? p_rows : q_rows) - 1;
         at = at < most ? at : most;
         src[e] = (in_p ? P : Q) + int64_t(at) * K + ((lane % 8) ^ (lane / 8)) * 8;
-        if constexpr (kSplit) src[T::kEach + e] = src[e] + (in_p ? a.p_plane : a.q_plane);
+        src[T::kEach + e] = src[e] + (in_p ? a.p_plane : a.q_plane);
     }
     const int slices = K / kK;
     const auto fetch = [&](int slice) {
@@ -347,10 +324,8 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
 #pragma unroll
             for (int j = 0; j < T::kJ; ++j) {
                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[half][0][i], q[half][0][j], acc[i][j], 0, 0, 0);
-                if constexpr (kSplit) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[half][0][i], q[half][1][j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[half][1][i], q[half][0][j], acc[i][j], 0, 0, 0);
-                }
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[half][0][i], q[half][1][j], acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[half][1][i], q[half][0][j], acc[i][j], 0, 0, 0);
             }
     };
 #pragma unroll
@@ -378,8 +353,6 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
     f16 *out = a.out + shift, *out_t = a.out_t + shift;
     const f16 *old = a.old + shift;
     const int64_t ld = a.ld, ld_t = a.ld_t, out_plane = a.out_plane;
-    // single products keep a low plane for a X alone, of 8 bits
-    const int8_t *u_low = reinterpret_cast<const int8_t *>(old + out_plane);
 #pragma unroll
     for (int i0 = 0; i0 < T::kI; i0 += T::kHigh) {
         const int r0 = bi * T::kM + wi + 16 * i0, c0 = bj * T::kN + wj;
@@ -397,8 +370,7 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
                 const int row = s / T::kJ * 4 + lane / 16, col = s % T::kJ * 16 + lane % 16;
                 const int64_t r = r0 + row, c = c0 + col;
                 if (r >= a.rows || c >= a.cols) continue;
-                float v = patch[row * T::kPatch + col] * a.f_c;
-                if constexpr (!kSplit) v += a.f_old * unpack_low(u_low[r * ld + c], old[r * ld + c]);
+                const float v = patch[row * T::kPatch + col] * a.f_c;
                 E *o = static_cast<E *>(a.W) + int64_t(blockIdx.z) * a.w_batch + r * a.w_stride + c;
                 *o = E(a.update ? a.keep * float(*o) - a.rate * v : v);
             }
@@ -412,39 +384,27 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
             const int64_t at = (r0 + row) * ld + c0 + col;
             float *v = patch + row * T::kPatch + col;
             half8 h, l, xh, xl;
-            byte8 q, xq;
             if constexpr (kProd == Prod::kPoly) {
                 xh = *reinterpret_cast<const half8 *>(old + at);
-                if constexpr (kSplit) xl = *reinterpret_cast<const half8 *>(old + out_plane + at);
-            } else if constexpr (kProd == Prod::kApply && !kSplit) {
-                xh = *reinterpret_cast<const half8 *>(old + at);
-                xq = *reinterpret_cast<const byte8 *>(u_low + at);
+                xl = *reinterpret_cast<const half8 *>(old + out_plane + at);
             }
 #pragma unroll
             for (int x8 = 0; x8 < 8; ++x8) {
                 float x = v[x8];
-                if constexpr (kProd == Prod::kGram) {
-                    x *= a.f_c;
-                } else if constexpr (kProd == Prod::kPoly) {
-                    const float av = kSplit ? float(xh[x8]) + float(xl[x8]) : float(xh[x8]);
-                    x = av * a.f_old + x * a.f_c;
-                    if (kSplit && r0 + row == c0 + col + x8) x += a.f_one;
+                if constexpr (kProd == Prod::kPoly) {
+                    x = (float(xh[x8]) + float(xl[x8])) * a.f_old + x * a.f_c;
+                    if (r0 + row == c0 + col + x8) x += a.f_one;
                 } else {
                     x *= a.f_c;
-                    if constexpr (!kSplit) x += a.f_old * unpack_low(xq[x8], xh[x8]);
                 }
                 f16 vh, vl;
                 split(x, vh, vl);
                 h[x8] = vh;
                 l[x8] = vl;
-                if constexpr (!kSplit && kProd == Prod::kApply) q[x8] = pack_low(x, vh);
                 v[x8] = x;
             }
             *reinterpret_cast<half8 *>(out + at) = h;
-            if constexpr (kSplit)
-                *reinterpret_cast<half8 *>(out + out_plane + at) = l;
-            else if constexpr (kProd == Prod::kApply)
-                *reinterpret_cast<byte8 *>(reinterpret_cast<int8_t *>(out + out_plane) + at) = q;
+            *reinterpret_cast<half8 *>(out + out_plane + at) = l;
         }
         if (kSymmetric && bi == bj) continue;
 #pragma unroll
@@ -461,15 +421,15 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
                 l[x8] = vl;
             }
             *reinterpret_cast<half8 *>(out_t + at) = h;
-            if constexpr (kSplit) *reinterpret_cast<half8 *>(out_t + out_plane + at) = l;
+            *reinterpret_cast<half8 *>(out_t + out_plane + at) = l;
         }
     }
 }
 
-template <typename T, bool kSplit, Prod kProd, typename E>
+template <typename T, Prod kProd, typename E>
 void run_product(const OrthArgs &a, const OrthSteps &steps, char *ws, const OrthLayout &L, int k, hipStream_t st)
 {
-    constexpr size_t kRing = size_t(T::kStages) * (kSplit ? 2 : 1) * (T::kM + T::kN) * kK * sizeof(f16);
+    constexpr size_t kRing = size_t(T::kStages) * 2 * (T::kM + T::kN) * kK * sizeof(f16);
     constexpr size_t kPatches = size_t(T::kWaves) * 16 * T::kHigh * T::kPatch * sizeof(float);
     constexpr size_t kLds = kRing > kPatches ? kRing : kPatches;
     static_assert(kLds <= 160 * 1024, "LDS of a CU");
@@ -516,7 +476,6 @@ void run_product(const OrthArgs &a, const OrthSteps &steps, char *ws, const Orth
         p.out_plane = plane;
         p.old = U;
         p.f_c = next_sx / (S.sb * S.sx);
-        p.f_old = float(S.a * next_sx / S.sx);
         p.keep = a.keep;
         p.rate = a.rate;
         p.update = a.M != nullptr;
@@ -526,7 +485,7 @@ void run_product(const OrthArgs &a, const OrthSteps &steps, char *ws, const Orth
         p.w_batch = a.w_batch;
         p.w_stride = a.w_stride;
     }
-    orth_product_kernel<T, kSplit, kProd, E><<<dim3(uint32_t(p.tiles), 1, uint32_t(a.batch)), T::kThreads, kLds, st>>>(p);
+    orth_product_kernel<T, kProd, E><<<dim3(uint32_t(p.tiles), 1, uint32_t(a.batch)), T::kThreads, kLds, st>>>(p);
 }
 
 // The tiles, each the best of several numbers of waves and buffers in the whole chain of products (whose operands come
@@ -535,34 +494,28 @@ using Tile32 = Tile<32, 32, 2, 2, 4>;
 using Tile64 = Tile<64, 64, 2, 4, 3>;
 using Tile64Several = Tile<64, 64, 2, 4, 2>; // less LDS: more blocks on a CU (1999 x 777 fp32: 40 us a step against 43)
 using Tile96 = Tile<96, 96, 6, 2, 3>;
-template <bool kSplit> using Tile128 = Tile<128, 128, kSplit ? 2 : 4, 4, 2>;
-using Tile192 = Tile<192, 192, 2, 4, 2>;
-using Tile256 = Tile<256, 256, 2, 4, 2>;
+using Tile128 = Tile<128, 128, 2, 4, 2>;
 
 // Which tile: the one whose busiest CU is done first.  Measured nanoseconds for a tile and slice of 64, of a CU that
-// has one tile and of one that has several, with one product of halves and with three.
+// has one tile and of one that has several.
 struct TileCost {
     int side;
-    float one[2], three[2];
+    float one, several;
 };
-constexpr TileCost kTileCosts[] = {{32, {150, 100}, {190, 131}},  {64, {270, 200}, {500, 361}},
-                                   {96, {560, 500}, {900, 820}},  {128, {780, 450}, {1390, 1110}},
-                                   {192, {1045, 1045}, {0, 0}},   {256, {1705, 1705}, {0, 0}}};
+constexpr TileCost kTileCosts[] = {{32, 190, 131}, {64, 500, 361}, {96, 900, 820}, {128, 1390, 1110}};
 struct TileChoice {
     int side;
     bool several; // tiles on a CU
 };
-TileChoice tile_of(bool split, bool symmetric, int64_t rows, int64_t cols, int64_t batch)
+TileChoice tile_of(bool symmetric, int64_t rows, int64_t cols, int64_t batch)
 {
     TileChoice best = {0, false};
     float least = 0.0f;
     for (const TileCost &c : kTileCosts) {
-        const float *ns = split ? c.three : c.one;
-        if (ns[0] == 0.0f) continue; // does not fit LDS
         const int64_t down = (rows + c.side - 1) / c.side, across = (cols + c.side - 1) / c.side;
         const int64_t tiles = batch * (symmetric ? down * (down + 1) / 2 : down * across);
         const int64_t each = (tiles + kCus - 1) / kCus;
-        const float cost = each <= 1 ? ns[0] : float(each) * ns[1];
+        const float cost = each <= 1 ? c.one : float(each) * c.several;
         if (best.side == 0 || cost < least) {
             best = {c.side, each > 1};
             least = cost;
@@ -571,32 +524,28 @@ TileChoice tile_of(bool split, bool symmetric, int64_t rows, int64_t cols, int64
     return best;
 }
 
-template <bool kSplit, Prod kProd, typename E>
+template <Prod kProd, typename E>
 void run_tile(TileChoice choice, const OrthArgs &a, const OrthSteps &steps, char *ws, const OrthLayout &L, int k, hipStream_t st)
 {
     const int tile = choice.side;
-    if (tile == 32) return run_product<Tile32, kSplit, kProd, E>(a, steps, ws, L, k, st);
-    if (tile == 64 && choice.several) return run_product<Tile64Several, kSplit, kProd, E>(a, steps, ws, L, k, st);
-    if (tile == 64) return run_product<Tile64, kSplit, kProd, E>(a, steps, ws, L, k, st);
-    if (tile == 96) return run_product<Tile96, kSplit, kProd, E>(a, steps, ws, L, k, st);
-    if constexpr (!kSplit) {
-        if (tile == 192) return run_product<Tile192, kSplit, kProd, E>(a, steps, ws, L, k, st);
-        if (tile == 256) return run_product<Tile256, kSplit, kProd, E>(a, steps, ws, L, k, st);
-    }
-    run_product<Tile128<kSplit>, kSplit, kProd, E>(a, steps, ws, L, k, st);
+    if (tile == 32) return run_product<Tile32, kProd, E>(a, steps, ws, L, k, st);
+    if (tile == 64 && choice.several) return run_product<Tile64Several, kProd, E>(a, steps, ws, L, k, st);
+    if (tile == 64) return run_product<Tile64, kProd, E>(a, steps, ws, L, k, st);
+    if (tile == 96) return run_product<Tile96, kProd, E>(a, steps, ws, L, k, st);
+    run_product<Tile128, kProd, E>(a, steps, ws, L, k, st);
 }
 
-template <typename E, bool kSplit>
+template <typename E>
 void run_steps(const OrthArgs &a, const OrthSteps &steps, char *ws, const OrthLayout &L, hipStream_t st)
 {
-    const TileChoice square = tile_of(kSplit, true, L.m, L.m, a.batch), full = tile_of(kSplit, false, L.rows, L.cols, a.batch);
+    const TileChoice square = tile_of(true, L.m, L.m, a.batch), full = tile_of(false, L.rows, L.cols, a.batch);
     for (int k = 0; k < steps.count; ++k) {
-        run_tile<kSplit, Prod::kGram, void>(square, a, steps, ws, L, k, st);
-        run_tile<kSplit, Prod::kPoly, void>(square, a, steps, ws, L, k, st);
+        run_tile<Prod::kGram, void>(square, a, steps, ws, L, k, st);
+        run_tile<Prod::kPoly, void>(square, a, steps, ws, L, k, st);
         if (k + 1 < steps.count)
-            run_tile<kSplit, Prod::kApply, void>(full, a, steps, ws, L, k, st);
+            run_tile<Prod::kApply, void>(full, a, steps, ws, L, k, st);
         else
-            run_tile<kSplit, Prod::kLast, E>(full, a, steps, ws, L, k, st);
+            run_tile<Prod::kLast, E>(full, a, steps, ws, L, k, st);
     }
 }
 
@@ -1156,7 +1105,7 @@ bool vectors(const void *p, int64_t stride, int64_t batch_stride, int64_t batch,
     return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(stride * bytes) | uintptr_t(batch > 1 ? batch_stride * bytes : 0)) & 15u) == 0;
 }
 
-template <typename E, bool kSplit> void run_wide(const OrthArgs &a, const OrthSteps &steps, char *ws, hipStream_t st)
+template <typename E> void run_wide(const OrthArgs &a, const OrthSteps &steps, char *ws, hipStream_t st)
 {
     const OrthLayout L = make_orth_layout(a.rows, a.cols);
     const int norm_blocks = norm_blocks_of(a.rows, a.cols);
@@ -1170,9 +1119,9 @@ template <typename E, bool kSplit> void run_wide(const OrthArgs &a, const OrthSt
         flat.m_vec = vectors(a.M, 0, a.m_batch, a.batch, 4);
     }
     orth_norm_kernel<E><<<dim3(norm_blocks, uint32_t(a.batch)), 256, 0, st>>>(flat, ws, int64_t(L.stride), L.norm);
-    orth_planes_kernel<E, kSplit><<<dim3(uint32_t(L.cols / kT), uint32_t(L.rows / kT), uint32_t(a.batch)), 256, 0, st>>>(
+    orth_planes_kernel<E><<<dim3(uint32_t(L.cols / kT), uint32_t(L.rows / kT), uint32_t(a.batch)), 256, 0, st>>>(
         a, ws, L, norm_blocks, steps.step[0].sx);
-    run_steps<E, kSplit>(a, steps, ws, L, st);
+    run_steps<E>(a, steps, ws, L, st);
 }
 
 template <typename E> void run_direct(const OrthArgs &a, const OrthSteps &steps, char *ws, hipStream_t st)
@@ -1204,9 +1153,7 @@ template <typename E> void run_type(const OrthArgs &a, const OrthSteps &steps, c
         if (L.tiles == 3) return run_narrow<E, 3>(a, narrow, ws, L, st);
         return run_narrow<E, 4>(a, narrow, ws, L, st);
     }
-    if constexpr (std::is_same<E, bf16>::value)
-        if (orth_single(a.type, a.rows, a.cols)) return run_wide<E, false>(a, steps, ws, st);
-    run_wide<E, true>(a, steps, ws, st);
+    run_wide<E>(a, steps, ws, st);
 }
 
 } // namespace

@@ -92,17 +92,6 @@ struct OrthSteps {
     OrthStep step[kOrthMaxSteps];
 };
 
-// Outputs of 8 bits (bf16) take one product of the high halves, finer ones three.
-// A direction's error is then up to 4e-3 where a + b + c cancels (the largest
-// singular values); it counts 1 / sqrt(m) in a matrix of m directions, so matrices
-// of few directions, whose products are bound by latency, take three for every type
-// (gaussian values at m = 65: 2.2e-3 before the rounding to bf16, whose own is 1.7e-3;
-// at m = 512 1.5e-3).
-constexpr int64_t kOrthSingle = 256;
-inline bool orth_single(Elem type, int64_t rows, int64_t cols)
-{
-    return type == Elem::kBF16 && (rows < cols ? rows : cols) > kOrthSingle;
-}
 constexpr int64_t kNarrow = 64;    // directions of a narrow matrix, which is stepped in fp64 on its Gram matrix
 constexpr int kNarrowSlice = 128;  // columns in LDS of one that takes two launches
 constexpr int kNarrowSlices = 32;  // partial Gram matrices
