@@ -65,7 +65,7 @@ double growth(const double *q, double most)
 
 // The scales of every step.  Singular values of X start in [0, 1]; `most` bounds
 // them through the steps, and with them every value of X (most), of A = X X^T
-// (most^2) and of B = a I + b A + c A^2 (|a| and b t + c t^2's largest on [0, most^2]).  Half of what fp16
+// (most^2) and of B = b A + c A^2 (b t + c t^2's largest on [0, most^2]).  Half of what fp16
 // holds is kept for rounding errors' growth.
 bool plan_steps(const double *coefficients, int steps, OrthSteps *plan)
 {
@@ -95,7 +95,7 @@ bool plan_steps(const double *coefficients, int steps, OrthSteps *plan)
         s.c = q[2];
         s.sx = power_of_two_below(kRoom / std::fmax(most, 1.0));
         s.sa = power_of_two_below(kRoom / std::fmax(t1, 1.0));
-        s.sb = power_of_two_below(kRoom / std::fmax(b + std::fabs(q[0]), 1.0));
+        s.sb = power_of_two_below(kRoom / std::fmax(b, 1.0));
         if (!(x < 64.0)) return false;
         most = x;
         noise = growth(q, t1) * noise + most * most; // and the next A's own rounding

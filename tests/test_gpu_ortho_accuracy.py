@@ -100,3 +100,48 @@ def test_batch_nonfinite_strides_and_graph_bf16():
     G[0, 5, 7], G[2, 100, 200], G[1] = float("nan"), float("inf"), 0.0
     bad = bh.orthogonalise(G, workspace=ws)
     assert bool(torch.isnan(bad[0]).all()) and bool(torch.isnan(bad[2]).all()) and bool((bad[1] == 0).all())
+
+
+def in_order(P, Q):
+    """P Q^T in 32 bits, term by term in one order: sums that no machine's library changes."""
+    acc = torch.zeros(P.shape[0], Q.shape[0], device=P.device)
+    for k in range(P.shape[1]):
+        acc = torch.addr(acc, P[:, k], Q[:, k])
+    return acc
+
+
+def plain_in_order(G, steps, coef):
+    X = G.double().t().contiguous() if G.shape[0] > G.shape[1] else G.double()
+    X = (X / (X.norm() + 1e-7)).float()
+    for k in range(steps):
+        a, b, c = coef[k] if hasattr(coef[0], "__len__") else coef
+        A = in_order(X, X)
+        X = a * X + in_order(b * A + c * in_order(A, A), X.t().contiguous())
+    return (X.t() if G.shape[0] > G.shape[1] else X).double().cpu()
+
+
+def check_in_order(G, steps, coef, got, say):
+    """As check, with the formula in 32 bits computed term by term: a library's order of sums depends on the machine."""
+    want = plain(G, steps, coef, torch.float64)
+    e32 = norm(plain_in_order(G, steps, coef) - want)
+    rounding = norm(want.to(G.dtype).double() - want)
+    err = norm(got.double().cpu() - want)
+    limit = 1.1 * rounding + 1.6 * e32 + 2.0 ** -21 * norm(want)
+    print(f"[orth] {say} err {err / norm(want):.2e} of {limit / norm(want):.2e} (32 bits {e32 / norm(want):.1e}, "
+          f"rounding {rounding / norm(want):.1e})", flush=True)
+    assert err <= limit
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("m,n", [(130, 200), (400, 300), (1024, 1030)])
+@pytest.mark.parametrize("kind", SPECTRA)
+def test_spectra_as_the_formula_in_32_bits(kind, m, n, dtype):
+    G = matrix(kind, m, n).to(dtype).to(DEV)
+    check_in_order(G, 5, COEF, bh.orthogonalise(G), f"{kind} {m}x{n} {dtype}")
+
+
+@pytest.mark.parametrize("steps,coef", STEPS)
+@pytest.mark.parametrize("kind", ["gauss", "equal", "rank 8 + noise"])
+def test_steps_as_the_formula_in_32_bits(kind, steps, coef):
+    G = matrix(kind, 200, 130).to(DEV)
+    check_in_order(G, steps, coef, bh.orthogonalise(G, steps=steps, coefficients=coef), f"{kind} {steps} steps fp32")
