@@ -66,24 +66,30 @@ double growth(const double *q, double most)
 // The scales of every step.  Singular values of X start in [0, 1]; `most` bounds
 // them through the steps, and with them every value of X (most), of A = X X^T
 // (most^2) and of B = b A + c A^2 (b t + c t^2's largest on [0, most^2]).  Half of what fp16
-// holds is kept for rounding errors' growth.
+// holds is kept for rounding errors' growth.  X's bound is followed down to
+// 2^-110, those of A and B, which do not count beside a X when they are small, to 2^-60.
 bool plan_steps(const double *coefficients, int steps, OrthSteps *plan)
 {
     constexpr double kRoom = 32768.0;
-    double most = 1.0, noise = 1.0;
-    plan->noise = 1.0;
+    constexpr double kLeast = 0x1p-110, kLeastSquare = 0x1p-60;
+    double most = 1.0, noise = 1.0, grown = 1.0;
+    plan->noise = plan->reach = 1.0;
     for (int k = 0; k < steps; ++k) {
         plan->noise = std::fmax(plan->noise, noise);
+        plan->reach = std::fmax(plan->reach, grown / std::fmax(most, kLeast));
         const double usual[3] = {3.4445, -4.7750, 2.0315};
         const double *q = coefficients ? coefficients + 3 * k : usual;
         if (!std::isfinite(q[0]) || !std::isfinite(q[1]) || !std::isfinite(q[2])) return false;
         const double t1 = most * most;
         const auto poly = [&](double t) { return std::fabs(q[1] * t + q[2] * t * t); };
         const auto next = [&](double t) { return std::fabs(std::sqrt(t) * (q[0] + q[1] * t + q[2] * t * t)); };
-        double b = poly(t1), x = next(t1);
+        double b = poly(t1), x = next(t1), g = std::fmax(std::fabs(q[0]), std::fabs(q[0] + q[1] * t1 + q[2] * t1 * t1));
         // extremes inside: of b t + c t^2, and of s (a + b s^2 + c s^4), both in t = s^2
         const double tb = -q[1] / (2.0 * q[2]);
-        if (tb > 0.0 && tb < t1) b = std::fmax(b, poly(tb));
+        if (tb > 0.0 && tb < t1) {
+            b = std::fmax(b, poly(tb));
+            g = std::fmax(g, std::fabs(q[0] + q[1] * tb + q[2] * tb * tb));
+        }
         const double disc = 9.0 * q[1] * q[1] - 20.0 * q[0] * q[2];
         const double roots[3] = {(-3.0 * q[1] + std::sqrt(disc)) / (10.0 * q[2]),
                                  (-3.0 * q[1] - std::sqrt(disc)) / (10.0 * q[2]), -q[0] / (3.0 * q[1])};
@@ -93,11 +99,12 @@ bool plan_steps(const double *coefficients, int steps, OrthSteps *plan)
         s.a = q[0];
         s.b = q[1];
         s.c = q[2];
-        s.sx = power_of_two_below(kRoom / std::fmax(most, 1.0));
-        s.sa = power_of_two_below(kRoom / std::fmax(t1, 1.0));
-        s.sb = power_of_two_below(kRoom / std::fmax(b, 1.0));
+        s.sx = power_of_two_below(kRoom / std::fmax(most, kLeast));
+        s.sa = power_of_two_below(kRoom / std::fmax(t1, kLeastSquare));
+        s.sb = power_of_two_below(kRoom / std::fmax(b, kLeastSquare));
         if (!(x < 64.0)) return false;
         most = x;
+        grown *= g;
         noise = growth(q, t1) * noise + most * most; // and the next A's own rounding
     }
     plan->count = steps;

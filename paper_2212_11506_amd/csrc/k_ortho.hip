@@ -114,10 +114,12 @@ __device__ inline void split(float v, f16 &h, f16 &l)
     l = f16(v - float(h));
 }
 
-// U / (|U| + eps) in planes, in both orientations, zeros in the padding.  Bound by its writes: 4096 x 4096 bf16 34 us for
+// U / (|U| + eps) in planes, in both orientations, zeros in the padding.  Where |U| is far below eps, X is small and
+// stays small, and fp16 would lose it: it is held larger by a power of two, 1 / `lift`, such that no step passes its
+// bound.  Only A and the output are formed with `lift`; the products that lead from X to X are linear in it.  Bound by its writes: 4096 x 4096 bf16 34 us for
 // 118 MB (3.4 TB/s); 1024 x 1024 9 us, of which the partial norms and the first values are some 3 of latency.
 template <typename E>
-__global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, OrthLayout L, int norm_blocks, float sx)
+__global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, OrthLayout L, int norm_blocks, float sx, double reach)
 {
     __shared__ float s_t[kT][kT + 1];
     const int64_t z = blockIdx.z, r0 = int64_t(blockIdx.y) * kT, c0 = int64_t(blockIdx.x) * kT;
@@ -143,7 +145,18 @@ __global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, 
         sq += k < norm_blocks ? v : 0.0;
     }
     sq = wave_sum(sq);
-    const double scale = double(sx) / (sqrt(sq) + a.eps);
+    const double norm = sqrt(sq), inverse = 1.0 / (norm + a.eps);
+    double scale = double(sx) * inverse;
+    const double top = norm * inverse * reach; // what |X| can reach beside its bounds, which allow 1
+    if (top > 0.0 && top < 0.5) {
+        constexpr int kMostLift = 110; // its inverse is a normal float, with digits to spare for the output
+        const int e = -ilogb(top) - 1;
+        const double up = ldexp(1.0, e < kMostLift ? e : kMostLift);
+        scale *= up;
+        if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *reinterpret_cast<float *>(base + L.lift) = float(1.0 / up);
+    } else if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+        *reinterpret_cast<float *>(base + L.lift) = 1.0f;
+    }
     f16 *uh = reinterpret_cast<f16 *>(base + L.u[0]), *ul = uh + L.rows * L.cols;
     f16 *vh = reinterpret_cast<f16 *>(base + L.v[0]), *vl = vh + L.rows * L.cols;
 #pragma unroll
@@ -231,6 +244,7 @@ struct alignas(64) OrthProduct {
     uint32_t per_four;        // 2^32 / across rounded up: t across < 2^32 for every tile t
     f16 *out, *out_t;         // C and its transpose in planes
     const f16 *old;           // A of kPoly, X of kApply and kLast
+    const float *lift;        // kGram and kLast: of the first matrix
     int64_t out_plane;
     int32_t ld, ld_t;
     float f_c, f_old;         // C becomes f_c C + f_old old
@@ -253,6 +267,9 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
     f16 *ring = reinterpret_cast<f16 *>(s_mem);
     const int64_t shift = int64_t(blockIdx.z) * (a.stride / int64_t(sizeof(f16)));
     const f16 *P = a.P + shift, *Q = a.Q + shift;
+    float lift = 1.0f;
+    if constexpr (kProd == Prod::kGram || kProd == Prod::kLast)
+        lift = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(a.lift) + int64_t(blockIdx.z) * a.stride);
     const int K = a.K, p_rows = a.p_rows, q_rows = a.q_rows;
     int bi, bj;
     const int t = xcd_tile(blockIdx.x, a.tiles);
@@ -356,6 +373,7 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
     f16 *out = a.out + shift, *out_t = a.out_t + shift;
     const f16 *old = a.old + shift;
     const int64_t ld = a.ld, ld_t = a.ld_t, out_plane = a.out_plane;
+    const float f_c = kProd == Prod::kGram ? a.f_c * (lift * lift) : a.f_c, f_old = a.f_old; // too small an A is zero
 #pragma unroll
     for (int i0 = 0; i0 < T::kI; i0 += T::kHigh) {
         const int r0 = bi * T::kM + wi + 16 * i0, c0 = bj * T::kN + wj;
@@ -374,7 +392,7 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
                 const int64_t r = r0 + row, c = c0 + col;
                 if (r >= a.rows || c >= a.cols) continue;
                 const float x = float(old[r * ld + c]) + float(old[out_plane + r * ld + c]);
-                const float v = patch[row * T::kPatch + col] * a.f_c + a.f_old * x;
+                const float v = (patch[row * T::kPatch + col] * f_c + f_old * x) * lift;
                 E *o = static_cast<E *>(a.W) + int64_t(blockIdx.z) * a.w_batch + r * a.w_stride + c;
                 *o = E(a.update ? a.keep * float(*o) - a.rate * v : v);
             }
@@ -395,8 +413,8 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
 #pragma unroll
             for (int x8 = 0; x8 < 8; ++x8) {
                 float x = v[x8];
-                x *= a.f_c;
-                if constexpr (kProd != Prod::kGram) x += a.f_old * (float(xh[x8]) + float(xl[x8]));
+                x *= f_c;
+                if constexpr (kProd != Prod::kGram) x += f_old * (float(xh[x8]) + float(xl[x8]));
                 f16 vh, vl;
                 split(x, vh, vl);
                 h[x8] = vh;
@@ -441,6 +459,7 @@ void run_product(const OrthArgs &a, const OrthSteps &steps, char *ws, const Orth
     const int64_t plane = L.rows * L.cols, square = L.m * L.m;
     OrthProduct p = {};
     p.stride = int64_t(L.stride);
+    p.lift = reinterpret_cast<const float *>(ws + L.lift);
     if constexpr (kProd == Prod::kGram || kProd == Prod::kPoly) {
         static_assert(T::kM == T::kN, "symmetric products");
         const int32_t mt = int32_t((L.m + T::kM - 1) / T::kM);
@@ -453,7 +472,7 @@ void run_product(const OrthArgs &a, const OrthSteps &steps, char *ws, const Orth
         p.out_plane = square;
         p.old = A;
         if constexpr (kProd == Prod::kGram) {
-            p.f_c = S.sa / (S.sx * S.sx);
+            p.f_c = float(S.sa / (double(S.sx) * S.sx));
         } else {
             p.f_c = float(S.c * S.sb / (double(S.sa) * S.sa));
             p.f_old = float(S.b * S.sb / S.sa);
@@ -474,7 +493,7 @@ void run_product(const OrthArgs &a, const OrthSteps &steps, char *ws, const Orth
         p.out_t = at(L.v[(k + 1) & 1]);
         p.out_plane = plane;
         p.old = U;
-        p.f_c = next_sx / (S.sb * S.sx);
+        p.f_c = float(next_sx / (double(S.sb) * S.sx));
         p.f_old = float(S.a * next_sx / S.sx);
         p.keep = a.keep;
         p.rate = a.rate;
@@ -1071,6 +1090,7 @@ OrthLayout make_orth_layout(int64_t rows, int64_t cols)
     L.a = take(planes * L.m * L.m);
     L.b = take(planes * L.m * L.m);
     L.norm = take(sizeof(double) * kOrthNormBlocks);
+    L.lift = take(sizeof(float));
     L.stride = at;
     return L;
 }
@@ -1120,7 +1140,7 @@ template <typename E> void run_wide(const OrthArgs &a, const OrthSteps &steps, c
     }
     orth_norm_kernel<E><<<dim3(norm_blocks, uint32_t(a.batch)), 256, 0, st>>>(flat, ws, int64_t(L.stride), L.norm);
     orth_planes_kernel<E><<<dim3(uint32_t(L.cols / kT), uint32_t(L.rows / kT), uint32_t(a.batch)), 256, 0, st>>>(
-        a, ws, L, norm_blocks, steps.step[0].sx);
+        a, ws, L, norm_blocks, steps.step[0].sx, steps.reach);
     run_steps<E>(a, steps, ws, L, st);
 }
 

@@ -88,6 +88,7 @@ struct OrthArgs {
 
 struct OrthSteps {
     int count;
+    double reach; // how far a small X can grow beyond the bound of its step: the largest of prod |B| / most over the steps
     double noise; // of stepping on A = X X^T alone: what a rounding error in A grows to, times itself
     OrthStep step[kOrthMaxSteps];
 };
@@ -125,6 +126,7 @@ struct OrthLayout {
     size_t u[2], v[2];    // U and its transpose, two buffers each: high plane, low plane behind it
     size_t a, b;          // A and B, planes as above
     size_t norm;          // kOrthNormBlocks doubles
+    size_t lift;          // a float: 1 / the power of two that X is held larger by
     size_t stride;        // bytes of one matrix' workspace
 };
 OrthLayout make_orth_layout(int64_t rows, int64_t cols);
