@@ -9,9 +9,9 @@
 // 2^k lanes of a wave (up to 1024 features at 16 a lane), or of a whole block
 // (up to 16384; backward, with two rows and the weights' sums, half of both),
 // so that the mean, the centred sum of squares and the outputs come from one
-// read; the next row's loads are in flight while a row is computed.  All sums
-// are fp32 (the weight gradients' last join fp64); the only rounding to fewer
-// bits is that of the outputs.
+// read; the next row's loads are in flight while a row is computed.  Sums are
+// fp32, of 16 terms a lane at most, and fp64 in longer rows and in the weight
+// gradients' last join; the only rounding to fewer bits is that of the outputs.
 #include <type_traits>
 
 #include "map.hpp"
@@ -179,6 +179,19 @@ __device__ inline float row_sum(float v, int team, float *red)
     return s;
 }
 
+// Sum over a block in fp64, for rows whose lanes have many terms: in fp32 a lane's sum of a hundred equal values is off by
+// several roundings, all one way (a constant row of 100.3 came out at 0.03 for d = 100000, at 0.24 for 2^20).
+// `red`: kNormMaxThreads / 64 doubles of LDS for this sum alone.
+__device__ inline double long_sum(double v, double *red)
+{
+    v = wave_sum(v);
+    if (lane_id() == 0) red[threadIdx.x / kWave] = v;
+    __syncthreads();
+    double s = 0.0;
+    for (int w = 0; w < int(blockDim.x) / kWave; ++w) s += red[w];
+    return s;
+}
+
 // The vectors of a lane: the k-th starts at feature (k team + lane) VEC.  All but the last few are full for every
 // lane, which is known without looking at the lanes.
 template <int VEC> struct Columns {
@@ -260,31 +273,34 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_kernel(NormArgs a, int t
 }
 
 // rows longer than a block's registers: one block a row, three passes over it, the last two from the caches at the rate
-// of these (2000 x 20000 fp32 130 us, 2.5 TB/s)
+// of these (2000 x 20000 fp32 117 us, 2.7 TB/s)
 template <typename E, int VEC, bool kWide>
 __global__ __launch_bounds__(kNormMaxThreads) void norm_long_kernel(NormArgs a)
 {
-    __shared__ float s_red[2][kNormMaxThreads / kWave];
+    __shared__ double s_red[2][kNormMaxThreads / kWave];
     const Params<kWide> weight = {a.weight, a.param == Elem::kF16}, bias = {a.bias, a.param == Elem::kF16};
     const int team = blockDim.x;
-    const float count = float(a.d), inv = 1.0f / count;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const E *x = static_cast<const E *>(a.x) + row * a.x_stride;
         E *y = static_cast<E *>(a.out) + row * a.out_stride;
-        float sum = 0.0f;
+        double sum = 0.0;
         for (int64_t c = int64_t(threadIdx.x) * VEC; c < a.d; c += int64_t(team) * VEC) {
             const Pack<E, VEC> p = load_pack<false, E, VEC>(x + c);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) sum += float(p.v[j]);
+            for (int j = 0; j < VEC; ++j) sum += double(p.v[j]);
         }
-        const float mean = share(row_sum(sum, team, s_red[0]), count, inv);
-        float sq = 0.0f;
+        const double centre = long_sum(sum, s_red[0]) / double(a.d);
+        const float mean = float(centre);
+        double sq = 0.0;
         for (int64_t c = int64_t(threadIdx.x) * VEC; c < a.d; c += int64_t(team) * VEC) {
             const Pack<E, VEC> p = load_pack<false, E, VEC>(x + c);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) sq += (float(p.v[j]) - mean) * (float(p.v[j]) - mean);
+            for (int j = 0; j < VEC; ++j) {
+                const double c = double(p.v[j]) - centre;
+                sq = fma(c, c, sq);
+            }
         }
-        const float rstd = inverse_root(share(row_sum(sq, team, s_red[1]), count, inv) + float(a.eps));
+        const float rstd = float(1.0 / sqrt(long_sum(sq, s_red[1]) / double(a.d) + a.eps));
         for (int64_t c = int64_t(threadIdx.x) * VEC; c < a.d; c += int64_t(team) * VEC) {
             const Pack<E, VEC> p = load_pack<false, E, VEC>(x + c);
             Pack<E, VEC> o;
@@ -428,28 +444,26 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_back_kernel(NormArgs a, 
 template <typename E, int VEC, bool kWide>
 __global__ __launch_bounds__(kNormMaxThreads) void norm_back_long_kernel(NormArgs a)
 {
-    __shared__ float s_red[2][kNormMaxThreads / kWave];
+    __shared__ double s_red[2][kNormMaxThreads / kWave];
     const Params<kWide> weight = {a.weight, a.param == Elem::kF16};
     const int team = blockDim.x;
-    const float count = float(a.d), inv = 1.0f / count;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const E *x = static_cast<const E *>(a.x) + row * a.x_stride;
         const E *dy = static_cast<const E *>(a.dy) + row * a.dy_stride;
         E *dx = static_cast<E *>(a.out) + row * a.out_stride;
         const float mean = a.mean[row], rstd = a.rstd[row];
-        float s1 = 0.0f, s2 = 0.0f;
+        double sum1 = 0.0, sum2 = 0.0;
         for (int64_t c = int64_t(threadIdx.x) * VEC; c < a.d; c += int64_t(team) * VEC) {
             const Pack<E, VEC> p = load_pack<false, E, VEC>(x + c), q = load_pack<false, E, VEC>(dy + c);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 const float w = a.weight ? weight.at(c + j) : 1.0f;
                 const float g = float(q.v[j]) * w;
-                s1 += g;
-                s2 += g * ((float(p.v[j]) - mean) * rstd);
+                sum1 += double(g);
+                sum2 += double(g) * double((float(p.v[j]) - mean) * rstd);
             }
         }
-        s1 = share(row_sum(s1, team, s_red[0]), count, inv);
-        s2 = share(row_sum(s2, team, s_red[1]), count, inv);
+        const float s1 = float(long_sum(sum1, s_red[0]) / double(a.d)), s2 = float(long_sum(sum2, s_red[1]) / double(a.d));
         for (int64_t c = int64_t(threadIdx.x) * VEC; c < a.d; c += int64_t(team) * VEC) {
             const Pack<E, VEC> p = load_pack<false, E, VEC>(x + c), q = load_pack<false, E, VEC>(dy + c);
             Pack<E, VEC> o;
