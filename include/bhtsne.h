@@ -561,7 +561,10 @@ typedef struct bhtsne_matrices {
  *   1 <= steps <= 32; eps finite and >= 0 (a zero matrix stays zero for eps > 0).
  * With a side of 64 or less the steps are computed in fp64; else the products run
  * on the matrix cores on pairs of fp16 values (22 bits an operand), with fp32 sums.
- * 0 <= batch <= 65535, 1 <= rows, cols <= 65536.  O's matrices must not overlap.
+ * 0 <= batch <= 65535, 1 <= rows, cols <= 65536.  O's matrices lie one behind the
+ * other (batch_stride >= (rows - 1) stride + cols), or their rows between one
+ * another's (batch_stride >= cols, stride >= (batch - 1) batch_stride + cols, as in
+ * an array of rows x batch x cols); other orders are refused.
  * The workspace is bhtsne_orthogonalise_workspace_size bytes (256-byte
  * aligned; 0 for sizes out of range).
  * Errors: BHTSNE_EINVAL, BHTSNE_EWORKSPACE, BHTSNE_EDEVICE. */
@@ -578,7 +581,7 @@ int bhtsne_orthogonalise(const bhtsne_matrices *G, int64_t batch, int64_t rows, 
  *   M       the momentum, fp32, updated in place (zero before the first step).
  *   learning_rate finite > 0; momentum in [0, 1); weight_decay finite >= 0;
  *   scale finite (the usual choice is sqrt(max(1, rows / cols))).
- * No two of W, G and M overlap.  Other arguments, workspace and errors as
+ * No two of W, G and M overlap; W's and M's matrices lie as O's do.  Other arguments, workspace and errors as
  * bhtsne_orthogonalise. */
 int bhtsne_muon_step(const bhtsne_matrices *W, const bhtsne_matrices *G, const bhtsne_matrices *M, int64_t batch,
                      int64_t rows, int64_t cols, int type, double learning_rate, double momentum, int nesterov,

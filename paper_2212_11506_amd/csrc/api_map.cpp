@@ -42,10 +42,12 @@ bool matrices_ok(const bhtsne_matrices *x, int64_t batch, int64_t rows, int64_t 
     if (x->stride < cols || x->stride > kMost) return false;
     return batch <= 1 || (x->batch_stride >= 0 && x->batch_stride < (int64_t(1) << 48));
 }
-// matrices that are written must not share elements: one behind the other, in whatever order the strides say
+// Matrices that are written must not share elements: each lies behind the one before, or their rows lie behind one
+// another's, all first rows, all second rows and so on.  The sizes and strides are known to be in range.
 bool apart(const bhtsne_matrices *x, int64_t batch, int64_t rows, int64_t cols)
 {
-    return batch <= 1 || x->batch_stride >= (rows - 1) * x->stride + cols;
+    if (batch <= 1 || x->batch_stride >= (rows - 1) * x->stride + cols) return true;
+    return x->batch_stride >= cols && x->batch_stride <= x->stride && x->stride >= (batch - 1) * x->batch_stride + cols;
 }
 
 float power_of_two_below(double x) { return float(std::exp2(std::floor(std::log2(x)))); }
@@ -235,7 +237,7 @@ int bhtsne_muon_step(const bhtsne_matrices *W, const bhtsne_matrices *G, const b
     if (!std::isfinite(learning_rate) || !(learning_rate > 0.0) || !(momentum >= 0.0 && momentum < 1.0))
         return BHTSNE_EINVAL;
     if (!std::isfinite(weight_decay) || weight_decay < 0.0 || !std::isfinite(scale)) return BHTSNE_EINVAL;
-    if (batch < 0 || rows < 1 || cols < 1) return BHTSNE_EINVAL;
+    if (bhtsne_orthogonalise_workspace_size(batch, rows, cols) == 0) return BHTSNE_EINVAL; // before sizes are multiplied
     if (!matrices_ok(M, batch, rows, cols, BHTSNE_F32) || !apart(M, batch, rows, cols)) return BHTSNE_EINVAL;
     OrthArgs a = {};
     a.M = static_cast<float *>(M->data);
