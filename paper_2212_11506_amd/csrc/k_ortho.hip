@@ -220,6 +220,15 @@ template <int M, int N, int Wm, int Wn, int Stages> struct Tile {
     static_assert(kGroups % kWaves == 0 && M % (16 * Wm) == 0 && N % (16 * Wn) == 0, "even shares");
 };
 
+// What lanes of a wave have put into LDS is there for its other lanes.  A wave's LDS accesses keep their order, so this
+// costs no instruction: it holds the compiler to that order.
+__device__ inline void wave_exchange()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 __device__ inline half8 fragment(const f16 *tile, int row, int piece)
 {
     return *reinterpret_cast<const half8 *>(tile + row * kK + ((piece ^ (row & 7)) * 8));
@@ -384,6 +393,7 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     patch[(16 * i + 4 * (lane / 16) + r) * T::kPatch + 16 * j + lane % 16] = acc[i0 + i][j][r];
+        wave_exchange();
         if constexpr (kProd == Prod::kLast) {
 #pragma unroll 4
             for (int s = 0; s < kDown * T::kJ / 4; ++s) {
@@ -396,6 +406,7 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
                 E *o = static_cast<E *>(a.W) + int64_t(blockIdx.z) * a.w_batch + r * a.w_stride + c;
                 *o = E(a.update ? a.keep * float(*o) - a.rate * v : v);
             }
+            wave_exchange(); // the patch is written again
             continue;
         }
         constexpr int kPieces = kDown * kAcross / 8;
@@ -424,6 +435,7 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
             *reinterpret_cast<half8 *>(out + at) = h;
             *reinterpret_cast<half8 *>(out + out_plane + at) = l;
         }
+        wave_exchange(); // the values of C are there, in either orientation; without one the patch is written again
         if (kSymmetric && bi == bj) continue;
 #pragma unroll
         for (int s = 0; s < (kPieces + kWave - 1) / kWave; ++s) {
@@ -441,6 +453,7 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
             *reinterpret_cast<half8 *>(out_t + at) = h;
             *reinterpret_cast<half8 *>(out_t + out_plane + at) = l;
         }
+        wave_exchange(); // the patch is written again
     }
 }
 
