@@ -811,8 +811,7 @@ def _matrix_sizes(t: torch.Tensor, where: str):
 
 
 @functools.lru_cache(maxsize=64)
-def _flat_coefficients(coefficients, steps: int):
-    flat = [float(v) for row in coefficients for v in (row if isinstance(row, tuple) else (row,))]
+def _flat_coefficients(flat, steps: int):
     if len(flat) == 3:
         flat = flat * max(1, steps)
     if len(flat) != 3 * steps and steps > 0:
@@ -821,10 +820,16 @@ def _flat_coefficients(coefficients, steps: int):
 
 
 def _coefficients(coefficients, steps: int):
-    """None, one (a, b, c) for every step, or one for each."""
+    """None, one (a, b, c) for every step, or one for each, as they are now: kept by their values alone."""
     if coefficients is None:
         return None
-    return _flat_coefficients(tuple(tuple(r) if hasattr(r, "__len__") else r for r in coefficients), int(steps))
+    flat = []
+    for row in coefficients:
+        if isinstance(row, (list, tuple)) or getattr(row, "ndim", 0) > 0:
+            flat.extend(map(float, row))
+        else:
+            flat.append(float(row))
+    return _flat_coefficients(tuple(flat), int(steps))
 
 
 @functools.lru_cache(maxsize=256)
