@@ -823,12 +823,15 @@ def _coefficients(coefficients, steps: int):
     """None, one (a, b, c) for every step, or one for each, as they are now: kept by their values alone."""
     if coefficients is None:
         return None
-    flat = []
-    for row in coefficients:
-        if isinstance(row, (list, tuple)) or getattr(row, "ndim", 0) > 0:
-            flat.extend(map(float, row))
-        else:
-            flat.append(float(row))
+    try:
+        flat = tuple(map(float, coefficients))
+    except (TypeError, ValueError, RuntimeError):  # not numbers: rows of them
+        flat = []
+        for row in coefficients:
+            if isinstance(row, (list, tuple)) or getattr(row, "ndim", 0) > 0:
+                flat.extend(map(float, row))
+            else:
+                flat.append(float(row))
     return _flat_coefficients(tuple(flat), int(steps))
 
 
