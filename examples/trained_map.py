@@ -19,21 +19,6 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 import paper_2212_11506_amd as bh  # noqa: E402
 
 
-class LayerNorm(torch.autograd.Function):
-    """The library's layer norm as a node of torch's graph."""
-
-    @staticmethod
-    def forward(ctx, x, weight, bias):
-        y, mean, rstd = bh.layer_norm(x, weight, bias)
-        ctx.save_for_backward(x, weight, mean, rstd)
-        return y
-
-    @staticmethod
-    def backward(ctx, dy):
-        x, weight, mean, rstd = ctx.saved_tensors
-        return bh.layer_norm_backward(dy.contiguous(), x, weight, mean, rstd)
-
-
 class Map:
     """Weights W (out x in), each hidden layer with a norm's weight and bias, and the momenta of all of them."""
 
@@ -49,7 +34,7 @@ class Map:
 
     def __call__(self, x):
         for w, (scale, shift) in zip(self.weights, self.norms):
-            x = F.gelu(LayerNorm.apply(x @ w.t(), scale, shift))
+            x = F.gelu(bh.layer_norm(x @ w.t(), scale, shift)[0])
         return x @ self.weights[-1].t()
 
     def step(self, learning_rate, momentum):

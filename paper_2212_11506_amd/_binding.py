@@ -13,6 +13,7 @@ import os
 from typing import Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = os.path.join(_HERE, "lib", "libbhtsne.so")
@@ -734,7 +735,19 @@ def _param_type(weight, bias, dtype) -> int:
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
                eps: float = 1e-5, out: Optional[torch.Tensor] = None):
-    """bhtsne_layer_norm over the rows of x (n x d, rows any distance apart): (y, mean, rstd); out may be x."""
+    """bhtsne_layer_norm over the rows of x (n x d, rows any distance apart): (y, mean, rstd); out may be x.
+
+    y's gradient goes to x, weight and bias through bhtsne_layer_norm_backward (once); mean and rstd have none, and
+    neither has a call with out."""
+    if torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad)
+                                    or (bias is not None and bias.requires_grad)):
+        if out is not None:
+            raise ValueError("out has no gradient: leave it out, or call under torch.no_grad()")
+        return _LayerNorm.apply(x, weight, bias, eps)
+    return _layer_norm(x, weight, bias, eps, out)
+
+
+def _layer_norm(x, weight, bias, eps, out=None):
     lib = load_library()
     if x.dim() != 2:
         raise ValueError(f"x must be n x d, got {tuple(x.shape)}")
@@ -754,6 +767,28 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     return y, mean, rstd
 
 
+class _LayerNorm(torch.autograd.Function):
+    """layer_norm as a node of torch's graph."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        y, mean, rstd = _layer_norm(x, weight, bias, eps)
+        ctx.save_for_backward(x, weight, mean, rstd)
+        ctx.bias_type = bias.dtype if bias is not None else None
+        ctx.mark_non_differentiable(mean, rstd)
+        return y, mean, rstd
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, _mean, _rstd):
+        x, weight, mean, rstd = ctx.saved_tensors
+        n, d = x.shape
+        if (d > 1 and dy.stride(1) != 1) or (n > 1 and 0 < dy.stride(0) < d):
+            dy = dy.contiguous()
+        dx, dweight, dbias = _layer_norm_backward(dy, x, weight, mean, rstd, ctx.bias_type)
+        return dx, dweight if weight is not None else None, dbias if ctx.bias_type is not None else None, None
+
+
 @functools.lru_cache(maxsize=256)
 def layer_norm_workspace_size(n: int, d: int) -> int:
     return int(load_library().bhtsne_layer_norm_workspace_size(int(n), int(d)))
@@ -763,7 +798,11 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
                         rstd: torch.Tensor, dx: Optional[torch.Tensor] = None,
                         workspace: Optional[torch.Tensor] = None):
     """bhtsne_layer_norm_backward: (dx, dweight, dbias), the last two of weight's type (x's without a weight);
-    dx may be dy or x."""
+    dx may be dy or x.  The results have no gradient of their own."""
+    return _layer_norm_backward(dy, x, weight, mean, rstd, None, dx, workspace)
+
+
+def _layer_norm_backward(dy, x, weight, mean, rstd, bias_type=None, dx=None, workspace=None):
     lib = load_library()
     if x.dim() != 2:
         raise ValueError(f"x must be n x d, got {tuple(x.shape)}")
@@ -781,11 +820,13 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
         workspace = x.new_empty(need, dtype=torch.uint8)
     else:
         need = _workspace_bytes(workspace)
-    ptype = weight.dtype if weight is not None else dtype
+    if weight is not None:
+        _type(weight, "weight")
+    ptype = weight.dtype if weight is not None else bias_type if bias_type is not None else dtype
     dweight, dbias = x.new_empty((2, d), dtype=ptype).unbind(0)
     rc = lib.bhtsne_layer_norm_backward(dy.data_ptr(), dy_stride, x.data_ptr(), x_stride, _vector(weight, "weight", d),
                                         _vector(mean, "mean", n, torch.float32), _vector(rstd, "rstd", n, torch.float32),
-                                        n, d, kind, _param_type(weight, None, dtype), dx.data_ptr(), dx_stride,
+                                        n, d, kind, _TYPES[ptype], dx.data_ptr(), dx_stride,
                                         dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr(), need, _stream_of(x))
     if rc:
         _check(rc, "bhtsne_layer_norm_backward")
@@ -851,8 +892,11 @@ def _orthogonal_workspace(sizes, like, ws):
 
 def orthogonalise(G: torch.Tensor, steps: int = 5, coefficients=None, eps: float = 1e-7,
                   out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """bhtsne_orthogonalise of G (rows x cols, or batch x rows x cols); out may be G."""
+    """bhtsne_orthogonalise of G (rows x cols, or batch x rows x cols); out may be G.  It has no gradient, and refuses a G
+    whose graph torch records."""
     lib = load_library()
+    if G.requires_grad and torch.is_grad_enabled():
+        raise ValueError("orthogonalise has no gradient: take G.detach(), or call under torch.no_grad()")
     sizes = _matrix_sizes(G, "G")
     kind, shape, dtype = _type(G, "G"), G.shape, G.dtype
     g = _matrices(G, "G", shape, dtype)
