@@ -675,6 +675,7 @@ class _Matrices(C.Structure):
 
 
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}  # BHTSNE_F32, BHTSNE_F16, BHTSNE_BF16
+_written = torch.autograd.graph.increment_version  # a graph that has saved the tensor must not use it any more
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
@@ -764,6 +765,8 @@ def _layer_norm(x, weight, bias, eps, out=None):
                                rstd.data_ptr(), _stream_of(x))
     if rc:
         _check(rc, "bhtsne_layer_norm")
+    if out is not None:
+        _written(out)
     return y, mean, rstd
 
 
@@ -812,6 +815,7 @@ def _layer_norm_backward(dy, x, weight, mean, rstd, bias_type=None, dx=None, wor
     if need == 0:
         raise BhtsneError(BHTSNE_EINVAL, "bhtsne_layer_norm_workspace_size")
     x_stride, dy_stride = _rows(x, "x", shape, dtype), _rows(dy, "dy", shape, dtype)
+    given = dx
     if dx is None:
         dx, dx_stride = torch.empty_like(x) if x_stride == d else x.new_empty(shape), d
     else:
@@ -830,6 +834,8 @@ def _layer_norm_backward(dy, x, weight, mean, rstd, bias_type=None, dx=None, wor
                                         dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr(), need, _stream_of(x))
     if rc:
         _check(rc, "bhtsne_layer_norm_backward")
+    if given is not None:
+        _written(given)
     return dx, dweight, dbias
 
 
@@ -907,6 +913,8 @@ def orthogonalise(G: torch.Tensor, steps: int = 5, coefficients=None, eps: float
                                   ws.data_ptr(), nbytes, _stream_of(G))
     if rc:
         _check(rc, "bhtsne_orthogonalise")
+    if out is not None:
+        _written(out)
     return O
 
 
@@ -914,7 +922,7 @@ def muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, learning_rate: 
               nesterov: bool = True, weight_decay: float = 0.0, scale: Optional[float] = None, steps: int = 5,
               coefficients=None, eps: float = 1e-7, workspace: Optional[torch.Tensor] = None) -> None:
     """bhtsne_muon_step: one step in place on the weights W and the fp32 momentum M (rows x cols, or batch x rows x
-    cols).  scale: None is sqrt(max(1, rows / cols))."""
+    cols), outside of torch's graph as an optimiser's.  scale: None is sqrt(max(1, rows / cols))."""
     lib = load_library()
     sizes = _matrix_sizes(W, "W")
     kind, shape = _type(W, "W"), W.shape
@@ -928,3 +936,4 @@ def muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, learning_rate: 
                               _stream_of(W))
     if rc:
         _check(rc, "bhtsne_muon_step")
+    _written((W, M))

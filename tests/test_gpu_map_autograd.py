@@ -93,3 +93,32 @@ def test_a_step_of_weights_that_require_gradients():
     before = w.detach().clone()
     bh.muon_step(w, w.grad, m, 0.1)
     assert w.is_leaf and w.requires_grad and not torch.equal(w.detach(), before)
+
+
+def overwrites():
+    x, w = gauss(8, 16, seed=7), gauss(16, seed=1)
+    mean, rstd = bh.layer_norm(x, w)[1:]
+    m = torch.zeros(8, 16, device=DEV)
+    yield "out=", lambda t: bh.layer_norm(t, w, out=t)
+    yield "dx=", lambda t: bh.layer_norm_backward(t, x, w, mean, rstd, dx=t)
+    yield "orthogonalise", lambda t: bh.orthogonalise(t, out=t)
+    yield "weights", lambda t: bh.muon_step(t, x, m.clone(), 0.1)
+    yield "momentum", lambda t: bh.muon_step(x.clone(), x, t, 0.1)
+
+
+def test_writing_in_place_is_known_to_the_graph():
+    """A graph that has saved a tensor does not run backward on what has been written into it since."""
+    for name, write in overwrites():
+        t, v = gauss(8, 16, seed=3), gauss(8, 16, seed=4).requires_grad_()
+        loss = (t * v).sum()  # saves t
+        before = t._version
+        with torch.no_grad():
+            write(t)
+        assert t._version > before, name
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+        if name != "momentum":
+            view = gauss(4, 8, 16, seed=5)
+            with torch.no_grad():
+                write(view[1])
+            assert view._version > 0, name
