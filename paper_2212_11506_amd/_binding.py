@@ -679,9 +679,22 @@ _written = torch.autograd.graph.increment_version  # a graph that has saved the 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream_of(t: torch.Tensor) -> int:
-    """The current stream of t's GPU."""
-    return _raw_stream(t.get_device()) if _raw_stream else torch.cuda.current_stream(t.device).cuda_stream
+_current_gpu = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _home(t: torch.Tensor, where: str) -> int:
+    """The GPU that a call runs on: the current one, which holds all its tensors."""
+    gpu = t.get_device()
+    if gpu < 0:
+        raise ValueError(f"{where} must be a GPU tensor")
+    if gpu != _current_gpu():
+        raise ValueError(f"{where} is on GPU {gpu}, the current one is {_current_gpu()}: call under torch.cuda.device({gpu})")
+    return gpu
+
+
+def _stream_of(gpu: int) -> int:
+    """The current stream of a GPU."""
+    return _raw_stream(gpu) if _raw_stream else torch.cuda.current_stream(gpu).cuda_stream
 
 
 def _type(t: torch.Tensor, where: str) -> int:
@@ -691,9 +704,11 @@ def _type(t: torch.Tensor, where: str) -> int:
     return kind
 
 
-def _refuse(t: torch.Tensor, where: str, shape, dtype):
+def _refuse(t: torch.Tensor, where: str, shape, dtype, gpu: int):
     if not t.is_cuda:
         raise ValueError(f"{where} must be a GPU tensor")
+    if t.get_device() != gpu:
+        raise ValueError(f"{where} is on GPU {t.get_device()}, the others on {gpu}")
     if t.dtype != dtype:
         raise ValueError(f"{where} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
@@ -701,29 +716,31 @@ def _refuse(t: torch.Tensor, where: str, shape, dtype):
     raise ValueError(f"{where} must be contiguous inside a row")
 
 
-def _rows(t: torch.Tensor, where: str, shape, dtype) -> int:
+def _rows(t: torch.Tensor, where: str, shape, dtype, gpu: int) -> int:
     """Checks a matrix with unit stride inside a row; the stride between its rows."""
-    if not (t.is_cuda and t.dtype == dtype and t.shape == shape):
-        _refuse(t, where, shape, dtype)
+    if not (t.get_device() == gpu and t.dtype == dtype and t.shape == shape):
+        _refuse(t, where, shape, dtype, gpu)
     row, inside = t.stride()
     if inside != 1 and shape[1] > 1:
-        _refuse(t, where, shape, dtype)
+        _refuse(t, where, shape, dtype, gpu)
     return row if shape[0] > 1 else shape[1]
 
 
-def _vector(t: Optional[torch.Tensor], where: str, size: int, dtype=None) -> Optional[int]:
+def _vector(t: Optional[torch.Tensor], where: str, size: int, gpu: int, dtype=None) -> Optional[int]:
     if t is None:
         return None
-    if t.is_cuda and t.numel() == size and t.is_contiguous() and (dtype is None or t.dtype == dtype):
+    if t.get_device() == gpu and t.numel() == size and t.is_contiguous() and (dtype is None or t.dtype == dtype):
         return t.data_ptr()
     if t.numel() != size:
         raise ValueError(f"{where} must have {size} values, got {t.numel()}")
-    return _ptr(t, dtype, where).value
+    _ptr(t, dtype, where)
+    raise ValueError(f"{where} is on GPU {t.get_device()}, the others on {gpu}")
 
 
-def _workspace_bytes(t: torch.Tensor) -> int:
-    if not t.is_cuda or not t.is_contiguous():
+def _workspace_bytes(t: torch.Tensor, gpu: int) -> int:
+    if t.get_device() != gpu or not t.is_contiguous():
         _ptr(t, None, "workspace")
+        raise ValueError(f"workspace is on GPU {t.get_device()}, the others on {gpu}")
     return t.numel() * t.element_size()
 
 
@@ -754,15 +771,16 @@ def _layer_norm(x, weight, bias, eps, out=None):
         raise ValueError(f"x must be n x d, got {tuple(x.shape)}")
     shape, dtype, kind = x.shape, x.dtype, _type(x, "x")
     n, d = shape
-    x_stride = _rows(x, "x", shape, dtype)
+    gpu = _home(x, "x")
+    x_stride = _rows(x, "x", shape, dtype, gpu)
     if out is None:
         y, y_stride = torch.empty_like(x) if x_stride == d else x.new_empty(shape), d
     else:
-        y, y_stride = out, _rows(out, "out", shape, dtype)
+        y, y_stride = out, _rows(out, "out", shape, dtype, gpu)
     mean, rstd = x.new_empty((2, n), dtype=torch.float32).unbind(0)
-    rc = lib.bhtsne_layer_norm(x.data_ptr(), x_stride, _vector(weight, "weight", d), _vector(bias, "bias", d), n, d, eps,
-                               kind, _param_type(weight, bias, dtype), y.data_ptr(), y_stride, mean.data_ptr(),
-                               rstd.data_ptr(), _stream_of(x))
+    rc = lib.bhtsne_layer_norm(x.data_ptr(), x_stride, _vector(weight, "weight", d, gpu), _vector(bias, "bias", d, gpu), n, d,
+                               eps, kind, _param_type(weight, bias, dtype), y.data_ptr(), y_stride, mean.data_ptr(),
+                               rstd.data_ptr(), _stream_of(gpu))
     if rc:
         _check(rc, "bhtsne_layer_norm")
     if out is not None:
@@ -811,27 +829,29 @@ def _layer_norm_backward(dy, x, weight, mean, rstd, bias_type=None, dx=None, wor
         raise ValueError(f"x must be n x d, got {tuple(x.shape)}")
     shape, dtype, kind = x.shape, x.dtype, _type(x, "x")
     n, d = shape
+    gpu = _home(x, "x")
     need = layer_norm_workspace_size(n, d)
     if need == 0:
         raise BhtsneError(BHTSNE_EINVAL, "bhtsne_layer_norm_workspace_size")
-    x_stride, dy_stride = _rows(x, "x", shape, dtype), _rows(dy, "dy", shape, dtype)
+    x_stride, dy_stride = _rows(x, "x", shape, dtype, gpu), _rows(dy, "dy", shape, dtype, gpu)
     given = dx
     if dx is None:
         dx, dx_stride = torch.empty_like(x) if x_stride == d else x.new_empty(shape), d
     else:
-        dx_stride = _rows(dx, "dx", shape, dtype)
+        dx_stride = _rows(dx, "dx", shape, dtype, gpu)
     if workspace is None:
         workspace = x.new_empty(need, dtype=torch.uint8)
     else:
-        need = _workspace_bytes(workspace)
+        need = _workspace_bytes(workspace, gpu)
     if weight is not None:
         _type(weight, "weight")
     ptype = weight.dtype if weight is not None else bias_type if bias_type is not None else dtype
     dweight, dbias = x.new_empty((2, d), dtype=ptype).unbind(0)
-    rc = lib.bhtsne_layer_norm_backward(dy.data_ptr(), dy_stride, x.data_ptr(), x_stride, _vector(weight, "weight", d),
-                                        _vector(mean, "mean", n, torch.float32), _vector(rstd, "rstd", n, torch.float32),
-                                        n, d, kind, _TYPES[ptype], dx.data_ptr(), dx_stride,
-                                        dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr(), need, _stream_of(x))
+    rc = lib.bhtsne_layer_norm_backward(dy.data_ptr(), dy_stride, x.data_ptr(), x_stride, _vector(weight, "weight", d, gpu),
+                                        _vector(mean, "mean", n, gpu, torch.float32),
+                                        _vector(rstd, "rstd", n, gpu, torch.float32), n, d, kind, _TYPES[ptype],
+                                        dx.data_ptr(), dx_stride, dweight.data_ptr(), dbias.data_ptr(),
+                                        workspace.data_ptr(), need, _stream_of(gpu))
     if rc:
         _check(rc, "bhtsne_layer_norm_backward")
     if given is not None:
@@ -839,12 +859,12 @@ def _layer_norm_backward(dy, x, weight, mean, rstd, bias_type=None, dx=None, wor
     return dx, dweight, dbias
 
 
-def _matrices(t: torch.Tensor, where: str, shape, dtype) -> _Matrices:
-    if not (t.is_cuda and t.dtype == dtype and t.shape == shape):
-        _refuse(t, where, shape, dtype)
+def _matrices(t: torch.Tensor, where: str, shape, dtype, gpu: int) -> _Matrices:
+    if not (t.get_device() == gpu and t.dtype == dtype and t.shape == shape):
+        _refuse(t, where, shape, dtype, gpu)
     stride = t.stride()
     if stride[-1] != 1 and shape[-1] > 1:
-        _refuse(t, where, shape, dtype)
+        _refuse(t, where, shape, dtype, gpu)
     return _Matrices(t.data_ptr(), stride[-2] if shape[-2] > 1 else shape[-1], stride[0] if len(shape) == 3 else 0)
 
 
@@ -887,9 +907,9 @@ def orthogonalise_workspace_size(batch: int, rows: int, cols: int) -> int:
     return int(load_library().bhtsne_orthogonalise_workspace_size(int(batch), int(rows), int(cols)))
 
 
-def _orthogonal_workspace(sizes, like, ws):
+def _orthogonal_workspace(sizes, like, ws, gpu: int):
     if ws is not None:
-        return ws, _workspace_bytes(ws)
+        return ws, _workspace_bytes(ws, gpu)
     need = orthogonalise_workspace_size(*sizes)
     if need == 0:
         raise BhtsneError(BHTSNE_EINVAL, "bhtsne_orthogonalise_workspace_size")
@@ -904,13 +924,13 @@ def orthogonalise(G: torch.Tensor, steps: int = 5, coefficients=None, eps: float
     if G.requires_grad and torch.is_grad_enabled():
         raise ValueError("orthogonalise has no gradient: take G.detach(), or call under torch.no_grad()")
     sizes = _matrix_sizes(G, "G")
-    kind, shape, dtype = _type(G, "G"), G.shape, G.dtype
-    g = _matrices(G, "G", shape, dtype)
+    kind, shape, dtype, gpu = _type(G, "G"), G.shape, G.dtype, _home(G, "G")
+    g = _matrices(G, "G", shape, dtype, gpu)
     O = out if out is not None else torch.empty_like(G, memory_format=torch.contiguous_format)
-    o = _matrices(O, "out", shape, dtype)
-    ws, nbytes = _orthogonal_workspace(sizes, G, workspace)
+    o = _matrices(O, "out", shape, dtype, gpu)
+    ws, nbytes = _orthogonal_workspace(sizes, G, workspace, gpu)
     rc = lib.bhtsne_orthogonalise(C.byref(g), *sizes, kind, _coefficients(coefficients, steps), steps, eps, C.byref(o),
-                                  ws.data_ptr(), nbytes, _stream_of(G))
+                                  ws.data_ptr(), nbytes, _stream_of(gpu))
     if rc:
         _check(rc, "bhtsne_orthogonalise")
     if out is not None:
@@ -925,15 +945,15 @@ def muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, learning_rate: 
     cols), outside of torch's graph as an optimiser's.  scale: None is sqrt(max(1, rows / cols))."""
     lib = load_library()
     sizes = _matrix_sizes(W, "W")
-    kind, shape = _type(W, "W"), W.shape
-    w, g = _matrices(W, "W", shape, W.dtype), _matrices(G, "G", shape, W.dtype)
-    m = _matrices(M, "M", shape, torch.float32)
+    kind, shape, gpu = _type(W, "W"), W.shape, _home(W, "W")
+    w, g = _matrices(W, "W", shape, W.dtype, gpu), _matrices(G, "G", shape, W.dtype, gpu)
+    m = _matrices(M, "M", shape, torch.float32, gpu)
     if scale is None:
         scale = max(1.0, sizes[1] / max(1, sizes[2])) ** 0.5
-    ws, nbytes = _orthogonal_workspace(sizes, W, workspace)
+    ws, nbytes = _orthogonal_workspace(sizes, W, workspace, gpu)
     rc = lib.bhtsne_muon_step(C.byref(w), C.byref(g), C.byref(m), *sizes, kind, learning_rate, momentum, bool(nesterov),
                               weight_decay, scale, _coefficients(coefficients, steps), steps, eps, ws.data_ptr(), nbytes,
-                              _stream_of(W))
+                              _stream_of(gpu))
     if rc:
         _check(rc, "bhtsne_muon_step")
     _written((W, M))
