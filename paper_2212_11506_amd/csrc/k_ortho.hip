@@ -12,9 +12,11 @@
 // factor of a each step against the largest, and the largest come out of terms
 // that cancel, so each product is three, high by high and the two mixed ones, for
 // outputs of every type.  a X is added to B X in fp32: as part of B, a I would
-// round with B's small values beside it, and errors of matrices of low rank would
-// double (eight directions over noise, 400 x 300: 4.5e-5 against 64 bits where the
-// formula in 32 bits is off by 2.5e-5, and this by 2.6e-5).
+// round with B's small values beside it, and matrices of low rank or of values that
+// fall off would lose by it (against 64 bits, eight directions over noise, 1024 x
+// 1030: 5.3e-5, apart 3.0e-5; the formula in 32 bits, term by term, 4.5e-5).  So
+// the result is as far from 64 bits as the formula in 32 bits, 1.2 times at most in
+// what was measured: 1e-6 to 2e-6 for gaussian values, 2e-4 for rank 1.
 #include <type_traits>
 
 #include "map.hpp"
@@ -116,8 +118,9 @@ __device__ inline void split(float v, f16 &h, f16 &l)
 
 // U / (|U| + eps) in planes, in both orientations, zeros in the padding.  Where |U| is far below eps, X is small and
 // stays small, and fp16 would lose it: it is held larger by a power of two, 1 / `lift`, such that no step passes its
-// bound.  Only A and the output are formed with `lift`; the products that lead from X to X are linear in it.  Bound by its writes: 4096 x 4096 bf16 34 us for
-// 118 MB (3.4 TB/s); 1024 x 1024 9 us, of which the partial norms and the first values are some 3 of latency.
+// bound.  Only A and the output are formed with `lift`; the products that lead from X to X are linear in it.
+// Bound by HBM: 4096 x 4096 bf16 34 us for 134 MB written and 34 read (4.9 TB/s); 1024 x 1024 11 us, of which the partial
+// norms and the first values are some 3 of latency.
 template <typename E>
 __global__ __launch_bounds__(256) void orth_planes_kernel(OrthArgs a, char *ws, OrthLayout L, int norm_blocks, float sx, double reach)
 {
@@ -202,11 +205,10 @@ enum class Prod { kGram, kPoly, kApply, kLast };
 // row r in place c ^ (r % 8)), so that the lanes of a fragment read, which take the same piece of 16 rows, fall on
 // different banks.  Tiles may hang over the padded sides: their loads repeat the last row, nothing is stored there.
 //
-// 4096 x 4096 bf16: symmetric products 76 us (0.9 PFLOP/s of the half that is computed, the other half is stored from
-// it), X' 133 us (1.0 PFLOP/s).  Of the latter the loop takes 109, in which the products alone would take 76 (at the
-// 1.7 GHz that they leave of the clock) and the loads alone 76; the rest is the epilogue's 128 MB, which all blocks move
-// at once.  1024 x 1024 bf16: 7.2 and 9.2 us, of which a launch is 2.5, the first slices 1.3, the loop 3 to 4 (16 TB/s from
-// the L2 caches) and the epilogue 1 to 2.
+// 4096 x 4096: symmetric products 315 us by tiles of 64 (0.65 PFLOP/s of the half that is computed, the other half is
+// stored from it; matrix cores busy 40 % of the time), X' 400 us by tiles of 128 (1.0 PFLOP/s, 48 %): bound by the loop,
+// in which every wave of a CU reads and multiplies at the same time (below).  1024 x 1024: 14.0 and 13.6 us, of which a
+// launch is 2.5 and the first slices 1.3.
 constexpr int kK = 64;
 typedef float float4v __attribute__((ext_vector_type(4)));
 template <int M, int N, int Wm, int Wn, int Stages> struct Tile {
@@ -242,8 +244,8 @@ __device__ inline int xcd_tile(int b, int blocks)
 }
 
 // What a product's blocks take.  The first 64 bytes are what the loop waits for: one line of the arguments, with the
-// pointers and quotients made on the host, so that the first loads are on their way early (1024 x 1024
-// bf16 127 us a pass against 131, 512 x 512 71 against 75).
+// pointers and quotients made on the host, so that the first loads are on their way early (with one product of halves
+// for three, 1024 x 1024 took 127 us a pass against 131, 512 x 512 71 against 75).
 struct alignas(64) OrthProduct {
     const f16 *P, *Q;         // of the first matrix
     int64_t stride;           // bytes between matrices
@@ -330,9 +332,11 @@ __global__ __launch_bounds__(T::kThreads) void orth_product_kernel(OrthProduct a
                     (__attribute__((address_space(3))) void *)(to + h * kPlane + (e * T::kWaves + w) * 8 * kK), 16, 0, 0);
     };
     const int wi = w / T::kWn * (T::kI * 16), wj = w % T::kWn * (T::kJ * 16);
-    // Two sets of fragments: one half of a slice is multiplied while the other is read.  In the middle of a slice both
-    // of its halves have been read, by every wave after the barrier, so its buffer is filled again there, and the next
-    // slice, which has landed, is read from there on.
+    // Two sets of fragments.  The second half of a slice is multiplied while the next slice's first is read.  The first
+    // half's products wait for both halves: the waits in the assembly below are not the compiler's, which still counts
+    // the first half's reads as under way and has one wait for all.  In the middle of a slice both of its halves have
+    // been read, by every wave after the barrier, so its buffer is filled again there, and the next slice, which has
+    // landed, is read from there on.
     float4v acc[T::kI][T::kJ] = {};
     half8 p[2][kPlanes][T::kI], q[2][kPlanes][T::kJ];
     const auto read = [&](int slice, int half) {
@@ -586,11 +590,13 @@ void run_steps(const OrthArgs &a, const OrthSteps &steps, char *ws, const OrthLa
 // B = a I + b A + c A^2 the product of the steps is Q <- B Q, and the next A is B A B.  So U is read for one Gram
 // matrix, the steps run on m x m matrices in one block's LDS, and Q is applied to U once: n enters twice, not
 // 3 steps times.  In fewer than 64 bits A would lose the small singular values (their squares against the largest's;
-// 1e-4 with 32); in fp64 on the matrix cores the result is off by its own rounding alone, and |U|^2 is A's trace.
+// 1e-4 with 32); in fp64 on the matrix cores the result is off by its own rounding and 2e-8 at most (kNarrowNoise), and
+// |U|^2 is A's trace.
 // One launch where one block is quick with all of it; else one for the slices' Gram matrices and one in which every
 // block adds them up in a fixed order, repeats the steps and applies Q to its columns.  Bound by the chain of products
 // in one CU: a step takes 0.85 / 1.9 / 3.6 / 7.3 us for 16 / 32 / 48 / 64 directions (50: 6.5), of which the matrix core's 64 cycles
-// a 16 x 16 x 4 product are two thirds at 64 (2 x 128 fp32 7.9 us in all, 256 x 50 8.8 and 42.7).
+// a 16 x 16 x 4 product are 64 % for 64 directions (eleven tiles after one another on the fullest SIMD, 16 products each) and
+// 58 % for 50 (13 each).  2 x 128 fp32 takes 7.9 us in all, 256 x 50 8.8 and 42.7.
 
 typedef double double4v __attribute__((ext_vector_type(4)));
 
