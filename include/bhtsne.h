@@ -556,11 +556,13 @@ typedef struct bhtsne_matrices {
  *     X <- a X + (b A + c A^2) X;     O = X.
  *   G, O    `batch` matrices of rows x cols of `type`; O may be G.
  *   coefficients  host, steps x 3 doubles (a, b, c of each step), nullable: the
- *           quintic (3.4445, -4.7750, 2.0315) for every step.  A singular value
+ *           quintic (3.4445, -4.7750, 2.0315) for every step, as published with the
+ *           Muon optimiser (K. Jordan and others, 2024).  A singular value
  *           of X in [0, 1] must stay below 64 under them (BHTSNE_EINVAL).
  *   1 <= steps <= 32; eps finite and >= 0 (a zero matrix stays zero for eps > 0).
  * With a side of 64 or less the steps are computed in fp64; else the products run
- * on the matrix cores on pairs of fp16 values (22 bits an operand), with fp32 sums.
+ * on the matrix cores on pairs of fp16 values (22 bits an operand), with fp32 sums:
+ * as far from the formula in 64 bits as the formula in 32 bits is.
  * 0 <= batch <= 65535, 1 <= rows, cols <= 65536.  O's matrices lie one behind the
  * other (batch_stride >= (rows - 1) stride + cols), or their rows between one
  * another's (batch_stride >= cols, stride >= (batch - 1) batch_stride + cols, as in
