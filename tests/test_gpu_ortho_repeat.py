@@ -13,8 +13,10 @@ DEV = "cuda"
 @pytest.mark.parametrize("shape", [(65, 300), (130, 200), (500, 520), (1024, 1030), (1500, 700), (2048, 2100), (4000, 4160)])
 def test_same_bits_again(shape, dtype):
     G = torch.randn(shape, generator=torch.Generator().manual_seed(shape[0])).to(dtype).to(DEV)
+    # memory of its own before the first call: what that call frees is still in use on this stream
+    side, other = torch.cuda.Stream(), torch.zeros(1 << 24, device=DEV)
+    side.wait_stream(torch.cuda.current_stream())
     first = bh.orthogonalise(G)
-    side, other = torch.cuda.Stream(), torch.empty(1 << 24, device=DEV)
     for k in range(3):
         with torch.cuda.stream(side):
             for _ in range(4):
