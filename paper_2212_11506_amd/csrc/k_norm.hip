@@ -9,9 +9,10 @@
 // 2^k lanes of a wave (up to 1024 features at 16 a lane), or of a whole block
 // (up to 16384; backward, with two rows and the weights' sums, half of both),
 // so that the mean, the centred sum of squares and the outputs come from one
-// read; the next row's loads are in flight while a row is computed.  Sums are
-// fp32, of 16 terms a lane at most, and fp64 in longer rows and in the weight
-// gradients' last join; the only rounding to fewer bits is that of the outputs.
+// read; the next row's loads are in flight while a row is computed.  A row's sums
+// are fp32, of 16 terms a lane at most, and fp64 in longer rows; the weights'
+// gradients are summed in fp32 by a block and in fp64 over the blocks.  The only
+// rounding to fewer bits is that of the outputs.
 #include <type_traits>
 
 #include "map.hpp"
