@@ -590,6 +590,107 @@ int bhtsne_muon_step(const bhtsne_matrices *W, const bhtsne_matrices *G, const b
                      double weight_decay, double scale, const double *coefficients, int steps, double eps,
                      void *workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* A gated hidden layer of n points from d to f features:
+ *     a = x gate^T,  b = x up^T,  h = act(a) b,
+ *     act(a) = a / (1 + exp(-a))              (BHTSNE_SILU)
+ *            = a / 2 (1 + erf(a / sqrt(2)))   (BHTSNE_GELU)
+ *   x         n x d of `type`; x_stride >= d, or 0 for one row that stands for all.
+ *   gate, up  f x d (a row a feature), of the same type.
+ *   h         n x f; a, b  n x f, each nullable: what the backward pass takes.
+ * Sums are fp32; h is computed from a and b before they are rounded.
+ * 0 <= n < 2^31, 1 <= d, f <= 65536, strides < 2^31.  No output overlaps an
+ * input or another output.
+ * Errors: BHTSNE_EINVAL, BHTSNE_EDEVICE. */
+enum {
+    BHTSNE_SILU = 0,
+    BHTSNE_GELU = 1
+};
+int bhtsne_gated_layer(const void *x, int64_t x_stride, const void *gate, int64_t gate_stride, const void *up,
+                       int64_t up_stride, int64_t n, int64_t d, int64_t f, int activation, int type, void *h,
+                       int64_t h_stride, void *a, int64_t a_stride, void *b, int64_t b_stride, hipStream_t stream);
+
+/* The backward pass, from a and b as they are given:
+ *     da = dh b act'(a),  db = dh act(a),
+ *     dx = da gate + db up,  dgate = da^T x,  dup = db^T x
+ *   dh, a, b  n x f of `type`, x n x d; a stride of 0 as above.
+ *   dx        n x d, nullable; dgate, dup  f x d, each nullable, overwritten
+ *             (zero for n = 0); one output at least is wanted.
+ * da and db are rounded to `type` before the products; the sums over features
+ * and points are fp32, those over parts of the points are joined in a fixed
+ * order: the same inputs give the same bits.  The workspace is
+ * bhtsne_gated_layer_workspace_size bytes (256-byte aligned; 0 for sizes out of
+ * range).  No output overlaps an input or another output.
+ * Errors: BHTSNE_EINVAL, BHTSNE_EWORKSPACE, BHTSNE_EDEVICE. */
+size_t bhtsne_gated_layer_workspace_size(int64_t n, int64_t d, int64_t f, int type);
+int bhtsne_gated_layer_backward(const void *dh, int64_t dh_stride, const void *x, int64_t x_stride, const void *gate,
+                                int64_t gate_stride, const void *up, int64_t up_stride, const void *a, int64_t a_stride,
+                                const void *b, int64_t b_stride, int64_t n, int64_t d, int64_t f, int activation,
+                                int type, void *dx, int64_t dx_stride, void *dgate, int64_t dgate_stride, void *dup,
+                                int64_t dup_stride, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Rows in 8 bits, with a scale for each: scale = max|x| / 127 (an fp32 quotient),
+ * q = x / scale rounded to the nearest integer, ties to even.  A row of zeros
+ * has the scale 0 and zeros; a row that holds a NaN or an infinity has the
+ * scale NaN and zeros, so that what is computed from it is NaN.
+ *   x  n x d of `type` (a stride of 0 as above);  q  n x d;  scale  n values.
+ * 0 <= n < 2^31, 1 <= d <= 131071, strides < 2^31.
+ * Errors: BHTSNE_EINVAL, BHTSNE_EDEVICE. */
+enum { BHTSNE_I8 = 3 };
+int bhtsne_quantise_rows(const void *x, int64_t x_stride, int64_t n, int64_t d, int type, int8_t *q, int64_t q_stride,
+                         float *scale, hipStream_t stream);
+
+/* A dense layer of 8-bit integers with a scale for each point and each feature:
+ *     out_ij = x_scale_i w_scale_j sum_k x_ik w_jk + bias_j
+ *   x        n x d: of x_type BHTSNE_I8 with x_scale (n values), or of one of the
+ *            other types with x_scale null: then its rows are quantised first, as
+ *            by bhtsne_quantise_rows.  x_stride >= d, or 0 as above.
+ *   w        f x d (a row a feature), w_scale  f values.
+ *   bias     f values of bias_type (`type` or BHTSNE_F32), nullable.
+ *   out      n x f of `type`.
+ * The sums are exact (32-bit integers; d <= 131071), the scales are applied in
+ * fp32.  0 <= n < 2^31, 1 <= f < 2^31, strides < 2^31.  out overlaps no input.
+ * The workspace (bhtsne_linear_i8_workspace_size bytes, 256-byte aligned; 0 for
+ * sizes out of range) is needed where x is not BHTSNE_I8.
+ * Errors: BHTSNE_EINVAL, BHTSNE_EWORKSPACE, BHTSNE_EDEVICE. */
+size_t bhtsne_linear_i8_workspace_size(int64_t n, int64_t d);
+int bhtsne_linear_i8(const void *x, int64_t x_stride, int x_type, const float *x_scale, const int8_t *w,
+                     int64_t w_stride, const float *w_scale, const void *bias, int64_t n, int64_t d, int64_t f, int type,
+                     int bias_type, void *out, int64_t out_stride, void *workspace, size_t workspace_bytes,
+                     hipStream_t stream);
+
+/* The loss of a map that gives each point logits z over v classes (points,
+ * landmarks), against the logits u of k listed ones (the teacher's largest; a
+ * point's neighbours with u = -d^2 / (2 sigma^2)), at a temperature T:
+ *     t = softmax(u / T) over the list,  q = softmax(z / T) over all v,
+ *     loss_i = sum_j t_j (log t_j - log q_idx(j)),   lse_i = log sum exp(z / T)
+ * and its gradient
+ *     dz = dloss_i / T (q - t at the listed places).
+ *   logits   n x v of `type`.
+ *   idx      n x k int32, teacher  n x k of teacher_type (`type` or BHTSNE_F32), in
+ *            any order.  An index outside [0, v) marks an entry that is absent; so
+ *            does a teacher's logit of minus infinity.  A row without entries has
+ *            the loss 0 and a gradient of zero.  A class that is listed more than
+ *            once gets the sum of its shares; the loss takes each entry by itself.
+ *            (idx and teacher may be null for k = 0.)
+ *   loss, lse  n fp32 values, each nullable, one at least is wanted.
+ *   dloss    n fp32 values; lse as the forward call gave it.
+ *   dlogits  n x v of `type`; may be logits (with their stride).
+ * Input strides are >= the row's length, or 0 for one row that stands for all.
+ * 0 <= n < 2^31, 1 <= v < 2^31, 0 <= k <= 2048, strides < 2^31, T in [1e-6, 1e6].
+ * Sums over v are fp32 in a lane and joined in fp64, in a fixed order.  The
+ * workspace (bhtsne_distil_loss_workspace_size bytes, 256-byte aligned; 0 for
+ * sizes out of range) is needed where it is more than 256 bytes: few long rows.
+ * Errors: BHTSNE_EINVAL, BHTSNE_EWORKSPACE, BHTSNE_EDEVICE. */
+size_t bhtsne_distil_loss_workspace_size(int64_t n, int64_t v);
+int bhtsne_distil_loss(const void *logits, int64_t stride, int64_t n, int64_t v, const int32_t *idx, int64_t idx_stride,
+                       const void *teacher, int64_t teacher_stride, int64_t k, double temperature, int type,
+                       int teacher_type, float *loss, float *lse, void *workspace, size_t workspace_bytes,
+                       hipStream_t stream);
+int bhtsne_distil_loss_backward(const float *dloss, const void *logits, int64_t stride, int64_t n, int64_t v,
+                                const int32_t *idx, int64_t idx_stride, const void *teacher, int64_t teacher_stride,
+                                int64_t k, const float *lse, double temperature, int type, int teacher_type,
+                                void *dlogits, int64_t dlogits_stride, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

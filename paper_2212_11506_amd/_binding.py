@@ -131,6 +131,20 @@ def load_library():
                                            vp]),
         "bhtsne_muon_step": (C.c_int, [vp, vp, vp, i64, i64, i64, C.c_int, C.c_double, C.c_double, C.c_int,
                                        C.c_double, C.c_double, f64p, C.c_int, C.c_double, vp, C.c_size_t, vp]),
+        "bhtsne_gated_layer": (C.c_int, [vp, i64, vp, i64, vp, i64, i64, i64, i64, C.c_int, C.c_int, vp, i64, vp, i64, vp,
+                                         i64, vp]),
+        "bhtsne_gated_layer_workspace_size": (C.c_size_t, [i64, i64, i64, C.c_int]),
+        "bhtsne_gated_layer_backward": (C.c_int, [vp, i64] * 6 + [i64, i64, i64, C.c_int, C.c_int] + [vp, i64] * 3
+                                        + [vp, C.c_size_t, vp]),
+        "bhtsne_quantise_rows": (C.c_int, [vp, i64, i64, i64, C.c_int, vp, i64, vp, vp]),
+        "bhtsne_linear_i8_workspace_size": (C.c_size_t, [i64, i64]),
+        "bhtsne_linear_i8": (C.c_int, [vp, i64, C.c_int, vp, vp, i64, vp, vp, i64, i64, i64, C.c_int, C.c_int, vp, i64, vp,
+                                       C.c_size_t, vp]),
+        "bhtsne_distil_loss_workspace_size": (C.c_size_t, [i64, i64]),
+        "bhtsne_distil_loss": (C.c_int, [vp, i64, i64, i64, vp, i64, vp, i64, i64, C.c_double, C.c_int, C.c_int, vp, vp, vp,
+                                         C.c_size_t, vp]),
+        "bhtsne_distil_loss_backward": (C.c_int, [vp, vp, i64, i64, i64, vp, i64, vp, i64, i64, vp, C.c_double, C.c_int,
+                                                  C.c_int, vp, i64, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -957,3 +971,279 @@ def muon_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, learning_rate: 
     if rc:
         _check(rc, "bhtsne_muon_step")
     _written((W, M))
+
+
+# ------------------------------------------------------------------ dense operators of a trained map
+_ACTIVATIONS = {"silu": 0, "gelu": 1}  # BHTSNE_SILU, BHTSNE_GELU
+_I8 = 3
+
+
+def _activation(name: str) -> int:
+    kind = _ACTIVATIONS.get(name)
+    if kind is None:
+        raise ValueError(f"activation must be one of {sorted(_ACTIVATIONS)}, got {name!r}")
+    return kind
+
+
+def _layer_sizes(x: torch.Tensor, gate: torch.Tensor):
+    if x.dim() != 2 or gate.dim() != 2:
+        raise ValueError(f"x must be n x d and gate f x d, got {tuple(x.shape)} and {tuple(gate.shape)}")
+    return x.shape[0], x.shape[1], gate.shape[0]
+
+
+def gated_layer(x: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, activation: str = "silu", keep: bool = False,
+                out: Optional[torch.Tensor] = None):
+    """bhtsne_gated_layer: h = act(x gate^T) (x up^T) of x (n x d) and the weights gate and up (f x d, a row a feature);
+    with keep (h, a, b), a = x gate^T and b = x up^T being what the backward pass takes.
+
+    h's gradient goes to x, gate and up through bhtsne_gated_layer_backward (once); a and b have none, and neither has a
+    call with out."""
+    if torch.is_grad_enabled() and (x.requires_grad or gate.requires_grad or up.requires_grad):
+        if out is not None:
+            raise ValueError("out has no gradient: leave it out, or call under torch.no_grad()")
+        h, a, b = _GatedLayer.apply(x, gate, up, activation)
+        return (h, a, b) if keep else h
+    h, a, b = _gated_layer(x, gate, up, activation, keep, out)
+    return (h, a, b) if keep else h
+
+
+def _gated_layer(x, gate, up, activation, keep, out=None):
+    lib = load_library()
+    n, d, f = _layer_sizes(x, gate)
+    act, dtype, kind, gpu = _activation(activation), x.dtype, _type(x, "x"), _home(x, "x")
+    x_stride = _rows(x, "x", x.shape, dtype, gpu)
+    gate_stride, up_stride = _rows(gate, "gate", (f, d), dtype, gpu), _rows(up, "up", (f, d), dtype, gpu)
+    h_stride = f if out is None else _rows(out, "out", (n, f), dtype, gpu)
+    h = out if out is not None else x.new_empty((n, f))
+    a, b = (x.new_empty((n, f)), x.new_empty((n, f))) if keep else (None, None)
+    rc = lib.bhtsne_gated_layer(x.data_ptr(), x_stride, gate.data_ptr(), gate_stride, up.data_ptr(), up_stride, n, d, f, act, kind,
+                                h.data_ptr(), h_stride, a.data_ptr() if keep else None, f, b.data_ptr() if keep else None, f,
+                                _stream_of(gpu))
+    if rc:
+        _check(rc, "bhtsne_gated_layer")
+    if out is not None:
+        _written(out)
+    return h, a, b
+
+
+class _GatedLayer(torch.autograd.Function):
+    """gated_layer as a node of torch's graph."""
+
+    @staticmethod
+    def forward(ctx, x, gate, up, activation):
+        h, a, b = _gated_layer(x, gate, up, activation, True)
+        ctx.save_for_backward(x, gate, up, a, b)
+        ctx.activation = activation
+        ctx.mark_non_differentiable(a, b)
+        return h, a, b
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dh, _a, _b):
+        x, gate, up, a, b = ctx.saved_tensors
+        if (dh.shape[1] > 1 and dh.stride(1) != 1) or (dh.shape[0] > 1 and 0 < dh.stride(0) < dh.shape[1]):
+            dh = dh.contiguous()
+        return (*_gated_layer_backward(dh, x, gate, up, a, b, ctx.activation, ctx.needs_input_grad[:3]), None)
+
+
+@functools.lru_cache(maxsize=256)
+def gated_layer_workspace_size(n: int, d: int, f: int, dtype: torch.dtype = torch.float32) -> int:
+    return int(load_library().bhtsne_gated_layer_workspace_size(int(n), int(d), int(f), _TYPES[dtype]))
+
+
+def gated_layer_backward(dh: torch.Tensor, x: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
+                         activation: str = "silu", workspace: Optional[torch.Tensor] = None):
+    """bhtsne_gated_layer_backward: (dx, dgate, dup) from a and b as gated_layer kept them.  The results have no gradient
+    of their own."""
+    return _gated_layer_backward(dh, x, gate, up, a, b, activation, (True, True, True), workspace)
+
+
+def _gated_layer_backward(dh, x, gate, up, a, b, activation, wanted, workspace=None):
+    lib = load_library()
+    n, d, f = _layer_sizes(x, gate)
+    act, dtype, kind, gpu = _activation(activation), x.dtype, _type(x, "x"), _home(x, "x")
+    need = gated_layer_workspace_size(n, d, f, dtype)
+    if need == 0:
+        raise BhtsneError(BHTSNE_EINVAL, "bhtsne_gated_layer_workspace_size")
+    wide, tall = (n, f), (f, d)
+    strides = (_rows(dh, "dh", wide, dtype, gpu), _rows(x, "x", x.shape, dtype, gpu), _rows(gate, "gate", tall, dtype, gpu),
+               _rows(up, "up", tall, dtype, gpu), _rows(a, "a", wide, dtype, gpu), _rows(b, "b", wide, dtype, gpu))
+    if workspace is None:
+        workspace = x.new_empty(need, dtype=torch.uint8)
+    else:
+        need = _workspace_bytes(workspace, gpu)
+    dx = x.new_empty((n, d)) if wanted[0] else None
+    dgate, dup = (x.new_empty(tall) if w else None for w in wanted[1:])
+    rc = lib.bhtsne_gated_layer_backward(dh.data_ptr(), strides[0], x.data_ptr(), strides[1], gate.data_ptr(), strides[2],
+                                         up.data_ptr(), strides[3], a.data_ptr(), strides[4], b.data_ptr(), strides[5], n, d, f,
+                                         act, kind, dx.data_ptr() if wanted[0] else None, d,
+                                         dgate.data_ptr() if wanted[1] else None, d, dup.data_ptr() if wanted[2] else None, d,
+                                         workspace.data_ptr(), need, _stream_of(gpu))
+    if rc:
+        _check(rc, "bhtsne_gated_layer_backward")
+    return dx, dgate, dup
+
+
+def quantise_rows(x: torch.Tensor):
+    """bhtsne_quantise_rows: (q, scale), int8 values of x's shape and a fp32 scale for each row."""
+    lib = load_library()
+    _no_gradient(x, "quantise_rows")
+    if x.dim() != 2:
+        raise ValueError(f"x must be n x d, got {tuple(x.shape)}")
+    n, d = x.shape
+    kind, gpu = _type(x, "x"), _home(x, "x")
+    stride = _rows(x, "x", x.shape, x.dtype, gpu)
+    q, scale = x.new_empty((n, d), dtype=torch.int8), x.new_empty(n, dtype=torch.float32)
+    rc = lib.bhtsne_quantise_rows(x.data_ptr(), stride, n, d, kind, q.data_ptr(), d, scale.data_ptr(), _stream_of(gpu))
+    if rc:
+        _check(rc, "bhtsne_quantise_rows")
+    return q, scale
+
+
+def _no_gradient(t: torch.Tensor, where: str):
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{where} has no gradient: detach its inputs, or call under torch.no_grad()")
+
+
+@functools.lru_cache(maxsize=256)
+def linear_i8_workspace_size(n: int, d: int) -> int:
+    return int(load_library().bhtsne_linear_i8_workspace_size(int(n), int(d)))
+
+
+def linear_i8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, x_scale: Optional[torch.Tensor] = None,
+              bias: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+              workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """bhtsne_linear_i8: x_scale_i w_scale_j sum_k x_ik w_jk + bias_j of x (n x d) and int8 weights w (f x d, a row a
+    feature, as quantise_rows gives them).  x is int8 with x_scale, or of another type without: its rows are then quantised
+    on the way.  dtype: of the result, None is out's, x's, or float32 for an int8 x; bias is of that type or float32.  It
+    has no gradient, and refuses inputs whose graph torch records."""
+    lib = load_library()
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError(f"x must be n x d and w f x d, got {tuple(x.shape)} and {tuple(w.shape)}")
+    for t in (x, w_scale, x_scale, bias):
+        if t is not None:
+            _no_gradient(t, "linear_i8")
+    (n, d), f = x.shape, w.shape[0]
+    whole, gpu = x.dtype == torch.int8, _home(x, "x")
+    if whole != (x_scale is not None):
+        raise ValueError("an int8 x comes with its x_scale, another without")
+    x_kind = _I8 if whole else _type(x, "x")
+    if out is not None and dtype is not None and out.dtype != dtype:
+        raise ValueError(f"out must be {dtype}, got {out.dtype}")
+    if dtype is None:
+        dtype = out.dtype if out is not None else torch.float32 if whole else x.dtype
+    kind = _TYPES.get(dtype)
+    if kind is None:
+        raise ValueError(f"dtype must be float32, float16 or bfloat16, got {dtype}")
+    x_stride, w_stride = _rows(x, "x", x.shape, x.dtype, gpu), _rows(w, "w", (f, d), torch.int8, gpu)
+    out_stride = f if out is None else _rows(out, "out", (n, f), dtype, gpu)
+    result = out if out is not None else x.new_empty((n, f), dtype=dtype)
+    bias_kind = kind
+    if bias is not None:
+        bias_kind = _TYPES.get(bias.dtype)
+        if bias_kind not in (kind, 0):
+            raise ValueError(f"bias must be {dtype} or float32, got {bias.dtype}")
+    need = 0
+    if workspace is not None:
+        need = _workspace_bytes(workspace, gpu)
+    elif not whole:
+        need = linear_i8_workspace_size(n, d)
+        if need == 0:
+            raise BhtsneError(BHTSNE_EINVAL, "bhtsne_linear_i8_workspace_size")
+        workspace = x.new_empty(need, dtype=torch.uint8)
+    rc = lib.bhtsne_linear_i8(x.data_ptr(), x_stride, x_kind, _vector(x_scale, "x_scale", n, gpu, torch.float32), w.data_ptr(), w_stride,
+                              _vector(w_scale, "w_scale", f, gpu, torch.float32), _vector(bias, "bias", f, gpu), n, d, f, kind,
+                              bias_kind, result.data_ptr(), out_stride, workspace.data_ptr() if workspace is not None else None, need,
+                              _stream_of(gpu))
+    if rc:
+        _check(rc, "bhtsne_linear_i8")
+    if out is not None:
+        _written(out)
+    return result
+
+
+def _lists(logits: torch.Tensor, idx: torch.Tensor, teacher: torch.Tensor):
+    """Checks what both directions of distil_loss take: the arguments from logits to k, and the two types."""
+    if logits.dim() != 2 or idx.dim() != 2:
+        raise ValueError(f"logits must be n x v and idx n x k, got {tuple(logits.shape)} and {tuple(idx.shape)}")
+    (n, v), k = logits.shape, idx.shape[1]
+    kind, gpu = _type(logits, "logits"), _home(logits, "logits")
+    teacher_kind = _type(teacher, "teacher")
+    if teacher_kind not in (kind, 0):
+        raise ValueError(f"teacher must be {logits.dtype} or float32, got {teacher.dtype}")
+    args = (logits.data_ptr(), _rows(logits, "logits", logits.shape, logits.dtype, gpu), n, v, idx.data_ptr(),
+            _rows(idx, "idx", (n, k), torch.int32, gpu), teacher.data_ptr(), _rows(teacher, "teacher", (n, k), teacher.dtype, gpu), k)
+    return args, kind, teacher_kind, gpu
+
+
+@functools.lru_cache(maxsize=256)
+def distil_loss_workspace_size(n: int, v: int) -> int:
+    return int(load_library().bhtsne_distil_loss_workspace_size(int(n), int(v)))
+
+
+def distil_loss(logits: torch.Tensor, idx: torch.Tensor, teacher: torch.Tensor, temperature: float = 1.0,
+                workspace: Optional[torch.Tensor] = None):
+    """bhtsne_distil_loss: (loss, lse), n values each, of logits (n x v) against the teacher's logits (n x k) of the classes
+    idx (n x k int32; outside [0, v): absent).
+
+    loss's gradient goes to the logits through bhtsne_distil_loss_backward (once); lse has none, and the teacher neither:
+    one whose graph torch records is refused."""
+    _no_gradient(teacher, "the teacher of distil_loss")
+    if logits.requires_grad and torch.is_grad_enabled():
+        return _DistilLoss.apply(logits, idx, teacher, float(temperature), workspace)
+    return _distil_loss(logits, idx, teacher, temperature, workspace)
+
+
+def _distil_loss(logits, idx, teacher, temperature, workspace=None):
+    lib = load_library()
+    args, kind, teacher_kind, gpu = _lists(logits, idx, teacher)
+    n, v = logits.shape
+    loss, lse = logits.new_empty((2, n), dtype=torch.float32).unbind(0)
+    if workspace is not None:
+        need = _workspace_bytes(workspace, gpu)
+    else:
+        need = distil_loss_workspace_size(n, v)
+        if need > 256:
+            workspace = logits.new_empty(need, dtype=torch.uint8)
+    rc = lib.bhtsne_distil_loss(*args, temperature, kind, teacher_kind, loss.data_ptr(), lse.data_ptr(),
+                                workspace.data_ptr() if workspace is not None else None, need, _stream_of(gpu))
+    if rc:
+        _check(rc, "bhtsne_distil_loss")
+    return loss, lse
+
+
+class _DistilLoss(torch.autograd.Function):
+    """distil_loss as a node of torch's graph."""
+
+    @staticmethod
+    def forward(ctx, logits, idx, teacher, temperature, workspace):
+        loss, lse = _distil_loss(logits, idx, teacher, temperature, workspace)
+        ctx.save_for_backward(logits, idx, teacher, lse)
+        ctx.temperature = temperature
+        ctx.mark_non_differentiable(lse)
+        return loss, lse
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss, _lse):
+        logits, idx, teacher, lse = ctx.saved_tensors
+        return distil_loss_backward(dloss.contiguous(), logits, idx, teacher, lse, ctx.temperature), None, None, None, None
+
+
+def distil_loss_backward(dloss: torch.Tensor, logits: torch.Tensor, idx: torch.Tensor, teacher: torch.Tensor, lse: torch.Tensor,
+                         temperature: float = 1.0, dlogits: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """bhtsne_distil_loss_backward: the gradient of the logits, of their type; dlogits may be the logits.  The result has no
+    gradient of its own."""
+    lib = load_library()
+    args, kind, teacher_kind, gpu = _lists(logits, idx, teacher)
+    n, v = logits.shape
+    stride = v if dlogits is None else _rows(dlogits, "dlogits", logits.shape, logits.dtype, gpu)
+    out = dlogits if dlogits is not None else logits.new_empty((n, v))
+    rc = lib.bhtsne_distil_loss_backward(_vector(dloss, "dloss", n, gpu, torch.float32), *args,
+                                         _vector(lse, "lse", n, gpu, torch.float32), temperature, kind, teacher_kind,
+                                         out.data_ptr(), stride, _stream_of(gpu))
+    if rc:
+        _check(rc, "bhtsne_distil_loss_backward")
+    if dlogits is not None:
+        _written(dlogits)
+    return out

@@ -20,7 +20,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["k_sort.hip", "k_tree.hip", "k_forces.hip", "k_layout.hip", "k_eval.hip", "k_affinity.hip",
-           "k_norm.hip", "k_ortho.hip", "api.cpp", "api_map.cpp"]
+           "k_norm.hip", "k_ortho.hip", "k_gated.hip", "k_linear8.hip", "k_distil.hip", "api.cpp", "api_map.cpp", "api_dense.cpp"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-I", CSRC, "-I", INCLUDE,
           "-Wall", "-Wno-unused-function",

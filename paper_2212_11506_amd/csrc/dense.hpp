@@ -1,0 +1,99 @@
+// Internal declarations of the dense operators of a trained map: gated hidden
+// layers, products of 8-bit integers, and the loss from neighbour lists.
+#pragma once
+
+#include "map.hpp"
+
+namespace bht {
+
+// ------------------------------------------------------- loss from neighbour lists
+constexpr int64_t kDistilMaxList = 2048;       // listed neighbours of a row: 16 bytes of LDS each
+constexpr int64_t kDistilSplit = 8192;         // values of a row at least that a block takes, of rows that are shared out
+constexpr int64_t kDistilBlocks = 2048;        // blocks that fill the chip: rows are shared out below so many
+constexpr int64_t kDistilWave = 2048;          // rows up to this are a wave's, longer ones a block's
+
+// blocks that share a row of v logits, of n rows
+inline int distil_parts(int64_t n, int64_t v)
+{
+    const int64_t most = (v + kDistilSplit - 1) / kDistilSplit, want = n > 0 ? kDistilBlocks / n : 1;
+    return int(want < 1 ? 1 : want < most ? want : most);
+}
+
+struct DistilArgs {
+    const void *logits;  // n x v
+    const int32_t *idx;  // n x k
+    const void *teacher; // n x k
+    const float *dloss;  // backward
+    const float *lse_in; // backward
+    float *loss, *lse;   // forward, each nullable
+    void *out;           // backward: n x v, may be logits
+    float2 *part;        // forward: (largest logit, sum) of each part of a row
+    int64_t stride, idx_stride, teacher_stride, out_stride;
+    int64_t n, v;
+    int32_t k, parts;
+    double temperature;
+    Elem type;
+    bool wide_teacher; // fp32, else of `type`
+};
+void launch_distil_loss(const DistilArgs &a, hipStream_t st);
+void launch_distil_loss_backward(const DistilArgs &a, hipStream_t st);
+
+// ---------------------------------------------------------------- gated layers
+enum class Act { kSilu = 0, kGelu = 1 };
+
+struct GatedArgs {
+    const void *x, *gate, *up; // n x d, f x d
+    void *h, *a, *b;           // n x f; a and b nullable
+    int64_t x_stride, gate_stride, up_stride, h_stride, a_stride, b_stride;
+    int64_t n, d, f;
+    Act act;
+    Elem type;
+};
+void launch_gated_layer(const GatedArgs &a, hipStream_t st);
+
+// Backward: da and db side by side (n rows), both transposed (2 f rows), x and the weights transposed, rows padded to
+// 16 bytes; partial sums of the weights' gradients where they are shared out over the points.
+constexpr int64_t pad16(int64_t count, int bytes) { return (count * bytes + 15) / 16 * 16 / bytes; }
+struct GatedBackLayout {
+    int64_t fp, np;      // padded features and points
+    int splits;          // of the sums over points
+    size_t d, dt, xt, wt, part, total;
+};
+GatedBackLayout make_gated_back_layout(int64_t n, int64_t d, int64_t f, Elem type);
+
+struct GatedBackArgs {
+    const void *dh, *x, *gate, *up, *a, *b;
+    void *dx, *dgate, *dup; // each nullable
+    int64_t dh_stride, x_stride, gate_stride, up_stride, a_stride, b_stride, dx_stride, dgate_stride, dup_stride;
+    int64_t n, d, f;
+    Act act;
+    Elem type;
+    void *ws;
+};
+void launch_gated_layer_backward(const GatedBackArgs &a, hipStream_t st);
+
+// ---------------------------------------------------------- products of 8-bit integers
+constexpr int64_t kLinearMaxDepth = 131071; // (-128)^2 so many times stays below 2^31
+
+struct QuantiseArgs {
+    const void *x;
+    int8_t *q;
+    float *scale;
+    int64_t x_stride, q_stride;
+    int64_t n, d;
+    Elem type;
+};
+void launch_quantise_rows(const QuantiseArgs &a, hipStream_t st);
+
+struct LinearArgs {
+    const int8_t *x, *w;
+    const float *x_scale, *w_scale;
+    const void *bias; // nullable
+    void *out;
+    int64_t x_stride, w_stride, out_stride;
+    int64_t n, d, f;
+    Elem type, bias_type;
+};
+void launch_linear_i8(const LinearArgs &a, hipStream_t st);
+
+} // namespace bht

@@ -1,0 +1,402 @@
+// A gated hidden layer: h = act(a) b with a = x gate^T, b = x up^T, and its backward pass.
+//
+// Forward is one product of x with both matrices: a wave holds a and b of the same
+// points and features in its registers, so the activation and the product are its
+// epilogue, and neither a nor b has to go to memory (they are written, rounded once,
+// where the backward pass will take them).
+//
+// Backward, with a and b as they were kept:
+//   da = dh b act'(a), db = dh act(a);  dx = da gate + db up;  dgate = da^T x, dup = db^T x
+// da and db are formed once, in fp32, and rounded to the inputs' type, as operands of
+// matrix instructions of that type: with bf16 their rounding adds to the output's own
+// (1.7e-3 each, 2.4e-3 together).  The sums over features and points are fp32.
+#include "products.hpp"
+
+namespace bht {
+namespace {
+
+using namespace prod;
+
+typedef Tile<256, 256, 2, 4, 2> TileLarge;
+typedef Tile<128, 128, 2, 2, 2> TileMiddle;
+typedef Tile<64, 64, 2, 2, 3> TileSmall;
+
+// ------------------------------------------------------------------ activations
+// fp32 with the library's exponential; 16-bit outputs do not show the instruction's last bits
+template <typename E> __device__ inline float sigmoid(float a)
+{
+    if constexpr (sizeof(E) == 4)
+        return 1.0f / (1.0f + expf(-a));
+    else
+        return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a * -1.44269504f));
+}
+template <typename E> __device__ inline float activate(float a, Act act)
+{
+    if (act == Act::kSilu) return a * sigmoid<E>(a);
+    return 0.5f * a * erfcf(a * -0.707106781f); // no difference of near values for a far below zero
+}
+template <typename E> __device__ inline void activate_both(float a, Act act, float &value, float &slope)
+{
+    if (act == Act::kSilu) {
+        const float s = sigmoid<E>(a);
+        value = a * s;
+        slope = s * (1.0f + a * (1.0f - s));
+    } else {
+        const float phi = 0.5f * erfcf(a * -0.707106781f);
+        value = a * phi;
+        slope = phi + a * (0.398942280f * __builtin_amdgcn_exp2f(a * a * -0.721347520f));
+    }
+}
+
+// ------------------------------------------------------------------ forward
+struct GatedOut {
+    void *h, *a, *b;
+    int64_t h_stride, a_stride, b_stride;
+    Act act;
+    bool vec_h, vec_a, vec_b;
+};
+
+template <typename E, typename T, bool kAny>
+__global__ __launch_bounds__(T::kThreads) void gated_kernel(Product p, GatedOut o)
+{
+    constexpr int kRun = 2 * T::kJ; // features of a lane
+    int32_t bi, bj;
+    place(p, bi, bj);
+    typename Ops<E>::Acc acc[T::kI][T::kJ] = {};
+    multiply_tile<E, T, true, kAny>(p, bi, bj, acc);
+    each_run<T, true>(bi, bj, [&](int64_t point, int64_t feature, int i) {
+        if (point >= p.rows) return;
+        float a[kRun], b[kRun], h[kRun];
+#pragma unroll
+        for (int e = 0; e < kRun; ++e) {
+            a[e] = acc[i][e / 4][e % 4];
+            b[e] = acc[i][T::kJ / 2 + e / 4][e % 4];
+            h[e] = activate<E>(a[e], o.act) * b[e];
+        }
+        const int64_t count = p.features - feature;
+        store_run(static_cast<E *>(o.h) + point * o.h_stride + feature, h, count, o.vec_h);
+        if (o.a) store_run(static_cast<E *>(o.a) + point * o.a_stride + feature, a, count, o.vec_a);
+        if (o.b) store_run(static_cast<E *>(o.b) + point * o.b_stride + feature, b, count, o.vec_b);
+    });
+}
+
+template <typename E, typename T, bool kAny> void run_gated(const GatedArgs &a, hipStream_t st)
+{
+    constexpr int64_t kF = T::kN / 2;
+    Product p = {};
+    p.B = static_cast<const char *>(a.gate);
+    p.B2 = static_cast<const char *>(a.up);
+    p.a_stride = a.x_stride * int64_t(sizeof(E));
+    p.b_stride = a.gate_stride * int64_t(sizeof(E));
+    p.b2_stride = a.up_stride * int64_t(sizeof(E));
+    p.features = a.f;
+    p.bytes = a.d * int64_t(sizeof(E));
+    p.slices = p.per_split = int32_t((p.bytes + kSlice - 1) / kSlice);
+    p.across = int32_t((a.f + kF - 1) / kF);
+    const size_t lds = size_t(kAny && p.slices == 1 ? 1 : T::kStages) * T::kBuffer;
+    const int64_t most = kMostTiles / p.across > 0 ? kMostTiles / p.across * T::kM : T::kM; // points of a launch
+    for (int64_t from = 0; from < a.n; from += most) {
+        p.A = static_cast<const char *>(a.x) + from * p.a_stride;
+        p.rows = a.n - from < most ? a.n - from : most;
+        p.down = int32_t((p.rows + T::kM - 1) / T::kM);
+        GatedOut o = {};
+        o.h = static_cast<E *>(a.h) + from * a.h_stride;
+        o.a = a.a ? static_cast<E *>(a.a) + from * a.a_stride : nullptr;
+        o.b = a.b ? static_cast<E *>(a.b) + from * a.b_stride : nullptr;
+        o.h_stride = a.h_stride;
+        o.a_stride = a.a_stride;
+        o.b_stride = a.b_stride;
+        o.act = a.act;
+        o.vec_h = aligned16(a.h, a.h_stride * int64_t(sizeof(E)));
+        o.vec_a = aligned16(a.a, a.a_stride * int64_t(sizeof(E)));
+        o.vec_b = aligned16(a.b, a.b_stride * int64_t(sizeof(E)));
+        gated_kernel<E, T, kAny><<<uint32_t(p.down) * uint32_t(p.across), T::kThreads, lds, st>>>(p, o);
+    }
+}
+
+int64_t tiles_of(int64_t rows, int64_t cols, int m, int n) { return (rows + m - 1) / m * ((cols + n - 1) / n); }
+
+template <typename E> void run_gated_type(const GatedArgs &a, hipStream_t st)
+{
+    const int64_t es = int64_t(sizeof(E));
+    const bool any = !aligned16(a.x, a.x_stride * es) || !aligned16(a.gate, a.gate_stride * es) || !aligned16(a.up, a.up_stride * es)
+                     || a.d * es % 16 != 0;
+    const bool large = tiles_of(a.n, a.f, 256, 128) >= kCus, middle = tiles_of(a.n, a.f, 128, 64) >= kCus;
+    if (any) {
+        if (large || middle) return run_gated<E, TileMiddle, true>(a, st);
+        return run_gated<E, TileSmall, true>(a, st);
+    }
+    if (large) return run_gated<E, TileLarge, false>(a, st);
+    if (middle) return run_gated<E, TileMiddle, false>(a, st);
+    run_gated<E, TileSmall, false>(a, st);
+}
+
+// ------------------------------------------------------------------ backward: operands
+constexpr int kT = 64;
+
+template <typename E> __device__ inline float load_or_zero(const void *p, int64_t stride, int64_t r, int64_t c, bool there)
+{
+    const E *e = static_cast<const E *>(p);
+    return float(e[there ? r * stride + c : 0]);
+}
+
+// Tiles of 64 points x 64 features: da and db in both orientations, zeros in the padding
+template <typename E> __global__ __launch_bounds__(256) void gated_slopes_kernel(GatedBackArgs a, GatedBackLayout L, int64_t row0)
+{
+    __shared__ float s_a[kT][kT + 1], s_b[kT][kT + 1];
+    const int64_t r0 = (row0 + blockIdx.y) * kT, c0 = int64_t(blockIdx.x) * kT;
+    char *ws = static_cast<char *>(a.ws);
+    E *d = reinterpret_cast<E *>(ws + L.d), *dt = reinterpret_cast<E *>(ws + L.dt);
+    for (int s = threadIdx.x; s < kT * kT; s += 256) {
+        const int row = s / kT, col = s % kT;
+        const int64_t r = r0 + row, c = c0 + col;
+        const bool there = r < a.n && c < a.f;
+        const float dh = load_or_zero<E>(a.dh, a.dh_stride, r, c, there);
+        const float av = load_or_zero<E>(a.a, a.a_stride, r, c, there), bv = load_or_zero<E>(a.b, a.b_stride, r, c, there);
+        float value, slope;
+        activate_both<E>(av, a.act, value, slope);
+        const float da = there ? dh * bv * slope : 0.0f, db = there ? dh * value : 0.0f;
+        s_a[row][col] = da;
+        s_b[row][col] = db;
+        if (a.dx && r < a.n && c < L.fp) {
+            d[r * 2 * L.fp + c] = E(da);
+            d[r * 2 * L.fp + L.fp + c] = E(db);
+        }
+    }
+    if (!a.dgate && !a.dup) return;
+    __syncthreads();
+    for (int s = threadIdx.x; s < kT * kT; s += 256) {
+        const int col = s / kT, row = s % kT;
+        const int64_t r = r0 + row, c = c0 + col;
+        if (r >= L.np || c >= a.f) continue;
+        dt[c * L.np + r] = E(s_a[row][col]);
+        dt[(a.f + c) * L.np + r] = E(s_b[row][col]);
+    }
+}
+
+// out[c][r] = in[r][c], rows of `out` `ld` long, zeros for r from rows up to `to`
+template <typename E>
+__global__ __launch_bounds__(256) void transpose_kernel(const E *in, int64_t stride, int64_t rows, int64_t cols, E *out, int64_t ld, int64_t to,
+                                                        int64_t row0)
+{
+    __shared__ E s_t[kT][kT + 2];
+    const int64_t r0 = (row0 + blockIdx.y) * kT, c0 = int64_t(blockIdx.x) * kT;
+    for (int s = threadIdx.x; s < kT * kT; s += 256) {
+        const int row = s / kT, col = s % kT;
+        const bool there = r0 + row < rows && c0 + col < cols;
+        const E v = in[there ? (r0 + row) * stride + c0 + col : 0];
+        s_t[row][col] = there ? v : E(0.0f);
+    }
+    __syncthreads();
+    for (int s = threadIdx.x; s < kT * kT; s += 256) {
+        const int col = s / kT, row = s % kT;
+        if (r0 + row < to && c0 + col < cols) out[(c0 + col) * ld + r0 + row] = s_t[row][col];
+    }
+}
+
+constexpr int64_t kMostRowTiles = 65535; // of a launch
+
+template <typename E>
+void transpose(const void *in, int64_t stride, int64_t rows, int64_t cols, E *out, int64_t ld, int64_t to, hipStream_t st)
+{
+    const int64_t down = (to + kT - 1) / kT;
+    for (int64_t from = 0; from < down; from += kMostRowTiles) {
+        const int64_t y = down - from < kMostRowTiles ? down - from : kMostRowTiles;
+        transpose_kernel<E><<<dim3(uint32_t((cols + kT - 1) / kT), uint32_t(y)), 256, 0, st>>>(static_cast<const E *>(in), stride, rows, cols,
+                                                                                               out, ld, to, from);
+    }
+}
+
+// ------------------------------------------------------------------ backward: products
+// kPart: fp32 partial sums of a split; else the outputs, whose rows from `first2` on are those of out2
+struct BackOut {
+    void *out, *out2;
+    float *part;
+    int64_t stride, stride2, first2;
+    bool vec, vec2;
+};
+
+template <typename E, typename T, bool kPart>
+__global__ __launch_bounds__(T::kThreads) void gated_back_kernel(Product p, BackOut o)
+{
+    constexpr int kRun = 4 * T::kJ;
+    int32_t bi, bj;
+    place(p, bi, bj);
+    typename Ops<E>::Acc acc[T::kI][T::kJ] = {};
+    multiply_tile<E, T, false, false>(p, bi, bj, acc);
+    each_run<T, false>(bi, bj, [&](int64_t row, int64_t feature, int i) {
+        if (row >= p.rows) return;
+        float v[kRun];
+#pragma unroll
+        for (int e = 0; e < kRun; ++e) v[e] = acc[i][e / 4][e % 4];
+        const int64_t count = p.features - feature;
+        if constexpr (kPart) {
+            store_run(o.part + (int64_t(blockIdx.y) * p.rows + row) * p.features + feature, v, count, o.vec);
+        } else {
+            const bool second = row >= o.first2;
+            E *out = static_cast<E *>(second ? o.out2 : o.out);
+            if (out) store_run(out + (second ? row - o.first2 : row) * (second ? o.stride2 : o.stride) + feature, v, count, second ? o.vec2 : o.vec);
+        }
+    });
+}
+
+// The splits' sums in a fixed order, fp64
+template <typename E> __global__ __launch_bounds__(256) void gated_join_kernel(BackOut o, int64_t rows, int64_t features, int splits)
+{
+    const int64_t total = rows * features;
+    for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < total; e += int64_t(gridDim.x) * 256) {
+        double sum = 0.0;
+        for (int s = 0; s < splits; ++s) sum += double(o.part[s * total + e]);
+        const int64_t row = e / features, col = e - row * features;
+        const bool second = row >= o.first2;
+        E *out = static_cast<E *>(second ? o.out2 : o.out);
+        if (out) out[(second ? row - o.first2 : row) * (second ? o.stride2 : o.stride) + col] = E(float(sum));
+    }
+}
+
+template <typename E, typename T>
+void run_back(Product p, const BackOut &o, int splits, hipStream_t st)
+{
+    p.slices = int32_t((p.bytes + kSlice - 1) / kSlice);
+    p.per_split = (p.slices + splits - 1) / splits;
+    p.across = int32_t((p.features + T::kN - 1) / T::kN);
+    const size_t lds = size_t(T::kStages) * T::kBuffer;
+    const int64_t all = p.rows, most = kMostTiles / p.across > 0 ? kMostTiles / p.across * T::kM : T::kM;
+    const char *A = p.A;
+    for (int64_t from = 0; from < all; from += most) { // several launches only for dx, which has no second matrix
+        p.A = A + from * p.a_stride;
+        p.rows = all - from < most ? all - from : most;
+        p.down = int32_t((p.rows + T::kM - 1) / T::kM);
+        BackOut q = o;
+        if (q.out) q.out = static_cast<E *>(o.out) + from * o.stride;
+        const dim3 grid(uint32_t(p.down) * uint32_t(p.across), uint32_t(splits));
+        if (splits > 1)
+            gated_back_kernel<E, T, true><<<grid, T::kThreads, lds, st>>>(p, q);
+        else
+            gated_back_kernel<E, T, false><<<grid, T::kThreads, lds, st>>>(p, q);
+    }
+}
+
+template <typename E> void run_back_tile(const Product &p, const BackOut &o, int splits, hipStream_t st)
+{
+    if (tiles_of(p.rows, p.features, 256, 256) * splits >= kCus) return run_back<E, TileLarge>(p, o, splits, st);
+    if (tiles_of(p.rows, p.features, 128, 128) * splits >= kCus) return run_back<E, TileMiddle>(p, o, splits, st);
+    run_back<E, TileSmall>(p, o, splits, st);
+}
+
+template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st)
+{
+    const GatedBackLayout L = make_gated_back_layout(a.n, a.d, a.f, a.type);
+    const int64_t es = int64_t(sizeof(E));
+    char *ws = static_cast<char *>(a.ws);
+    E *d = reinterpret_cast<E *>(ws + L.d), *dt = reinterpret_cast<E *>(ws + L.dt);
+    E *xt = reinterpret_cast<E *>(ws + L.xt), *wt = reinterpret_cast<E *>(ws + L.wt);
+    const bool weights = a.dgate || a.dup;
+    const int64_t cols = L.fp > a.f ? L.fp : a.f, down = (L.np + kT - 1) / kT;
+    for (int64_t from = 0; from < down; from += kMostRowTiles) {
+        const int64_t y = down - from < kMostRowTiles ? down - from : kMostRowTiles;
+        gated_slopes_kernel<E><<<dim3(uint32_t((cols + kT - 1) / kT), uint32_t(y)), 256, 0, st>>>(a, L, from);
+    }
+    if (a.dx) {
+        transpose<E>(a.gate, a.gate_stride, a.f, a.d, wt, 2 * L.fp, L.fp, st);
+        transpose<E>(a.up, a.up_stride, a.f, a.d, wt + L.fp, 2 * L.fp, L.fp, st);
+        Product p = {};
+        p.A = reinterpret_cast<const char *>(d);
+        p.B = reinterpret_cast<const char *>(wt);
+        p.a_stride = p.b_stride = p.bytes = 2 * L.fp * es;
+        p.rows = a.n;
+        p.features = a.d;
+        BackOut o = {};
+        o.out = a.dx;
+        o.stride = a.dx_stride;
+        o.first2 = int64_t(1) << 62;
+        o.vec = aligned16(a.dx, a.dx_stride * es);
+        run_back_tile<E>(p, o, 1, st);
+    }
+    if (weights) {
+        transpose<E>(a.x, a.x_stride, a.n, a.d, xt, L.np, L.np, st);
+        Product p = {};
+        p.A = reinterpret_cast<const char *>(dt);
+        p.B = reinterpret_cast<const char *>(xt);
+        p.a_stride = p.b_stride = p.bytes = L.np * es;
+        p.rows = 2 * a.f;
+        p.features = a.d;
+        BackOut o = {};
+        o.out = a.dgate;
+        o.out2 = a.dup;
+        o.stride = a.dgate_stride;
+        o.stride2 = a.dup_stride;
+        o.first2 = a.f;
+        o.part = reinterpret_cast<float *>(ws + L.part);
+        o.vec = L.splits > 1 ? a.d % 4 == 0 : aligned16(a.dgate, a.dgate_stride * es);
+        o.vec2 = aligned16(a.dup, a.dup_stride * es);
+        run_back_tile<E>(p, o, L.splits, st);
+        if (L.splits > 1) {
+            const int64_t blocks = (2 * a.f * a.d + 255) / 256;
+            gated_join_kernel<E><<<uint32_t(blocks < 8192 ? blocks : 8192), 256, 0, st>>>(o, 2 * a.f, a.d, L.splits);
+        }
+    }
+}
+
+template <typename E> __global__ __launch_bounds__(256) void gated_zero_kernel(E *p, int64_t stride, int64_t rows, int64_t cols)
+{
+    const int64_t total = rows * cols;
+    for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < total; e += int64_t(gridDim.x) * 256)
+        p[e / cols * stride + e % cols] = E(0.0f);
+}
+
+// no points: the weights' gradients are zero
+template <typename E> void run_gated_zero(const GatedBackArgs &a, hipStream_t st)
+{
+    const int64_t blocks = (a.f * a.d + 255) / 256;
+    const uint32_t grid = uint32_t(blocks < 8192 ? blocks : 8192);
+    if (a.dgate) gated_zero_kernel<E><<<grid, 256, 0, st>>>(static_cast<E *>(a.dgate), a.dgate_stride, a.f, a.d);
+    if (a.dup) gated_zero_kernel<E><<<grid, 256, 0, st>>>(static_cast<E *>(a.dup), a.dup_stride, a.f, a.d);
+}
+
+} // namespace
+
+GatedBackLayout make_gated_back_layout(int64_t n, int64_t d, int64_t f, Elem type)
+{
+    const int es = elem_bytes(type);
+    GatedBackLayout L = {};
+    L.fp = pad16(f, es);
+    L.np = pad16(n, es);
+    // enough tiles of the weights' gradients for the chip, of eight slices at least each
+    const int64_t slices = (L.np * es + kSlice - 1) / kSlice;
+    const int64_t tiles = tiles_of(2 * f, d, 128, 128), most = (slices + 7) / 8;
+    int64_t splits = (2 * kCus + tiles - 1) / tiles;
+    splits = splits < 1 ? 1 : splits < most ? splits : most < 1 ? 1 : most;
+    const int64_t each = (slices + splits - 1) / splits;
+    L.splits = int(each > 0 ? (slices + each - 1) / each : 1); // none of them empty
+    size_t at = 0;
+    const auto take = [&](int64_t count, int bytes) {
+        const size_t here = at;
+        at += (size_t(count) * size_t(bytes) + 255) / 256 * 256;
+        return here;
+    };
+    L.d = take(n * 2 * L.fp, es);
+    L.dt = take(2 * f * L.np, es);
+    L.xt = take(d * L.np, es);
+    L.wt = take(d * 2 * L.fp, es);
+    L.part = take(L.splits > 1 ? L.splits * 2 * f * d : 0, 4);
+    L.total = at > 0 ? at : 256;
+    return L;
+}
+
+void launch_gated_layer(const GatedArgs &a, hipStream_t st)
+{
+    if (a.n == 0) return;
+    if (a.type == Elem::kF32) return run_gated_type<float>(a, st);
+    if (a.type == Elem::kF16) return run_gated_type<f16>(a, st);
+    run_gated_type<bf16>(a, st);
+}
+
+void launch_gated_layer_backward(const GatedBackArgs &a, hipStream_t st)
+{
+    if (a.type == Elem::kF32) return a.n == 0 ? run_gated_zero<float>(a, st) : run_gated_back<float>(a, st);
+    if (a.type == Elem::kF16) return a.n == 0 ? run_gated_zero<f16>(a, st) : run_gated_back<f16>(a, st);
+    a.n == 0 ? run_gated_zero<bf16>(a, st) : run_gated_back<bf16>(a, st);
+}
+
+} // namespace bht

@@ -1,0 +1,217 @@
+// Products of 8-bit integers with a scale for each point and each feature.
+//
+//   quantise:  s = max|x| / 127 (fp32),  q = x / s rounded to the nearest integer, ties to even
+//   product:   out = s_i t_j sum_k q_ik w_jk + bias_j
+//
+// The sums are exact: 32-bit integers hold 131071 products of 8-bit values.  The
+// quantisation reads a row once, into the registers of a wave or a block, and is
+// bound by HBM; the product runs on the matrix cores' 8-bit instructions.
+#include "products.hpp"
+
+namespace bht {
+namespace {
+
+using namespace prod;
+
+// ------------------------------------------------------------------ quantisation
+constexpr int kRowValues = 16; // of a thread at a time
+
+// 16 values from p, of which `left` exist, zeros behind
+template <typename E> __device__ inline void load_values(const E *p, int64_t left, float (&v)[kRowValues])
+{
+    constexpr int kV = 16 / int(sizeof(E));
+#pragma unroll
+    for (int h = 0; h < kRowValues / kV; ++h) {
+        const Piece x = any_piece<E>(reinterpret_cast<const char *>(p + h * kV), (left - h * kV) * int64_t(sizeof(E)));
+        E e[kV];
+        __builtin_memcpy(e, &x, 16);
+#pragma unroll
+        for (int k = 0; k < kV; ++k) v[h * kV + k] = float(e[k]);
+    }
+}
+
+// x / s rounded as the quotient in 64 bits is.  The product with 1 / s is off by some 2e-5 at most: nearer to the border
+// of two integers (and where 1 / s is infinite) the division decides, which is exact there.
+__device__ inline int quantise(float x, float s, float inverse)
+{
+    const float r = x * inverse, k = rintf(r);
+    int q = int(k);
+    if (!(fabsf(r - k) < 0.4999f)) {
+        const double d = rint(double(x) / double(s));
+        q = int(fmin(fmax(d, -127.0), 127.0)); // a scale among the smallest numbers is a rough one
+    }
+    return q;
+}
+
+template <typename E, int kThreads> __global__ __launch_bounds__(kThreads) void quantise_kernel(QuantiseArgs a)
+{
+    constexpr int kWaves = kThreads / kWave;
+    __shared__ float s_max[kWaves];
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        const E *x = static_cast<const E *>(a.x) + row * a.x_stride;
+        int8_t *q = a.q + row * a.q_stride;
+        float v[kRowValues], top = 0.0f;
+        const auto take = [&](int64_t at) {
+            load_values(x + at, a.d - at, v);
+#pragma unroll
+            for (int e = 0; e < kRowValues; ++e) {
+                const float m = fabsf(v[e]);
+                top = m <= top ? top : m < INFINITY ? m : INFINITY; // NaN counts as an infinity, which stays
+            }
+        };
+        for (int64_t at = int64_t(threadIdx.x) * kRowValues; at < a.d; at += kThreads * kRowValues) take(at);
+        top = wave_max(top);
+        if constexpr (kWaves > 1) {
+            if (lane_id() == 0) s_max[threadIdx.x / kWave] = top;
+            __syncthreads();
+            top = s_max[0];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_max[w]);
+            __syncthreads();
+        }
+        const bool finite = top < INFINITY;
+        const float scale = finite ? top / 127.0f : NAN, inverse = 1.0f / scale;
+        if (threadIdx.x == 0) a.scale[row] = scale;
+        const bool aligned = (reinterpret_cast<uintptr_t>(q) & 15) == 0;
+        for (int64_t at = int64_t(threadIdx.x) * kRowValues; at < a.d; at += kThreads * kRowValues) {
+            if (a.d > kThreads * kRowValues) load_values(x + at, a.d - at, v);
+            struct alignas(16) {
+                int8_t v[kRowValues];
+            } out;
+#pragma unroll
+            for (int e = 0; e < kRowValues; ++e) out.v[e] = int8_t(finite && scale > 0.0f ? quantise(v[e], scale, inverse) : 0);
+            if (aligned && at + kRowValues <= a.d) {
+                *reinterpret_cast<Piece *>(q + at) = __builtin_bit_cast(Piece, out);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kRowValues; ++e)
+                    if (at + e < a.d) q[at + e] = out.v[e];
+            }
+        }
+    }
+}
+
+template <typename E> void run_quantise(const QuantiseArgs &a, hipStream_t st)
+{
+    const uint32_t blocks = uint32_t(a.n < (int64_t(1) << 20) ? a.n : int64_t(1) << 20);
+    if (a.d <= 64 * kRowValues)
+        quantise_kernel<E, 64><<<blocks, 64, 0, st>>>(a);
+    else if (a.d <= 128 * kRowValues)
+        quantise_kernel<E, 128><<<blocks, 128, 0, st>>>(a);
+    else if (a.d <= 256 * kRowValues)
+        quantise_kernel<E, 256><<<blocks, 256, 0, st>>>(a);
+    else
+        quantise_kernel<E, 1024><<<blocks, 1024, 0, st>>>(a);
+}
+
+// ------------------------------------------------------------------ product
+typedef Tile<256, 256, 2, 4, 2> TileLarge;
+typedef Tile<128, 128, 2, 2, 2> TileMiddle;
+typedef Tile<64, 64, 2, 2, 3> TileSmall;
+
+struct LinearOut {
+    const float *x_scale, *w_scale;
+    const void *bias;
+    void *out;
+    int64_t stride;
+    bool wide_bias, vec;
+};
+
+template <typename E, typename T, bool kAny>
+__global__ __launch_bounds__(T::kThreads) void linear8_kernel(Product p, LinearOut o)
+{
+    constexpr int kRun = 4 * T::kJ;
+    int32_t bi, bj;
+    place(p, bi, bj);
+    Ops<int8_t>::Acc acc[T::kI][T::kJ] = {};
+    multiply_tile<int8_t, T, false, kAny>(p, bi, bj, acc);
+    float scale[kRun], bias[kRun];
+    each_run<T, false>(bi, bj, [&](int64_t point, int64_t feature, int i) {
+        if (i == 0) {
+#pragma unroll
+            for (int e = 0; e < kRun; ++e) {
+                const int64_t at = feature + e < p.features ? feature + e : p.features - 1;
+                scale[e] = o.w_scale[at];
+                bias[e] = 0.0f;
+            }
+        }
+        if (i == 0 && o.bias) {
+            if (o.wide_bias) {
+#pragma unroll
+                for (int e = 0; e < kRun; ++e) bias[e] = static_cast<const float *>(o.bias)[feature + e < p.features ? feature + e : p.features - 1];
+            } else {
+#pragma unroll
+                for (int e = 0; e < kRun; ++e) bias[e] = float(static_cast<const E *>(o.bias)[feature + e < p.features ? feature + e : p.features - 1]);
+            }
+        }
+        if (point >= p.rows) return;
+        const float s = o.x_scale[point];
+        float v[kRun];
+#pragma unroll
+        for (int e = 0; e < kRun; ++e) v[e] = float(acc[i][e / 4][e % 4]) * s * scale[e] + bias[e];
+        store_run(static_cast<E *>(o.out) + point * o.stride + feature, v, p.features - feature, o.vec);
+    });
+}
+
+template <typename E, typename T, bool kAny> void run_linear(const LinearArgs &a, hipStream_t st)
+{
+    Product p = {};
+    p.B = reinterpret_cast<const char *>(a.w);
+    p.a_stride = a.x_stride;
+    p.b_stride = a.w_stride;
+    p.features = a.f;
+    p.bytes = a.d;
+    p.slices = p.per_split = int32_t((a.d + kSlice - 1) / kSlice);
+    p.across = int32_t((a.f + T::kN - 1) / T::kN);
+    const size_t lds = size_t(kAny && p.slices == 1 ? 1 : T::kStages) * T::kBuffer;
+    const int64_t most = kMostTiles / p.across > 0 ? kMostTiles / p.across * T::kM : T::kM;
+    for (int64_t from = 0; from < a.n; from += most) {
+        p.A = reinterpret_cast<const char *>(a.x) + from * a.x_stride;
+        p.rows = a.n - from < most ? a.n - from : most;
+        p.down = int32_t((p.rows + T::kM - 1) / T::kM);
+        LinearOut o = {};
+        o.x_scale = a.x_scale + from;
+        o.w_scale = a.w_scale;
+        o.bias = a.bias;
+        o.out = static_cast<E *>(a.out) + from * a.out_stride;
+        o.stride = a.out_stride;
+        o.wide_bias = a.bias_type == Elem::kF32;
+        o.vec = aligned16(a.out, a.out_stride * int64_t(sizeof(E)));
+        linear8_kernel<E, T, kAny><<<uint32_t(p.down) * uint32_t(p.across), T::kThreads, lds, st>>>(p, o);
+    }
+}
+
+int64_t tiles_of(int64_t rows, int64_t cols, int side) { return (rows + side - 1) / side * ((cols + side - 1) / side); }
+
+template <typename E> void run_linear_type(const LinearArgs &a, hipStream_t st)
+{
+    const bool any = !aligned16(a.x, a.x_stride) || !aligned16(a.w, a.w_stride) || a.d % 16 != 0;
+    const bool large = tiles_of(a.n, a.f, 256) >= kCus, middle = tiles_of(a.n, a.f, 128) >= kCus;
+    if (any) {
+        if (large || middle) return run_linear<E, TileMiddle, true>(a, st);
+        return run_linear<E, TileSmall, true>(a, st);
+    }
+    if (large) return run_linear<E, TileLarge, false>(a, st);
+    if (middle) return run_linear<E, TileMiddle, false>(a, st);
+    run_linear<E, TileSmall, false>(a, st);
+}
+
+} // namespace
+
+void launch_quantise_rows(const QuantiseArgs &a, hipStream_t st)
+{
+    if (a.n == 0) return;
+    if (a.type == Elem::kF32) return run_quantise<float>(a, st);
+    if (a.type == Elem::kF16) return run_quantise<f16>(a, st);
+    run_quantise<bf16>(a, st);
+}
+
+void launch_linear_i8(const LinearArgs &a, hipStream_t st)
+{
+    if (a.n == 0) return;
+    if (a.type == Elem::kF32) return run_linear_type<float>(a, st);
+    if (a.type == Elem::kF16) return run_linear_type<f16>(a, st);
+    run_linear_type<bf16>(a, st);
+}
+
+} // namespace bht

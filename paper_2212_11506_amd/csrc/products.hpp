@@ -1,0 +1,265 @@
+// The product C = A B^T of row-major operands on the matrix cores, with an
+// epilogue of the caller's: A's rows are points, B's rows are features.
+//
+// All types go through one loop on bytes.  A block makes a tile of kM points x
+// kN rows of B; slices of 128 bytes of every row (32 fp32, 64 fp16 or bf16, 128
+// int8 values) go through a ring in LDS.  A row's eight 16-byte pieces are stored
+// in an order that depends on the row (piece c of row r in place c ^ (r % 8)), so
+// that the lanes of a fragment read, which take the same piece of 16 rows, fall on
+// different banks.  A fragment is 16 bytes a lane: row lane % 16, piece lane / 16
+// of a half slice, which is what one matrix instruction takes of 16 and 8 bits;
+// fp32 takes four, each with one of a piece's values (the sum over K has the same
+// terms in another order).
+//
+// Features are the rows of the instruction's output and points its columns, so a
+// lane holds 4 features of a point a block; B's rows are put into LDS in an order
+// that makes the lane's blocks consecutive features.  Outputs go to memory from
+// registers, as vectors of a lane and whole 64 or 128-byte runs of a point.
+#pragma once
+
+#include <type_traits>
+
+#include "dense.hpp"
+
+namespace bht {
+namespace prod {
+
+typedef int32_t int4v __attribute__((ext_vector_type(4)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef f16 half8 __attribute__((ext_vector_type(8)));
+typedef bf16 bhalf8 __attribute__((ext_vector_type(8)));
+
+typedef int4v Piece; // 16 bytes of a row
+constexpr int kSlice = 128;
+
+template <typename E> struct Ops;
+template <> struct Ops<f16> {
+    typedef float4v Acc;
+    static __device__ inline Acc mul(Piece p, Piece q, Acc c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, p), __builtin_bit_cast(half8, q), c, 0, 0, 0);
+    }
+};
+template <> struct Ops<bf16> {
+    typedef float4v Acc;
+    static __device__ inline Acc mul(Piece p, Piece q, Acc c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bhalf8, p), __builtin_bit_cast(bhalf8, q), c, 0, 0, 0);
+    }
+};
+template <> struct Ops<int8_t> {
+    typedef int4v Acc;
+    static __device__ inline Acc mul(Piece p, Piece q, Acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(p, q, c, 0, 0, 0); }
+};
+template <> struct Ops<float> {
+    typedef float4v Acc;
+    static __device__ inline Acc mul(Piece p, Piece q, Acc c)
+    {
+        const float4v a = __builtin_bit_cast(float4v, p), b = __builtin_bit_cast(float4v, q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+};
+
+template <int M, int N, int Wm, int Wn, int Stages> struct Tile {
+    static constexpr int kM = M, kN = N, kWm = Wm, kWn = Wn, kStages = Stages;
+    static constexpr int kWaves = Wm * Wn, kThreads = kWaves * kWave;
+    static constexpr int kI = M / Wm / 16, kJ = N / Wn / 16; // 16 x 16 blocks of a wave: points, rows of B
+    static constexpr int kGroups = (M + N) / 8;              // groups of 8 rows in a slice, A's first
+    static constexpr int kEach = kGroups / kWaves;           // groups a wave loads
+    static constexpr int kBuffer = (M + N) * kSlice;         // bytes
+    static_assert(kGroups % kWaves == 0 && M % (16 * Wm) == 0 && N % (16 * Wn) == 0, "even shares");
+};
+
+// Operands and grid of a product.  Rows are `bytes` long.
+struct Product {
+    const char *A, *B, *B2;      // kDual: B and B2 give the features' two values
+    int64_t a_stride, b_stride, b2_stride; // bytes between rows
+    int64_t rows, features;
+    int64_t bytes;
+    int32_t down, across;        // tiles
+    int32_t slices, per_split;   // of a row, and of a split (blockIdx.y)
+};
+
+__device__ __align__(16) const char kZeros[16] = {};
+
+// Where a block's tile lies: blocks are dealt to the 8 XCDs in turn and each XCD gets consecutive tiles, four rows of
+// tiles at a time, column by column.
+__device__ inline void place(const Product &a, int32_t &bi, int32_t &bj)
+{
+    const uint32_t tiles = uint32_t(a.down) * uint32_t(a.across);
+    const uint32_t x = blockIdx.x % 8, q = tiles / 8, r = tiles % 8;
+    const uint32_t t = x * q + (x < r ? x : r) + blockIdx.x / 8;
+    const uint32_t group = t / (4u * uint32_t(a.across)), in = t - group * 4u * uint32_t(a.across), top = group * 4;
+    const uint32_t left = uint32_t(a.down) - top, high = left < 4 ? left : 4;
+    bj = int32_t(in / high);
+    bi = int32_t(top + in % high);
+}
+
+// Piece `c` of a row with `left` bytes from p on, of elements E at their own alignment; zeros behind the end
+template <typename E> __device__ inline Piece any_piece(const char *p, int64_t left)
+{
+    constexpr int kV = 16 / int(sizeof(E));
+    Piece v = {0, 0, 0, 0};
+    if (left >= 16) {
+        __builtin_memcpy(&v, p, 16);
+    } else {
+        E x[kV];
+#pragma unroll
+        for (int e = 0; e < kV; ++e) x[e] = e * int(sizeof(E)) < left ? reinterpret_cast<const E *>(p)[e] : E(0);
+        __builtin_memcpy(&v, x, 16);
+    }
+    return v;
+}
+
+// A wave's blocks: acc[i][j] holds rows 16 j .. of the wave's part of B against points 16 i ..  kDual: the first half of
+// the blocks j is B's, the second B2's.  kAny: rows of any alignment and length, through registers; else rows, their
+// strides and lengths are multiples of 16 bytes and loads write LDS directly.
+template <typename E, typename T, bool kDual, bool kAny>
+__device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ])
+{
+    extern __shared__ __align__(16) char s_mem[];
+    constexpr int kTogether = kDual ? T::kJ / 2 : T::kJ; // blocks whose rows are a lane's consecutive features
+    const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id();
+    const int32_t first = int32_t(blockIdx.y) * a.per_split;
+    const int32_t slices = (first + a.per_split < a.slices ? first + a.per_split : a.slices) - first;
+
+    // this lane's piece of each group of eight rows that the wave loads
+    const char *src[T::kEach];
+#pragma unroll
+    for (int e = 0; e < T::kEach; ++e) {
+        const int row = (e * T::kWaves + w) * 8 + lane / 8;
+        if ((e * T::kWaves + w) * 8 < T::kM) {
+            const int64_t at = int64_t(bi) * T::kM + row;
+            src[e] = a.A + (at < a.rows ? at : a.rows - 1) * a.a_stride;
+        } else {
+            const int in = row - T::kM, part = in % (16 * T::kJ), block = part / 16, i = part % 16;
+            const bool second = kDual && block >= kTogether;
+            const int64_t at = int64_t(bj) * (kDual ? T::kN / 2 : T::kN) + in / (16 * T::kJ) * (16 * kTogether)
+                               + i / 4 * (4 * kTogether) + (second ? block - kTogether : block) * 4 + i % 4;
+            const int64_t held = at < a.features ? at : a.features - 1;
+            src[e] = second ? a.B2 + held * a.b2_stride : a.B + held * a.b_stride;
+        }
+        src[e] += int64_t(first) * kSlice + ((lane % 8) ^ (lane / 8)) * 16;
+    }
+    const int wi = w / T::kWn * (T::kI * 16), wj = T::kM + w % T::kWn * (T::kJ * 16);
+    const auto fragment = [&](const char *in, int row, int piece) {
+        return *reinterpret_cast<const Piece *>(in + row * kSlice + ((piece ^ (row & 7)) * 16));
+    };
+    Piece p[2][T::kI], q[2][T::kJ];
+    const auto read = [&](const char *in, int half) {
+        const int piece = half * 4 + lane / 16;
+#pragma unroll
+        for (int j = 0; j < T::kJ; ++j) q[half][j] = fragment(in, wj + 16 * j + lane % 16, piece);
+#pragma unroll
+        for (int i = 0; i < T::kI; ++i) p[half][i] = fragment(in, wi + 16 * i + lane % 16, piece);
+    };
+    const auto multiply = [&](int half) {
+#pragma unroll
+        for (int i = 0; i < T::kI; ++i)
+#pragma unroll
+            for (int j = 0; j < T::kJ; ++j) acc[i][j] = Ops<E>::mul(q[half][j], p[half][i], acc[i][j]);
+    };
+    // bytes of the row from this lane's piece of a slice on
+    const int64_t left0 = a.bytes - int64_t(first) * kSlice - ((lane % 8) ^ (lane / 8)) * 16;
+
+    if constexpr (kAny) {
+        Piece x[T::kEach];
+        const auto load = [&](int slice) {
+#pragma unroll
+            for (int e = 0; e < T::kEach; ++e)
+                x[e] = any_piece<E>(src[e] + int64_t(slice) * kSlice, left0 - int64_t(slice) * kSlice);
+        };
+        load(0);
+        for (int slice = 0; slice < slices; ++slice) {
+            char *to = s_mem + slice % 2 * T::kBuffer;
+#pragma unroll
+            for (int e = 0; e < T::kEach; ++e)
+                *reinterpret_cast<Piece *>(to + (e * T::kWaves + w) * 8 * kSlice + lane * 16) = x[e];
+            __syncthreads(); // the other buffer's readers are past it too: they have written this one
+            if (slice + 1 < slices) load(slice + 1);
+            read(to, 0);
+            read(to, 1);
+            multiply(0);
+            multiply(1);
+        }
+    } else {
+        constexpr int kLoads = T::kEach;
+        const auto fetch = [&](int slice) {
+            // past the end the last slice again, into a buffer that nobody reads: every wait counts alike
+            const int32_t k = slice < slices ? slice : slices - 1;
+            char *to = s_mem + slice % T::kStages * T::kBuffer;
+            const bool zero = left0 - int64_t(k) * kSlice <= 0; // behind the row's end
+#pragma unroll
+            for (int e = 0; e < T::kEach; ++e) {
+                const char *from = zero ? kZeros : src[e] + int64_t(k) * kSlice;
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                                 (__attribute__((address_space(3))) void *)(to + (e * T::kWaves + w) * 8 * kSlice),
+                                                 16, 0, 0);
+            }
+        };
+#pragma unroll
+        for (int e = 0; e < T::kStages; ++e) fetch(e);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((T::kStages - 1) * kLoads) : "memory");
+        read(s_mem, 0);
+        for (int slice = 0; slice < slices; ++slice) {
+            read(s_mem + slice % T::kStages * T::kBuffer, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(0);
+            __builtin_amdgcn_sched_barrier(0);
+            // this wave's loads of the next slice have landed and its reads of this one are done; then everybody's
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((T::kStages - 2) * kLoads) : "memory");
+            fetch(slice + T::kStages);
+            read(s_mem + (slice + 1) % T::kStages * T::kBuffer, 0); // behind the last slice: not used
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); // no load is under way when the block's LDS is given on
+    }
+}
+
+// Points and features of a lane: f(point, feature, i) for each block i of points, with the lane's first feature, of
+// 4 kTogether consecutive ones.
+template <typename T, bool kDual, typename F> __device__ inline void each_run(int32_t bi, int32_t bj, F f)
+{
+    constexpr int kTogether = kDual ? T::kJ / 2 : T::kJ;
+    const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id();
+    const int64_t feature = int64_t(bj) * (kDual ? T::kN / 2 : T::kN) + w % T::kWn * (16 * kTogether) + lane / 16 * (4 * kTogether);
+#pragma unroll
+    for (int i = 0; i < T::kI; ++i) f(int64_t(bi) * T::kM + w / T::kWn * (T::kI * 16) + 16 * i + lane % 16, feature, i);
+}
+
+// N consecutive values to p, of which `count` exist; vec: aligned to 16 bytes, or to N values where those are fewer
+template <typename E, int N> __device__ inline void store_run(E *p, const float (&v)[N], int64_t count, bool vec)
+{
+    constexpr int kV = 16 / int(sizeof(E)) < N ? 16 / int(sizeof(E)) : N;
+    struct alignas(sizeof(E) * kV) Pack {
+        E v[kV];
+    };
+    if (vec && count >= N) {
+#pragma unroll
+        for (int h = 0; h < N / kV; ++h) {
+            Pack x;
+#pragma unroll
+            for (int e = 0; e < kV; ++e) x.v[e] = E(v[h * kV + e]);
+            reinterpret_cast<Pack *>(p)[h] = x;
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if (e < count) p[e] = E(v[e]);
+}
+
+inline bool aligned16(const void *p, int64_t stride_bytes)
+{
+    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride_bytes % 16 == 0;
+}
+
+// A launch takes at most kMostTiles tiles: rows are cut into several launches beyond
+constexpr int64_t kMostTiles = int64_t(1) << 22;
+
+} // namespace prod
+} // namespace bht
