@@ -17,7 +17,6 @@ namespace {
 
 using namespace prod;
 
-typedef Tile<256, 256, 2, 4, 2> TileLarge;
 typedef Tile<128, 128, 2, 2, 2> TileMiddle;
 typedef Tile<64, 64, 2, 2, 3> TileSmall;
 
@@ -60,10 +59,7 @@ template <typename E, typename T, bool kAny>
 __global__ __launch_bounds__(T::kThreads) void gated_kernel(Product p, GatedOut o)
 {
     constexpr int kRun = 2 * T::kJ; // features of a lane
-    int32_t bi, bj;
-    place(p, bi, bj);
-    typename Ops<E>::Acc acc[T::kI][T::kJ] = {};
-    multiply_tile<E, T, true, kAny>(p, bi, bj, acc);
+    each_tile<E, T, true, kAny>(p, [&](int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ]) {
     each_run<T, true>(bi, bj, [&](int64_t point, int64_t feature, int i) {
         if (point >= p.rows) return;
         float a[kRun], b[kRun], h[kRun];
@@ -77,6 +73,7 @@ __global__ __launch_bounds__(T::kThreads) void gated_kernel(Product p, GatedOut 
         store_run(static_cast<E *>(o.h) + point * o.h_stride + feature, h, count, o.vec_h);
         if (o.a) store_run(static_cast<E *>(o.a) + point * o.a_stride + feature, a, count, o.vec_a);
         if (o.b) store_run(static_cast<E *>(o.b) + point * o.b_stride + feature, b, count, o.vec_b);
+    });
     });
 }
 
@@ -110,7 +107,7 @@ template <typename E, typename T, bool kAny> void run_gated(const GatedArgs &a, 
         o.vec_h = aligned16(a.h, a.h_stride * int64_t(sizeof(E)));
         o.vec_a = aligned16(a.a, a.a_stride * int64_t(sizeof(E)));
         o.vec_b = aligned16(a.b, a.b_stride * int64_t(sizeof(E)));
-        gated_kernel<E, T, kAny><<<uint32_t(p.down) * uint32_t(p.across), T::kThreads, lds, st>>>(p, o);
+        gated_kernel<E, T, kAny><<<blocks_of<T>(uint32_t(p.down) * uint32_t(p.across)), T::kThreads, lds, st>>>(p, o);
     }
 }
 
@@ -121,7 +118,7 @@ template <typename E> void run_gated_type(const GatedArgs &a, hipStream_t st)
     const int64_t es = int64_t(sizeof(E));
     const bool any = !aligned16(a.x, a.x_stride * es) || !aligned16(a.gate, a.gate_stride * es) || !aligned16(a.up, a.up_stride * es)
                      || a.d * es % 16 != 0;
-    const bool large = tiles_of(a.n, a.f, 256, 128) >= kCus, middle = tiles_of(a.n, a.f, 128, 64) >= kCus;
+    const bool large = tiles_of(a.n, a.f, 256, 128) >= kCus && a.d * es > kSlice, middle = tiles_of(a.n, a.f, 128, 64) >= kCus;
     if (any) {
         if (large || middle) return run_gated<E, TileMiddle, true>(a, st);
         return run_gated<E, TileSmall, true>(a, st);
@@ -220,10 +217,7 @@ template <typename E, typename T, bool kPart>
 __global__ __launch_bounds__(T::kThreads) void gated_back_kernel(Product p, BackOut o)
 {
     constexpr int kRun = 4 * T::kJ;
-    int32_t bi, bj;
-    place(p, bi, bj);
-    typename Ops<E>::Acc acc[T::kI][T::kJ] = {};
-    multiply_tile<E, T, false, false>(p, bi, bj, acc);
+    each_tile<E, T, false, false>(p, [&](int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ]) {
     each_run<T, false>(bi, bj, [&](int64_t row, int64_t feature, int i) {
         if (row >= p.rows) return;
         float v[kRun];
@@ -237,6 +231,7 @@ __global__ __launch_bounds__(T::kThreads) void gated_back_kernel(Product p, Back
             E *out = static_cast<E *>(second ? o.out2 : o.out);
             if (out) store_run(out + (second ? row - o.first2 : row) * (second ? o.stride2 : o.stride) + feature, v, count, second ? o.vec2 : o.vec);
         }
+    });
     });
 }
 
@@ -269,7 +264,7 @@ void run_back(Product p, const BackOut &o, int splits, hipStream_t st)
         p.down = int32_t((p.rows + T::kM - 1) / T::kM);
         BackOut q = o;
         if (q.out) q.out = static_cast<E *>(o.out) + from * o.stride;
-        const dim3 grid(uint32_t(p.down) * uint32_t(p.across), uint32_t(splits));
+        const dim3 grid(blocks_of<T>(uint32_t(p.down) * uint32_t(p.across)), uint32_t(splits));
         if (splits > 1)
             gated_back_kernel<E, T, true><<<grid, T::kThreads, lds, st>>>(p, q);
         else
@@ -279,7 +274,8 @@ void run_back(Product p, const BackOut &o, int splits, hipStream_t st)
 
 template <typename E> void run_back_tile(const Product &p, const BackOut &o, int splits, hipStream_t st)
 {
-    if (tiles_of(p.rows, p.features, 256, 256) * splits >= kCus) return run_back<E, TileLarge>(p, o, splits, st);
+    const int64_t slices = (p.bytes + kSlice - 1) / kSlice, last = slices - (splits - 1) * ((slices + splits - 1) / splits);
+    if (tiles_of(p.rows, p.features, 256, 256) * splits >= kCus && last >= 2) return run_back<E, TileLarge>(p, o, splits, st);
     if (tiles_of(p.rows, p.features, 128, 128) * splits >= kCus) return run_back<E, TileMiddle>(p, o, splits, st);
     run_back<E, TileSmall>(p, o, splits, st);
 }

@@ -105,7 +105,6 @@ template <typename E> void run_quantise(const QuantiseArgs &a, hipStream_t st)
 }
 
 // ------------------------------------------------------------------ product
-typedef Tile<256, 256, 2, 4, 2> TileLarge;
 typedef Tile<128, 128, 2, 2, 2> TileMiddle;
 typedef Tile<64, 64, 2, 2, 3> TileSmall;
 
@@ -121,10 +120,7 @@ template <typename E, typename T, bool kAny>
 __global__ __launch_bounds__(T::kThreads) void linear8_kernel(Product p, LinearOut o)
 {
     constexpr int kRun = 4 * T::kJ;
-    int32_t bi, bj;
-    place(p, bi, bj);
-    Ops<int8_t>::Acc acc[T::kI][T::kJ] = {};
-    multiply_tile<int8_t, T, false, kAny>(p, bi, bj, acc);
+    each_tile<int8_t, T, false, kAny>(p, [&](int32_t bi, int32_t bj, Ops<int8_t>::Acc (&acc)[T::kI][T::kJ]) {
     float scale[kRun], bias[kRun];
     each_run<T, false>(bi, bj, [&](int64_t point, int64_t feature, int i) {
         if (i == 0) {
@@ -150,6 +146,7 @@ __global__ __launch_bounds__(T::kThreads) void linear8_kernel(Product p, LinearO
 #pragma unroll
         for (int e = 0; e < kRun; ++e) v[e] = float(acc[i][e / 4][e % 4]) * s * scale[e] + bias[e];
         store_run(static_cast<E *>(o.out) + point * o.stride + feature, v, p.features - feature, o.vec);
+    });
     });
 }
 
@@ -177,7 +174,7 @@ template <typename E, typename T, bool kAny> void run_linear(const LinearArgs &a
         o.stride = a.out_stride;
         o.wide_bias = a.bias_type == Elem::kF32;
         o.vec = aligned16(a.out, a.out_stride * int64_t(sizeof(E)));
-        linear8_kernel<E, T, kAny><<<uint32_t(p.down) * uint32_t(p.across), T::kThreads, lds, st>>>(p, o);
+        linear8_kernel<E, T, kAny><<<blocks_of<T>(uint32_t(p.down) * uint32_t(p.across)), T::kThreads, lds, st>>>(p, o);
     }
 }
 
@@ -186,7 +183,7 @@ int64_t tiles_of(int64_t rows, int64_t cols, int side) { return (rows + side - 1
 template <typename E> void run_linear_type(const LinearArgs &a, hipStream_t st)
 {
     const bool any = !aligned16(a.x, a.x_stride) || !aligned16(a.w, a.w_stride) || a.d % 16 != 0;
-    const bool large = tiles_of(a.n, a.f, 256) >= kCus, middle = tiles_of(a.n, a.f, 128) >= kCus;
+    const bool large = tiles_of(a.n, a.f, 256) >= kCus && a.d > kSlice, middle = tiles_of(a.n, a.f, 128) >= kCus;
     if (any) {
         if (large || middle) return run_linear<E, TileMiddle, true>(a, st);
         return run_linear<E, TileSmall, true>(a, st);

@@ -84,13 +84,13 @@ struct Product {
 
 __device__ __align__(16) const char kZeros[16] = {};
 
-// Where a block's tile lies: blocks are dealt to the 8 XCDs in turn and each XCD gets consecutive tiles, four rows of
+// Where the b-th tile lies: blocks are dealt to the 8 XCDs in turn and each XCD gets consecutive tiles, four rows of
 // tiles at a time, column by column.
-__device__ inline void place(const Product &a, int32_t &bi, int32_t &bj)
+__device__ inline void place(const Product &a, uint32_t b, int32_t &bi, int32_t &bj)
 {
     const uint32_t tiles = uint32_t(a.down) * uint32_t(a.across);
-    const uint32_t x = blockIdx.x % 8, q = tiles / 8, r = tiles % 8;
-    const uint32_t t = x * q + (x < r ? x : r) + blockIdx.x / 8;
+    const uint32_t x = b % 8, q = tiles / 8, r = tiles % 8;
+    const uint32_t t = x * q + (x < r ? x : r) + b / 8;
     const uint32_t group = t / (4u * uint32_t(a.across)), in = t - group * 4u * uint32_t(a.across), top = group * 4;
     const uint32_t left = uint32_t(a.down) - top, high = left < 4 ? left : 4;
     bj = int32_t(in / high);
@@ -218,6 +218,182 @@ __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, t
         }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); // no load is under way when the block's LDS is given on
     }
+}
+
+// ------------------------------------------------------------------ large tiles
+// Tiles of 256 x 256 by two groups of four waves, one of each on a SIMD.  A wave's 128 x 64 values are four quarters of
+// 64 x 32; a slice takes four steps, one a quarter, and a step has two parts with a barrier behind each: in the first the wave
+// reads fragments from LDS and starts its share of the loads, in the second it multiplies (16 blocks of 16 x 16, both halves
+// of the slice).  The second group is a part behind the first, so one group's products cover the other's reads.
+//
+// A slice's four regions (halves of A's and B's rows, 16 KB each) are read in steps 3 (of the slice before), 0, 1 and 2, and
+// filled again two steps later, when both groups' reads have been waited for: B0 in step 1, A0 in 2, B1 in 3, A1 in step 0 of the
+// next.  So a load has six steps until it is read; a wave waits for its own loads of a region in the first part of the step
+// before (loads of five steps, two each, may still be under way), and the barrier behind that is everybody's.
+//
+// A CU has one such block, which goes on to its next tile: the loads of the last two slices' steps are the next tile's
+// first, so they are under way while the outputs are formed and stored.  Rows have two slices at least.
+typedef Tile<256, 256, 2, 4, 2> TileLarge;
+constexpr int kRegion = 128 * kSlice;
+
+template <typename E, bool kDual, typename F> __device__ inline void large_tiles(const Product &a, F finish)
+{
+    extern __shared__ __align__(16) char s_mem[];
+    constexpr int kA0 = 0, kA1 = 1, kB0 = 2, kB1 = 3; // regions
+    constexpr int kTogether = kDual ? 2 : 4;
+    const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id(), group = w / 4, column = w % 4;
+    const int32_t first = int32_t(blockIdx.y) * a.per_split;
+    const int32_t slices = (first + a.per_split < a.slices ? first + a.per_split : a.slices) - first;
+    const uint32_t tiles = uint32_t(a.down) * uint32_t(a.across);
+    const int own = ((lane % 8) ^ (lane / 8)) * 16;
+    const int64_t left = a.bytes - int64_t(first) * kSlice - own; // of the row, from this lane's first piece on
+
+    // Regions' rows: A's half h has the h-th 64 of each group's 128 points, B's the blocks 2 h and 2 h + 1 of each column of
+    // waves.  This lane's pieces of the two groups of eight rows that the wave loads of each region.
+    const char *src[4][2];
+    const auto point = [&](int r, int32_t bi, int32_t bj) {
+        const int h = r & 1;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int row = (e * 8 + w) * 8 + lane / 8; // of the region
+            if (r < kB0) {
+                const int64_t at = int64_t(bi) * 256 + row / 64 * 128 + h * 64 + row % 64;
+                src[r][e] = a.A + (at < a.rows ? at : a.rows - 1) * a.a_stride;
+            } else {
+                const int block = 2 * h + row % 32 / 16, i = row % 16;
+                const bool second = kDual && h == 1;
+                const int64_t at = int64_t(bj) * (64 * kTogether) + row / 32 * (16 * kTogether) + i / 4 * (4 * kTogether)
+                                   + (second ? block - 2 : block) * 4 + i % 4;
+                const int64_t held = at < a.features ? at : a.features - 1;
+                src[r][e] = second ? a.B2 + held * a.b2_stride : a.B + held * a.b_stride;
+            }
+            src[r][e] += int64_t(first) * kSlice + own;
+        }
+    };
+    // region r of a slice into the buffers of its parity
+    const auto fetch = [&](int r, int32_t slice, int parity) {
+        char *to = s_mem + parity * (4 * kRegion) + r * kRegion;
+        const bool zero = left - int64_t(slice) * kSlice <= 0; // behind the row's end
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const char *from = zero ? kZeros : src[r][e] + int64_t(slice) * kSlice;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                             (__attribute__((address_space(3))) void *)(to + (e * 8 + w) * 8 * kSlice), 16, 0, 0);
+        }
+    };
+    const int at0 = lane % 16 * kSlice + ((lane / 16) ^ (lane & 7)) * 16, at1 = at0 ^ 64; // the two halves of a slice
+    Piece p[2][4], q[2][2][2]; // A's half that is under way; both of B's
+    const auto read_a = [&](int h, int parity) {
+        const char *in = s_mem + parity * (4 * kRegion) + h * kRegion + group * 64 * kSlice;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[0][i] = *reinterpret_cast<const Piece *>(in + i * 16 * kSlice + at0);
+            p[1][i] = *reinterpret_cast<const Piece *>(in + i * 16 * kSlice + at1);
+        }
+    };
+    const auto read_b = [&](int h, int parity) {
+        const char *in = s_mem + parity * (4 * kRegion) + (kB0 + h) * kRegion + column * 32 * kSlice;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            q[h][0][j] = *reinterpret_cast<const Piece *>(in + j * 16 * kSlice + at0);
+            q[h][1][j] = *reinterpret_cast<const Piece *>(in + j * 16 * kSlice + at1);
+        }
+    };
+    typename Ops<E>::Acc acc[8][4];
+    // the barrier between a step's parts, with the wait for the loads that the next step reads; and the part that multiplies
+    const auto multiply = [&](int ha, int hb) {
+        asm volatile("s_waitcnt vmcnt(10)\n\ts_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    acc[4 * ha + i][2 * hb + j] = Ops<E>::mul(q[hb][half][j], p[half][i], acc[4 * ha + i][2 * hb + j]);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    uint32_t t = blockIdx.x;
+    int32_t bi, bj;
+    place(a, t, bi, bj);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) point(r, bi, bj);
+    fetch(kB0, 0, 0);
+    fetch(kA0, 0, 0);
+    fetch(kB1, 0, 0);
+    fetch(kA1, 0, 0);
+    fetch(kB0, 1, 1);
+    fetch(kA0, 1, 1);
+    fetch(kB1, 1, 1);
+    asm volatile("s_waitcnt vmcnt(10)\n\ts_barrier" ::: "memory");
+    int parity = 0;
+    for (;;) {
+        const uint32_t next = t + gridDim.x;
+        const bool more = next < tiles; // without, the last loads are this tile's first again, which nobody reads
+        int32_t ni = bi, nj = bj;
+        if (more) place(a, next, ni, nj);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = {};
+        read_b(0, parity);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // the first group fills this region again in its step 1
+        if (group == 1) asm volatile("s_barrier" ::: "memory"); // a part behind
+        __builtin_amdgcn_sched_barrier(0);
+        for (int32_t slice = 0; slice < slices; ++slice, parity ^= 1) {
+            const int32_t one = slice + 1 < slices ? slice + 1 : 0, two = slice + 2 < slices ? slice + 2 : slice + 2 - slices;
+            if (slice == slices - 1) point(kA1, ni, nj);
+            read_a(0, parity);
+            fetch(kA1, one, parity ^ 1);
+            multiply(0, 0);
+            if (slice == slices - 2) {
+                point(kB0, ni, nj);
+                point(kA0, ni, nj);
+                point(kB1, ni, nj);
+            }
+            read_b(1, parity);
+            fetch(kB0, two, parity);
+            multiply(0, 1);
+            read_a(1, parity);
+            fetch(kA0, two, parity);
+            multiply(1, 0);
+            read_b(0, parity ^ 1); // behind the tile's last slice: the next one's, read again
+            fetch(kB1, two, parity);
+            multiply(1, 1);
+        }
+        if (group == 0) asm volatile("s_barrier" ::: "memory"); // the groups meet, so that both form their outputs at once
+        __builtin_amdgcn_sched_barrier(0);
+        finish(bi, bj, acc);
+        if (!more) break;
+        t = next;
+        bi = ni;
+        bj = nj;
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); // no load is under way when the block's LDS is given on
+}
+
+// The tiles of a launch: finish(bi, bj, acc) takes each one's sums
+template <typename E, typename T, bool kDual, bool kAny, typename F> __device__ inline void each_tile(const Product &a, F finish)
+{
+    if constexpr (std::is_same<T, TileLarge>::value) {
+        large_tiles<E, kDual>(a, finish);
+    } else {
+        int32_t bi, bj;
+        place(a, blockIdx.x, bi, bj);
+        typename Ops<E>::Acc acc[T::kI][T::kJ] = {};
+        multiply_tile<E, T, kDual, kAny>(a, bi, bj, acc);
+        finish(bi, bj, acc);
+    }
+}
+template <typename T> inline uint32_t blocks_of(uint32_t tiles)
+{
+    return std::is_same<T, TileLarge>::value && tiles > uint32_t(kCus) ? uint32_t(kCus) : tiles;
 }
 
 // Points and features of a lane: f(point, feature, i) for each block i of points, with the lane's first feature, of
