@@ -29,10 +29,32 @@ template <typename E> __device__ inline float sigmoid(float a)
     else
         return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a * -1.44269504f));
 }
+// Half of erfc(|a| / sqrt(2)) = exp(-a^2 / 2) t P(t) with t = 1 / (1 + c |a|): P is fitted to the scaled function over all
+// |a| by least squares, reweighted towards the largest relative error: of degree 8 for fp32 (1.3e-7; with its own roundings
+// 4.6e-7), of degree 5 for outputs of 16 bits (2.8e-5, a seventeenth of fp16's rounding).  No difference of near values, so a far
+// below zero keeps its digits.  The exponential is a square, so that values near the smallest fp32 and bf16 numbers do not
+// vanish in the instruction.
+template <typename E> __device__ inline float tail(float a, float &root)
+{
+    constexpr bool kWide = sizeof(E) == 4;
+    constexpr int kDegree = kWide ? 8 : 5;
+    constexpr float kWideP[9] = {0.11283793300390244f, 0.11283478140830994f, 0.10392161458730698f, 0.08426911383867264f, 0.07072257250547409f,
+                                 -0.0028178293723613024f, 0.08455897867679596f, -0.09146063029766083f, 0.0251335259526968f};
+    constexpr float kNarrowP[9] = {0.12976588308811188f, 0.12951643764972687f, 0.12026726454496384f, 0.06271062791347504f, 0.12091848254203796f, -0.06318359076976776f};
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(a), kWide ? 0.28284273f : 0.32526913f, 1.0f));
+    float p = kWide ? kWideP[8] : kNarrowP[5];
+#pragma unroll
+    for (int k = kDegree - 1; k >= 0; --k) p = fmaf(p, t, kWide ? kWideP[k] : kNarrowP[k]);
+    root = __builtin_amdgcn_exp2f(a * (a * -0.360673760f));
+    return p * t * root * root;
+}
+// (value) a Phi(a), which is max(a, 0) - |a| tail(a), and (slope) Phi(a) + a phi(a); or the sigmoid's
 template <typename E> __device__ inline float activate(float a, Act act)
 {
     if (act == Act::kSilu) return a * sigmoid<E>(a);
-    return 0.5f * a * erfcf(a * -0.707106781f); // no difference of near values for a far below zero
+    float root;
+    const float h = tail<E>(a, root), above = a < 0.0f ? 0.0f : a; // NaN stays
+    return fmaf(-fabsf(a), h, above);
 }
 template <typename E> __device__ inline void activate_both(float a, Act act, float &value, float &slope)
 {
@@ -41,9 +63,10 @@ template <typename E> __device__ inline void activate_both(float a, Act act, flo
         value = a * s;
         slope = s * (1.0f + a * (1.0f - s));
     } else {
-        const float phi = 0.5f * erfcf(a * -0.707106781f);
-        value = a * phi;
-        slope = phi + a * (0.398942280f * __builtin_amdgcn_exp2f(a * a * -0.721347520f));
+        float root;
+        const float h = tail<E>(a, root), phi = a < 0.0f ? h : 1.0f - h;
+        value = fmaf(-fabsf(a), h, a < 0.0f ? 0.0f : a);
+        slope = phi + a * (0.398942280f * root * root);
     }
 }
 
@@ -58,37 +81,61 @@ struct GatedOut {
 template <typename E, typename T, bool kAny>
 __global__ __launch_bounds__(T::kThreads) void gated_kernel(Product p, GatedOut o)
 {
-    constexpr int kRun = 2 * T::kJ; // features of a lane
+    constexpr int kRun = T::kJ / 2; // features of a lane
     each_tile<E, T, true, kAny>(p, [&](int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ]) {
-    each_run<T, true>(bi, bj, [&](int64_t point, int64_t feature, int i) {
-        if (point >= p.rows) return;
-        float a[kRun], b[kRun], h[kRun];
+        each_run<T, true>(bi, bj, [&](int64_t point, int64_t feature, int i, int r) {
+            if (point >= p.rows) return;
+            float a[kRun], b[kRun], h[kRun];
 #pragma unroll
-        for (int e = 0; e < kRun; ++e) {
-            a[e] = acc[i][e / 4][e % 4];
-            b[e] = acc[i][T::kJ / 2 + e / 4][e % 4];
-            h[e] = activate<E>(a[e], o.act) * b[e];
-        }
-        const int64_t count = p.features - feature;
-        store_run(static_cast<E *>(o.h) + point * o.h_stride + feature, h, count, o.vec_h);
-        if (o.a) store_run(static_cast<E *>(o.a) + point * o.a_stride + feature, a, count, o.vec_a);
-        if (o.b) store_run(static_cast<E *>(o.b) + point * o.b_stride + feature, b, count, o.vec_b);
+            for (int e = 0; e < kRun; ++e) {
+                a[e] = acc[i][e][r];
+                b[e] = acc[i][kRun + e][r];
+                h[e] = activate<E>(a[e], o.act) * b[e];
+            }
+            const int64_t count = p.features - feature;
+            store_run(static_cast<E *>(o.h) + point * o.h_stride + feature, h, count, o.vec_h);
+            if (o.a) store_run(static_cast<E *>(o.a) + point * o.a_stride + feature, a, count, o.vec_a);
+            if (o.b) store_run(static_cast<E *>(o.b) + point * o.b_stride + feature, b, count, o.vec_b);
+        });
     });
-    });
+}
+
+template <typename E, int kRun> GatedOut gated_out(const GatedArgs &a)
+{
+    GatedOut o = {};
+    o.h = a.h;
+    o.a = a.a;
+    o.b = a.b;
+    o.h_stride = a.h_stride;
+    o.a_stride = a.a_stride;
+    o.b_stride = a.b_stride;
+    o.act = a.act;
+    o.vec_h = runs_aligned<E, kRun>(a.h, a.h_stride);
+    o.vec_a = runs_aligned<E, kRun>(a.a, a.a_stride);
+    o.vec_b = runs_aligned<E, kRun>(a.b, a.b_stride);
+    return o;
+}
+
+Product gated_product(const GatedArgs &a, int64_t es)
+{
+    Product p = {};
+    p.A = static_cast<const char *>(a.x);
+    p.B = static_cast<const char *>(a.gate);
+    p.B2 = static_cast<const char *>(a.up);
+    p.a_stride = a.x_stride * es;
+    p.b_stride = a.gate_stride * es;
+    p.b2_stride = a.up_stride * es;
+    p.rows = a.n;
+    p.features = a.f;
+    p.bytes = a.d * es;
+    p.slices = p.per_split = int32_t((p.bytes + kSlice - 1) / kSlice);
+    return p;
 }
 
 template <typename E, typename T, bool kAny> void run_gated(const GatedArgs &a, hipStream_t st)
 {
     constexpr int64_t kF = T::kN / 2;
-    Product p = {};
-    p.B = static_cast<const char *>(a.gate);
-    p.B2 = static_cast<const char *>(a.up);
-    p.a_stride = a.x_stride * int64_t(sizeof(E));
-    p.b_stride = a.gate_stride * int64_t(sizeof(E));
-    p.b2_stride = a.up_stride * int64_t(sizeof(E));
-    p.features = a.f;
-    p.bytes = a.d * int64_t(sizeof(E));
-    p.slices = p.per_split = int32_t((p.bytes + kSlice - 1) / kSlice);
+    Product p = gated_product(a, int64_t(sizeof(E)));
     p.across = int32_t((a.f + kF - 1) / kF);
     const size_t lds = size_t(kAny && p.slices == 1 ? 1 : T::kStages) * T::kBuffer;
     const int64_t most = kMostTiles / p.across > 0 ? kMostTiles / p.across * T::kM : T::kM; // points of a launch
@@ -96,26 +143,208 @@ template <typename E, typename T, bool kAny> void run_gated(const GatedArgs &a, 
         p.A = static_cast<const char *>(a.x) + from * p.a_stride;
         p.rows = a.n - from < most ? a.n - from : most;
         p.down = int32_t((p.rows + T::kM - 1) / T::kM);
-        GatedOut o = {};
+        GatedOut o = gated_out<E, T::kJ / 2>(a);
         o.h = static_cast<E *>(a.h) + from * a.h_stride;
         o.a = a.a ? static_cast<E *>(a.a) + from * a.a_stride : nullptr;
         o.b = a.b ? static_cast<E *>(a.b) + from * a.b_stride : nullptr;
-        o.h_stride = a.h_stride;
-        o.a_stride = a.a_stride;
-        o.b_stride = a.b_stride;
-        o.act = a.act;
-        o.vec_h = aligned16(a.h, a.h_stride * int64_t(sizeof(E)));
-        o.vec_a = aligned16(a.a, a.a_stride * int64_t(sizeof(E)));
-        o.vec_b = aligned16(a.b, a.b_stride * int64_t(sizeof(E)));
         gated_kernel<E, T, kAny><<<blocks_of<T>(uint32_t(p.down) * uint32_t(p.across)), T::kThreads, lds, st>>>(p, o);
+    }
+}
+
+// Short rows (16 to kHalves 64 bytes): the weights of 32 features stay in a wave's registers, and a block's waves have the
+// same points, kShortPoints at a time: their rows come through LDS, read as pieces that lie side by side in memory, at any
+// alignment; the next ones are under way meanwhile.  Outputs go through LDS too, and from there as whole rows of the block's
+// features.  A row's last piece is its last 16 bytes, of which only those count that the piece before does not have: the others
+// are masked out, in points and weights alike.
+constexpr int kShortWaves = 8;   // of a block at most
+constexpr int kShortPoints = 32;
+constexpr int kShortBlocks = 4 * 2 * kCus; // some rounds of two blocks a CU
+constexpr int kShortPitch(int kHalves) { return kHalves * 64 + 16; } // bytes of a row in LDS: 8 rows on different banks
+
+struct ShortShape {
+    int64_t per_block;   // points, a multiple of kShortPoints
+    int32_t features;    // of a block
+    int32_t pitch;       // bytes of a row of outputs in LDS: a row's own where the outputs are without gaps
+    int32_t vectors;     // of a row; 0: outputs are not aligned for them, values one by one
+    bool flat;           // a tile of outputs is one run of memory
+};
+
+// The outputs of `rows` points from LDS
+template <typename E, typename V>
+__device__ inline void store_rows(const char *tile, const ShortShape &z, E *out, int64_t stride, int rows, int each)
+{
+    int r = int(threadIdx.x) / each, c = int(threadIdx.x) - r * each;
+    const int down = int(blockDim.x) / each, right = int(blockDim.x) - down * each;
+    while (r < rows) {
+        *reinterpret_cast<V *>(reinterpret_cast<char *>(out + r * stride) + c * int(sizeof(V))) = *reinterpret_cast<const V *>(tile + r * z.pitch + c * int(sizeof(V)));
+        r += down;
+        c += right;
+        if (c >= each) {
+            c -= each;
+            ++r;
+        }
+    }
+}
+template <typename E> __device__ inline void store_tile(const char *tile, const ShortShape &z, E *out, int64_t stride, int rows, int features)
+{
+    if (z.flat) { // rows of 16 bytes
+        char *to = reinterpret_cast<char *>(out);
+        const int bytes = rows * z.pitch;
+        for (int t = int(threadIdx.x) * 16; t < bytes; t += int(blockDim.x) * 16) *reinterpret_cast<Piece *>(to + t) = *reinterpret_cast<const Piece *>(tile + t);
+    } else if (z.vectors > 0 && features * int(sizeof(E)) % 16 == 0) {
+        store_rows<E, Piece>(tile, z, out, stride, rows, features * int(sizeof(E)) / 16);
+    } else {
+        store_rows<E, E>(tile, z, out, stride, rows, features);
+    }
+}
+
+template <typename E, int kHalves, bool kGelu, bool kKeep>
+__global__ __launch_bounds__(kShortWaves *kWave) void gated_short_kernel(Product p, GatedOut o, ShortShape z)
+{
+    extern __shared__ __align__(16) char s_mem[];
+    constexpr int kPitch = kShortPitch(kHalves), kGroups = kShortPoints / 16, kRowPieces = kHalves * 4;
+    constexpr int kPieces = kShortPoints * kRowPieces, kOuts = kKeep ? 3 : 1;
+    constexpr int kHeld = (kPieces + kWave - 1) / kWave; // pieces of a thread at most
+    char *s_out = s_mem + 2 * kShortPoints * kPitch;
+    const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id(), threads = int(blockDim.x);
+    const int64_t block = int64_t(blockIdx.y) * z.features;
+    const int features = int(p.features - block < z.features ? p.features - block : z.features);
+    const int mine = w * 32 + lane % 16 * 2; // of the block's features
+    const int bytes = int(p.bytes);
+    // the place of piece c of a row, and what of it counts
+    const auto place_of = [&](int c, Piece &mask) {
+        const int begin = c * 16, at = begin < bytes - 16 ? begin : bytes - 16, skip = begin - at;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int part = skip - 4 * e;
+            mask[e] = part <= 0 ? -1 : part >= 4 ? 0 : int(0xffffffffu << (8 * part));
+        }
+        return at;
+    };
+    Piece weights[4][kHalves]; // two blocks of gate's features, two of up's
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) {
+        Piece mask;
+        const int at = place_of(h * 4 + lane / 16, mask);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t f = block + mine + j % 2, held = f < p.features ? f : p.features - 1;
+            weights[j][h] = inner_piece((j < 2 ? p.B + held * p.b_stride : p.B2 + held * p.b2_stride) + at) & mask;
+        }
+    }
+    const int64_t from = int64_t(blockIdx.x) * z.per_block, to = from + z.per_block < p.rows ? from + z.per_block : p.rows;
+    // a thread loads the same piece of every row that it loads
+    Piece mask, held[kHeld];
+    const int column = int(threadIdx.x) % kRowPieces, row0 = int(threadIdx.x) / kRowPieces, down = threads / kRowPieces;
+    const char *base = p.A + place_of(column, mask);
+    const auto take = [&](int64_t first) {
+#pragma unroll
+        for (int q = 0; q < kHeld; ++q) {
+            if (q * down >= kShortPoints) break;
+            const int64_t point = first + row0 + q * down;
+            held[q] = inner_piece(base + (point < p.rows ? point : p.rows - 1) * p.a_stride);
+        }
+    };
+    const auto put = [&](int parity) {
+#pragma unroll
+        for (int q = 0; q < kHeld; ++q) {
+            if (q * down >= kShortPoints) break;
+            const int row = row0 + q * down;
+            if (row < kShortPoints) *reinterpret_cast<Piece *>(s_mem + (parity * kShortPoints + row) * kPitch + column * 16) = held[q] & mask;
+        }
+    };
+    take(from);
+    put(0);
+    __syncthreads();
+    int parity = 0;
+    for (int64_t first = from; first < to; first += kShortPoints, parity ^= 1) {
+        take(first + kShortPoints < to ? first + kShortPoints : first);
+        char *tile = s_out + parity * (kOuts * kShortPoints) * z.pitch;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            typename Ops<E>::Acc acc[4] = {};
+            const char *in = s_mem + (parity * kShortPoints + g * 16 + lane % 16) * kPitch + lane / 16 * 16;
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                const Piece x = *reinterpret_cast<const Piece *>(in + h * 64);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[j] = Ops<E>::mul(x, weights[j][h], acc[j]);
+            }
+            struct Two {
+                E v[2];
+            };
+            const bool there = mine < z.features, both = mine + 1 < z.features; // a row in LDS has no room for others
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                constexpr Act kAct = kGelu ? Act::kGelu : Act::kSilu;
+                Two t[3];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float a = acc[e][r], b = acc[2 + e][r];
+                    t[0].v[e] = E(activate<E>(a, kAct) * b);
+                    t[1].v[e] = E(a);
+                    t[2].v[e] = E(b);
+                }
+                char *at = tile + (g * 16 + lane / 16 * 4 + r) * z.pitch + mine * int(sizeof(E));
+#pragma unroll
+                for (int k = 0; k < kOuts; ++k) {
+                    E *q = reinterpret_cast<E *>(at + k * kShortPoints * z.pitch);
+                    if (z.features % 2 == 0) { // every row starts at an even value
+                        typedef typename std::conditional<sizeof(E) == 2, uint32_t, uint64_t>::type Bits;
+                        if (there) *reinterpret_cast<Bits *>(q) = __builtin_bit_cast(Bits, t[k]);
+                    } else {
+                        if (there) q[0] = t[k].v[0];
+                        if (both) q[1] = t[k].v[1];
+                    }
+                }
+            }
+        }
+        // the next points' loads are waited for here, and with them the stores before them, but none behind
+        put(parity ^ 1);
+        __syncthreads(); // tiles and rows alternate: one barrier for all
+        const int rows = int(to - first < kShortPoints ? to - first : kShortPoints);
+        store_tile(tile, z, static_cast<E *>(o.h) + first * o.h_stride + block, o.h_stride, rows, features);
+        if constexpr (kKeep) {
+            tile += kShortPoints * z.pitch;
+            store_tile(tile, z, static_cast<E *>(o.a) + first * o.a_stride + block, o.a_stride, rows, features);
+            tile += kShortPoints * z.pitch;
+            store_tile(tile, z, static_cast<E *>(o.b) + first * o.b_stride + block, o.b_stride, rows, features);
+        }
     }
 }
 
 int64_t tiles_of(int64_t rows, int64_t cols, int m, int n) { return (rows + m - 1) / m * ((cols + n - 1) / n); }
 
+template <typename E, int kHalves> void run_gated_short(const GatedArgs &a, hipStream_t st)
+{
+    constexpr int kEs = int(sizeof(E)), kV = 16 / kEs;
+    const Product p = gated_product(a, kEs);
+    const GatedOut o = gated_out<E, kV>(a);
+    const bool keep = a.a != nullptr;
+    const int64_t all = (a.f + 31) / 32, groups = (all + kShortWaves - 1) / kShortWaves, waves = (all + groups - 1) / groups;
+    ShortShape z = {};
+    z.features = int32_t(a.f < waves * 32 ? a.f : waves * 32);
+    const bool vec = o.vec_h && (!keep || (o.vec_a && o.vec_b));
+    z.vectors = vec ? z.features / kV : 0;
+    z.flat = vec && a.f == z.features && a.h_stride == a.f && (!keep || (a.a_stride == a.f && a.b_stride == a.f));
+    z.pitch = z.flat ? z.features * kEs : (z.features * kEs + 15) / 16 * 16 + 16;
+    const int64_t want = (kShortBlocks + groups - 1) / groups, most = (a.n + want - 1) / want;
+    z.per_block = (most + kShortPoints - 1) / kShortPoints * kShortPoints;
+    const dim3 grid(uint32_t((a.n + z.per_block - 1) / z.per_block), uint32_t(groups));
+    const uint32_t threads = uint32_t(waves) * kWave;
+    const size_t lds = 2 * kShortPoints * (kShortPitch(kHalves) + size_t(keep ? 3 : 1) * size_t(z.pitch));
+    const auto launch = [&](auto kernel) { kernel<<<grid, threads, lds, st>>>(p, o, z); };
+    if (a.act == Act::kGelu)
+        keep ? launch(gated_short_kernel<E, kHalves, true, true>) : launch(gated_short_kernel<E, kHalves, true, false>);
+    else
+        keep ? launch(gated_short_kernel<E, kHalves, false, true>) : launch(gated_short_kernel<E, kHalves, false, false>);
+}
+
 template <typename E> void run_gated_type(const GatedArgs &a, hipStream_t st)
 {
     const int64_t es = int64_t(sizeof(E));
+    if (a.d * es >= 16 && a.d * es <= 128 && (a.a == nullptr) == (a.b == nullptr))
+        return a.d * es <= 64 ? run_gated_short<E, 1>(a, st) : run_gated_short<E, 2>(a, st);
     const bool any = !aligned16(a.x, a.x_stride * es) || !aligned16(a.gate, a.gate_stride * es) || !aligned16(a.up, a.up_stride * es)
                      || a.d * es % 16 != 0;
     const bool large = tiles_of(a.n, a.f, 256, 128) >= kCus && a.d * es > kSlice, middle = tiles_of(a.n, a.f, 128, 64) >= kCus;
@@ -216,22 +445,22 @@ struct BackOut {
 template <typename E, typename T, bool kPart>
 __global__ __launch_bounds__(T::kThreads) void gated_back_kernel(Product p, BackOut o)
 {
-    constexpr int kRun = 4 * T::kJ;
+    constexpr int kRun = T::kJ;
     each_tile<E, T, false, false>(p, [&](int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ]) {
-    each_run<T, false>(bi, bj, [&](int64_t row, int64_t feature, int i) {
-        if (row >= p.rows) return;
-        float v[kRun];
+        each_run<T, false>(bi, bj, [&](int64_t row, int64_t feature, int i, int r) {
+            if (row >= p.rows) return;
+            float v[kRun];
 #pragma unroll
-        for (int e = 0; e < kRun; ++e) v[e] = acc[i][e / 4][e % 4];
-        const int64_t count = p.features - feature;
-        if constexpr (kPart) {
-            store_run(o.part + (int64_t(blockIdx.y) * p.rows + row) * p.features + feature, v, count, o.vec);
-        } else {
-            const bool second = row >= o.first2;
-            E *out = static_cast<E *>(second ? o.out2 : o.out);
-            if (out) store_run(out + (second ? row - o.first2 : row) * (second ? o.stride2 : o.stride) + feature, v, count, second ? o.vec2 : o.vec);
-        }
-    });
+            for (int e = 0; e < kRun; ++e) v[e] = acc[i][e][r];
+            const int64_t count = p.features - feature;
+            if constexpr (kPart) {
+                store_run(o.part + (int64_t(blockIdx.y) * p.rows + row) * p.features + feature, v, count, o.vec);
+            } else {
+                const bool second = row >= o.first2;
+                E *out = static_cast<E *>(second ? o.out2 : o.out);
+                if (out) store_run(out + (second ? row - o.first2 : row) * (second ? o.stride2 : o.stride) + feature, v, count, second ? o.vec2 : o.vec);
+            }
+        });
     });
 }
 

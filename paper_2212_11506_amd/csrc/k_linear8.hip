@@ -16,13 +16,13 @@ using namespace prod;
 // ------------------------------------------------------------------ quantisation
 constexpr int kRowValues = 16; // of a thread at a time
 
-// 16 values from p, of which `left` exist, zeros behind
-template <typename E> __device__ inline void load_values(const E *p, int64_t left, float (&v)[kRowValues])
+// 16 values of a row of d from `at` on, zeros behind its end
+template <typename E> __device__ inline void load_values(const E *row, int64_t at, int64_t d, float (&v)[kRowValues])
 {
     constexpr int kV = 16 / int(sizeof(E));
 #pragma unroll
     for (int h = 0; h < kRowValues / kV; ++h) {
-        const Piece x = any_piece<E>(reinterpret_cast<const char *>(p + h * kV), (left - h * kV) * int64_t(sizeof(E)));
+        const Piece x = any_piece<E>(reinterpret_cast<const char *>(row), (at + h * kV) * int64_t(sizeof(E)), d * int64_t(sizeof(E)));
         E e[kV];
         __builtin_memcpy(e, &x, 16);
 #pragma unroll
@@ -52,7 +52,7 @@ template <typename E, int kThreads> __global__ __launch_bounds__(kThreads) void 
         int8_t *q = a.q + row * a.q_stride;
         float v[kRowValues], top = 0.0f;
         const auto take = [&](int64_t at) {
-            load_values(x + at, a.d - at, v);
+            load_values(x, at, a.d, v);
 #pragma unroll
             for (int e = 0; e < kRowValues; ++e) {
                 const float m = fabsf(v[e]);
@@ -74,7 +74,7 @@ template <typename E, int kThreads> __global__ __launch_bounds__(kThreads) void 
         if (threadIdx.x == 0) a.scale[row] = scale;
         const bool aligned = (reinterpret_cast<uintptr_t>(q) & 15) == 0;
         for (int64_t at = int64_t(threadIdx.x) * kRowValues; at < a.d; at += kThreads * kRowValues) {
-            if (a.d > kThreads * kRowValues) load_values(x + at, a.d - at, v);
+            if (a.d > kThreads * kRowValues) load_values(x, at, a.d, v);
             struct alignas(16) {
                 int8_t v[kRowValues];
             } out;
@@ -119,34 +119,34 @@ struct LinearOut {
 template <typename E, typename T, bool kAny>
 __global__ __launch_bounds__(T::kThreads) void linear8_kernel(Product p, LinearOut o)
 {
-    constexpr int kRun = 4 * T::kJ;
+    constexpr int kRun = T::kJ;
     each_tile<int8_t, T, false, kAny>(p, [&](int32_t bi, int32_t bj, Ops<int8_t>::Acc (&acc)[T::kI][T::kJ]) {
-    float scale[kRun], bias[kRun];
-    each_run<T, false>(bi, bj, [&](int64_t point, int64_t feature, int i) {
-        if (i == 0) {
+        float scale[kRun], bias[kRun];
+        each_run<T, false>(bi, bj, [&](int64_t point, int64_t feature, int i, int r) {
+            if (i == 0 && r == 0) {
 #pragma unroll
-            for (int e = 0; e < kRun; ++e) {
-                const int64_t at = feature + e < p.features ? feature + e : p.features - 1;
-                scale[e] = o.w_scale[at];
-                bias[e] = 0.0f;
+                for (int e = 0; e < kRun; ++e) {
+                    const int64_t at = feature + e < p.features ? feature + e : p.features - 1;
+                    scale[e] = o.w_scale[at];
+                    bias[e] = 0.0f;
+                }
             }
-        }
-        if (i == 0 && o.bias) {
-            if (o.wide_bias) {
+            if (i == 0 && r == 0 && o.bias) {
+                if (o.wide_bias) {
 #pragma unroll
-                for (int e = 0; e < kRun; ++e) bias[e] = static_cast<const float *>(o.bias)[feature + e < p.features ? feature + e : p.features - 1];
-            } else {
+                    for (int e = 0; e < kRun; ++e) bias[e] = static_cast<const float *>(o.bias)[feature + e < p.features ? feature + e : p.features - 1];
+                } else {
 #pragma unroll
-                for (int e = 0; e < kRun; ++e) bias[e] = float(static_cast<const E *>(o.bias)[feature + e < p.features ? feature + e : p.features - 1]);
+                    for (int e = 0; e < kRun; ++e) bias[e] = float(static_cast<const E *>(o.bias)[feature + e < p.features ? feature + e : p.features - 1]);
+                }
             }
-        }
-        if (point >= p.rows) return;
-        const float s = o.x_scale[point];
-        float v[kRun];
+            if (point >= p.rows) return;
+            const float s = o.x_scale[point];
+            float v[kRun];
 #pragma unroll
-        for (int e = 0; e < kRun; ++e) v[e] = float(acc[i][e / 4][e % 4]) * s * scale[e] + bias[e];
-        store_run(static_cast<E *>(o.out) + point * o.stride + feature, v, p.features - feature, o.vec);
-    });
+            for (int e = 0; e < kRun; ++e) v[e] = float(acc[i][e][r]) * s * scale[e] + bias[e];
+            store_run(static_cast<E *>(o.out) + point * o.stride + feature, v, p.features - feature, o.vec);
+        });
     });
 }
 
@@ -173,7 +173,7 @@ template <typename E, typename T, bool kAny> void run_linear(const LinearArgs &a
         o.out = static_cast<E *>(a.out) + from * a.out_stride;
         o.stride = a.out_stride;
         o.wide_bias = a.bias_type == Elem::kF32;
-        o.vec = aligned16(a.out, a.out_stride * int64_t(sizeof(E)));
+        o.vec = runs_aligned<E, T::kJ>(a.out, a.out_stride);
         linear8_kernel<E, T, kAny><<<blocks_of<T>(uint32_t(p.down) * uint32_t(p.across)), T::kThreads, lds, st>>>(p, o);
     }
 }

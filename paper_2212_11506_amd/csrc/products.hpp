@@ -11,10 +11,13 @@
 // fp32 takes four, each with one of a piece's values (the sum over K has the same
 // terms in another order).
 //
-// Features are the rows of the instruction's output and points its columns, so a
-// lane holds 4 features of a point a block; B's rows are put into LDS in an order
+// Features are the columns of the instruction's output and points its rows, so a
+// lane holds 4 points of a feature a block; B's rows are put into LDS in an order
 // that makes the lane's blocks consecutive features.  Outputs go to memory from
-// registers, as vectors of a lane and whole 64 or 128-byte runs of a point.
+// registers: a lane stores its features of a point as one vector, and 16 lanes
+// next to each other a run of the point's (64 bytes or more of tiles of 128 on).
+// Lanes side by side have to be neighbours in memory for that: with points along
+// the lanes, each lane's 16 bytes were a request of its own.
 #pragma once
 
 #include <type_traits>
@@ -97,19 +100,40 @@ __device__ inline void place(const Product &a, uint32_t b, int32_t &bi, int32_t 
     bi = int32_t(top + in % high);
 }
 
-// Piece `c` of a row with `left` bytes from p on, of elements E at their own alignment; zeros behind the end
-template <typename E> __device__ inline Piece any_piece(const char *p, int64_t left)
+// 16 bytes of a row at p, of elements at their own alignment, with `left` bytes from p to the row's end: zeros behind it.
+// The last piece is the row's last 16 bytes, shifted; a row that has fewer is read value by value.
+template <typename E> __device__ inline Piece any_piece(const char *row, int64_t at, int64_t bytes)
 {
-    constexpr int kV = 16 / int(sizeof(E));
-    Piece v = {0, 0, 0, 0};
-    if (left >= 16) {
-        __builtin_memcpy(&v, p, 16);
-    } else {
+    if (bytes < 16) { // the same for all lanes
+        constexpr int kV = 16 / int(sizeof(E));
         E x[kV];
 #pragma unroll
-        for (int e = 0; e < kV; ++e) x[e] = e * int(sizeof(E)) < left ? reinterpret_cast<const E *>(p)[e] : E(0);
+        for (int e = 0; e < kV; ++e) {
+            const bool there = at + e * int(sizeof(E)) < bytes;
+            const E v = *reinterpret_cast<const E *>(row + (there ? at + e * int(sizeof(E)) : 0));
+            x[e] = there ? v : E(0);
+        }
+        Piece v;
         __builtin_memcpy(&v, x, 16);
+        return v;
     }
+    const int64_t most = bytes - 16;
+    const int over = int(at <= most ? 0 : at - most < 16 ? at - most : 16); // bytes behind the end
+    uint64_t v[2];
+    __builtin_memcpy(v, row + (over == 0 ? at : most), 16);
+    const int s = 8 * over;
+    const uint64_t low = s == 0 ? v[0] : s < 64 ? v[0] >> s | v[1] << (64 - s) : s < 128 ? v[1] >> (s - 64) : 0;
+    const uint64_t high = s < 64 ? v[1] >> s : 0;
+    const uint64_t both[2] = {low, high};
+    Piece r;
+    __builtin_memcpy(&r, both, 16);
+    return r;
+}
+// ... of a piece that lies inside its row
+__device__ inline Piece inner_piece(const char *p)
+{
+    Piece v;
+    __builtin_memcpy(&v, p, 16);
     return v;
 }
 
@@ -137,11 +161,11 @@ __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, t
             const int in = row - T::kM, part = in % (16 * T::kJ), block = part / 16, i = part % 16;
             const bool second = kDual && block >= kTogether;
             const int64_t at = int64_t(bj) * (kDual ? T::kN / 2 : T::kN) + in / (16 * T::kJ) * (16 * kTogether)
-                               + i / 4 * (4 * kTogether) + (second ? block - kTogether : block) * 4 + i % 4;
+                               + i * kTogether + (second ? block - kTogether : block);
             const int64_t held = at < a.features ? at : a.features - 1;
             src[e] = second ? a.B2 + held * a.b2_stride : a.B + held * a.b_stride;
         }
-        src[e] += int64_t(first) * kSlice + ((lane % 8) ^ (lane / 8)) * 16;
+        if constexpr (!kAny) src[e] += int64_t(first) * kSlice + ((lane % 8) ^ (lane / 8)) * 16;
     }
     const int wi = w / T::kWn * (T::kI * 16), wj = T::kM + w % T::kWn * (T::kJ * 16);
     const auto fragment = [&](const char *in, int row, int piece) {
@@ -159,7 +183,7 @@ __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, t
 #pragma unroll
         for (int i = 0; i < T::kI; ++i)
 #pragma unroll
-            for (int j = 0; j < T::kJ; ++j) acc[i][j] = Ops<E>::mul(q[half][j], p[half][i], acc[i][j]);
+            for (int j = 0; j < T::kJ; ++j) acc[i][j] = Ops<E>::mul(p[half][i], q[half][j], acc[i][j]);
     };
     // bytes of the row from this lane's piece of a slice on
     const int64_t left0 = a.bytes - int64_t(first) * kSlice - ((lane % 8) ^ (lane / 8)) * 16;
@@ -167,9 +191,14 @@ __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, t
     if constexpr (kAny) {
         Piece x[T::kEach];
         const auto load = [&](int slice) {
+            const int64_t at = int64_t(first + slice) * kSlice + ((lane % 8) ^ (lane / 8)) * 16;
+            if (int64_t(first + slice + 1) * kSlice <= a.bytes) {
 #pragma unroll
-            for (int e = 0; e < T::kEach; ++e)
-                x[e] = any_piece<E>(src[e] + int64_t(slice) * kSlice, left0 - int64_t(slice) * kSlice);
+                for (int e = 0; e < T::kEach; ++e) x[e] = inner_piece(src[e] + at);
+            } else {
+#pragma unroll
+                for (int e = 0; e < T::kEach; ++e) x[e] = any_piece<E>(src[e], at, a.bytes);
+            }
         };
         load(0);
         for (int slice = 0; slice < slices; ++slice) {
@@ -262,8 +291,8 @@ template <typename E, bool kDual, typename F> __device__ inline void large_tiles
             } else {
                 const int block = 2 * h + row % 32 / 16, i = row % 16;
                 const bool second = kDual && h == 1;
-                const int64_t at = int64_t(bj) * (64 * kTogether) + row / 32 * (16 * kTogether) + i / 4 * (4 * kTogether)
-                                   + (second ? block - 2 : block) * 4 + i % 4;
+                const int64_t at = int64_t(bj) * (64 * kTogether) + row / 32 * (16 * kTogether) + i * kTogether
+                                   + (second ? block - 2 : block);
                 const int64_t held = at < a.features ? at : a.features - 1;
                 src[r][e] = second ? a.B2 + held * a.b2_stride : a.B + held * a.b_stride;
             }
@@ -313,7 +342,7 @@ template <typename E, bool kDual, typename F> __device__ inline void large_tiles
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    acc[4 * ha + i][2 * hb + j] = Ops<E>::mul(q[hb][half][j], p[half][i], acc[4 * ha + i][2 * hb + j]);
+                    acc[4 * ha + i][2 * hb + j] = Ops<E>::mul(p[half][i], q[hb][half][j], acc[4 * ha + i][2 * hb + j]);
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_barrier" ::: "memory");
@@ -396,18 +425,21 @@ template <typename T> inline uint32_t blocks_of(uint32_t tiles)
     return std::is_same<T, TileLarge>::value && tiles > uint32_t(kCus) ? uint32_t(kCus) : tiles;
 }
 
-// Points and features of a lane: f(point, feature, i) for each block i of points, with the lane's first feature, of
-// 4 kTogether consecutive ones.
+// Points and features of a lane: f(point, feature, i, r) for row r of each block i of points, with the lane's first
+// feature, of kTogether consecutive ones: acc[i][..][r].
 template <typename T, bool kDual, typename F> __device__ inline void each_run(int32_t bi, int32_t bj, F f)
 {
     constexpr int kTogether = kDual ? T::kJ / 2 : T::kJ;
     const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id();
-    const int64_t feature = int64_t(bj) * (kDual ? T::kN / 2 : T::kN) + w % T::kWn * (16 * kTogether) + lane / 16 * (4 * kTogether);
+    const int64_t feature = int64_t(bj) * (kDual ? T::kN / 2 : T::kN) + w % T::kWn * (16 * kTogether) + lane % 16 * kTogether;
+    const int64_t point = int64_t(bi) * T::kM + w / T::kWn * (T::kI * 16) + lane / 16 * 4;
 #pragma unroll
-    for (int i = 0; i < T::kI; ++i) f(int64_t(bi) * T::kM + w / T::kWn * (T::kI * 16) + 16 * i + lane % 16, feature, i);
+    for (int i = 0; i < T::kI; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) f(point + 16 * i + r, feature, i, r);
 }
 
-// N consecutive values to p, of which `count` exist; vec: aligned to 16 bytes, or to N values where those are fewer
+// N consecutive values to p, of which `count` exist; vec: aligned to 16 bytes, or to N values where those are less
 template <typename E, int N> __device__ inline void store_run(E *p, const float (&v)[N], int64_t count, bool vec)
 {
     constexpr int kV = 16 / int(sizeof(E)) < N ? 16 / int(sizeof(E)) : N;
@@ -429,9 +461,16 @@ template <typename E, int N> __device__ inline void store_run(E *p, const float 
         if (e < count) p[e] = E(v[e]);
 }
 
-inline bool aligned16(const void *p, int64_t stride_bytes)
+inline bool aligned_to(int bytes, const void *p, int64_t stride_bytes)
 {
-    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride_bytes % 16 == 0;
+    return reinterpret_cast<uintptr_t>(p) % uintptr_t(bytes) == 0 && stride_bytes % bytes == 0;
+}
+inline bool aligned16(const void *p, int64_t stride_bytes) { return aligned_to(16, p, stride_bytes); }
+// whether store_run's vectors of N values can be used
+template <typename E, int N> inline bool runs_aligned(const void *p, int64_t stride)
+{
+    constexpr int kBytes = int(sizeof(E)) * N;
+    return aligned_to(kBytes < 16 ? kBytes : 16, p, stride * int64_t(sizeof(E)));
 }
 
 // A launch takes at most kMostTiles tiles: rows are cut into several launches beyond
