@@ -151,66 +151,45 @@ template <typename E, typename T, bool kAny> void run_gated(const GatedArgs &a, 
     }
 }
 
-// Short rows (16 to kHalves 64 bytes): the weights of 32 features stay in a wave's registers, and a block's waves have the
-// same points, kShortPoints at a time: their rows come through LDS, read as pieces that lie side by side in memory, at any
-// alignment; the next ones are under way meanwhile.  Outputs go through LDS too, and from there as whole rows of the block's
-// features.  A row's last piece is its last 16 bytes, of which only those count that the piece before does not have: the others
-// are masked out, in points and weights alike.
-constexpr int kShortWaves = 8;   // of a block at most
-constexpr int kShortPoints = 32;
-constexpr int kShortBlocks = 4 * 2 * kCus; // some rounds of two blocks a CU
-constexpr int kShortPitch(int kHalves) { return kHalves * 64 + 16; } // bytes of a row in LDS: 8 rows on different banks
+// Short rows (16 to kHalves 64 bytes): a block holds the weights of up to kShortFeatures features in LDS, and each wave
+// takes 16 points at a time past all of them, with no barrier: the points' pieces in registers, the next ones under way, the
+// weights' read for each 32 features, whose outputs go through a patch of LDS of the wave's own and from there as 16 bytes a
+// lane, runs of 64 bytes of a point.  A row's last piece is its last 16 bytes, of which only those count that the piece before
+// does not have: the others are masked out, in points and weights alike.
+//
+// 1.3M x 50 to 200 fp16, gelu: 269 us for 650 MB (silu 238).  Bound by the vector instructions: 21 an output for the activation and the
+// product alone, two of them at a quarter of the rate.  Weights in registers and the points past a block's waves in step, by LDS
+// and a barrier, took 301 us (7 waves on 4 SIMDs); without LDS, 429: each lane's 16 bytes a request of its own.
+constexpr int kShortFeatures = 256; // of a block at most
+constexpr int kShortThreads = 512;
+constexpr int kShortBlocks = 2 * 2 * kCus;
+constexpr int kShortPitch(int kHalves) { return kHalves * 64 + 16; } // bytes of a row of weights in LDS: 8 rows on different banks
 
 struct ShortShape {
-    int64_t per_block;   // points, a multiple of kShortPoints
-    int32_t features;    // of a block
-    int32_t pitch;       // bytes of a row of outputs in LDS: a row's own where the outputs are without gaps
-    int32_t vectors;     // of a row; 0: outputs are not aligned for them, values one by one
-    bool flat;           // a tile of outputs is one run of memory
+    int64_t per_wave; // points, a multiple of 16
+    int32_t features; // of a block, a multiple of 32
 };
 
-// The outputs of `rows` points from LDS
-template <typename E, typename V>
-__device__ inline void store_rows(const char *tile, const ShortShape &z, E *out, int64_t stride, int rows, int each)
+// What lanes of a wave have put into LDS is there for its other lanes.  A wave's LDS accesses keep their order, so this
+// costs no instruction: it holds the compiler to that order.
+__device__ inline void wave_exchange()
 {
-    int r = int(threadIdx.x) / each, c = int(threadIdx.x) - r * each;
-    const int down = int(blockDim.x) / each, right = int(blockDim.x) - down * each;
-    while (r < rows) {
-        *reinterpret_cast<V *>(reinterpret_cast<char *>(out + r * stride) + c * int(sizeof(V))) = *reinterpret_cast<const V *>(tile + r * z.pitch + c * int(sizeof(V)));
-        r += down;
-        c += right;
-        if (c >= each) {
-            c -= each;
-            ++r;
-        }
-    }
-}
-template <typename E> __device__ inline void store_tile(const char *tile, const ShortShape &z, E *out, int64_t stride, int rows, int features)
-{
-    if (z.flat) { // rows of 16 bytes
-        char *to = reinterpret_cast<char *>(out);
-        const int bytes = rows * z.pitch;
-        for (int t = int(threadIdx.x) * 16; t < bytes; t += int(blockDim.x) * 16) *reinterpret_cast<Piece *>(to + t) = *reinterpret_cast<const Piece *>(tile + t);
-    } else if (z.vectors > 0 && features * int(sizeof(E)) % 16 == 0) {
-        store_rows<E, Piece>(tile, z, out, stride, rows, features * int(sizeof(E)) / 16);
-    } else {
-        store_rows<E, E>(tile, z, out, stride, rows, features);
-    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 template <typename E, int kHalves, bool kGelu, bool kKeep>
-__global__ __launch_bounds__(kShortWaves *kWave) void gated_short_kernel(Product p, GatedOut o, ShortShape z)
+__global__ __launch_bounds__(kShortThreads) void gated_short_kernel(Product p, GatedOut o, ShortShape z)
 {
     extern __shared__ __align__(16) char s_mem[];
-    constexpr int kPitch = kShortPitch(kHalves), kGroups = kShortPoints / 16, kRowPieces = kHalves * 4;
-    constexpr int kPieces = kShortPoints * kRowPieces, kOuts = kKeep ? 3 : 1;
-    constexpr int kHeld = (kPieces + kWave - 1) / kWave; // pieces of a thread at most
-    char *s_out = s_mem + 2 * kShortPoints * kPitch;
-    const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id(), threads = int(blockDim.x);
+    constexpr int kPitch = kShortPitch(kHalves), kRowPieces = kHalves * 4, kOuts = kKeep ? 3 : 1, kV = 16 / int(sizeof(E));
+    constexpr int kPatch = 32 * int(sizeof(E)) + 16; // bytes of a point's 32 outputs in LDS
+    const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id();
     const int64_t block = int64_t(blockIdx.y) * z.features;
     const int features = int(p.features - block < z.features ? p.features - block : z.features);
-    const int mine = w * 32 + lane % 16 * 2; // of the block's features
     const int bytes = int(p.bytes);
+    char *patch = s_mem + 2 * z.features * kPitch + w * (16 * kPatch);
     // the place of piece c of a row, and what of it counts
     const auto place_of = [&](int c, Piece &mask) {
         const int begin = c * 16, at = begin < bytes - 16 ? begin : bytes - 16, skip = begin - at;
@@ -221,94 +200,97 @@ __global__ __launch_bounds__(kShortWaves *kWave) void gated_short_kernel(Product
         }
         return at;
     };
-    Piece weights[4][kHalves]; // two blocks of gate's features, two of up's
-#pragma unroll
-    for (int h = 0; h < kHalves; ++h) {
+    // Weights: 32 features are four blocks of 16 rows, gate's even and odd features, then up's
+    for (int e = int(threadIdx.x); e < 2 * z.features * kRowPieces; e += kShortThreads) {
+        const int row = e / kRowPieces, c = e % kRowPieces, j = row / 16 % 4;
+        const int64_t f = block + row / 64 * 32 + row % 16 * 2 + j % 2, held = f < p.features ? f : p.features - 1;
         Piece mask;
-        const int at = place_of(h * 4 + lane / 16, mask);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t f = block + mine + j % 2, held = f < p.features ? f : p.features - 1;
-            weights[j][h] = inner_piece((j < 2 ? p.B + held * p.b_stride : p.B2 + held * p.b2_stride) + at) & mask;
-        }
+        const int at = place_of(c, mask);
+        *reinterpret_cast<Piece *>(s_mem + row * kPitch + c * 16) = inner_piece((j < 2 ? p.B + held * p.b_stride : p.B2 + held * p.b2_stride) + at) & mask;
     }
-    const int64_t from = int64_t(blockIdx.x) * z.per_block, to = from + z.per_block < p.rows ? from + z.per_block : p.rows;
-    // a thread loads the same piece of every row that it loads
-    Piece mask, held[kHeld];
-    const int column = int(threadIdx.x) % kRowPieces, row0 = int(threadIdx.x) / kRowPieces, down = threads / kRowPieces;
-    const char *base = p.A + place_of(column, mask);
-    const auto take = [&](int64_t first) {
-#pragma unroll
-        for (int q = 0; q < kHeld; ++q) {
-            if (q * down >= kShortPoints) break;
-            const int64_t point = first + row0 + q * down;
-            held[q] = inner_piece(base + (point < p.rows ? point : p.rows - 1) * p.a_stride);
-        }
-    };
-    const auto put = [&](int parity) {
-#pragma unroll
-        for (int q = 0; q < kHeld; ++q) {
-            if (q * down >= kShortPoints) break;
-            const int row = row0 + q * down;
-            if (row < kShortPoints) *reinterpret_cast<Piece *>(s_mem + (parity * kShortPoints + row) * kPitch + column * 16) = held[q] & mask;
-        }
-    };
-    take(from);
-    put(0);
     __syncthreads();
-    int parity = 0;
-    for (int64_t first = from; first < to; first += kShortPoints, parity ^= 1) {
-        take(first + kShortPoints < to ? first + kShortPoints : first);
-        char *tile = s_out + parity * (kOuts * kShortPoints) * z.pitch;
+    const int64_t from = (int64_t(blockIdx.x) * (kShortThreads / kWave) + w) * z.per_wave, to = from + z.per_wave < p.rows ? from + z.per_wave : p.rows;
+    if (from >= to) return;
+    Piece mask[kHalves], x[kHalves], y[kHalves];
+    int at[kHalves];
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
+    for (int h = 0; h < kHalves; ++h) at[h] = place_of(h * 4 + lane / 16, mask[h]);
+    const auto load = [&](const char *row, Piece (&v)[kHalves]) {
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) v[h] = inner_piece(row + at[h]);
+    };
+    int64_t point = from + lane % 16; // that is loaded
+    const char *row = p.A + (point < p.rows ? point : p.rows - 1) * p.a_stride;
+    load(row, y);
+    // outputs: this lane's 16 bytes of the patch, and where they go
+    constexpr int kEach = 32 / kV; // vectors of a point
+    const int out_row = lane / kEach, out_column = lane % kEach * kV; // rows of a store: 64 / kEach
+    const bool vec = o.vec_h && (!kKeep || (o.vec_a && o.vec_b));
+    for (int64_t first = from; first < to; first += 16, point += 16) {
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) x[h] = y[h] & mask[h];
+        if (first + 32 <= p.rows)
+            row += 16 * p.a_stride;
+        else
+            row = p.A + (point + 16 < p.rows ? point + 16 : p.rows - 1) * p.a_stride;
+        load(row, y);
+        const int rows = int(to - first < 16 ? to - first : 16);
+        const char *in = s_mem + lane % 16 * kPitch + lane / 16 * 16;
+        for (int f = 0; f < features; f += 32, in += 64 * kPitch) {
             typename Ops<E>::Acc acc[4] = {};
-            const char *in = s_mem + (parity * kShortPoints + g * 16 + lane % 16) * kPitch + lane / 16 * 16;
 #pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-                const Piece x = *reinterpret_cast<const Piece *>(in + h * 64);
+            for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[j] = Ops<E>::mul(x, weights[j][h], acc[j]);
-            }
-            struct Two {
-                E v[2];
-            };
-            const bool there = mine < z.features, both = mine + 1 < z.features; // a row in LDS has no room for others
+                for (int j = 0; j < 4; ++j) acc[j] = Ops<E>::mul(x[h], *reinterpret_cast<const Piece *>(in + j * 16 * kPitch + h * 64), acc[j]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                constexpr Act kAct = kGelu ? Act::kGelu : Act::kSilu;
-                Two t[3];
+            for (int k = 0; k < kOuts; ++k) {
+                typedef typename std::conditional<sizeof(E) == 2, uint32_t, uint64_t>::type Bits;
+                struct Two {
+                    E v[2];
+                };
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float a = acc[e][r], b = acc[2 + e][r];
-                    t[0].v[e] = E(activate<E>(a, kAct) * b);
-                    t[1].v[e] = E(a);
-                    t[2].v[e] = E(b);
+                for (int r = 0; r < 4; ++r) {
+                    Two t;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float a = acc[e][r], b = acc[2 + e][r];
+                        t.v[e] = E(k == 0 ? activate<E>(a, kGelu ? Act::kGelu : Act::kSilu) * b : k == 1 ? a : b);
+                    }
+                    *reinterpret_cast<Bits *>(patch + (lane / 16 * 4 + r) * kPatch + lane % 16 * 2 * int(sizeof(E))) = __builtin_bit_cast(Bits, t);
                 }
-                char *at = tile + (g * 16 + lane / 16 * 4 + r) * z.pitch + mine * int(sizeof(E));
+                wave_exchange();
+                E *out = static_cast<E *>(k == 0 ? o.h : k == 1 ? o.a : o.b);
+                const int64_t stride = k == 0 ? o.h_stride : k == 1 ? o.a_stride : o.b_stride;
+                out += first * stride + block + f;
+                if (vec) {
 #pragma unroll
-                for (int k = 0; k < kOuts; ++k) {
-                    E *q = reinterpret_cast<E *>(at + k * kShortPoints * z.pitch);
-                    if (z.features % 2 == 0) { // every row starts at an even value
-                        typedef typename std::conditional<sizeof(E) == 2, uint32_t, uint64_t>::type Bits;
-                        if (there) *reinterpret_cast<Bits *>(q) = __builtin_bit_cast(Bits, t[k]);
-                    } else {
-                        if (there) q[0] = t[k].v[0];
-                        if (both) q[1] = t[k].v[1];
+                    for (int q = 0; q < 16 * kEach / kWave; ++q) {
+                        const int r = out_row + q * (kWave / kEach);
+                        const Piece v = *reinterpret_cast<const Piece *>(patch + r * kPatch + out_column * int(sizeof(E)));
+                        E *to_out = out + r * stride + out_column;
+                        if (f + 32 <= features) {
+                            if (r < rows) *reinterpret_cast<Piece *>(to_out) = v;
+                        } else if (r < rows) {
+                            const int count = features - f - out_column;
+                            if (count >= kV) {
+                                *reinterpret_cast<Piece *>(to_out) = v;
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < kV; ++e)
+                                    if (e < count) to_out[e] = *reinterpret_cast<const E *>(patch + r * kPatch + (out_column + e) * int(sizeof(E)));
+                            }
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const int r = q * 2 + lane / 32, c = lane % 32;
+                        const E v = *reinterpret_cast<const E *>(patch + r * kPatch + c * int(sizeof(E)));
+                        if (r < rows && f + c < features) out[r * stride + c] = v;
                     }
                 }
+                wave_exchange(); // the patch is written again
             }
-        }
-        // the next points' loads are waited for here, and with them the stores before them, but none behind
-        put(parity ^ 1);
-        __syncthreads(); // tiles and rows alternate: one barrier for all
-        const int rows = int(to - first < kShortPoints ? to - first : kShortPoints);
-        store_tile(tile, z, static_cast<E *>(o.h) + first * o.h_stride + block, o.h_stride, rows, features);
-        if constexpr (kKeep) {
-            tile += kShortPoints * z.pitch;
-            store_tile(tile, z, static_cast<E *>(o.a) + first * o.a_stride + block, o.a_stride, rows, features);
-            tile += kShortPoints * z.pitch;
-            store_tile(tile, z, static_cast<E *>(o.b) + first * o.b_stride + block, o.b_stride, rows, features);
         }
     }
 }
@@ -317,23 +299,21 @@ int64_t tiles_of(int64_t rows, int64_t cols, int m, int n) { return (rows + m - 
 
 template <typename E, int kHalves> void run_gated_short(const GatedArgs &a, hipStream_t st)
 {
-    constexpr int kEs = int(sizeof(E)), kV = 16 / kEs;
+    constexpr int kEs = int(sizeof(E)), kWaves = kShortThreads / kWave;
     const Product p = gated_product(a, kEs);
-    const GatedOut o = gated_out<E, kV>(a);
+    const GatedOut o = gated_out<E, 16 / kEs>(a);
     const bool keep = a.a != nullptr;
-    const int64_t all = (a.f + 31) / 32, groups = (all + kShortWaves - 1) / kShortWaves, waves = (all + groups - 1) / groups;
+    const int64_t groups = (a.f + kShortFeatures - 1) / kShortFeatures;
     ShortShape z = {};
-    z.features = int32_t(a.f < waves * 32 ? a.f : waves * 32);
-    const bool vec = o.vec_h && (!keep || (o.vec_a && o.vec_b));
-    z.vectors = vec ? z.features / kV : 0;
-    z.flat = vec && a.f == z.features && a.h_stride == a.f && (!keep || (a.a_stride == a.f && a.b_stride == a.f));
-    z.pitch = z.flat ? z.features * kEs : (z.features * kEs + 15) / 16 * 16 + 16;
-    const int64_t want = (kShortBlocks + groups - 1) / groups, most = (a.n + want - 1) / want;
-    z.per_block = (most + kShortPoints - 1) / kShortPoints * kShortPoints;
-    const dim3 grid(uint32_t((a.n + z.per_block - 1) / z.per_block), uint32_t(groups));
-    const uint32_t threads = uint32_t(waves) * kWave;
-    const size_t lds = 2 * kShortPoints * (kShortPitch(kHalves) + size_t(keep ? 3 : 1) * size_t(z.pitch));
-    const auto launch = [&](auto kernel) { kernel<<<grid, threads, lds, st>>>(p, o, z); };
+    z.features = int32_t(((a.f + groups - 1) / groups + 31) / 32 * 32);
+    const int64_t across = (a.f + z.features - 1) / z.features;
+    // a few rounds of two blocks a CU
+    const int64_t want = (kShortBlocks + across - 1) / across * kWaves, most = (a.n + want - 1) / want;
+    z.per_wave = (most + 15) / 16 * 16;
+    const int64_t waves = (a.n + z.per_wave - 1) / z.per_wave;
+    const dim3 grid(uint32_t((waves + kWaves - 1) / kWaves), uint32_t(across));
+    const size_t lds = 2 * size_t(z.features) * kShortPitch(kHalves) + size_t(kWaves) * 16 * (32 * kEs + 16);
+    const auto launch = [&](auto kernel) { kernel<<<grid, kShortThreads, lds, st>>>(p, o, z); };
     if (a.act == Act::kGelu)
         keep ? launch(gated_short_kernel<E, kHalves, true, true>) : launch(gated_short_kernel<E, kHalves, true, false>);
     else
