@@ -51,13 +51,13 @@ struct GatedArgs {
 };
 void launch_gated_layer(const GatedArgs &a, hipStream_t st);
 
-// Backward: da and db side by side (n rows), both transposed (2 f rows), x and the weights transposed, rows padded to
-// 16 bytes; partial sums of the weights' gradients where they are shared out over the points.
+// Backward: da and db side by side (n rows), x with padded rows, the weights transposed and side by side; partial sums of
+// the weights' gradients where they are shared out over the points.  Rows are padded to 16 bytes.
 constexpr int64_t pad16(int64_t count, int bytes) { return (count * bytes + 15) / 16 * 16 / bytes; }
 struct GatedBackLayout {
-    int64_t fp, np;      // padded features and points
-    int splits;          // of the sums over points
-    size_t d, dt, xt, wt, part, total;
+    int64_t fp, dp; // padded f and d
+    int splits;     // of the sums over points
+    size_t d, xp, wt, part, total;
 };
 GatedBackLayout make_gated_back_layout(int64_t n, int64_t d, int64_t f, Elem type);
 

@@ -82,8 +82,8 @@ template <typename E, typename T, bool kAny>
 __global__ __launch_bounds__(T::kThreads) void gated_kernel(Product p, GatedOut o)
 {
     constexpr int kRun = T::kJ / 2; // features of a lane
-    each_tile<E, T, true, kAny>(p, [&](int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ]) {
-        each_run<T, true>(bi, bj, [&](int64_t point, int64_t feature, int i, int r) {
+    each_tile<E, T, Form::kDual, kAny>(p, [&](int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ]) {
+        each_run<T, Form::kDual>(bi, bj, [&](int64_t point, int64_t feature, int i, int r) {
             if (point >= p.rows) return;
             float a[kRun], b[kRun], h[kRun];
 #pragma unroll
@@ -338,127 +338,145 @@ template <typename E> void run_gated_type(const GatedArgs &a, hipStream_t st)
 }
 
 // ------------------------------------------------------------------ backward: operands
-constexpr int kT = 64;
+// One launch: da and db side by side, a row a point; the weights transposed and side by side; x with rows that are padded to
+// 16 bytes, where its own are not.  Blocks are dealt to the three by their number.
+constexpr int kT = 64; // side of a tile that is transposed
 
-template <typename E> __device__ inline float load_or_zero(const void *p, int64_t stride, int64_t r, int64_t c, bool there)
+struct Operands {
+    const void *dh, *a, *b, *x, *gate, *up;
+    char *d, *xp, *wt;
+    int64_t dh_stride, a_stride, b_stride, x_stride, gate_stride, up_stride;
+    int64_t n, features, f;
+    int64_t fp, dp;                 // padded to 16 bytes
+    uint32_t slope_blocks, weight_blocks, x_blocks;
+    Act act;
+    bool straight;                  // rows of f values of dh, a and b are whole pieces
+};
+
+template <typename E> __device__ inline Piece row_piece(const void *p, int64_t row_bytes, int64_t row, int64_t c, int64_t bytes, bool straight)
 {
-    const E *e = static_cast<const E *>(p);
-    return float(e[there ? r * stride + c : 0]);
+    const char *r = static_cast<const char *>(p) + row * row_bytes;
+    return straight ? inner_piece(r + c * 16) : any_piece<E>(r, c * 16, bytes);
 }
 
-// Tiles of 64 points x 64 features: da and db in both orientations, zeros in the padding
-template <typename E> __global__ __launch_bounds__(256) void gated_slopes_kernel(GatedBackArgs a, GatedBackLayout L, int64_t row0)
+template <typename E> __global__ __launch_bounds__(256) void gated_operands_kernel(Operands g)
 {
-    __shared__ float s_a[kT][kT + 1], s_b[kT][kT + 1];
-    const int64_t r0 = (row0 + blockIdx.y) * kT, c0 = int64_t(blockIdx.x) * kT;
-    char *ws = static_cast<char *>(a.ws);
-    E *d = reinterpret_cast<E *>(ws + L.d), *dt = reinterpret_cast<E *>(ws + L.dt);
-    for (int s = threadIdx.x; s < kT * kT; s += 256) {
-        const int row = s / kT, col = s % kT;
-        const int64_t r = r0 + row, c = c0 + col;
-        const bool there = r < a.n && c < a.f;
-        const float dh = load_or_zero<E>(a.dh, a.dh_stride, r, c, there);
-        const float av = load_or_zero<E>(a.a, a.a_stride, r, c, there), bv = load_or_zero<E>(a.b, a.b_stride, r, c, there);
-        float value, slope;
-        activate_both<E>(av, a.act, value, slope);
-        const float da = there ? dh * bv * slope : 0.0f, db = there ? dh * value : 0.0f;
-        s_a[row][col] = da;
-        s_b[row][col] = db;
-        if (a.dx && r < a.n && c < L.fp) {
-            d[r * 2 * L.fp + c] = E(da);
-            d[r * 2 * L.fp + L.fp + c] = E(db);
-        }
-    }
-    if (!a.dgate && !a.dup) return;
-    __syncthreads();
-    for (int s = threadIdx.x; s < kT * kT; s += 256) {
-        const int col = s / kT, row = s % kT;
-        const int64_t r = r0 + row, c = c0 + col;
-        if (r >= L.np || c >= a.f) continue;
-        dt[c * L.np + r] = E(s_a[row][col]);
-        dt[(a.f + c) * L.np + r] = E(s_b[row][col]);
-    }
-}
-
-// out[c][r] = in[r][c], rows of `out` `ld` long, zeros for r from rows up to `to`
-template <typename E>
-__global__ __launch_bounds__(256) void transpose_kernel(const E *in, int64_t stride, int64_t rows, int64_t cols, E *out, int64_t ld, int64_t to,
-                                                        int64_t row0)
-{
+    constexpr int kEs = int(sizeof(E)), kV = 16 / kEs;
+    struct alignas(16) Values {
+        E v[kV];
+    };
     __shared__ E s_t[kT][kT + 2];
-    const int64_t r0 = (row0 + blockIdx.y) * kT, c0 = int64_t(blockIdx.x) * kT;
-    for (int s = threadIdx.x; s < kT * kT; s += 256) {
-        const int row = s / kT, col = s % kT;
-        const bool there = r0 + row < rows && c0 + col < cols;
-        const E v = in[there ? (r0 + row) * stride + c0 + col : 0];
-        s_t[row][col] = there ? v : E(0.0f);
+    uint32_t b = blockIdx.x;
+    if (b < g.slope_blocks) {
+        const int64_t each = g.fp / kV, total = g.n * each;
+        for (int64_t t = int64_t(b) * 256 + threadIdx.x; t < total; t += int64_t(g.slope_blocks) * 256) {
+            const int64_t row = total <= 0xffffffffll ? uint32_t(t) / uint32_t(each) : t / each, c = t - row * each;
+            const int64_t bytes = g.f * kEs;
+            const Values dh = __builtin_bit_cast(Values, row_piece<E>(g.dh, g.dh_stride * kEs, row, c, bytes, g.straight));
+            const Values av = __builtin_bit_cast(Values, row_piece<E>(g.a, g.a_stride * kEs, row, c, bytes, g.straight));
+            const Values bv = __builtin_bit_cast(Values, row_piece<E>(g.b, g.b_stride * kEs, row, c, bytes, g.straight));
+            Values da, db;
+#pragma unroll
+            for (int e = 0; e < kV; ++e) {
+                float value, slope;
+                activate_both<E>(float(av.v[e]), g.act, value, slope);
+                const float d = float(dh.v[e]);
+                da.v[e] = E(d * float(bv.v[e]) * slope);
+                db.v[e] = E(d * value);
+            }
+            char *out = g.d + (row * 2 * g.fp + c * kV) * kEs;
+            *reinterpret_cast<Values *>(out) = da;
+            *reinterpret_cast<Values *>(out + g.fp * kEs) = db;
+        }
+        return;
     }
-    __syncthreads();
-    for (int s = threadIdx.x; s < kT * kT; s += 256) {
-        const int col = s / kT, row = s % kT;
-        if (r0 + row < to && c0 + col < cols) out[(c0 + col) * ld + r0 + row] = s_t[row][col];
+    b -= g.slope_blocks;
+    if (b < g.weight_blocks) {
+        const uint32_t across = uint32_t((g.features + kT - 1) / kT), down = uint32_t((g.fp + kT - 1) / kT);
+        const bool second = b >= across * down;
+        if (second) b -= across * down;
+        const E *in = static_cast<const E *>(second ? g.up : g.gate);
+        const int64_t stride = second ? g.up_stride : g.gate_stride, r0 = int64_t(b / across) * kT, c0 = int64_t(b % across) * kT;
+        for (int s = int(threadIdx.x); s < kT * kT; s += 256) {
+            const int row = s / kT, col = s % kT;
+            const bool there = r0 + row < g.f && c0 + col < g.features;
+            const E v = in[there ? (r0 + row) * stride + c0 + col : 0];
+            s_t[row][col] = there ? v : E(0.0f);
+        }
+        __syncthreads();
+        E *out = reinterpret_cast<E *>(g.wt) + (second ? g.fp : 0);
+        for (int s = int(threadIdx.x); s < kT * kT; s += 256) {
+            const int col = s / kT, row = s % kT;
+            if (r0 + row < g.fp && c0 + col < g.features) out[(c0 + col) * 2 * g.fp + r0 + row] = s_t[row][col];
+        }
+        return;
     }
-}
-
-constexpr int64_t kMostRowTiles = 65535; // of a launch
-
-template <typename E>
-void transpose(const void *in, int64_t stride, int64_t rows, int64_t cols, E *out, int64_t ld, int64_t to, hipStream_t st)
-{
-    const int64_t down = (to + kT - 1) / kT;
-    for (int64_t from = 0; from < down; from += kMostRowTiles) {
-        const int64_t y = down - from < kMostRowTiles ? down - from : kMostRowTiles;
-        transpose_kernel<E><<<dim3(uint32_t((cols + kT - 1) / kT), uint32_t(y)), 256, 0, st>>>(static_cast<const E *>(in), stride, rows, cols,
-                                                                                               out, ld, to, from);
+    b -= g.weight_blocks;
+    const int64_t each = g.dp / kV, total = g.n * each;
+    for (int64_t t = int64_t(b) * 256 + threadIdx.x; t < total; t += int64_t(g.x_blocks) * 256) {
+        const int64_t row = t / each, c = t - row * each;
+        *reinterpret_cast<Piece *>(g.xp + t * 16) = any_piece<E>(static_cast<const char *>(g.x) + row * g.x_stride * kEs, c * 16, g.features * kEs);
     }
 }
 
 // ------------------------------------------------------------------ backward: products
-// kPart: fp32 partial sums of a split; else the outputs, whose rows from `first2` on are those of out2
+// dx: rows as they are.  The weights' gradients: rows 0 .. f - 1 are dgate's, rows from `first2` on dup's; kPart: fp32 partial
+// sums of a split.
 struct BackOut {
     void *out, *out2;
     float *part;
-    int64_t stride, stride2, first2;
-    bool vec, vec2;
+    int64_t stride, stride2, first2, f, features;
+    bool vec;
 };
 
-template <typename E, typename T, bool kPart>
+template <typename E, typename T, Form kForm, bool kPart>
 __global__ __launch_bounds__(T::kThreads) void gated_back_kernel(Product p, BackOut o)
 {
     constexpr int kRun = T::kJ;
-    each_tile<E, T, false, false>(p, [&](int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ]) {
-        each_run<T, false>(bi, bj, [&](int64_t row, int64_t feature, int i, int r) {
+    each_tile<E, T, kForm, false>(p, [&](int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ]) {
+        each_run<T, kForm>(bi, bj, [&](int64_t row, int64_t feature, int i, int r) {
             if (row >= p.rows) return;
             float v[kRun];
 #pragma unroll
             for (int e = 0; e < kRun; ++e) v[e] = acc[i][e][r];
-            const int64_t count = p.features - feature;
-            if constexpr (kPart) {
-                store_run(o.part + (int64_t(blockIdx.y) * p.rows + row) * p.features + feature, v, count, o.vec);
+            const int64_t count = o.features - feature; // p.features may be padded
+            if constexpr (kForm == Form::kRows) {
+                store_run(static_cast<E *>(o.out) + row * o.stride + feature, v, count, o.vec);
             } else {
                 const bool second = row >= o.first2;
+                const int64_t at = second ? row - o.first2 : row;
                 E *out = static_cast<E *>(second ? o.out2 : o.out);
-                if (out) store_run(out + (second ? row - o.first2 : row) * (second ? o.stride2 : o.stride) + feature, v, count, second ? o.vec2 : o.vec);
+                if (at >= o.f) return;
+#pragma unroll
+                for (int e = 0; e < kRun; ++e) {
+                    if (16 * e >= count) continue;
+                    if constexpr (kPart)
+                        o.part[(int64_t(blockIdx.y) * 2 * o.f + (second ? o.f : 0) + at) * o.features + feature + 16 * e] = v[e];
+                    else if (out)
+                        out[at * (second ? o.stride2 : o.stride) + feature + 16 * e] = E(v[e]);
+                }
             }
         });
     });
 }
 
-// The splits' sums in a fixed order, fp64
-template <typename E> __global__ __launch_bounds__(256) void gated_join_kernel(BackOut o, int64_t rows, int64_t features, int splits)
+// The splits' sums in a fixed order, fp64: rows 0 .. 2 f - 1
+template <typename E> __global__ __launch_bounds__(256) void gated_join_kernel(BackOut o, int splits)
 {
-    const int64_t total = rows * features;
+    const int64_t features = o.features;
+    const int64_t total = 2 * o.f * features;
     for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < total; e += int64_t(gridDim.x) * 256) {
         double sum = 0.0;
+#pragma unroll 4
         for (int s = 0; s < splits; ++s) sum += double(o.part[s * total + e]);
-        const int64_t row = e / features, col = e - row * features;
-        const bool second = row >= o.first2;
+        const int64_t row = total <= 0xffffffffll ? uint32_t(e) / uint32_t(features) : e / features, col = e - row * features;
+        const bool second = row >= o.f;
         E *out = static_cast<E *>(second ? o.out2 : o.out);
-        if (out) out[(second ? row - o.first2 : row) * (second ? o.stride2 : o.stride) + col] = E(float(sum));
+        if (out) out[(second ? row - o.f : row) * (second ? o.stride2 : o.stride) + col] = E(float(sum));
     }
 }
 
-template <typename E, typename T>
+template <typename E, typename T, Form kForm>
 void run_back(Product p, const BackOut &o, int splits, hipStream_t st)
 {
     p.slices = int32_t((p.bytes + kSlice - 1) / kSlice);
@@ -467,78 +485,101 @@ void run_back(Product p, const BackOut &o, int splits, hipStream_t st)
     const size_t lds = size_t(T::kStages) * T::kBuffer;
     const int64_t all = p.rows, most = kMostTiles / p.across > 0 ? kMostTiles / p.across * T::kM : T::kM;
     const char *A = p.A;
-    for (int64_t from = 0; from < all; from += most) { // several launches only for dx, which has no second matrix
+    for (int64_t from = 0; from < all; from += most) { // several launches only of kRows: the weights have fewer tiles
         p.A = A + from * p.a_stride;
         p.rows = all - from < most ? all - from : most;
         p.down = int32_t((p.rows + T::kM - 1) / T::kM);
         BackOut q = o;
-        if (q.out) q.out = static_cast<E *>(o.out) + from * o.stride;
+        if (kForm == Form::kRows) q.out = static_cast<E *>(o.out) + from * o.stride;
         const dim3 grid(blocks_of<T>(uint32_t(p.down) * uint32_t(p.across)), uint32_t(splits));
-        if (splits > 1)
-            gated_back_kernel<E, T, true><<<grid, T::kThreads, lds, st>>>(p, q);
+        if (kForm == Form::kColumns && splits > 1)
+            gated_back_kernel<E, T, kForm, kForm == Form::kColumns><<<grid, T::kThreads, lds, st>>>(p, q);
         else
-            gated_back_kernel<E, T, false><<<grid, T::kThreads, lds, st>>>(p, q);
+            gated_back_kernel<E, T, kForm, false><<<grid, T::kThreads, lds, st>>>(p, q);
     }
 }
 
-template <typename E> void run_back_tile(const Product &p, const BackOut &o, int splits, hipStream_t st)
+template <typename E, Form kForm> void run_back_tile(const Product &p, const BackOut &o, int splits, hipStream_t st)
 {
     const int64_t slices = (p.bytes + kSlice - 1) / kSlice, last = slices - (splits - 1) * ((slices + splits - 1) / splits);
-    if (tiles_of(p.rows, p.features, 256, 256) * splits >= kCus && last >= 2) return run_back<E, TileLarge>(p, o, splits, st);
-    if (tiles_of(p.rows, p.features, 128, 128) * splits >= kCus) return run_back<E, TileMiddle>(p, o, splits, st);
-    run_back<E, TileSmall>(p, o, splits, st);
+    if (tiles_of(p.rows, p.features, 256, 256) * splits >= kCus && last >= 2) return run_back<E, TileLarge, kForm>(p, o, splits, st);
+    if (tiles_of(p.rows, p.features, 128, 128) * splits >= kCus) return run_back<E, TileMiddle, kForm>(p, o, splits, st);
+    run_back<E, TileSmall, kForm>(p, o, splits, st);
 }
 
 template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st)
 {
     const GatedBackLayout L = make_gated_back_layout(a.n, a.d, a.f, a.type);
-    const int64_t es = int64_t(sizeof(E));
+    const int64_t es = int64_t(sizeof(E)), kV = 16 / es;
     char *ws = static_cast<char *>(a.ws);
-    E *d = reinterpret_cast<E *>(ws + L.d), *dt = reinterpret_cast<E *>(ws + L.dt);
-    E *xt = reinterpret_cast<E *>(ws + L.xt), *wt = reinterpret_cast<E *>(ws + L.wt);
-    const bool weights = a.dgate || a.dup;
-    const int64_t cols = L.fp > a.f ? L.fp : a.f, down = (L.np + kT - 1) / kT;
-    for (int64_t from = 0; from < down; from += kMostRowTiles) {
-        const int64_t y = down - from < kMostRowTiles ? down - from : kMostRowTiles;
-        gated_slopes_kernel<E><<<dim3(uint32_t((cols + kT - 1) / kT), uint32_t(y)), 256, 0, st>>>(a, L, from);
-    }
+    const bool weights = a.dgate || a.dup, pad_x = weights && (!aligned16(a.x, a.x_stride * es) || a.d * es % 16 != 0);
+    Operands g = {};
+    g.dh = a.dh;
+    g.a = a.a;
+    g.b = a.b;
+    g.x = a.x;
+    g.gate = a.gate;
+    g.up = a.up;
+    g.dh_stride = a.dh_stride;
+    g.a_stride = a.a_stride;
+    g.b_stride = a.b_stride;
+    g.x_stride = a.x_stride;
+    g.gate_stride = a.gate_stride;
+    g.up_stride = a.up_stride;
+    g.n = a.n;
+    g.features = a.d;
+    g.f = a.f;
+    g.fp = L.fp;
+    g.dp = L.dp;
+    g.d = ws + L.d;
+    g.xp = ws + L.xp;
+    g.wt = ws + L.wt;
+    g.act = a.act;
+    g.straight = a.f * es % 16 == 0;
+    const auto blocks_for = [](int64_t pieces) {
+        const int64_t blocks = (pieces + 255) / 256;
+        return uint32_t(blocks < 16 * kCus ? blocks : 16 * kCus);
+    };
+    g.slope_blocks = blocks_for(a.n * (L.fp / kV));
+    g.weight_blocks = a.dx ? uint32_t(2 * tiles_of(L.fp, a.d, kT, kT)) : 0;
+    g.x_blocks = pad_x ? blocks_for(a.n * (L.dp / kV)) : 0;
+    gated_operands_kernel<E><<<g.slope_blocks + g.weight_blocks + g.x_blocks, 256, 0, st>>>(g);
     if (a.dx) {
-        transpose<E>(a.gate, a.gate_stride, a.f, a.d, wt, 2 * L.fp, L.fp, st);
-        transpose<E>(a.up, a.up_stride, a.f, a.d, wt + L.fp, 2 * L.fp, L.fp, st);
         Product p = {};
-        p.A = reinterpret_cast<const char *>(d);
-        p.B = reinterpret_cast<const char *>(wt);
+        p.A = g.d;
+        p.B = g.wt;
         p.a_stride = p.b_stride = p.bytes = 2 * L.fp * es;
         p.rows = a.n;
         p.features = a.d;
         BackOut o = {};
         o.out = a.dx;
+        o.features = a.d;
         o.stride = a.dx_stride;
-        o.first2 = int64_t(1) << 62;
         o.vec = aligned16(a.dx, a.dx_stride * es);
-        run_back_tile<E>(p, o, 1, st);
+        run_back_tile<E, Form::kRows>(p, o, 1, st);
     }
     if (weights) {
-        transpose<E>(a.x, a.x_stride, a.n, a.d, xt, L.np, L.np, st);
         Product p = {};
-        p.A = reinterpret_cast<const char *>(dt);
-        p.B = reinterpret_cast<const char *>(xt);
-        p.a_stride = p.b_stride = p.bytes = L.np * es;
-        p.rows = 2 * a.f;
-        p.features = a.d;
+        p.A = g.d;
+        p.B = pad_x ? g.xp : static_cast<const char *>(a.x);
+        p.a_stride = 2 * L.fp * es;
+        p.b_stride = (pad_x ? L.dp : a.x_stride) * es;
+        p.bytes = a.n * es;
+        p.rows = 2 * L.fp;
+        p.features = pad_x ? L.dp : a.d;
         BackOut o = {};
         o.out = a.dgate;
         o.out2 = a.dup;
         o.stride = a.dgate_stride;
         o.stride2 = a.dup_stride;
-        o.first2 = a.f;
+        o.first2 = L.fp;
+        o.f = a.f;
+        o.features = a.d;
         o.part = reinterpret_cast<float *>(ws + L.part);
-        o.vec = L.splits > 1 ? a.d % 4 == 0 : aligned16(a.dgate, a.dgate_stride * es);
-        o.vec2 = aligned16(a.dup, a.dup_stride * es);
-        run_back_tile<E>(p, o, L.splits, st);
+        run_back_tile<E, Form::kColumns>(p, o, L.splits, st);
         if (L.splits > 1) {
             const int64_t blocks = (2 * a.f * a.d + 255) / 256;
-            gated_join_kernel<E><<<uint32_t(blocks < 8192 ? blocks : 8192), 256, 0, st>>>(o, 2 * a.f, a.d, L.splits);
+            gated_join_kernel<E><<<uint32_t(blocks < 8192 ? blocks : 8192), 256, 0, st>>>(o, L.splits);
         }
     }
 }
@@ -566,10 +607,10 @@ GatedBackLayout make_gated_back_layout(int64_t n, int64_t d, int64_t f, Elem typ
     const int es = elem_bytes(type);
     GatedBackLayout L = {};
     L.fp = pad16(f, es);
-    L.np = pad16(n, es);
+    L.dp = pad16(d, es);
     // enough tiles of the weights' gradients for the chip, of eight slices at least each
-    const int64_t slices = (L.np * es + kSlice - 1) / kSlice;
-    const int64_t tiles = tiles_of(2 * f, d, 128, 128), most = (slices + 7) / 8;
+    const int64_t slices = (n * es + kSlice - 1) / kSlice;
+    const int64_t tiles = tiles_of(2 * L.fp, d, 128, 128), most = (slices + 7) / 8;
     int64_t splits = (2 * kCus + tiles - 1) / tiles;
     splits = splits < 1 ? 1 : splits < most ? splits : most < 1 ? 1 : most;
     const int64_t each = (slices + splits - 1) / splits;
@@ -581,10 +622,9 @@ GatedBackLayout make_gated_back_layout(int64_t n, int64_t d, int64_t f, Elem typ
         return here;
     };
     L.d = take(n * 2 * L.fp, es);
-    L.dt = take(2 * f * L.np, es);
-    L.xt = take(d * L.np, es);
+    L.xp = take(n * L.dp, es);
     L.wt = take(d * 2 * L.fp, es);
-    L.part = take(L.splits > 1 ? L.splits * 2 * f * d : 0, 4);
+    L.part = take(L.splits > 1 ? L.splits * 2 * f * L.dp : 0, 4);
     L.total = at > 0 ? at : 256;
     return L;
 }

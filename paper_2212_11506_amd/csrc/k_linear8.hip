@@ -120,9 +120,9 @@ template <typename E, typename T, bool kAny>
 __global__ __launch_bounds__(T::kThreads) void linear8_kernel(Product p, LinearOut o)
 {
     constexpr int kRun = T::kJ;
-    each_tile<int8_t, T, false, kAny>(p, [&](int32_t bi, int32_t bj, Ops<int8_t>::Acc (&acc)[T::kI][T::kJ]) {
+    each_tile<int8_t, T, Form::kRows, kAny>(p, [&](int32_t bi, int32_t bj, Ops<int8_t>::Acc (&acc)[T::kI][T::kJ]) {
         float scale[kRun], bias[kRun];
-        each_run<T, false>(bi, bj, [&](int64_t point, int64_t feature, int i, int r) {
+        each_run<T, Form::kRows>(bi, bj, [&](int64_t point, int64_t feature, int i, int r) {
             if (i == 0 && r == 0) {
 #pragma unroll
                 for (int e = 0; e < kRun; ++e) {

@@ -75,12 +75,17 @@ template <int M, int N, int Wm, int Wn, int Stages> struct Tile {
     static_assert(kGroups % kWaves == 0 && M % (16 * Wm) == 0 && N % (16 * Wn) == 0, "even shares");
 };
 
-// Operands and grid of a product.  Rows are `bytes` long.
+// How a product's operands lie.  kRows: C = A B^T of rows as above.  kDual: two such products of one A, by B and B2, whose
+// values a lane has side by side.  kColumns: C = A^T B, both summed over their rows (points): a slice is so many rows that
+// its columns are kSlice bytes high, and fragments are read across the rows (16-bit values by transposing LDS loads).
+enum class Form { kRows, kDual, kColumns };
+
+// Operands and grid of a product.
 struct Product {
-    const char *A, *B, *B2;      // kDual: B and B2 give the features' two values
+    const char *A, *B, *B2;
     int64_t a_stride, b_stride, b2_stride; // bytes between rows
-    int64_t rows, features;
-    int64_t bytes;
+    int64_t rows, features;                // of the output (kColumns: columns of A and of B)
+    int64_t bytes;                         // of a row; kColumns: rows summed over, times the size of a value
     int32_t down, across;        // tiles
     int32_t slices, per_split;   // of a row, and of a split (blockIdx.y)
 };
@@ -137,37 +142,79 @@ __device__ inline Piece inner_piece(const char *p)
     return v;
 }
 
-// A wave's blocks: acc[i][j] holds rows 16 j .. of the wave's part of B against points 16 i ..  kDual: the first half of
+// Columns in LDS: `kPitch` bytes a row.  The pieces of a row are stored in an order that depends on the row, such that the
+// 16 columns of a block, in four rows next to each other, fall on different banks.
+template <typename E> __device__ inline int column_piece(int c, int row) { return c ^ (int(sizeof(E)) * (row & 3)); }
+
+// What a lane takes of columns 16 `block` .. in half a slice: a fragment's values for column lane % 16.  16 bits: a transposing
+// load gives 4 x 16 values of each 16 lanes, which name the four rows' pieces; two make the 8 rows of a lane.  32 bits: one by one.
+template <typename E, int kPitch> __device__ inline Piece column_fragment(const char *in, int block, int half)
+{
+    const int lane = lane_id();
+    Piece v;
+    if constexpr (sizeof(E) == 2) {
+        typedef short Four __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) Four *Place;
+        const int q = lane % 16 / 4;
+        const char *at = in + (32 * half + lane / 16 * 8 + q) * kPitch + (block ^ q) * 32 + lane % 4 * 8;
+        const Four low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)at);
+        const Four high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(at + 4 * kPitch));
+        const Four both[2] = {low, high};
+        __builtin_memcpy(&v, both, 16);
+    } else {
+        const char *at = in + (16 * half + lane / 16) * kPitch + (block ^ (lane / 16)) * 64 + lane % 16 * 4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const int32_t *>(at + 4 * e * kPitch);
+    }
+    return v;
+}
+
+// A wave's blocks: acc[i][j] holds points 16 i .. against rows 16 j .. of the wave's part of B.  kDual: the first half of
 // the blocks j is B's, the second B2's.  kAny: rows of any alignment and length, through registers; else rows, their
 // strides and lengths are multiples of 16 bytes and loads write LDS directly.
-template <typename E, typename T, bool kDual, bool kAny>
+template <typename E, typename T, Form kForm, bool kAny>
 __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ])
 {
     extern __shared__ __align__(16) char s_mem[];
-    constexpr int kTogether = kDual ? T::kJ / 2 : T::kJ; // blocks whose rows are a lane's consecutive features
+    constexpr bool kDual = kForm == Form::kDual, kColumns = kForm == Form::kColumns;
+    constexpr int kEs = int(sizeof(E)), kTogether = kDual ? T::kJ / 2 : T::kJ; // blocks whose rows are a lane's consecutive features
     const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id();
     const int32_t first = int32_t(blockIdx.y) * a.per_split;
     const int32_t slices = (first + a.per_split < a.slices ? first + a.per_split : a.slices) - first;
 
-    // this lane's piece of each group of eight rows that the wave loads
+    // this lane's piece of each kilobyte that the wave loads, and where that ends: bytes left of the row (of the column)
     const char *src[T::kEach];
+    int64_t left[kColumns ? T::kEach : 1], step[2]; // step: from slice to slice, of A and of B
+    left[0] = a.bytes - int64_t(first) * kSlice - ((lane % 8) ^ (lane / 8)) * 16;
+    step[0] = kColumns ? kSlice / kEs * a.a_stride : kSlice;
+    step[1] = kColumns ? kSlice / kEs * a.b_stride : kSlice;
 #pragma unroll
     for (int e = 0; e < T::kEach; ++e) {
-        const int row = (e * T::kWaves + w) * 8 + lane / 8;
-        if ((e * T::kWaves + w) * 8 < T::kM) {
-            const int64_t at = int64_t(bi) * T::kM + row;
-            src[e] = a.A + (at < a.rows ? at : a.rows - 1) * a.a_stride;
+        const bool in_a = (e * T::kWaves + w) * 8 < T::kM;
+        if constexpr (kColumns) {
+            const int part = (e * T::kWaves + w) * 8 - (in_a ? 0 : T::kM); // eighths of a kilobyte before this one
+            const int pieces = (in_a ? T::kM : T::kN) * kEs / 16, at = part * 8 + lane, row = at / pieces;
+            const int64_t column = int64_t(in_a ? bi * T::kM : bj * T::kN) * kEs + column_piece<E>(at % pieces, row) * 16;
+            const int64_t most = (in_a ? a.rows : a.features) * kEs - 16, stride = in_a ? a.a_stride : a.b_stride;
+            src[e] = (in_a ? a.A : a.B) + (int64_t(first) * (kSlice / kEs) + row) * stride + (column < most ? column : most);
+            left[e] = a.bytes - int64_t(first) * kSlice - row * kEs;
         } else {
-            const int in = row - T::kM, part = in % (16 * T::kJ), block = part / 16, i = part % 16;
-            const bool second = kDual && block >= kTogether;
-            const int64_t at = int64_t(bj) * (kDual ? T::kN / 2 : T::kN) + in / (16 * T::kJ) * (16 * kTogether)
-                               + i * kTogether + (second ? block - kTogether : block);
-            const int64_t held = at < a.features ? at : a.features - 1;
-            src[e] = second ? a.B2 + held * a.b2_stride : a.B + held * a.b_stride;
+            const int row = (e * T::kWaves + w) * 8 + lane / 8;
+            if (in_a) {
+                const int64_t at = int64_t(bi) * T::kM + row;
+                src[e] = a.A + (at < a.rows ? at : a.rows - 1) * a.a_stride;
+            } else {
+                const int in = row - T::kM, part = in % (16 * T::kJ), block = part / 16, i = part % 16;
+                const bool second = kDual && block >= kTogether;
+                const int64_t at = int64_t(bj) * (kDual ? T::kN / 2 : T::kN) + in / (16 * T::kJ) * (16 * kTogether) + i * kTogether
+                                   + (second ? block - kTogether : block);
+                const int64_t held = at < a.features ? at : a.features - 1;
+                src[e] = second ? a.B2 + held * a.b2_stride : a.B + held * a.b_stride;
+            }
+            if constexpr (!kAny) src[e] += int64_t(first) * kSlice + ((lane % 8) ^ (lane / 8)) * 16;
         }
-        if constexpr (!kAny) src[e] += int64_t(first) * kSlice + ((lane % 8) ^ (lane / 8)) * 16;
     }
-    const int wi = w / T::kWn * (T::kI * 16), wj = T::kM + w % T::kWn * (T::kJ * 16);
+    const int wi = w / T::kWn * (T::kI * 16), wj = w % T::kWn * (T::kJ * 16);
     const auto fragment = [&](const char *in, int row, int piece) {
         return *reinterpret_cast<const Piece *>(in + row * kSlice + ((piece ^ (row & 7)) * 16));
     };
@@ -175,9 +222,19 @@ __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, t
     const auto read = [&](const char *in, int half) {
         const int piece = half * 4 + lane / 16;
 #pragma unroll
-        for (int j = 0; j < T::kJ; ++j) q[half][j] = fragment(in, wj + 16 * j + lane % 16, piece);
+        for (int j = 0; j < T::kJ; ++j) {
+            if constexpr (kColumns)
+                q[half][j] = column_fragment<E, T::kN * kEs>(in + T::kM * kSlice, wj / 16 + j, half);
+            else
+                q[half][j] = fragment(in, T::kM + wj + 16 * j + lane % 16, piece);
+        }
 #pragma unroll
-        for (int i = 0; i < T::kI; ++i) p[half][i] = fragment(in, wi + 16 * i + lane % 16, piece);
+        for (int i = 0; i < T::kI; ++i) {
+            if constexpr (kColumns)
+                p[half][i] = column_fragment<E, T::kM * kEs>(in, wi / 16 + i, half);
+            else
+                p[half][i] = fragment(in, wi + 16 * i + lane % 16, piece);
+        }
     };
     const auto multiply = [&](int half) {
 #pragma unroll
@@ -185,8 +242,6 @@ __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, t
 #pragma unroll
             for (int j = 0; j < T::kJ; ++j) acc[i][j] = Ops<E>::mul(p[half][i], q[half][j], acc[i][j]);
     };
-    // bytes of the row from this lane's piece of a slice on
-    const int64_t left0 = a.bytes - int64_t(first) * kSlice - ((lane % 8) ^ (lane / 8)) * 16;
 
     if constexpr (kAny) {
         Piece x[T::kEach];
@@ -219,10 +274,10 @@ __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, t
             // past the end the last slice again, into a buffer that nobody reads: every wait counts alike
             const int32_t k = slice < slices ? slice : slices - 1;
             char *to = s_mem + slice % T::kStages * T::kBuffer;
-            const bool zero = left0 - int64_t(k) * kSlice <= 0; // behind the row's end
 #pragma unroll
             for (int e = 0; e < T::kEach; ++e) {
-                const char *from = zero ? kZeros : src[e] + int64_t(k) * kSlice;
+                const bool zero = left[kColumns ? e : 0] - int64_t(k) * kSlice <= 0; // behind the end
+                const char *from = zero ? kZeros : src[e] + k * step[(e * T::kWaves + w) * 8 < T::kM ? 0 : 1];
                 __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
                                                  (__attribute__((address_space(3))) void *)(to + (e * T::kWaves + w) * 8 * kSlice),
                                                  16, 0, 0);
@@ -265,9 +320,11 @@ __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, t
 typedef Tile<256, 256, 2, 4, 2> TileLarge;
 constexpr int kRegion = 128 * kSlice;
 
-template <typename E, bool kDual, typename F> __device__ inline void large_tiles(const Product &a, F finish)
+template <typename E, Form kForm, typename F> __device__ inline void large_tiles(const Product &a, F finish)
 {
     extern __shared__ __align__(16) char s_mem[];
+    constexpr bool kDual = kForm == Form::kDual, kColumns = kForm == Form::kColumns;
+    constexpr int kEs = int(sizeof(E)), kRowPieces = 128 * kEs / 16; // kColumns: pieces of a region's row
     constexpr int kA0 = 0, kA1 = 1, kB0 = 2, kB1 = 3; // regions
     constexpr int kTogether = kDual ? 2 : 4;
     const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id(), group = w / 4, column = w % 4;
@@ -275,7 +332,10 @@ template <typename E, bool kDual, typename F> __device__ inline void large_tiles
     const int32_t slices = (first + a.per_split < a.slices ? first + a.per_split : a.slices) - first;
     const uint32_t tiles = uint32_t(a.down) * uint32_t(a.across);
     const int own = ((lane % 8) ^ (lane / 8)) * 16;
-    const int64_t left = a.bytes - int64_t(first) * kSlice - own; // of the row, from this lane's first piece on
+    const int row0 = (w * kWave + lane) / kRowPieces, piece0 = (w * kWave + lane) % kRowPieces; // kColumns: of the first of two
+    // of the row (of the column), from this lane's first piece on
+    const int64_t left = a.bytes - int64_t(first) * kSlice - (kColumns ? row0 * kEs : own);
+    const int64_t a_step = kColumns ? kSlice / kEs * a.a_stride : kSlice, b_step = kColumns ? kSlice / kEs * a.b_stride : kSlice;
 
     // Regions' rows: A's half h has the h-th 64 of each group's 128 points, B's the blocks 2 h and 2 h + 1 of each column of
     // waves.  This lane's pieces of the two groups of eight rows that the wave loads of each region.
@@ -284,6 +344,14 @@ template <typename E, bool kDual, typename F> __device__ inline void large_tiles
         const int h = r & 1;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
+            if constexpr (kColumns) {
+                const int row = row0 + e * (8 * kWave / kRowPieces), value = column_piece<E>(piece0, row) * (16 / kEs);
+                const int64_t at = r < kB0 ? int64_t(bi) * 256 + value / 64 * 128 + h * 64 + value % 64
+                                           : int64_t(bj) * 256 + value / 32 * 64 + h * 32 + value % 32;
+                const int64_t most = (r < kB0 ? a.rows : a.features) - 16 / kEs, stride = r < kB0 ? a.a_stride : a.b_stride;
+                src[r][e] = (r < kB0 ? a.A : a.B) + (int64_t(first) * (kSlice / kEs) + row) * stride + (at < most ? at : most) * kEs;
+                continue;
+            }
             const int row = (e * 8 + w) * 8 + lane / 8; // of the region
             if (r < kB0) {
                 const int64_t at = int64_t(bi) * 256 + row / 64 * 128 + h * 64 + row % 64;
@@ -302,10 +370,10 @@ template <typename E, bool kDual, typename F> __device__ inline void large_tiles
     // region r of a slice into the buffers of its parity
     const auto fetch = [&](int r, int32_t slice, int parity) {
         char *to = s_mem + parity * (4 * kRegion) + r * kRegion;
-        const bool zero = left - int64_t(slice) * kSlice <= 0; // behind the row's end
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const char *from = zero ? kZeros : src[r][e] + int64_t(slice) * kSlice;
+            const int64_t more = left - int64_t(slice) * kSlice - (kColumns ? e * (8 * kWave / kRowPieces) * kEs : 0);
+            const char *from = more <= 0 ? kZeros : src[r][e] + slice * (r < kB0 ? a_step : b_step); // zeros behind the end
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
                                              (__attribute__((address_space(3))) void *)(to + (e * 8 + w) * 8 * kSlice), 16, 0, 0);
         }
@@ -313,6 +381,14 @@ template <typename E, bool kDual, typename F> __device__ inline void large_tiles
     const int at0 = lane % 16 * kSlice + ((lane / 16) ^ (lane & 7)) * 16, at1 = at0 ^ 64; // the two halves of a slice
     Piece p[2][4], q[2][2][2]; // A's half that is under way; both of B's
     const auto read_a = [&](int h, int parity) {
+        if constexpr (kColumns) {
+            const char *in = s_mem + parity * (4 * kRegion) + h * kRegion;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[half][i] = column_fragment<E, 128 * kEs>(in + group * 64 * kEs, i, half);
+            return;
+        }
         const char *in = s_mem + parity * (4 * kRegion) + h * kRegion + group * 64 * kSlice;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -321,6 +397,14 @@ template <typename E, bool kDual, typename F> __device__ inline void large_tiles
         }
     };
     const auto read_b = [&](int h, int parity) {
+        if constexpr (kColumns) { // 32 of 64 columns that are stored in an order of their own
+            const char *in = s_mem + parity * (4 * kRegion) + (kB0 + h) * kRegion + column / 2 * 64 * kEs;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) q[h][half][j] = column_fragment<E, 128 * kEs>(in, column % 2 * 2 + j, half);
+            return;
+        }
         const char *in = s_mem + parity * (4 * kRegion) + (kB0 + h) * kRegion + column * 32 * kSlice;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -408,15 +492,15 @@ template <typename E, bool kDual, typename F> __device__ inline void large_tiles
 }
 
 // The tiles of a launch: finish(bi, bj, acc) takes each one's sums
-template <typename E, typename T, bool kDual, bool kAny, typename F> __device__ inline void each_tile(const Product &a, F finish)
+template <typename E, typename T, Form kForm, bool kAny, typename F> __device__ inline void each_tile(const Product &a, F finish)
 {
     if constexpr (std::is_same<T, TileLarge>::value) {
-        large_tiles<E, kDual>(a, finish);
+        large_tiles<E, kForm>(a, finish);
     } else {
         int32_t bi, bj;
         place(a, blockIdx.x, bi, bj);
         typename Ops<E>::Acc acc[T::kI][T::kJ] = {};
-        multiply_tile<E, T, kDual, kAny>(a, bi, bj, acc);
+        multiply_tile<E, T, kForm, kAny>(a, bi, bj, acc);
         finish(bi, bj, acc);
     }
 }
@@ -426,12 +510,13 @@ template <typename T> inline uint32_t blocks_of(uint32_t tiles)
 }
 
 // Points and features of a lane: f(point, feature, i, r) for row r of each block i of points, with the lane's first
-// feature, of kTogether consecutive ones: acc[i][..][r].
-template <typename T, bool kDual, typename F> __device__ inline void each_run(int32_t bi, int32_t bj, F f)
+// feature, of kTogether consecutive ones: acc[i][..][r].  kColumns: features 16 apart.
+template <typename T, Form kForm, typename F> __device__ inline void each_run(int32_t bi, int32_t bj, F f)
 {
-    constexpr int kTogether = kDual ? T::kJ / 2 : T::kJ;
+    constexpr int kTogether = kForm == Form::kDual ? T::kJ / 2 : T::kJ;
     const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id();
-    const int64_t feature = int64_t(bj) * (kDual ? T::kN / 2 : T::kN) + w % T::kWn * (16 * kTogether) + lane % 16 * kTogether;
+    const int64_t feature = int64_t(bj) * (kForm == Form::kDual ? T::kN / 2 : T::kN) + w % T::kWn * (16 * kTogether)
+                            + lane % 16 * (kForm == Form::kColumns ? 1 : kTogether);
     const int64_t point = int64_t(bi) * T::kM + w / T::kWn * (T::kI * 16) + lane / 16 * 4;
 #pragma unroll
     for (int i = 0; i < T::kI; ++i)
