@@ -182,7 +182,7 @@ int bhtsne_quantise_rows(const void *x, int64_t x_stride, int64_t n, int64_t d, 
 size_t bhtsne_linear_i8_workspace_size(int64_t n, int64_t d)
 {
     if (n < 0 || n > kMost || d < 1 || d > kLinearMaxDepth) return 0;
-    const size_t depth = (size_t(d) + 15) / 16 * 16;
+    const size_t depth = (size_t(d) + kLinearSlice - 1) / kLinearSlice * kLinearSlice;
     return (size_t(n) * 4 + 255) / 256 * 256 + (size_t(n) * depth + 255) / 256 * 256 + 256;
 }
 
@@ -221,7 +221,7 @@ int bhtsne_linear_i8(const void *x, int64_t x_stride, int x_type, const float *x
         q.x_stride = x_stride;
         q.scale = static_cast<float *>(workspace);
         q.q = static_cast<int8_t *>(workspace) + (size_t(n) * 4 + 255) / 256 * 256;
-        q.q_stride = (d + 15) / 16 * 16;
+        q.q_stride = q.pad = (d + kLinearSlice - 1) / kLinearSlice * kLinearSlice;
         q.n = n;
         q.d = d;
         q.type = Elem(x_type);
@@ -229,6 +229,7 @@ int bhtsne_linear_i8(const void *x, int64_t x_stride, int x_type, const float *x
         a.x = q.q;
         a.x_stride = q.q_stride;
         a.x_scale = q.scale;
+        a.padded = true;
     }
     launch_linear_i8(a, stream);
     return status();

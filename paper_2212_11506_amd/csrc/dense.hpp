@@ -38,6 +38,19 @@ struct DistilArgs {
 void launch_distil_loss(const DistilArgs &a, hipStream_t st);
 void launch_distil_loss_backward(const DistilArgs &a, hipStream_t st);
 
+// ------------------------------------------------------------------- products
+// Tiles that a product is made of, and the parts that its sums are shared out over
+enum class Side { kSmall = 64, kMiddle = 128, kLarge = 256 };
+struct Plan {
+    Side side;
+    int splits; // 1: none
+};
+constexpr int kMostSplits = 64;
+constexpr int64_t kMostPart = int64_t(1) << 29; // bytes of partial sums
+// rows x columns of output, of `slices` slices of K each; wide: fp32 operands.  may_split: partial sums have a place;
+// may_large: operands are aligned for tiles of 256.
+Plan plan_product(int64_t rows, int64_t columns, int64_t slices, bool wide, bool may_split, bool may_large);
+
 // ---------------------------------------------------------------- gated layers
 enum class Act { kSilu = 0, kGelu = 1 };
 
@@ -52,11 +65,12 @@ struct GatedArgs {
 void launch_gated_layer(const GatedArgs &a, hipStream_t st);
 
 // Backward: da and db side by side (n rows), x with padded rows, the weights transposed and side by side; partial sums of
-// the weights' gradients where they are shared out over the points.  Rows are padded to 16 bytes.
+// the weights' gradients where they are shared out over the points.
 constexpr int64_t pad16(int64_t count, int bytes) { return (count * bytes + 15) / 16 * 16 / bytes; }
 struct GatedBackLayout {
-    int64_t fp, dp; // padded f and d
-    int splits;     // of the sums over points
+    int64_t fp, dp;  // padded f and d: to whole slices, and to 16 bytes
+    int64_t np;      // points, padded to whole slices
+    Plan x, weights; // of dx, and of the weights' gradients
     size_t d, xp, wt, part, total;
 };
 GatedBackLayout make_gated_back_layout(int64_t n, int64_t d, int64_t f, Elem type);
@@ -73,6 +87,7 @@ struct GatedBackArgs {
 void launch_gated_layer_backward(const GatedBackArgs &a, hipStream_t st);
 
 // ---------------------------------------------------------- products of 8-bit integers
+constexpr int64_t kLinearSlice = 128;       // values of a slice of a row
 constexpr int64_t kLinearMaxDepth = 131071; // (-128)^2 so many times stays below 2^31
 
 struct QuantiseArgs {
@@ -81,6 +96,7 @@ struct QuantiseArgs {
     float *scale;
     int64_t x_stride, q_stride;
     int64_t n, d;
+    int64_t pad; // zeros behind each row's values, up to so many (<= q_stride)
     Elem type;
 };
 void launch_quantise_rows(const QuantiseArgs &a, hipStream_t st);
@@ -93,6 +109,7 @@ struct LinearArgs {
     int64_t x_stride, w_stride, out_stride;
     int64_t n, d, f;
     Elem type, bias_type;
+    bool padded; // x's rows go on with zeros to whole slices
 };
 void launch_linear_i8(const LinearArgs &a, hipStream_t st);
 

@@ -10,15 +10,14 @@
 // da and db are formed once, in fp32, and rounded to the inputs' type, as operands of
 // matrix instructions of that type: with bf16 their rounding adds to the output's own
 // (1.7e-3 each, 2.4e-3 together).  The sums over features and points are fp32.
+#include <cmath>
+
 #include "products.hpp"
 
 namespace bht {
 namespace {
 
 using namespace prod;
-
-typedef Tile<128, 128, 2, 2, 2> TileMiddle;
-typedef Tile<64, 64, 2, 2, 3> TileSmall;
 
 // ------------------------------------------------------------------ activations
 // fp32 with the library's exponential; 16-bit outputs do not show the instruction's last bits
@@ -78,11 +77,11 @@ struct GatedOut {
     bool vec_h, vec_a, vec_b;
 };
 
-template <typename E, typename T, bool kAny>
+template <typename E, typename T, bool kAny, Tail kTail>
 __global__ __launch_bounds__(T::kThreads) void gated_kernel(Product p, GatedOut o)
 {
     constexpr int kRun = T::kJ / 2; // features of a lane
-    each_tile<E, T, Form::kDual, kAny>(p, [&](int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ]) {
+    each_tile<E, T, Form::kDual, kAny, kTail>(p, [&](int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ]) {
         each_run<T, Form::kDual>(bi, bj, [&](int64_t point, int64_t feature, int i, int r) {
             if (point >= p.rows) return;
             float a[kRun], b[kRun], h[kRun];
@@ -132,7 +131,7 @@ Product gated_product(const GatedArgs &a, int64_t es)
     return p;
 }
 
-template <typename E, typename T, bool kAny> void run_gated(const GatedArgs &a, hipStream_t st)
+template <typename E, typename T, bool kAny, Tail kTail = Tail::kWhole> void run_gated(const GatedArgs &a, hipStream_t st)
 {
     constexpr int64_t kF = T::kN / 2;
     Product p = gated_product(a, int64_t(sizeof(E)));
@@ -147,7 +146,7 @@ template <typename E, typename T, bool kAny> void run_gated(const GatedArgs &a, 
         o.h = static_cast<E *>(a.h) + from * a.h_stride;
         o.a = a.a ? static_cast<E *>(a.a) + from * a.a_stride : nullptr;
         o.b = a.b ? static_cast<E *>(a.b) + from * a.b_stride : nullptr;
-        gated_kernel<E, T, kAny><<<blocks_of<T>(uint32_t(p.down) * uint32_t(p.across)), T::kThreads, lds, st>>>(p, o);
+        gated_kernel<E, T, kAny, kTail><<<blocks_of<T>(uint32_t(p.down) * uint32_t(p.across)), T::kThreads, lds, st>>>(p, o);
     }
 }
 
@@ -327,13 +326,14 @@ template <typename E> void run_gated_type(const GatedArgs &a, hipStream_t st)
         return a.d * es <= 64 ? run_gated_short<E, 1>(a, st) : run_gated_short<E, 2>(a, st);
     const bool any = !aligned16(a.x, a.x_stride * es) || !aligned16(a.gate, a.gate_stride * es) || !aligned16(a.up, a.up_stride * es)
                      || a.d * es % 16 != 0;
-    const bool large = tiles_of(a.n, a.f, 256, 128) >= kCus && a.d * es > kSlice, middle = tiles_of(a.n, a.f, 128, 64) >= kCus;
+    const bool near = a.x_stride * es <= kLargeStride && a.gate_stride * es <= kLargeStride && a.up_stride * es <= kLargeStride;
+    const Side side = plan_product(a.n, 2 * a.f, slices_of(a.d * es), es == 4, false, !any && near).side;
     if (any) {
-        if (large || middle) return run_gated<E, TileMiddle, true>(a, st);
+        if (side == Side::kMiddle) return run_gated<E, TileMiddle, true>(a, st);
         return run_gated<E, TileSmall, true>(a, st);
     }
-    if (large) return run_gated<E, TileLarge, false>(a, st);
-    if (middle) return run_gated<E, TileMiddle, false>(a, st);
+    if (side == Side::kLarge) return a.d * es % kSlice == 0 ? run_gated<E, TileLarge, false, Tail::kWhole>(a, st) : run_gated<E, TileLarge, false, Tail::kZeros>(a, st);
+    if (side == Side::kMiddle) return run_gated<E, TileMiddle, false>(a, st);
     run_gated<E, TileSmall, false>(a, st);
 }
 
@@ -347,7 +347,7 @@ struct Operands {
     char *d, *xp, *wt;
     int64_t dh_stride, a_stride, b_stride, x_stride, gate_stride, up_stride;
     int64_t n, features, f;
-    int64_t fp, dp;                 // padded to 16 bytes
+    int64_t np, fp, dp;             // padded
     uint32_t slope_blocks, weight_blocks, x_blocks;
     Act act;
     bool straight;                  // rows of f values of dh, a and b are whole pieces
@@ -368,10 +368,16 @@ template <typename E> __global__ __launch_bounds__(256) void gated_operands_kern
     __shared__ E s_t[kT][kT + 2];
     uint32_t b = blockIdx.x;
     if (b < g.slope_blocks) {
-        const int64_t each = g.fp / kV, total = g.n * each;
+        const int64_t each = g.fp / kV, total = g.np * each;
         for (int64_t t = int64_t(b) * 256 + threadIdx.x; t < total; t += int64_t(g.slope_blocks) * 256) {
             const int64_t row = total <= 0xffffffffll ? uint32_t(t) / uint32_t(each) : t / each, c = t - row * each;
             const int64_t bytes = g.f * kEs;
+            char *out = g.d + (row * 2 * g.fp + c * kV) * kEs;
+            if (row >= g.n || c * kV >= g.f) { // padding
+                *reinterpret_cast<Piece *>(out) = Piece{0, 0, 0, 0};
+                *reinterpret_cast<Piece *>(out + g.fp * kEs) = Piece{0, 0, 0, 0};
+                continue;
+            }
             const Values dh = __builtin_bit_cast(Values, row_piece<E>(g.dh, g.dh_stride * kEs, row, c, bytes, g.straight));
             const Values av = __builtin_bit_cast(Values, row_piece<E>(g.a, g.a_stride * kEs, row, c, bytes, g.straight));
             const Values bv = __builtin_bit_cast(Values, row_piece<E>(g.b, g.b_stride * kEs, row, c, bytes, g.straight));
@@ -384,7 +390,6 @@ template <typename E> __global__ __launch_bounds__(256) void gated_operands_kern
                 da.v[e] = E(d * float(bv.v[e]) * slope);
                 db.v[e] = E(d * value);
             }
-            char *out = g.d + (row * 2 * g.fp + c * kV) * kEs;
             *reinterpret_cast<Values *>(out) = da;
             *reinterpret_cast<Values *>(out + g.fp * kEs) = db;
         }
@@ -420,12 +425,13 @@ template <typename E> __global__ __launch_bounds__(256) void gated_operands_kern
 }
 
 // ------------------------------------------------------------------ backward: products
-// dx: rows as they are.  The weights' gradients: rows 0 .. f - 1 are dgate's, rows from `first2` on dup's; kPart: fp32 partial
-// sums of a split.
+// dx: rows as they are.  The weights' gradients: rows 0 .. f - 1 are dgate's, rows from `first2` on dup's (dx: none are).
+// kPart: fp32 partial sums of a split, of 2 f rows (dx: of n).
 struct BackOut {
     void *out, *out2;
     float *part;
-    int64_t stride, stride2, first2, f, features;
+    int64_t stride, stride2, first2, f, features; // f: rows of an output
+    int64_t part_rows;
     bool vec;
 };
 
@@ -433,7 +439,7 @@ template <typename E, typename T, Form kForm, bool kPart>
 __global__ __launch_bounds__(T::kThreads) void gated_back_kernel(Product p, BackOut o)
 {
     constexpr int kRun = T::kJ;
-    each_tile<E, T, kForm, false>(p, [&](int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ]) {
+    each_tile<E, T, kForm, false, Tail::kWhole>(p, [&](int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ]) {
         each_run<T, kForm>(bi, bj, [&](int64_t row, int64_t feature, int i, int r) {
             if (row >= p.rows) return;
             float v[kRun];
@@ -441,7 +447,10 @@ __global__ __launch_bounds__(T::kThreads) void gated_back_kernel(Product p, Back
             for (int e = 0; e < kRun; ++e) v[e] = acc[i][e][r];
             const int64_t count = o.features - feature; // p.features may be padded
             if constexpr (kForm == Form::kRows) {
-                store_run(static_cast<E *>(o.out) + row * o.stride + feature, v, count, o.vec);
+                if constexpr (kPart)
+                    store_run(o.part + (int64_t(blockIdx.y) * o.part_rows + row) * o.features + feature, v, count, o.vec);
+                else
+                    store_run(static_cast<E *>(o.out) + row * o.stride + feature, v, count, o.vec);
             } else {
                 const bool second = row >= o.first2;
                 const int64_t at = second ? row - o.first2 : row;
@@ -451,7 +460,7 @@ __global__ __launch_bounds__(T::kThreads) void gated_back_kernel(Product p, Back
                 for (int e = 0; e < kRun; ++e) {
                     if (16 * e >= count) continue;
                     if constexpr (kPart)
-                        o.part[(int64_t(blockIdx.y) * 2 * o.f + (second ? o.f : 0) + at) * o.features + feature + 16 * e] = v[e];
+                        o.part[(int64_t(blockIdx.y) * o.part_rows + (second ? o.f : 0) + at) * o.features + feature + 16 * e] = v[e];
                     else if (out)
                         out[at * (second ? o.stride2 : o.stride) + feature + 16 * e] = E(v[e]);
                 }
@@ -460,51 +469,79 @@ __global__ __launch_bounds__(T::kThreads) void gated_back_kernel(Product p, Back
     });
 }
 
-// The splits' sums in a fixed order, fp64: rows 0 .. 2 f - 1
-template <typename E> __global__ __launch_bounds__(256) void gated_join_kernel(BackOut o, int splits)
+// The splits' sums in a fixed order, fp64: two values a thread where rows have an even number
+template <typename E, int kV> __global__ __launch_bounds__(256) void gated_join_kernel(BackOut o, int splits)
 {
-    const int64_t features = o.features;
-    const int64_t total = 2 * o.f * features;
+    struct alignas(4 * kV) Part {
+        float v[kV];
+    };
+    struct alignas(sizeof(E) * kV) Out {
+        E v[kV];
+    };
+    const int64_t each = o.features / kV, total = o.part_rows * each;
+    const Part *part = reinterpret_cast<const Part *>(o.part);
     for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < total; e += int64_t(gridDim.x) * 256) {
-        double sum = 0.0;
-#pragma unroll 4
-        for (int s = 0; s < splits; ++s) sum += double(o.part[s * total + e]);
-        const int64_t row = total <= 0xffffffffll ? uint32_t(e) / uint32_t(features) : e / features, col = e - row * features;
+        double sum[kV] = {};
+#pragma unroll 8
+        for (int s = 0; s < splits; ++s) {
+            const Part x = part[s * total + e];
+#pragma unroll
+            for (int k = 0; k < kV; ++k) sum[k] += double(x.v[k]);
+        }
+        const int64_t row = total <= 0xffffffffll ? uint32_t(e) / uint32_t(each) : e / each, col = (e - row * each) * kV;
         const bool second = row >= o.f;
         E *out = static_cast<E *>(second ? o.out2 : o.out);
-        if (out) out[(second ? row - o.f : row) * (second ? o.stride2 : o.stride) + col] = E(float(sum));
+        if (!out) continue;
+        out += (second ? row - o.f : row) * (second ? o.stride2 : o.stride) + col;
+        Out y;
+#pragma unroll
+        for (int k = 0; k < kV; ++k) y.v[k] = E(float(sum[k]));
+        *reinterpret_cast<Out *>(out) = y;
     }
 }
 
 template <typename E, typename T, Form kForm>
 void run_back(Product p, const BackOut &o, int splits, hipStream_t st)
 {
-    p.slices = int32_t((p.bytes + kSlice - 1) / kSlice);
+    p.slices = int32_t(slices_of(p.bytes));
     p.per_split = (p.slices + splits - 1) / splits;
     p.across = int32_t((p.features + T::kN - 1) / T::kN);
     const size_t lds = size_t(T::kStages) * T::kBuffer;
     const int64_t all = p.rows, most = kMostTiles / p.across > 0 ? kMostTiles / p.across * T::kM : T::kM;
     const char *A = p.A;
-    for (int64_t from = 0; from < all; from += most) { // several launches only of kRows: the weights have fewer tiles
+    for (int64_t from = 0; from < all; from += most) { // several launches only of kRows without splits: others have fewer tiles
         p.A = A + from * p.a_stride;
         p.rows = all - from < most ? all - from : most;
         p.down = int32_t((p.rows + T::kM - 1) / T::kM);
         BackOut q = o;
         if (kForm == Form::kRows) q.out = static_cast<E *>(o.out) + from * o.stride;
         const dim3 grid(blocks_of<T>(uint32_t(p.down) * uint32_t(p.across)), uint32_t(splits));
-        if (kForm == Form::kColumns && splits > 1)
-            gated_back_kernel<E, T, kForm, kForm == Form::kColumns><<<grid, T::kThreads, lds, st>>>(p, q);
+        if (splits > 1)
+            gated_back_kernel<E, T, kForm, true><<<grid, T::kThreads, lds, st>>>(p, q);
         else
             gated_back_kernel<E, T, kForm, false><<<grid, T::kThreads, lds, st>>>(p, q);
     }
 }
 
-template <typename E, Form kForm> void run_back_tile(const Product &p, const BackOut &o, int splits, hipStream_t st)
+template <typename E, Form kForm> void run_back_plan(const Product &p, BackOut o, Plan plan, hipStream_t st)
 {
-    const int64_t slices = (p.bytes + kSlice - 1) / kSlice, last = slices - (splits - 1) * ((slices + splits - 1) / splits);
-    if (tiles_of(p.rows, p.features, 256, 256) * splits >= kCus && last >= 2) return run_back<E, TileLarge, kForm>(p, o, splits, st);
-    if (tiles_of(p.rows, p.features, 128, 128) * splits >= kCus) return run_back<E, TileMiddle, kForm>(p, o, splits, st);
-    run_back<E, TileSmall, kForm>(p, o, splits, st);
+    constexpr int64_t es = int64_t(sizeof(E));
+    o.part_rows = kForm == Form::kRows ? o.f : 2 * o.f;
+    const bool pairs = o.features % 2 == 0 && aligned_to(2 * es, o.out, o.stride * es) && aligned_to(2 * es, o.out2, o.stride2 * es);
+    if (plan.splits > 1) o.vec = o.features % 4 == 0; // of the partial sums
+    if (plan.side == Side::kLarge)
+        run_back<E, TileLarge, kForm>(p, o, plan.splits, st);
+    else if (plan.side == Side::kMiddle)
+        run_back<E, TileMiddle, kForm>(p, o, plan.splits, st);
+    else
+        run_back<E, TileSmall, kForm>(p, o, plan.splits, st);
+    if (plan.splits == 1) return;
+    const int64_t blocks = (o.part_rows * o.features / (pairs ? 2 : 1) + 255) / 256;
+    const uint32_t grid = uint32_t(blocks < 16384 ? blocks : 16384);
+    if (pairs)
+        gated_join_kernel<E, 2><<<grid, 256, 0, st>>>(o, plan.splits);
+    else
+        gated_join_kernel<E, 1><<<grid, 256, 0, st>>>(o, plan.splits);
 }
 
 template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st)
@@ -512,7 +549,7 @@ template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st
     const GatedBackLayout L = make_gated_back_layout(a.n, a.d, a.f, a.type);
     const int64_t es = int64_t(sizeof(E)), kV = 16 / es;
     char *ws = static_cast<char *>(a.ws);
-    const bool weights = a.dgate || a.dup, pad_x = weights && (!aligned16(a.x, a.x_stride * es) || a.d * es % 16 != 0);
+    const bool weights = a.dgate || a.dup, pad_x = weights && (!aligned16(a.x, a.x_stride * es) || a.d * es % 16 != 0 || a.x_stride * es > kLargeStride);
     Operands g = {};
     g.dh = a.dh;
     g.a = a.a;
@@ -529,6 +566,7 @@ template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st
     g.n = a.n;
     g.features = a.d;
     g.f = a.f;
+    g.np = L.np;
     g.fp = L.fp;
     g.dp = L.dp;
     g.d = ws + L.d;
@@ -540,7 +578,7 @@ template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st
         const int64_t blocks = (pieces + 255) / 256;
         return uint32_t(blocks < 16 * kCus ? blocks : 16 * kCus);
     };
-    g.slope_blocks = blocks_for(a.n * (L.fp / kV));
+    g.slope_blocks = blocks_for(L.np * (L.fp / kV));
     g.weight_blocks = a.dx ? uint32_t(2 * tiles_of(L.fp, a.d, kT, kT)) : 0;
     g.x_blocks = pad_x ? blocks_for(a.n * (L.dp / kV)) : 0;
     gated_operands_kernel<E><<<g.slope_blocks + g.weight_blocks + g.x_blocks, 256, 0, st>>>(g);
@@ -553,10 +591,13 @@ template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st
         p.features = a.d;
         BackOut o = {};
         o.out = a.dx;
-        o.features = a.d;
         o.stride = a.dx_stride;
+        o.first2 = int64_t(1) << 62;
+        o.f = a.n;
+        o.features = a.d;
+        o.part = reinterpret_cast<float *>(ws + L.part);
         o.vec = aligned16(a.dx, a.dx_stride * es);
-        run_back_tile<E, Form::kRows>(p, o, 1, st);
+        run_back_plan<E, Form::kRows>(p, o, L.x, st);
     }
     if (weights) {
         Product p = {};
@@ -576,11 +617,7 @@ template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st
         o.f = a.f;
         o.features = a.d;
         o.part = reinterpret_cast<float *>(ws + L.part);
-        run_back_tile<E, Form::kColumns>(p, o, L.splits, st);
-        if (L.splits > 1) {
-            const int64_t blocks = (2 * a.f * a.d + 255) / 256;
-            gated_join_kernel<E><<<uint32_t(blocks < 8192 ? blocks : 8192), 256, 0, st>>>(o, L.splits);
-        }
+        run_back_plan<E, Form::kColumns>(p, o, L.weights, st);
     }
 }
 
@@ -602,29 +639,63 @@ template <typename E> void run_gated_zero(const GatedBackArgs &a, hipStream_t st
 
 } // namespace
 
+// By the time of the busiest CU, in us, from what blocks of 8-bit products took a slice (fp32's matrix instructions take eight
+// times as long, which is all that counts there): a tile of 256 alone on a CU 1.0, and 1.42 with all CUs at it; one of 128
+// 0.73, two a CU 1.1; one of 64 0.32, three a CU 0.6, and so on by their number.  A tile's start and end take 9, 5 and 2.5;
+// joining partial sums a launch and their bytes.
+Plan plan_product(int64_t rows, int64_t columns, int64_t slices, bool wide, bool may_split, bool may_large)
+{
+    struct Kind {
+        Side side;
+        double base, each, fixed;
+        int at_once;
+    };
+    const Kind narrow_kinds[3] = {{Side::kSmall, 0.32, 0.00078, 2.5, 768}, {Side::kMiddle, 0.73, 0.00215, 5.0, 512}, {Side::kLarge, 1.0, 0.00555, 9.0, 256}};
+    const Kind wide_kinds[3] = {{Side::kSmall, 0.46, 0.0018, 2.5, 768}, {Side::kMiddle, 1.75, 0.0069, 5.0, 512}, {Side::kLarge, 6.9, 0.027, 9.0, 256}};
+    Plan best = {Side::kSmall, 1};
+    double least = INFINITY;
+    for (const Kind &k : wide ? wide_kinds : narrow_kinds) {
+        if (k.side == Side::kLarge && !may_large) continue;
+        const int64_t tiles = tiles_of(rows, columns, int(k.side), int(k.side));
+        for (int want = 1; want <= (may_split ? kMostSplits : 1); want += want < 8 ? 1 : want / 4) {
+            const int64_t per = (slices + want - 1) / want;
+            if (per < 1 || (want > 1 && per < 4)) break;
+            const int splits = int((slices + per - 1) / per);
+            if (k.side == Side::kLarge && (per < 2 || slices - (splits - 1) * per < 2)) continue;
+            if (splits > 1 && splits * rows * columns * 4 > kMostPart) break;
+            const int64_t blocks = tiles * splits, rounds = (blocks + k.at_once - 1) / k.at_once;
+            const double busy = k.each * double(blocks > k.at_once ? rounds * k.at_once : blocks);
+            const double t = k.fixed * double(rounds) + double(per) * (busy > k.base ? busy : k.base)
+                             + (splits > 1 ? 4.0 + double(splits) * double(rows) * double(columns) * 8.0 / 4.5e6 : 0.0);
+            if (t < least) {
+                least = t;
+                best = {k.side, splits};
+            }
+        }
+    }
+    return best;
+}
+
 GatedBackLayout make_gated_back_layout(int64_t n, int64_t d, int64_t f, Elem type)
 {
     const int es = elem_bytes(type);
     GatedBackLayout L = {};
-    L.fp = pad16(f, es);
+    L.fp = (f * es + kSlice - 1) / kSlice * kSlice / es;
+    L.np = (n * es + kSlice - 1) / kSlice * kSlice / es;
     L.dp = pad16(d, es);
-    // enough tiles of the weights' gradients for the chip, of eight slices at least each
-    const int64_t slices = (n * es + kSlice - 1) / kSlice;
-    const int64_t tiles = tiles_of(2 * L.fp, d, 128, 128), most = (slices + 7) / 8;
-    int64_t splits = (2 * kCus + tiles - 1) / tiles;
-    splits = splits < 1 ? 1 : splits < most ? splits : most < 1 ? 1 : most;
-    const int64_t each = (slices + splits - 1) / splits;
-    L.splits = int(each > 0 ? (slices + each - 1) / each : 1); // none of them empty
+    L.x = plan_product(n, d, slices_of(2 * L.fp * es), es == 4, true, true);
+    L.weights = plan_product(2 * L.fp, d, slices_of(n * es), es == 4, true, true);
     size_t at = 0;
     const auto take = [&](int64_t count, int bytes) {
         const size_t here = at;
         at += (size_t(count) * size_t(bytes) + 255) / 256 * 256;
         return here;
     };
-    L.d = take(n * 2 * L.fp, es);
+    L.d = take(L.np * 2 * L.fp, es);
     L.xp = take(n * L.dp, es);
     L.wt = take(d * 2 * L.fp, es);
-    L.part = take(L.splits > 1 ? L.splits * 2 * f * L.dp : 0, 4);
+    const int64_t x_part = L.x.splits > 1 ? L.x.splits * n * d : 0, w_part = L.weights.splits > 1 ? L.weights.splits * 2 * f * d : 0;
+    L.part = take(x_part > w_part ? x_part : w_part, 4);
     L.total = at > 0 ? at : 256;
     return L;
 }

@@ -59,6 +59,8 @@ template <typename E, int kThreads> __global__ __launch_bounds__(kThreads) void 
                 top = m <= top ? top : m < INFINITY ? m : INFINITY; // NaN counts as an infinity, which stays
             }
         };
+#pragma unroll
+        for (int e = 0; e < kRowValues; ++e) v[e] = 0.0f; // behind the row's end
         for (int64_t at = int64_t(threadIdx.x) * kRowValues; at < a.d; at += kThreads * kRowValues) take(at);
         top = wave_max(top);
         if constexpr (kWaves > 1) {
@@ -73,19 +75,20 @@ template <typename E, int kThreads> __global__ __launch_bounds__(kThreads) void 
         const float scale = finite ? top / 127.0f : NAN, inverse = 1.0f / scale;
         if (threadIdx.x == 0) a.scale[row] = scale;
         const bool aligned = (reinterpret_cast<uintptr_t>(q) & 15) == 0;
-        for (int64_t at = int64_t(threadIdx.x) * kRowValues; at < a.d; at += kThreads * kRowValues) {
-            if (a.d > kThreads * kRowValues) load_values(x, at, a.d, v);
+        const int64_t width = a.pad > a.d ? a.pad : a.d;
+        for (int64_t at = int64_t(threadIdx.x) * kRowValues; at < width; at += kThreads * kRowValues) {
+            if (width > kThreads * kRowValues) load_values(x, at, a.d, v);
             struct alignas(16) {
                 int8_t v[kRowValues];
             } out;
 #pragma unroll
             for (int e = 0; e < kRowValues; ++e) out.v[e] = int8_t(finite && scale > 0.0f ? quantise(v[e], scale, inverse) : 0);
-            if (aligned && at + kRowValues <= a.d) {
+            if (aligned && at + kRowValues <= width) {
                 *reinterpret_cast<Piece *>(q + at) = __builtin_bit_cast(Piece, out);
             } else {
 #pragma unroll
                 for (int e = 0; e < kRowValues; ++e)
-                    if (at + e < a.d) q[at + e] = out.v[e];
+                    if (at + e < width) q[at + e] = out.v[e];
             }
         }
     }
@@ -105,9 +108,6 @@ template <typename E> void run_quantise(const QuantiseArgs &a, hipStream_t st)
 }
 
 // ------------------------------------------------------------------ product
-typedef Tile<128, 128, 2, 2, 2> TileMiddle;
-typedef Tile<64, 64, 2, 2, 3> TileSmall;
-
 struct LinearOut {
     const float *x_scale, *w_scale;
     const void *bias;
@@ -116,11 +116,11 @@ struct LinearOut {
     bool wide_bias, vec;
 };
 
-template <typename E, typename T, bool kAny>
+template <typename E, typename T, bool kAny, Tail kTail>
 __global__ __launch_bounds__(T::kThreads) void linear8_kernel(Product p, LinearOut o)
 {
     constexpr int kRun = T::kJ;
-    each_tile<int8_t, T, Form::kRows, kAny>(p, [&](int32_t bi, int32_t bj, Ops<int8_t>::Acc (&acc)[T::kI][T::kJ]) {
+    each_tile<int8_t, T, Form::kRows, kAny, kTail>(p, [&](int32_t bi, int32_t bj, Ops<int8_t>::Acc (&acc)[T::kI][T::kJ]) {
         float scale[kRun], bias[kRun];
         each_run<T, Form::kRows>(bi, bj, [&](int64_t point, int64_t feature, int i, int r) {
             if (i == 0 && r == 0) {
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(T::kThreads) void linear8_kernel(Product p, LinearO
     });
 }
 
-template <typename E, typename T, bool kAny> void run_linear(const LinearArgs &a, hipStream_t st)
+template <typename E, typename T, bool kAny, Tail kTail = Tail::kWhole> void run_linear(const LinearArgs &a, hipStream_t st)
 {
     Product p = {};
     p.B = reinterpret_cast<const char *>(a.w);
@@ -174,22 +174,23 @@ template <typename E, typename T, bool kAny> void run_linear(const LinearArgs &a
         o.stride = a.out_stride;
         o.wide_bias = a.bias_type == Elem::kF32;
         o.vec = runs_aligned<E, T::kJ>(a.out, a.out_stride);
-        linear8_kernel<E, T, kAny><<<blocks_of<T>(uint32_t(p.down) * uint32_t(p.across)), T::kThreads, lds, st>>>(p, o);
+        linear8_kernel<E, T, kAny, kTail><<<blocks_of<T>(uint32_t(p.down) * uint32_t(p.across)), T::kThreads, lds, st>>>(p, o);
     }
 }
-
-int64_t tiles_of(int64_t rows, int64_t cols, int side) { return (rows + side - 1) / side * ((cols + side - 1) / side); }
 
 template <typename E> void run_linear_type(const LinearArgs &a, hipStream_t st)
 {
     const bool any = !aligned16(a.x, a.x_stride) || !aligned16(a.w, a.w_stride) || a.d % 16 != 0;
-    const bool large = tiles_of(a.n, a.f, 256) >= kCus && a.d > kSlice, middle = tiles_of(a.n, a.f, 128) >= kCus;
+    const Side side = plan_product(a.n, a.f, slices_of(a.d), false, false, !any && a.x_stride <= kLargeStride && a.w_stride <= kLargeStride).side;
     if (any) {
-        if (large || middle) return run_linear<E, TileMiddle, true>(a, st);
+        if (side == Side::kMiddle) return run_linear<E, TileMiddle, true>(a, st);
         return run_linear<E, TileSmall, true>(a, st);
     }
-    if (large) return run_linear<E, TileLarge, false>(a, st);
-    if (middle) return run_linear<E, TileMiddle, false>(a, st);
+    if (side == Side::kLarge) {
+        if (a.d % kSlice == 0) return run_linear<E, TileLarge, false, Tail::kWhole>(a, st);
+        return a.padded ? run_linear<E, TileLarge, false, Tail::kFirst>(a, st) : run_linear<E, TileLarge, false, Tail::kZeros>(a, st);
+    }
+    if (side == Side::kMiddle) return run_linear<E, TileMiddle, false>(a, st);
     run_linear<E, TileSmall, false>(a, st);
 }
 

@@ -75,6 +75,10 @@ template <int M, int N, int Wm, int Wn, int Stages> struct Tile {
     static_assert(kGroups % kWaves == 0 && M % (16 * Wm) == 0 && N % (16 * Wn) == 0, "even shares");
 };
 
+typedef Tile<256, 256, 2, 4, 2> TileLarge;
+typedef Tile<128, 128, 2, 2, 2> TileMiddle;
+typedef Tile<64, 64, 2, 2, 3> TileSmall;
+
 // How a product's operands lie.  kRows: C = A B^T of rows as above.  kDual: two such products of one A, by B and B2, whose
 // values a lane has side by side.  kColumns: C = A^T B, both summed over their rows (points): a slice is so many rows that
 // its columns are kSlice bytes high, and fragments are read across the rows (16-bit values by transposing LDS loads).
@@ -142,29 +146,37 @@ __device__ inline Piece inner_piece(const char *p)
     return v;
 }
 
-// Columns in LDS: `kPitch` bytes a row.  The pieces of a row are stored in an order that depends on the row, such that the
-// 16 columns of a block, in four rows next to each other, fall on different banks.
-template <typename E> __device__ inline int column_piece(int c, int row) { return c ^ (int(sizeof(E)) * (row & 3)); }
+// Columns in LDS: `kPitch` bytes a row.  The blocks of 16 columns of a row are stored in an order that depends on the row, such
+// that what 32 lanes take of a block (16 bits: rows 0 to 3 and 8 to 11 of it; 32 bits: four rows) falls on different banks.
+template <typename E, int kPitch> __device__ inline int column_turn(int row)
+{
+    if (sizeof(E) == 4) return row & 3;
+    return kPitch < 256 ? (row >> 1 & 1) | (row >> 3 & 1) << 1 : (row & 3) | (row >> 3 & 1) << 2;
+}
+// Piece c of a row's, and the place it is stored in, either way
+template <typename E, int kPitch> __device__ inline int column_piece(int c, int row) { return c ^ (int(sizeof(E)) * column_turn<E, kPitch>(row)); }
 
 // What a lane takes of columns 16 `block` .. in half a slice: a fragment's values for column lane % 16.  16 bits: a transposing
 // load gives 4 x 16 values of each 16 lanes, which name the four rows' pieces; two make the 8 rows of a lane.  32 bits: one by one.
-template <typename E, int kPitch> __device__ inline Piece column_fragment(const char *in, int block, int half)
+// column_place: the lane's part of the address (rows further down turn alike).
+template <typename E, int kPitch> __device__ inline int column_place(int block)
 {
-    const int lane = lane_id();
+    const int lane = lane_id(), row = sizeof(E) == 2 ? lane / 16 * 8 + lane % 16 / 4 : lane / 16;
+    return row * kPitch + (block ^ column_turn<E, kPitch>(row)) * (16 * int(sizeof(E))) + (sizeof(E) == 2 ? lane % 4 * 8 : lane % 16 * 4);
+}
+template <typename E, int kPitch> __device__ inline Piece column_fragment(const char *at, int half)
+{
     Piece v;
     if constexpr (sizeof(E) == 2) {
         typedef short Four __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) Four *Place;
-        const int q = lane % 16 / 4;
-        const char *at = in + (32 * half + lane / 16 * 8 + q) * kPitch + (block ^ q) * 32 + lane % 4 * 8;
-        const Four low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)at);
-        const Four high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(at + 4 * kPitch));
+        const Four low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(at + 32 * half * kPitch));
+        const Four high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(at + (32 * half + 4) * kPitch));
         const Four both[2] = {low, high};
         __builtin_memcpy(&v, both, 16);
     } else {
-        const char *at = in + (16 * half + lane / 16) * kPitch + (block ^ (lane / 16)) * 64 + lane % 16 * 4;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const int32_t *>(at + 4 * e * kPitch);
+        for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const int32_t *>(at + (16 * half + 4 * e) * kPitch);
     }
     return v;
 }
@@ -194,7 +206,8 @@ __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, t
         if constexpr (kColumns) {
             const int part = (e * T::kWaves + w) * 8 - (in_a ? 0 : T::kM); // eighths of a kilobyte before this one
             const int pieces = (in_a ? T::kM : T::kN) * kEs / 16, at = part * 8 + lane, row = at / pieces;
-            const int64_t column = int64_t(in_a ? bi * T::kM : bj * T::kN) * kEs + column_piece<E>(at % pieces, row) * 16;
+            const int turned = in_a ? column_piece<E, T::kM * kEs>(at % pieces, row) : column_piece<E, T::kN * kEs>(at % pieces, row);
+            const int64_t column = int64_t(in_a ? bi * T::kM : bj * T::kN) * kEs + turned * 16;
             const int64_t most = (in_a ? a.rows : a.features) * kEs - 16, stride = in_a ? a.a_stride : a.b_stride;
             src[e] = (in_a ? a.A : a.B) + (int64_t(first) * (kSlice / kEs) + row) * stride + (column < most ? column : most);
             left[e] = a.bytes - int64_t(first) * kSlice - row * kEs;
@@ -224,14 +237,14 @@ __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, t
 #pragma unroll
         for (int j = 0; j < T::kJ; ++j) {
             if constexpr (kColumns)
-                q[half][j] = column_fragment<E, T::kN * kEs>(in + T::kM * kSlice, wj / 16 + j, half);
+                q[half][j] = column_fragment<E, T::kN * kEs>(in + T::kM * kSlice + column_place<E, T::kN * kEs>(wj / 16 + j), half);
             else
                 q[half][j] = fragment(in, T::kM + wj + 16 * j + lane % 16, piece);
         }
 #pragma unroll
         for (int i = 0; i < T::kI; ++i) {
             if constexpr (kColumns)
-                p[half][i] = column_fragment<E, T::kM * kEs>(in, wi / 16 + i, half);
+                p[half][i] = column_fragment<E, T::kM * kEs>(in + column_place<E, T::kM * kEs>(wi / 16 + i), half);
             else
                 p[half][i] = fragment(in, wi + 16 * i + lane % 16, piece);
         }
@@ -317,10 +330,16 @@ __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, t
 //
 // A CU has one such block, which goes on to its next tile: the loads of the last two slices' steps are the next tile's
 // first, so they are under way while the outputs are formed and stored.  Rows have two slices at least.
-typedef Tile<256, 256, 2, 4, 2> TileLarge;
 constexpr int kRegion = 128 * kSlice;
+constexpr int64_t kLargeStride = int64_t(1) << 23; // bytes
+enum class Tail { kWhole, kFirst, kZeros };
 
-template <typename E, Form kForm, typename F> __device__ inline void large_tiles(const Product &a, F finish)
+//
+// Behind the end of K: kWhole, K ends with a slice (kColumns: A has rows of zeros up to there; B's last row is read again and
+// cut off in the fragments).  kFirst: A's rows go on with zeros, and B's last piece is read again (integers: zero times any).
+// kZeros: both operands' pieces are zeros, by a branch at every load, which costs 10 % (16384 x 8192 to 8192 bf16 3.23 ms a
+// pass, without it 2.92).
+template <typename E, Form kForm, Tail kTail, typename F> __device__ inline void large_tiles(const Product &a, F finish)
 {
     extern __shared__ __align__(16) char s_mem[];
     constexpr bool kDual = kForm == Form::kDual, kColumns = kForm == Form::kColumns;
@@ -338,55 +357,74 @@ template <typename E, Form kForm, typename F> __device__ inline void large_tiles
     const int64_t a_step = kColumns ? kSlice / kEs * a.a_stride : kSlice, b_step = kColumns ? kSlice / kEs * a.b_stride : kSlice;
 
     // Regions' rows: A's half h has the h-th 64 of each group's 128 points, B's the blocks 2 h and 2 h + 1 of each column of
-    // waves.  This lane's pieces of the two groups of eight rows that the wave loads of each region.
-    const char *src[4][2];
+    // waves.  This lane's pieces of the two kilobytes that the wave loads of each region: where they lie behind the tile's
+    // first value, in 32 bits (strides are kLargeStride at most), so that the addresses' high parts stay in scalar registers.
+    const char *base[4];
+    uint32_t off[4][2];
     const auto point = [&](int r, int32_t bi, int32_t bj) {
         const int h = r & 1;
+        const bool of_a = r < kB0, second = kDual && !of_a && h == 1;
+        const int64_t stride = of_a ? a.a_stride : second ? a.b2_stride : a.b_stride;
+        const int64_t tile = int64_t(of_a ? bi : bj) * (kDual && !of_a ? 128 : 256), most = (of_a ? a.rows : a.features) - tile; // values left
+        base[r] = (of_a ? a.A : second ? a.B2 : a.B) + (kColumns ? tile * kEs + int64_t(first) * (kSlice / kEs) * stride : tile * stride + int64_t(first) * kSlice);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             if constexpr (kColumns) {
-                const int row = row0 + e * (8 * kWave / kRowPieces), value = column_piece<E>(piece0, row) * (16 / kEs);
-                const int64_t at = r < kB0 ? int64_t(bi) * 256 + value / 64 * 128 + h * 64 + value % 64
-                                           : int64_t(bj) * 256 + value / 32 * 64 + h * 32 + value % 32;
-                const int64_t most = (r < kB0 ? a.rows : a.features) - 16 / kEs, stride = r < kB0 ? a.a_stride : a.b_stride;
-                src[r][e] = (r < kB0 ? a.A : a.B) + (int64_t(first) * (kSlice / kEs) + row) * stride + (at < most ? at : most) * kEs;
-                continue;
-            }
-            const int row = (e * 8 + w) * 8 + lane / 8; // of the region
-            if (r < kB0) {
-                const int64_t at = int64_t(bi) * 256 + row / 64 * 128 + h * 64 + row % 64;
-                src[r][e] = a.A + (at < a.rows ? at : a.rows - 1) * a.a_stride;
+                const int row = row0 + e * (8 * kWave / kRowPieces), value = column_piece<E, 128 * kEs>(piece0, row) * (16 / kEs);
+                const int at = of_a ? value / 64 * 128 + h * 64 + value % 64 : value / 32 * 64 + h * 32 + value % 32, last = 16 / kEs;
+                off[r][e] = uint32_t(row) * uint32_t(stride) + uint32_t(at + last <= most ? at : int(most) - last) * kEs;
             } else {
-                const int block = 2 * h + row % 32 / 16, i = row % 16;
-                const bool second = kDual && h == 1;
-                const int64_t at = int64_t(bj) * (64 * kTogether) + row / 32 * (16 * kTogether) + i * kTogether
-                                   + (second ? block - 2 : block);
-                const int64_t held = at < a.features ? at : a.features - 1;
-                src[r][e] = second ? a.B2 + held * a.b2_stride : a.B + held * a.b_stride;
+                const int row = (e * 8 + w) * 8 + lane / 8, i = row % 16, block = row % 32 / 16; // of the region
+                const int at = of_a ? row / 64 * 128 + h * 64 + row % 64
+                                    : row / 32 * (16 * kTogether) + i * kTogether + (second ? block : 2 * h + block);
+                off[r][e] = uint32_t(at < most ? at : int(most) - 1) * uint32_t(stride) + uint32_t(own);
             }
-            src[r][e] += int64_t(first) * kSlice + own;
         }
     };
     // region r of a slice into the buffers of its parity
+    const int32_t rest = int32_t(a.bytes - int64_t(first) * kSlice < (int64_t(1) << 30) ? a.bytes - int64_t(first) * kSlice : int64_t(1) << 30);
     const auto fetch = [&](int r, int32_t slice, int parity) {
         char *to = s_mem + parity * (4 * kRegion) + r * kRegion;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int64_t more = left - int64_t(slice) * kSlice - (kColumns ? e * (8 * kWave / kRowPieces) * kEs : 0);
-            const char *from = more <= 0 ? kZeros : src[r][e] + slice * (r < kB0 ? a_step : b_step); // zeros behind the end
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+        const char *from = base[r] + slice * (r < kB0 ? a_step : b_step);
+        const auto load = [&](const char *p, int e) {
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)p,
                                              (__attribute__((address_space(3))) void *)(to + (e * 8 + w) * 8 * kSlice), 16, 0, 0);
+        };
+        if (kTail == Tail::kZeros && int64_t(slice + 1) * kSlice > int64_t(rest)) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) load(left - int64_t(slice) * kSlice <= 0 ? kZeros : from + off[r][e], e);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                uint32_t o = off[r][e];
+                if constexpr (kTail == Tail::kFirst) {
+                    const int over = slice * kSlice + own - (rest - 16); // bytes behind the last piece
+                    if (r >= kB0) o -= uint32_t(over > 0 ? over : 0);
+                }
+                if constexpr (kColumns) {
+                    const int over = (slice * kSlice - rest) / kEs + 1 + row0 + e * (8 * kWave / kRowPieces); // rows behind the last one
+                    if (r >= kB0) o -= uint32_t(over > 0 ? over : 0) * uint32_t(a.b_stride);
+                }
+                load(from + o, e);
+            }
         }
     };
     const int at0 = lane % 16 * kSlice + ((lane / 16) ^ (lane & 7)) * 16, at1 = at0 ^ 64; // the two halves of a slice
     Piece p[2][4], q[2][2][2]; // A's half that is under way; both of B's
+    // kColumns: the lane's places in this slice's buffers
+    const char *in_a[4], *in_b[2];
+    if constexpr (kColumns) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) in_a[i] = s_mem + column_place<E, 128 * kEs>(group * 4 + i);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) in_b[j] = s_mem + column_place<E, 128 * kEs>(column * 2 + j);
+    }
     const auto read_a = [&](int h, int parity) {
         if constexpr (kColumns) {
-            const char *in = s_mem + parity * (4 * kRegion) + h * kRegion;
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[half][i] = column_fragment<E, 128 * kEs>(in + group * 64 * kEs, i, half);
+                for (int i = 0; i < 4; ++i) p[half][i] = column_fragment<E, 128 * kEs>(in_a[i] + h * kRegion, half);
             return;
         }
         const char *in = s_mem + parity * (4 * kRegion) + h * kRegion + group * 64 * kSlice;
@@ -396,13 +434,12 @@ template <typename E, Form kForm, typename F> __device__ inline void large_tiles
             p[1][i] = *reinterpret_cast<const Piece *>(in + i * 16 * kSlice + at1);
         }
     };
-    const auto read_b = [&](int h, int parity) {
-        if constexpr (kColumns) { // 32 of 64 columns that are stored in an order of their own
-            const char *in = s_mem + parity * (4 * kRegion) + (kB0 + h) * kRegion + column / 2 * 64 * kEs;
+    const auto read_b = [&](int h, int parity, bool ahead = false) {
+        if constexpr (kColumns) {
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) q[h][half][j] = column_fragment<E, 128 * kEs>(in, column % 2 * 2 + j, half);
+                for (int j = 0; j < 2; ++j) q[h][half][j] = column_fragment<E, 128 * kEs>(in_b[j] + (ahead ? (parity ? 4 : -4) * kRegion : 0) + (kB0 + h) * kRegion, half);
             return;
         }
         const char *in = s_mem + parity * (4 * kRegion) + (kB0 + h) * kRegion + column * 32 * kSlice;
@@ -414,10 +451,28 @@ template <typename E, Form kForm, typename F> __device__ inline void large_tiles
     };
     typename Ops<E>::Acc acc[8][4];
     // the barrier between a step's parts, with the wait for the loads that the next step reads; and the part that multiplies
-    const auto multiply = [&](int ha, int hb) {
+    const auto multiply = [&](int ha, int hb, int32_t slice) {
         asm volatile("s_waitcnt vmcnt(10)\n\ts_barrier" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if constexpr (kColumns) {
+            const int rows = (rest - slice * kSlice) / kEs; // of this slice
+            if (rows < kSlice / kEs) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if constexpr (kEs == 2) {
+                                const int more = rows - 32 * half - lane / 16 * 8 - 2 * e; // of two
+                                q[hb][half][j][e] = more >= 2 ? q[hb][half][j][e] : more == 1 ? q[hb][half][j][e] & 0xffff : 0;
+                            } else {
+                                q[hb][half][j][e] = 16 * half + 4 * e + lane / 16 < rows ? q[hb][half][j][e] : 0;
+                            }
+                        }
+            }
+        }
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -464,7 +519,7 @@ template <typename E, Form kForm, typename F> __device__ inline void large_tiles
             if (slice == slices - 1) point(kA1, ni, nj);
             read_a(0, parity);
             fetch(kA1, one, parity ^ 1);
-            multiply(0, 0);
+            multiply(0, 0, slice);
             if (slice == slices - 2) {
                 point(kB0, ni, nj);
                 point(kA0, ni, nj);
@@ -472,13 +527,20 @@ template <typename E, Form kForm, typename F> __device__ inline void large_tiles
             }
             read_b(1, parity);
             fetch(kB0, two, parity);
-            multiply(0, 1);
+            multiply(0, 1, slice);
             read_a(1, parity);
             fetch(kA0, two, parity);
-            multiply(1, 0);
-            read_b(0, parity ^ 1); // behind the tile's last slice: the next one's, read again
+            multiply(1, 0, slice);
+            read_b(0, parity ^ 1, true); // behind the tile's last slice: the next one's, read again
             fetch(kB1, two, parity);
-            multiply(1, 1);
+            multiply(1, 1, slice);
+            if constexpr (kColumns) {
+                const int flip = parity ? -4 * kRegion : 4 * kRegion;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) in_a[i] += flip;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) in_b[j] += flip;
+            }
         }
         if (group == 0) asm volatile("s_barrier" ::: "memory"); // the groups meet, so that both form their outputs at once
         __builtin_amdgcn_sched_barrier(0);
@@ -492,10 +554,10 @@ template <typename E, Form kForm, typename F> __device__ inline void large_tiles
 }
 
 // The tiles of a launch: finish(bi, bj, acc) takes each one's sums
-template <typename E, typename T, Form kForm, bool kAny, typename F> __device__ inline void each_tile(const Product &a, F finish)
+template <typename E, typename T, Form kForm, bool kAny, Tail kTail, typename F> __device__ inline void each_tile(const Product &a, F finish)
 {
     if constexpr (std::is_same<T, TileLarge>::value) {
-        large_tiles<E, kForm>(a, finish);
+        large_tiles<E, kForm, kTail>(a, finish);
     } else {
         int32_t bi, bj;
         place(a, blockIdx.x, bi, bj);
@@ -557,6 +619,8 @@ template <typename E, int N> inline bool runs_aligned(const void *p, int64_t str
     constexpr int kBytes = int(sizeof(E)) * N;
     return aligned_to(kBytes < 16 ? kBytes : 16, p, stride * int64_t(sizeof(E)));
 }
+
+inline int64_t slices_of(int64_t bytes) { return (bytes + kSlice - 1) / kSlice; }
 
 // A launch takes at most kMostTiles tiles: rows are cut into several launches beyond
 constexpr int64_t kMostTiles = int64_t(1) << 22;
