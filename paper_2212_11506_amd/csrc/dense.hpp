@@ -70,6 +70,7 @@ constexpr int64_t pad16(int64_t count, int bytes) { return (count * bytes + 15) 
 struct GatedBackLayout {
     int64_t fp, dp;  // padded f and d: to whole slices, and to 16 bytes
     int64_t np;      // points, padded to whole slices
+    int64_t ld;      // values from row to row of da and db
     Plan x, weights; // of dx, and of the weights' gradients
     size_t d, xp, wt, part, total;
 };

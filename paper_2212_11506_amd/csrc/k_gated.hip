@@ -347,7 +347,7 @@ struct Operands {
     char *d, *xp, *wt;
     int64_t dh_stride, a_stride, b_stride, x_stride, gate_stride, up_stride;
     int64_t n, features, f;
-    int64_t np, fp, dp;             // padded
+    int64_t np, fp, dp, ld;         // padded; from row to row of d
     uint32_t slope_blocks, weight_blocks, x_blocks;
     Act act;
     bool straight;                  // rows of f values of dh, a and b are whole pieces
@@ -372,7 +372,7 @@ template <typename E> __global__ __launch_bounds__(256) void gated_operands_kern
         for (int64_t t = int64_t(b) * 256 + threadIdx.x; t < total; t += int64_t(g.slope_blocks) * 256) {
             const int64_t row = total <= 0xffffffffll ? uint32_t(t) / uint32_t(each) : t / each, c = t - row * each;
             const int64_t bytes = g.f * kEs;
-            char *out = g.d + (row * 2 * g.fp + c * kV) * kEs;
+            char *out = g.d + (row * g.ld + c * kV) * kEs;
             if (row >= g.n || c * kV >= g.f) { // padding
                 *reinterpret_cast<Piece *>(out) = Piece{0, 0, 0, 0};
                 *reinterpret_cast<Piece *>(out + g.fp * kEs) = Piece{0, 0, 0, 0};
@@ -567,6 +567,7 @@ template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st
     g.features = a.d;
     g.f = a.f;
     g.np = L.np;
+    g.ld = L.ld;
     g.fp = L.fp;
     g.dp = L.dp;
     g.d = ws + L.d;
@@ -586,7 +587,8 @@ template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st
         Product p = {};
         p.A = g.d;
         p.B = g.wt;
-        p.a_stride = p.b_stride = p.bytes = 2 * L.fp * es;
+        p.a_stride = L.ld * es;
+        p.b_stride = p.bytes = 2 * L.fp * es;
         p.rows = a.n;
         p.features = a.d;
         BackOut o = {};
@@ -603,7 +605,7 @@ template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st
         Product p = {};
         p.A = g.d;
         p.B = pad_x ? g.xp : static_cast<const char *>(a.x);
-        p.a_stride = 2 * L.fp * es;
+        p.a_stride = L.ld * es;
         p.b_stride = (pad_x ? L.dp : a.x_stride) * es;
         p.bytes = a.n * es;
         p.rows = 2 * L.fp;
@@ -691,7 +693,8 @@ GatedBackLayout make_gated_back_layout(int64_t n, int64_t d, int64_t f, Elem typ
         at += (size_t(count) * size_t(bytes) + 255) / 256 * 256;
         return here;
     };
-    L.d = take(L.np * 2 * L.fp, es);
+    L.ld = 2 * L.fp + 256 / es; // rows side by side in other channels of the caches
+    L.d = take(L.np * L.ld, es);
     L.xp = take(n * L.dp, es);
     L.wt = take(d * 2 * L.fp, es);
     const int64_t x_part = L.x.splits > 1 ? L.x.splits * n * d : 0, w_part = L.weights.splits > 1 ? L.weights.splits * 2 * f * d : 0;

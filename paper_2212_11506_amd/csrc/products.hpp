@@ -164,21 +164,94 @@ template <typename E, int kPitch> __device__ inline int column_place(int block)
     const int lane = lane_id(), row = sizeof(E) == 2 ? lane / 16 * 8 + lane % 16 / 4 : lane / 16;
     return row * kPitch + (block ^ column_turn<E, kPitch>(row)) * (16 * int(sizeof(E))) + (sizeof(E) == 2 ? lane % 4 * 8 : lane % 16 * 4);
 }
-template <typename E, int kPitch> __device__ inline Piece column_fragment(const char *at, int half)
+// N of them (2 or 4), kOffset bytes behind `at`.  The transposing loads are written out, with their wait: before the builtin
+// the compiler waits for every load into LDS that is under way, whatever it fills (16384 x 512 to 2048 108 us, 2.3 a slice).
+template <typename E, int kPitch, int kOffset, int N> __device__ inline void column_fragments(const char *const (&at)[N], Piece (&v)[N])
 {
-    Piece v;
+    static_assert(N == 2 || N == 4, "written out for these");
     if constexpr (sizeof(E) == 2) {
-        typedef short Four __attribute__((ext_vector_type(4)));
-        typedef __attribute__((address_space(3))) Four *Place;
-        const Four low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(at + 32 * half * kPitch));
-        const Four high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(at + (32 * half + 4) * kPitch));
-        const Four both[2] = {low, high};
-        __builtin_memcpy(&v, both, 16);
+        typedef int32_t Two __attribute__((ext_vector_type(2)));
+        typedef const __attribute__((address_space(3))) char *Place;
+        Two low[N], high[N];
+        if constexpr (N == 4) {
+            asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%12\n\t"
+                         "ds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+                         "ds_read_b64_tr_b16 %2, %9 offset:%12\n\t"
+                         "ds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+                         "ds_read_b64_tr_b16 %4, %10 offset:%12\n\t"
+                         "ds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+                         "ds_read_b64_tr_b16 %6, %11 offset:%12\n\t"
+                         "ds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+                         "s_waitcnt lgkmcnt(0)"
+                         : "=&v"(low[0]), "=&v"(high[0]), "=&v"(low[1]), "=&v"(high[1]), "=&v"(low[2]), "=&v"(high[2]), "=&v"(low[3]), "=&v"(high[3])
+                         : "v"((Place)at[0]), "v"((Place)at[1]), "v"((Place)at[2]), "v"((Place)at[3]), "n"(kOffset), "n"(kOffset + 4 * kPitch)
+                         : "memory");
+        } else {
+            asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%6\n\t"
+                         "ds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
+                         "ds_read_b64_tr_b16 %2, %5 offset:%6\n\t"
+                         "ds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+                         "s_waitcnt lgkmcnt(0)"
+                         : "=&v"(low[0]), "=&v"(high[0]), "=&v"(low[1]), "=&v"(high[1])
+                         : "v"((Place)at[0]), "v"((Place)at[1]), "n"(kOffset), "n"(kOffset + 4 * kPitch)
+                         : "memory");
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = Piece{low[i][0], low[i][1], high[i][0], high[i][1]};
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const int32_t *>(at + (16 * half + 4 * e) * kPitch);
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[i][e] = *reinterpret_cast<const int32_t *>(at[i] + kOffset + 4 * e * kPitch);
     }
-    return v;
+}
+// ... and both halves of a slice, with one wait
+template <typename E, int kPitch, int kOffset, int N> __device__ inline void column_slices(const char *const (&at)[N], Piece (&v)[2][N])
+{
+    static_assert(N == 2 || N == 4, "written out for these");
+    constexpr int kHalf = (sizeof(E) == 2 ? 32 : 16) * kPitch;
+    if constexpr (sizeof(E) == 2 && N == 4) {
+        typedef int32_t Two __attribute__((ext_vector_type(2)));
+        typedef const __attribute__((address_space(3))) char *Place;
+        Two x[16];
+        asm volatile("ds_read_b64_tr_b16 %0, %16 offset:%20\n\t"
+                     "ds_read_b64_tr_b16 %1, %16 offset:%21\n\t"
+                     "ds_read_b64_tr_b16 %2, %17 offset:%20\n\t"
+                     "ds_read_b64_tr_b16 %3, %17 offset:%21\n\t"
+                     "ds_read_b64_tr_b16 %4, %18 offset:%20\n\t"
+                     "ds_read_b64_tr_b16 %5, %18 offset:%21\n\t"
+                     "ds_read_b64_tr_b16 %6, %19 offset:%20\n\t"
+                     "ds_read_b64_tr_b16 %7, %19 offset:%21\n\t"
+                     "ds_read_b64_tr_b16 %8, %16 offset:%22\n\t"
+                     "ds_read_b64_tr_b16 %9, %16 offset:%23\n\t"
+                     "ds_read_b64_tr_b16 %10, %17 offset:%22\n\t"
+                     "ds_read_b64_tr_b16 %11, %17 offset:%23\n\t"
+                     "ds_read_b64_tr_b16 %12, %18 offset:%22\n\t"
+                     "ds_read_b64_tr_b16 %13, %18 offset:%23\n\t"
+                     "ds_read_b64_tr_b16 %14, %19 offset:%22\n\t"
+                     "ds_read_b64_tr_b16 %15, %19 offset:%23\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7]), "=&v"(x[8]),
+                       "=&v"(x[9]), "=&v"(x[10]), "=&v"(x[11]), "=&v"(x[12]), "=&v"(x[13]), "=&v"(x[14]), "=&v"(x[15])
+                     : "v"((Place)at[0]), "v"((Place)at[1]), "v"((Place)at[2]), "v"((Place)at[3]), "n"(kOffset), "n"(kOffset + 4 * kPitch),
+                       "n"(kOffset + kHalf), "n"(kOffset + kHalf + 4 * kPitch)
+                     : "memory");
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[h][i] = Piece{x[8 * h + 2 * i][0], x[8 * h + 2 * i][1], x[8 * h + 2 * i + 1][0], x[8 * h + 2 * i + 1][1]};
+    } else if constexpr (sizeof(E) == 2) {
+        const char *const four[4] = {at[0], at[1], at[0] + kHalf, at[1] + kHalf};
+        Piece x[4];
+        column_fragments<E, kPitch, kOffset>(four, x);
+        v[0][0] = x[0];
+        v[0][1] = x[1];
+        v[1][0] = x[2];
+        v[1][1] = x[3];
+    } else {
+        column_fragments<E, kPitch, kOffset>(at, v[0]);
+        column_fragments<E, kPitch, kOffset + kHalf>(at, v[1]);
+    }
 }
 
 // A wave's blocks: acc[i][j] holds points 16 i .. against rows 16 j .. of the wave's part of B.  kDual: the first half of
@@ -232,22 +305,30 @@ __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, t
         return *reinterpret_cast<const Piece *>(in + row * kSlice + ((piece ^ (row & 7)) * 16));
     };
     Piece p[2][T::kI], q[2][T::kJ];
+    int own_a[T::kI], own_b[T::kJ]; // kColumns: the lane's places
+    if constexpr (kColumns) {
+#pragma unroll
+        for (int i = 0; i < T::kI; ++i) own_a[i] = column_place<E, T::kM * kEs>(wi / 16 + i);
+#pragma unroll
+        for (int j = 0; j < T::kJ; ++j) own_b[j] = T::kM * kSlice + column_place<E, T::kN * kEs>(wj / 16 + j);
+    }
     const auto read = [&](const char *in, int half) {
+        if constexpr (kColumns) {
+            const char *a_at[T::kI], *b_at[T::kJ];
+            constexpr int kRows = kSlice / kEs / 2;
+#pragma unroll
+            for (int i = 0; i < T::kI; ++i) a_at[i] = in + own_a[i] + half * kRows * T::kM * kEs;
+#pragma unroll
+            for (int j = 0; j < T::kJ; ++j) b_at[j] = in + own_b[j] + half * kRows * T::kN * kEs;
+            column_fragments<E, T::kN * kEs, 0>(b_at, q[half]);
+            column_fragments<E, T::kM * kEs, 0>(a_at, p[half]);
+            return;
+        }
         const int piece = half * 4 + lane / 16;
 #pragma unroll
-        for (int j = 0; j < T::kJ; ++j) {
-            if constexpr (kColumns)
-                q[half][j] = column_fragment<E, T::kN * kEs>(in + T::kM * kSlice + column_place<E, T::kN * kEs>(wj / 16 + j), half);
-            else
-                q[half][j] = fragment(in, T::kM + wj + 16 * j + lane % 16, piece);
-        }
+        for (int j = 0; j < T::kJ; ++j) q[half][j] = fragment(in, T::kM + wj + 16 * j + lane % 16, piece);
 #pragma unroll
-        for (int i = 0; i < T::kI; ++i) {
-            if constexpr (kColumns)
-                p[half][i] = column_fragment<E, T::kM * kEs>(in + column_place<E, T::kM * kEs>(wi / 16 + i), half);
-            else
-                p[half][i] = fragment(in, wi + 16 * i + lane % 16, piece);
-        }
+        for (int i = 0; i < T::kI; ++i) p[half][i] = fragment(in, wi + 16 * i + lane % 16, piece);
     };
     const auto multiply = [&](int half) {
 #pragma unroll
@@ -421,10 +502,10 @@ template <typename E, Form kForm, Tail kTail, typename F> __device__ inline void
     }
     const auto read_a = [&](int h, int parity) {
         if constexpr (kColumns) {
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[half][i] = column_fragment<E, 128 * kEs>(in_a[i] + h * kRegion, half);
+            if (h)
+                column_slices<E, 128 * kEs, kRegion>(in_a, p);
+            else
+                column_slices<E, 128 * kEs, 0>(in_a, p);
             return;
         }
         const char *in = s_mem + parity * (4 * kRegion) + h * kRegion + group * 64 * kSlice;
@@ -436,10 +517,12 @@ template <typename E, Form kForm, Tail kTail, typename F> __device__ inline void
     };
     const auto read_b = [&](int h, int parity, bool ahead = false) {
         if constexpr (kColumns) {
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) q[h][half][j] = column_fragment<E, 128 * kEs>(in_b[j] + (ahead ? (parity ? 4 : -4) * kRegion : 0) + (kB0 + h) * kRegion, half);
+            const int by = ahead ? (parity ? 4 : -4) * kRegion : 0;
+            const char *const at[2] = {in_b[0] + by, in_b[1] + by};
+            if (h)
+                column_slices<E, 128 * kEs, kB1 * kRegion>(at, q[1]);
+            else
+                column_slices<E, 128 * kEs, kB0 * kRegion>(at, q[0]);
             return;
         }
         const char *in = s_mem + parity * (4 * kRegion) + (kB0 + h) * kRegion + column * 32 * kSlice;
