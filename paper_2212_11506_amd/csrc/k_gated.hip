@@ -367,7 +367,8 @@ template <typename E> __global__ __launch_bounds__(256) void gated_operands_kern
     };
     __shared__ E s_t[kT][kT + 2];
     uint32_t b = blockIdx.x;
-    if (b < g.slope_blocks) {
+    if (b >= g.weight_blocks && b < g.weight_blocks + g.slope_blocks) {
+        b -= g.weight_blocks;
         const int64_t each = g.fp / kV, total = g.np * each;
         for (int64_t t = int64_t(b) * 256 + threadIdx.x; t < total; t += int64_t(g.slope_blocks) * 256) {
             const int64_t row = total <= 0xffffffffll ? uint32_t(t) / uint32_t(each) : t / each, c = t - row * each;
@@ -395,31 +396,35 @@ template <typename E> __global__ __launch_bounds__(256) void gated_operands_kern
         }
         return;
     }
-    b -= g.slope_blocks;
     if (b < g.weight_blocks) {
         const uint32_t across = uint32_t((g.features + kT - 1) / kT), down = uint32_t((g.fp + kT - 1) / kT);
         const bool second = b >= across * down;
         if (second) b -= across * down;
         const E *in = static_cast<const E *>(second ? g.up : g.gate);
         const int64_t stride = second ? g.up_stride : g.gate_stride, r0 = int64_t(b / across) * kT, c0 = int64_t(b % across) * kT;
-        for (int s = int(threadIdx.x); s < kT * kT; s += 256) {
-            const int row = s / kT, col = s % kT;
-            const bool there = r0 + row < g.f && c0 + col < g.features;
-            const E v = in[there ? (r0 + row) * stride + c0 + col : 0];
-            s_t[row][col] = there ? v : E(0.0f);
+        constexpr int kEach = kT * kT / 256;
+        const int col = int(threadIdx.x) % kT, row = int(threadIdx.x) / kT; // every fourth row; all loads asked for at once
+        E v[kEach];
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            const int64_t r = r0 + row + q * (256 / kT), c = c0 + col;
+            v[q] = in[(r < g.f ? r : g.f - 1) * stride + (c < g.features ? c : g.features - 1)];
         }
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) s_t[row + q * (256 / kT)][col] = r0 + row + q * (256 / kT) < g.f ? v[q] : E(0.0f);
         __syncthreads();
         E *out = reinterpret_cast<E *>(g.wt) + (second ? g.fp : 0);
-        for (int s = int(threadIdx.x); s < kT * kT; s += 256) {
-            const int col = s / kT, row = s % kT;
-            if (r0 + row < g.fp && c0 + col < g.features) out[(c0 + col) * 2 * g.fp + r0 + row] = s_t[row][col];
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            const int c = row + q * (256 / kT);
+            if (r0 + col < g.fp && c0 + c < g.features) out[(c0 + c) * 2 * g.fp + r0 + col] = s_t[col][c];
         }
         return;
     }
-    b -= g.weight_blocks;
+    b -= g.weight_blocks + g.slope_blocks;
     const int64_t each = g.dp / kV, total = g.n * each;
     for (int64_t t = int64_t(b) * 256 + threadIdx.x; t < total; t += int64_t(g.x_blocks) * 256) {
-        const int64_t row = t / each, c = t - row * each;
+        const int64_t row = total <= 0xffffffffll ? uint32_t(t) / uint32_t(each) : t / each, c = t - row * each;
         *reinterpret_cast<Piece *>(g.xp + t * 16) = any_piece<E>(static_cast<const char *>(g.x) + row * g.x_stride * kEs, c * 16, g.features * kEs);
     }
 }
@@ -641,37 +646,38 @@ template <typename E> void run_gated_zero(const GatedBackArgs &a, hipStream_t st
 
 } // namespace
 
-// By the time of the busiest CU, in us, from what blocks of 8-bit products took a slice (fp32's matrix instructions take eight
-// times as long, which is all that counts there): a tile of 256 alone on a CU 1.0, and 1.42 with all CUs at it; one of 128
-// 0.73, two a CU 1.1; one of 64 0.32, three a CU 0.6, and so on by their number.  A tile's start and end take 9, 5 and 2.5;
-// joining partial sums a launch and their bytes.
+// By the time of the busiest CU, in us, from what slices took of 8-bit products (fp32's matrix instructions take eight times as
+// long, which is all that counts there).  A tile of 256 alone on a CU: 1.0, and 1.42 with all CUs at it.  One of 128: 0.73,
+// two on a CU 1.1, and so on by half that each.  One of 64: 0.32, two 0.45, then 0.2 each.  A tile's start and end take 9, 5 and
+// 2.5; joining partial sums a launch and their bytes.
 Plan plan_product(int64_t rows, int64_t columns, int64_t slices, bool wide, bool may_split, bool may_large)
 {
-    struct Kind {
-        Side side;
-        double base, each, fixed;
-        int at_once;
+    const auto slice_time = [&](Side side, int64_t blocks) {
+        const int64_t each = (blocks + kCus - 1) / kCus; // of the busiest CU
+        if (wide) return double(each) * (side == Side::kSmall ? 0.46 : side == Side::kMiddle ? 1.75 : 6.9);
+        if (side == Side::kLarge) return each > 1 ? 1.42 * double(each) : 1.0 + 0.42 * double(blocks) / kCus;
+        if (side == Side::kMiddle) return each > 1 ? 0.55 * double(each) : 0.73;
+        return each > 2 ? 0.2 * double(each) + 0.05 : each > 1 ? 0.45 : 0.32;
     };
-    const Kind narrow_kinds[3] = {{Side::kSmall, 0.32, 0.00078, 2.5, 768}, {Side::kMiddle, 0.73, 0.00215, 5.0, 512}, {Side::kLarge, 1.0, 0.00555, 9.0, 256}};
-    const Kind wide_kinds[3] = {{Side::kSmall, 0.46, 0.0018, 2.5, 768}, {Side::kMiddle, 1.75, 0.0069, 5.0, 512}, {Side::kLarge, 6.9, 0.027, 9.0, 256}};
     Plan best = {Side::kSmall, 1};
     double least = INFINITY;
-    for (const Kind &k : wide ? wide_kinds : narrow_kinds) {
-        if (k.side == Side::kLarge && !may_large) continue;
-        const int64_t tiles = tiles_of(rows, columns, int(k.side), int(k.side));
+    for (const Side side : {Side::kSmall, Side::kMiddle, Side::kLarge}) {
+        if (side == Side::kLarge && !may_large) continue;
+        const int64_t tiles = tiles_of(rows, columns, int(side), int(side));
+        const double fixed = side == Side::kSmall ? 2.5 : side == Side::kMiddle ? 5.0 : 9.0;
+        const int at_once = side == Side::kSmall ? 3 * kCus : side == Side::kMiddle ? 2 * kCus : kCus;
         for (int want = 1; want <= (may_split ? kMostSplits : 1); want += want < 8 ? 1 : want / 4) {
             const int64_t per = (slices + want - 1) / want;
             if (per < 1 || (want > 1 && per < 4)) break;
             const int splits = int((slices + per - 1) / per);
-            if (k.side == Side::kLarge && (per < 2 || slices - (splits - 1) * per < 2)) continue;
+            if (side == Side::kLarge && (per < 2 || slices - (splits - 1) * per < 2)) continue;
             if (splits > 1 && splits * rows * columns * 4 > kMostPart) break;
-            const int64_t blocks = tiles * splits, rounds = (blocks + k.at_once - 1) / k.at_once;
-            const double busy = k.each * double(blocks > k.at_once ? rounds * k.at_once : blocks);
-            const double t = k.fixed * double(rounds) + double(per) * (busy > k.base ? busy : k.base)
+            const int64_t blocks = tiles * splits, rounds = (blocks + at_once - 1) / at_once;
+            const double t = fixed * double(rounds) + double(per) * slice_time(side, blocks)
                              + (splits > 1 ? 4.0 + double(splits) * double(rows) * double(columns) * 8.0 / 4.5e6 : 0.0);
             if (t < least) {
                 least = t;
-                best = {k.side, splits};
+                best = {side, splits};
             }
         }
     }
