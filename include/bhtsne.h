@@ -599,7 +599,7 @@ int bhtsne_muon_step(const bhtsne_matrices *W, const bhtsne_matrices *G, const b
  *   h         n x f; a, b  n x f, each nullable: what the backward pass takes.
  * Sums are fp32; h is computed from a and b before they are rounded.
  * 0 <= n < 2^31, 1 <= d, f <= 65536, strides < 2^31.  No output overlaps an
- * input or another output.
+ * input or another output (one that is at the same address is refused).
  * Errors: BHTSNE_EINVAL, BHTSNE_EDEVICE. */
 enum {
     BHTSNE_SILU = 0,
@@ -650,7 +650,8 @@ int bhtsne_quantise_rows(const void *x, int64_t x_stride, int64_t n, int64_t d, 
  * The sums are exact (32-bit integers; d <= 131071), the scales are applied in
  * fp32.  0 <= n < 2^31, 1 <= f < 2^31, strides < 2^31.  out overlaps no input.
  * The workspace (bhtsne_linear_i8_workspace_size bytes, 256-byte aligned; 0 for
- * sizes out of range) is needed where x is not BHTSNE_I8.
+ * sizes out of range) is needed where x is not BHTSNE_I8 and it is more than 256
+ * bytes: a few points need none.
  * Errors: BHTSNE_EINVAL, BHTSNE_EWORKSPACE, BHTSNE_EDEVICE. */
 size_t bhtsne_linear_i8_workspace_size(int64_t n, int64_t d);
 int bhtsne_linear_i8(const void *x, int64_t x_stride, int x_type, const float *x_scale, const int8_t *w,

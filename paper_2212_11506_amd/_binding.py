@@ -1150,7 +1150,8 @@ def linear_i8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, x_scale: 
         need = linear_i8_workspace_size(n, d)
         if need == 0:
             raise BhtsneError(BHTSNE_EINVAL, "bhtsne_linear_i8_workspace_size")
-        workspace = x.new_empty(need, dtype=torch.uint8)
+        if need > 256:
+            workspace = x.new_empty(need, dtype=torch.uint8)
     rc = lib.bhtsne_linear_i8(x.data_ptr(), x_stride, x_kind, _vector(x_scale, "x_scale", n, gpu, torch.float32), w.data_ptr(), w_stride,
                               _vector(w_scale, "w_scale", f, gpu, torch.float32), _vector(bias, "bias", f, gpu), n, d, f, kind,
                               bias_kind, result.data_ptr(), out_stride, workspace.data_ptr() if workspace is not None else None, need,

@@ -38,6 +38,18 @@ bool layer_sizes_ok(int64_t n, int64_t d, int64_t f)
 {
     return n >= 0 && n <= kMost && d >= 1 && d <= kMaxSide && f >= 1 && f <= kMaxSide;
 }
+// no output is an input or another output (rows of one buffer may lie between another's, so ranges say nothing)
+template <size_t kOuts, size_t kIns> bool apart(const void *const (&outs)[kOuts], const void *const (&ins)[kIns])
+{
+    for (size_t i = 0; i < kOuts; ++i) {
+        if (!outs[i]) continue;
+        for (const void *p : ins)
+            if (outs[i] == p) return false;
+        for (size_t k = i + 1; k < kOuts; ++k)
+            if (outs[i] == outs[k]) return false;
+    }
+    return true;
+}
 bool act_ok(int act) { return act == BHTSNE_SILU || act == BHTSNE_GELU; }
 
 int status() { return hipGetLastError() == hipSuccess ? BHTSNE_OK : BHTSNE_EDEVICE; }
@@ -86,6 +98,7 @@ int bhtsne_gated_layer(const void *x, int64_t x_stride, const void *gate, int64_
         return BHTSNE_EINVAL;
     if (!output_ok(h, h_stride, n, f, type) || (a && !output_ok(a, a_stride, n, f, type)) || (b && !output_ok(b, b_stride, n, f, type)))
         return BHTSNE_EINVAL;
+    if (n > 0 && !apart({h, a, b}, {x, gate, up})) return BHTSNE_EINVAL;
     GatedArgs g = {};
     g.x = x;
     g.x_stride = x_stride;
@@ -130,6 +143,7 @@ int bhtsne_gated_layer_backward(const void *dh, int64_t dh_stride, const void *x
     if ((dx && !output_ok(dx, dx_stride, n, d, type)) || (dgate && !output_ok(dgate, dgate_stride, f, d, type))
         || (dup && !output_ok(dup, dup_stride, f, d, type)))
         return BHTSNE_EINVAL;
+    if (!apart({n > 0 ? dx : nullptr, dgate, dup}, {dh, x, gate, up, a, b})) return BHTSNE_EINVAL;
     if (!workspace_ok(workspace, workspace_bytes, bhtsne_gated_layer_workspace_size(n, d, f, type))) return BHTSNE_EWORKSPACE;
     GatedBackArgs g = {};
     g.dh = dh;
@@ -166,6 +180,7 @@ int bhtsne_quantise_rows(const void *x, int64_t x_stride, int64_t n, int64_t d, 
     if (n < 0 || n > kMost || d < 1 || d > kLinearMaxDepth || !type_ok(type)) return BHTSNE_EINVAL;
     if (!input_ok(x, x_stride, n, d, type) || !output_ok(q, q_stride, n, d, BHTSNE_I8)) return BHTSNE_EINVAL;
     if (!output_ok(scale, 1, n, 1, BHTSNE_F32)) return BHTSNE_EINVAL;
+    if (n > 0 && !apart({q, scale}, {x})) return BHTSNE_EINVAL;
     QuantiseArgs a = {};
     a.x = x;
     a.x_stride = x_stride;
@@ -182,6 +197,7 @@ int bhtsne_quantise_rows(const void *x, int64_t x_stride, int64_t n, int64_t d, 
 size_t bhtsne_linear_i8_workspace_size(int64_t n, int64_t d)
 {
     if (n < 0 || n > kMost || d < 1 || d > kLinearMaxDepth) return 0;
+    if (linear_few(n, d)) return 256; // none is needed
     const size_t depth = (size_t(d) + kLinearSlice - 1) / kLinearSlice * kLinearSlice;
     return (size_t(n) * 4 + 255) / 256 * 256 + (size_t(n) * depth + 255) / 256 * 256 + 256;
 }
@@ -198,6 +214,7 @@ int bhtsne_linear_i8(const void *x, int64_t x_stride, int x_type, const float *x
         return BHTSNE_EINVAL;
     if (whole ? !x_scale && n > 0 : x_scale != nullptr) return BHTSNE_EINVAL;
     if (!output_ok(out, out_stride, n, f, type)) return BHTSNE_EINVAL;
+    if (n > 0 && !apart({out}, {x, x_scale, w, w_scale, bias})) return BHTSNE_EINVAL;
     LinearArgs a = {};
     a.w = w;
     a.w_stride = w_stride;
@@ -215,21 +232,20 @@ int bhtsne_linear_i8(const void *x, int64_t x_stride, int x_type, const float *x
         a.x_stride = x_stride;
         a.x_scale = x_scale;
     } else {
-        if (!workspace_ok(workspace, workspace_bytes, bhtsne_linear_i8_workspace_size(n, d))) return BHTSNE_EWORKSPACE;
+        if (!linear_few(n, d) && !workspace_ok(workspace, workspace_bytes, bhtsne_linear_i8_workspace_size(n, d))) return BHTSNE_EWORKSPACE;
         QuantiseArgs q = {};
         q.x = x;
         q.x_stride = x_stride;
-        q.scale = static_cast<float *>(workspace);
-        q.q = static_cast<int8_t *>(workspace) + (size_t(n) * 4 + 255) / 256 * 256;
+        if (!linear_few(n, d)) {
+            q.scale = static_cast<float *>(workspace);
+            q.q = static_cast<int8_t *>(workspace) + (size_t(n) * 4 + 255) / 256 * 256;
+        }
         q.q_stride = q.pad = (d + kLinearSlice - 1) / kLinearSlice * kLinearSlice;
         q.n = n;
         q.d = d;
         q.type = Elem(x_type);
-        launch_quantise_rows(q, stream);
-        a.x = q.q;
-        a.x_stride = q.q_stride;
-        a.x_scale = q.scale;
-        a.padded = true;
+        launch_linear_values(a, q, stream);
+        return status();
     }
     launch_linear_i8(a, stream);
     return status();

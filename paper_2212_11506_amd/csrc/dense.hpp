@@ -91,6 +91,13 @@ void launch_gated_layer_backward(const GatedBackArgs &a, hipStream_t st);
 constexpr int64_t kLinearSlice = 128;       // values of a slice of a row
 constexpr int64_t kLinearMaxDepth = 131071; // (-128)^2 so many times stays below 2^31
 
+// A few points, which their product quantises itself (kFewValues values, with the rows' padding)
+constexpr int64_t kFewPoints = 16, kFewValues = 8192;
+inline bool linear_few(int64_t n, int64_t d)
+{
+    return n <= kFewPoints && n * ((d + kLinearSlice - 1) / kLinearSlice * kLinearSlice) <= kFewValues;
+}
+
 struct QuantiseArgs {
     const void *x;
     int8_t *q;
@@ -113,5 +120,6 @@ struct LinearArgs {
     bool padded; // x's rows go on with zeros to whole slices
 };
 void launch_linear_i8(const LinearArgs &a, hipStream_t st);
+void launch_linear_values(LinearArgs a, const QuantiseArgs &q, hipStream_t st); // of the rows that q quantises
 
 } // namespace bht

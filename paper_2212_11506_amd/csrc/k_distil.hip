@@ -25,6 +25,20 @@ template <typename E> struct alignas(16) Vec {
     E v[kV];
 };
 
+// 16 bytes at the values' own alignment; and 16 aligned ones, which leave no lines in the caches (2048 x 70000 bf16, 573 MB
+// read and written: 141 us without, 125 so; 16 x 1.3M fp16 19.6 and 19.1; loads that leave none 137)
+template <typename E> __device__ inline Vec<E> load_vec(const E *p)
+{
+    Vec<E> v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+template <typename E> __device__ inline void store_vec(E *p, const Vec<E> &v)
+{
+    __builtin_nontemporal_store(__builtin_bit_cast(uint4v, v), reinterpret_cast<uint4v *>(p));
+}
+
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // The running maximum m and sum of exp2((z - m) c) of a lane's logits.  Logits of minus infinity count nothing; NaN and
@@ -287,26 +301,34 @@ __global__ __launch_bounds__(kThreads) void distil_back_kernel(DistilArgs a)
         const E *p = z + from;
         E *o = out + from;
         const int64_t count = to - from;
-        const uintptr_t off = reinterpret_cast<uintptr_t>(p) & 15;
-        if (off == (reinterpret_cast<uintptr_t>(o) & 15)) {
-            int64_t head = int64_t((16 - off) & 15) / int64_t(sizeof(E));
-            if (head > count) head = count;
-            if (int64_t(threadIdx.x) < head) o[threadIdx.x] = dense(float(p[threadIdx.x]));
-            p += head;
-            o += head;
-            const int64_t vectors = (count - head) / kV;
-            for (int64_t i = threadIdx.x; i < vectors; i += kThreads) {
-                const Vec<E> x = reinterpret_cast<const Vec<E> *>(p)[i];
-                Vec<E> y;
+        // single values up to the output's first 16-byte boundary, vectors, rest; the logits at whatever alignment they have
+        int64_t head = int64_t((16 - (reinterpret_cast<uintptr_t>(o) & 15)) & 15) / int64_t(sizeof(E));
+        if (head > count) head = count;
+        if (int64_t(threadIdx.x) < head) o[threadIdx.x] = dense(float(p[threadIdx.x]));
+        p += head;
+        o += head;
+        const int64_t vectors = (count - head) / kV;
+        constexpr int kAtOnce = 4;
+        int64_t i = threadIdx.x;
+        for (; i + (kAtOnce - 1) * kThreads < vectors; i += kAtOnce * kThreads) {
+            Vec<E> x[kAtOnce];
 #pragma unroll
-                for (int e = 0; e < kV; ++e) y.v[e] = dense(float(x.v[e]));
-                reinterpret_cast<Vec<E> *>(o)[i] = y;
+            for (int u = 0; u < kAtOnce; ++u) x[u] = load_vec(p + (i + u * kThreads) * kV);
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+#pragma unroll
+                for (int e = 0; e < kV; ++e) x[u].v[e] = dense(float(x[u].v[e]));
+                store_vec(o + (i + u * kThreads) * kV, x[u]);
             }
-            const int64_t rest = vectors * kV + threadIdx.x;
-            if (rest < count - head) o[rest] = dense(float(p[rest]));
-        } else {
-            for (int64_t i = threadIdx.x; i < count; i += kThreads) o[i] = dense(float(p[i]));
         }
+        for (; i < vectors; i += kThreads) {
+            Vec<E> x = load_vec(p + i * kV);
+#pragma unroll
+            for (int e = 0; e < kV; ++e) x.v[e] = dense(float(x.v[e]));
+            store_vec(o + i * kV, x);
+        }
+        const int64_t rest = vectors * kV + threadIdx.x;
+        if (rest < count - head) o[rest] = dense(float(p[rest]));
         __syncthreads();
         for (int j = threadIdx.x; j < a.k; j += kThreads) {
             const int32_t at = s_at[j];

@@ -178,8 +178,111 @@ template <typename E, typename T, bool kAny, Tail kTail = Tail::kWhole> void run
     }
 }
 
+// A few points (few_points).  X: their type; int8 as they are, else the block quantises them into LDS while its weights are
+// under way to it: one launch (1 x 2048 to 8192 bf16 8.4 us, of which a launch is 2.5; by two 12 and the gap between them).
+template <typename E, typename X>
+__global__ __launch_bounds__(kFewWaves *kWave) void linear8_few_kernel(Product p, LinearOut o)
+{
+    constexpr bool kWhole = sizeof(X) == 1;
+    constexpr int kThreads = kFewWaves * kWave;
+    __shared__ int32_t s_sum[kFewWaves][1][kFewPoints * 16];
+    __shared__ float s_scale[kFewPoints], s_max[kFewWaves];
+    __shared__ __align__(16) int8_t s_x[kWhole ? 16 : kFewValues];
+    const int64_t feature = int64_t(blockIdx.x) * 16;
+    const int lane = lane_id(), point_row = lane % 16 < p.rows ? lane % 16 : int(p.rows) - 1;
+    const int32_t width = p.slices * kSlice;
+    const auto quantise_all = [&] {
+        if constexpr (kWhole) return;
+        for (int r = 0; r < int(p.rows); ++r) {
+            const X *x = reinterpret_cast<const X *>(p.A + r * p.a_stride);
+            float v[kRowValues], top = 0.0f;
+#pragma unroll
+            for (int e = 0; e < kRowValues; ++e) v[e] = 0.0f;
+            const int at = int(threadIdx.x) * kRowValues; // the whole row at once
+            static_assert(kFewValues <= kThreads * kRowValues, "a row is in the threads' registers");
+            if (at < p.bytes) load_values(x, at, p.bytes, v);
+#pragma unroll
+            for (int e = 0; e < kRowValues; ++e) {
+                const float m = fabsf(v[e]);
+                top = m <= top ? top : m < INFINITY ? m : INFINITY;
+            }
+            top = wave_max(top);
+            if (lane == 0) s_max[threadIdx.x / kWave] = top;
+            __syncthreads();
+            top = s_max[0];
+#pragma unroll
+            for (int k = 1; k < kFewWaves; ++k) top = fmaxf(top, s_max[k]);
+            const bool finite = top < INFINITY;
+            const float scale = finite ? top / 127.0f : NAN, inverse = 1.0f / scale;
+            if (threadIdx.x == 0) s_scale[r] = scale;
+            if (at < width) {
+                struct alignas(16) {
+                    int8_t v[kRowValues];
+                } q;
+#pragma unroll
+                for (int e = 0; e < kRowValues; ++e) q.v[e] = int8_t(finite && scale > 0.0f ? quantise(v[e], scale, inverse) : 0);
+                *reinterpret_cast<Piece *>(s_x + r * width + at) = __builtin_bit_cast(Piece, q);
+            }
+            __syncthreads();
+        }
+    };
+    const char *row = p.A + point_row * p.a_stride;
+    const auto x = [&](int32_t slice, int half) {
+        const int64_t k = int64_t(slice) * kSlice + half * 64 + lane / 16 * 16;
+        if constexpr (kWhole)
+            return int64_t(slice + 1) * kSlice <= p.bytes ? inner_piece(row + k) : any_piece<int8_t>(row, k, p.bytes);
+        else
+            return *reinterpret_cast<const Piece *>(s_x + point_row * width + k);
+    };
+    Ops<int8_t>::Acc acc[1] = {};
+    few_points<int8_t, 1>(p, feature, quantise_all, x, acc);
+    int32_t v[1];
+    few_join(acc, s_sum, v);
+    const int64_t point = int(threadIdx.x) / 16, at = feature + int(threadIdx.x) % 16;
+    const int64_t held = at < p.features ? at : p.features - 1;
+    float bias = 0.0f;
+    if (o.bias) bias = o.wide_bias ? static_cast<const float *>(o.bias)[held] : float(static_cast<const E *>(o.bias)[held]);
+    if (point >= p.rows || at >= p.features) return;
+    const float s = kWhole ? o.x_scale[point] : s_scale[point];
+    static_cast<E *>(o.out)[point * o.stride + at] = E(float(v[0]) * s * o.w_scale[at] + bias);
+}
+
+template <typename E, typename X> void run_linear_few(const LinearArgs &a, const void *x, int64_t x_stride, hipStream_t st)
+{
+    Product p = {};
+    p.A = static_cast<const char *>(x);
+    p.B = reinterpret_cast<const char *>(a.w);
+    p.a_stride = x_stride * int64_t(sizeof(X));
+    p.b_stride = a.w_stride;
+    p.rows = a.n;
+    p.features = a.f;
+    p.bytes = a.d;
+    p.slices = p.per_split = int32_t(slices_of(a.d));
+    LinearOut o = {};
+    o.x_scale = a.x_scale;
+    o.w_scale = a.w_scale;
+    o.bias = a.bias;
+    o.out = a.out;
+    o.stride = a.out_stride;
+    o.wide_bias = a.bias_type == Elem::kF32;
+    linear8_few_kernel<E, X><<<uint32_t((a.f + 15) / 16), kFewWaves * kWave, 0, st>>>(p, o);
+}
+
+template <typename E> bool few_and_quantised(const LinearArgs &a, const QuantiseArgs &q, hipStream_t st)
+{
+    if (!linear_few(a.n, a.d)) return false;
+    if (q.type == Elem::kF32)
+        run_linear_few<E, float>(a, q.x, q.x_stride, st);
+    else if (q.type == Elem::kF16)
+        run_linear_few<E, f16>(a, q.x, q.x_stride, st);
+    else
+        run_linear_few<E, bf16>(a, q.x, q.x_stride, st);
+    return true;
+}
+
 template <typename E> void run_linear_type(const LinearArgs &a, hipStream_t st)
 {
+    if (a.n <= kFewPoints) return run_linear_few<E, int8_t>(a, a.x, a.x_stride, st);
     const bool any = !aligned16(a.x, a.x_stride) || !aligned16(a.w, a.w_stride) || a.d % 16 != 0;
     const Side side = plan_product(a.n, a.f, slices_of(a.d), false, false, !any && a.x_stride <= kLargeStride && a.w_stride <= kLargeStride).side;
     if (any) {
@@ -210,6 +313,19 @@ void launch_linear_i8(const LinearArgs &a, hipStream_t st)
     if (a.type == Elem::kF32) return run_linear_type<float>(a, st);
     if (a.type == Elem::kF16) return run_linear_type<f16>(a, st);
     run_linear_type<bf16>(a, st);
+}
+
+void launch_linear_values(LinearArgs a, const QuantiseArgs &q, hipStream_t st)
+{
+    if (a.n == 0) return;
+    const bool done = a.type == Elem::kF32 ? few_and_quantised<float>(a, q, st) : a.type == Elem::kF16 ? few_and_quantised<f16>(a, q, st) : few_and_quantised<bf16>(a, q, st);
+    if (done) return;
+    launch_quantise_rows(q, st);
+    a.x = q.q;
+    a.x_stride = q.q_stride;
+    a.x_scale = q.scale;
+    a.padded = true;
+    launch_linear_i8(a, st);
 }
 
 } // namespace bht

@@ -398,6 +398,71 @@ __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, t
     }
 }
 
+// ------------------------------------------------------------------ few points
+// Up to 16 points: a block makes 16 features of all of them, its waves share K out in slices, every kFewWaves-th each, and take
+// fragments straight from memory: the weights are read once, a line of 16 rows at a time, four of them in flight a wave.  Rows
+// of any alignment.  x(slice, half): the points' fragment, zeros behind the end.
+constexpr int kFewWaves = 8, kFewAtOnce = 4; // slices of one matrix in flight, of two half of that
+// ready(): called once by every wave while the first weights are under way.
+template <typename E, int kMats, typename G, typename F>
+__device__ inline void few_points(const Product &a, int64_t feature, G ready, F x, typename Ops<E>::Acc (&acc)[kMats])
+{
+    constexpr int kAtOnce = kFewAtOnce / kMats;
+    const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id();
+    const int64_t at = feature + lane % 16, held = at < a.features ? at : a.features - 1;
+    const char *row[2] = {a.B + held * a.b_stride, kMats == 2 ? a.B2 + held * a.b2_stride : nullptr};
+    Piece q[kAtOnce][kMats][2];
+    const auto load = [&](int32_t s0) {
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int32_t s = s0 + u * kFewWaves < a.slices ? s0 + u * kFewWaves : s0; // again, and not used
+#pragma unroll
+            for (int m = 0; m < kMats; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int64_t k = int64_t(s) * kSlice + h * 64 + lane / 16 * 16;
+                    if (int64_t(s + 1) * kSlice <= a.bytes)
+                        q[u][m][h] = inner_piece(row[m] + k);
+                    else
+                        q[u][m][h] = any_piece<E>(row[m], k, a.bytes);
+                }
+        }
+    };
+    if (w < a.slices) load(w);
+    ready();
+    for (int32_t s0 = w; s0 < a.slices;) {
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            if (s0 + u * kFewWaves >= a.slices) break;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const Piece p = x(s0 + u * kFewWaves, h);
+#pragma unroll
+                for (int m = 0; m < kMats; ++m) acc[m] = Ops<E>::mul(p, q[u][m][h], acc[m]);
+            }
+        }
+        s0 += kFewWaves * kAtOnce;
+        if (s0 < a.slices) load(s0);
+    }
+}
+// The waves' sums, in order: value(t, m) for the block's threads t < 256, of point t / 16 and feature t % 16
+template <typename V, int kMats, typename Acc>
+__device__ inline void few_join(const Acc (&acc)[kMats], V (*s_sum)[kMats][kFewPoints * 16], V (&sum)[kMats])
+{
+    const int w = int(threadIdx.x) / kWave, lane = lane_id(), t = int(threadIdx.x) % (kFewPoints * 16);
+#pragma unroll
+    for (int m = 0; m < kMats; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s_sum[w][m][(lane / 16 * 4 + r) * 16 + lane % 16] = acc[m][r];
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < kMats; ++m) {
+        sum[m] = V(0);
+#pragma unroll
+        for (int k = 0; k < kFewWaves; ++k) sum[m] += s_sum[k][m][t];
+    }
+}
+
 // ------------------------------------------------------------------ large tiles
 // Tiles of 256 x 256 by two groups of four waves, one of each on a SIMD.  A wave's 128 x 64 values are four quarters of
 // 64 x 32; a slice takes four steps, one a quarter, and a step has two parts with a barrier behind each: in the first the wave

@@ -7,7 +7,8 @@ import paper_2212_11506_amd as bh
 from paper_2212_11506_amd import _binding as b
 from tests.test_map_binding import Elsewhere
 
-FAKE = 1 << 20  # a non-null, 256-aligned address that is never dereferenced on rejection
+FAKE = 1 << 20  # non-null, 256-aligned addresses that are never dereferenced on rejection
+X_, A_, B_, W_ = (FAKE + 4096 * k for k in range(1, 5))
 BIG = 1 << 50
 INF, NAN = float("inf"), float("nan")
 
@@ -20,7 +21,7 @@ def call(name, order, given, bad):
 
 def gated(**bad):
     return call("bhtsne_gated_layer", "x xs g gs u us n d f act t h hs a as_ b bs",
-                dict(x=FAKE, xs=8, g=FAKE, gs=8, u=FAKE, us=8, n=4, d=8, f=16, act=0, t=0, h=FAKE, hs=16, a=FAKE, as_=16, b=FAKE, bs=16), bad)
+                dict(x=FAKE, xs=8, g=FAKE, gs=8, u=FAKE, us=8, n=4, d=8, f=16, act=0, t=0, h=X_, hs=16, a=A_, as_=16, b=B_, bs=16), bad)
 
 
 LAYER = [dict(n=-1), dict(n=1 << 31), dict(d=0), dict(d=65537), dict(f=0), dict(f=65537), dict(act=2), dict(act=-1), dict(t=3), dict(t=-1), dict(x=None),
@@ -28,20 +29,21 @@ LAYER = [dict(n=-1), dict(n=1 << 31), dict(d=0), dict(d=65537), dict(f=0), dict(
          dict(x=FAKE + 2), dict(g=FAKE + 1), dict(u=FAKE + 2), dict(as_=15), dict(bs=0), dict(a=FAKE + 1), dict(b=FAKE + 2)]
 
 
-@pytest.mark.parametrize("bad", LAYER + [dict(h=None), dict(hs=15), dict(hs=0), dict(h=FAKE + 2)])
+@pytest.mark.parametrize("bad", LAYER + [dict(h=None), dict(hs=15), dict(hs=0), dict(h=FAKE + 2), dict(h=FAKE), dict(a=FAKE), dict(h=A_), dict(a=B_)])
 def test_gated_layer_refuses(bad):
     assert gated(**bad) == bh.BHTSNE_EINVAL
 
 
 def gated_back(**bad):
     return call("bhtsne_gated_layer_backward", "dh dhs x xs g gs u us a as_ b bs n d f act t dx dxs dg dgs du dus ws wsb",
-                dict(dh=FAKE, dhs=16, x=FAKE, xs=8, g=FAKE, gs=8, u=FAKE, us=8, a=FAKE, as_=16, b=FAKE, bs=16, n=4, d=8, f=16, act=0, t=0, dx=FAKE, dxs=8,
-                     dg=FAKE, dgs=8, du=FAKE, dus=8, ws=FAKE, wsb=BIG), bad)
+                dict(dh=FAKE, dhs=16, x=FAKE, xs=8, g=FAKE, gs=8, u=FAKE, us=8, a=FAKE, as_=16, b=FAKE, bs=16, n=4, d=8, f=16, act=0, t=0, dx=X_, dxs=8,
+                     dg=A_, dgs=8, du=B_, dus=8, ws=FAKE, wsb=BIG), bad)
 
 
 @pytest.mark.parametrize("bad", [c for c in LAYER if c != dict(bs=0)] + [
     dict(dh=None), dict(a=None), dict(b=None), dict(dhs=15), dict(bs=15), dict(dxs=7), dict(dxs=0), dict(dgs=7), dict(dus=0),
-    dict(dx=FAKE + 1), dict(dg=FAKE + 2), dict(du=FAKE + 3), dict(dx=None, dg=None, du=None)])
+    dict(dx=FAKE + 1), dict(dg=FAKE + 2), dict(du=FAKE + 3), dict(dx=None, dg=None, du=None), dict(dx=FAKE), dict(dg=FAKE),
+    dict(dx=A_), dict(dg=B_)])
 def test_gated_layer_backward_refuses(bad):
     assert gated_back(**bad) == bh.BHTSNE_EINVAL
 
@@ -59,24 +61,24 @@ def test_gated_layer_workspace_size():
 
 
 def quantise(**bad):
-    return call("bhtsne_quantise_rows", "x xs n d t q qs s", dict(x=FAKE, xs=8, n=4, d=8, t=0, q=FAKE, qs=8, s=FAKE), bad)
+    return call("bhtsne_quantise_rows", "x xs n d t q qs s", dict(x=FAKE, xs=8, n=4, d=8, t=0, q=X_, qs=8, s=A_), bad)
 
 
 @pytest.mark.parametrize("bad", [dict(x=None), dict(xs=7), dict(n=-1), dict(n=1 << 31), dict(d=0), dict(d=131072), dict(t=3), dict(q=None), dict(qs=7),
-                                 dict(s=None), dict(s=FAKE + 2), dict(x=FAKE + 2)])
+                                 dict(s=None), dict(s=FAKE + 2), dict(x=FAKE + 2), dict(q=FAKE), dict(s=X_)])
 def test_quantise_rows_refuses(bad):
     assert quantise(**bad) == bh.BHTSNE_EINVAL
 
 
 def linear(**bad):
     return call("bhtsne_linear_i8", "x xs xt xsc w ws_ wsc bias n d f t bt out os ws wsb",
-                dict(x=FAKE, xs=8, xt=0, xsc=None, w=FAKE, ws_=8, wsc=FAKE, bias=FAKE, n=4, d=8, f=16, t=0, bt=0, out=FAKE, os=16, ws=FAKE, wsb=BIG), bad)
+                dict(x=FAKE, xs=8, xt=0, xsc=None, w=FAKE, ws_=8, wsc=FAKE, bias=FAKE, n=100, d=8, f=16, t=0, bt=0, out=X_, os=16, ws=FAKE, wsb=BIG), bad)
 
 
 @pytest.mark.parametrize("bad", [dict(x=None), dict(xs=7), dict(xt=4), dict(xt=-1), dict(xsc=FAKE), dict(xt=3), dict(xt=3, xsc=FAKE + 1), dict(w=None),
                                  dict(ws_=0), dict(ws_=7), dict(wsc=None), dict(wsc=FAKE + 2), dict(bias=FAKE + 1), dict(n=-1), dict(d=0),
                                  dict(d=131072), dict(f=0), dict(f=1 << 31), dict(t=3), dict(bt=1), dict(t=1, bt=2), dict(out=None), dict(os=15),
-                                 dict(out=FAKE + 1), dict(x=FAKE + 2)])
+                                 dict(out=FAKE + 1), dict(x=FAKE + 2), dict(out=FAKE)])
 def test_linear_i8_refuses(bad):
     assert linear(**bad) == bh.BHTSNE_EINVAL
 
@@ -90,6 +92,7 @@ def test_linear_i8_workspace_size():
     size = bh.linear_i8_workspace_size
     assert size(-1, 8) == size(4, 0) == size(4, 131072) == 0 and size(0, 8) > 0
     assert size(100, 20) >= 100 * 32 + 400 and size(100, 20) % 256 == 0
+    assert size(1, 8192) == size(16, 512) == size(4, 1) == 256 < size(1, 8193) and size(17, 8) > 256 and size(16, 513) > 256
 
 
 def distil(**bad):
