@@ -678,7 +678,8 @@ int bhtsne_linear_i8(const void *x, int64_t x_stride, int x_type, const float *x
  *   dlogits  n x v of `type`; may be logits (with their stride).
  * Input strides are >= the row's length, or 0 for one row that stands for all.
  * 0 <= n < 2^31, 1 <= v < 2^31, 0 <= k <= 2048, strides < 2^31, T in [1e-6, 1e6].
- * Sums over v are fp32 in a lane and joined in fp64, in a fixed order.  The
+ * Sums over v are fp32 in a lane and joined in fp64, in an order that goes by
+ * sizes and the logits' alignment alone: the same call gives the same bits.  The
  * workspace (bhtsne_distil_loss_workspace_size bytes, 256-byte aligned; 0 for
  * sizes out of range) is needed where it is more than 256 bytes: few long rows.
  * Errors: BHTSNE_EINVAL, BHTSNE_EWORKSPACE, BHTSNE_EDEVICE. */

@@ -124,7 +124,8 @@ __device__ inline List list_of(const DistilArgs &a, int64_t row, float c, double
     return l;
 }
 
-// Logits [from, to) of a row through a lane's running sum: single values up to the first 16-byte boundary, vectors, rest
+// Logits [from, to) of a row through a lane's running sum: single values up to the first 16-byte boundary, vectors, rest.
+// (Vectors at any alignment, whose sums would not depend on it: 4096 x 70001 bf16 133 us, so 112.)
 template <typename E, int kThreads>
 __device__ inline Running run_over(const E *row, int64_t from, int64_t to, float c)
 {
