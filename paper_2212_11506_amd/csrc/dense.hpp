@@ -72,6 +72,7 @@ struct GatedBackLayout {
     int64_t np;      // points, padded to whole slices
     int64_t ld;      // values from row to row of da and db
     Plan x, weights; // of dx, and of the weights' gradients
+    bool wide;       // operands in fp32
     size_t d, xp, wt, part, total;
 };
 GatedBackLayout make_gated_back_layout(int64_t n, int64_t d, int64_t f, Elem type);

@@ -9,7 +9,9 @@
 //   da = dh b act'(a), db = dh act(a);  dx = da gate + db up;  dgate = da^T x, dup = db^T x
 // da and db are formed once, in fp32, and rounded to the inputs' type, as operands of
 // matrix instructions of that type: with bf16 their rounding adds to the output's own
-// (1.7e-3 each, 2.4e-3 together).  The sums over features and points are fp32.
+// (1.7e-3 each, 2.4e-3 together).  Where outputs are few and the products small, that
+// average does not hold for them and costs nothing to do without: operands are fp32
+// (kFewOutputs).  The sums over features and points are fp32.
 #include <cmath>
 
 #include "products.hpp"
@@ -385,13 +387,17 @@ template <typename E> __device__ inline Piece row_piece(const void *p, int64_t r
     return straight ? inner_piece(r + c * 16) : any_piece<E>(r, c * 16, bytes);
 }
 
-template <typename E> __global__ __launch_bounds__(256) void gated_operands_kernel(Operands g)
+// C: of the operands, E or fp32
+template <typename E, typename C> __global__ __launch_bounds__(256) void gated_operands_kernel(Operands g)
 {
-    constexpr int kEs = int(sizeof(E)), kV = 16 / kEs;
+    constexpr int kEs = int(sizeof(E)), kCs = int(sizeof(C)), kV = 16 / kEs; // values at a time
     struct alignas(16) Values {
         E v[kV];
     };
-    __shared__ E s_t[kT][kT + 2];
+    struct alignas(16) Made {
+        C v[kV];
+    };
+    __shared__ C s_t[kT][kT + 2];
     uint32_t b = blockIdx.x;
     if (b >= g.weight_blocks && b < g.weight_blocks + g.slope_blocks) {
         b -= g.weight_blocks;
@@ -399,26 +405,26 @@ template <typename E> __global__ __launch_bounds__(256) void gated_operands_kern
         for (int64_t t = int64_t(b) * 256 + threadIdx.x; t < total; t += int64_t(g.slope_blocks) * 256) {
             const int64_t row = total <= 0xffffffffll ? uint32_t(t) / uint32_t(each) : t / each, c = t - row * each;
             const int64_t bytes = g.f * kEs;
-            char *out = g.d + (row * g.ld + c * kV) * kEs;
+            char *out = g.d + (row * g.ld + c * kV) * kCs;
             if (row >= g.n || c * kV >= g.f) { // padding
-                *reinterpret_cast<Piece *>(out) = Piece{0, 0, 0, 0};
-                *reinterpret_cast<Piece *>(out + g.fp * kEs) = Piece{0, 0, 0, 0};
+                *reinterpret_cast<Made *>(out) = Made{};
+                *reinterpret_cast<Made *>(out + g.fp * kCs) = Made{};
                 continue;
             }
             const Values dh = __builtin_bit_cast(Values, row_piece<E>(g.dh, g.dh_stride * kEs, row, c, bytes, g.straight));
             const Values av = __builtin_bit_cast(Values, row_piece<E>(g.a, g.a_stride * kEs, row, c, bytes, g.straight));
             const Values bv = __builtin_bit_cast(Values, row_piece<E>(g.b, g.b_stride * kEs, row, c, bytes, g.straight));
-            Values da, db;
+            Made da, db;
 #pragma unroll
             for (int e = 0; e < kV; ++e) {
                 float value, slope;
                 activate_both<E>(float(av.v[e]), g.act, value, slope);
                 const float d = float(dh.v[e]);
-                da.v[e] = E(d * float(bv.v[e]) * slope);
-                db.v[e] = E(d * value);
+                da.v[e] = C(d * float(bv.v[e]) * slope);
+                db.v[e] = C(d * value);
             }
-            *reinterpret_cast<Values *>(out) = da;
-            *reinterpret_cast<Values *>(out + g.fp * kEs) = db;
+            *reinterpret_cast<Made *>(out) = da;
+            *reinterpret_cast<Made *>(out + g.fp * kCs) = db;
         }
         return;
     }
@@ -437,9 +443,9 @@ template <typename E> __global__ __launch_bounds__(256) void gated_operands_kern
             v[q] = in[(r < g.f ? r : g.f - 1) * stride + (c < g.features ? c : g.features - 1)];
         }
 #pragma unroll
-        for (int q = 0; q < kEach; ++q) s_t[row + q * (256 / kT)][col] = r0 + row + q * (256 / kT) < g.f ? v[q] : E(0.0f);
+        for (int q = 0; q < kEach; ++q) s_t[row + q * (256 / kT)][col] = r0 + row + q * (256 / kT) < g.f ? C(float(v[q])) : C(0.0f);
         __syncthreads();
-        E *out = reinterpret_cast<E *>(g.wt) + (second ? g.fp : 0);
+        C *out = reinterpret_cast<C *>(g.wt) + (second ? g.fp : 0);
 #pragma unroll
         for (int q = 0; q < kEach; ++q) {
             const int c = row + q * (256 / kT);
@@ -451,7 +457,11 @@ template <typename E> __global__ __launch_bounds__(256) void gated_operands_kern
     const int64_t each = g.dp / kV, total = g.n * each;
     for (int64_t t = int64_t(b) * 256 + threadIdx.x; t < total; t += int64_t(g.x_blocks) * 256) {
         const int64_t row = total <= 0xffffffffll ? uint32_t(t) / uint32_t(each) : t / each, c = t - row * each;
-        *reinterpret_cast<Piece *>(g.xp + t * 16) = any_piece<E>(static_cast<const char *>(g.x) + row * g.x_stride * kEs, c * 16, g.features * kEs);
+        const Values x = __builtin_bit_cast(Values, any_piece<E>(static_cast<const char *>(g.x) + row * g.x_stride * kEs, c * 16, g.features * kEs));
+        Made y;
+#pragma unroll
+        for (int e = 0; e < kV; ++e) y.v[e] = C(float(x.v[e]));
+        *reinterpret_cast<Made *>(g.xp + t * (kV * kCs)) = y;
     }
 }
 
@@ -466,11 +476,12 @@ struct BackOut {
     bool vec;
 };
 
-template <typename E, typename T, Form kForm, bool kPart>
+// C: of the operands, E: of the outputs
+template <typename E, typename C, typename T, Form kForm, bool kPart>
 __global__ __launch_bounds__(T::kThreads) void gated_back_kernel(Product p, BackOut o)
 {
     constexpr int kRun = T::kJ;
-    each_tile<E, T, kForm, false, Tail::kWhole>(p, [&](int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ]) {
+    each_tile<C, T, kForm, false, Tail::kWhole>(p, [&](int32_t bi, int32_t bj, typename Ops<C>::Acc (&acc)[T::kI][T::kJ]) {
         each_run<T, kForm>(bi, bj, [&](int64_t row, int64_t feature, int i, int r) {
             if (row >= p.rows) return;
             float v[kRun];
@@ -531,7 +542,7 @@ template <typename E, int kV> __global__ __launch_bounds__(256) void gated_join_
     }
 }
 
-template <typename E, typename T, Form kForm>
+template <typename E, typename C, typename T, Form kForm>
 void run_back(Product p, const BackOut &o, int splits, hipStream_t st)
 {
     p.slices = int32_t(slices_of(p.bytes));
@@ -548,24 +559,24 @@ void run_back(Product p, const BackOut &o, int splits, hipStream_t st)
         if (kForm == Form::kRows) q.out = static_cast<E *>(o.out) + from * o.stride;
         const dim3 grid(blocks_of<T>(uint32_t(p.down) * uint32_t(p.across)), uint32_t(splits));
         if (splits > 1)
-            gated_back_kernel<E, T, kForm, true><<<grid, T::kThreads, lds, st>>>(p, q);
+            gated_back_kernel<E, C, T, kForm, true><<<grid, T::kThreads, lds, st>>>(p, q);
         else
-            gated_back_kernel<E, T, kForm, false><<<grid, T::kThreads, lds, st>>>(p, q);
+            gated_back_kernel<E, C, T, kForm, false><<<grid, T::kThreads, lds, st>>>(p, q);
     }
 }
 
-template <typename E, Form kForm> void run_back_plan(const Product &p, BackOut o, Plan plan, hipStream_t st)
+template <typename E, typename C, Form kForm> void run_back_plan(const Product &p, BackOut o, Plan plan, hipStream_t st)
 {
     constexpr int64_t es = int64_t(sizeof(E));
     o.part_rows = kForm == Form::kRows ? o.f : 2 * o.f;
     const bool pairs = o.features % 2 == 0 && aligned_to(2 * es, o.out, o.stride * es) && aligned_to(2 * es, o.out2, o.stride2 * es);
     if (plan.splits > 1) o.vec = o.features % 4 == 0; // of the partial sums
     if (plan.side == Side::kLarge)
-        run_back<E, TileLarge, kForm>(p, o, plan.splits, st);
+        run_back<E, C, TileLarge, kForm>(p, o, plan.splits, st);
     else if (plan.side == Side::kMiddle)
-        run_back<E, TileMiddle, kForm>(p, o, plan.splits, st);
+        run_back<E, C, TileMiddle, kForm>(p, o, plan.splits, st);
     else
-        run_back<E, TileSmall, kForm>(p, o, plan.splits, st);
+        run_back<E, C, TileSmall, kForm>(p, o, plan.splits, st);
     if (plan.splits == 1) return;
     const int64_t blocks = (o.part_rows * o.features / (pairs ? 2 : 1) + 255) / 256;
     const uint32_t grid = uint32_t(blocks < 16384 ? blocks : 16384);
@@ -575,12 +586,11 @@ template <typename E, Form kForm> void run_back_plan(const Product &p, BackOut o
         gated_join_kernel<E, 1><<<grid, 256, 0, st>>>(o, plan.splits);
 }
 
-template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st)
+template <typename E, typename C> void run_gated_back_of(const GatedBackArgs &a, const GatedBackLayout &L, hipStream_t st)
 {
-    const GatedBackLayout L = make_gated_back_layout(a.n, a.d, a.f, a.type);
-    const int64_t es = int64_t(sizeof(E)), kV = 16 / es;
+    const int64_t es = int64_t(sizeof(E)), cs = int64_t(sizeof(C)), kV = 16 / es;
     char *ws = static_cast<char *>(a.ws);
-    const bool weights = a.dgate || a.dup, pad_x = weights && (!aligned16(a.x, a.x_stride * es) || a.d * es % 16 != 0 || a.x_stride * es > kLargeStride);
+    const bool weights = a.dgate || a.dup, pad_x = weights && (cs != es || !aligned16(a.x, a.x_stride * es) || a.d * es % 16 != 0 || a.x_stride * es > kLargeStride);
     Operands g = {};
     g.dh = a.dh;
     g.a = a.a;
@@ -613,13 +623,13 @@ template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st
     g.slope_blocks = blocks_for(L.np * (L.fp / kV));
     g.weight_blocks = a.dx ? uint32_t(2 * tiles_of(L.fp, a.d, kT, kT)) : 0;
     g.x_blocks = pad_x ? blocks_for(a.n * (L.dp / kV)) : 0;
-    gated_operands_kernel<E><<<g.slope_blocks + g.weight_blocks + g.x_blocks, 256, 0, st>>>(g);
+    gated_operands_kernel<E, C><<<g.slope_blocks + g.weight_blocks + g.x_blocks, 256, 0, st>>>(g);
     if (a.dx) {
         Product p = {};
         p.A = g.d;
         p.B = g.wt;
-        p.a_stride = L.ld * es;
-        p.b_stride = p.bytes = 2 * L.fp * es;
+        p.a_stride = L.ld * cs;
+        p.b_stride = p.bytes = 2 * L.fp * cs;
         p.rows = a.n;
         p.features = a.d;
         BackOut o = {};
@@ -630,15 +640,15 @@ template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st
         o.features = a.d;
         o.part = reinterpret_cast<float *>(ws + L.part);
         o.vec = aligned16(a.dx, a.dx_stride * es);
-        run_back_plan<E, Form::kRows>(p, o, L.x, st);
+        run_back_plan<E, C, Form::kRows>(p, o, L.x, st);
     }
     if (weights) {
         Product p = {};
         p.A = g.d;
         p.B = pad_x ? g.xp : static_cast<const char *>(a.x);
-        p.a_stride = L.ld * es;
-        p.b_stride = (pad_x ? L.dp : a.x_stride) * es;
-        p.bytes = a.n * es;
+        p.a_stride = L.ld * cs;
+        p.b_stride = (pad_x ? L.dp : a.x_stride) * cs;
+        p.bytes = a.n * cs;
         p.rows = 2 * L.fp;
         p.features = pad_x ? L.dp : a.d;
         BackOut o = {};
@@ -650,8 +660,14 @@ template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st
         o.f = a.f;
         o.features = a.d;
         o.part = reinterpret_cast<float *>(ws + L.part);
-        run_back_plan<E, Form::kColumns>(p, o, L.weights, st);
+        run_back_plan<E, C, Form::kColumns>(p, o, L.weights, st);
     }
+}
+
+template <typename E> void run_gated_back(const GatedBackArgs &a, hipStream_t st)
+{
+    const GatedBackLayout L = make_gated_back_layout(a.n, a.d, a.f, a.type);
+    L.wide ? run_gated_back_of<E, float>(a, L, st) : run_gated_back_of<E, E>(a, L, st);
 }
 
 template <typename E> __global__ __launch_bounds__(256) void gated_zero_kernel(E *p, int64_t stride, int64_t rows, int64_t cols)
@@ -710,13 +726,20 @@ Plan plan_product(int64_t rows, int64_t columns, int64_t slices, bool wide, bool
     return best;
 }
 
+// The rounding of 16-bit operands is as large as that of the outputs, 1.41 times it together where sums are of many unlike
+// terms; over a few outputs that can come out at twice it (bf16, dx of 100 values 3.0e-3 against 1.6e-3).  So small products of
+// few outputs take fp32 operands (2^27 points x features x features are 7 us of matrix instructions).
+constexpr int64_t kFewOutputs = 4096;
+constexpr double kFewProducts = 134217728.0;
+
 GatedBackLayout make_gated_back_layout(int64_t n, int64_t d, int64_t f, Elem type)
 {
-    const int es = elem_bytes(type);
     GatedBackLayout L = {};
+    L.wide = type == Elem::kF32 || ((n * d < kFewOutputs || f * d < kFewOutputs) && double(n) * double(d) * double(f) < kFewProducts);
+    const int es = L.wide ? 4 : 2;
     L.fp = (f * es + kSlice - 1) / kSlice * kSlice / es;
     L.np = (n * es + kSlice - 1) / kSlice * kSlice / es;
-    L.dp = pad16(d, es);
+    L.dp = pad16(d, elem_bytes(type)); // of the inputs' pieces
     L.x = plan_product(n, d, slices_of(2 * L.fp * es), es == 4, true, true);
     L.weights = plan_product(2 * L.fp, d, slices_of(n * es), es == 4, true, true);
     size_t at = 0;
