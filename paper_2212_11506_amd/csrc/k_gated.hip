@@ -299,25 +299,37 @@ __global__ __launch_bounds__(kShortThreads) void gated_short_kernel(Product p, G
 int64_t tiles_of(int64_t rows, int64_t cols, int m, int n) { return (rows + m - 1) / m * ((cols + n - 1) / n); }
 
 // A few points (few_points): 1 x 512 to 2048 bf16 4.4 us, of which a launch is 2.5.
-template <typename E> __global__ __launch_bounds__(kFewWaves *kWave) void gated_few_kernel(Product p, GatedOut o)
+template <typename E, int kI> __global__ __launch_bounds__(kFewWaves *kWave) void gated_few_kernel(Product p, GatedOut o)
 {
-    __shared__ float s_sum[kFewWaves][2][kFewPoints * 16];
-    const int64_t feature = int64_t(blockIdx.x) * 16;
+    __shared__ float s_sum[kFewWaves][2][kI][256];
+    const int64_t feature = int64_t(blockIdx.x) * 16, first = int64_t(blockIdx.y) * (16 * kI);
     const int lane = lane_id();
-    const char *row = p.A + (lane % 16 < p.rows ? lane % 16 : p.rows - 1) * p.a_stride;
-    const auto x = [&](int32_t slice, int half) {
+    const char *row[kI];
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+        const int64_t point = first + 16 * i + lane % 16;
+        row[i] = p.A + (point < p.rows ? point : p.rows - 1) * p.a_stride;
+    }
+    const auto x = [&](int32_t slice, int half, int i) {
         const int64_t k = int64_t(slice) * kSlice + half * 64 + lane / 16 * 16;
-        return int64_t(slice + 1) * kSlice <= p.bytes ? inner_piece(row + k) : any_piece<E>(row, k, p.bytes);
+        return int64_t(slice + 1) * kSlice <= p.bytes ? inner_piece(row[i] + k) : any_piece<E>(row[i], k, p.bytes);
     };
-    typename Ops<E>::Acc acc[2] = {};
-    few_points<E, 2>(p, feature, [] {}, x, acc);
-    float v[2];
-    few_join(acc, s_sum, v);
-    const int64_t point = int(threadIdx.x) / 16, at = feature + int(threadIdx.x) % 16;
-    if (point >= p.rows || at >= p.features) return;
-    static_cast<E *>(o.h)[point * o.h_stride + at] = E(activate<E>(v[0], o.act) * v[1]);
-    if (o.a) static_cast<E *>(o.a)[point * o.a_stride + at] = E(v[0]);
-    if (o.b) static_cast<E *>(o.b)[point * o.b_stride + at] = E(v[1]);
+    typename Ops<E>::Acc acc[2][kI] = {};
+    few_points<E, 2, kI>(p, feature, [] {}, x, acc);
+    few_put(acc, s_sum);
+    for (int t = int(threadIdx.x); t < 256 * kI; t += kFewWaves * kWave) {
+        const int64_t point = first + t / 16, at = feature + t % 16;
+        if (point >= p.rows || at >= p.features) continue;
+        const float a = few_sum(s_sum, 0, t / 256, t % 256), b = few_sum(s_sum, 1, t / 256, t % 256);
+        static_cast<E *>(o.h)[point * o.h_stride + at] = E(activate<E>(a, o.act) * b);
+        if (o.a) static_cast<E *>(o.a)[point * o.a_stride + at] = E(a);
+        if (o.b) static_cast<E *>(o.b)[point * o.b_stride + at] = E(b);
+    }
+}
+template <typename E, int kI> void run_gated_few(const GatedArgs &a, hipStream_t st)
+{
+    const dim3 grid(uint32_t((a.f + 15) / 16), uint32_t((a.n + 16 * kI - 1) / (16 * kI)));
+    gated_few_kernel<E, kI><<<grid, kFewWaves * kWave, 0, st>>>(gated_product(a, int64_t(sizeof(E))), gated_out<E, 1>(a));
 }
 
 template <typename E, int kHalves> void run_gated_short(const GatedArgs &a, hipStream_t st)
@@ -346,14 +358,12 @@ template <typename E, int kHalves> void run_gated_short(const GatedArgs &a, hipS
 template <typename E> void run_gated_type(const GatedArgs &a, hipStream_t st)
 {
     const int64_t es = int64_t(sizeof(E));
-    if (a.n <= kFewPoints) {
-        gated_few_kernel<E><<<uint32_t((a.f + 15) / 16), kFewWaves * kWave, 0, st>>>(gated_product(a, es), gated_out<E, 1>(a));
-        return;
-    }
+    if (a.n <= kFewPoints) return run_gated_few<E, 1>(a, st);
     if (a.d * es >= 16 && a.d * es <= 128 && (a.a == nullptr) == (a.b == nullptr))
         return a.d * es <= 64 ? run_gated_short<E, 1>(a, st) : run_gated_short<E, 2>(a, st);
     const bool any = !aligned16(a.x, a.x_stride * es) || !aligned16(a.gate, a.gate_stride * es) || !aligned16(a.up, a.up_stride * es)
                      || a.d * es % 16 != 0;
+    if (few_tiles(a.n, a.f, !any || es == 4)) return run_gated_few<E, kFewRows / 16>(a, st);
     const bool near = a.x_stride * es <= kLargeStride && a.gate_stride * es <= kLargeStride && a.up_stride * es <= kLargeStride;
     const Side side = plan_product(a.n, 2 * a.f, slices_of(a.d * es), es == 4, false, !any && near).side;
     if (any) {

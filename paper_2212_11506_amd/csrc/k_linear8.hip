@@ -180,15 +180,16 @@ template <typename E, typename T, bool kAny, Tail kTail = Tail::kWhole> void run
 
 // A few points (few_points).  X: their type; int8 as they are, else the block quantises them into LDS while its weights are
 // under way to it: one launch (1 x 2048 to 8192 bf16 8.4 us, of which a launch is 2.5; by two 12 and the gap between them).
-template <typename E, typename X>
+template <typename E, typename X, int kI>
 __global__ __launch_bounds__(kFewWaves *kWave) void linear8_few_kernel(Product p, LinearOut o)
 {
     constexpr bool kWhole = sizeof(X) == 1;
     constexpr int kThreads = kFewWaves * kWave;
-    __shared__ int32_t s_sum[kFewWaves][1][kFewPoints * 16];
+    static_assert(kWhole || kI == 1, "few points are quantised");
+    __shared__ int32_t s_sum[kFewWaves][1][kI][256];
     __shared__ float s_scale[kFewPoints], s_max[kFewWaves];
     __shared__ __align__(16) int8_t s_x[kWhole ? 16 : kFewValues];
-    const int64_t feature = int64_t(blockIdx.x) * 16;
+    const int64_t feature = int64_t(blockIdx.x) * 16, first = int64_t(blockIdx.y) * (16 * kI);
     const int lane = lane_id(), point_row = lane % 16 < p.rows ? lane % 16 : int(p.rows) - 1;
     const int32_t width = p.slices * kSlice;
     const auto quantise_all = [&] {
@@ -226,28 +227,33 @@ __global__ __launch_bounds__(kFewWaves *kWave) void linear8_few_kernel(Product p
             __syncthreads();
         }
     };
-    const char *row = p.A + point_row * p.a_stride;
-    const auto x = [&](int32_t slice, int half) {
+    const char *row[kI];
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+        const int64_t point = first + 16 * i + lane % 16;
+        row[i] = p.A + (point < p.rows ? point : p.rows - 1) * p.a_stride;
+    }
+    const auto x = [&](int32_t slice, int half, int i) {
         const int64_t k = int64_t(slice) * kSlice + half * 64 + lane / 16 * 16;
         if constexpr (kWhole)
-            return int64_t(slice + 1) * kSlice <= p.bytes ? inner_piece(row + k) : any_piece<int8_t>(row, k, p.bytes);
+            return int64_t(slice + 1) * kSlice <= p.bytes ? inner_piece(row[i] + k) : any_piece<int8_t>(row[i], k, p.bytes);
         else
             return *reinterpret_cast<const Piece *>(s_x + point_row * width + k);
     };
-    Ops<int8_t>::Acc acc[1] = {};
-    few_points<int8_t, 1>(p, feature, quantise_all, x, acc);
-    int32_t v[1];
-    few_join(acc, s_sum, v);
-    const int64_t point = int(threadIdx.x) / 16, at = feature + int(threadIdx.x) % 16;
-    const int64_t held = at < p.features ? at : p.features - 1;
-    float bias = 0.0f;
-    if (o.bias) bias = o.wide_bias ? static_cast<const float *>(o.bias)[held] : float(static_cast<const E *>(o.bias)[held]);
-    if (point >= p.rows || at >= p.features) return;
-    const float s = kWhole ? o.x_scale[point] : s_scale[point];
-    static_cast<E *>(o.out)[point * o.stride + at] = E(float(v[0]) * s * o.w_scale[at] + bias);
+    Ops<int8_t>::Acc acc[1][kI] = {};
+    few_points<int8_t, 1, kI>(p, feature, quantise_all, x, acc);
+    few_put(acc, s_sum);
+    for (int t = int(threadIdx.x); t < 256 * kI; t += kThreads) {
+        const int64_t point = first + t / 16, at = feature + t % 16, held = at < p.features ? at : p.features - 1;
+        float bias = 0.0f;
+        if (o.bias) bias = o.wide_bias ? static_cast<const float *>(o.bias)[held] : float(static_cast<const E *>(o.bias)[held]);
+        if (point >= p.rows || at >= p.features) continue;
+        const float s = kWhole ? o.x_scale[point] : s_scale[t / 16 % kFewPoints];
+        static_cast<E *>(o.out)[point * o.stride + at] = E(float(few_sum(s_sum, 0, t / 256, t % 256)) * s * o.w_scale[at] + bias);
+    }
 }
 
-template <typename E, typename X> void run_linear_few(const LinearArgs &a, const void *x, int64_t x_stride, hipStream_t st)
+template <typename E, typename X, int kI> void run_linear_few(const LinearArgs &a, const void *x, int64_t x_stride, hipStream_t st)
 {
     Product p = {};
     p.A = static_cast<const char *>(x);
@@ -265,25 +271,27 @@ template <typename E, typename X> void run_linear_few(const LinearArgs &a, const
     o.out = a.out;
     o.stride = a.out_stride;
     o.wide_bias = a.bias_type == Elem::kF32;
-    linear8_few_kernel<E, X><<<uint32_t((a.f + 15) / 16), kFewWaves * kWave, 0, st>>>(p, o);
+    const dim3 grid(uint32_t((a.f + 15) / 16), uint32_t((a.n + 16 * kI - 1) / (16 * kI)));
+    linear8_few_kernel<E, X, kI><<<grid, kFewWaves * kWave, 0, st>>>(p, o);
 }
 
 template <typename E> bool few_and_quantised(const LinearArgs &a, const QuantiseArgs &q, hipStream_t st)
 {
     if (!linear_few(a.n, a.d)) return false;
     if (q.type == Elem::kF32)
-        run_linear_few<E, float>(a, q.x, q.x_stride, st);
+        run_linear_few<E, float, 1>(a, q.x, q.x_stride, st);
     else if (q.type == Elem::kF16)
-        run_linear_few<E, f16>(a, q.x, q.x_stride, st);
+        run_linear_few<E, f16, 1>(a, q.x, q.x_stride, st);
     else
-        run_linear_few<E, bf16>(a, q.x, q.x_stride, st);
+        run_linear_few<E, bf16, 1>(a, q.x, q.x_stride, st);
     return true;
 }
 
 template <typename E> void run_linear_type(const LinearArgs &a, hipStream_t st)
 {
-    if (a.n <= kFewPoints) return run_linear_few<E, int8_t>(a, a.x, a.x_stride, st);
+    if (a.n <= kFewPoints) return run_linear_few<E, int8_t, 1>(a, a.x, a.x_stride, st);
     const bool any = !aligned16(a.x, a.x_stride) || !aligned16(a.w, a.w_stride) || a.d % 16 != 0;
+    if (few_tiles(a.n, a.f, !any)) return run_linear_few<E, int8_t, kFewRows / 16>(a, a.x, a.x_stride, st);
     const Side side = plan_product(a.n, a.f, slices_of(a.d), false, false, !any && a.x_stride <= kLargeStride && a.w_stride <= kLargeStride).side;
     if (any) {
         if (side == Side::kMiddle) return run_linear<E, TileMiddle, true>(a, st);

@@ -399,15 +399,16 @@ __device__ inline void multiply_tile(const Product &a, int32_t bi, int32_t bj, t
 }
 
 // ------------------------------------------------------------------ few points
-// Up to 16 points: a block makes 16 features of all of them, its waves share K out in slices, every kFewWaves-th each, and take
-// fragments straight from memory: the weights are read once, a line of 16 rows at a time, four of them in flight a wave.  Rows
-// of any alignment.  x(slice, half): the points' fragment, zeros behind the end.
-constexpr int kFewWaves = 8, kFewAtOnce = 4; // slices of one matrix in flight, of two half of that
-// ready(): called once by every wave while the first weights are under way.
-template <typename E, int kMats, typename G, typename F>
-__device__ inline void few_points(const Product &a, int64_t feature, G ready, F x, typename Ops<E>::Acc (&acc)[kMats])
+// A block makes 16 features of 16 kI points, its waves share K out in slices, every kFewWaves-th each, and take fragments
+// straight from memory: the weights are read once for so many points, a line of 16 rows at a time.  Rows of any alignment.
+// For up to 16 points; and for more where tiles are so few that each one's slices, one after another, are what takes time.
+// x(slice, half, i): the points' fragment, zeros behind the end.  ready(): called once by every wave while the first weights
+// are under way.
+constexpr int kFewWaves = 8;
+template <typename E, int kMats, int kI, typename G, typename F>
+__device__ inline void few_points(const Product &a, int64_t feature, G ready, F x, typename Ops<E>::Acc (&acc)[kMats][kI])
 {
-    constexpr int kAtOnce = kFewAtOnce / kMats;
+    constexpr int kAtOnce = kI > 1 ? 1 : 4 / kMats; // slices in flight
     const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id();
     const int64_t at = feature + lane % 16, held = at < a.features ? at : a.features - 1;
     const char *row[2] = {a.B + held * a.b_stride, kMats == 2 ? a.B2 + held * a.b2_stride : nullptr};
@@ -431,36 +432,59 @@ __device__ inline void few_points(const Product &a, int64_t feature, G ready, F 
     if (w < a.slices) load(w);
     ready();
     for (int32_t s0 = w; s0 < a.slices;) {
+        if constexpr (kI > 1) {
+            Piece now[kMats][2], p[2][kI];
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-            if (s0 + u * kFewWaves >= a.slices) break;
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const Piece p = x(s0 + u * kFewWaves, h);
+                for (int i = 0; i < kI; ++i) p[h][i] = x(s0, h, i);
 #pragma unroll
-                for (int m = 0; m < kMats; ++m) acc[m] = Ops<E>::mul(p, q[u][m][h], acc[m]);
+            for (int m = 0; m < kMats; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) now[m][h] = q[0][m][h];
+            s0 += kFewWaves;
+            if (s0 < a.slices) load(s0);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int m = 0; m < kMats; ++m)
+#pragma unroll
+                    for (int i = 0; i < kI; ++i) acc[m][i] = Ops<E>::mul(p[h][i], now[m][h], acc[m][i]);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                if (s0 + u * kFewWaves >= a.slices) break;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const Piece p = x(s0 + u * kFewWaves, h, 0);
+#pragma unroll
+                    for (int m = 0; m < kMats; ++m) acc[m][0] = Ops<E>::mul(p, q[u][m][h], acc[m][0]);
+                }
             }
+            s0 += kFewWaves * kAtOnce;
+            if (s0 < a.slices) load(s0);
         }
-        s0 += kFewWaves * kAtOnce;
-        if (s0 < a.slices) load(s0);
     }
 }
-// The waves' sums, in order: value(t, m) for the block's threads t < 256, of point t / 16 and feature t % 16
-template <typename V, int kMats, typename Acc>
-__device__ inline void few_join(const Acc (&acc)[kMats], V (*s_sum)[kMats][kFewPoints * 16], V (&sum)[kMats])
+// The waves' sums, in order: sum[m] of the block's thread t < 256 for block i of points, of point 16 i + t / 16 and feature t % 16
+template <typename V, int kMats, int kI, typename Acc>
+__device__ inline void few_put(const Acc (&acc)[kMats][kI], V (*s_sum)[kMats][kI][256])
 {
-    const int w = int(threadIdx.x) / kWave, lane = lane_id(), t = int(threadIdx.x) % (kFewPoints * 16);
+    const int w = int(threadIdx.x) / kWave, lane = lane_id();
 #pragma unroll
     for (int m = 0; m < kMats; ++m)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s_sum[w][m][(lane / 16 * 4 + r) * 16 + lane % 16] = acc[m][r];
+        for (int i = 0; i < kI; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s_sum[w][m][i][(lane / 16 * 4 + r) * 16 + lane % 16] = acc[m][i][r];
     __syncthreads();
+}
+template <typename V, int kMats, int kI> __device__ inline V few_sum(const V (*s_sum)[kMats][kI][256], int m, int i, int t)
+{
+    V sum = V(0);
 #pragma unroll
-    for (int m = 0; m < kMats; ++m) {
-        sum[m] = V(0);
-#pragma unroll
-        for (int k = 0; k < kFewWaves; ++k) sum[m] += s_sum[k][m][t];
-    }
+    for (int k = 0; k < kFewWaves; ++k) sum += s_sum[k][m][i][t];
+    return sum;
 }
 
 // ------------------------------------------------------------------ large tiles

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2212_11506_amd as bh
-from tests.test_gpu_gated import check_backward, check_forward, mat, operands
+from tests.test_gpu_gated import ACTS, U, act64, act_error, check_backward, check_forward, close, mat, operands
 from tests.test_gpu_linear8 import check, ints, quantise64
 from tests.test_gpu_linear8 import mat as values
 
@@ -81,3 +81,51 @@ def test_linear_of_one_type_to_another(kind, dtype):
         out = bh.linear_i8(x, w, ws, dtype=dtype)
         assert out.dtype == dtype
         check(*quantise64(x), w, ws, None, out)
+
+
+# more than a few points, and few tiles: one block of 64 points, several, an end inside one, and one feature more than is shared
+FEW = [(17, 128, 15), (64, 4096, 33), (65, 260, 256), (130, 72, 700), (1000, 144, 250), (1025, 400, 240), (1025, 400, 241), (64, 272, 4097)]
+
+
+@pytest.mark.parametrize("dtype", HALVES + [torch.float32])
+@pytest.mark.parametrize("n,d,f", FEW + [(65, 777, 100), (200, 131, 20)])
+def test_forward_of_few_tiles(n, d, f, dtype):
+    x, gate, up = mat(n, d, dtype, 1, 8), mat(f, d, dtype, 2, 16, d ** -0.5), mat(f, d, dtype, 3, 0, d ** -0.5)
+    for kind in ACTS:
+        got = bh.gated_layer(x, gate, up, kind, keep=True)
+        check_forward(x, gate, up, kind, *got)
+        assert torch.equal(bh.gated_layer(x, gate, up, kind), got[0])
+    x = x.clone()
+    x[n // 2, d - 1] = float("nan")  # stays in its row
+    h = bh.gated_layer(x, gate, up, kind)
+    assert bool(h[n // 2].isnan().all()) and torch.equal(h[: n // 2], got[0][: n // 2]) and torch.equal(h[n // 2 + 1 :], got[0][n // 2 + 1 :])
+
+
+@pytest.mark.parametrize("dtype", HALVES + [torch.float32])
+@pytest.mark.parametrize("n,d,f", FEW)
+def test_linear_of_few_tiles(n, d, f, dtype):
+    w, ws, bias = ints(f, d, 2), values(f, 1, torch.float32, 4).abs().flatten() / d, values(f, 1, dtype, 5).flatten()
+    q, s = ints(n, d, 1), values(n, 1, torch.float32, 3).abs().flatten()
+    check(q, s, w, ws, bias, bh.linear_i8(q, w, ws, s, bias, dtype=dtype))
+    x = values(n, d, dtype, 6)
+    check(*quantise64(x), w, ws, bias, bh.linear_i8(x, w, ws, bias=bias))
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("n,d,f", [(2000, 10, 40), (3000, 1, 2), (20, 200, 300), (1, 2000, 700), (63, 65, 2000), (20_000, 50, 80)])
+def test_backward_of_few_outputs(n, d, f, dtype):
+    """Sums of few outputs are formed from gradients of 32 bits: nothing but the outputs is rounded to the type."""
+    o = operands(n, d, f, dtype)
+    for kind in ACTS:
+        got = bh.gated_layer_backward(*o, kind)
+        dh, x, gate, up, a, b = (t.double() for t in o)
+        value, slope, size = act64(a, kind)
+        rel = act_error(a, kind, dtype) + 4 * U
+        da, db = dh * b * slope, dh * value
+        ta, tb = rel * (dh * b).abs() * size, rel * db.abs()
+        k = (2 * f + 8) * U
+        close(got[0], da @ gate + db @ up, ta @ gate.abs() + tb @ up.abs() + k * (da.abs() @ gate.abs() + db.abs() @ up.abs()), dtype)
+        k = (n + 8) * U
+        for grad, e, t in ((got[1], da, ta), (got[2], db, tb)):
+            e, t = e.T.contiguous(), t.T.contiguous()
+            close(grad, e @ x, t @ x.abs() + k * (e.abs() @ x.abs()), dtype)
