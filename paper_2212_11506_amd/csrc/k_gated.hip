@@ -76,14 +76,46 @@ struct GatedOut {
     void *h, *a, *b;
     int64_t h_stride, a_stride, b_stride;
     Act act;
-    bool vec_h, vec_a, vec_b;
+    bool vec_h, vec_a, vec_b, inner;
 };
+
+// A tile inside the outputs
+template <typename E, typename T, Act kAct, bool kKeep>
+__device__ inline void put_inner(int32_t bi, int32_t bj, const GatedOut &o, const typename Ops<E>::Acc (&acc)[T::kI][T::kJ])
+{
+    typedef InnerRuns<T, Form::kDual> Runs;
+    constexpr int kRun = Runs::kTogether;
+    const Runs runs(bi, bj);
+    const auto to_h = runs.template to<E>(o.h, o.h_stride), to_a = runs.template to<E>(o.a, o.a_stride), to_b = runs.template to<E>(o.b, o.b_stride);
+#pragma unroll
+    for (int i = 0; i < T::kI; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float a[kRun], b[kRun], h[kRun];
+#pragma unroll
+            for (int e = 0; e < kRun; ++e) {
+                a[e] = acc[i][e][r];
+                b[e] = acc[i][kRun + e][r];
+                h[e] = activate<E>(a[e], kAct) * b[e];
+            }
+            to_h.put(i, r, h);
+            if constexpr (kKeep) {
+                to_a.put(i, r, a);
+                to_b.put(i, r, b);
+            }
+        }
+}
 
 template <typename E, typename T, bool kAny, Tail kTail>
 __global__ __launch_bounds__(T::kThreads) void gated_kernel(Product p, GatedOut o)
 {
     constexpr int kRun = T::kJ / 2; // features of a lane
     each_tile<E, T, Form::kDual, kAny, kTail>(p, [&](int32_t bi, int32_t bj, typename Ops<E>::Acc (&acc)[T::kI][T::kJ]) {
+        if (o.inner && tile_inside<T, Form::kDual>(p, bi, bj)) {
+            if (o.act == Act::kSilu)
+                return o.a ? put_inner<E, T, Act::kSilu, true>(bi, bj, o, acc) : put_inner<E, T, Act::kSilu, false>(bi, bj, o, acc);
+            return o.a ? put_inner<E, T, Act::kGelu, true>(bi, bj, o, acc) : put_inner<E, T, Act::kGelu, false>(bi, bj, o, acc);
+        }
         each_run<T, Form::kDual>(bi, bj, [&](int64_t point, int64_t feature, int i, int r) {
             if (point >= p.rows) return;
             float a[kRun], b[kRun], h[kRun];
@@ -114,6 +146,8 @@ template <typename E, int kRun> GatedOut gated_out(const GatedArgs &a)
     o.vec_h = runs_aligned<E, kRun>(a.h, a.h_stride);
     o.vec_a = runs_aligned<E, kRun>(a.a, a.a_stride);
     o.vec_b = runs_aligned<E, kRun>(a.b, a.b_stride);
+    o.inner = runs_inner<E, kRun>(a.h, a.h_stride) && runs_inner<E, kRun>(a.a, a.a_stride) && runs_inner<E, kRun>(a.b, a.b_stride)
+              && (a.a == nullptr) == (a.b == nullptr);
     return o;
 }
 
@@ -321,7 +355,7 @@ template <typename E, int kI> __global__ __launch_bounds__(kFewWaves *kWave) voi
         const int64_t point = first + t / 16, at = feature + t % 16;
         if (point >= p.rows || at >= p.features) continue;
         const float a = few_sum(s_sum, 0, t / 256, t % 256), b = few_sum(s_sum, 1, t / 256, t % 256);
-        static_cast<E *>(o.h)[point * o.h_stride + at] = E(activate<E>(a, o.act) * b);
+        static_cast<E *>(o.h)[point * o.h_stride + at] = rounded<E>(activate<E>(a, o.act) * b);
         if (o.a) static_cast<E *>(o.a)[point * o.a_stride + at] = E(a);
         if (o.b) static_cast<E *>(o.b)[point * o.b_stride + at] = E(b);
     }
@@ -483,7 +517,7 @@ struct BackOut {
     float *part;
     int64_t stride, stride2, first2, f, features; // f: rows of an output
     int64_t part_rows;
-    bool vec;
+    bool vec, inner;
 };
 
 // C: of the operands, E: of the outputs
@@ -492,6 +526,23 @@ __global__ __launch_bounds__(T::kThreads) void gated_back_kernel(Product p, Back
 {
     constexpr int kRun = T::kJ;
     each_tile<C, T, kForm, false, Tail::kWhole>(p, [&](int32_t bi, int32_t bj, typename Ops<C>::Acc (&acc)[T::kI][T::kJ]) {
+        if constexpr (kForm == Form::kRows) {
+            if (o.inner && tile_inside<T, kForm>(p, bi, bj)) {
+                typedef std::conditional_t<kPart, float, E> Out;
+                const auto to = InnerRuns<T, kForm>(bi, bj).template to<Out>(kPart ? o.part + int64_t(blockIdx.y) * o.part_rows * o.features : o.out,
+                                                                             kPart ? o.features : o.stride);
+#pragma unroll
+                for (int i = 0; i < T::kI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float v[kRun];
+#pragma unroll
+                        for (int e = 0; e < kRun; ++e) v[e] = acc[i][e][r];
+                        to.put(i, r, v);
+                    }
+                return;
+            }
+        }
         each_run<T, kForm>(bi, bj, [&](int64_t row, int64_t feature, int i, int r) {
             if (row >= p.rows) return;
             float v[kRun];
@@ -581,6 +632,7 @@ template <typename E, typename C, Form kForm> void run_back_plan(const Product &
     o.part_rows = kForm == Form::kRows ? o.f : 2 * o.f;
     const bool pairs = o.features % 2 == 0 && aligned_to(2 * es, o.out, o.stride * es) && aligned_to(2 * es, o.out2, o.stride2 * es);
     if (plan.splits > 1) o.vec = o.features % 4 == 0; // of the partial sums
+    o.inner = o.vec && (plan.splits > 1 ? o.features * 4 : o.stride * es) <= kLargeStride;
     if (plan.side == Side::kLarge)
         run_back<E, C, TileLarge, kForm>(p, o, plan.splits, st);
     else if (plan.side == Side::kMiddle)

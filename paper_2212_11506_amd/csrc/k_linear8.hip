@@ -113,7 +113,7 @@ struct LinearOut {
     const void *bias;
     void *out;
     int64_t stride;
-    bool wide_bias, vec;
+    bool wide_bias, vec, inner;
 };
 
 template <typename E, typename T, bool kAny, Tail kTail>
@@ -121,6 +121,31 @@ __global__ __launch_bounds__(T::kThreads) void linear8_kernel(Product p, LinearO
 {
     constexpr int kRun = T::kJ;
     each_tile<int8_t, T, Form::kRows, kAny, kTail>(p, [&](int32_t bi, int32_t bj, Ops<int8_t>::Acc (&acc)[T::kI][T::kJ]) {
+        if (o.inner && tile_inside<T, Form::kRows>(p, bi, bj)) {
+            const InnerRuns<T, Form::kRows> runs(bi, bj);
+            const auto to = runs.template to<E>(o.out, o.stride);
+            float scale[kRun], bias[kRun];
+#pragma unroll
+            for (int e = 0; e < kRun; ++e) {
+                const int64_t at = runs.feature + runs.lane_feature + e;
+                scale[e] = o.w_scale[at];
+                bias[e] = !o.bias ? 0.0f : o.wide_bias ? static_cast<const float *>(o.bias)[at] : float(static_cast<const E *>(o.bias)[at]);
+            }
+#pragma unroll
+            for (int i = 0; i < T::kI; ++i) {
+                float s[4]; // before the stores, which a load behind them waits for (one by one: 416 us a call for 400)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[r] = (o.x_scale + runs.row + (16 * i + r))[runs.lane_row];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float v[kRun];
+#pragma unroll
+                    for (int e = 0; e < kRun; ++e) v[e] = float(acc[i][e][r]) * s[r] * scale[e] + bias[e];
+                    to.put(i, r, v);
+                }
+            }
+            return;
+        }
         float scale[kRun], bias[kRun];
         each_run<T, Form::kRows>(bi, bj, [&](int64_t point, int64_t feature, int i, int r) {
             if (i == 0 && r == 0) {
@@ -173,6 +198,7 @@ template <typename E, typename T, bool kAny, Tail kTail = Tail::kWhole> void run
         o.out = static_cast<E *>(a.out) + from * a.out_stride;
         o.stride = a.out_stride;
         o.wide_bias = a.bias_type == Elem::kF32;
+        o.inner = runs_inner<E, T::kJ>(a.out, a.out_stride);
         o.vec = runs_aligned<E, T::kJ>(a.out, a.out_stride);
         linear8_kernel<E, T, kAny, kTail><<<blocks_of<T>(uint32_t(p.down) * uint32_t(p.across)), T::kThreads, lds, st>>>(p, o);
     }
@@ -249,7 +275,7 @@ __global__ __launch_bounds__(kFewWaves *kWave) void linear8_few_kernel(Product p
         if (o.bias) bias = o.wide_bias ? static_cast<const float *>(o.bias)[held] : float(static_cast<const E *>(o.bias)[held]);
         if (point >= p.rows || at >= p.features) continue;
         const float s = kWhole ? o.x_scale[point] : s_scale[t / 16 % kFewPoints];
-        static_cast<E *>(o.out)[point * o.stride + at] = E(float(few_sum(s_sum, 0, t / 256, t % 256)) * s * o.w_scale[at] + bias);
+        static_cast<E *>(o.out)[point * o.stride + at] = rounded<E>(float(few_sum(s_sum, 0, t / 256, t % 256)) * s * o.w_scale[at] + bias);
     }
 }
 

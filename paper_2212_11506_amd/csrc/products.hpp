@@ -758,6 +758,14 @@ template <typename T, Form kForm, typename F> __device__ inline void each_run(in
         for (int r = 0; r < 4; ++r) f(point + 16 * i + r, feature, i, r);
 }
 
+// An output of the value: rounded from 32 bits.  In fp16 the compiler rounds some products once, from all of their bits, and
+// others not; what is stored is not to depend on which.
+template <typename E> __device__ inline E rounded(float v)
+{
+    if constexpr (std::is_same<E, f16>::value) asm("" : "+v"(v));
+    return E(v);
+}
+
 // N consecutive values to p, of which `count` exist; vec: aligned to 16 bytes, or to N values where those are less
 template <typename E, int N> __device__ inline void store_run(E *p, const float (&v)[N], int64_t count, bool vec)
 {
@@ -770,15 +778,63 @@ template <typename E, int N> __device__ inline void store_run(E *p, const float 
         for (int h = 0; h < N / kV; ++h) {
             Pack x;
 #pragma unroll
-            for (int e = 0; e < kV; ++e) x.v[e] = E(v[h * kV + e]);
+            for (int e = 0; e < kV; ++e) x.v[e] = rounded<E>(v[h * kV + e]);
             reinterpret_cast<Pack *>(p)[h] = x;
         }
         return;
     }
 #pragma unroll
     for (int e = 0; e < N; ++e)
-        if (e < count) p[e] = E(v[e]);
+        if (e < count) p[e] = rounded<E>(v[e]);
 }
+
+// Tiles inside the output whose runs are vectors: a run's place is the wave's, the same for all lanes, and one 32-bit offset of
+// the lane's for all rows (strides are kLargeStride at most).  With each run's own 64-bit place, count and branches a tile of
+// 256 x 256 took 5 us more (16384 x 2048 to 8192 bf16, with three outputs, 914 us for 836; 70001 x 2000 to 2000 in 8 bits 445
+// for 400).
+template <typename T, Form kForm> __device__ inline bool tile_inside(const Product &a, int32_t bi, int32_t bj)
+{
+    constexpr int kN = kForm == Form::kDual ? T::kN / 2 : T::kN;
+    return int64_t(bi) * T::kM + T::kM <= a.rows && int64_t(bj) * kN + kN <= a.features;
+}
+template <typename T, Form kForm> struct InnerRuns {
+    static constexpr int kTogether = kForm == Form::kDual ? T::kJ / 2 : T::kJ;
+    int64_t row, feature; // the wave's first
+    uint32_t lane_row, lane_feature;
+    __device__ inline InnerRuns(int32_t bi, int32_t bj)
+    {
+        const int w = int(uniform(threadIdx.x / kWave)), lane = lane_id();
+        row = int64_t(bi) * T::kM + w / T::kWn * (T::kI * 16);
+        feature = int64_t(bj) * (kForm == Form::kDual ? T::kN / 2 : T::kN) + w % T::kWn * (16 * kTogether);
+        lane_row = uint32_t(lane / 16 * 4);
+        lane_feature = uint32_t(lane % 16 * kTogether);
+    }
+    // kTogether values of the lane's point 16 i + r
+    template <typename E> struct To {
+        char *first;
+        int64_t stride; // bytes
+        uint32_t lane;
+        __device__ inline void put(int i, int r, const float (&v)[kTogether]) const
+        {
+            constexpr int kV = 16 / int(sizeof(E)) < kTogether ? 16 / int(sizeof(E)) : kTogether;
+            struct alignas(sizeof(E) * kV) Pack {
+                E v[kV];
+            };
+#pragma unroll
+            for (int h = 0; h < kTogether / kV; ++h) {
+                Pack x;
+#pragma unroll
+                for (int e = 0; e < kV; ++e) x.v[e] = rounded<E>(v[h * kV + e]);
+                *reinterpret_cast<Pack *>(first + (16 * i + r) * stride + lane + h * sizeof(Pack)) = x;
+            }
+        }
+    };
+    template <typename E> __device__ inline To<E> to(void *out, int64_t stride) const
+    {
+        const int64_t s = stride * int64_t(sizeof(E));
+        return {static_cast<char *>(out) + row * s + feature * int64_t(sizeof(E)), s, lane_row * uint32_t(s) + lane_feature * uint32_t(sizeof(E))};
+    }
+};
 
 inline bool aligned_to(int bytes, const void *p, int64_t stride_bytes)
 {
@@ -790,6 +846,12 @@ template <typename E, int N> inline bool runs_aligned(const void *p, int64_t str
 {
     constexpr int kBytes = int(sizeof(E)) * N;
     return aligned_to(kBytes < 16 ? kBytes : 16, p, stride * int64_t(sizeof(E)));
+}
+
+// ... and InnerRuns: no output is such, too
+template <typename E, int N> inline bool runs_inner(const void *p, int64_t stride)
+{
+    return !p || (runs_aligned<E, N>(p, stride) && stride * int64_t(sizeof(E)) <= kLargeStride);
 }
 
 inline int64_t slices_of(int64_t bytes) { return (bytes + kSlice - 1) / kSlice; }
