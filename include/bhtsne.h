@@ -615,9 +615,10 @@ int bhtsne_gated_layer(const void *x, int64_t x_stride, const void *gate, int64_
  *   dh, a, b  n x f of `type`, x n x d; a stride of 0 as above.
  *   dx        n x d, nullable; dgate, dup  f x d, each nullable, overwritten
  *             (zero for n = 0); one output at least is wanted.
- * da and db are rounded to `type` before the products; the sums over features
- * and points are fp32, those over parts of the points are joined in a fixed
- * order: the same inputs give the same bits.  The workspace is
+ * da and db are rounded to `type` before the products, but for small products
+ * of few outputs (n d or f d below 4096 and n d f below 2^27), where they stay
+ * fp32; the sums over features and points are fp32, those over parts of the
+ * points are joined in a fixed order: the same inputs give the same bits.  The workspace is
  * bhtsne_gated_layer_workspace_size bytes (256-byte aligned; 0 for sizes out of
  * range).  No output overlaps an input or another output.
  * Errors: BHTSNE_EINVAL, BHTSNE_EWORKSPACE, BHTSNE_EDEVICE. */
@@ -648,7 +649,7 @@ int bhtsne_quantise_rows(const void *x, int64_t x_stride, int64_t n, int64_t d, 
  *   bias     f values of bias_type (`type` or BHTSNE_F32), nullable.
  *   out      n x f of `type`.
  * The sums are exact (32-bit integers; d <= 131071), the scales are applied in
- * fp32.  0 <= n < 2^31, 1 <= f < 2^31, strides < 2^31.  out overlaps no input.
+ * fp32.  0 <= n < 2^31, 1 <= f <= 2^26, strides < 2^31.  out overlaps no input.
  * The workspace (bhtsne_linear_i8_workspace_size bytes, 256-byte aligned; 0 for
  * sizes out of range) is needed where x is not BHTSNE_I8 and it is more than 256
  * bytes: a few points need none.

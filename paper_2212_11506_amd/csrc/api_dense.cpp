@@ -206,7 +206,7 @@ int bhtsne_linear_i8(const void *x, int64_t x_stride, int x_type, const float *x
                      const float *w_scale, const void *bias, int64_t n, int64_t d, int64_t f, int type, int bias_type, void *out,
                      int64_t out_stride, void *workspace, size_t workspace_bytes, hipStream_t stream)
 {
-    if (n < 0 || n > kMost || d < 1 || d > kLinearMaxDepth || f < 1 || f > kMost) return BHTSNE_EINVAL;
+    if (n < 0 || n > kMost || d < 1 || d > kLinearMaxDepth || f < 1 || f > kLinearMaxFeatures) return BHTSNE_EINVAL;
     const bool whole = x_type == BHTSNE_I8;
     if (!type_ok(type) || (!whole && !type_ok(x_type)) || (bias_type != type && bias_type != BHTSNE_F32)) return BHTSNE_EINVAL;
     if (!input_ok(x, x_stride, n, d, x_type) || !output_ok(const_cast<int8_t *>(w), w_stride, f, d, BHTSNE_I8)) return BHTSNE_EINVAL;

@@ -102,6 +102,7 @@ void launch_gated_layer_backward(const GatedBackArgs &a, hipStream_t st);
 // ---------------------------------------------------------- products of 8-bit integers
 constexpr int64_t kLinearSlice = 128;       // values of a slice of a row
 constexpr int64_t kLinearMaxDepth = 131071; // (-128)^2 so many times stays below 2^31
+constexpr int64_t kLinearMaxFeatures = int64_t(1) << 26; // a launch has fewer than 2^32 threads: 512 for 16 features
 
 // A few points, which their product quantises itself (kFewValues values, with the rows' padding)
 constexpr int64_t kFewPoints = 16, kFewValues = 8192;

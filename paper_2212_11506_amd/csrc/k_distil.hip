@@ -8,7 +8,8 @@
 // A row's logits are read once: forward with the running maximum and sum of a
 // softmax in each lane, joined over the lanes and, where few rows are shared out
 // over several blocks, over the parts by a second launch.  Backward reads and
-// writes each once, four operations and an exponential a value.  HBM bounds both.
+// writes each once, four operations and an exponential a value.  HBM bounds both:
+// 4096 x 70001 bf16 105 us forward (5.5 TB/s), 2048 x 70000 124 backward (4.6).
 // Maximum and sum of a lane are fp32 (300 terms at most a lane, in vectors), the
 // joined sum and the list's terms fp64; the only rounding to fewer bits is that of dz.
 #include <type_traits>

@@ -4,8 +4,11 @@
 //   product:   out = s_i t_j sum_k q_ik w_jk + bias_j
 //
 // The sums are exact: 32-bit integers hold 131071 products of 8-bit values.  The
-// quantisation reads a row once, into the registers of a wave or a block, and is
-// bound by HBM; the product runs on the matrix cores' 8-bit instructions.
+// quantisation reads a row once, into the registers of a wave or a block: 70001 x
+// 2000 bf16, 422 MB, 93 to 104 us (4.5 TB/s), bound by HBM and by the vector
+// instructions, which are issued in 98 % of that time.  The product runs on the matrix
+// cores' 8-bit instructions: 70001 x 2000 to 2000, 0.56 TOP, 310 us, nine rounds of
+// CUs of which each ends with outputs that nothing covers.
 #include "products.hpp"
 
 namespace bht {

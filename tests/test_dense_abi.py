@@ -57,7 +57,9 @@ def test_gated_layer_workspace_size():
     size = bh.gated_layer_workspace_size
     assert size(-1, 8, 8) == size(4, 0, 8) == size(4, 8, 0) == size(1 << 31, 8, 8) == size(4, 65537, 8) == size(4, 8, 65537) == 0
     assert size(0, 8, 8) > 0 and size(5, 7, 9) % 256 == 0
-    assert size(1000, 50, 60, torch.float32) > size(1000, 50, 60, torch.float16) == size(1000, 50, 60, torch.bfloat16)
+    assert size(1000, 500, 600, torch.float32) > size(1000, 500, 600, torch.float16) == size(1000, 500, 600, torch.bfloat16)
+    # few outputs: operands of 32 bits for every type
+    assert size(1000, 50, 60, torch.float16) == size(1000, 50, 60, torch.bfloat16) >= (2 * 1000 * 60 + 2 * 60 * 50) * 4
 
 
 def quantise(**bad):
@@ -86,6 +88,11 @@ def test_linear_i8_refuses(bad):
 @pytest.mark.parametrize("bad", [dict(ws=None), dict(ws=FAKE + 128), dict(wsb=64)])
 def test_linear_i8_wants_its_workspace(bad):
     assert linear(**bad) == bh.BHTSNE_EWORKSPACE
+
+
+def test_linear_i8_refuses_features_beyond_a_launch():
+    for n in (1, 100):
+        assert linear(n=n, f=(1 << 26) + 1, os=1 << 30) == bh.BHTSNE_EINVAL
 
 
 def test_linear_i8_workspace_size():
