@@ -34,9 +34,9 @@ template <typename E> __device__ inline float sigmoid(float a)
 }
 // Half of erfc(|a| / sqrt(2)) = exp(-a^2 / 2) t P(t) with t = 1 / (1 + c |a|): P is fitted to the scaled function over all
 // |a| by least squares, reweighted towards the largest relative error: of degree 8 for fp32 (1.3e-7; with its own roundings
-// 4.6e-7), of degree 5 for outputs of 16 bits (1.8e-5, a twenty-seventh of fp16's rounding).  No difference of near values, so a far
-// below zero keeps its digits.  The exponential is a square, so that values near the smallest fp32 and bf16 numbers do not
-// vanish in the instruction.
+// 4.6e-7), of degree 5 for outputs of 16 bits (1.8e-5, a twenty-seventh of fp16's rounding).  No difference of near values, so
+// a far below zero keeps its digits.  The exponential is a square, so that values near the smallest fp32 and bf16 numbers do
+// not vanish in the instruction.
 template <typename E> __device__ inline float tail(float a, float &root)
 {
     constexpr bool kWide = sizeof(E) == 4;
@@ -194,10 +194,11 @@ template <typename E, typename T, bool kAny, Tail kTail = Tail::kWhole> void run
 // lane, runs of 64 bytes of a point.  A row's last piece is its last 16 bytes, of which only those count that the piece before
 // does not have: the others are masked out, in points and weights alike.
 //
-// 1.3M x 50 to 200 fp16, gelu: 240 to 269 us for 650 MB, by the card.  Bound by the vector instructions, which a CU issues in 89 %
-// of the time: some 17 an output for the activation and the product, two of them at a quarter of the rate, and 7 blocks of 32
-// features for 6.25.  Rows of 400 bytes end inside a line, so 608 MB are written for 520.  Weights in registers and the points past a block's waves in step, by LDS
-// and a barrier, took 301 us (7 waves on 4 SIMDs); without LDS, 429: each lane's 16 bytes a request of its own.
+// 1.3M x 50 to 200 fp16, gelu: 240 to 269 us for 650 MB, by the card.  Bound by the vector instructions, which a CU issues in
+// 89 % of the time: some 17 an output for the activation and the product, two of them at a quarter of the rate, and 7 blocks
+// of 32 features for 6.25.  Rows of 400 bytes end inside a line, so 608 MB are written for 520.  Weights in registers and the
+// points past a block's waves in step, by LDS and a barrier, took 301 us (7 waves on 4 SIMDs); without LDS, 429: each lane's
+// 16 bytes a request of its own.
 constexpr int kShortFeatures = 256; // of a block at most
 constexpr int kShortThreads = 512;
 constexpr int kShortBlocks = 2 * 2 * kCus;
@@ -414,8 +415,8 @@ template <typename E> void run_gated_type(const GatedArgs &a, hipStream_t st)
 
 // ------------------------------------------------------------------ backward: operands
 // One launch: da and db side by side, a row a point; the weights transposed and side by side; x with rows that are padded to
-// 16 bytes, where its own are not.  Blocks are dealt to the three by their number.  Bound by HBM: 70000 x 512 to 2048 bf16, 0.86 GB
-// read and 0.58 written, 276 us.
+// 16 bytes, where its own are not.  Blocks are dealt to the three by their number.  Bound by HBM: 70000 x 512 to 2048 bf16,
+// 0.86 GB read and 0.58 written, 276 us.
 constexpr int kT = 64; // side of a tile that is transposed
 
 struct Operands {
@@ -515,9 +516,10 @@ template <typename E, typename C> __global__ __launch_bounds__(256) void gated_o
 
 // ------------------------------------------------------------------ backward: products
 // dx: rows as they are.  The weights' gradients: rows 0 .. f - 1 are dgate's, rows from `first2` on dup's (dx: none are).
-// kPart: fp32 partial sums of a split, of 2 f rows (dx: of n).  70000 x 512 to 2048 bf16, 0.29 TFLOP each: dx 284 us, whose 550 tiles
-// are three rounds of CUs, the weights 262 (1.1 PFLOP/s) and 12 to join 8 parts; their operands' rows are read across (kColumns),
-// which costs no copy of da, db and x on its other side (with one 1417 us a pass, so 991 then).
+// kPart: fp32 partial sums of a split, of 2 f rows (dx: of n).  70000 x 512 to 2048 bf16, 0.29 TFLOP each: dx 284 us, whose
+// 550 tiles are three rounds of CUs, the weights 262 to 318 (1.1 to 0.9 PFLOP/s) by the card, and 14 to join 8 parts; their
+// operands' rows are read across (kColumns), which costs no copy of da, db and x on its other side (with one 1417 us a pass,
+// so 991 then).
 struct BackOut {
     void *out, *out2;
     float *part;

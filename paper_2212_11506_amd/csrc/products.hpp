@@ -501,9 +501,10 @@ template <typename V, int kMats, int kI> __device__ inline V few_sum(const V (*s
 // A CU has one such block, which goes on to its next tile: the loads of the last two slices' steps are the next tile's
 // first, so they are under way while the outputs are formed and stored.  Rows have two slices at least.
 //
-// 8192 x 8192 to 8192 at 1.47 PFLOP/s in 16 bits and 2.6 POP/s in 8; matrix cores busy 75 % of the CUs' time over 8750 points a
-// part.  At 512 to 2048 deep the outputs count, during which they rest: 1.0 to 1.3.  (Blocks started apart from each other, by
-// XCD or by CU, so that some would store while others multiply: no difference.)
+// 8192 x 8192 to 8192 at 1.47 PFLOP/s in 16 bits and 2.6 POP/s in 8; matrix cores busy 75 % of the CUs' time at 4096 deep (dx
+// of 70000 x 512), 54 % in a product across the rows (8750 points a part).  At 512 to 2048 deep the outputs count, during
+// which they rest: 1.0 to 1.3.  (Blocks started apart from each other, by XCD or by CU, so that some would store while others
+// multiply: no difference.)
 constexpr int kRegion = 128 * kSlice;
 constexpr int64_t kLargeStride = int64_t(1) << 23; // bytes
 enum class Tail { kWhole, kFirst, kZeros };
