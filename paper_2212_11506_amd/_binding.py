@@ -997,7 +997,8 @@ def gated_layer(x: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, activatio
     with keep (h, a, b), a = x gate^T and b = x up^T being what the backward pass takes.
 
     h's gradient goes to x, gate and up through bhtsne_gated_layer_backward (once); a and b have none, and neither has a
-    call with out."""
+    call with out.  A backward pass that is captured in a graph wants leaves that no graph recorded outside of the capture
+    still holds, as every one of torch's does."""
     if torch.is_grad_enabled() and (x.requires_grad or gate.requires_grad or up.requires_grad):
         if out is not None:
             raise ValueError("out has no gradient: leave it out, or call under torch.no_grad()")
@@ -1188,7 +1189,7 @@ def distil_loss(logits: torch.Tensor, idx: torch.Tensor, teacher: torch.Tensor, 
     idx (n x k int32; outside [0, v): absent).
 
     loss's gradient goes to the logits through bhtsne_distil_loss_backward (once); lse has none, and the teacher neither:
-    one whose graph torch records is refused."""
+    one whose graph torch records is refused.  For a captured backward pass see gated_layer."""
     _no_gradient(teacher, "the teacher of distil_loss")
     if logits.requires_grad and torch.is_grad_enabled():
         return _DistilLoss.apply(logits, idx, teacher, float(temperature), workspace)
@@ -1199,7 +1200,7 @@ def _distil_loss(logits, idx, teacher, temperature, workspace=None):
     lib = load_library()
     args, kind, teacher_kind, gpu = _lists(logits, idx, teacher)
     n, v = logits.shape
-    loss, lse = logits.new_empty((2, n), dtype=torch.float32).unbind(0)
+    loss, lse = logits.new_empty(n, dtype=torch.float32), logits.new_empty(n, dtype=torch.float32)  # two: each may be changed in place
     if workspace is not None:
         need = _workspace_bytes(workspace, gpu)
     else:

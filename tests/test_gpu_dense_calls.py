@@ -227,3 +227,50 @@ def test_ints_of_a_wider_array():
     q = ints(50, 70, 3, 5)
     out = bh.linear_i8(q, w, ws, torch.ones(50, device=DEV))
     assert torch.equal(out.double(), q.double() @ w.double().T.contiguous())
+
+
+def test_a_loss_changed_in_place():
+    z, idx, u = lists(70, 400, 9, torch.float32, 8)
+    scale = torch.rand(70, device=DEV) + 0.5
+    leaf = z.clone().requires_grad_()
+    loss, lse = bh.distil_loss(leaf, idx, u)
+    kept = lse.clone()
+    loss.mul_(scale)
+    loss.sum().backward()
+    assert torch.equal(lse, kept) and torch.equal(leaf.grad, bh.distil_loss_backward(scale, z, idx, u, kept))
+
+
+@pytest.mark.parametrize("n", [3, 70, 900])
+def test_a_captured_training_step(n):
+    """Forward and backward of all nodes in one graph, replayed on other points, against the eager pass."""
+    d, f, v, k, t = 48, 96, 200, 9, torch.bfloat16
+    weights = [mat(*s, t, 2 + i, 0, s[1] ** -0.5) for i, s in enumerate(((f, d), (f, d), (v, f), (v, f)))]
+    idx, u = lists(n, v, k, t, 5)[1:]
+    points = [mat(n, d, t, 20 + i) for i in range(3)]
+
+    def step(x, leaves):
+        h = bh.gated_layer(x, leaves[0], leaves[1])
+        z = bh.gated_layer(h, leaves[2], leaves[3], "gelu")
+        loss = bh.distil_loss(z, idx, u, 0.5)[0].sum()
+        return [loss.detach(), *torch.autograd.grad(loss, leaves)]
+
+    wants = [[r.clone() for r in step(x, [w.clone().requires_grad_() for w in weights])] for x in points]
+    x, leaves = points[0].clone(), [w.clone().requires_grad_() for w in weights]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            step(x, leaves)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(x, leaves)
+    for turn in (1, 0, 2, 2):
+        x.copy_(points[turn])
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (p, q) in enumerate(zip(got[1:], wants[turn][1:])):
+            assert torch.equal(p, q), (turn, i)
+        assert abs(float(got[0]) - float(wants[turn][0])) <= n * 2.0 ** -23 * max(1.0, abs(float(wants[turn][0])))
+        step(x, [w.clone().requires_grad_() for w in weights])
