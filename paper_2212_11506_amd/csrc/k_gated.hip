@@ -641,8 +641,8 @@ template <typename E, typename C, Form kForm> void run_back_plan(const Product &
     const bool pairs = o.features % 2 == 0 && aligned_to(2 * es, o.out, o.stride * es) && aligned_to(2 * es, o.out2, o.stride2 * es);
     if (plan.splits > 1) o.vec = o.features % 4 == 0; // of the partial sums
     o.inner = o.vec && (plan.splits > 1 ? o.features * 4 : o.stride * es) <= kLargeStride;
-    if (plan.side == Side::kLarge)
-        run_back<E, C, TileLarge, kForm>(p, o, plan.splits, st);
+    if (std::is_same<E, C>::value && plan.side == Side::kLarge)
+        run_back<E, E, TileLarge, kForm>(p, o, plan.splits, st);
     else if (plan.side == Side::kMiddle)
         run_back<E, C, TileMiddle, kForm>(p, o, plan.splits, st);
     else
@@ -810,8 +810,9 @@ GatedBackLayout make_gated_back_layout(int64_t n, int64_t d, int64_t f, Elem typ
     L.fp = (f * es + kSlice - 1) / kSlice * kSlice / es;
     L.np = (n * es + kSlice - 1) / kSlice * kSlice / es;
     L.dp = pad16(d, elem_bytes(type)); // of the inputs' pieces
-    L.x = plan_product(n, d, slices_of(2 * L.fp * es), es == 4, true, true);
-    L.weights = plan_product(2 * L.fp, d, slices_of(n * es), es == 4, true, true);
+    const bool large = !L.wide || type == Elem::kF32; // small products never gain by it
+    L.x = plan_product(n, d, slices_of(2 * L.fp * es), es == 4, true, large);
+    L.weights = plan_product(2 * L.fp, d, slices_of(n * es), es == 4, true, large);
     size_t at = 0;
     const auto take = [&](int64_t count, int bytes) {
         const size_t here = at;

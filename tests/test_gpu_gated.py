@@ -260,3 +260,18 @@ def test_in_torch_graph():
         g, = torch.autograd.grad(y.square().sum(), x, create_graph=True)
         with pytest.raises(RuntimeError):
             g.sum().backward()
+
+
+@pytest.mark.parametrize("n,d,f", [(300, 50, 200), (3, 64, 33), (300, 300, 512), (1000, 144, 250), (2600, 512, 2304)])
+def test_one_of_the_products_kept(n, d, f):
+    """The C call may leave out a or b: the others are written as with both."""
+    lib, t, stream = bh.load_library(), torch.float16, torch.cuda.current_stream().cuda_stream
+    x, gate, up = mat(n, d, t, 1), mat(f, d, t, 2, 0, d ** -0.5), mat(f, d, t, 3, 0, d ** -0.5)
+    want = bh.gated_layer(x, gate, up, "gelu", keep=True)
+    for which in (1, 2):
+        got = [torch.full((n, f), -7.0, dtype=t, device=DEV) for _ in range(3)]
+        a, b = (got[1].data_ptr(), None) if which == 1 else (None, got[2].data_ptr())
+        assert lib.bhtsne_gated_layer(x.data_ptr(), d, gate.data_ptr(), d, up.data_ptr(), d, n, d, f, 1, 1, got[0].data_ptr(), f, a, f, b, f, stream) == 0
+        torch.cuda.synchronize()
+        check_forward(x, gate, up, "gelu", got[0], got[1] if which == 1 else want[1], got[2] if which == 2 else want[2])
+        assert bool((got[3 - which] == -7.0).all())
