@@ -48,8 +48,8 @@ struct Plan {
 constexpr int kMostSplits = 64;
 constexpr int64_t kMostPart = int64_t(1) << 29; // bytes of partial sums
 // rows x columns of output, of `slices` slices of K each; wide: fp32 operands.  may_split: partial sums have a place;
-// may_large: operands are aligned for tiles of 256.
-Plan plan_product(int64_t rows, int64_t columns, int64_t slices, bool wide, bool may_split, bool may_large);
+// most: the largest side that may be taken (256 of aligned operands).
+Plan plan_product(int64_t rows, int64_t columns, int64_t slices, bool wide, bool may_split, Side most);
 
 // Whether a product of more than a few points has so few tiles that its slices are better shared out over the waves of blocks
 // of kFewRows points x 16 features: while there is a CU for each block.  Then 64 x 1024 to 512 takes 19.5 us for 27.7 (fp32),

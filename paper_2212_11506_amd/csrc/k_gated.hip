@@ -403,7 +403,7 @@ template <typename E> void run_gated_type(const GatedArgs &a, hipStream_t st)
                      || a.d * es % 16 != 0;
     if (few_tiles(a.n, a.f, !any || es == 4)) return run_gated_few<E, kFewRows / 16>(a, st);
     const bool near = a.x_stride * es <= kLargeStride && a.gate_stride * es <= kLargeStride && a.up_stride * es <= kLargeStride;
-    const Side side = plan_product(a.n, 2 * a.f, slices_of(a.d * es), es == 4, false, !any && near).side;
+    const Side side = plan_product(a.n, 2 * a.f, slices_of(a.d * es), es == 4, false, any || !near ? Side::kMiddle : Side::kLarge).side;
     if (any) {
         if (side == Side::kMiddle) return run_gated<E, TileMiddle, true>(a, st);
         return run_gated<E, TileSmall, true>(a, st);
@@ -641,8 +641,10 @@ template <typename E, typename C, Form kForm> void run_back_plan(const Product &
     const bool pairs = o.features % 2 == 0 && aligned_to(2 * es, o.out, o.stride * es) && aligned_to(2 * es, o.out2, o.stride2 * es);
     if (plan.splits > 1) o.vec = o.features % 4 == 0; // of the partial sums
     o.inner = o.vec && (plan.splits > 1 ? o.features * 4 : o.stride * es) <= kLargeStride;
-    if (std::is_same<E, C>::value && plan.side == Side::kLarge)
-        run_back<E, E, TileLarge, kForm>(p, o, plan.splits, st);
+    if constexpr (!std::is_same<E, C>::value)
+        run_back<E, C, TileSmall, kForm>(p, o, plan.splits, st);
+    else if (plan.side == Side::kLarge)
+        run_back<E, C, TileLarge, kForm>(p, o, plan.splits, st);
     else if (plan.side == Side::kMiddle)
         run_back<E, C, TileMiddle, kForm>(p, o, plan.splits, st);
     else
@@ -762,7 +764,7 @@ template <typename E> void run_gated_zero(const GatedBackArgs &a, hipStream_t st
 // long, which is all that counts there).  A tile of 256 alone on a CU: 1.0, and 1.42 with all CUs at it.  One of 128: 0.73,
 // two on a CU 1.1, and so on by half that each.  One of 64: 0.32, two 0.45, then 0.2 each.  A tile's start and end take 9, 5 and
 // 2.5; joining partial sums a launch and their bytes.
-Plan plan_product(int64_t rows, int64_t columns, int64_t slices, bool wide, bool may_split, bool may_large)
+Plan plan_product(int64_t rows, int64_t columns, int64_t slices, bool wide, bool may_split, Side most)
 {
     const auto slice_time = [&](Side side, int64_t blocks) {
         const int64_t each = (blocks + kCus - 1) / kCus; // of the busiest CU
@@ -774,7 +776,7 @@ Plan plan_product(int64_t rows, int64_t columns, int64_t slices, bool wide, bool
     Plan best = {Side::kSmall, 1};
     double least = INFINITY;
     for (const Side side : {Side::kSmall, Side::kMiddle, Side::kLarge}) {
-        if (side == Side::kLarge && !may_large) continue;
+        if (int(side) > int(most)) continue;
         const int64_t tiles = tiles_of(rows, columns, int(side), int(side));
         const double fixed = side == Side::kSmall ? 2.5 : side == Side::kMiddle ? 5.0 : 9.0;
         const int at_once = side == Side::kSmall ? 3 * kCus : side == Side::kMiddle ? 2 * kCus : kCus;
@@ -810,9 +812,9 @@ GatedBackLayout make_gated_back_layout(int64_t n, int64_t d, int64_t f, Elem typ
     L.fp = (f * es + kSlice - 1) / kSlice * kSlice / es;
     L.np = (n * es + kSlice - 1) / kSlice * kSlice / es;
     L.dp = pad16(d, elem_bytes(type)); // of the inputs' pieces
-    const bool large = !L.wide || type == Elem::kF32; // small products never gain by it
-    L.x = plan_product(n, d, slices_of(2 * L.fp * es), es == 4, true, large);
-    L.weights = plan_product(2 * L.fp, d, slices_of(n * es), es == 4, true, large);
+    const Side most = L.wide && type != Elem::kF32 ? Side::kSmall : Side::kLarge; // small products gain nothing by more
+    L.x = plan_product(n, d, slices_of(2 * L.fp * es), es == 4, true, most);
+    L.weights = plan_product(2 * L.fp, d, slices_of(n * es), es == 4, true, most);
     size_t at = 0;
     const auto take = [&](int64_t count, int bytes) {
         const size_t here = at;

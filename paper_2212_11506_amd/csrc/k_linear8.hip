@@ -321,7 +321,8 @@ template <typename E> void run_linear_type(const LinearArgs &a, hipStream_t st)
     if (a.n <= kFewPoints) return run_linear_few<E, int8_t, 1>(a, a.x, a.x_stride, st);
     const bool any = !aligned16(a.x, a.x_stride) || !aligned16(a.w, a.w_stride) || a.d % 16 != 0;
     if (few_tiles(a.n, a.f, !any)) return run_linear_few<E, int8_t, kFewRows / 16>(a, a.x, a.x_stride, st);
-    const Side side = plan_product(a.n, a.f, slices_of(a.d), false, false, !any && a.x_stride <= kLargeStride && a.w_stride <= kLargeStride).side;
+    const Side side = plan_product(a.n, a.f, slices_of(a.d), false, false,
+                                   any || a.x_stride > kLargeStride || a.w_stride > kLargeStride ? Side::kMiddle : Side::kLarge).side;
     if (any) {
         if (side == Side::kMiddle) return run_linear<E, TileMiddle, true>(a, st);
         return run_linear<E, TileSmall, true>(a, st);
