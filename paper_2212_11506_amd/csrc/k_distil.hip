@@ -103,10 +103,12 @@ template <int kThreads> __device__ inline double block_sum(double v, double *s_s
 }
 
 // The teacher's softmax over a row's list: the largest u of a class that exists, and the sum of exp((u - top) / T).
-// Entries whose index is no class are absent.
+// Entries whose index is no class are absent.  A list without entries has the sum 0, and no other has: the largest u adds 1
+// (NaN leaves no trace in the top, but makes the sum NaN).
 struct List {
     float top;
     double sum;
+    __device__ inline bool empty() const { return sum == 0.0; }
 };
 template <typename TE, int kThreads>
 __device__ inline List list_of(const DistilArgs &a, int64_t row, float c, double *s_sum, float *s_max)
@@ -198,7 +200,7 @@ __device__ inline void finish(const DistilArgs &a, int64_t row, float m, double 
         const double t = double(exp2_fast(above * c)) / l.sum;
         const double zj = double(float(z[there ? at : 0]));
         const double term = t * (double(above) / a.temperature - log_sum - zj / a.temperature + lse);
-        sum += l.top == -INFINITY || t == 0.0 ? 0.0 : term;
+        sum += l.empty() || t == 0.0 ? 0.0 : term;
     }
     sum = block_sum<kThreads>(sum, s_sum);
     if (threadIdx.x == 0) a.loss[row] = float(sum);
@@ -270,7 +272,7 @@ __global__ __launch_bounds__(kThreads) void distil_back_kernel(DistilArgs a)
         const E *z = static_cast<const E *>(a.logits) + row * a.stride;
         E *out = static_cast<E *>(a.out) + row * a.out_stride;
         const List l = list_of<TE, kThreads>(a, row, c, s_sum, s_max);
-        const bool empty = l.top == -INFINITY;
+        const bool empty = l.empty();
         // q = exp2((z - top) c) factor, with lse T as a high and a low part
         const double g = double(a.dloss[row]) / a.temperature, lse = double(a.lse_in[row]) * a.temperature;
         const float high = float(lse), f = float(g), low = high == high && fabsf(high) < INFINITY ? float(lse - double(high)) : 0.0f;

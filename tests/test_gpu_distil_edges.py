@@ -1,0 +1,50 @@
+"""The loss from neighbour lists where lists or logits leave the finite numbers."""
+import math
+
+import pytest
+import torch
+
+import paper_2212_11506_amd as bh
+from tests.test_gpu_distil import TYPES, case
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+NAN = float("nan")
+ROWS = [(6, 40), (6, 3000), (3, 30_000)]  # a wave's, a block's, shared out over several blocks
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,v", ROWS)
+@pytest.mark.parametrize("k", [1, 2, 90])
+def test_a_list_of_nan_is_no_empty_list(n, v, k, dtype):
+    """NaN in every entry that a row has: NaN is what the loss and the listed places' gradient are, not 0."""
+    k = min(k, v)
+    for teacher in {dtype, torch.float32}:
+        z, idx, u = case(n, v, k, dtype, n + v + k, 3, teacher)
+        dloss = torch.ones(n, device=DEV)
+        want, lse = bh.distil_loss(z, idx, u)
+        dz = bh.distil_loss_backward(dloss, z, idx, u, lse)
+        u[0] = NAN
+        if k > 1:  # beside entries that are absent by either mark
+            u[1], idx[1, 1:] = NAN, -1
+            u[2], u[2, 1:] = NAN, -math.inf
+        bad = [0, 1, 2] if k > 1 else [0]
+        good = [r for r in range(n) if r not in bad]
+        loss, lse2 = bh.distil_loss(z, idx, u)
+        got = bh.distil_loss_backward(dloss, z, idx, u, lse)
+        assert torch.equal(lse, lse2) and torch.equal(loss[good], want[good]) and torch.equal(got[good], dz[good])
+        assert bool(loss[bad].isnan().all())
+        for r in bad:
+            listed = torch.zeros(v, dtype=torch.bool, device=DEV)
+            listed[idx[r][idx[r] >= 0].long()] = True
+            nan = torch.zeros(v, dtype=torch.bool, device=DEV)
+            nan[idx[r][(idx[r] >= 0) & u[r].isnan()].long()] = True
+            assert bool(got[r][nan].isnan().all())
+            # what is not listed has its probability alone, as in any row with a list: half a step of bf16, and some u of the
+            # exponential and lse, are below 2^-7; half the spacing of fp16's subnormals is 2^-25
+            q = torch.exp(z[r].double() - lse[r].double())
+            assert bool(((got[r].double() - q).abs() <= 2.0 ** -7 * q + 2.0 ** -24)[~listed].all())
+        # through torch's graph too
+        leaf = z.clone().requires_grad_()
+        bh.distil_loss(leaf, idx, u)[0].sum().backward()
+        assert bool(leaf.grad[0].isnan().any())
