@@ -594,6 +594,7 @@ int bhtsne_muon_step(const bhtsne_matrices *W, const bhtsne_matrices *G, const b
  *     a = x gate^T,  b = x up^T,  h = act(a) b,
  *     act(a) = a / (1 + exp(-a))              (BHTSNE_SILU)
  *            = a / 2 (1 + erf(a / sqrt(2)))   (BHTSNE_GELU)
+ * (act of plus infinity is infinity, of minus infinity NaN.)
  *   x         n x d of `type`; x_stride >= d, or 0 for one row that stands for all.
  *   gate, up  f x d (a row a feature), of the same type.
  *   h         n x f; a, b  n x f, each nullable: what the backward pass takes.
@@ -612,6 +613,7 @@ int bhtsne_gated_layer(const void *x, int64_t x_stride, const void *gate, int64_
 /* The backward pass, from a and b as they are given:
  *     da = dh b act'(a),  db = dh act(a),
  *     dx = da gate + db up,  dgate = da^T x,  dup = db^T x
+ * (act' of an infinite a is NaN.)
  *   dh, a, b  n x f of `type`, x n x d; a stride of 0 as above.
  *   dx        n x d, nullable; dgate, dup  f x d, each nullable, overwritten
  *             (zero for n = 0); one output at least is wanted.

@@ -51,13 +51,14 @@ template <typename E> __device__ inline float tail(float a, float &root)
     root = __builtin_amdgcn_exp2f(a * (a * -0.360673760f));
     return p * t * root * root;
 }
-// (value) a Phi(a), which is max(a, 0) - |a| tail(a), and (slope) Phi(a) + a phi(a); or the sigmoid's
+// (value) a Phi(a) and (slope) Phi(a) + a phi(a); or the sigmoid's.  Phi is the tail or one less it, and a its factor: max(a, 0) -
+// |a| tail(a) is an instruction less (1.3M x 50 to 200 fp16 263 us for 270), but infinity less infinity times 0 above zero.
+__device__ inline float phi_of(float a, float h) { return a < 0.0f ? h : 1.0f - h; }
 template <typename E> __device__ inline float activate(float a, Act act)
 {
     if (act == Act::kSilu) return a * sigmoid<E>(a);
     float root;
-    const float h = tail<E>(a, root), above = a < 0.0f ? 0.0f : a; // NaN stays
-    return fmaf(-fabsf(a), h, above);
+    return a * phi_of(a, tail<E>(a, root));
 }
 template <typename E> __device__ inline void activate_both(float a, Act act, float &value, float &slope)
 {
@@ -67,8 +68,8 @@ template <typename E> __device__ inline void activate_both(float a, Act act, flo
         slope = s * (1.0f + a * (1.0f - s));
     } else {
         float root;
-        const float h = tail<E>(a, root), phi = a < 0.0f ? h : 1.0f - h;
-        value = fmaf(-fabsf(a), h, a < 0.0f ? 0.0f : a);
+        const float phi = phi_of(a, tail<E>(a, root));
+        value = a * phi;
         slope = phi + a * (0.398942280f * root * root);
     }
 }
