@@ -180,12 +180,13 @@ __device__ inline void part_of(const DistilArgs &a, int part, int64_t &from, int
     to = from + each < a.v ? from + each : a.v;
 }
 
-// The row's outputs from its maximum and sum
+// The row's outputs from its maximum and sum.  The loss takes a listed logit's distance from the maximum before anything is
+// added to it: next to logits as large as the type's lowest value, for classes that are masked out, the sum's logarithm vanishes.
 template <typename E, typename TE, int kThreads>
 __device__ inline void finish(const DistilArgs &a, int64_t row, float m, double s, float c, double *s_sum, float *s_max)
 {
-    const double lse = double(m) / a.temperature + log(s);
-    if (a.lse && threadIdx.x == 0) a.lse[row] = float(lse);
+    const double log_s = log(s);
+    if (a.lse && threadIdx.x == 0) a.lse[row] = float(double(m) / a.temperature + log_s);
     if (!a.loss) return;
     const List l = list_of<TE, kThreads>(a, row, c, s_sum, s_max);
     const E *z = static_cast<const E *>(a.logits) + row * a.stride;
@@ -199,7 +200,7 @@ __device__ inline void finish(const DistilArgs &a, int64_t row, float m, double 
         const float above = (there ? float(u[j]) : -INFINITY) - l.top; // NaN where the list is empty
         const double t = double(exp2_fast(above * c)) / l.sum;
         const double zj = double(float(z[there ? at : 0]));
-        const double term = t * (double(above) / a.temperature - log_sum - zj / a.temperature + lse);
+        const double term = t * (double(above) / a.temperature - log_sum + (double(m) - zj) / a.temperature + log_s);
         sum += l.empty() || t == 0.0 ? 0.0 : term;
     }
     sum = block_sum<kThreads>(sum, s_sum);

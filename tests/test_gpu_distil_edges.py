@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2212_11506_amd as bh
-from tests.test_gpu_distil import TYPES, case
+from tests.test_gpu_distil import TYPES, case, check_forward, reference
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -48,3 +48,41 @@ def test_a_list_of_nan_is_no_empty_list(n, v, k, dtype):
         leaf = z.clone().requires_grad_()
         bh.distil_loss(leaf, idx, u)[0].sum().backward()
         assert bool(leaf.grad[0].isnan().any())
+
+
+def far_rows(n, v, dtype, T, seed):
+    """Rows that leave no class (the type's lowest value everywhere), nearly none, or lie as far off as the type reaches."""
+    z, idx, u = case(n, v, min(v, 7), dtype, seed)
+    lowest, largest = torch.finfo(dtype).min, torch.finfo(dtype).max
+    z[0] = lowest
+    z[1], z[1, idx[1, :3].long()] = lowest, z[1, idx[1, :3].long()]
+    z[2] = largest
+    if n > 3:
+        z[3], z[3, idx[3, 0].long()] = lowest / 2, lowest
+        z[4] = z[4] * (largest / 64)
+        z[5] = z[5] * T + largest / 1024
+    return z, idx, u
+
+
+def shifted(z):
+    """The same softmax, in 64 bits: logits less their row's largest."""
+    return z.double() - z.double().amax(1, keepdim=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,v", ROWS)
+def test_loss_of_rows_far_off(n, v, dtype):
+    for T in (1.0, 0.05, 1e-6, 300.0):
+        z, idx, u = far_rows(n, v, dtype, T, n + v)
+        loss, _ = bh.distil_loss(z, idx, u, T)
+        near = shifted(z)
+        lse = torch.logsumexp(near / T, 1).float()
+        # a loss beyond the largest fp32 number is rounded to infinity
+        held = reference(near, idx, u, T)[5].sum(1) <= torch.finfo(torch.float32).max
+        assert bool((loss.cpu()[~held] == math.inf).all())
+        held = held.to(DEV)
+        check_forward(near[held], idx[held], u[held], T, (loss[held], lse[held]))
+    # no class at all: log v less the list's entropy
+    t = torch.softmax(u[0].double(), 0)
+    loss = bh.distil_loss(z, idx, u)[0]
+    assert abs(float(loss[0]) - float((t * t.log()).sum()) - math.log(v)) <= 100 * 2.0 ** -24 * math.log(v)
