@@ -676,8 +676,14 @@ int bhtsne_linear_i8(const void *x, int64_t x_stride, int x_type, const float *x
  *            the loss 0 and a gradient of zero; one that has a NaN the loss NaN.  A class that is listed more than
  *            once gets the sum of its shares; the loss takes each entry by itself.
  *            (idx and teacher may be null for k = 0.)
- *   loss, lse  n fp32 values, each nullable, one at least is wanted.
- *   dloss    n fp32 values; lse as the forward call gave it.
+ *   loss, lse  n fp32 values, each nullable, one at least (or kept) is wanted.
+ *   kept     n x 2 fp32, nullable: a row's largest logit m and s = sum exp((z - m) / T),
+ *            of which lse = m / T + log s is the rounded sum.
+ *   dloss    n fp32 values; lse, and kept, as the forward call gave them.  q is
+ *            exp(z / T - lse), which the rounding of lse makes off by |lse| 2^-24
+ *            of itself: a unit of fp32 for ordinary logits, but all of it for a row
+ *            of 1e38 or of masked classes alone.  With kept, q of a row whose |lse|
+ *            is 16 or more is exp((z - m) / T) / s, which is not.
  *   dlogits  n x v of `type`; may be logits (with their stride).
  * Input strides are >= the row's length, or 0 for one row that stands for all.
  * 0 <= n < 2^31, 1 <= v < 2^31, 0 <= k <= 2048, strides < 2^31, T in [1e-6, 1e6].
@@ -691,10 +697,19 @@ int bhtsne_distil_loss(const void *logits, int64_t stride, int64_t n, int64_t v,
                        const void *teacher, int64_t teacher_stride, int64_t k, double temperature, int type,
                        int teacher_type, float *loss, float *lse, void *workspace, size_t workspace_bytes,
                        hipStream_t stream);
+int bhtsne_distil_loss_kept(const void *logits, int64_t stride, int64_t n, int64_t v, const int32_t *idx,
+                            int64_t idx_stride, const void *teacher, int64_t teacher_stride, int64_t k,
+                            double temperature, int type, int teacher_type, float *loss, float *lse, float *kept,
+                            void *workspace, size_t workspace_bytes, hipStream_t stream);
 int bhtsne_distil_loss_backward(const float *dloss, const void *logits, int64_t stride, int64_t n, int64_t v,
                                 const int32_t *idx, int64_t idx_stride, const void *teacher, int64_t teacher_stride,
                                 int64_t k, const float *lse, double temperature, int type, int teacher_type,
                                 void *dlogits, int64_t dlogits_stride, hipStream_t stream);
+int bhtsne_distil_loss_backward_kept(const float *dloss, const void *logits, int64_t stride, int64_t n, int64_t v,
+                                     const int32_t *idx, int64_t idx_stride, const void *teacher,
+                                     int64_t teacher_stride, int64_t k, const float *lse, const float *kept,
+                                     double temperature, int type, int teacher_type, void *dlogits,
+                                     int64_t dlogits_stride, hipStream_t stream);
 
 #ifdef __cplusplus
 }

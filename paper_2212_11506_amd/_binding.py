@@ -143,8 +143,12 @@ def load_library():
         "bhtsne_distil_loss_workspace_size": (C.c_size_t, [i64, i64]),
         "bhtsne_distil_loss": (C.c_int, [vp, i64, i64, i64, vp, i64, vp, i64, i64, C.c_double, C.c_int, C.c_int, vp, vp, vp,
                                          C.c_size_t, vp]),
+        "bhtsne_distil_loss_kept": (C.c_int, [vp, i64, i64, i64, vp, i64, vp, i64, i64, C.c_double, C.c_int, C.c_int, vp, vp, vp,
+                                              vp, C.c_size_t, vp]),
         "bhtsne_distil_loss_backward": (C.c_int, [vp, vp, i64, i64, i64, vp, i64, vp, i64, i64, vp, C.c_double, C.c_int,
                                                   C.c_int, vp, i64, vp]),
+        "bhtsne_distil_loss_backward_kept": (C.c_int, [vp, vp, i64, i64, i64, vp, i64, vp, i64, i64, vp, vp, C.c_double, C.c_int,
+                                                       C.c_int, vp, i64, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -1184,34 +1188,39 @@ def distil_loss_workspace_size(n: int, v: int) -> int:
 
 
 def distil_loss(logits: torch.Tensor, idx: torch.Tensor, teacher: torch.Tensor, temperature: float = 1.0,
-                workspace: Optional[torch.Tensor] = None):
+                workspace: Optional[torch.Tensor] = None, keep: bool = False):
     """bhtsne_distil_loss: (loss, lse), n values each, of logits (n x v) against the teacher's logits (n x k) of the classes
-    idx (n x k int32; outside [0, v): absent).
+    idx (n x k int32; outside [0, v): absent); with keep (loss, lse, kept), kept (n x 2) being what lse is rounded from, for the
+    backward pass of rows with a large lse.
 
-    loss's gradient goes to the logits through bhtsne_distil_loss_backward (once); lse has none, and the teacher neither:
-    one whose graph torch records is refused.  For a captured backward pass see gated_layer."""
+    loss's gradient goes to the logits through bhtsne_distil_loss_backward_kept (once); lse and kept have none, and the teacher
+    neither: one whose graph torch records is refused.  For a captured backward pass see gated_layer."""
     _no_gradient(teacher, "the teacher of distil_loss")
     if logits.requires_grad and torch.is_grad_enabled():
-        return _DistilLoss.apply(logits, idx, teacher, float(temperature), workspace)
-    return _distil_loss(logits, idx, teacher, temperature, workspace)
+        loss, lse, kept = _DistilLoss.apply(logits, idx, teacher, float(temperature), workspace)
+    else:
+        loss, lse, kept = _distil_loss(logits, idx, teacher, temperature, workspace, keep)
+    return (loss, lse, kept) if keep else (loss, lse)
 
 
-def _distil_loss(logits, idx, teacher, temperature, workspace=None):
+def _distil_loss(logits, idx, teacher, temperature, workspace=None, keep=False):
     lib = load_library()
     args, kind, teacher_kind, gpu = _lists(logits, idx, teacher)
     n, v = logits.shape
     loss, lse = logits.new_empty(n, dtype=torch.float32), logits.new_empty(n, dtype=torch.float32)  # two: each may be changed in place
+    kept = logits.new_empty((n, 2), dtype=torch.float32) if keep else None
     if workspace is not None:
         need = _workspace_bytes(workspace, gpu)
     else:
         need = distil_loss_workspace_size(n, v)
         if need > 256:
             workspace = logits.new_empty(need, dtype=torch.uint8)
-    rc = lib.bhtsne_distil_loss(*args, temperature, kind, teacher_kind, loss.data_ptr(), lse.data_ptr(),
-                                workspace.data_ptr() if workspace is not None else None, need, _stream_of(gpu))
+    rc = lib.bhtsne_distil_loss_kept(*args, temperature, kind, teacher_kind, loss.data_ptr(), lse.data_ptr(),
+                                     kept.data_ptr() if keep else None, workspace.data_ptr() if workspace is not None else None,
+                                     need, _stream_of(gpu))
     if rc:
         _check(rc, "bhtsne_distil_loss")
-    return loss, lse
+    return loss, lse, kept
 
 
 class _DistilLoss(torch.autograd.Function):
@@ -1219,31 +1228,33 @@ class _DistilLoss(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, logits, idx, teacher, temperature, workspace):
-        loss, lse = _distil_loss(logits, idx, teacher, temperature, workspace)
-        ctx.save_for_backward(logits, idx, teacher, lse)
+        loss, lse, kept = _distil_loss(logits, idx, teacher, temperature, workspace, True)
+        ctx.save_for_backward(logits, idx, teacher, lse, kept)
         ctx.temperature = temperature
-        ctx.mark_non_differentiable(lse)
-        return loss, lse
+        ctx.mark_non_differentiable(lse, kept)
+        return loss, lse, kept
 
     @staticmethod
     @once_differentiable
-    def backward(ctx, dloss, _lse):
-        logits, idx, teacher, lse = ctx.saved_tensors
-        return distil_loss_backward(dloss.contiguous(), logits, idx, teacher, lse, ctx.temperature), None, None, None, None
+    def backward(ctx, dloss, _lse, _kept):
+        logits, idx, teacher, lse, kept = ctx.saved_tensors
+        return distil_loss_backward(dloss.contiguous(), logits, idx, teacher, lse, ctx.temperature, kept=kept), None, None, None, None
 
 
 def distil_loss_backward(dloss: torch.Tensor, logits: torch.Tensor, idx: torch.Tensor, teacher: torch.Tensor, lse: torch.Tensor,
-                         temperature: float = 1.0, dlogits: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """bhtsne_distil_loss_backward: the gradient of the logits, of their type; dlogits may be the logits.  The result has no
+                         temperature: float = 1.0, dlogits: Optional[torch.Tensor] = None,
+                         kept: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """bhtsne_distil_loss_backward: the gradient of the logits, of their type; dlogits may be the logits.  From lse as
+    distil_loss gave it, which is off by its rounding, |lse| 2^-24; with kept as well that counts no more.  The result has no
     gradient of its own."""
     lib = load_library()
     args, kind, teacher_kind, gpu = _lists(logits, idx, teacher)
     n, v = logits.shape
     stride = v if dlogits is None else _rows(dlogits, "dlogits", logits.shape, logits.dtype, gpu)
     out = dlogits if dlogits is not None else logits.new_empty((n, v))
-    rc = lib.bhtsne_distil_loss_backward(_vector(dloss, "dloss", n, gpu, torch.float32), *args,
-                                         _vector(lse, "lse", n, gpu, torch.float32), temperature, kind, teacher_kind,
-                                         out.data_ptr(), stride, _stream_of(gpu))
+    rc = lib.bhtsne_distil_loss_backward_kept(_vector(dloss, "dloss", n, gpu, torch.float32), *args,
+                                              _vector(lse, "lse", n, gpu, torch.float32), _vector(kept, "kept", 2 * n, gpu, torch.float32),
+                                              temperature, kind, teacher_kind, out.data_ptr(), stride, _stream_of(gpu))
     if rc:
         _check(rc, "bhtsne_distil_loss_backward")
     if dlogits is not None:

@@ -258,19 +258,50 @@ size_t bhtsne_distil_loss_workspace_size(int64_t n, int64_t v)
     return 256 + (parts > 1 ? (size_t(n) * size_t(parts) * sizeof(float2) + 255) / 256 * 256 : 0); // 256: none is needed
 }
 
-int bhtsne_distil_loss(const void *logits, int64_t stride, int64_t n, int64_t v, const int32_t *idx, int64_t idx_stride,
-                       const void *teacher, int64_t teacher_stride, int64_t k, double temperature, int type, int teacher_type,
-                       float *loss, float *lse, void *workspace, size_t workspace_bytes, hipStream_t stream)
+int bhtsne_distil_loss_kept(const void *logits, int64_t stride, int64_t n, int64_t v, const int32_t *idx, int64_t idx_stride,
+                            const void *teacher, int64_t teacher_stride, int64_t k, double temperature, int type, int teacher_type,
+                            float *loss, float *lse, float *kept, void *workspace, size_t workspace_bytes, hipStream_t stream)
 {
     DistilArgs a = {};
     if (!distil_inputs(&a, logits, stride, n, v, idx, idx_stride, teacher, teacher_stride, k, temperature, type, teacher_type))
         return BHTSNE_EINVAL;
-    if ((!loss && !lse && n > 0) || !aligned(loss, BHTSNE_F32) || !aligned(lse, BHTSNE_F32)) return BHTSNE_EINVAL;
+    if ((!loss && !lse && !kept && n > 0) || !aligned(loss, BHTSNE_F32) || !aligned(lse, BHTSNE_F32) || !aligned(kept, BHTSNE_F32))
+        return BHTSNE_EINVAL;
     if (a.parts > 1 && !workspace_ok(workspace, workspace_bytes, bhtsne_distil_loss_workspace_size(n, v))) return BHTSNE_EWORKSPACE;
     a.loss = loss;
     a.lse = lse;
+    a.kept = kept;
     a.part = static_cast<float2 *>(workspace);
     launch_distil_loss(a, stream);
+    return status();
+}
+
+int bhtsne_distil_loss(const void *logits, int64_t stride, int64_t n, int64_t v, const int32_t *idx, int64_t idx_stride,
+                       const void *teacher, int64_t teacher_stride, int64_t k, double temperature, int type, int teacher_type,
+                       float *loss, float *lse, void *workspace, size_t workspace_bytes, hipStream_t stream)
+{
+    if (!loss && !lse && n > 0) return BHTSNE_EINVAL;
+    return bhtsne_distil_loss_kept(logits, stride, n, v, idx, idx_stride, teacher, teacher_stride, k, temperature, type, teacher_type,
+                                   loss, lse, nullptr, workspace, workspace_bytes, stream);
+}
+
+int bhtsne_distil_loss_backward_kept(const float *dloss, const void *logits, int64_t stride, int64_t n, int64_t v, const int32_t *idx,
+                                     int64_t idx_stride, const void *teacher, int64_t teacher_stride, int64_t k, const float *lse,
+                                     const float *kept, double temperature, int type, int teacher_type, void *dlogits,
+                                     int64_t dlogits_stride, hipStream_t stream)
+{
+    DistilArgs a = {};
+    if (!distil_inputs(&a, logits, stride, n, v, idx, idx_stride, teacher, teacher_stride, k, temperature, type, teacher_type))
+        return BHTSNE_EINVAL;
+    if (((!dloss || !lse) && n > 0) || !aligned(dloss, BHTSNE_F32) || !aligned(lse, BHTSNE_F32) || !aligned(kept, BHTSNE_F32))
+        return BHTSNE_EINVAL;
+    if (!output_ok(dlogits, dlogits_stride, n, v, type)) return BHTSNE_EINVAL;
+    a.dloss = dloss;
+    a.lse_in = lse;
+    a.kept_in = kept;
+    a.out = dlogits;
+    a.out_stride = dlogits_stride;
+    launch_distil_loss_backward(a, stream);
     return status();
 }
 
@@ -279,17 +310,8 @@ int bhtsne_distil_loss_backward(const float *dloss, const void *logits, int64_t 
                                 double temperature, int type, int teacher_type, void *dlogits, int64_t dlogits_stride,
                                 hipStream_t stream)
 {
-    DistilArgs a = {};
-    if (!distil_inputs(&a, logits, stride, n, v, idx, idx_stride, teacher, teacher_stride, k, temperature, type, teacher_type))
-        return BHTSNE_EINVAL;
-    if (((!dloss || !lse) && n > 0) || !aligned(dloss, BHTSNE_F32) || !aligned(lse, BHTSNE_F32)) return BHTSNE_EINVAL;
-    if (!output_ok(dlogits, dlogits_stride, n, v, type)) return BHTSNE_EINVAL;
-    a.dloss = dloss;
-    a.lse_in = lse;
-    a.out = dlogits;
-    a.out_stride = dlogits_stride;
-    launch_distil_loss_backward(a, stream);
-    return status();
+    return bhtsne_distil_loss_backward_kept(dloss, logits, stride, n, v, idx, idx_stride, teacher, teacher_stride, k, lse, nullptr,
+                                            temperature, type, teacher_type, dlogits, dlogits_stride, stream);
 }
 
 } // extern "C"

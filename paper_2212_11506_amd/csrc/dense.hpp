@@ -11,6 +11,9 @@ constexpr int64_t kDistilMaxList = 2048;       // listed neighbours of a row: 16
 constexpr int64_t kDistilSplit = 8192;         // values of a row at least that a block takes, of rows that are shared out
 constexpr int64_t kDistilBlocks = 2048;        // blocks that fill the chip: rows are shared out below so many
 constexpr int64_t kDistilWave = 2048;          // rows up to this are a wave's, longer ones a block's
+// Backward: |lse| up to which the rounded lse is good enough, being off by 2^-21 at most, 8 units of the exponentials' own
+// roundings, which are 16 and more.  (There the gradient is the same bits with what was kept and without.)
+constexpr float kDistilNear = 16.0f;
 
 // blocks that share a row of v logits, of n rows
 inline int distil_parts(int64_t n, int64_t v)
@@ -26,6 +29,8 @@ struct DistilArgs {
     const float *dloss;  // backward
     const float *lse_in; // backward
     float *loss, *lse;   // forward, each nullable
+    float *kept;         // forward, nullable: n x 2, a row's largest logit and its sum of exponentials
+    const float *kept_in; // backward, nullable
     void *out;           // backward: n x v, may be logits
     float2 *part;        // forward: (largest logit, sum) of each part of a row
     int64_t stride, idx_stride, teacher_stride, out_stride;

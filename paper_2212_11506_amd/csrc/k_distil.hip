@@ -186,7 +186,13 @@ template <typename E, typename TE, int kThreads>
 __device__ inline void finish(const DistilArgs &a, int64_t row, float m, double s, float c, double *s_sum, float *s_max)
 {
     const double log_s = log(s);
-    if (a.lse && threadIdx.x == 0) a.lse[row] = float(double(m) / a.temperature + log_s);
+    if (threadIdx.x == 0) {
+        if (a.lse) a.lse[row] = float(double(m) / a.temperature + log_s);
+        if (a.kept) {
+            a.kept[2 * row] = m;
+            a.kept[2 * row + 1] = float(s);
+        }
+    }
     if (!a.loss) return;
     const List l = list_of<TE, kThreads>(a, row, c, s_sum, s_max);
     const E *z = static_cast<const E *>(a.logits) + row * a.stride;
@@ -274,10 +280,18 @@ __global__ __launch_bounds__(kThreads) void distil_back_kernel(DistilArgs a)
         E *out = static_cast<E *>(a.out) + row * a.out_stride;
         const List l = list_of<TE, kThreads>(a, row, c, s_sum, s_max);
         const bool empty = l.empty();
-        // q = exp2((z - top) c) factor, with lse T as a high and a low part
-        const double g = double(a.dloss[row]) / a.temperature, lse = double(a.lse_in[row]) * a.temperature;
-        const float high = float(lse), f = float(g), low = high == high && fabsf(high) < INFINITY ? float(lse - double(high)) : 0.0f;
-        const float factor = f * exp2_fast(-low * c);
+        // q = exp2((z - high) c) factor: from the row's largest logit and its sum, which lose nothing; or with lse T as a high
+        // and a low part, where lse's rounding makes q off by |lse| 2^-24
+        const float given = a.lse_in[row];
+        const double g = double(a.dloss[row]) / a.temperature, lse = double(given) * a.temperature;
+        float high = float(lse), factor;
+        if (a.kept_in && !(fabsf(given) < kDistilNear)) {
+            high = a.kept_in[2 * row];
+            factor = float(g / double(a.kept_in[2 * row + 1]));
+        } else {
+            const float low = high == high && fabsf(high) < INFINITY ? float(lse - double(high)) : 0.0f;
+            factor = float(g) * exp2_fast(-low * c);
+        }
         const int32_t *idx = a.idx + row * a.idx_stride;
         const TE *u = static_cast<const TE *>(a.teacher) + row * a.teacher_stride;
         for (int j = threadIdx.x; j < a.k; j += kThreads) {

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2212_11506_amd as bh
-from tests.test_gpu_distil import TYPES, case, check_forward, reference
+from tests.test_gpu_distil import HALF, TINY, TYPES, U, case, check_forward, reference, terms_of
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -86,3 +86,77 @@ def test_loss_of_rows_far_off(n, v, dtype):
     t = torch.softmax(u[0].double(), 0)
     loss = bh.distil_loss(z, idx, u)[0]
     assert abs(float(loss[0]) - float((t * t.log()).sum()) - math.log(v)) <= 100 * 2.0 ** -24 * math.log(v)
+
+
+def same(p, q):
+    return torch.equal(p.isnan(), q.isnan()) and torch.equal(p.nan_to_num(nan=0.0), q.nan_to_num(nan=0.0))
+
+
+def check_gradient(dloss, z, idx, u, T, got):
+    """As the list's own test has it, but against the softmax itself, not the rounded lse.  q is the quotient of an exponential
+    and the row's sum, which is off as the forward pass' is; where |lse| < 16 lse's rounding, 8 u, and its product with T's,
+    as much again, take the sum's place.  An exponential below 2^-126 is 0."""
+    dtype, v = got.dtype, z.shape[1]
+    near, at, t, x_t, lse, _ = reference(shifted(z), idx, u, T)
+    g = dloss.double().cpu()[:, None] / T
+    q = torch.exp(near - lse[:, None]) * t.sum(1, keepdim=True).round()
+    want = (g * q).scatter_add_(1, at, -g * t)
+    of_sum = U * (4 * (q * -near).nan_to_num(nan=0.0).sum(1, keepdim=True) + terms_of(v))  # x e^-x: 0 at infinity
+    share = U * (4 * x_t + 4 * (t * x_t).sum(1, keepdim=True) + 16) * t
+    tol = (g.abs() * ((q * (U * (4 * -near + 32) + of_sum)).nan_to_num(nan=0.0) + 2.0 ** -126)).scatter_add_(1, at, g.abs() * share)
+    tol = tol + HALF[dtype] * (want.abs() + tol) + TINY[dtype]
+    err = (got.double().cpu() - want).abs()
+    assert bool((err <= tol).all()), float((err / tol).max())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,v", ROWS)
+def test_gradient_of_rows_far_off(n, v, dtype):
+    """The gradient through torch's graph where lse is so large that its rounding counts."""
+    for T in (1.0, 0.05, 1e-6, 300.0):
+        for far in (True, False):
+            if far:
+                z, idx, u = far_rows(n, v, dtype, T, n + v)
+            else:  # any row of a head whose logits have drifted
+                z, idx, u = case(n, v, min(v, 7), dtype, n + v)
+                z = ((z.double() * T + torch.linspace(-1000 * T, 60_000 * min(T, 1.0), n, device=DEV)[:, None])).to(dtype)
+            dloss = T * torch.linspace(-1.0, 1.5, n, device=DEV)
+            leaf = z.clone().requires_grad_()
+            loss, lse, kept = bh.distil_loss(leaf, idx, u, T, keep=True)
+            loss.backward(dloss)
+            there = z.amax(1) > -math.inf  # rows that the type holds: others are minus infinity, and NaN by the formula
+            check_gradient(dloss[there], z[there], idx[there], u[there], T, leaf.grad[there])
+            assert bool(leaf.grad[~there].isnan().all())
+            assert not kept.requires_grad and torch.equal(kept[:, 0], z.float().amax(1))
+            # the calls by themselves, in place too
+            for p, q in zip(bh.distil_loss(z, idx, u, T, keep=True), (loss, lse, kept)):
+                assert same(p, q)
+            assert same(bh.distil_loss_backward(dloss, z, idx, u, lse, T, dlogits=z, kept=kept), leaf.grad)
+
+
+def test_kept_changes_nothing_near_zero():
+    for n, v in ROWS:
+        z, idx, u = case(n, v, 5, torch.float32, v)
+        loss, lse, kept = bh.distil_loss(z, idx, u, keep=True)
+        assert bool((lse.abs() < 16).all())
+        assert torch.equal(bh.distil_loss_backward(loss, z, idx, u, lse), bh.distil_loss_backward(loss, z, idx, u, lse, kept=kept))
+
+
+def test_kept_of_rows_that_are_not_finite():
+    for v in (40, 3000, 30_000):
+        z, idx, u = case(4, v, 5, torch.float32, v)
+        z[0], z[1, v // 2], z[2, v // 3] = -math.inf, NAN, math.inf
+        leaf = z.clone().requires_grad_()
+        loss, lse, kept = bh.distil_loss(leaf, idx, u, keep=True)
+        loss.sum().backward()
+        assert bool(loss[:3].isnan().all()) and bool(leaf.grad[:3].isnan().any(1).all()) and bool(leaf.grad[3].isfinite().all())
+        want = bh.distil_loss_backward(torch.ones(4, device=DEV), z, idx, u, lse)
+        assert torch.equal(leaf.grad[3], want[3])
+
+
+def test_kept_is_refused():
+    z, idx, u = case(4, 50, 5, torch.float32, 1)
+    loss, lse, kept = bh.distil_loss(z, idx, u, keep=True)
+    for bad in (kept[:3], kept.double(), kept.t(), kept.cpu(), lse):
+        with pytest.raises(ValueError, match="kept"):
+            bh.distil_loss_backward(loss, z, idx, u, lse, kept=bad)
