@@ -685,6 +685,8 @@ int bhtsne_linear_i8(const void *x, int64_t x_stride, int x_type, const float *x
  *            of 1e38 or of masked classes alone.  With kept, q of a row whose |lse|
  *            is 16 or more is exp((z - m) / T) / s, which is not.
  *   dlogits  n x v of `type`; may be logits (with their stride).
+ * No output else overlaps an input or another output (one that is at the same
+ * address is refused).
  * Input strides are >= the row's length, or 0 for one row that stands for all.
  * 0 <= n < 2^31, 1 <= v < 2^31, 0 <= k <= 2048, strides < 2^31, T in [1e-6, 1e6].
  * Sums over v are fp32 in a lane and joined in fp64, in an order that goes by

@@ -268,6 +268,8 @@ int bhtsne_distil_loss_kept(const void *logits, int64_t stride, int64_t n, int64
     if ((!loss && !lse && !kept && n > 0) || !aligned(loss, BHTSNE_F32) || !aligned(lse, BHTSNE_F32) || !aligned(kept, BHTSNE_F32))
         return BHTSNE_EINVAL;
     if (a.parts > 1 && !workspace_ok(workspace, workspace_bytes, bhtsne_distil_loss_workspace_size(n, v))) return BHTSNE_EWORKSPACE;
+    if (n > 0 && !apart({loss, lse, kept}, {logits, k > 0 ? idx : nullptr, k > 0 ? teacher : nullptr, a.parts > 1 ? workspace : nullptr}))
+        return BHTSNE_EINVAL;
     a.loss = loss;
     a.lse = lse;
     a.kept = kept;
@@ -296,6 +298,9 @@ int bhtsne_distil_loss_backward_kept(const float *dloss, const void *logits, int
     if (((!dloss || !lse) && n > 0) || !aligned(dloss, BHTSNE_F32) || !aligned(lse, BHTSNE_F32) || !aligned(kept, BHTSNE_F32))
         return BHTSNE_EINVAL;
     if (!output_ok(dlogits, dlogits_stride, n, v, type)) return BHTSNE_EINVAL;
+    if (n > 0 && !apart({dlogits}, {dloss, lse, kept, k > 0 ? idx : nullptr, k > 0 ? teacher : nullptr})) return BHTSNE_EINVAL;
+    // over the logits, row by row: with another stride a row would be written where another is still to be read
+    if (n > 1 && dlogits == logits && dlogits_stride != stride) return BHTSNE_EINVAL;
     a.dloss = dloss;
     a.lse_in = lse;
     a.kept_in = kept;
