@@ -815,11 +815,14 @@ class _LayerNorm(torch.autograd.Function):
         ctx.save_for_backward(x, weight, mean, rstd)
         ctx.bias_type = bias.dtype if bias is not None else None
         ctx.mark_non_differentiable(mean, rstd)
+        ctx.set_materialize_grads(False)
         return y, mean, rstd
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy, _mean, _rstd):
+        if dy is None:
+            return None, None, None, None
         x, weight, mean, rstd = ctx.saved_tensors
         n, d = x.shape
         if (d > 1 and dy.stride(1) != 1) or (n > 1 and 0 < dy.stride(0) < d):
@@ -1040,11 +1043,14 @@ class _GatedLayer(torch.autograd.Function):
         ctx.save_for_backward(x, gate, up, a, b)
         ctx.activation = activation
         ctx.mark_non_differentiable(a, b)
+        ctx.set_materialize_grads(False)  # a's and b's would be arrays of zeros, as large as they are
         return h, a, b
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dh, _a, _b):
+        if dh is None:
+            return None, None, None, None
         x, gate, up, a, b = ctx.saved_tensors
         if (dh.shape[1] > 1 and dh.stride(1) != 1) or (dh.shape[0] > 1 and 0 < dh.stride(0) < dh.shape[1]):
             dh = dh.contiguous()
@@ -1232,11 +1238,14 @@ class _DistilLoss(torch.autograd.Function):
         ctx.save_for_backward(logits, idx, teacher, lse, kept)
         ctx.temperature = temperature
         ctx.mark_non_differentiable(lse, kept)
+        ctx.set_materialize_grads(False)
         return loss, lse, kept
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dloss, _lse, _kept):
+        if dloss is None:
+            return None, None, None, None, None
         logits, idx, teacher, lse, kept = ctx.saved_tensors
         return distil_loss_backward(dloss.contiguous(), logits, idx, teacher, lse, ctx.temperature, kept=kept), None, None, None, None
 
