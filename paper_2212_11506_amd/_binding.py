@@ -694,6 +694,7 @@ class _Matrices(C.Structure):
 
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}  # BHTSNE_F32, BHTSNE_F16, BHTSNE_BF16
 _written = torch.autograd.graph.increment_version  # a graph that has saved the tensor must not use it any more
+_forward = torch.autograd.forward_ad
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
@@ -734,8 +735,15 @@ def _refuse(t: torch.Tensor, where: str, shape, dtype, gpu: int):
     raise ValueError(f"{where} must be contiguous inside a row")
 
 
+def _no_tangent(t: torch.Tensor, where: str):
+    if _forward.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{where} has a tangent, which the call would lose: it has no derivative in forward mode")
+
+
 def _rows(t: torch.Tensor, where: str, shape, dtype, gpu: int) -> int:
     """Checks a matrix with unit stride inside a row; the stride between its rows."""
+    if _forward._current_level >= 0:
+        _no_tangent(t, where)
     if not (t.get_device() == gpu and t.dtype == dtype and t.shape == shape):
         _refuse(t, where, shape, dtype, gpu)
     row, inside = t.stride()
@@ -747,6 +755,8 @@ def _rows(t: torch.Tensor, where: str, shape, dtype, gpu: int) -> int:
 def _vector(t: Optional[torch.Tensor], where: str, size: int, gpu: int, dtype=None) -> Optional[int]:
     if t is None:
         return None
+    if _forward._current_level >= 0:
+        _no_tangent(t, where)
     if t.get_device() == gpu and t.numel() == size and t.is_contiguous() and (dtype is None or t.dtype == dtype):
         return t.data_ptr()
     if t.numel() != size:
@@ -881,6 +891,8 @@ def _layer_norm_backward(dy, x, weight, mean, rstd, bias_type=None, dx=None, wor
 
 
 def _matrices(t: torch.Tensor, where: str, shape, dtype, gpu: int) -> _Matrices:
+    if _forward._current_level >= 0:
+        _no_tangent(t, where)
     if not (t.get_device() == gpu and t.dtype == dtype and t.shape == shape):
         _refuse(t, where, shape, dtype, gpu)
     stride = t.stride()
