@@ -1023,6 +1023,8 @@ def gated_layer(x: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, activatio
             raise ValueError("out has no gradient: leave it out, or call under torch.no_grad()")
         h, a, b = _GatedLayer.apply(x, gate, up, activation)
         return (h, a, b) if keep else h
+    if out is not None:
+        _no_gradient(out, "a gated_layer with out")
     h, a, b = _gated_layer(x, gate, up, activation, keep, out)
     return (h, a, b) if keep else h
 
@@ -1125,7 +1127,7 @@ def quantise_rows(x: torch.Tensor):
 
 def _no_gradient(t: torch.Tensor, where: str):
     if t.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{where} has no gradient: detach its inputs, or call under torch.no_grad()")
+        raise ValueError(f"{where} has no gradient: detach its tensors, or call under torch.no_grad()")
 
 
 @functools.lru_cache(maxsize=256)
@@ -1143,7 +1145,7 @@ def linear_i8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, x_scale: 
     lib = load_library()
     if x.dim() != 2 or w.dim() != 2:
         raise ValueError(f"x must be n x d and w f x d, got {tuple(x.shape)} and {tuple(w.shape)}")
-    for t in (x, w_scale, x_scale, bias):
+    for t in (x, w_scale, x_scale, bias, out):
         if t is not None:
             _no_gradient(t, "linear_i8")
     (n, d), f = x.shape, w.shape[0]

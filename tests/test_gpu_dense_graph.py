@@ -63,3 +63,21 @@ def test_memory_of_a_backward_pass():
     more = torch.cuda.max_memory_allocated() - before
     # rounded up to the allocator's blocks: half an array is room for them and for the gradients
     assert more <= bh.gated_layer_workspace_size(n, d, f, t) + n * f * 2 + n * f * 2 // 2
+
+
+def test_outputs_that_torch_records_are_refused():
+    """What is written over a recorded tensor is not in its graph, whose gradients would be those of the values before."""
+    x, gate, up = (mat(*s, torch.float32, k) for k, s in enumerate([(5, 24), (30, 24), (30, 24)]))
+    w, ws = bh.quantise_rows(gate)
+    calls = [lambda out: bh.gated_layer(x, gate, up, out=out), lambda out: bh.gated_layer(x, gate, up, "gelu", keep=True, out=out)[0],
+             lambda out: bh.linear_i8(x, w, ws, out=out)]
+    leaf = torch.zeros(5, 30, device=DEV).requires_grad_()
+    for call in calls:
+        for out in (leaf, leaf * 2):
+            before = out.detach().clone()
+            with pytest.raises(ValueError, match="gradient"):
+                call(out)
+            assert torch.equal(out.detach(), before)
+            with torch.no_grad():
+                assert call(out) is out
+                leaf.zero_()
