@@ -617,7 +617,8 @@ int bhtsne_gated_layer(const void *x, int64_t x_stride, const void *gate, int64_
  *   dh, a, b  n x f of `type`, x n x d; a stride of 0 as above.
  *   dx        n x d, nullable; dgate, dup  f x d, each nullable, overwritten
  *             (zero for n = 0); one output at least is wanted.
- * da and db are rounded to `type` before the products, but for small products
+ * da and db are rounded to `type` before the products (fp16: to infinity beyond
+ * 65520, whatever the products would come to), but for small products
  * of few outputs (n d or f d below 4096 and n d f below 2^27), where they stay
  * fp32; the sums over features and points are fp32, those over parts of the
  * points are joined in a fixed order: the same inputs give the same bits.  The workspace is

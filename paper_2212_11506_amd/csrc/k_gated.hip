@@ -195,8 +195,8 @@ template <typename E, typename T, bool kAny, Tail kTail = Tail::kWhole> void run
 // lane, runs of 64 bytes of a point.  A row's last piece is its last 16 bytes, of which only those count that the piece before
 // does not have: the others are masked out, in points and weights alike.
 //
-// 1.3M x 50 to 200 fp16, gelu: 240 to 269 us for 650 MB, by the card.  Bound by the vector instructions, which a CU issues in
-// 89 % of the time: some 17 an output for the activation and the product, two of them at a quarter of the rate, and 7 blocks
+// 1.3M x 50 to 200 fp16, gelu: 245 to 270 us for 650 MB, by the card.  Bound by the vector instructions, which a CU issues in
+// 92 % of the time: some 18 an output for the activation and the product, two of them at a quarter of the rate, and 7 blocks
 // of 32 features for 6.25.  Rows of 400 bytes end inside a line, so 608 MB are written for 520.  Weights in registers and the
 // points past a block's waves in step, by LDS and a barrier, took 301 us (7 waves on 4 SIMDs); without LDS, 429: each lane's
 // 16 bytes a request of its own.
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(kShortThreads) void gated_short_kernel(Product p, G
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const float a = acc[e][r], b = acc[2 + e][r];
-                        t.v[e] = E(k == 0 ? activate<E>(a, kGelu ? Act::kGelu : Act::kSilu) * b : k == 1 ? a : b);
+                        t.v[e] = rounded<E>(k == 0 ? activate<E>(a, kGelu ? Act::kGelu : Act::kSilu) * b : k == 1 ? a : b);
                     }
                     *reinterpret_cast<Bits *>(patch + (lane / 16 * 4 + r) * kPatch + lane % 16 * 2 * int(sizeof(E))) = __builtin_bit_cast(Bits, t);
                 }
