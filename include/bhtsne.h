@@ -674,8 +674,9 @@ int bhtsne_linear_i8(const void *x, int64_t x_stride, int x_type, const float *x
  *   idx      n x k int32, teacher  n x k of teacher_type (`type` or BHTSNE_F32), in
  *            any order.  An index outside [0, v) marks an entry that is absent; so
  *            does a teacher's logit of minus infinity.  A row without entries has
- *            the loss 0 and a gradient of zero; one that has a NaN the loss NaN.  A class that is listed more than
- *            once gets the sum of its shares; the loss takes each entry by itself.
+ *            the loss 0 and a gradient of zero; one that has a NaN the loss NaN.
+ *            A class that is listed more than once gets the sum of its shares; the
+ *            loss takes each entry by itself.
  *            (idx and teacher may be null for k = 0.)
  *   loss, lse  n fp32 values, each nullable, one at least (or kept) is wanted.
  *   kept     n x 2 fp32, nullable: a row's largest logit m and s = sum exp((z - m) / T),
